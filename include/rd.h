@@ -458,6 +458,100 @@ RD_API int rd_schedule_status(rd_schedule_t *s, int *device_status);
 /* rd_destroy -- frees the schedule and its device tables.  NULL is allowed. */
 RD_API void rd_destroy(rd_schedule_t *s);
 
+/* ------------------------------------------------------------------------------------------------------
+ * Operators on a vocabulary (the paper has no counterpart).  What training programs reduce over processes
+ * are sums of embeddings, softmax statistics and gradients; these operators produce them on one GPU, for a
+ * whole vocabulary or for the slice of it that a process holds, so that rd_reduce / rd_allreduce can join
+ * the slices.
+ *   - A slice holds `rows` consecutive vocabulary entries, the first of which is `first_row`.
+ *   - Matrices are row-major with a row stride in elements (>= dim; grad_out and hidden also 0: every row is the
+ *     same one); rows need only be aligned to the element.  Rows that begin and end on 16-byte boundaries are faster: see each function.
+ *   - Every call is asynchronous on cuda_stream, allocates nothing, keeps nothing, and may be recorded into a
+ *     CUDA graph.  A workspace belongs to the call until the stream has passed it; its contents need not be
+ *     kept or cleared between calls.  It is aligned to 256 bytes; too small a one is RD_ERR_TOO_SMALL.
+ *   - Results depend on the arguments alone: no sum depends on timing.
+ *   - RD_ERR_INVALID_ARG: null pointers, misaligned pointers, a stride below dim, a dim outside 1..65536, no rows, a negative
+ *     first_row, factors that are not finite, an output that overlaps an input, another output or the workspace.
+ *     RD_ERR_UNSUPPORTED: an element type that the operator does not have, or 2^31 or more rows or tokens.
+ *   - Thread safety: any calls from any threads.
+ */
+
+/*
+ * rd_embed -- embedding lookup: out[i] = scale * table[ids[i] - first_row], one fp32 multiplication rounded
+ * once; a row of zeros where the table does not hold that row (ids outside the slice, negative ids).
+ *   dtype    RD_FP32, RD_BF16 or RD_FP16: table and out.
+ *   id_type  RD_INT32 or RD_INT64.
+ * Rows of table and out that begin and end on 16-byte boundaries move as 128-bit words, others by element.
+ */
+RD_API int rd_embed(const void *d_table, size_t table_stride, size_t rows, size_t dim, rd_dtype_t dtype, const void *d_ids, rd_dtype_t id_type,
+                    size_t n, int64_t first_row, float scale, void *d_out, size_t out_stride, void *cuda_stream);
+
+/*
+ * rd_embed_grad -- the gradient of rd_embed with respect to the table:
+ *   grad_table[v] = (accumulate ? grad_table[v] : 0) + scale * sum over the i with ids[i] - first_row = v of grad_out[i].
+ * Tokens are sorted by row; sums are fp32, in ascending order of i (in runs of 64 tokens, whose sums are added in
+ * ascending order), rounded once.  Every row of the table is written; with accumulate only those that have tokens.
+ *   dtype        RD_FP32, RD_BF16 or RD_FP16: grad_out.
+ *   table_dtype  dtype, or RD_FP32.
+ * rd_embed_grad_workspace reports the bytes that the call needs.
+ */
+RD_API int rd_embed_grad_workspace(size_t rows, size_t dim, size_t n, size_t *bytes);
+RD_API int rd_embed_grad(const void *d_grad_out, size_t grad_stride, rd_dtype_t dtype, const void *d_ids, rd_dtype_t id_type, size_t n,
+                         int64_t first_row, float scale, void *d_grad_table, size_t table_stride, rd_dtype_t table_dtype, size_t rows, size_t dim,
+                         int accumulate, void *d_workspace, size_t workspace_bytes, void *cuda_stream);
+
+/* The operands of rd_vocab_loss and rd_vocab_loss_grad. */
+typedef struct {
+    const void *hidden;       /* DEVICE; n x dim                                                            */
+    size_t hidden_stride;
+    const void *weight;       /* DEVICE; rows x dim: the slice of the output matrix                         */
+    size_t weight_stride;
+    const void *labels;       /* DEVICE; n vocabulary entries; a negative one: the token counts for nothing */
+    size_t n, rows, dim;
+    int64_t first_row;
+    rd_dtype_t dtype;         /* RD_BF16 or RD_FP16: hidden and weight                                      */
+    rd_dtype_t label_type;    /* RD_INT32 or RD_INT64                                                       */
+    float scale, z_loss;
+} rd_vocab_t;
+
+/*
+ * rd_vocab_loss -- softmax cross entropy of the logits x[v] = scale * hidden . weight[v], which are never stored:
+ *   lse = log(sum over the slice's v of exp(x[v])),  target = x[label] (0 when the slice does not hold the label),
+ *   loss = lse - target + z_loss * lse^2;
+ * all three fp32, 0 for tokens whose label is negative, whatever their hidden rows hold.  Products are exact, sums
+ * fp32.  An infinite logit gives an infinite lse, a NaN one a NaN.
+ *   d_loss, d_lse, d_target   DEVICE; n values each; any may be NULL, not all.
+ * For a vocabulary in slices, join the slices' results: lse = log(sum exp(lse_i)) (rd_reduce with max, then sum),
+ * target = sum target_i; d_loss is the whole loss only when the slice is the whole vocabulary.
+ * A weight whose base or stride is not a multiple of 16 bytes is copied into the workspace by every call.
+ */
+RD_API int rd_vocab_loss_workspace(const rd_vocab_t *v, size_t *bytes);
+RD_API int rd_vocab_loss(const rd_vocab_t *v, float *d_loss, float *d_lse, float *d_target, void *d_workspace, size_t workspace_bytes, void *cuda_stream);
+
+/*
+ * rd_vocab_loss_grad -- the gradients of sum_i grad_loss[i] * loss[i]:
+ *   dx[v] = grad_loss * ((1 + 2 z_loss lse) exp(x[v] - lse) - [v = label])
+ *   grad_hidden = scale * sum over v of dx[v] weight[v],   grad_weight[v] = scale * sum over tokens of dx[v] hidden.
+ * The logits are computed once more, in pieces of the vocabulary; dx is rounded to dtype once (fp16: after a
+ * multiplication by a power of two that suits the largest grad_loss, taken off again at the end), sums are fp32, results
+ * rounded once.  Rows of grad_hidden whose label is negative are zeros.
+ *   d_lse          DEVICE; n values: the normaliser of the WHOLE vocabulary (rd_vocab_loss, joined over slices).
+ *   d_grad_loss    DEVICE; value i at d_grad_loss[i * grad_loss_stride]; stride 0: one value for all tokens.
+ *   d_grad_hidden  DEVICE, n x dim, dtype; or NULL.  For a slice: the slice's part; add the parts (rd_allreduce).
+ *   d_grad_weight  DEVICE, rows x dim, dtype; or NULL.  Not both NULL.
+ */
+RD_API int rd_vocab_loss_grad_workspace(const rd_vocab_t *v, int want_hidden, int want_weight, size_t *bytes);
+RD_API int rd_vocab_loss_grad(const rd_vocab_t *v, const float *d_lse, const float *d_grad_loss, size_t grad_loss_stride, void *d_grad_hidden,
+                              size_t grad_hidden_stride, void *d_grad_weight, size_t grad_weight_stride, void *d_workspace, size_t workspace_bytes,
+                              void *cuda_stream);
+
+/*
+ * rd_vocab_status -- waits for the current device and returns the word in which the kernels of rd_vocab_loss and
+ * rd_vocab_loss_grad note a bounded wait that they gave up (it should never happen): 0, or RD_ERR_TIMEOUT if some launch since the
+ * last query did (its results are then not valid); the word is cleared.
+ */
+RD_API int rd_vocab_status(int *device_status);
+
 /* rd_strerror -- static, never NULL. */
 RD_API const char *rd_strerror(int status);
 

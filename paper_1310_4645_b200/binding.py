@@ -31,7 +31,9 @@ EXPORTS = ("rd_schedule_create", "rd_schedule_create_segments", "rd_optimal_segm
            "rd_schedule_events", "rd_schedule_segments", "rd_schedule_program", "rd_reduce",
            "rd_schedule_upload", "rd_reduce_host", "rd_destroy", "rd_strerror", "rd_schedule_set_wait_budget",
            "rd_schedule_trace", "rd_schedule_faithful_shape", "rd_schedule_actions", "rd_reduce_faithful_static", "rd_search_segmentation", "rd_schedule_status",
-           "rd_reduce_batch", "rd_schedule_set_tree_variant", "rd_schedule_tree_shape", "rd_allreduce")
+           "rd_reduce_batch", "rd_schedule_set_tree_variant", "rd_schedule_tree_shape", "rd_allreduce",
+           "rd_embed", "rd_embed_grad", "rd_embed_grad_workspace", "rd_vocab_loss", "rd_vocab_loss_workspace", "rd_vocab_loss_grad",
+           "rd_vocab_loss_grad_workspace", "rd_vocab_status")
 
 
 class rd_model_t(C.Structure):
@@ -42,6 +44,12 @@ class rd_stats_t(C.Structure):
     _fields_ = [("kernel_ms", C.c_double), ("gbytes_per_s", C.c_double), ("makespan_ns", C.c_double),
                 ("predicted_s", C.c_double), ("bytes_moved", C.c_uint64), ("device_status", C.c_int32),
                 ("n_launches", C.c_int32)]
+
+
+class rd_vocab_t(C.Structure):
+    _fields_ = [("hidden", C.c_void_p), ("hidden_stride", C.c_size_t), ("weight", C.c_void_p), ("weight_stride", C.c_size_t),
+                ("labels", C.c_void_p), ("n", C.c_size_t), ("rows", C.c_size_t), ("dim", C.c_size_t), ("first_row", C.c_int64),
+                ("dtype", C.c_int), ("label_type", C.c_int), ("scale", C.c_float), ("z_loss", C.c_float)]
 
 
 EVENT_DTYPE = np.dtype(
@@ -93,6 +101,15 @@ def lib():
                                              C.POINTER(C.c_int64)]
         L.rd_schedule_status.argtypes = [vp, C.POINTER(i32)]
         L.rd_reduce_batch.argtypes = [sz, C.POINTER(vp), C.POINTER(vp), C.POINTER(vp), C.POINTER(sz), i32, i32, vp]
+        f32, i64 = C.c_float, C.c_int64
+        L.rd_embed.argtypes = [vp, sz, sz, sz, i32, vp, i32, sz, i64, f32, vp, sz, vp]
+        L.rd_embed_grad_workspace.argtypes = [sz, sz, sz, C.POINTER(sz)]
+        L.rd_embed_grad.argtypes = [vp, sz, i32, vp, i32, sz, i64, f32, vp, sz, i32, sz, sz, i32, vp, sz, vp]
+        L.rd_vocab_loss_workspace.argtypes = [C.POINTER(rd_vocab_t), C.POINTER(sz)]
+        L.rd_vocab_loss.argtypes = [C.POINTER(rd_vocab_t), vp, vp, vp, vp, sz, vp]
+        L.rd_vocab_loss_grad_workspace.argtypes = [C.POINTER(rd_vocab_t), i32, i32, C.POINTER(sz)]
+        L.rd_vocab_loss_grad.argtypes = [C.POINTER(rd_vocab_t), vp, vp, sz, vp, sz, vp, sz, vp, sz, vp]
+        L.rd_vocab_status.argtypes = [C.POINTER(i32)]
         L.rd_destroy.argtypes = [vp]
         L.rd_destroy.restype = None
         L.rd_strerror.argtypes = [i32]
@@ -401,3 +418,178 @@ def rd_schedule_status(h) -> int:
 
 def rd_destroy(h) -> None:
     lib().rd_destroy(h)
+
+
+# ---------------------------------------------------------------------------------------------------------------
+# Vocabulary operators
+
+
+def _matrix(t, what):
+    """A 2-D CUDA tensor whose rows are contiguous: (address, row stride in elements)."""
+    if not t.is_cuda or t.dim() != 2:
+        raise ValueError("%s must be a 2-D CUDA tensor" % what)
+    stride, inner = t.stride()
+    if inner != 1 and t.shape[1] > 1:
+        raise ValueError("the rows of %s must be contiguous" % what)
+    return t.data_ptr(), stride if t.shape[0] > 1 else t.shape[1]
+
+
+def _vector(t, what, n, device):
+    if not t.is_cuda or t.device != device or t.dim() != 1 or t.shape[0] != n or not t.is_contiguous():
+        raise ValueError("%s must be a contiguous CUDA vector with one value per token, on the operands' device" % what)
+    return t.data_ptr()
+
+
+class _On:
+    """Makes a tensor's device current for a call, and gives the stream and, there, temporary memory."""
+
+    def __init__(self, device, stream):
+        import torch
+        self.device = device
+        self.stream = stream if stream is not None else torch.cuda.current_stream(device)
+        self.other = stream is not None and stream != torch.cuda.current_stream(device)
+
+    def __enter__(self):
+        import torch
+        self.prev = torch.cuda.current_device()
+        if self.prev != self.device.index:
+            torch.cuda.set_device(self.device)
+        return self
+
+    def __exit__(self, *exc):
+        import torch
+        if self.prev != self.device.index:
+            torch.cuda.set_device(self.prev)
+
+    def empty(self, shape, dtype):
+        """Memory of the call's stream: the allocator may hand it out again once that stream has passed the call."""
+        import torch
+        if self.other:
+            with torch.cuda.stream(self.stream):
+                return torch.empty(shape, dtype=dtype, device=self.device)
+        return torch.empty(shape, dtype=dtype, device=self.device)
+
+    def workspace(self, given, need):
+        import torch
+        if given is None:
+            return self.empty(need, torch.uint8)
+        if not given.is_cuda or given.device != self.device or not given.is_contiguous():
+            raise ValueError("workspace must be a contiguous CUDA tensor on the operands' device")
+        return given
+
+
+def rd_embed(table, ids, out=None, first_row=0, scale=1.0, stream=None):
+    """scale * table[ids - first_row], rows of zeros where the table does not hold an id.  table: [rows, dim] float32,
+    bfloat16 or float16; ids: int32 or int64 vector; out: [n, dim] of table's dtype (allocated when None).  Returns out."""
+    addr, stride = _matrix(table, "table")
+    n, (rows, dim) = ids.numel(), table.shape
+    ids_addr = _vector(ids, "ids", n, table.device)
+    with _On(table.device, stream) as on:
+        if out is None:
+            out = on.empty((n, dim), table.dtype)
+        out_addr, out_stride = _matrix(out, "out")
+        if out.shape != (n, dim) or out.dtype != table.dtype or out.device != table.device:
+            raise ValueError("out must be [n, dim] with table's dtype and device")
+        _check(lib().rd_embed(addr, stride, rows, dim, _dtype_code(table), ids_addr, _dtype_code(ids), n, first_row, scale,
+                              out_addr, out_stride, on.stream.cuda_stream), "rd_embed")
+    return out
+
+
+def rd_embed_grad_workspace(rows, dim, n) -> int:
+    need = C.c_size_t()
+    _check(lib().rd_embed_grad_workspace(rows, dim, n, C.byref(need)), "rd_embed_grad_workspace")
+    return need.value
+
+
+def rd_embed_grad(grad_out, ids, grad_table, first_row=0, scale=1.0, accumulate=False, workspace=None, stream=None):
+    """grad_table[v] (+)= scale * sum of grad_out[i] over the tokens with ids[i] - first_row = v.  grad_out: [n, dim]; grad_table:
+    [rows, dim] of grad_out's dtype or float32; workspace: rd_embed_grad_workspace bytes (allocated when None).  Returns grad_table."""
+    addr, stride = _matrix(grad_out, "grad_out")
+    taddr, tstride = _matrix(grad_table, "grad_table")
+    (n, dim), rows = grad_out.shape, grad_table.shape[0]
+    ids_addr = _vector(ids, "ids", n, grad_out.device)
+    if grad_table.shape[1] != dim or grad_table.device != grad_out.device:
+        raise ValueError("grad_table must be [rows, dim] on grad_out's device")
+    with _On(grad_out.device, stream) as on:
+        ws = on.workspace(workspace, rd_embed_grad_workspace(rows, dim, n))
+        _check(lib().rd_embed_grad(addr, stride, _dtype_code(grad_out), ids_addr, _dtype_code(ids), n, first_row, scale, taddr, tstride,
+                                   _dtype_code(grad_table), rows, dim, int(accumulate), ws.data_ptr(), ws.numel() * ws.element_size(),
+                                   on.stream.cuda_stream), "rd_embed_grad")
+    return grad_table
+
+
+def _vocab(hidden, weight, labels, first_row, scale, z_loss):
+    addr, stride = _matrix(hidden, "hidden")
+    waddr, wstride = _matrix(weight, "weight")
+    (n, dim), rows = hidden.shape, weight.shape[0]
+    if weight.shape[1] != dim or weight.dtype != hidden.dtype or weight.device != hidden.device:
+        raise ValueError("weight must be [rows, dim] with hidden's dtype and device")
+    return rd_vocab_t(addr, stride, waddr, wstride, _vector(labels, "labels", n, hidden.device), n, rows, dim, first_row,
+                      _dtype_code(hidden), _dtype_code(labels), scale, z_loss)
+
+
+def rd_vocab_loss_workspace(hidden, weight, labels) -> int:
+    need = C.c_size_t()
+    _check(lib().rd_vocab_loss_workspace(C.byref(_vocab(hidden, weight, labels, 0, 1.0, 0.0)), C.byref(need)), "rd_vocab_loss_workspace")
+    return need.value
+
+
+def rd_vocab_loss(hidden, weight, labels, first_row=0, scale=1.0, z_loss=0.0, workspace=None, stream=None):
+    """Softmax cross entropy of the logits scale * hidden @ weight.T: (loss, lse, target), float32 vectors with one value per token,
+    0 where the label is negative.  hidden: [n, dim], weight: [rows, dim], both bfloat16 or float16; labels: int32 or int64."""
+    import torch
+    v = _vocab(hidden, weight, labels, first_row, scale, z_loss)
+    with _On(hidden.device, stream) as on:
+        out = on.empty((3, v.n), torch.float32)
+        need = C.c_size_t()
+        _check(lib().rd_vocab_loss_workspace(C.byref(v), C.byref(need)), "rd_vocab_loss")
+        ws = on.workspace(workspace, need.value)
+        at = out.data_ptr()
+        _check(lib().rd_vocab_loss(C.byref(v), at, at + 4 * v.n, at + 8 * v.n, ws.data_ptr(), ws.numel() * ws.element_size(),
+                                   on.stream.cuda_stream), "rd_vocab_loss")
+    return out[0], out[1], out[2]
+
+
+def rd_vocab_loss_grad_workspace(hidden, weight, labels, want_hidden=True, want_weight=True) -> int:
+    need = C.c_size_t()
+    _check(lib().rd_vocab_loss_grad_workspace(C.byref(_vocab(hidden, weight, labels, 0, 1.0, 0.0)), int(want_hidden), int(want_weight),
+                                              C.byref(need)), "rd_vocab_loss_grad_workspace")
+    return need.value
+
+
+def rd_vocab_loss_grad(hidden, weight, labels, lse, grad_loss, grad_hidden=None, grad_weight=None, first_row=0, scale=1.0, z_loss=0.0,
+                       workspace=None, stream=None):
+    """Gradients of sum(grad_loss * loss) into grad_hidden [n, dim] and grad_weight [rows, dim] (one may be None: not computed).
+    lse: rd_vocab_loss's, joined over the slices of the vocabulary; grad_loss: float32 vector, may be a broadcast one, or a scalar
+    tensor.  Returns (grad_hidden, grad_weight)."""
+    import torch
+    v = _vocab(hidden, weight, labels, first_row, scale, z_loss)
+    lse_addr = _vector(lse, "lse", v.n, hidden.device)
+    if grad_loss.dim() == 0:
+        grad_loss = grad_loss.expand(v.n)
+    if not grad_loss.is_cuda or grad_loss.device != hidden.device or grad_loss.shape != (v.n,) or \
+            grad_loss.dtype != torch.float32 or lse.dtype != torch.float32:
+        raise ValueError("lse and grad_loss must be float32 CUDA vectors with one value per token")
+    gh = gw = (None, 0)
+    if grad_hidden is not None:
+        gh = _matrix(grad_hidden, "grad_hidden")
+    if grad_weight is not None:
+        gw = _matrix(grad_weight, "grad_weight")
+    for g, like in ((grad_hidden, hidden), (grad_weight, weight)):
+        if g is not None and (g.shape != like.shape or g.dtype != like.dtype or g.device != like.device):
+            raise ValueError("a gradient has its operand's shape, dtype and device")
+    with _On(hidden.device, stream) as on:
+        need = C.c_size_t()
+        _check(lib().rd_vocab_loss_grad_workspace(C.byref(v), int(grad_hidden is not None), int(grad_weight is not None), C.byref(need)),
+               "rd_vocab_loss_grad")
+        ws = on.workspace(workspace, need.value)
+        _check(lib().rd_vocab_loss_grad(C.byref(v), lse_addr, grad_loss.data_ptr(), grad_loss.stride(0), *gh, *gw, ws.data_ptr(),
+                                        ws.numel() * ws.element_size(), on.stream.cuda_stream), "rd_vocab_loss_grad")
+    return grad_hidden, grad_weight
+
+
+def rd_vocab_status() -> int:
+    """Waits for the current device and returns (and clears) the status word of the loss kernels: 0 or RD_ERR_TIMEOUT."""
+    st = C.c_int(0)
+    _check(lib().rd_vocab_status(C.byref(st)), "rd_vocab_status")
+    return st.value

@@ -1,0 +1,1000 @@
+// sm_100a kernels of softmax cross entropy over a large vocabulary and of its gradient, without the logits in memory.
+//
+//   x_v  = scale * h . w_v                 for the rows w_v of the weight that the call holds
+//   lse  = log sum_v exp(x_v),  target = x_label,  loss = lse - target + z * lse^2
+//   dx_v = g * ((1 + 2 z lse) exp(x_v - lse) - [v = label]),   dh = scale * sum_v dx_v w_v,   dw_v = scale * sum_tokens dx_v h
+//
+// Tokens with a negative label count for nothing: a first kernel packs the hidden rows of the others one after another, in
+// order, so that ignored rows cost no products and nothing they hold (infinities, NaN) can reach a sum.  Everything after it
+// works on the packed rows; how many there are is known on the device only.
+//
+// Loss.  One matrix product of n x rows x dim whose epilogue keeps, per token and vocabulary tile, the running maximum and
+// the sum of exponentials instead of the logits, and picks out the label's logit; a small kernel joins the tiles.
+// Gradient.  In pieces of the vocabulary: the product once more, its epilogue turns logits into dx (16 bits, one rounding:
+// the operand type of the products that follow; fp16 dx is scaled by a power of two so that the largest factor g comes near
+// the top of the type's range), then both products of the piece in one launch, dw complete, dh added up in fp32 over the pieces.
+//
+// All three products run on one kernel: tiles of 128 x 256 accumulators in tensor memory (two of them, so that one is read
+// while the next is computed), operands brought in by TMA into a ring of shared-memory stages, one thread issuing tcgen05.mma.
+#include "rd_vocab.h"
+
+#include <cuda.h>
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+
+#include <atomic>
+
+#include "rd.h"
+
+namespace rd {
+
+namespace {
+
+constexpr int kPackThreads = 256;
+constexpr int kPackRows = 8;              // tokens per thread block of the packing kernel, one warp each
+constexpr int kCountTile = 256;           // tokens per thread block of the counting kernel
+constexpr int kRowPad = 256;              // packed rows are padded with zero rows to a multiple of this
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLn2 = 0.6931471805599453f;
+
+struct Meta {
+    uint32_t m;               // packed rows
+    float boost, unboost;     // power of two that dx is multiplied by, and its inverse
+    uint32_t pad;
+};
+struct TileCount {
+    uint32_t n;               // tokens of the tile that count
+    float most;               // largest finite |factor of dx| among them
+};
+
+__device__ int g_vocab_status;
+
+__device__ __forceinline__ long long label_of(const void *labels, bool wide, size_t i)
+{
+    return wide ? static_cast<const long long *>(labels)[i] : static_cast<const int *>(labels)[i];
+}
+
+struct PackParams {
+    const uint16_t *hidden;
+    const void *labels;
+    size_t hidden_stride, n, rows;
+    uint32_t dim, packed_stride;
+    long long first;
+    bool wide_labels, copy16;
+    float scale, z;
+    uint16_t *packed;
+    int *index, *label;       // per packed row: the token, its label's row in this weight or -1
+    const TileCount *tiles;
+    Meta *meta;
+    // loss
+    float *loss, *lse_out, *target;
+    // gradient
+    const float *lse, *grad_loss;
+    size_t grad_loss_stride;
+    float *gp, *gt, *lse2;    // per packed row: factor of the probability, of the label's one, lse * log2(e)
+    uint16_t *grad_hidden;
+    size_t grad_hidden_stride;
+    bool gradient, fp16;
+};
+
+__device__ __forceinline__ void factors(const PackParams &p, size_t i, float &gp, float &gt)
+{
+    const float g = p.grad_loss[i * p.grad_loss_stride] * p.scale;
+    gt = g;
+    gp = p.z != 0.0f ? fmaf(2.0f * p.z * p.lse[i], g, g) : g;
+}
+
+__global__ void __launch_bounds__(kCountTile) rd_vocab_count_kernel(PackParams p, TileCount *tiles)
+{
+    __shared__ float warp_most[kCountTile / 32];
+    const size_t i = size_t(blockIdx.x) * kCountTile + threadIdx.x;
+    const bool counts = i < p.n && label_of(p.labels, p.wide_labels, i) >= 0;
+    float most = 0.0f;
+    if (p.gradient && counts) {
+        float gp, gt;
+        factors(p, i, gp, gt);
+        if (isfinite(gp)) most = fabsf(gp);
+        if (isfinite(gt)) most = fmaxf(most, fabsf(gt));
+    }
+#pragma unroll
+    for (int d = 16; d; d /= 2) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, d));
+    if ((threadIdx.x & 31) == 0) warp_most[threadIdx.x >> 5] = most;
+    const int n = __syncthreads_count(counts);
+    if (threadIdx.x == 0) {
+#pragma unroll
+        for (int k = 1; k < kCountTile / 32; k++) most = fmaxf(most, warp_most[k]);
+        tiles[blockIdx.x] = TileCount{uint32_t(n), most};
+    }
+}
+
+__device__ __forceinline__ void copy_row(uint16_t *dst, const uint16_t *src, uint32_t n, uint32_t padded, bool wide, int lane)
+{
+    if (wide) {
+        const uint4 *s = reinterpret_cast<const uint4 *>(src);
+        uint4 *d = reinterpret_cast<uint4 *>(dst);
+#pragma unroll 4
+        for (uint32_t j = lane; j < n / 8; j += 32) d[j] = s[j];
+    } else {
+        for (uint32_t j = lane; j < padded; j += 32) dst[j] = j < n ? src[j] : uint16_t(0);
+    }
+}
+
+// Thread blocks below pack_blocks: kPackRows tokens each.  The others: the zero rows behind the packed ones.
+__global__ void __launch_bounds__(kPackThreads) rd_vocab_pack_kernel(PackParams p, uint32_t pack_blocks, uint32_t n_tiles)
+{
+    __shared__ uint32_t sums[2][kPackThreads / 32];
+    __shared__ float mosts[kPackThreads / 32];
+    __shared__ uint32_t mask_of_block;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const bool packs = blockIdx.x < pack_blocks;
+    const size_t base = size_t(blockIdx.x) * kPackRows;               // first token of the block
+    const uint32_t own_tile = packs ? uint32_t(base / kCountTile) : n_tiles;
+    // tokens that count: before the block's count tile, in all, and within the tile before the block
+    uint32_t before = 0, all = 0;
+    float most = 0.0f;
+    for (uint32_t t = threadIdx.x; t < n_tiles; t += kPackThreads) {
+        const TileCount c = p.tiles[t];
+        all += c.n;
+        if (t < own_tile) before += c.n;
+        most = fmaxf(most, c.most);
+    }
+    if (packs) {
+        const size_t i = size_t(own_tile) * kCountTile + threadIdx.x;
+        if (i < base && label_of(p.labels, p.wide_labels, i) >= 0) before++;
+    }
+#pragma unroll
+    for (int d = 16; d; d /= 2) {
+        before += __shfl_xor_sync(0xffffffffu, before, d);
+        all += __shfl_xor_sync(0xffffffffu, all, d);
+        most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, d));
+    }
+    if (lane == 0) {
+        sums[0][warp] = before;
+        sums[1][warp] = all;
+        mosts[warp] = most;
+    }
+    if (threadIdx.x < 32 && packs) {
+        const bool counts = lane < kPackRows && base + lane < p.n && label_of(p.labels, p.wide_labels, base + lane) >= 0;
+        const uint32_t b = __ballot_sync(0xffffffffu, counts);
+        if (lane == 0) mask_of_block = b;
+    }
+    __syncthreads();
+    before = all = 0;
+    most = 0.0f;
+#pragma unroll
+    for (int k = 0; k < kPackThreads / 32; k++) {
+        before += sums[0][k];
+        all += sums[1][k];
+        most = fmaxf(most, mosts[k]);
+    }
+    if (blockIdx.x == 0 && threadIdx.x == 0) {
+        // fp16: the largest factor goes to [2^13, 2^14): probabilities down to 2^-27 of it stay normal numbers
+        float boost = 1.0f;
+        if (p.fp16 && most > 0.0f) {
+            int e;
+            frexpf(most, &e);
+            e = 14 - e;
+            boost = ldexpf(1.0f, e > 100 ? 100 : e < -100 ? -100 : e);
+        }
+        *p.meta = Meta{all, boost, 1.0f / boost, 0};
+    }
+    if (!packs) {
+        const size_t r = size_t(all) + (blockIdx.x - pack_blocks) * kPackRows + warp;
+        if (r >= (size_t(all) + kRowPad - 1) / kRowPad * kRowPad) return;
+        for (uint32_t j = lane; j < p.packed_stride; j += 32) p.packed[r * p.packed_stride + j] = 0;
+        if (lane == 0) {
+            p.index[r] = -1;
+            p.label[r] = -1;
+            if (p.gradient) p.gp[r] = p.gt[r] = p.lse2[r] = 0.0f;
+        }
+        return;
+    }
+    const size_t i = base + warp;
+    if (i >= p.n) return;
+    const uint32_t mask = mask_of_block;
+    if (!(mask >> warp & 1)) {
+        if (p.gradient) {
+            if (p.grad_hidden)
+                for (uint32_t j = lane; j < p.dim; j += 32) p.grad_hidden[i * p.grad_hidden_stride + j] = 0;
+        } else if (lane == 0) {
+            if (p.loss) p.loss[i] = 0.0f;
+            if (p.lse_out) p.lse_out[i] = 0.0f;
+            if (p.target) p.target[i] = 0.0f;
+        }
+        return;
+    }
+    const size_t r = size_t(before) + __popc(mask & ((1u << warp) - 1));
+    copy_row(p.packed + r * p.packed_stride, p.hidden + i * p.hidden_stride, p.dim, p.packed_stride, p.copy16, lane);
+    if (lane == 0) {
+        const long long l = label_of(p.labels, p.wide_labels, i);
+        p.index[r] = int(i);
+        p.label[r] = l >= p.first && l - p.first < static_cast<long long>(p.rows) ? int(l - p.first) : -1;
+        if (p.gradient) {
+            float gp, gt;
+            factors(p, i, gp, gt);
+            p.gp[r] = gp;
+            p.gt[r] = gt;
+            p.lse2[r] = p.lse[i] * kLog2e;
+        }
+    }
+}
+
+// Copies a weight whose rows TMA cannot address (unaligned base or stride) to rows that it can.
+__global__ void __launch_bounds__(kPackThreads) rd_vocab_align_kernel(uint16_t *dst, uint32_t dst_stride, const uint16_t *src, size_t src_stride, size_t rows, uint32_t dim)
+{
+    for (size_t r = size_t(blockIdx.x) * (kPackThreads / 32) + (threadIdx.x >> 5); r < rows; r += size_t(gridDim.x) * (kPackThreads / 32))
+        copy_row(dst + r * dst_stride, src + r * src_stride, dim, dst_stride, false, threadIdx.x & 31);
+}
+
+// ------------------------------------------------------------------------------------------------ the products
+
+constexpr int kTileN = 256;
+constexpr int kTileK = 64;                // 128 bytes: one swizzle span
+constexpr int kEpilogueWarps = 8;
+constexpr int kMmaThreads = 128 + 32 * kEpilogueWarps;
+constexpr long long kWaitCycles = 4000000000ll;     // a wait gives up after about two seconds of SM clock
+constexpr long long kDrainCycles = 20000000ll;      // after that, copies in flight get ten milliseconds to land
+
+enum { kStats = 0, kDlogits = 1, kGrads = 2 };
+
+struct alignas(64) MmaParams {
+    CUtensorMap a_k;          // rows of the left operand, 64 x 128 boxes: packed hidden (stats, dlogits), dx (dh)
+    CUtensorMap b_k;          // rows of the weight, 64 x 256 boxes (stats, dlogits)
+    CUtensorMap a_mn;         // dx as the transposed left operand of dw, 64 x 64 boxes
+    CUtensorMap b_mn;         // weight as the transposed right operand of dh
+    CUtensorMap b2_mn;        // packed hidden as the transposed right operand of dw
+    const Meta *meta;
+    const int *label;
+    const float *gp, *gt, *lse2;
+    float2 *part;             // stats: (maximum, sum) in base 2, [half tile][packed row]
+    float *target;            // stats: the label's logit, per packed row
+    uint16_t *dx;             // dlogits: packed rows x dx_stride
+    float *dh;                // grads: [split][packed row][dh_stride]
+    uint16_t *dw;
+    size_t part_stride, dx_stride, dh_stride, dh_rows, dw_stride;
+    uint32_t rows;            // rows of the weight in all
+    uint32_t piece0, piece;   // first row of the piece and its rows
+    uint32_t dim;
+    uint32_t group;           // token tiles that go over the vocabulary together
+    uint32_t splits;          // parts that the sum over the piece is cut into for dh
+    bool first_piece, want_dh, want_dw, dw_wide;
+    float scale2;             // scale * log2(e)
+    float scale;
+};
+
+__device__ __forceinline__ uint32_t smem_addr(const void *p) { return uint32_t(__cvta_generic_to_shared(p)); }
+
+__device__ __forceinline__ void bar_init(uint32_t bar, uint32_t count)
+{
+    asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory");
+}
+__device__ __forceinline__ void bar_expect(uint32_t bar, uint32_t bytes)
+{
+    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void bar_arrive(uint32_t bar)
+{
+    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ bool bar_try(uint32_t bar, uint32_t parity)
+{
+    uint32_t ok;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+        "selp.b32 %0, 1, 0, p;\n\t}"
+        : "=r"(ok)
+        : "r"(bar), "r"(parity)
+        : "memory");
+    return ok;
+}
+__device__ __noinline__ bool bar_wait_slow(uint32_t bar, uint32_t parity)
+{
+    const long long t0 = clock64();
+    do {
+        if (bar_try(bar, parity)) return true;
+    } while (clock64() - t0 < kWaitCycles);
+    atomicExch(&g_vocab_status, 1);
+    return false;
+}
+__device__ __noinline__ void drain()
+{
+    const long long t0 = clock64();
+    while (clock64() - t0 < kDrainCycles) {}
+}
+// False when the wait gave up.
+__device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity) { return bar_try(bar, parity) || bar_wait_slow(bar, parity); }
+
+__device__ __forceinline__ void tma_load(uint32_t dst, const CUtensorMap *map, uint32_t x, uint32_t y, uint32_t bar)
+{
+    asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(dst), "l"(map), "r"(x),
+                 "r"(y), "r"(bar)
+                 : "memory");
+}
+
+// Shared-memory operand descriptor, 128-byte swizzle.  Operands with the summed index innermost: rows of 128 bytes, 8 rows
+// make a swizzle atom of 1024 bytes (the stride).  Transposed operands: 64 x 64 boxes, each line of 128 bytes holds 64 rows of
+// one summed index; 8 lines make an atom (the stride), the next 64 rows begin 8192 bytes further (the leading offset).
+__device__ __forceinline__ uint64_t operand(uint32_t addr, bool transposed)
+{
+    return uint64_t(addr >> 4) | uint64_t(transposed ? 8192 >> 4 : 1) << 16 | uint64_t(1024 >> 4) << 32 | uint64_t(1) << 46 | uint64_t(2) << 61;
+}
+
+__device__ __forceinline__ void mma(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool add)
+{
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d),
+        "l"(a), "l"(b), "r"(idesc), "r"(uint32_t(add))
+        : "memory");
+}
+__device__ __forceinline__ void mma_commit(uint32_t bar)
+{
+    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+}
+
+__device__ __forceinline__ void tmem_load32(uint32_t addr, uint32_t (&v)[32])
+{
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+        "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];\n\t"
+        "tcgen05.wait::ld.sync.aligned;"
+        : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]), "=r"(v[8]), "=r"(v[9]), "=r"(v[10]), "=r"(v[11]),
+          "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15]), "=r"(v[16]), "=r"(v[17]), "=r"(v[18]), "=r"(v[19]), "=r"(v[20]), "=r"(v[21]), "=r"(v[22]),
+          "=r"(v[23]), "=r"(v[24]), "=r"(v[25]), "=r"(v[26]), "=r"(v[27]), "=r"(v[28]), "=r"(v[29]), "=r"(v[30]), "=r"(v[31])
+        : "r"(addr)
+        : "memory");
+}
+
+__device__ __forceinline__ float exp2_fast(float x)
+{
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+
+template <bool BF16> __device__ __forceinline__ uint32_t pack2(float lo, float hi)
+{
+    uint32_t r;
+    if (BF16) asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    else asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+__device__ __forceinline__ void store32(void *p, const uint32_t (&v)[8])
+{
+    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7])
+                 : "memory");
+}
+__device__ __forceinline__ void load32(const void *p, float (&v)[8])
+{
+    asm volatile("ld.global.v8.f32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                 : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7])
+                 : "l"(p)
+                 : "memory");
+}
+
+constexpr int kTileM = 128;
+constexpr uint32_t kStageA = kTileM * kTileK * 2, kStageB = kTileN * kTileK * 2;
+constexpr int kStages = 4;
+constexpr uint32_t kMmaSmem = kStages * (kStageA + kStageB) + 1024 + 256;
+
+// One unit of work: an output tile and the range of the summed index that goes into it.
+struct Work {
+    int product;              // 0 logits, 1 dh, 2 dw
+    uint32_t m0, n0, k0, kblocks, split;
+};
+
+template <int KIND> struct Plan {
+    uint32_t tiles_m, tiles_n, group;                 // logits
+    uint32_t dh_n, dh_tiles, dh_units, k_per_split, k_piece;   // dh
+    uint32_t dw_tiles, k_tokens;                      // dw
+    uint32_t units;
+
+    __device__ __forceinline__ Plan(const MmaParams &p, uint32_t m)
+    {
+        tiles_m = (m + kTileM - 1) / kTileM;
+        group = p.group;
+        if (KIND != kGrads) {
+            tiles_n = (p.piece + kTileN - 1) / kTileN;
+            units = tiles_m * tiles_n;
+        } else {
+            dh_n = (p.dim + kTileN - 1) / kTileN;
+            k_piece = (p.piece + kTileK - 1) / kTileK;
+            k_per_split = (k_piece + p.splits - 1) / p.splits;
+            dh_tiles = tiles_m * dh_n;
+            dh_units = p.want_dh ? dh_tiles * p.splits : 0;
+            k_tokens = (m + kTileK - 1) / kTileK;
+            dw_tiles = p.want_dw ? (p.piece + kTileM - 1) / kTileM * dh_n : 0;
+            units = dh_units + dw_tiles;
+        }
+    }
+    __device__ __forceinline__ Work at(uint32_t u, const MmaParams &p) const
+    {
+        Work w;
+        if (KIND != kGrads) {
+            const uint32_t per = group * tiles_n, g = u / per, in = u - g * per;
+            const uint32_t wide = min(group, tiles_m - g * group);
+            w = Work{0, (g * group + in % wide) * kTileM, in / wide * kTileN, 0, (p.dim + kTileK - 1) / kTileK, 0};
+        } else if (u < dh_units) {
+            const uint32_t s = u / dh_tiles, t = u - s * dh_tiles;
+            const uint32_t k0 = s * k_per_split, k1 = min(k0 + k_per_split, k_piece);
+            w = Work{1, t / dh_n * kTileM, t % dh_n * kTileN, k0 * kTileK, k1 > k0 ? k1 - k0 : 0, s};
+        } else {
+            const uint32_t t = u - dh_units;
+            w = Work{2, t / dh_n * kTileM, t % dh_n * kTileN, 0, k_tokens, 0};
+        }
+        return w;
+    }
+};
+
+template <int KIND, bool BF16>
+__global__ void __launch_bounds__(kMmaThreads, 1) rd_vocab_mma_kernel(const __grid_constant__ MmaParams p)
+{
+    extern __shared__ unsigned char smem_raw[];
+    const uint32_t smem = (smem_addr(smem_raw) + 1023) & ~1023u;
+    const uint32_t bars = smem + kStages * (kStageA + kStageB);
+    // barriers: full[stage], empty[stage], accumulator full[2], empty[2]; then the tensor memory address
+    const uint32_t full = bars, empty = bars + 8 * kStages, acc_full = bars + 16 * kStages, acc_empty = acc_full + 16, tmem_slot = acc_empty + 16;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < kStages; s++) {
+            bar_init(full + 8 * s, 1);
+            bar_init(empty + 8 * s, 1);
+        }
+        for (int b = 0; b < 2; b++) {
+            bar_init(acc_full + 8 * b, 1);
+            bar_init(acc_empty + 8 * b, kEpilogueWarps);
+        }
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 2) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(tmem_slot) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    __syncthreads();
+    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+    uint32_t tmem;
+    asm volatile("ld.shared.b32 %0, [%1];" : "=r"(tmem) : "r"(tmem_slot));
+
+    const uint32_t m = p.meta->m;
+    const Plan<KIND> plan(p, m);
+    bool dead = false;
+
+    if (warp == 0) {
+        if (lane == 0) {
+            uint32_t it = 0;
+            for (uint32_t u = blockIdx.x; u < plan.units && !dead; u += gridDim.x) {
+                const Work w = plan.at(u, p);
+                for (uint32_t k = 0; k < w.kblocks; k++, it++) {
+                    const uint32_t s = it % kStages, a = smem + s * (kStageA + kStageB), b = a + kStageA, bar = full + 8 * s;
+                    if (!bar_wait(empty + 8 * s, (it / kStages & 1) ^ 1)) { dead = true; break; }
+                    bar_expect(bar, kStageA + kStageB);
+                    const uint32_t kk = w.k0 + k * kTileK;
+                    if (KIND != kGrads) {
+                        tma_load(a, &p.a_k, kk, w.m0, bar);
+                        tma_load(b, &p.b_k, kk, p.piece0 + w.n0, bar);
+                    } else if (w.product == 1) {
+                        tma_load(a, &p.a_k, kk, w.m0, bar);
+#pragma unroll
+                        for (int j = 0; j < kTileN / 64; j++) tma_load(b + j * 8192, &p.b_mn, w.n0 + 64 * j, p.piece0 + kk, bar);
+                    } else {
+#pragma unroll
+                        for (int j = 0; j < kTileM / 64; j++) tma_load(a + j * 8192, &p.a_mn, w.m0 + 64 * j, kk, bar);
+#pragma unroll
+                        for (int j = 0; j < kTileN / 64; j++) tma_load(b + j * 8192, &p.b2_mn, w.n0 + 64 * j, kk, bar);
+                    }
+                }
+            }
+            // the last stages' arrivals have to land while the barriers still exist
+            for (int s = 0; s < kStages && !dead; s++, it++) dead = !bar_wait(empty + 8 * (it % kStages), (it / kStages & 1) ^ 1);
+            if (dead) drain();
+        }
+    } else if (warp == 1) {
+        if (lane == 0) {
+            constexpr uint32_t kDesc = 1u << 4 | (BF16 ? 1u << 7 | 1u << 10 : 0u) | uint32_t(kTileN / 8) << 17 | uint32_t(kTileM / 16) << 24;
+            uint32_t it = 0, tile = 0;
+            for (uint32_t u = blockIdx.x; u < plan.units && !dead; u += gridDim.x) {
+                const Work w = plan.at(u, p);
+                if (w.kblocks == 0) continue;            // the epilogue takes zeros
+                const uint32_t buf = tile & 1;
+                if (!bar_wait(acc_empty + 8 * buf, (tile / 2 & 1) ^ 1)) { dead = true; break; }
+                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                const bool ta = w.product == 2, tb = w.product != 0;
+                const uint32_t idesc = kDesc | (ta ? 1u << 15 : 0u) | (tb ? 1u << 16 : 0u);
+                const uint32_t step_a = ta ? 2048 >> 4 : 32 >> 4, step_b = tb ? 2048 >> 4 : 32 >> 4;
+                for (uint32_t k = 0; k < w.kblocks; k++, it++) {
+                    const uint32_t s = it % kStages, a = smem + s * (kStageA + kStageB), b = a + kStageA;
+                    if (!bar_wait(full + 8 * s, it / kStages & 1)) { dead = true; break; }
+                    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                    const uint64_t da = operand(a, ta), db = operand(b, tb);
+#pragma unroll
+                    for (int j = 0; j < kTileK / 16; j++) mma(tmem + buf * kTileN, da + j * step_a, db + j * step_b, idesc, k != 0 || j != 0);
+                    mma_commit(empty + 8 * s);
+                }
+                if (!dead) mma_commit(acc_full + 8 * buf);
+                tile++;
+            }
+            if (dead) drain();
+        }
+    } else if (warp >= 4) {
+        const int quarter = warp & 3, half = (warp - 4) >> 2;        // rows 32 * quarter.., columns 128 * half.. of the tile
+        uint32_t tile = 0;
+        for (uint32_t u = blockIdx.x; u < plan.units; u += gridDim.x) {
+            const Work w = plan.at(u, p);
+            const uint32_t row = w.m0 + 32 * quarter + lane, col0 = w.n0 + 128 * half;
+            const uint32_t buf = tile & 1;
+            if (w.kblocks) {
+                if (!bar_wait(acc_full + 8 * buf, tile / 2 & 1)) break;
+                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+            }
+            const uint32_t acc = tmem + buf * kTileN + 128 * half + (uint32_t(32 * quarter) << 16);
+            // the row's numbers (stats and dlogits; rows up to the next multiple of 128 exist and hold neutral values)
+            int label = -1;
+            float lse2 = 0.0f, gp = 0.0f, gt = 0.0f, top = -INFINITY, sum = 0.0f;
+            if (KIND != kGrads) label = p.label[row] - int(p.piece0);
+            if (KIND == kDlogits) {
+                const float boost = p.meta->boost;
+                lse2 = p.lse2[row];
+                gp = p.gp[row] * boost;
+                gt = p.gt[row] * boost;
+                if (p.label[row] < 0) label = -1;
+            }
+            const float unboost = KIND == kGrads ? p.meta->unboost : 1.0f;
+#pragma unroll 1
+            for (int c = 0; c < 4; c++) {
+                const uint32_t col = col0 + 32 * c;
+                uint32_t v[32];
+                if (w.kblocks) {
+                    tmem_load32(acc + 32 * c, v);
+                } else {
+#pragma unroll
+                    for (int j = 0; j < 32; j++) v[j] = 0;
+                }
+                if (KIND == kStats) {
+                    float y[32], most = -INFINITY;
+#pragma unroll
+                    for (int j = 0; j < 32; j++) {
+                        y[j] = __uint_as_float(v[j]) * p.scale2;
+                        if (col + 32 > p.piece && col + j >= p.piece) y[j] = -INFINITY;
+                        most = fmaxf(most, y[j]);
+                    }
+                    // an infinite maximum must not meet itself in a difference: exp2(inf) and exp2(-inf) are right as they are
+                    most = fmaxf(most, top);
+                    const float ref = fabsf(most) == INFINITY ? 0.0f : most;
+                    float s = top == -INFINITY ? 0.0f : sum * exp2_fast(top - ref);
+                    if (fabsf(top) == INFINITY) s = sum;
+#pragma unroll
+                    for (int j = 0; j < 32; j++) s += exp2_fast(y[j] - ref);
+                    sum = s;
+                    top = most;
+                    if (label >= 0 && uint32_t(label) - col < 32u && row < m) {
+#pragma unroll
+                        for (int j = 0; j < 32; j++)
+                            if (uint32_t(label) == col + j) p.target[row] = __uint_as_float(v[j]) * p.scale;
+                    }
+                } else if (KIND == kDlogits) {
+                    float y[32];
+#pragma unroll
+                    for (int j = 0; j < 32; j++) {
+                        y[j] = exp2_fast(fmaf(__uint_as_float(v[j]), p.scale2, -lse2)) * gp;
+                        if (col + j == uint32_t(label)) y[j] -= gt;
+                        if (row >= m || col + j >= p.piece) y[j] = 0.0f;
+                    }
+                    uint16_t *dst = p.dx + size_t(row) * p.dx_stride + col;
+#pragma unroll
+                    for (int q = 0; q < 2; q++) {
+                        uint32_t o[8];
+#pragma unroll
+                        for (int j = 0; j < 8; j++) o[j] = pack2<BF16>(y[16 * q + 2 * j], y[16 * q + 2 * j + 1]);
+                        store32(dst + 16 * q, o);
+                    }
+                } else if (w.product == 1) {
+                    if (row < m) {
+                        float *dst = p.dh + (size_t(w.split) * p.dh_rows + row) * p.dh_stride + col;
+#pragma unroll
+                        for (int q = 0; q < 4; q++) {
+                            if (col + 8 * q >= p.dh_stride) break;
+                            uint32_t o[8];
+                            float old[8] = {};
+                            if (!p.first_piece) load32(dst + 8 * q, old);
+#pragma unroll
+                            for (int j = 0; j < 8; j++) o[j] = __float_as_uint(old[j] + __uint_as_float(v[8 * q + j]));
+                            store32(dst + 8 * q, o);
+                        }
+                    }
+                } else if (row < p.piece) {
+                    uint16_t *dst = p.dw + size_t(p.piece0 + row) * p.dw_stride + col;
+#pragma unroll
+                    for (int q = 0; q < 4; q++) {
+                        uint32_t o[4];
+#pragma unroll
+                        for (int j = 0; j < 4; j++)
+                            o[j] = pack2<BF16>(__uint_as_float(v[8 * q + 2 * j]) * unboost, __uint_as_float(v[8 * q + 2 * j + 1]) * unboost);
+                        if (p.dw_wide && col + 8 * q + 8 <= p.dim) {
+                            *reinterpret_cast<uint4 *>(dst + 8 * q) = make_uint4(o[0], o[1], o[2], o[3]);
+                        } else {
+#pragma unroll
+                            for (int j = 0; j < 8; j++)
+                                if (col + 8 * q + j < p.dim) dst[8 * q + j] = uint16_t(o[j / 2] >> (j & 1 ? 16 : 0));
+                        }
+                    }
+                }
+            }
+            if (KIND == kStats) {
+                if (row < m) p.part[size_t(col0 / 128) * p.part_stride + row] = make_float2(top, sum);
+            }
+            if (w.kblocks) {
+                asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+                __syncwarp();
+                if (lane == 0) bar_arrive(acc_empty + 8 * buf);
+                tile++;
+            }
+        }
+    }
+    __syncthreads();
+    if (warp == 2) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
+}
+
+// ------------------------------------------------------------------------------------------------ joins
+
+struct JoinParams {
+    const float2 *part;
+    const float *packed_target;
+    const int *index, *label;
+    const Meta *meta;
+    size_t part_stride;
+    uint32_t parts;
+    float z;
+    float *loss, *lse, *target;
+};
+
+// 32 packed rows per thread block; eight warps share the parts.
+__global__ void __launch_bounds__(256) rd_vocab_join_kernel(JoinParams p)
+{
+    __shared__ float2 s[8][32];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const uint32_t row = blockIdx.x * 32 + lane;
+    const bool live = row < p.meta->m;
+    float top = -INFINITY, sum = 0.0f;
+    auto add = [&](float2 x) {
+        const float most = fmaxf(top, x.x);
+        const float ref = fabsf(most) == INFINITY ? 0.0f : most;
+        // a part whose maximum is infinite has its sum relative to 0 already
+        const float a = fabsf(top) == INFINITY ? sum : sum * exp2f(top - ref);
+        const float b = fabsf(x.x) == INFINITY ? x.y : x.y * exp2f(x.x - ref);
+        sum = a + b;
+        top = most;
+    };
+    if (live)
+        for (uint32_t k = warp; k < p.parts; k += 8) add(p.part[size_t(k) * p.part_stride + row]);
+    s[warp][lane] = make_float2(top, sum);
+    __syncthreads();
+    if (warp || !live) return;
+#pragma unroll
+    for (int k = 1; k < 8; k++) add(s[k][lane]);
+    const float ref = fabsf(top) == INFINITY ? 0.0f : top;
+    const float lse = (ref + log2f(sum)) * kLn2;
+    const float target = p.label[row] >= 0 ? p.packed_target[row] : 0.0f;
+    const int i = p.index[row];
+    // without the penalty an infinite lse is an infinite loss, not 0 * inf
+    if (p.loss) p.loss[i] = p.z != 0.0f ? lse - target + p.z * lse * lse : lse - target;
+    if (p.lse) p.lse[i] = lse;
+    if (p.target) p.target[i] = target;
+}
+
+struct FinishParams {
+    const float *dh;
+    const int *index;
+    const Meta *meta;
+    size_t dh_rows, dh_stride, out_stride;
+    uint32_t dim, splits;
+    uint16_t *out;
+};
+
+// Adds the parts of dh, takes the power of two off and rounds; one packed row per thread block and turn.
+template <bool BF16> __global__ void __launch_bounds__(256) rd_vocab_finish_kernel(FinishParams p)
+{
+    const uint32_t m = p.meta->m;
+    const float unboost = p.meta->unboost;
+    for (uint32_t row = blockIdx.x; row < m; row += gridDim.x) {
+        const size_t i = size_t(p.index[row]);
+        for (uint32_t j = threadIdx.x; j < p.dim; j += 256) {
+            float sum = 0.0f;
+            for (uint32_t s = 0; s < p.splits; s++) sum += p.dh[(size_t(s) * p.dh_rows + row) * p.dh_stride + j];
+            p.out[i * p.out_stride + j] = uint16_t(pack2<BF16>(sum * unboost, 0.0f));
+        }
+    }
+}
+
+// ------------------------------------------------------------------------------------------------ host
+
+size_t round_up(size_t x, size_t to) { return (x + to - 1) / to * to; }
+
+struct Part {
+    char *base;
+    size_t at = 0;
+    explicit Part(void *p) : base(static_cast<char *>(p)) {}
+    template <typename T> T *take(size_t count)
+    {
+        T *p = reinterpret_cast<T *>(base + at);
+        at += round_up(count * sizeof(T), 1024);
+        return p;
+    }
+};
+
+// TMA wants 16-byte aligned rows.
+bool needs_align(const VocabArgs &a) { return reinterpret_cast<uintptr_t>(a.weight) % 16 != 0 || a.weight_stride * 2 % 16 != 0; }
+
+struct Layout {
+    Meta *meta;
+    TileCount *tiles;
+    int *index, *label;
+    float *gp, *gt, *lse2, *target, *dh;
+    float2 *part;
+    uint16_t *packed, *dx, *weight;
+    size_t rows_padded, packed_stride, dx_stride, piece, splits, dh_stride, bytes;
+};
+
+constexpr size_t kSms = 148;
+constexpr size_t kDxBytes = size_t(256) << 20;    // what the gradient keeps of dx at a time
+
+Layout lay_out(const VocabArgs &a, bool gradient, bool want_hidden)
+{
+    Layout l{};
+    if (a.n == 0) return l;
+    Part w(a.workspace);
+    l.rows_padded = round_up(a.n, kRowPad);
+    l.packed_stride = round_up(a.dim, 8);
+    l.meta = w.take<Meta>(1);
+    l.tiles = w.take<TileCount>((a.n + kCountTile - 1) / kCountTile);
+    l.index = w.take<int>(l.rows_padded);
+    l.label = w.take<int>(l.rows_padded);
+    l.packed = w.take<uint16_t>(l.rows_padded * l.packed_stride);
+    if (needs_align(a)) l.weight = w.take<uint16_t>(a.rows * l.packed_stride);
+    if (!gradient) {
+        l.target = w.take<float>(l.rows_padded);
+        l.part = w.take<float2>(l.rows_padded * (2 * ((a.rows + kTileN - 1) / kTileN)));
+    } else {
+        l.gp = w.take<float>(l.rows_padded);
+        l.gt = w.take<float>(l.rows_padded);
+        l.lse2 = w.take<float>(l.rows_padded);
+        const size_t most = kDxBytes / (l.rows_padded * 2) / kTileN * kTileN;
+        l.piece = round_up(a.rows, kTileN);
+        if (l.piece > most) l.piece = most < 1024 ? 1024 : most;
+        if (l.piece > round_up(a.rows, kTileN)) l.piece = round_up(a.rows, kTileN);
+        l.dx_stride = l.piece;
+        l.dx = w.take<uint16_t>(l.rows_padded * l.dx_stride);
+        l.dh_stride = l.packed_stride;
+        const size_t tiles = (a.n + kTileM - 1) / kTileM * ((a.dim + kTileN - 1) / kTileN);
+        const size_t k_blocks = l.piece / kTileK;
+        l.splits = tiles >= kSms ? 1 : (kSms + tiles - 1) / tiles;
+        if (l.splits > (k_blocks + 7) / 8) l.splits = (k_blocks + 7) / 8;
+        if (want_hidden) l.dh = w.take<float>(l.splits * a.n * l.dh_stride);
+    }
+    l.bytes = w.at;
+    return l;
+}
+
+using EncodeTiled = CUresult (*)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *, const cuuint32_t *, const cuuint32_t *,
+                                 CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+EncodeTiled encoder()
+{
+    static std::atomic<EncodeTiled> known{nullptr};
+    EncodeTiled f = known.load(std::memory_order_acquire);
+    if (!f) {
+        void *p = nullptr;
+        cudaDriverEntryPointQueryResult q;
+        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &q) != cudaSuccess || q != cudaDriverEntryPointSuccess) return nullptr;
+        f = reinterpret_cast<EncodeTiled>(p);
+        known.store(f, std::memory_order_release);
+    }
+    return f;
+}
+
+// A matrix of 16-bit values, `inner` contiguous ones per row, read in boxes of 64 values x box_rows rows.
+bool encode(CUtensorMap *map, bool bf16, const void *base, size_t inner, size_t rows, size_t stride, uint32_t box_rows)
+{
+    const EncodeTiled f = encoder();
+    if (!f) return false;
+    const cuuint64_t dims[2] = {inner, rows}, strides[1] = {stride * 2};
+    const cuuint32_t box[2] = {64, box_rows}, one[2] = {1, 1};
+    return f(map, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 2, const_cast<void *>(base), dims, strides, box, one,
+             CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+int sm_count_of(int device)
+{
+    static std::atomic<int> known[64];
+    if (device < 0 || device >= 64) return 148;
+    int n = known[device].load(std::memory_order_relaxed);
+    if (!n) {
+        if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, device) != cudaSuccess || n < 1) n = 148;
+        known[device].store(n, std::memory_order_relaxed);
+    }
+    return n;
+}
+
+template <int KIND, bool BF16> cudaError_t launch_mma(const MmaParams &p, int device, int sm_count, size_t most_units, cudaStream_t stream)
+{
+    static std::atomic<bool> ready[64];
+    if (device >= 64 || !ready[device].load(std::memory_order_acquire)) {
+        const cudaError_t e = cudaFuncSetAttribute(rd_vocab_mma_kernel<KIND, BF16>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMmaSmem);
+        if (e != cudaSuccess) return e;
+        if (device < 64) ready[device].store(true, std::memory_order_release);
+    }
+    const unsigned grid = unsigned(most_units < size_t(sm_count) ? most_units : size_t(sm_count));
+    rd_vocab_mma_kernel<KIND, BF16><<<grid, kMmaThreads, kMmaSmem, stream>>>(p);
+    return cudaGetLastError();
+}
+template <int KIND> cudaError_t launch_mma(const MmaParams &p, bool bf16, int device, int sm_count, size_t most_units, cudaStream_t stream)
+{
+    return bf16 ? launch_mma<KIND, true>(p, device, sm_count, most_units, stream) : launch_mma<KIND, false>(p, device, sm_count, most_units, stream);
+}
+
+// Counting and packing, and the weight's aligned copy where one is needed.
+cudaError_t prepare(const VocabArgs &a, const Layout &l, bool gradient, const uint16_t **weight, size_t *weight_stride)
+{
+    PackParams p{};
+    p.hidden = static_cast<const uint16_t *>(a.hidden);
+    p.labels = a.labels;
+    p.hidden_stride = a.hidden_stride;
+    p.n = a.n;
+    p.rows = a.rows;
+    p.dim = uint32_t(a.dim);
+    p.packed_stride = uint32_t(l.packed_stride);
+    p.first = a.first_row;
+    p.wide_labels = a.wide_labels;
+    p.copy16 = reinterpret_cast<uintptr_t>(a.hidden) % 16 == 0 && a.hidden_stride % 8 == 0 && a.dim % 8 == 0;
+    p.scale = a.scale;
+    p.z = a.z_loss;
+    p.packed = l.packed;
+    p.index = l.index;
+    p.label = l.label;
+    p.tiles = l.tiles;
+    p.meta = l.meta;
+    p.loss = a.loss;
+    p.lse_out = a.lse_out;
+    p.target = a.target;
+    p.lse = a.lse;
+    p.grad_loss = a.grad_loss;
+    p.grad_loss_stride = a.grad_loss_stride;
+    p.gp = l.gp;
+    p.gt = l.gt;
+    p.lse2 = l.lse2;
+    p.grad_hidden = static_cast<uint16_t *>(a.grad_hidden);
+    p.grad_hidden_stride = a.grad_hidden_stride;
+    p.gradient = gradient;
+    p.fp16 = !a.bf16;
+    const unsigned tiles = unsigned((a.n + kCountTile - 1) / kCountTile), blocks = unsigned((a.n + kPackRows - 1) / kPackRows);
+    rd_vocab_count_kernel<<<tiles, kCountTile, 0, a.stream>>>(p, l.tiles);
+    rd_vocab_pack_kernel<<<blocks + kRowPad / kPackRows, kPackThreads, 0, a.stream>>>(p, blocks, tiles);
+    *weight = static_cast<const uint16_t *>(a.weight);
+    *weight_stride = a.weight_stride;
+    if (l.weight) {
+        rd_vocab_align_kernel<<<1184, kPackThreads, 0, a.stream>>>(l.weight, uint32_t(l.packed_stride), *weight, a.weight_stride, a.rows, uint32_t(a.dim));
+        *weight = l.weight;
+        *weight_stride = l.packed_stride;
+    }
+    return cudaGetLastError();
+}
+
+// Token tiles that go over the vocabulary together: their hidden rows (tile x dim) should stay in L2 beside the weight's.
+uint32_t token_group(size_t dim)
+{
+    const size_t g = (size_t(32) << 20) / (kTileM * dim * 2);
+    return uint32_t(g < 1 ? 1 : g > 64 ? 64 : g);
+}
+
+void common(MmaParams &q, const VocabArgs &a, const Layout &l)
+{
+    q.meta = l.meta;
+    q.label = l.label;
+    q.rows = uint32_t(a.rows);
+    q.dim = uint32_t(a.dim);
+    q.group = token_group(a.dim);
+    q.scale = a.scale;
+    q.scale2 = a.scale * kLog2e;
+}
+
+}  // namespace
+
+size_t vocab_loss_workspace(const VocabArgs &a) { return lay_out(a, false, false).bytes; }
+
+cudaError_t vocab_loss(const VocabArgs &a)
+{
+    int device = 0;
+    cudaError_t e = cudaGetDevice(&device);
+    if (e != cudaSuccess) return e;
+    const int sms = sm_count_of(device);
+    const Layout l = lay_out(a, false, false);
+    const uint16_t *weight;
+    size_t weight_stride;
+    e = prepare(a, l, false, &weight, &weight_stride);
+    if (e != cudaSuccess) return e;
+    MmaParams q{};
+    common(q, a, l);
+    if (!encode(&q.a_k, a.bf16, l.packed, a.dim, l.rows_padded, l.packed_stride, kTileM) || !encode(&q.b_k, a.bf16, weight, a.dim, a.rows, weight_stride, kTileN))
+        return cudaErrorInvalidValue;
+    q.part = l.part;
+    q.part_stride = l.rows_padded;
+    q.target = l.target;
+    q.piece0 = 0;
+    q.piece = uint32_t(a.rows);
+    const size_t units = (a.n + kTileM - 1) / kTileM * ((a.rows + kTileN - 1) / kTileN);
+    e = launch_mma<kStats>(q, a.bf16, device, sms, units, a.stream);
+    if (e != cudaSuccess) return e;
+    const JoinParams j{l.part, l.target, l.index, l.label, l.meta, l.rows_padded, uint32_t(2 * ((a.rows + kTileN - 1) / kTileN)), a.z_loss, a.loss, a.lse_out, a.target};
+    rd_vocab_join_kernel<<<unsigned((a.n + 31) / 32), 256, 0, a.stream>>>(j);
+    return cudaGetLastError();
+}
+
+size_t vocab_loss_grad_workspace(const VocabArgs &a, bool want_hidden) { return lay_out(a, true, want_hidden).bytes; }
+
+cudaError_t vocab_loss_grad(const VocabArgs &a)
+{
+    int device = 0;
+    cudaError_t e = cudaGetDevice(&device);
+    if (e != cudaSuccess) return e;
+    const int sms = sm_count_of(device);
+    const Layout l = lay_out(a, true, a.grad_hidden != nullptr);
+    const uint16_t *weight;
+    size_t weight_stride;
+    e = prepare(a, l, true, &weight, &weight_stride);
+    if (e != cudaSuccess) return e;
+    MmaParams logits{}, grads{};
+    common(logits, a, l);
+    common(grads, a, l);
+    logits.gp = l.gp;
+    logits.gt = l.gt;
+    logits.lse2 = l.lse2;
+    logits.dx = l.dx;
+    logits.dx_stride = l.dx_stride;
+    grads.dh = l.dh;
+    grads.dh_rows = a.n;
+    grads.dh_stride = l.dh_stride;
+    grads.splits = uint32_t(l.splits);
+    grads.dw = static_cast<uint16_t *>(a.grad_weight);
+    grads.dw_stride = a.grad_weight_stride;
+    grads.dw_wide = reinterpret_cast<uintptr_t>(a.grad_weight) % 16 == 0 && a.grad_weight_stride % 8 == 0;
+    grads.want_dh = a.grad_hidden != nullptr;
+    grads.want_dw = a.grad_weight != nullptr;
+    if (!encode(&logits.a_k, a.bf16, l.packed, a.dim, l.rows_padded, l.packed_stride, kTileM) || !encode(&logits.b_k, a.bf16, weight, a.dim, a.rows, weight_stride, kTileN) ||
+        !encode(&grads.a_k, a.bf16, l.dx, l.dx_stride, l.rows_padded, l.dx_stride, kTileM) || !encode(&grads.a_mn, a.bf16, l.dx, l.dx_stride, l.rows_padded, l.dx_stride, 64) ||
+        !encode(&grads.b_mn, a.bf16, weight, a.dim, a.rows, weight_stride, 64) || !encode(&grads.b2_mn, a.bf16, l.packed, a.dim, l.rows_padded, l.packed_stride, 64))
+        return cudaErrorInvalidValue;
+    const size_t tiles_m = (a.n + kTileM - 1) / kTileM, tiles_d = (a.dim + kTileN - 1) / kTileN;
+    for (size_t v = 0; v < a.rows; v += l.piece) {
+        const size_t piece = a.rows - v < l.piece ? a.rows - v : l.piece;
+        logits.piece0 = grads.piece0 = uint32_t(v);
+        logits.piece = grads.piece = uint32_t(piece);
+        grads.first_piece = v == 0;
+        e = launch_mma<kDlogits>(logits, a.bf16, device, sms, tiles_m * ((piece + kTileN - 1) / kTileN), a.stream);
+        if (e != cudaSuccess) return e;
+        const size_t units = (grads.want_dh ? tiles_m * tiles_d * l.splits : 0) + (grads.want_dw ? (piece + kTileM - 1) / kTileM * tiles_d : 0);
+        e = launch_mma<kGrads>(grads, a.bf16, device, sms, units, a.stream);
+        if (e != cudaSuccess) return e;
+    }
+    if (a.grad_hidden) {
+        const FinishParams f{l.dh, l.index, l.meta, a.n, l.dh_stride, a.grad_hidden_stride, uint32_t(a.dim), uint32_t(l.splits), static_cast<uint16_t *>(a.grad_hidden)};
+        const unsigned grid = unsigned(a.n < 1184 ? a.n : 1184);
+        if (a.bf16) rd_vocab_finish_kernel<true><<<grid, 256, 0, a.stream>>>(f);
+        else rd_vocab_finish_kernel<false><<<grid, 256, 0, a.stream>>>(f);
+    }
+    return cudaGetLastError();
+}
+
+cudaError_t vocab_status(int *status)
+{
+    cudaError_t e = cudaDeviceSynchronize();
+    if (e != cudaSuccess) return e;
+    e = cudaMemcpyFromSymbol(status, g_vocab_status, sizeof(int));
+    if (e != cudaSuccess) return e;
+    const int zero = 0;
+    return *status ? cudaMemcpyToSymbol(g_vocab_status, &zero, sizeof(int)) : cudaSuccess;
+}
+
+}  // namespace rd
