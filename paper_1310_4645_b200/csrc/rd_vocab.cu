@@ -272,9 +272,18 @@ __device__ __forceinline__ void bar_expect(uint32_t bar, uint32_t bytes)
 {
     asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
 }
-__device__ __forceinline__ void bar_arrive(uint32_t bar)
+// The same barrier in the first thread block of the pair.
+template <int CG> __device__ __forceinline__ uint32_t leader_bar(uint32_t bar)
 {
-    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
+    if (CG == 1) return bar;
+    uint32_t r;
+    asm("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(r) : "r"(bar));
+    return r;
+}
+template <int CG> __device__ __forceinline__ void bar_arrive_leader(uint32_t bar)
+{
+    if (CG == 1) asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
+    else asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(leader_bar<CG>(bar)) : "memory");
 }
 __device__ __forceinline__ bool bar_try(uint32_t bar, uint32_t parity)
 {
@@ -305,9 +314,13 @@ __device__ __noinline__ void drain()
 // False when the wait gave up.
 __device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity) { return bar_try(bar, parity) || bar_wait_slow(bar, parity); }
 
-__device__ __forceinline__ void tma_load(uint32_t dst, const CUtensorMap *map, uint32_t x, uint32_t y, uint32_t bar)
+template <int CG> __device__ __forceinline__ void tma_load(uint32_t dst, const CUtensorMap *map, uint32_t x, uint32_t y, uint32_t bar)
 {
-    asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(dst), "l"(map), "r"(x),
+    if (CG == 2)
+        asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.cta_group::2 [%0], [%1, {%2, %3}], [%4];" ::"r"(dst), "l"(map),
+                     "r"(x), "r"(y), "r"(bar)
+                     : "memory");
+    else asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(dst), "l"(map), "r"(x),
                  "r"(y), "r"(bar)
                  : "memory");
 }
@@ -320,18 +333,28 @@ __device__ __forceinline__ uint64_t operand(uint32_t addr, bool transposed)
     return uint64_t(addr >> 4) | uint64_t(transposed ? 8192 >> 4 : 1) << 16 | uint64_t(1024 >> 4) << 32 | uint64_t(1) << 46 | uint64_t(2) << 61;
 }
 
-__device__ __forceinline__ void mma(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool add)
+template <int CG> __device__ __forceinline__ void mma(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool add)
 {
-    asm volatile(
+    if (CG == 2)
+        asm volatile(
+            "{\n\t.reg .pred p;\n\t"
+            "setp.ne.b32 p, %4, 0;\n\t"
+            "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d),
+            "l"(a), "l"(b), "r"(idesc), "r"(uint32_t(add))
+            : "memory");
+    else asm volatile(
         "{\n\t.reg .pred p;\n\t"
         "setp.ne.b32 p, %4, 0;\n\t"
         "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d),
         "l"(a), "l"(b), "r"(idesc), "r"(uint32_t(add))
         : "memory");
 }
-__device__ __forceinline__ void mma_commit(uint32_t bar)
+// Arrives, once the products issued so far are done, at the barrier of every thread block that took part.
+template <int CG> __device__ __forceinline__ void mma_commit(uint32_t bar)
 {
-    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+    if (CG == 2)
+        asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(bar), "h"(uint16_t(3)) : "memory");
+    else asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
 }
 
 __device__ __forceinline__ void tmem_load32(uint32_t addr, uint32_t (&v)[32])
@@ -374,10 +397,15 @@ __device__ __forceinline__ void load32(const void *p, float (&v)[8])
                  : "memory");
 }
 
-constexpr int kTileM = 128;
-constexpr uint32_t kStageA = kTileM * kTileK * 2, kStageB = kTileN * kTileK * 2;
-constexpr int kStages = 4;
-constexpr uint32_t kMmaSmem = kStages * (kStageA + kStageB) + 1024 + 256;
+// CG thread blocks (one, or a pair) compute a tile of 128 * CG x 256 together: each has 128 rows of the left operand and of the
+// accumulators, and 256 / CG rows of the right operand.
+constexpr int kRowsM = 128;
+template <int CG> struct Shape {
+    static constexpr int tile_m = kRowsM * CG, rows_n = kTileN / CG;
+    static constexpr uint32_t stage_a = kRowsM * kTileK * 2, stage_b = rows_n * kTileK * 2, stage = stage_a + stage_b;
+    static constexpr int stages = CG == 2 ? 6 : 4;
+    static constexpr uint32_t smem = stages * stage + 1024 + 256;
+};
 
 // One unit of work: an output tile and the range of the summed index that goes into it.
 struct Work {
@@ -385,7 +413,8 @@ struct Work {
     uint32_t m0, n0, k0, kblocks, split;
 };
 
-template <int KIND> struct Plan {
+template <int KIND, int CG> struct Plan {
+    static constexpr uint32_t kTileM = Shape<CG>::tile_m;
     uint32_t tiles_m, tiles_n, group;                 // logits
     uint32_t dh_n, dh_tiles, dh_units, k_per_split, k_piece;   // dh
     uint32_t dw_tiles, k_tokens;                      // dw
@@ -428,15 +457,27 @@ template <int KIND> struct Plan {
     }
 };
 
-template <int KIND, bool BF16>
+template <int CG> __device__ __forceinline__ void pair_sync()
+{
+    __syncthreads();
+    if (CG == 2) {
+        asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+        asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+    }
+}
+
+template <int KIND, bool BF16, int CG>
 __global__ void __launch_bounds__(kMmaThreads, 1) rd_vocab_mma_kernel(const __grid_constant__ MmaParams p)
 {
+    using S = Shape<CG>;
+    constexpr int kStages = S::stages;
     extern __shared__ unsigned char smem_raw[];
     const uint32_t smem = (smem_addr(smem_raw) + 1023) & ~1023u;
-    const uint32_t bars = smem + kStages * (kStageA + kStageB);
+    const uint32_t bars = smem + kStages * S::stage;
     // barriers: full[stage], empty[stage], accumulator full[2], empty[2]; then the tensor memory address
     const uint32_t full = bars, empty = bars + 8 * kStages, acc_full = bars + 16 * kStages, acc_empty = acc_full + 16, tmem_slot = acc_empty + 16;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t rank = CG == 2 ? blockIdx.x & 1 : 0, first_unit = blockIdx.x / CG, unit_step = gridDim.x / CG;
 
     if (threadIdx.x == 0) {
         for (int s = 0; s < kStages; s++) {
@@ -445,46 +486,53 @@ __global__ void __launch_bounds__(kMmaThreads, 1) rd_vocab_mma_kernel(const __gr
         }
         for (int b = 0; b < 2; b++) {
             bar_init(acc_full + 8 * b, 1);
-            bar_init(acc_empty + 8 * b, kEpilogueWarps);
+            bar_init(acc_empty + 8 * b, kEpilogueWarps * CG);
         }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == 2) {
-        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(tmem_slot) : "memory");
-        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+        if (CG == 2) {
+            asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(tmem_slot) : "memory");
+            asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+        } else {
+            asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(tmem_slot) : "memory");
+            asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+        }
     }
     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-    __syncthreads();
+    pair_sync<CG>();
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
     uint32_t tmem;
     asm volatile("ld.shared.b32 %0, [%1];" : "=r"(tmem) : "r"(tmem_slot));
 
     const uint32_t m = p.meta->m;
-    const Plan<KIND> plan(p, m);
+    const Plan<KIND, CG> plan(p, m);
     bool dead = false;
 
     if (warp == 0) {
         if (lane == 0) {
             uint32_t it = 0;
-            for (uint32_t u = blockIdx.x; u < plan.units && !dead; u += gridDim.x) {
+            for (uint32_t u = first_unit; u < plan.units && !dead; u += unit_step) {
                 const Work w = plan.at(u, p);
                 for (uint32_t k = 0; k < w.kblocks; k++, it++) {
-                    const uint32_t s = it % kStages, a = smem + s * (kStageA + kStageB), b = a + kStageA, bar = full + 8 * s;
+                    const uint32_t s = it % kStages, a = smem + s * S::stage, b = a + S::stage_a, bar = leader_bar<CG>(full + 8 * s);
                     if (!bar_wait(empty + 8 * s, (it / kStages & 1) ^ 1)) { dead = true; break; }
-                    bar_expect(bar, kStageA + kStageB);
-                    const uint32_t kk = w.k0 + k * kTileK;
-                    if (KIND != kGrads) {
-                        tma_load(a, &p.a_k, kk, w.m0, bar);
-                        tma_load(b, &p.b_k, kk, p.piece0 + w.n0, bar);
-                    } else if (w.product == 1) {
-                        tma_load(a, &p.a_k, kk, w.m0, bar);
+                    // both thread blocks' copies count at the first one's barrier
+                    if (rank == 0) bar_expect(full + 8 * s, CG * S::stage);
+                    const uint32_t kk = w.k0 + k * kTileK, m0 = w.m0 + rank * kRowsM, n0 = w.n0 + rank * S::rows_n;
+                    if (w.product == 2) {
 #pragma unroll
-                        for (int j = 0; j < kTileN / 64; j++) tma_load(b + j * 8192, &p.b_mn, w.n0 + 64 * j, p.piece0 + kk, bar);
+                        for (int j = 0; j < kRowsM / 64; j++) tma_load<CG>(a + j * 8192, &p.a_mn, m0 + 64 * j, kk, bar);
                     } else {
+                        tma_load<CG>(a, &p.a_k, kk, m0, bar);
+                    }
+                    if (KIND != kGrads) {
+                        tma_load<CG>(b, &p.b_k, kk, p.piece0 + n0, bar);
+                    } else {
+                        const CUtensorMap *map = w.product == 1 ? &p.b_mn : &p.b2_mn;
+                        const uint32_t y = w.product == 1 ? p.piece0 + kk : kk;
 #pragma unroll
-                        for (int j = 0; j < kTileM / 64; j++) tma_load(a + j * 8192, &p.a_mn, w.m0 + 64 * j, kk, bar);
-#pragma unroll
-                        for (int j = 0; j < kTileN / 64; j++) tma_load(b + j * 8192, &p.b2_mn, w.n0 + 64 * j, kk, bar);
+                        for (int j = 0; j < S::rows_n / 64; j++) tma_load<CG>(b + j * 8192, map, n0 + 64 * j, y, bar);
                     }
                 }
             }
@@ -493,10 +541,10 @@ __global__ void __launch_bounds__(kMmaThreads, 1) rd_vocab_mma_kernel(const __gr
             if (dead) drain();
         }
     } else if (warp == 1) {
-        if (lane == 0) {
-            constexpr uint32_t kDesc = 1u << 4 | (BF16 ? 1u << 7 | 1u << 10 : 0u) | uint32_t(kTileN / 8) << 17 | uint32_t(kTileM / 16) << 24;
+        if (lane == 0 && rank == 0) {
+            constexpr uint32_t kDesc = 1u << 4 | (BF16 ? 1u << 7 | 1u << 10 : 0u) | uint32_t(kTileN / 8) << 17 | uint32_t(S::tile_m / 16) << 24;
             uint32_t it = 0, tile = 0;
-            for (uint32_t u = blockIdx.x; u < plan.units && !dead; u += gridDim.x) {
+            for (uint32_t u = first_unit; u < plan.units && !dead; u += unit_step) {
                 const Work w = plan.at(u, p);
                 if (w.kblocks == 0) continue;            // the epilogue takes zeros
                 const uint32_t buf = tile & 1;
@@ -506,15 +554,15 @@ __global__ void __launch_bounds__(kMmaThreads, 1) rd_vocab_mma_kernel(const __gr
                 const uint32_t idesc = kDesc | (ta ? 1u << 15 : 0u) | (tb ? 1u << 16 : 0u);
                 const uint32_t step_a = ta ? 2048 >> 4 : 32 >> 4, step_b = tb ? 2048 >> 4 : 32 >> 4;
                 for (uint32_t k = 0; k < w.kblocks; k++, it++) {
-                    const uint32_t s = it % kStages, a = smem + s * (kStageA + kStageB), b = a + kStageA;
+                    const uint32_t s = it % kStages, a = smem + s * S::stage, b = a + S::stage_a;
                     if (!bar_wait(full + 8 * s, it / kStages & 1)) { dead = true; break; }
                     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                     const uint64_t da = operand(a, ta), db = operand(b, tb);
 #pragma unroll
-                    for (int j = 0; j < kTileK / 16; j++) mma(tmem + buf * kTileN, da + j * step_a, db + j * step_b, idesc, k != 0 || j != 0);
-                    mma_commit(empty + 8 * s);
+                    for (int j = 0; j < kTileK / 16; j++) mma<CG>(tmem + buf * kTileN, da + j * step_a, db + j * step_b, idesc, k != 0 || j != 0);
+                    mma_commit<CG>(empty + 8 * s);
                 }
-                if (!dead) mma_commit(acc_full + 8 * buf);
+                if (!dead) mma_commit<CG>(acc_full + 8 * buf);
                 tile++;
             }
             if (dead) drain();
@@ -522,9 +570,9 @@ __global__ void __launch_bounds__(kMmaThreads, 1) rd_vocab_mma_kernel(const __gr
     } else if (warp >= 4) {
         const int quarter = warp & 3, half = (warp - 4) >> 2;        // rows 32 * quarter.., columns 128 * half.. of the tile
         uint32_t tile = 0;
-        for (uint32_t u = blockIdx.x; u < plan.units; u += gridDim.x) {
+        for (uint32_t u = first_unit; u < plan.units; u += unit_step) {
             const Work w = plan.at(u, p);
-            const uint32_t row = w.m0 + 32 * quarter + lane, col0 = w.n0 + 128 * half;
+            const uint32_t row = w.m0 + rank * kRowsM + 32 * quarter + lane, col0 = w.n0 + 128 * half;
             const uint32_t buf = tile & 1;
             if (w.kblocks) {
                 if (!bar_wait(acc_full + 8 * buf, tile / 2 & 1)) break;
@@ -629,13 +677,17 @@ __global__ void __launch_bounds__(kMmaThreads, 1) rd_vocab_mma_kernel(const __gr
             if (w.kblocks) {
                 asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
                 __syncwarp();
-                if (lane == 0) bar_arrive(acc_empty + 8 * buf);
+                if (lane == 0) bar_arrive_leader<CG>(acc_empty + 8 * buf);
                 tile++;
             }
         }
     }
-    __syncthreads();
-    if (warp == 2) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
+    __syncwarp();
+    pair_sync<CG>();                             // neither block of a pair leaves while the other may still signal it
+    if (warp == 2) {
+        if (CG == 2) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
+        else asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
+    }
 }
 
 // ------------------------------------------------------------------------------------------------ joins
@@ -728,6 +780,9 @@ struct Part {
 // TMA wants 16-byte aligned rows.
 bool needs_align(const VocabArgs &a) { return reinterpret_cast<uintptr_t>(a.weight) % 16 != 0 || a.weight_stride * 2 % 16 != 0; }
 
+// Whether pairs of thread blocks compute tiles of 256 x 256: as soon as there is more than one tile of 128 tokens.
+int pair_or_single(size_t n) { return n > kRowsM ? 2 : 1; }
+
 struct Layout {
     Meta *meta;
     TileCount *tiles;
@@ -768,9 +823,10 @@ Layout lay_out(const VocabArgs &a, bool gradient, bool want_hidden)
         l.dx_stride = l.piece;
         l.dx = w.take<uint16_t>(l.rows_padded * l.dx_stride);
         l.dh_stride = l.packed_stride;
-        const size_t tiles = (a.n + kTileM - 1) / kTileM * ((a.dim + kTileN - 1) / kTileN);
+        const size_t tile_m = size_t(kRowsM) * pair_or_single(a.n), tiles = (a.n + tile_m - 1) / tile_m * ((a.dim + kTileN - 1) / kTileN);
         const size_t k_blocks = l.piece / kTileK;
-        l.splits = tiles >= kSms ? 1 : (kSms + tiles - 1) / tiles;
+        const size_t groups = kSms * kRowsM / tile_m;
+        l.splits = tiles >= groups ? 1 : (groups + tiles - 1) / tiles;
         if (l.splits > (k_blocks + 7) / 8) l.splits = (k_blocks + 7) / 8;
         if (want_hidden) l.dh = w.take<float>(l.splits * a.n * l.dh_stride);
     }
@@ -818,21 +874,33 @@ int sm_count_of(int device)
     return n;
 }
 
-template <int KIND, bool BF16> cudaError_t launch_mma(const MmaParams &p, int device, int sm_count, size_t most_units, cudaStream_t stream)
+template <int KIND, bool BF16, int CG> cudaError_t launch_mma(const MmaParams &p, int device, size_t most_units, cudaStream_t stream)
 {
+    constexpr uint32_t smem = Shape<CG>::smem;
     static std::atomic<bool> ready[64];
     if (device >= 64 || !ready[device].load(std::memory_order_acquire)) {
-        const cudaError_t e = cudaFuncSetAttribute(rd_vocab_mma_kernel<KIND, BF16>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMmaSmem);
+        const cudaError_t e = cudaFuncSetAttribute(rd_vocab_mma_kernel<KIND, BF16, CG>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
         if (e != cudaSuccess) return e;
         if (device < 64) ready[device].store(true, std::memory_order_release);
     }
-    const unsigned grid = unsigned(most_units < size_t(sm_count) ? most_units : size_t(sm_count));
-    rd_vocab_mma_kernel<KIND, BF16><<<grid, kMmaThreads, kMmaSmem, stream>>>(p);
-    return cudaGetLastError();
+    const size_t groups = size_t(sm_count_of(device)) / CG;
+    cudaLaunchConfig_t c{};
+    c.gridDim = dim3(unsigned((most_units < groups ? most_units : groups) * CG));
+    c.blockDim = dim3(kMmaThreads);
+    c.dynamicSmemBytes = smem;
+    c.stream = stream;
+    cudaLaunchAttribute cluster;
+    cluster.id = cudaLaunchAttributeClusterDimension;
+    cluster.val.clusterDim.x = CG;
+    cluster.val.clusterDim.y = cluster.val.clusterDim.z = 1;
+    c.attrs = &cluster;
+    c.numAttrs = 1;
+    return cudaLaunchKernelEx(&c, rd_vocab_mma_kernel<KIND, BF16, CG>, p);
 }
-template <int KIND> cudaError_t launch_mma(const MmaParams &p, bool bf16, int device, int sm_count, size_t most_units, cudaStream_t stream)
+template <int KIND> cudaError_t launch_mma(const MmaParams &p, bool bf16, int cg, int device, size_t most_units, cudaStream_t stream)
 {
-    return bf16 ? launch_mma<KIND, true>(p, device, sm_count, most_units, stream) : launch_mma<KIND, false>(p, device, sm_count, most_units, stream);
+    if (cg == 2) return bf16 ? launch_mma<KIND, true, 2>(p, device, most_units, stream) : launch_mma<KIND, false, 2>(p, device, most_units, stream);
+    return bf16 ? launch_mma<KIND, true, 1>(p, device, most_units, stream) : launch_mma<KIND, false, 1>(p, device, most_units, stream);
 }
 
 // Counting and packing, and the weight's aligned copy where one is needed.
@@ -883,19 +951,19 @@ cudaError_t prepare(const VocabArgs &a, const Layout &l, bool gradient, const ui
 }
 
 // Token tiles that go over the vocabulary together: their hidden rows (tile x dim) should stay in L2 beside the weight's.
-uint32_t token_group(size_t dim)
+uint32_t token_group(size_t dim, size_t tile_m)
 {
-    const size_t g = (size_t(32) << 20) / (kTileM * dim * 2);
+    const size_t g = (size_t(32) << 20) / (tile_m * dim * 2);
     return uint32_t(g < 1 ? 1 : g > 64 ? 64 : g);
 }
 
-void common(MmaParams &q, const VocabArgs &a, const Layout &l)
+void common(MmaParams &q, const VocabArgs &a, const Layout &l, int cg)
 {
     q.meta = l.meta;
     q.label = l.label;
     q.rows = uint32_t(a.rows);
     q.dim = uint32_t(a.dim);
-    q.group = token_group(a.dim);
+    q.group = token_group(a.dim, size_t(kRowsM) * cg);
     q.scale = a.scale;
     q.scale2 = a.scale * kLog2e;
 }
@@ -909,23 +977,24 @@ cudaError_t vocab_loss(const VocabArgs &a)
     int device = 0;
     cudaError_t e = cudaGetDevice(&device);
     if (e != cudaSuccess) return e;
-    const int sms = sm_count_of(device);
+    const int cg = pair_or_single(a.n);
+    const size_t tile_m = size_t(kRowsM) * cg;
     const Layout l = lay_out(a, false, false);
     const uint16_t *weight;
     size_t weight_stride;
     e = prepare(a, l, false, &weight, &weight_stride);
     if (e != cudaSuccess) return e;
     MmaParams q{};
-    common(q, a, l);
-    if (!encode(&q.a_k, a.bf16, l.packed, a.dim, l.rows_padded, l.packed_stride, kTileM) || !encode(&q.b_k, a.bf16, weight, a.dim, a.rows, weight_stride, kTileN))
+    common(q, a, l, cg);
+    if (!encode(&q.a_k, a.bf16, l.packed, a.dim, l.rows_padded, l.packed_stride, kRowsM) || !encode(&q.b_k, a.bf16, weight, a.dim, a.rows, weight_stride, kTileN / cg))
         return cudaErrorInvalidValue;
     q.part = l.part;
     q.part_stride = l.rows_padded;
     q.target = l.target;
     q.piece0 = 0;
     q.piece = uint32_t(a.rows);
-    const size_t units = (a.n + kTileM - 1) / kTileM * ((a.rows + kTileN - 1) / kTileN);
-    e = launch_mma<kStats>(q, a.bf16, device, sms, units, a.stream);
+    const size_t units = (a.n + tile_m - 1) / tile_m * ((a.rows + kTileN - 1) / kTileN);
+    e = launch_mma<kStats>(q, a.bf16, cg, device, units, a.stream);
     if (e != cudaSuccess) return e;
     const JoinParams j{l.part, l.target, l.index, l.label, l.meta, l.rows_padded, uint32_t(2 * ((a.rows + kTileN - 1) / kTileN)), a.z_loss, a.loss, a.lse_out, a.target};
     rd_vocab_join_kernel<<<unsigned((a.n + 31) / 32), 256, 0, a.stream>>>(j);
@@ -939,15 +1008,16 @@ cudaError_t vocab_loss_grad(const VocabArgs &a)
     int device = 0;
     cudaError_t e = cudaGetDevice(&device);
     if (e != cudaSuccess) return e;
-    const int sms = sm_count_of(device);
+    const int cg = pair_or_single(a.n);
+    const size_t tile_m = size_t(kRowsM) * cg;
     const Layout l = lay_out(a, true, a.grad_hidden != nullptr);
     const uint16_t *weight;
     size_t weight_stride;
     e = prepare(a, l, true, &weight, &weight_stride);
     if (e != cudaSuccess) return e;
     MmaParams logits{}, grads{};
-    common(logits, a, l);
-    common(grads, a, l);
+    common(logits, a, l, cg);
+    common(grads, a, l, cg);
     logits.gp = l.gp;
     logits.gt = l.gt;
     logits.lse2 = l.lse2;
@@ -962,20 +1032,20 @@ cudaError_t vocab_loss_grad(const VocabArgs &a)
     grads.dw_wide = reinterpret_cast<uintptr_t>(a.grad_weight) % 16 == 0 && a.grad_weight_stride % 8 == 0;
     grads.want_dh = a.grad_hidden != nullptr;
     grads.want_dw = a.grad_weight != nullptr;
-    if (!encode(&logits.a_k, a.bf16, l.packed, a.dim, l.rows_padded, l.packed_stride, kTileM) || !encode(&logits.b_k, a.bf16, weight, a.dim, a.rows, weight_stride, kTileN) ||
-        !encode(&grads.a_k, a.bf16, l.dx, l.dx_stride, l.rows_padded, l.dx_stride, kTileM) || !encode(&grads.a_mn, a.bf16, l.dx, l.dx_stride, l.rows_padded, l.dx_stride, 64) ||
+    if (!encode(&logits.a_k, a.bf16, l.packed, a.dim, l.rows_padded, l.packed_stride, kRowsM) || !encode(&logits.b_k, a.bf16, weight, a.dim, a.rows, weight_stride, kTileN / cg) ||
+        !encode(&grads.a_k, a.bf16, l.dx, l.dx_stride, l.rows_padded, l.dx_stride, kRowsM) || !encode(&grads.a_mn, a.bf16, l.dx, l.dx_stride, l.rows_padded, l.dx_stride, 64) ||
         !encode(&grads.b_mn, a.bf16, weight, a.dim, a.rows, weight_stride, 64) || !encode(&grads.b2_mn, a.bf16, l.packed, a.dim, l.rows_padded, l.packed_stride, 64))
         return cudaErrorInvalidValue;
-    const size_t tiles_m = (a.n + kTileM - 1) / kTileM, tiles_d = (a.dim + kTileN - 1) / kTileN;
+    const size_t tiles_m = (a.n + tile_m - 1) / tile_m, tiles_d = (a.dim + kTileN - 1) / kTileN;
     for (size_t v = 0; v < a.rows; v += l.piece) {
         const size_t piece = a.rows - v < l.piece ? a.rows - v : l.piece;
         logits.piece0 = grads.piece0 = uint32_t(v);
         logits.piece = grads.piece = uint32_t(piece);
         grads.first_piece = v == 0;
-        e = launch_mma<kDlogits>(logits, a.bf16, device, sms, tiles_m * ((piece + kTileN - 1) / kTileN), a.stream);
+        e = launch_mma<kDlogits>(logits, a.bf16, cg, device, tiles_m * ((piece + kTileN - 1) / kTileN), a.stream);
         if (e != cudaSuccess) return e;
-        const size_t units = (grads.want_dh ? tiles_m * tiles_d * l.splits : 0) + (grads.want_dw ? (piece + kTileM - 1) / kTileM * tiles_d : 0);
-        e = launch_mma<kGrads>(grads, a.bf16, device, sms, units, a.stream);
+        const size_t units = (grads.want_dh ? tiles_m * tiles_d * l.splits : 0) + (grads.want_dw ? (piece + tile_m - 1) / tile_m * tiles_d : 0);
+        e = launch_mma<kGrads>(grads, a.bf16, cg, device, units, a.stream);
         if (e != cudaSuccess) return e;
     }
     if (a.grad_hidden) {
