@@ -511,7 +511,7 @@ typedef struct {
     int64_t first_row;
     rd_dtype_t dtype;         /* RD_BF16 or RD_FP16: hidden and weight                                      */
     rd_dtype_t label_type;    /* RD_INT32 or RD_INT64                                                       */
-    float scale, z_loss;
+    float scale, z_loss;      /* scale: not 0                                                               */
 } rd_vocab_t;
 
 /*

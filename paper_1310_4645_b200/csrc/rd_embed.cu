@@ -22,6 +22,7 @@
 #include <cuda_fp16.h>
 
 #include "rd.h"
+#include "rd_launch.h"
 
 namespace rd {
 
@@ -61,6 +62,7 @@ __global__ void __launch_bounds__(kThreads) rd_embed_kernel(const T *__restrict_
                                                             bool wide, long long first, uint32_t vecs, size_t total, float scale,
                                                             T *__restrict__ out, size_t out_stride)
 {
+    pdl_start();
     const size_t base = size_t(blockIdx.x) * (kThreads * kGatherUnroll);
     const size_t row0 = base / vecs;
     const uint32_t off0 = uint32_t(base - row0 * vecs);
@@ -100,9 +102,8 @@ template <typename T, int V> cudaError_t launch_embed(const EmbedArgs &a)
     const size_t per = size_t(kThreads) * kGatherUnroll;
     const size_t blocks = (total + per - 1) / per;
     if (blocks > 0x7fffffffu) return cudaErrorInvalidConfiguration;
-    rd_embed_kernel<T, V><<<unsigned(blocks), kThreads, 0, a.stream>>>(static_cast<const T *>(a.table), a.table_stride, a.rows, a.ids, a.wide_ids,
-                                                                      a.first_row, vecs, total, a.scale, static_cast<T *>(a.out), a.out_stride);
-    return cudaGetLastError();
+    return launch(rd_embed_kernel<T, V>, unsigned(blocks), kThreads, a.stream, static_cast<const T *>(a.table), a.table_stride, a.rows, a.ids, a.wide_ids, a.first_row,
+                  vecs, total, a.scale, static_cast<T *>(a.out), a.out_stride);
 }
 
 bool vector_rows(const void *p, size_t stride, size_t dim, size_t esize)
@@ -164,6 +165,7 @@ GradWork layout(void *workspace, size_t rows, size_t dim, size_t n)
 __global__ void __launch_bounds__(kThreads) rd_embed_count_kernel(const void *__restrict__ ids, bool wide, long long first, size_t rows, uint32_t n,
                                                                   uint32_t *__restrict__ cnt, uint32_t *__restrict__ rank)
 {
+    pdl_start();
     const uint32_t i = blockIdx.x * kThreads + threadIdx.x;
     const long long r = i < n ? row_of(ids, wide, i, first, rows) : -1;
     // lanes with the same row count together: one atomic each
@@ -180,6 +182,7 @@ __global__ void __launch_bounds__(kThreads) rd_embed_count_kernel(const void *__
 __global__ void __launch_bounds__(1024) rd_embed_ranges_kernel(const uint32_t *__restrict__ cnt, uint32_t *__restrict__ start, size_t rows, GradMeta *meta,
                                                                uint32_t *__restrict__ long_row, uint32_t *__restrict__ long_chunk, uint32_t *__restrict__ chunk_row)
 {
+    pdl_start();
     __shared__ uint32_t warp_sum[32];
     __shared__ uint32_t block_base;
     const size_t v = size_t(blockIdx.x) * 1024 + threadIdx.x;
@@ -219,6 +222,7 @@ __global__ void __launch_bounds__(1024) rd_embed_ranges_kernel(const uint32_t *_
 __global__ void __launch_bounds__(kThreads) rd_embed_place_kernel(const void *__restrict__ ids, bool wide, long long first, size_t rows, uint32_t n,
                                                                   const uint32_t *__restrict__ start, const uint32_t *__restrict__ rank, uint32_t *__restrict__ arrived)
 {
+    pdl_start();
     const uint32_t i = blockIdx.x * kThreads + threadIdx.x;
     if (i >= n) return;
     const long long r = row_of(ids, wide, i, first, rows);
@@ -233,6 +237,7 @@ __global__ void __launch_bounds__(kThreads) rd_embed_sort_kernel(const void *__r
                                                                  const uint32_t *__restrict__ arrived, uint32_t *__restrict__ list, const GradMeta *meta,
                                                                  const uint32_t *__restrict__ long_row, uint32_t token_blocks)
 {
+    pdl_start();
     __shared__ uint32_t bits[kBitmapWords];
     __shared__ uint32_t warp_sum[kThreads / 32];
     if (blockIdx.x < token_blocks) {
@@ -329,6 +334,7 @@ template <typename T, typename O, int V>
 __global__ void __launch_bounds__(kThreads) rd_embed_sum_kernel(const T *__restrict__ grad, size_t grad_stride, O *__restrict__ table, size_t table_stride, size_t rows,
                                                                 uint32_t vecs, uint32_t lanes, float scale, bool accumulate, GradWork w, uint32_t row_blocks)
 {
+    pdl_start();
     const uint32_t per_block = kThreads / lanes, lane = threadIdx.x % lanes, group = threadIdx.x / lanes;
     if (blockIdx.x < row_blocks) {
         const size_t v = size_t(blockIdx.x) * per_block + group;
@@ -361,6 +367,7 @@ __global__ void __launch_bounds__(kThreads) rd_embed_sum_kernel(const T *__restr
 template <typename O>
 __global__ void __launch_bounds__(kThreads) rd_embed_join_kernel(O *__restrict__ table, size_t table_stride, uint32_t dim, float scale, bool accumulate, GradWork w)
 {
+    pdl_start();
     const uint32_t n_long = w.meta->n_long;
     const size_t stride = (size_t(dim) + 3) / 4 * 4;
     const uint32_t slabs = (dim + kThreads - 1) / kThreads;
@@ -392,11 +399,15 @@ template <typename T, typename O, int V> cudaError_t launch_grad(const EmbedGrad
     const unsigned token_blocks = (n + kThreads - 1) / kThreads;
     const unsigned long_blocks = unsigned(max_long(n) < 296 ? max_long(n) : 296);
     if (n) {
-        rd_embed_count_kernel<<<token_blocks, kThreads, 0, a.stream>>>(a.ids, a.wide_ids, a.first_row, a.rows, n, w.cnt, w.rank);
-        rd_embed_ranges_kernel<<<unsigned((a.rows + 1023) / 1024), 1024, 0, a.stream>>>(w.cnt, w.start, a.rows, w.meta, w.long_row, w.long_chunk, w.chunk_row);
-        rd_embed_place_kernel<<<token_blocks, kThreads, 0, a.stream>>>(a.ids, a.wide_ids, a.first_row, a.rows, n, w.start, w.rank, w.arrived);
-        rd_embed_sort_kernel<<<token_blocks + long_blocks, kThreads, 0, a.stream>>>(a.ids, a.wide_ids, a.first_row, a.rows, n, w.cnt, w.start, w.arrived, w.list,
-                                                                                     w.meta, w.long_row, token_blocks);
+        e = launch(rd_embed_count_kernel, token_blocks, kThreads, a.stream, a.ids, a.wide_ids, a.first_row, a.rows, n, w.cnt, w.rank);
+        if (e != cudaSuccess) return e;
+        e = launch(rd_embed_ranges_kernel, unsigned((a.rows + 1023) / 1024), 1024, a.stream, w.cnt, w.start, a.rows, w.meta, w.long_row, w.long_chunk, w.chunk_row);
+        if (e != cudaSuccess) return e;
+        e = launch(rd_embed_place_kernel, token_blocks, kThreads, a.stream, a.ids, a.wide_ids, a.first_row, a.rows, n, w.start, w.rank, w.arrived);
+        if (e != cudaSuccess) return e;
+        e = launch(rd_embed_sort_kernel, token_blocks + long_blocks, kThreads, a.stream, a.ids, a.wide_ids, a.first_row, a.rows, n, w.cnt, w.start, w.arrived, w.list,
+                   w.meta, w.long_row, token_blocks);
+        if (e != cudaSuccess) return e;
     }
     const uint32_t vecs = uint32_t(a.dim / V);
     uint32_t lanes = 8;
@@ -405,10 +416,10 @@ template <typename T, typename O, int V> cudaError_t launch_grad(const EmbedGrad
     const size_t chunk_blocks = (max_chunks(n) + kThreads / lanes - 1) / (kThreads / lanes);
     const unsigned extra = unsigned(chunk_blocks < 1184 ? chunk_blocks : 1184);
     if (row_blocks + extra > 0x7fffffffu) return cudaErrorInvalidConfiguration;
-    rd_embed_sum_kernel<T, O, V><<<unsigned(row_blocks) + extra, kThreads, 0, a.stream>>>(static_cast<const T *>(a.grad), a.grad_stride, static_cast<O *>(a.table),
-                                                                                        a.table_stride, a.rows, vecs, lanes, a.scale, a.accumulate, w, uint32_t(row_blocks));
-    if (long_blocks) rd_embed_join_kernel<O><<<592, kThreads, 0, a.stream>>>(static_cast<O *>(a.table), a.table_stride, uint32_t(a.dim), a.scale, a.accumulate, w);
-    return cudaGetLastError();
+    e = launch(rd_embed_sum_kernel<T, O, V>, unsigned(row_blocks) + extra, kThreads, a.stream, static_cast<const T *>(a.grad), a.grad_stride, static_cast<O *>(a.table),
+               a.table_stride, a.rows, vecs, lanes, a.scale, a.accumulate, w, uint32_t(row_blocks));
+    if (e != cudaSuccess || !long_blocks) return e;
+    return launch(rd_embed_join_kernel<O>, 592, kThreads, a.stream, static_cast<O *>(a.table), a.table_stride, uint32_t(a.dim), a.scale, a.accumulate, w);
 }
 
 template <typename T, typename O, int V> cudaError_t pick_grad(const EmbedGradArgs &a)

@@ -25,15 +25,17 @@
 #include <atomic>
 
 #include "rd.h"
+#include "rd_launch.h"
 
 namespace rd {
 
 namespace {
 
 constexpr int kPackThreads = 256;
-constexpr int kPackRows = 8;              // tokens per thread block of the packing kernel, one warp each
 constexpr int kCountTile = 256;           // tokens per thread block of the counting kernel
-constexpr int kRowPad = 256;              // packed rows are padded with zero rows to a multiple of this
+constexpr size_t kCountFrom = 4097;       // from this many tokens on they are counted by a kernel of their own
+constexpr int kRowPad = 256;              // room for packed rows is a multiple of this
+constexpr int kZeroPad = 64;              // gradient: zero rows up to a multiple of this, one step of a sum over tokens
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 
@@ -84,18 +86,23 @@ __device__ __forceinline__ void factors(const PackParams &p, size_t i, float &gp
     gp = p.z != 0.0f ? fmaf(2.0f * p.z * p.lse[i], g, g) : g;
 }
 
+// The largest finite factor of dx that token i brings (fp16 only: it decides the power of two).
+__device__ __forceinline__ float largest_factor(const PackParams &p, size_t i)
+{
+    float gp, gt, most = 0.0f;
+    factors(p, i, gp, gt);
+    if (isfinite(gp)) most = fabsf(gp);
+    if (isfinite(gt)) most = fmaxf(most, fabsf(gt));
+    return most;
+}
+
 __global__ void __launch_bounds__(kCountTile) rd_vocab_count_kernel(PackParams p, TileCount *tiles)
 {
     __shared__ float warp_most[kCountTile / 32];
+    pdl_start();
     const size_t i = size_t(blockIdx.x) * kCountTile + threadIdx.x;
     const bool counts = i < p.n && label_of(p.labels, p.wide_labels, i) >= 0;
-    float most = 0.0f;
-    if (p.gradient && counts) {
-        float gp, gt;
-        factors(p, i, gp, gt);
-        if (isfinite(gp)) most = fabsf(gp);
-        if (isfinite(gt)) most = fmaxf(most, fabsf(gt));
-    }
+    float most = p.gradient && p.fp16 && counts ? largest_factor(p, i) : 0.0f;
 #pragma unroll
     for (int d = 16; d; d /= 2) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, d));
     if ((threadIdx.x & 31) == 0) warp_most[threadIdx.x >> 5] = most;
@@ -107,40 +114,52 @@ __global__ void __launch_bounds__(kCountTile) rd_vocab_count_kernel(PackParams p
     }
 }
 
-__device__ __forceinline__ void copy_row(uint16_t *dst, const uint16_t *src, uint32_t n, uint32_t padded, bool wide, int lane)
+// `threads` threads copy a row; the copy's row has room for a multiple of 8 elements, and zeros there.
+__device__ __forceinline__ void copy_row(uint16_t *dst, const uint16_t *src, uint32_t n, uint32_t padded, bool wide, int t, int threads)
 {
     if (wide) {
         const uint4 *s = reinterpret_cast<const uint4 *>(src);
         uint4 *d = reinterpret_cast<uint4 *>(dst);
-#pragma unroll 4
-        for (uint32_t j = lane; j < n / 8; j += 32) d[j] = s[j];
+#pragma unroll 8
+        for (uint32_t j = t; j < n / 8; j += threads) d[j] = s[j];
     } else {
-        for (uint32_t j = lane; j < padded; j += 32) dst[j] = j < n ? src[j] : uint16_t(0);
+#pragma unroll 4
+        for (uint32_t j = t; j < padded; j += threads) dst[j] = j < n ? src[j] : uint16_t(0);
     }
 }
 
-// Thread blocks below pack_blocks: kPackRows tokens each.  The others: the zero rows behind the packed ones.
-__global__ void __launch_bounds__(kPackThreads) rd_vocab_pack_kernel(PackParams p, uint32_t pack_blocks, uint32_t n_tiles)
+// Thread blocks below pack_blocks: R tokens each, kPackThreads / R threads copy a row.  Every block finds out for itself how many
+// tokens before its own count, from the counting kernel's tiles or, where there are none (n_tiles = 0), from the labels.
+// The other blocks (gradient): the zero rows behind the packed ones.
+template <int R> __global__ void __launch_bounds__(kPackThreads) rd_vocab_pack_kernel(PackParams p, uint32_t pack_blocks, uint32_t n_tiles)
 {
-    __shared__ uint32_t sums[2][kPackThreads / 32];
-    __shared__ float mosts[kPackThreads / 32];
+    constexpr int kWarps = kPackThreads / 32, kRowThreads = kPackThreads / R;
+    __shared__ uint32_t sums[2][kWarps];
+    __shared__ float mosts[kWarps];
     __shared__ uint32_t mask_of_block;
+    pdl_start();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const bool packs = blockIdx.x < pack_blocks;
-    const size_t base = size_t(blockIdx.x) * kPackRows;               // first token of the block
-    const uint32_t own_tile = packs ? uint32_t(base / kCountTile) : n_tiles;
-    // tokens that count: before the block's count tile, in all, and within the tile before the block
-    uint32_t before = 0, all = 0;
+    const bool packs = blockIdx.x < pack_blocks, first = blockIdx.x == 0;
+    const size_t base = packs ? size_t(blockIdx.x) * R : p.n;          // first token of the block
+    uint32_t before = 0, all = 0;                                      // tokens that count, before the block and in all
     float most = 0.0f;
-    for (uint32_t t = threadIdx.x; t < n_tiles; t += kPackThreads) {
-        const TileCount c = p.tiles[t];
-        all += c.n;
-        if (t < own_tile) before += c.n;
-        most = fmaxf(most, c.most);
-    }
-    if (packs) {
+    if (n_tiles) {
+        const uint32_t own_tile = uint32_t(base / kCountTile);
+        for (uint32_t t = threadIdx.x; t < n_tiles; t += kPackThreads) {
+            const TileCount c = p.tiles[t];
+            all += c.n;
+            if (t < own_tile) before += c.n;
+            most = fmaxf(most, c.most);
+        }
         const size_t i = size_t(own_tile) * kCountTile + threadIdx.x;
-        if (i < base && label_of(p.labels, p.wide_labels, i) >= 0) before++;
+        if (i < base && i < p.n && label_of(p.labels, p.wide_labels, i) >= 0) before++;
+    } else {
+        for (size_t i = threadIdx.x; i < p.n; i += kPackThreads) {
+            if (label_of(p.labels, p.wide_labels, i) < 0) continue;
+            all++;
+            if (i < base) before++;
+            if (p.gradient && p.fp16 && first) most = fmaxf(most, largest_factor(p, i));
+        }
     }
 #pragma unroll
     for (int d = 16; d; d /= 2) {
@@ -153,8 +172,8 @@ __global__ void __launch_bounds__(kPackThreads) rd_vocab_pack_kernel(PackParams 
         sums[1][warp] = all;
         mosts[warp] = most;
     }
-    if (threadIdx.x < 32 && packs) {
-        const bool counts = lane < kPackRows && base + lane < p.n && label_of(p.labels, p.wide_labels, base + lane) >= 0;
+    if (warp == 0 && packs) {
+        const bool counts = lane < R && base + lane < p.n && label_of(p.labels, p.wide_labels, base + lane) >= 0;
         const uint32_t b = __ballot_sync(0xffffffffu, counts);
         if (lane == 0) mask_of_block = b;
     }
@@ -162,12 +181,12 @@ __global__ void __launch_bounds__(kPackThreads) rd_vocab_pack_kernel(PackParams 
     before = all = 0;
     most = 0.0f;
 #pragma unroll
-    for (int k = 0; k < kPackThreads / 32; k++) {
+    for (int k = 0; k < kWarps; k++) {
         before += sums[0][k];
         all += sums[1][k];
         most = fmaxf(most, mosts[k]);
     }
-    if (blockIdx.x == 0 && threadIdx.x == 0) {
+    if (first && threadIdx.x == 0) {
         // fp16: the largest factor goes to [2^13, 2^14): probabilities down to 2^-27 of it stay normal numbers
         float boost = 1.0f;
         if (p.fp16 && most > 0.0f) {
@@ -178,34 +197,31 @@ __global__ void __launch_bounds__(kPackThreads) rd_vocab_pack_kernel(PackParams 
         }
         *p.meta = Meta{all, boost, 1.0f / boost, 0};
     }
+    const int row = threadIdx.x / kRowThreads, t = threadIdx.x % kRowThreads;
     if (!packs) {
-        const size_t r = size_t(all) + (blockIdx.x - pack_blocks) * kPackRows + warp;
-        if (r >= (size_t(all) + kRowPad - 1) / kRowPad * kRowPad) return;
-        for (uint32_t j = lane; j < p.packed_stride; j += 32) p.packed[r * p.packed_stride + j] = 0;
-        if (lane == 0) {
-            p.index[r] = -1;
-            p.label[r] = -1;
-            if (p.gradient) p.gp[r] = p.gt[r] = p.lse2[r] = 0.0f;
-        }
+        const size_t r = size_t(all) + (blockIdx.x - pack_blocks) * R + row;
+        if (r >= (size_t(all) + kZeroPad - 1) / kZeroPad * kZeroPad) return;
+        uint4 *dst = reinterpret_cast<uint4 *>(p.packed + r * p.packed_stride);
+        for (uint32_t j = t; j < p.packed_stride / 8; j += kRowThreads) dst[j] = make_uint4(0, 0, 0, 0);
         return;
     }
-    const size_t i = base + warp;
+    const size_t i = base + row;
     if (i >= p.n) return;
     const uint32_t mask = mask_of_block;
-    if (!(mask >> warp & 1)) {
+    if (!(mask >> row & 1)) {
         if (p.gradient) {
             if (p.grad_hidden)
-                for (uint32_t j = lane; j < p.dim; j += 32) p.grad_hidden[i * p.grad_hidden_stride + j] = 0;
-        } else if (lane == 0) {
+                for (uint32_t j = t; j < p.dim; j += kRowThreads) p.grad_hidden[i * p.grad_hidden_stride + j] = 0;
+        } else if (t == 0) {
             if (p.loss) p.loss[i] = 0.0f;
             if (p.lse_out) p.lse_out[i] = 0.0f;
             if (p.target) p.target[i] = 0.0f;
         }
         return;
     }
-    const size_t r = size_t(before) + __popc(mask & ((1u << warp) - 1));
-    copy_row(p.packed + r * p.packed_stride, p.hidden + i * p.hidden_stride, p.dim, p.packed_stride, p.copy16, lane);
-    if (lane == 0) {
+    const size_t r = size_t(before) + __popc(mask & ((1u << row) - 1));
+    copy_row(p.packed + r * p.packed_stride, p.hidden + i * p.hidden_stride, p.dim, p.packed_stride, p.copy16, t, kRowThreads);
+    if (t == 0) {
         const long long l = label_of(p.labels, p.wide_labels, i);
         p.index[r] = int(i);
         p.label[r] = l >= p.first && l - p.first < static_cast<long long>(p.rows) ? int(l - p.first) : -1;
@@ -222,8 +238,9 @@ __global__ void __launch_bounds__(kPackThreads) rd_vocab_pack_kernel(PackParams 
 // Copies a weight whose rows TMA cannot address (unaligned base or stride) to rows that it can.
 __global__ void __launch_bounds__(kPackThreads) rd_vocab_align_kernel(uint16_t *dst, uint32_t dst_stride, const uint16_t *src, size_t src_stride, size_t rows, uint32_t dim)
 {
+    pdl_start();
     for (size_t r = size_t(blockIdx.x) * (kPackThreads / 32) + (threadIdx.x >> 5); r < rows; r += size_t(gridDim.x) * (kPackThreads / 32))
-        copy_row(dst + r * dst_stride, src + r * src_stride, dim, dst_stride, false, threadIdx.x & 31);
+        copy_row(dst + r * dst_stride, src + r * src_stride, dim, dst_stride, false, threadIdx.x & 31, 32);
 }
 
 // ------------------------------------------------------------------------------------------------ the products
@@ -246,13 +263,13 @@ struct alignas(64) MmaParams {
     const Meta *meta;
     const int *label;
     const float *gp, *gt, *lse2;
-    float2 *part;             // stats: (maximum, sum) in base 2, [half tile][packed row]
+    float2 *part;             // stats: (maximum, sum) in base 2, [packed row][half tile]
     float *target;            // stats: the label's logit, per packed row
     uint16_t *dx;             // dlogits: packed rows x dx_stride
     float *dh;                // grads: [split][packed row][dh_stride]
     uint16_t *dw;
-    size_t part_stride, dx_stride, dh_stride, dh_rows, dw_stride;
-    uint32_t rows;            // rows of the weight in all
+    size_t dx_stride, dh_stride, dh_rows, dw_stride;
+    uint32_t parts;           // stats: half tiles per row
     uint32_t piece0, piece;   // first row of the piece and its rows
     uint32_t dim;
     uint32_t group;           // token tiles that go over the vocabulary together
@@ -505,6 +522,7 @@ __global__ void __launch_bounds__(kMmaThreads, 1) rd_vocab_mma_kernel(const __gr
     uint32_t tmem;
     asm volatile("ld.shared.b32 %0, [%1];" : "=r"(tmem) : "r"(tmem_slot));
 
+    pdl_start();
     const uint32_t m = p.meta->m;
     const Plan<KIND, CG> plan(p, m);
     bool dead = false;
@@ -579,16 +597,18 @@ __global__ void __launch_bounds__(kMmaThreads, 1) rd_vocab_mma_kernel(const __gr
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
             }
             const uint32_t acc = tmem + buf * kTileN + 128 * half + (uint32_t(32 * quarter) << 16);
-            // the row's numbers (stats and dlogits; rows up to the next multiple of 128 exist and hold neutral values)
+            // the row's numbers (stats and dlogits)
             int label = -1;
             float lse2 = 0.0f, gp = 0.0f, gt = 0.0f, top = -INFINITY, sum = 0.0f;
-            if (KIND != kGrads) label = p.label[row] - int(p.piece0);
-            if (KIND == kDlogits) {
-                const float boost = p.meta->boost;
-                lse2 = p.lse2[row];
-                gp = p.gp[row] * boost;
-                gt = p.gt[row] * boost;
-                if (p.label[row] < 0) label = -1;
+            if (KIND != kGrads && row < m) {
+                label = p.label[row];
+                if (KIND == kDlogits) {
+                    const float boost = p.meta->boost;
+                    lse2 = p.lse2[row];
+                    gp = p.gp[row] * boost;
+                    gt = p.gt[row] * boost;
+                    label = label < int(p.piece0) ? -1 : label - int(p.piece0);
+                }
             }
             const float unboost = KIND == kGrads ? p.meta->unboost : 1.0f;
 #pragma unroll 1
@@ -602,21 +622,28 @@ __global__ void __launch_bounds__(kMmaThreads, 1) rd_vocab_mma_kernel(const __gr
                     for (int j = 0; j < 32; j++) v[j] = 0;
                 }
                 if (KIND == kStats) {
-                    float y[32], most = -INFINITY;
+                    // the lowest value in the columns that the vocabulary does not have
+                    const uint32_t lowest = __float_as_uint(p.scale2 >= 0.0f ? -INFINITY : INFINITY);
+                    if (col + 32 > p.piece) {
 #pragma unroll
-                    for (int j = 0; j < 32; j++) {
-                        y[j] = __uint_as_float(v[j]) * p.scale2;
-                        if (col + 32 > p.piece && col + j >= p.piece) y[j] = -INFINITY;
-                        most = fmaxf(most, y[j]);
+                        for (int j = 0; j < 32; j++)
+                            if (col + j >= p.piece) v[j] = lowest;
+                    }
+                    float most = __uint_as_float(v[0]);
+                    if (p.scale2 >= 0.0f) {
+#pragma unroll
+                        for (int j = 1; j < 32; j++) most = fmaxf(most, __uint_as_float(v[j]));
+                    } else {
+#pragma unroll
+                        for (int j = 1; j < 32; j++) most = fminf(most, __uint_as_float(v[j]));
                     }
                     // an infinite maximum must not meet itself in a difference: exp2(inf) and exp2(-inf) are right as they are
-                    most = fmaxf(most, top);
+                    most = fmaxf(most * p.scale2, top);
                     const float ref = fabsf(most) == INFINITY ? 0.0f : most;
-                    float s = top == -INFINITY ? 0.0f : sum * exp2_fast(top - ref);
-                    if (fabsf(top) == INFINITY) s = sum;
+                    float s[4] = {fabsf(top) == INFINITY ? sum : sum * exp2_fast(top - ref), 0.0f, 0.0f, 0.0f};
 #pragma unroll
-                    for (int j = 0; j < 32; j++) s += exp2_fast(y[j] - ref);
-                    sum = s;
+                    for (int j = 0; j < 32; j++) s[j & 3] += exp2_fast(fmaf(__uint_as_float(v[j]), p.scale2, -ref));
+                    sum = (s[0] + s[1]) + (s[2] + s[3]);
                     top = most;
                     if (label >= 0 && uint32_t(label) - col < 32u && row < m) {
 #pragma unroll
@@ -672,7 +699,7 @@ __global__ void __launch_bounds__(kMmaThreads, 1) rd_vocab_mma_kernel(const __gr
                 }
             }
             if (KIND == kStats) {
-                if (row < m) p.part[size_t(col0 / 128) * p.part_stride + row] = make_float2(top, sum);
+                if (row < m) p.part[size_t(row) * p.parts + col0 / 128] = make_float2(top, sum);
             }
             if (w.kblocks) {
                 asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
@@ -697,19 +724,18 @@ struct JoinParams {
     const float *packed_target;
     const int *index, *label;
     const Meta *meta;
-    size_t part_stride;
     uint32_t parts;
     float z;
     float *loss, *lse, *target;
 };
 
-// 32 packed rows per thread block; eight warps share the parts.
+// A warp per packed row.
 __global__ void __launch_bounds__(256) rd_vocab_join_kernel(JoinParams p)
 {
-    __shared__ float2 s[8][32];
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const uint32_t row = blockIdx.x * 32 + lane;
-    const bool live = row < p.meta->m;
+    pdl_start();
+    const int lane = threadIdx.x & 31;
+    const uint32_t row = blockIdx.x * 8 + (threadIdx.x >> 5);
+    if (row >= p.meta->m) return;
     float top = -INFINITY, sum = 0.0f;
     auto add = [&](float2 x) {
         const float most = fmaxf(top, x.x);
@@ -720,13 +746,19 @@ __global__ void __launch_bounds__(256) rd_vocab_join_kernel(JoinParams p)
         sum = a + b;
         top = most;
     };
-    if (live)
-        for (uint32_t k = warp; k < p.parts; k += 8) add(p.part[size_t(k) * p.part_stride + row]);
-    s[warp][lane] = make_float2(top, sum);
-    __syncthreads();
-    if (warp || !live) return;
+    const float2 *part = p.part + size_t(row) * p.parts;
+    uint32_t k = lane;
+    for (; k + 96 < p.parts; k += 128) {
+        float2 x[4];
 #pragma unroll
-    for (int k = 1; k < 8; k++) add(s[k][lane]);
+        for (int u = 0; u < 4; u++) x[u] = part[k + 32 * u];
+#pragma unroll
+        for (int u = 0; u < 4; u++) add(x[u]);
+    }
+    for (; k < p.parts; k += 32) add(part[k]);
+#pragma unroll
+    for (int d = 16; d; d /= 2) add(make_float2(__shfl_down_sync(0xffffffffu, top, d), __shfl_down_sync(0xffffffffu, sum, d)));
+    if (lane) return;
     const float ref = fabsf(top) == INFINITY ? 0.0f : top;
     const float lse = (ref + log2f(sum)) * kLn2;
     const float target = p.label[row] >= 0 ? p.packed_target[row] : 0.0f;
@@ -744,19 +776,40 @@ struct FinishParams {
     size_t dh_rows, dh_stride, out_stride;
     uint32_t dim, splits;
     uint16_t *out;
+    bool wide;
 };
 
-// Adds the parts of dh, takes the power of two off and rounds; one packed row per thread block and turn.
+constexpr uint32_t kFinishColumns = 1024;         // per thread block: 256 threads with four each
+
+// Adds the parts of dh in order, takes the power of two off and rounds.
 template <bool BF16> __global__ void __launch_bounds__(256) rd_vocab_finish_kernel(FinishParams p)
 {
+    pdl_start();
+    const uint32_t j = blockIdx.y * kFinishColumns + threadIdx.x * 4;
     const uint32_t m = p.meta->m;
     const float unboost = p.meta->unboost;
+    if (j >= p.dim) return;
+    const size_t step = p.dh_rows * p.dh_stride;
     for (uint32_t row = blockIdx.x; row < m; row += gridDim.x) {
-        const size_t i = size_t(p.index[row]);
-        for (uint32_t j = threadIdx.x; j < p.dim; j += 256) {
-            float sum = 0.0f;
-            for (uint32_t s = 0; s < p.splits; s++) sum += p.dh[(size_t(s) * p.dh_rows + row) * p.dh_stride + j];
-            p.out[i * p.out_stride + j] = uint16_t(pack2<BF16>(sum * unboost, 0.0f));
+        const float *src = p.dh + size_t(row) * p.dh_stride + j;        // rows hold a multiple of 8 values
+        uint16_t *dst = p.out + size_t(p.index[row]) * p.out_stride + j;
+        float4 sum = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll 4
+        for (uint32_t s = 0; s < p.splits; s++) {
+            const float4 x = *reinterpret_cast<const float4 *>(src + s * step);
+            sum.x += x.x;
+            sum.y += x.y;
+            sum.z += x.z;
+            sum.w += x.w;
+        }
+        const uint32_t lo = pack2<BF16>(sum.x * unboost, sum.y * unboost), hi = pack2<BF16>(sum.z * unboost, sum.w * unboost);
+        if (p.wide && j + 4 <= p.dim) {
+            *reinterpret_cast<uint2 *>(dst) = make_uint2(lo, hi);
+        } else {
+            const uint16_t v[4] = {uint16_t(lo), uint16_t(lo >> 16), uint16_t(hi), uint16_t(hi >> 16)};
+#pragma unroll
+            for (int k = 0; k < 4; k++)
+                if (j + k < p.dim) dst[k] = v[k];
         }
     }
 }
@@ -889,12 +942,12 @@ template <int KIND, bool BF16, int CG> cudaError_t launch_mma(const MmaParams &p
     c.blockDim = dim3(kMmaThreads);
     c.dynamicSmemBytes = smem;
     c.stream = stream;
-    cudaLaunchAttribute cluster;
-    cluster.id = cudaLaunchAttributeClusterDimension;
-    cluster.val.clusterDim.x = CG;
-    cluster.val.clusterDim.y = cluster.val.clusterDim.z = 1;
-    c.attrs = &cluster;
-    c.numAttrs = 1;
+    cudaLaunchAttribute attrs[2] = {pdl_attribute()};
+    attrs[1].id = cudaLaunchAttributeClusterDimension;
+    attrs[1].val.clusterDim.x = CG;
+    attrs[1].val.clusterDim.y = attrs[1].val.clusterDim.z = 1;
+    c.attrs = attrs;
+    c.numAttrs = 2;
     return cudaLaunchKernelEx(&c, rd_vocab_mma_kernel<KIND, BF16, CG>, p);
 }
 template <int KIND> cudaError_t launch_mma(const MmaParams &p, bool bf16, int cg, int device, size_t most_units, cudaStream_t stream)
@@ -937,17 +990,30 @@ cudaError_t prepare(const VocabArgs &a, const Layout &l, bool gradient, const ui
     p.grad_hidden_stride = a.grad_hidden_stride;
     p.gradient = gradient;
     p.fp16 = !a.bf16;
-    const unsigned tiles = unsigned((a.n + kCountTile - 1) / kCountTile), blocks = unsigned((a.n + kPackRows - 1) / kPackRows);
-    rd_vocab_count_kernel<<<tiles, kCountTile, 0, a.stream>>>(p, l.tiles);
-    rd_vocab_pack_kernel<<<blocks + kRowPad / kPackRows, kPackThreads, 0, a.stream>>>(p, blocks, tiles);
+    cudaError_t e = cudaSuccess;
+    unsigned tiles = 0;
+    if (a.n >= kCountFrom) {
+        tiles = unsigned((a.n + kCountTile - 1) / kCountTile);
+        e = launch(rd_vocab_count_kernel, tiles, kCountTile, a.stream, p, l.tiles);
+        if (e != cudaSuccess) return e;
+    }
+    // few tokens: a thread block for each, so that their rows are copied by many threads
+    if (a.n <= 1024) {
+        const unsigned blocks = unsigned(a.n);
+        e = launch(rd_vocab_pack_kernel<1>, blocks + (gradient ? kZeroPad : 0), kPackThreads, a.stream, p, blocks, tiles);
+    } else {
+        const unsigned blocks = unsigned((a.n + 7) / 8);
+        e = launch(rd_vocab_pack_kernel<8>, blocks + (gradient ? kZeroPad / 8 : 0), kPackThreads, a.stream, p, blocks, tiles);
+    }
+    if (e != cudaSuccess) return e;
     *weight = static_cast<const uint16_t *>(a.weight);
     *weight_stride = a.weight_stride;
     if (l.weight) {
-        rd_vocab_align_kernel<<<1184, kPackThreads, 0, a.stream>>>(l.weight, uint32_t(l.packed_stride), *weight, a.weight_stride, a.rows, uint32_t(a.dim));
+        e = launch(rd_vocab_align_kernel, 1184, kPackThreads, a.stream, l.weight, uint32_t(l.packed_stride), *weight, a.weight_stride, a.rows, uint32_t(a.dim));
         *weight = l.weight;
         *weight_stride = l.packed_stride;
     }
-    return cudaGetLastError();
+    return e;
 }
 
 // Token tiles that go over the vocabulary together: their hidden rows (tile x dim) should stay in L2 beside the weight's.
@@ -961,7 +1027,6 @@ void common(MmaParams &q, const VocabArgs &a, const Layout &l, int cg)
 {
     q.meta = l.meta;
     q.label = l.label;
-    q.rows = uint32_t(a.rows);
     q.dim = uint32_t(a.dim);
     q.group = token_group(a.dim, size_t(kRowsM) * cg);
     q.scale = a.scale;
@@ -989,16 +1054,15 @@ cudaError_t vocab_loss(const VocabArgs &a)
     if (!encode(&q.a_k, a.bf16, l.packed, a.dim, l.rows_padded, l.packed_stride, kRowsM) || !encode(&q.b_k, a.bf16, weight, a.dim, a.rows, weight_stride, kTileN / cg))
         return cudaErrorInvalidValue;
     q.part = l.part;
-    q.part_stride = l.rows_padded;
+    q.parts = uint32_t(2 * ((a.rows + kTileN - 1) / kTileN));
     q.target = l.target;
     q.piece0 = 0;
     q.piece = uint32_t(a.rows);
     const size_t units = (a.n + tile_m - 1) / tile_m * ((a.rows + kTileN - 1) / kTileN);
     e = launch_mma<kStats>(q, a.bf16, cg, device, units, a.stream);
     if (e != cudaSuccess) return e;
-    const JoinParams j{l.part, l.target, l.index, l.label, l.meta, l.rows_padded, uint32_t(2 * ((a.rows + kTileN - 1) / kTileN)), a.z_loss, a.loss, a.lse_out, a.target};
-    rd_vocab_join_kernel<<<unsigned((a.n + 31) / 32), 256, 0, a.stream>>>(j);
-    return cudaGetLastError();
+    const JoinParams j{l.part, l.target, l.index, l.label, l.meta, q.parts, a.z_loss, a.loss, a.lse_out, a.target};
+    return launch(rd_vocab_join_kernel, unsigned((a.n + 7) / 8), 256, a.stream, j);
 }
 
 size_t vocab_loss_grad_workspace(const VocabArgs &a, bool want_hidden) { return lay_out(a, true, want_hidden).bytes; }
@@ -1049,12 +1113,12 @@ cudaError_t vocab_loss_grad(const VocabArgs &a)
         if (e != cudaSuccess) return e;
     }
     if (a.grad_hidden) {
-        const FinishParams f{l.dh, l.index, l.meta, a.n, l.dh_stride, a.grad_hidden_stride, uint32_t(a.dim), uint32_t(l.splits), static_cast<uint16_t *>(a.grad_hidden)};
-        const unsigned grid = unsigned(a.n < 1184 ? a.n : 1184);
-        if (a.bf16) rd_vocab_finish_kernel<true><<<grid, 256, 0, a.stream>>>(f);
-        else rd_vocab_finish_kernel<false><<<grid, 256, 0, a.stream>>>(f);
+        const bool wide = reinterpret_cast<uintptr_t>(a.grad_hidden) % 8 == 0 && a.grad_hidden_stride % 4 == 0;
+        const FinishParams f{l.dh, l.index, l.meta, a.n, l.dh_stride, a.grad_hidden_stride, uint32_t(a.dim), uint32_t(l.splits), static_cast<uint16_t *>(a.grad_hidden), wide};
+        const dim3 grid(unsigned(a.n < 65536 ? a.n : 65536), unsigned((a.dim + kFinishColumns - 1) / kFinishColumns));
+        e = a.bf16 ? launch(rd_vocab_finish_kernel<true>, grid, 256, a.stream, f) : launch(rd_vocab_finish_kernel<false>, grid, 256, a.stream, f);
     }
-    return cudaGetLastError();
+    return e;
 }
 
 cudaError_t vocab_status(int *status)

@@ -38,7 +38,7 @@ int check_vocab(const rd_vocab_t *v)
 {
     if (!v) return RD_ERR_INVALID_ARG;
     if (!known(v->dtype) || (v->label_type != RD_INT32 && v->label_type != RD_INT64)) return RD_ERR_INVALID_ARG;
-    if (v->dim < 1 || v->dim > kMostDim || v->rows < 1 || v->first_row < 0 || !std::isfinite(v->scale) || !std::isfinite(v->z_loss)) return RD_ERR_INVALID_ARG;
+    if (v->dim < 1 || v->dim > kMostDim || v->rows < 1 || v->first_row < 0 || !std::isfinite(v->scale) || v->scale == 0.0f || !std::isfinite(v->z_loss)) return RD_ERR_INVALID_ARG;
     if (v->dtype != RD_BF16 && v->dtype != RD_FP16) return RD_ERR_UNSUPPORTED;
     if (v->rows > kMostRows || v->n > kMostRows) return RD_ERR_UNSUPPORTED;
     // output tiles are counted in 32 bits

@@ -481,7 +481,7 @@ def vocab_struct(hidden=P, hs=8, weight=2 * P, ws=8, labels=4 * P, n=4, rows=16,
 
 
 BAD_VOCAB = (dict(hidden=None), dict(weight=None), dict(labels=None), dict(hidden=P + 1), dict(weight=2 * P + 1), dict(labels=4 * P + 4), dict(hs=7), dict(ws=7), dict(ws=0),
-             dict(rows=0), dict(dim=0), dict(dim=65537, hs=65537, ws=65537), dict(first=-1), dict(dtype=12), dict(lt=rd.RD_FP16), dict(scale=math.inf), dict(z=math.nan))
+             dict(rows=0), dict(dim=0), dict(dim=65537, hs=65537, ws=65537), dict(first=-1), dict(dtype=12), dict(lt=rd.RD_FP16), dict(scale=math.inf), dict(scale=0.0), dict(z=math.nan))
 
 
 def test_vocab_loss_refusals():
