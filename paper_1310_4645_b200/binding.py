@@ -424,74 +424,88 @@ def rd_destroy(h) -> None:
 # Vocabulary operators
 
 
+# A call costs its user a few microseconds of host time, as much as a small kernel, so the checks below are written for few
+# Python operations: integers instead of device objects, one dictionary per dtype, no context manager on the usual path.
+
+_DTYPES = None      # torch dtype -> rd_dtype_t, filled on first use (torch is imported lazily)
+_torch = None
+
+
+def _setup():
+    global _torch, _DTYPES
+    import torch
+    _DTYPES = {torch.int32: RD_INT32, torch.float32: RD_FP32, torch.int64: RD_INT64, torch.float64: RD_FP64,
+               torch.bfloat16: RD_BF16, torch.float16: RD_FP16}
+    _torch = torch
+
+
+def _elsewhere(t, stream):
+    """Whether a call has to change the current device or stream first."""
+    if _torch is None:
+        _setup()
+    return stream is not None or t.get_device() != _torch.cuda.current_device()
+
+
+def _there(f, t, stream, *args, **kw):
+    """Makes the tensor's device and the stream current for a call, so that what it allocates belongs to that stream."""
+    if not t.is_cuda:
+        raise ValueError("CUDA tensors are expected")
+    with _torch.cuda.device(t.device):
+        with _torch.cuda.stream(stream if stream is not None else _torch.cuda.current_stream()):
+            return f(*args, **kw)
+
+
+def _stream(device):
+    return _torch._C._cuda_getCurrentRawStream(device)
+
+
+def _code(t):
+    code = _DTYPES.get(t.dtype)
+    return code if code is not None else _dtype_code(t)
+
+
 def _matrix(t, what):
     """A 2-D CUDA tensor whose rows are contiguous: (address, row stride in elements)."""
     if not t.is_cuda or t.dim() != 2:
         raise ValueError("%s must be a 2-D CUDA tensor" % what)
     stride, inner = t.stride()
-    if inner != 1 and t.shape[1] > 1:
+    rows, dim = t.shape
+    if inner != 1 and dim > 1:
         raise ValueError("the rows of %s must be contiguous" % what)
-    return t.data_ptr(), stride if t.shape[0] > 1 else t.shape[1]
+    return t.data_ptr(), stride if rows > 1 else dim
 
 
 def _vector(t, what, n, device):
-    if not t.is_cuda or t.device != device or t.dim() != 1 or t.shape[0] != n or not t.is_contiguous():
+    if t.get_device() != device or t.shape != (n,) or not t.is_contiguous():
         raise ValueError("%s must be a contiguous CUDA vector with one value per token, on the operands' device" % what)
     return t.data_ptr()
 
 
-class _On:
-    """Makes a tensor's device current for a call, and gives the stream and, there, temporary memory."""
-
-    def __init__(self, device, stream):
-        import torch
-        self.device = device
-        self.stream = stream if stream is not None else torch.cuda.current_stream(device)
-        self.other = stream is not None and stream != torch.cuda.current_stream(device)
-
-    def __enter__(self):
-        import torch
-        self.prev = torch.cuda.current_device()
-        if self.prev != self.device.index:
-            torch.cuda.set_device(self.device)
-        return self
-
-    def __exit__(self, *exc):
-        import torch
-        if self.prev != self.device.index:
-            torch.cuda.set_device(self.prev)
-
-    def empty(self, shape, dtype):
-        """Memory of the call's stream: the allocator may hand it out again once that stream has passed the call."""
-        import torch
-        if self.other:
-            with torch.cuda.stream(self.stream):
-                return torch.empty(shape, dtype=dtype, device=self.device)
-        return torch.empty(shape, dtype=dtype, device=self.device)
-
-    def workspace(self, given, need):
-        import torch
-        if given is None:
-            return self.empty(need, torch.uint8)
-        if not given.is_cuda or given.device != self.device or not given.is_contiguous():
-            raise ValueError("workspace must be a contiguous CUDA tensor on the operands' device")
-        return given
+def _workspace(given, need, device):
+    if given is None:
+        given = _torch.empty(need, dtype=_torch.uint8, device="cuda")
+    elif given.get_device() != device or not given.is_contiguous():
+        raise ValueError("workspace must be a contiguous CUDA tensor on the operands' device")
+    return given.data_ptr(), given.numel() * given.element_size(), given
 
 
 def rd_embed(table, ids, out=None, first_row=0, scale=1.0, stream=None):
     """scale * table[ids - first_row], rows of zeros where the table does not hold an id.  table: [rows, dim] float32,
     bfloat16 or float16; ids: int32 or int64 vector; out: [n, dim] of table's dtype (allocated when None).  Returns out."""
+    if _elsewhere(table, stream):
+        return _there(rd_embed, table, stream, table, ids, out, first_row, scale)
     addr, stride = _matrix(table, "table")
-    n, (rows, dim) = ids.numel(), table.shape
-    ids_addr = _vector(ids, "ids", n, table.device)
-    with _On(table.device, stream) as on:
-        if out is None:
-            out = on.empty((n, dim), table.dtype)
+    device, n, (rows, dim) = table.get_device(), ids.numel(), table.shape
+    ids_addr = _vector(ids, "ids", n, device)
+    if out is None:
+        out = table.new_empty((n, dim))
+        out_addr, out_stride = out.data_ptr(), dim
+    else:
         out_addr, out_stride = _matrix(out, "out")
-        if out.shape != (n, dim) or out.dtype != table.dtype or out.device != table.device:
+        if out.shape != (n, dim) or out.dtype != table.dtype or out.get_device() != device:
             raise ValueError("out must be [n, dim] with table's dtype and device")
-        _check(lib().rd_embed(addr, stride, rows, dim, _dtype_code(table), ids_addr, _dtype_code(ids), n, first_row, scale,
-                              out_addr, out_stride, on.stream.cuda_stream), "rd_embed")
+    _check(lib().rd_embed(addr, stride, rows, dim, _code(table), ids_addr, _code(ids), n, first_row, scale, out_addr, out_stride,
+                          _stream(device)), "rd_embed")
     return out
 
 
@@ -504,31 +518,33 @@ def rd_embed_grad_workspace(rows, dim, n) -> int:
 def rd_embed_grad(grad_out, ids, grad_table, first_row=0, scale=1.0, accumulate=False, workspace=None, stream=None):
     """grad_table[v] (+)= scale * sum of grad_out[i] over the tokens with ids[i] - first_row = v.  grad_out: [n, dim]; grad_table:
     [rows, dim] of grad_out's dtype or float32; workspace: rd_embed_grad_workspace bytes (allocated when None).  Returns grad_table."""
+    if _elsewhere(grad_out, stream):
+        return _there(rd_embed_grad, grad_out, stream, grad_out, ids, grad_table, first_row, scale, accumulate, workspace)
     addr, stride = _matrix(grad_out, "grad_out")
     taddr, tstride = _matrix(grad_table, "grad_table")
-    (n, dim), rows = grad_out.shape, grad_table.shape[0]
-    ids_addr = _vector(ids, "ids", n, grad_out.device)
-    if grad_table.shape[1] != dim or grad_table.device != grad_out.device:
+    device, (n, dim), rows = grad_out.get_device(), grad_out.shape, grad_table.shape[0]
+    ids_addr = _vector(ids, "ids", n, device)
+    if grad_table.shape[1] != dim or grad_table.get_device() != device:
         raise ValueError("grad_table must be [rows, dim] on grad_out's device")
-    with _On(grad_out.device, stream) as on:
-        ws = on.workspace(workspace, rd_embed_grad_workspace(rows, dim, n))
-        _check(lib().rd_embed_grad(addr, stride, _dtype_code(grad_out), ids_addr, _dtype_code(ids), n, first_row, scale, taddr, tstride,
-                                   _dtype_code(grad_table), rows, dim, int(accumulate), ws.data_ptr(), ws.numel() * ws.element_size(),
-                                   on.stream.cuda_stream), "rd_embed_grad")
+    ws, size, _keep = _workspace(workspace, rd_embed_grad_workspace(rows, dim, n), device)
+    _check(lib().rd_embed_grad(addr, stride, _code(grad_out), ids_addr, _code(ids), n, first_row, scale, taddr, tstride, _code(grad_table),
+                               rows, dim, int(accumulate), ws, size, _stream(device)), "rd_embed_grad")
     return grad_table
 
 
 def _vocab(hidden, weight, labels, first_row, scale, z_loss):
     addr, stride = _matrix(hidden, "hidden")
     waddr, wstride = _matrix(weight, "weight")
-    (n, dim), rows = hidden.shape, weight.shape[0]
-    if weight.shape[1] != dim or weight.dtype != hidden.dtype or weight.device != hidden.device:
+    device, (n, dim), rows = hidden.get_device(), hidden.shape, weight.shape[0]
+    if weight.shape[1] != dim or weight.dtype != hidden.dtype or weight.get_device() != device:
         raise ValueError("weight must be [rows, dim] with hidden's dtype and device")
-    return rd_vocab_t(addr, stride, waddr, wstride, _vector(labels, "labels", n, hidden.device), n, rows, dim, first_row,
-                      _dtype_code(hidden), _dtype_code(labels), scale, z_loss)
+    return rd_vocab_t(addr, stride, waddr, wstride, _vector(labels, "labels", n, device), n, rows, dim, first_row, _code(hidden),
+                      _code(labels), scale, z_loss)
 
 
 def rd_vocab_loss_workspace(hidden, weight, labels) -> int:
+    if _torch is None:
+        _setup()
     need = C.c_size_t()
     _check(lib().rd_vocab_loss_workspace(C.byref(_vocab(hidden, weight, labels, 0, 1.0, 0.0)), C.byref(need)), "rd_vocab_loss_workspace")
     return need.value
@@ -537,20 +553,22 @@ def rd_vocab_loss_workspace(hidden, weight, labels) -> int:
 def rd_vocab_loss(hidden, weight, labels, first_row=0, scale=1.0, z_loss=0.0, workspace=None, stream=None):
     """Softmax cross entropy of the logits scale * hidden @ weight.T: (loss, lse, target), float32 vectors with one value per token,
     0 where the label is negative.  hidden: [n, dim], weight: [rows, dim], both bfloat16 or float16; labels: int32 or int64."""
-    import torch
+    if _elsewhere(hidden, stream):
+        return _there(rd_vocab_loss, hidden, stream, hidden, weight, labels, first_row, scale, z_loss, workspace)
     v = _vocab(hidden, weight, labels, first_row, scale, z_loss)
-    with _On(hidden.device, stream) as on:
-        out = on.empty((3, v.n), torch.float32)
-        need = C.c_size_t()
-        _check(lib().rd_vocab_loss_workspace(C.byref(v), C.byref(need)), "rd_vocab_loss")
-        ws = on.workspace(workspace, need.value)
-        at = out.data_ptr()
-        _check(lib().rd_vocab_loss(C.byref(v), at, at + 4 * v.n, at + 8 * v.n, ws.data_ptr(), ws.numel() * ws.element_size(),
-                                   on.stream.cuda_stream), "rd_vocab_loss")
-    return out[0], out[1], out[2]
+    device, n, ref = hidden.get_device(), hidden.shape[0], C.byref(v)
+    out = hidden.new_empty((3, n), dtype=_torch.float32)
+    need = C.c_size_t()
+    _check(lib().rd_vocab_loss_workspace(ref, C.byref(need)), "rd_vocab_loss")
+    ws, size, _keep = _workspace(workspace, need.value, device)
+    at = out.data_ptr()
+    _check(lib().rd_vocab_loss(ref, at, at + 4 * n, at + 8 * n, ws, size, _stream(device)), "rd_vocab_loss")
+    return out.unbind()
 
 
 def rd_vocab_loss_grad_workspace(hidden, weight, labels, want_hidden=True, want_weight=True) -> int:
+    if _torch is None:
+        _setup()
     need = C.c_size_t()
     _check(lib().rd_vocab_loss_grad_workspace(C.byref(_vocab(hidden, weight, labels, 0, 1.0, 0.0)), int(want_hidden), int(want_weight),
                                               C.byref(need)), "rd_vocab_loss_grad_workspace")
@@ -562,30 +580,34 @@ def rd_vocab_loss_grad(hidden, weight, labels, lse, grad_loss, grad_hidden=None,
     """Gradients of sum(grad_loss * loss) into grad_hidden [n, dim] and grad_weight [rows, dim] (one may be None: not computed).
     lse: rd_vocab_loss's, joined over the slices of the vocabulary; grad_loss: float32 vector, may be a broadcast one, or a scalar
     tensor.  Returns (grad_hidden, grad_weight)."""
-    import torch
+    if _elsewhere(hidden, stream):
+        return _there(rd_vocab_loss_grad, hidden, stream, hidden, weight, labels, lse, grad_loss, grad_hidden, grad_weight, first_row, scale,
+                      z_loss, workspace)
     v = _vocab(hidden, weight, labels, first_row, scale, z_loss)
-    lse_addr = _vector(lse, "lse", v.n, hidden.device)
+    device, n, ref = hidden.get_device(), hidden.shape[0], C.byref(v)
+    lse_addr = _vector(lse, "lse", n, device)
     if grad_loss.dim() == 0:
-        grad_loss = grad_loss.expand(v.n)
-    if not grad_loss.is_cuda or grad_loss.device != hidden.device or grad_loss.shape != (v.n,) or \
-            grad_loss.dtype != torch.float32 or lse.dtype != torch.float32:
+        grad_loss = grad_loss.expand(n)
+    if grad_loss.get_device() != device or grad_loss.shape != (n,) or grad_loss.dtype != _torch.float32 or lse.dtype != _torch.float32:
         raise ValueError("lse and grad_loss must be float32 CUDA vectors with one value per token")
     gh = gw = (None, 0)
     if grad_hidden is not None:
         gh = _matrix(grad_hidden, "grad_hidden")
+        _like(grad_hidden, hidden)
     if grad_weight is not None:
         gw = _matrix(grad_weight, "grad_weight")
-    for g, like in ((grad_hidden, hidden), (grad_weight, weight)):
-        if g is not None and (g.shape != like.shape or g.dtype != like.dtype or g.device != like.device):
-            raise ValueError("a gradient has its operand's shape, dtype and device")
-    with _On(hidden.device, stream) as on:
-        need = C.c_size_t()
-        _check(lib().rd_vocab_loss_grad_workspace(C.byref(v), int(grad_hidden is not None), int(grad_weight is not None), C.byref(need)),
-               "rd_vocab_loss_grad")
-        ws = on.workspace(workspace, need.value)
-        _check(lib().rd_vocab_loss_grad(C.byref(v), lse_addr, grad_loss.data_ptr(), grad_loss.stride(0), *gh, *gw, ws.data_ptr(),
-                                        ws.numel() * ws.element_size(), on.stream.cuda_stream), "rd_vocab_loss_grad")
+        _like(grad_weight, weight)
+    need = C.c_size_t()
+    _check(lib().rd_vocab_loss_grad_workspace(ref, grad_hidden is not None, grad_weight is not None, C.byref(need)), "rd_vocab_loss_grad")
+    ws, size, _keep = _workspace(workspace, need.value, device)
+    _check(lib().rd_vocab_loss_grad(ref, lse_addr, grad_loss.data_ptr(), grad_loss.stride(0), *gh, *gw, ws, size, _stream(device)),
+           "rd_vocab_loss_grad")
     return grad_hidden, grad_weight
+
+
+def _like(grad, operand):
+    if grad.shape != operand.shape or grad.dtype != operand.dtype or grad.get_device() != operand.get_device():
+        raise ValueError("a gradient has its operand's shape, dtype and device")
 
 
 def rd_vocab_status() -> int:
