@@ -6,20 +6,26 @@
 // Both only move data, so both are bound by HBM: the lookup reads and writes n rows, the gradient reads n rows and writes
 // the whole table (the rows no token has get zeros in the same pass).  Sums are fp32 and rounded once at the end.
 //
-// Gradient.  Tokens are grouped by row, so that every row of the table is written once, by one owner, without
-// floating-point atomics: the order of the additions, hence every bit of the result, depends on the ids alone.
-//   count    cnt[v] = number of tokens of row v; integer atomics, one per distinct row and warp
-//   place    every row with tokens gets a range of the token list (where in the list does not matter), in list order
-//            of arrival, which does depend on timing ...
-//   sort     ... and is put in ascending order here: each token looks up how many of its row's tokens come before it.
-//            Rows with more than kChunk tokens go through a bitmap of token positions in shared memory instead.
-//   sum      one group of threads per row adds its tokens' gradients in ascending order.  Rows with more than kChunk
-//            tokens are cut into chunks of kChunk, summed side by side into fp32 partial rows,
-//   join     which are added in ascending order.
+// Gradient.  Tokens are grouped by row, so that every row of the table is summed without floating-point atomics: the order of
+// the additions, hence every bit of the result, depends on the ids alone.  The work list has items: a row and at most kChunk of
+// its tokens, ascending.
+//   up to kSmallTokens tokens: rank    every token counts, over all tokens, those of lower rows, of its row, and of its row before
+//          it; that is its place in the list, and whether an item begins there.
+//   more:  count   cnt[v] = number of tokens of row v; integer atomics, one per distinct row and warp
+//          ranges  every row with tokens gets a range of the token list (where in the list does not matter) and its items
+//          place   puts the tokens there, in order of arrival, which does depend on timing ...
+//          sort    ... and in ascending order here: each token looks up how many of its row's tokens come before it; rows with
+//                  more than kChunk tokens go through a bitmap of token positions in shared memory instead.
+//   fill   zeros in the whole table.  It needs nothing of the above, so it runs beside it: beside rank, because it does not wait
+//          for it; beside the others, because those go to a stream of the library's own, forked off and joined by events.
+//   sum    a group of threads per item and slab of columns adds up the gradients; a row with several items has them added in
+//          ascending order by whichever group finishes last.
 #include "rd_vocab.h"
 
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
+
+#include <mutex>
 
 #include "rd.h"
 #include "rd_launch.h"
@@ -29,7 +35,9 @@ namespace rd {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr uint32_t kChunk = 64;         // tokens one thread group adds up by itself
+constexpr uint32_t kChunk = 32;         // tokens that one thread group adds up
+constexpr uint32_t kBigItem = 8;        // items with more tokens are dealt out first, so that no thread group meets one at its end
+constexpr uint32_t kSmallTokens = 8192; // up to here every token counts over all others
 
 template <typename T> __device__ __forceinline__ float widen(T v);
 template <> __device__ __forceinline__ float widen<float>(float v) { return v; }
@@ -40,11 +48,38 @@ template <> __device__ __forceinline__ float narrow<float>(float v) { return v; 
 template <> __device__ __forceinline__ __nv_bfloat16 narrow<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
 template <> __device__ __forceinline__ __half narrow<__half>(float v) { return __float2half_rn(v); }
 
-// V consecutive elements, moved as one access of up to 16 bytes (two for fp32 results of 16-bit vectors).
-template <typename T, int V> struct alignas(sizeof(T) * V < 16 ? sizeof(T) * V : 16) Vec { T v[V]; };
+// V consecutive elements, moved in accesses of up to 32 bytes (of up to 16 when the vector's type only promises that much).
+template <typename T, int V> struct alignas(sizeof(T) * V < 32 ? sizeof(T) * V : 32) Vec { T v[V]; };
 
-template <typename T, int V> __device__ __forceinline__ Vec<T, V> load(const T *p) { return *reinterpret_cast<const Vec<T, V> *>(p); }
-template <typename T, int V> __device__ __forceinline__ void store(T *p, const Vec<T, V> &x) { *reinterpret_cast<Vec<T, V> *>(p) = x; }
+template <typename T, int V> __device__ __forceinline__ Vec<T, V> load(const T *p)
+{
+    Vec<T, V> x;
+    if constexpr (sizeof(x) == 32) {
+        uint32_t(&w)[8] = *reinterpret_cast<uint32_t(*)[8]>(&x);
+        asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                     : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]), "=r"(w[4]), "=r"(w[5]), "=r"(w[6]), "=r"(w[7])
+                     : "l"(p));
+    } else if constexpr (sizeof(x) > 32) {
+#pragma unroll
+        for (int k = 0; k < V; k += 32 / sizeof(T)) *reinterpret_cast<Vec<T, 32 / sizeof(T)> *>(x.v + k) = load<T, 32 / sizeof(T)>(p + k);
+    } else {
+        x = *reinterpret_cast<const Vec<T, V> *>(p);
+    }
+    return x;
+}
+template <typename T, int V> __device__ __forceinline__ void store(T *p, const Vec<T, V> &x)
+{
+    if constexpr (sizeof(x) == 32) {
+        const uint32_t(&w)[8] = *reinterpret_cast<const uint32_t(*)[8]>(&x);
+        asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7])
+                     : "memory");
+    } else if constexpr (sizeof(x) > 32) {
+#pragma unroll
+        for (int k = 0; k < V; k += 32 / sizeof(T)) store<T, 32 / sizeof(T)>(p + k, *reinterpret_cast<const Vec<T, 32 / sizeof(T)> *>(x.v + k));
+    } else {
+        *reinterpret_cast<Vec<T, V> *>(p) = x;
+    }
+}
 
 // The table row of token i, or a negative number when the table does not hold it.
 __device__ __forceinline__ long long row_of(const void *ids, bool wide, size_t i, long long first, size_t rows)
@@ -54,7 +89,7 @@ __device__ __forceinline__ long long row_of(const void *ids, bool wide, size_t i
     return id - first < static_cast<long long>(rows) ? id - first : -1;
 }
 
-constexpr int kGatherUnroll = 4;
+constexpr int kGatherUnroll = 2;
 
 // A thread block copies kThreads * kGatherUnroll consecutive vectors of the flattened output.
 template <typename T, int V>
@@ -106,19 +141,30 @@ template <typename T, int V> cudaError_t launch_embed(const EmbedArgs &a)
                   vecs, total, a.scale, static_cast<T *>(a.out), a.out_stride);
 }
 
-bool vector_rows(const void *p, size_t stride, size_t dim, size_t esize)
+// Whether rows begin and end on multiples of `to` bytes.
+bool vector_rows(const void *p, size_t stride, size_t dim, size_t esize, size_t to)
 {
-    return reinterpret_cast<uintptr_t>(p) % 16 == 0 && stride * esize % 16 == 0 && dim * esize % 16 == 0;
+    return reinterpret_cast<uintptr_t>(p) % to == 0 && stride * esize % to == 0 && dim * esize % to == 0;
 }
 
 // ---------------------------------------------------------------------------------------------------- gradient
 
 struct GradMeta {
     uint32_t list_used;       // entries of the token list handed out to rows
+    uint32_t n_big;           // items with more than kBigItem tokens: items[0 ..
+    uint32_t n_items;         // the others, from items[big_room] on; some may be empty
     uint32_t n_long;          // rows with more than kChunk tokens
-    uint32_t n_chunks;        // their chunks
+};
+
+struct Item {
+    uint32_t row, begin, count;       // list[begin .. begin + count)
+    uint32_t part, parts;             // which of the row's items this is, and how many there are
     uint32_t pad;
 };
+
+// Where the partial sums of part k of a row go whose tokens begin at list[begin]: no two parts of rows with more than kChunk tokens
+// get the same one, since of kChunk consecutive list entries at most one begins a first part and at most one a later one.
+__host__ __device__ __forceinline__ uint32_t slot_of(uint32_t begin, uint32_t k) { return 2 * ((begin + k * kChunk) / kChunk) + (k == 0); }
 
 struct GradWork {             // the workspace's parts
     GradMeta *meta;
@@ -128,18 +174,31 @@ struct GradWork {             // the workspace's parts
     uint32_t *arrived;        // n: token list, in order of arrival within a row
     uint32_t *list;           // n: token list, ascending within a row
     uint32_t *long_row;       // rows with more than kChunk tokens
-    uint32_t *long_chunk;     // their first chunk
-    uint32_t *chunk_row;      // per chunk: index into long_row
-    float *partial;           // per chunk: dim fp32 values
-    size_t bytes, zero_bytes;
+    Item *items;
+    uint32_t *done;           // per slot and slab: items of the row that have their partial sums written
+    float *partial;           // per slot: dim fp32 values
+    uint32_t big_room;
+    size_t partial_stride, bytes, zero_bytes;
 };
 
+constexpr unsigned kSumBlocks = 148 * 3;
+constexpr uint32_t kMostLanes = 32;       // threads per item and slab: within a warp
 size_t max_long(size_t n) { return n / (kChunk + 1); }
-size_t max_chunks(size_t n) { return n / kChunk + max_long(n); }
+size_t max_slots(size_t n) { return n > kChunk ? 2 * (n / kChunk + 1) : 0; }
+size_t max_big(size_t n) { return n <= kSmallTokens ? 0 : n / (kBigItem + 1); }
+size_t max_items(size_t n, size_t rows) { return n <= kSmallTokens ? n : (n < rows ? n : rows) + n / kChunk; }
+uint32_t lanes_for(uint32_t vecs)
+{
+    uint32_t lanes = 8;
+    while (lanes < kMostLanes && lanes < vecs) lanes *= 2;
+    return lanes;
+}
+// Slabs of columns when a thread moves one element at a time: the most there can be.
+size_t max_slabs(size_t dim) { return (dim + kMostLanes - 1) / kMostLanes; }
 
 GradWork layout(void *workspace, size_t rows, size_t dim, size_t n)
 {
-    GradWork w;
+    GradWork w{};
     size_t at = 0;
     char *base = static_cast<char *>(workspace);
     auto take = [&](size_t bytes) {
@@ -147,17 +206,22 @@ GradWork layout(void *workspace, size_t rows, size_t dim, size_t n)
         at += (bytes + 255) / 256 * 256;
         return p;
     };
+    const bool small = n <= kSmallTokens;
+    w.partial_stride = (dim + 7) / 8 * 8;
     w.meta = reinterpret_cast<GradMeta *>(take(sizeof(GradMeta)));
-    w.cnt = reinterpret_cast<uint32_t *>(take(rows * 4));
-    w.zero_bytes = at;
-    w.start = reinterpret_cast<uint32_t *>(take(rows * 4));
-    w.rank = reinterpret_cast<uint32_t *>(take(n * 4));
-    w.arrived = reinterpret_cast<uint32_t *>(take(n * 4));
+    if (!small) {
+        w.cnt = reinterpret_cast<uint32_t *>(take(rows * 4));
+        w.zero_bytes = at;
+        w.start = reinterpret_cast<uint32_t *>(take(rows * 4));
+        w.rank = reinterpret_cast<uint32_t *>(take(n * 4));
+        w.arrived = reinterpret_cast<uint32_t *>(take(n * 4));
+        w.long_row = reinterpret_cast<uint32_t *>(take(max_long(n) * 4));
+    }
     w.list = reinterpret_cast<uint32_t *>(take(n * 4));
-    w.long_row = reinterpret_cast<uint32_t *>(take(max_long(n) * 4));
-    w.long_chunk = reinterpret_cast<uint32_t *>(take(max_long(n) * 4));
-    w.chunk_row = reinterpret_cast<uint32_t *>(take(max_chunks(n) * 4));
-    w.partial = reinterpret_cast<float *>(take(max_chunks(n) * ((dim + 3) / 4 * 4) * 4));
+    w.big_room = uint32_t(max_big(n));
+    w.items = reinterpret_cast<Item *>(take((max_big(n) + max_items(n, rows)) * sizeof(Item)));
+    w.done = reinterpret_cast<uint32_t *>(take(max_slots(n) * max_slabs(dim) * 4));
+    w.partial = reinterpret_cast<float *>(take(max_slots(n) * w.partial_stride * 4));
     w.bytes = at;
     return w;
 }
@@ -165,7 +229,7 @@ GradWork layout(void *workspace, size_t rows, size_t dim, size_t n)
 __global__ void __launch_bounds__(kThreads) rd_embed_count_kernel(const void *__restrict__ ids, bool wide, long long first, size_t rows, uint32_t n,
                                                                   uint32_t *__restrict__ cnt, uint32_t *__restrict__ rank)
 {
-    pdl_start();
+    pdl_wait_first();
     const uint32_t i = blockIdx.x * kThreads + threadIdx.x;
     const long long r = i < n ? row_of(ids, wide, i, first, rows) : -1;
     // lanes with the same row count together: one atomic each
@@ -178,45 +242,97 @@ __global__ void __launch_bounds__(kThreads) rd_embed_count_kernel(const void *__
     if (i < n) rank[i] = base + __popc(peers & ((1u << lane) - 1));
 }
 
-// Hands every row a range of the token list: the ranges of a thread block's rows follow each other.
-__global__ void __launch_bounds__(1024) rd_embed_ranges_kernel(const uint32_t *__restrict__ cnt, uint32_t *__restrict__ start, size_t rows, GradMeta *meta,
-                                                               uint32_t *__restrict__ long_row, uint32_t *__restrict__ long_chunk, uint32_t *__restrict__ chunk_row)
+// Inclusive sum over a thread block of 1024; `total` is the whole block's.  Two barriers; `shared` has 33 words.
+__device__ __forceinline__ uint32_t block_sum(uint32_t x, uint32_t *shared, uint32_t &total)
 {
-    pdl_start();
-    __shared__ uint32_t warp_sum[32];
-    __shared__ uint32_t block_base;
-    const size_t v = size_t(blockIdx.x) * 1024 + threadIdx.x;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const uint32_t c = v < rows ? cnt[v] : 0;
-    uint32_t incl = c;
 #pragma unroll
     for (int d = 1; d < 32; d *= 2) {
-        const uint32_t o = __shfl_up_sync(0xffffffffu, incl, d);
-        if (lane >= d) incl += o;
+        const uint32_t o = __shfl_up_sync(0xffffffffu, x, d);
+        if (lane >= d) x += o;
     }
-    if (lane == 31) warp_sum[warp] = incl;
     __syncthreads();
-    if (warp == 0) {
-        uint32_t s = warp_sum[lane];
+    if (lane == 31) shared[warp] = x;
+    __syncthreads();
+    uint32_t s = shared[lane];
 #pragma unroll
-        for (int d = 1; d < 32; d *= 2) {
-            const uint32_t o = __shfl_up_sync(0xffffffffu, s, d);
-            if (lane >= d) s += o;
-        }
-        warp_sum[lane] = s;
-        if (lane == 31) block_base = s ? atomicAdd(&meta->list_used, s) : 0;
+    for (int d = 1; d < 32; d *= 2) {
+        const uint32_t o = __shfl_up_sync(0xffffffffu, s, d);
+        if (lane >= d) s += o;
+    }
+    total = __shfl_sync(0xffffffffu, s, 31);
+    const uint32_t before = __shfl_sync(0xffffffffu, s, warp ? warp - 1 : 0);
+    return x + (warp ? before : 0);
+}
+
+// Hands every row a range of the token list, its items and their partial rows: those of a thread block's rows follow each other.
+__global__ void __launch_bounds__(1024) rd_embed_ranges_kernel(GradWork w, size_t rows, uint32_t slabs)
+{
+    __shared__ uint32_t shared[32];
+    __shared__ uint32_t bases[3];
+    pdl_start();
+    const size_t v = size_t(blockIdx.x) * 1024 + threadIdx.x;
+    const uint32_t c = v < rows ? w.cnt[v] : 0;
+    const uint32_t parts = (c + kChunk - 1) / kChunk;
+    const uint32_t last = c - (parts ? parts - 1 : 0) * kChunk;          // tokens of the last part; the others have kChunk
+    const uint32_t n_big = parts ? parts - (last <= kBigItem) : 0;
+    uint32_t all_tokens, all_big, all_items;
+    const uint32_t tokens = block_sum(c, shared, all_tokens) - c;
+    const uint32_t big = block_sum(n_big, shared, all_big) - n_big;
+    const uint32_t items = block_sum(parts - n_big, shared, all_items) - (parts - n_big);
+    if (threadIdx.x == 0) {
+        bases[0] = all_tokens ? atomicAdd(&w.meta->list_used, all_tokens) : 0;
+        bases[1] = all_big ? atomicAdd(&w.meta->n_big, all_big) : 0;
+        bases[2] = all_items ? atomicAdd(&w.meta->n_items, all_items) : 0;
     }
     __syncthreads();
-    if (v >= rows) return;
-    start[v] = block_base + (warp ? warp_sum[warp - 1] : 0) + incl - c;
-    if (c > kChunk) {
-        const uint32_t k = atomicAdd(&meta->n_long, 1u);
-        const uint32_t chunks = (c + kChunk - 1) / kChunk;
-        const uint32_t b = atomicAdd(&meta->n_chunks, chunks);
-        long_row[k] = uint32_t(v);
-        long_chunk[k] = b;
-        for (uint32_t j = 0; j < chunks; j++) chunk_row[b + j] = k;
+    if (c == 0) return;
+    const uint32_t begin = bases[0] + tokens;
+    w.start[v] = begin;
+    for (uint32_t k = 0; k < n_big; k++) w.items[bases[1] + big + k] = Item{uint32_t(v), begin + k * kChunk, min(kChunk, c - k * kChunk), k, parts, 0};
+    if (n_big < parts) w.items[w.big_room + bases[2] + items] = Item{uint32_t(v), begin + n_big * kChunk, last, n_big, parts, 0};
+    if (parts > 1) {
+        w.long_row[atomicAdd(&w.meta->n_long, 1u)] = uint32_t(v);
+        for (uint32_t k = 0; k < slabs; k++) w.done[size_t(slot_of(begin, 0)) * slabs + k] = 0;
     }
+}
+
+// All of it for few tokens: a warp per token counts over all of them.
+__global__ void __launch_bounds__(1024) rd_embed_rank_kernel(const void *__restrict__ ids, bool wide, long long first, size_t rows, uint32_t n, GradWork w, uint32_t slabs)
+{
+    __shared__ __align__(16) uint32_t row[kSmallTokens];
+    pdl_wait_first();
+    const int lane = threadIdx.x & 31;
+    const uint32_t padded = (n + 127) / 128 * 128, i = blockIdx.x * 32 + (threadIdx.x >> 5);
+    for (uint32_t k = threadIdx.x; k < padded; k += 1024) {
+        const long long r = k < n ? row_of(ids, wide, k, first, rows) : -1;
+        row[k] = r >= 0 ? uint32_t(r) : 0xffffffffu;          // tokens of other slices come last
+    }
+    __syncthreads();
+    if (blockIdx.x == 0 && threadIdx.x == 0) *w.meta = GradMeta{0, 0, n, 0};
+    if (i >= n) return;
+    const uint32_t mine = row[i];
+    uint32_t lower = 0, same = 0, before = 0;
+    for (uint32_t k = 4 * lane; k < padded; k += 128) {
+        const uint4 x = *reinterpret_cast<const uint4 *>(row + k);
+        const uint32_t v[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+        for (int u = 0; u < 4; u++) {
+            lower += v[u] < mine;
+            same += v[u] == mine;
+            before += v[u] == mine && k + u < i;
+        }
+    }
+    lower = __reduce_add_sync(0xffffffffu, lower);
+    same = __reduce_add_sync(0xffffffffu, same);
+    before = __reduce_add_sync(0xffffffffu, before);
+    if (lane) return;
+    const uint32_t at = lower + before, parts = (same + kChunk - 1) / kChunk;
+    const bool here = mine != 0xffffffffu, opens = here && before % kChunk == 0;
+    if (here) w.list[at] = i;
+    w.items[at] = Item{mine, at, opens ? min(kChunk, same - before) : 0, before / kChunk, parts, 0};
+    if (opens && before == 0 && parts > 1)
+        for (uint32_t k = 0; k < slabs; k++) w.done[size_t(slot_of(at, 0)) * slabs + k] = 0;
 }
 
 __global__ void __launch_bounds__(kThreads) rd_embed_place_kernel(const void *__restrict__ ids, bool wide, long long first, size_t rows, uint32_t n,
@@ -291,24 +407,27 @@ __global__ void __launch_bounds__(kThreads) rd_embed_sort_kernel(const void *__r
     }
 }
 
-// Sum over list[0..c) of the V values at column j, in list order; four rows in flight.
+// Sum over c tokens of the V values at column col, in order, four of them in flight.  The tokens are in the lanes
+// of the warp (token t in lane t) or, for groups narrower than a warp, in list.
 template <typename T, int V>
-__device__ __forceinline__ void add_rows(const T *__restrict__ grad, size_t stride, size_t col, const uint32_t *__restrict__ list, uint32_t c, float (&acc)[V])
+__device__ __forceinline__ void add_rows(const T *__restrict__ grad, size_t stride, uint32_t token, const uint32_t *__restrict__ list, uint32_t c, float (&acc)[V])
 {
+    constexpr int U = 4;
+    auto row = [&](uint32_t t) { return load<T, V>(grad + size_t(list ? list[t] : __shfl_sync(0xffffffffu, token, t)) * stride); };
 #pragma unroll
     for (int k = 0; k < V; k++) acc[k] = 0.0f;
     uint32_t t = 0;
-    for (; t + 4 <= c; t += 4) {
-        Vec<T, V> x[4];
+    for (; t + U <= c; t += U) {
+        Vec<T, V> x[U];
 #pragma unroll
-        for (int u = 0; u < 4; u++) x[u] = load<T, V>(grad + size_t(list[t + u]) * stride + col);
+        for (int u = 0; u < U; u++) x[u] = row(t + u);
 #pragma unroll
-        for (int u = 0; u < 4; u++)
+        for (int u = 0; u < U; u++)
 #pragma unroll
             for (int k = 0; k < V; k++) acc[k] += widen<T>(x[u].v[k]);
     }
     for (; t < c; t++) {
-        const Vec<T, V> x = load<T, V>(grad + size_t(list[t]) * stride + col);
+        const Vec<T, V> x = row(t);
 #pragma unroll
         for (int k = 0; k < V; k++) acc[k] += widen<T>(x.v[k]);
     }
@@ -329,124 +448,242 @@ __device__ __forceinline__ void write_row(O *p, const float (&acc)[V], float sca
     store<O, V>(p, y);
 }
 
-// `lanes` (a power of two) threads share a row; thread blocks from row_blocks on take chunks of rows with many tokens.
+// `lanes` threads (a power of two, within a warp) work on an item and a slab of lanes * V columns.  An item, its tokens and their
+// rows are three loads that depend on each other; the item after the next one and the next one's tokens are on their way
+// while a group adds up the rows of the present one.
 template <typename T, typename O, int V>
-__global__ void __launch_bounds__(kThreads) rd_embed_sum_kernel(const T *__restrict__ grad, size_t grad_stride, O *__restrict__ table, size_t table_stride, size_t rows,
-                                                                uint32_t vecs, uint32_t lanes, float scale, bool accumulate, GradWork w, uint32_t row_blocks)
+__global__ void __launch_bounds__(kThreads, 3) rd_embed_sum_kernel(const T *__restrict__ grad, size_t grad_stride, O *__restrict__ table, size_t table_stride, uint32_t vecs,
+                                                                uint32_t lanes, uint32_t slabs, float scale, bool accumulate, GradWork w)
 {
     pdl_start();
     const uint32_t per_block = kThreads / lanes, lane = threadIdx.x % lanes, group = threadIdx.x / lanes;
-    if (blockIdx.x < row_blocks) {
-        const size_t v = size_t(blockIdx.x) * per_block + group;
-        if (v >= rows) return;
-        const uint32_t c = w.cnt[v];
-        if (c > kChunk || (accumulate && c == 0)) return;
-        const uint32_t *list = c ? w.list + w.start[v] : w.list;
-        for (uint32_t j = lane; j < vecs; j += lanes) {
+    const uint32_t mask = (lanes == 32 ? 0xffffffffu : (1u << lanes) - 1) << (threadIdx.x % 32 / lanes * lanes);     // the group within its warp
+    const uint32_t n_big = w.meta->n_big, others = w.big_room - n_big;
+    const uint64_t units = (uint64_t(n_big) + w.meta->n_items) * slabs, step = uint64_t(gridDim.x) * per_block;
+    const bool by_lane = lanes == 32;
+    auto item = [&](uint64_t u) {
+        if (u >= units) return Item{};
+        const size_t k = u / slabs;
+        return w.items[k < n_big ? k : k + others];
+    };
+    auto tokens = [&](const Item &it) { return by_lane && lane < it.count ? w.list[it.begin + lane] : 0; };
+    uint64_t u = uint64_t(blockIdx.x) * per_block + group;
+    Item it = item(u), next = item(u + step);
+    uint32_t token = tokens(it);
+    for (; u < units; u += step) {
+        const Item after = item(u + 2 * step);
+        const uint32_t next_token = tokens(next);
+        if (it.count) {
+            const uint32_t slab = uint32_t(u % slabs), j = slab * lanes + lane;
+            const bool mine = j < vecs;
+            const size_t col = mine ? size_t(j) * V : 0;          // lanes beyond the row read its beginning and write nothing
             float acc[V];
-            add_rows<T, V>(grad, grad_stride, size_t(j) * V, list, c, acc);
-            write_row<O, V>(table + v * table_stride + size_t(j) * V, acc, scale, accumulate);
-        }
-        return;
-    }
-    const uint32_t n_chunks = w.meta->n_chunks;
-    for (uint32_t q = (blockIdx.x - row_blocks) * per_block + group; q < n_chunks; q += (gridDim.x - row_blocks) * per_block) {
-        const uint32_t k = w.chunk_row[q], v = w.long_row[k], part = q - w.long_chunk[k];
-        const uint32_t left = w.cnt[v] - part * kChunk, c = left < kChunk ? left : kChunk;
-        const uint32_t *list = w.list + w.start[v] + part * kChunk;
-        for (uint32_t j = lane; j < vecs; j += lanes) {
-            float acc[V];
-            add_rows<T, V>(grad, grad_stride, size_t(j) * V, list, c, acc);
-            float *p = w.partial + size_t(q) * ((size_t(vecs) * V + 3) / 4 * 4) + size_t(j) * V;
+            add_rows<T, V>(grad + col, grad_stride, token, by_lane ? nullptr : w.list + it.begin, it.count, acc);
+            O *out = table + size_t(it.row) * table_stride + col;
+            if (it.parts == 1) {
+                if (mine) write_row<O, V>(out, acc, scale, accumulate);
+            } else {
+                // a row of several items: whichever group is last adds the partial rows up, in order
+                const uint32_t begin = it.begin - it.part * kChunk;
+                float *partial = w.partial + col;
+                if (mine) {
+                    Vec<float, V> x;
 #pragma unroll
-            for (int e = 0; e < V; e++) p[e] = acc[e];
+                    for (int e = 0; e < V; e++) x.v[e] = acc[e];
+                    store<float, V>(partial + size_t(slot_of(begin, it.part)) * w.partial_stride, x);
+                }
+                __threadfence();
+                __syncwarp(mask);
+                uint32_t finished = lane == 0 ? atomicAdd(&w.done[size_t(slot_of(begin, 0)) * slabs + slab], 1u) + 1 : 0;
+                finished = __shfl_sync(mask, finished, 0, lanes);
+                if (finished == it.parts && mine) {
+                    __threadfence();
+#pragma unroll
+                    for (int e = 0; e < V; e++) acc[e] = 0.0f;
+#pragma unroll 2
+                    for (uint32_t k = 0; k < it.parts; k++) {
+                        const Vec<float, V> x = load<float, V>(partial + size_t(slot_of(begin, k)) * w.partial_stride);
+#pragma unroll
+                        for (int e = 0; e < V; e++) acc[e] += x.v[e];
+                    }
+                    write_row<O, V>(out, acc, scale, accumulate);
+                }
+            }
         }
+        it = next;
+        next = after;
+        token = next_token;
     }
 }
 
-template <typename O>
-__global__ void __launch_bounds__(kThreads) rd_embed_join_kernel(O *__restrict__ table, size_t table_stride, uint32_t dim, float scale, bool accumulate, GradWork w)
+// Zeros.  Thread blocks of a plain grid write 16 KB each, one after the other in memory: at 7.4 TB/s against 6.3 TB/s when the
+// blocks of a resident grid stride over the table (1 GiB, B200), whose stores drift apart.
+constexpr uint32_t kFillBytes = 16384;
+
+__device__ __forceinline__ void fill_span(char *p, size_t bytes, uint32_t t, uint32_t threads)
 {
-    pdl_start();
-    const uint32_t n_long = w.meta->n_long;
-    const size_t stride = (size_t(dim) + 3) / 4 * 4;
-    const uint32_t slabs = (dim + kThreads - 1) / kThreads;
-    for (uint64_t u = blockIdx.x; u < uint64_t(n_long) * slabs; u += gridDim.x) {
-        const uint32_t q = uint32_t(u / slabs), j = uint32_t(u % slabs) * kThreads + threadIdx.x;
-        if (j >= dim) continue;
-        const uint32_t v = w.long_row[q], chunks = (w.cnt[v] + kChunk - 1) / kChunk;
-        const float *p = w.partial + size_t(w.long_chunk[q]) * stride + j;
-        float acc[1] = {0.0f};
-        uint32_t k = 0;
-        for (; k + 8 <= chunks; k += 8) {
-            float x[8];
-#pragma unroll
-            for (int e = 0; e < 8; e++) x[e] = p[size_t(k + e) * stride];
-#pragma unroll
-            for (int e = 0; e < 8; e++) acc[0] += x[e];
-        }
-        for (; k < chunks; k++) acc[0] += p[size_t(k) * stride];
-        write_row<O, 1>(table + size_t(v) * table_stride + j, acc, scale, accumulate);
+    // single elements up to a 32-byte boundary and behind the last one
+    const size_t head = (32 - reinterpret_cast<uintptr_t>(p) % 32) % 32, h = head < bytes ? head : bytes;
+    for (size_t i = 2 * t; i < h; i += 2 * threads) *reinterpret_cast<uint16_t *>(p + i) = 0;
+    p += h;
+    bytes -= h;
+    const size_t wide = bytes / 32 * 32;
+    for (size_t i = size_t(t) * 32; i < wide; i += size_t(threads) * 32)
+        asm volatile("st.global.v8.b32 [%0], {%1, %1, %1, %1, %1, %1, %1, %1};" ::"l"(p + i), "r"(0) : "memory");
+    for (size_t i = wide + 2 * t; i < bytes; i += 2 * threads) *reinterpret_cast<uint16_t *>(p + i) = 0;
+}
+
+// span > 0: the table is one piece of memory of that many bytes.  Otherwise rows of row_bytes, pitch apart, a warp each.
+// Only the last thread block waits for the kernels before: what comes after this kernel then comes after them too.  That the
+// stream's earlier work is done is known from the first of them, which waits for it before it lets anything follow.
+__global__ void __launch_bounds__(kThreads) rd_embed_fill_kernel(char *__restrict__ table, size_t span, size_t rows, size_t row_bytes, size_t pitch, bool alone)
+{
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    if (alone || blockIdx.x == gridDim.x - 1) asm volatile("griddepcontrol.wait;" ::: "memory");
+    if (span) {
+        const size_t from = size_t(blockIdx.x) * kFillBytes;
+        // cut at addresses that are multiples of 32 bytes
+        const size_t skew = reinterpret_cast<uintptr_t>(table) % 32;
+        const size_t begin = blockIdx.x ? from - skew : 0, end = from + kFillBytes - skew;
+        if (begin < span) fill_span(table + begin, (end < span ? end : span) - begin, threadIdx.x, kThreads);
+    } else {
+        const size_t row = size_t(blockIdx.x) * (kThreads / 32) + threadIdx.x / 32;
+        if (row < rows) fill_span(table + row * pitch, row_bytes, threadIdx.x % 32, 32);
     }
 }
+
+// A stream and two events of the library's own per device, made on the first call that wants them and kept.  Calls take turns to
+// enqueue, so the events always stand for the call that holds the lock.
+struct Lane {
+    bool tried = false, ready = false;
+    cudaStream_t side = nullptr;
+    cudaEvent_t fork = nullptr, join = nullptr;
+};
+constexpr int kMaxDevices = 64;
+Lane g_lane[kMaxDevices];
+std::mutex g_lane_mutex;
+
+// Null where the sort has to stay on the caller's stream: no such stream to be had, or the call is being recorded into a graph.
+Lane *lane_for(cudaStream_t stream)
+{
+    int device = 0;
+    cudaStreamCaptureStatus capture = cudaStreamCaptureStatusNone;
+    if (cudaGetDevice(&device) != cudaSuccess || device >= kMaxDevices) return nullptr;
+    if (cudaStreamIsCapturing(stream, &capture) != cudaSuccess || capture != cudaStreamCaptureStatusNone) return nullptr;
+    Lane &l = g_lane[device];
+    if (!l.tried) {
+        l.tried = true;
+        // of the highest priority: its few thread blocks go ahead of the many of the fill that are queued already
+        int lowest = 0, highest = 0;
+        l.ready = cudaDeviceGetStreamPriorityRange(&lowest, &highest) == cudaSuccess &&
+                  cudaStreamCreateWithPriority(&l.side, cudaStreamNonBlocking, highest) == cudaSuccess && cudaEventCreateWithFlags(&l.fork, cudaEventDisableTiming) == cudaSuccess &&
+                  cudaEventCreateWithFlags(&l.join, cudaEventDisableTiming) == cudaSuccess;
+        if (!l.ready) (void)cudaGetLastError();
+    }
+    return l.ready ? &l : nullptr;
+}
+
+// The work list of more than kSmallTokens tokens.
+cudaError_t launch_sort(const EmbedGradArgs &a, const GradWork &w, uint32_t slabs, cudaStream_t stream)
+{
+    const uint32_t n = uint32_t(a.n);
+    const unsigned token_blocks = (n + kThreads - 1) / kThreads;
+    const unsigned long_blocks = unsigned(max_long(n) < 296 ? max_long(n) : 296);
+    cudaError_t e = cudaMemsetAsync(a.workspace, 0, w.zero_bytes, stream);
+    if (e == cudaSuccess) e = launch(rd_embed_count_kernel, token_blocks, kThreads, stream, a.ids, a.wide_ids, a.first_row, a.rows, n, w.cnt, w.rank);
+    if (e == cudaSuccess) e = launch(rd_embed_ranges_kernel, unsigned((a.rows + 1023) / 1024), 1024, stream, w, a.rows, slabs);
+    if (e == cudaSuccess) e = launch(rd_embed_place_kernel, token_blocks, kThreads, stream, a.ids, a.wide_ids, a.first_row, a.rows, n, w.start, w.rank, w.arrived);
+    if (e == cudaSuccess)
+        e = launch(rd_embed_sort_kernel, token_blocks + long_blocks, kThreads, stream, a.ids, a.wide_ids, a.first_row, a.rows, n, w.cnt, w.start, w.arrived, w.list, w.meta,
+                   w.long_row, token_blocks);
+    return e;
+}
+
+// `alone`: nothing of the call before it has waited for the stream's earlier work.
+template <typename O> cudaError_t launch_fill(const EmbedGradArgs &a, bool alone)
+{
+    const size_t row_bytes = a.dim * sizeof(O), pitch = a.table_stride * sizeof(O);
+    const size_t span = pitch == row_bytes || a.rows == 1 ? a.rows * row_bytes : 0;
+    const size_t blocks = span ? (span + 31) / kFillBytes + 1 : (a.rows + kThreads / 32 - 1) / (kThreads / 32);
+    if (blocks > 0x7fffffffu) return cudaErrorInvalidConfiguration;
+    return launch(rd_embed_fill_kernel, unsigned(blocks), kThreads, a.stream, static_cast<char *>(a.table), span, a.rows, row_bytes, pitch, alone);
+}
+
+// From this size of table on the fork pays: the sort takes some 20 us, a fork and a join a few.
+constexpr size_t kForkBytes = size_t(32) << 20;
 
 template <typename T, typename O, int V> cudaError_t launch_grad(const EmbedGradArgs &a)
 {
     const GradWork w = layout(a.workspace, a.rows, a.dim, a.n);
     const uint32_t n = uint32_t(a.n);
-    cudaError_t e = cudaMemsetAsync(a.workspace, 0, w.zero_bytes, a.stream);
-    if (e != cudaSuccess) return e;
-    const unsigned token_blocks = (n + kThreads - 1) / kThreads;
-    const unsigned long_blocks = unsigned(max_long(n) < 296 ? max_long(n) : 296);
-    if (n) {
-        e = launch(rd_embed_count_kernel, token_blocks, kThreads, a.stream, a.ids, a.wide_ids, a.first_row, a.rows, n, w.cnt, w.rank);
-        if (e != cudaSuccess) return e;
-        e = launch(rd_embed_ranges_kernel, unsigned((a.rows + 1023) / 1024), 1024, a.stream, w.cnt, w.start, a.rows, w.meta, w.long_row, w.long_chunk, w.chunk_row);
-        if (e != cudaSuccess) return e;
-        e = launch(rd_embed_place_kernel, token_blocks, kThreads, a.stream, a.ids, a.wide_ids, a.first_row, a.rows, n, w.start, w.rank, w.arrived);
-        if (e != cudaSuccess) return e;
-        e = launch(rd_embed_sort_kernel, token_blocks + long_blocks, kThreads, a.stream, a.ids, a.wide_ids, a.first_row, a.rows, n, w.cnt, w.start, w.arrived, w.list,
-                   w.meta, w.long_row, token_blocks);
-        if (e != cudaSuccess) return e;
+    const uint32_t vecs = uint32_t(a.dim / V), lanes = lanes_for(vecs), slabs = (vecs + lanes - 1) / lanes;
+    if (n == 0) return a.accumulate ? cudaSuccess : launch_fill<O>(a, true);
+    cudaError_t e = cudaSuccess;
+    if (n <= kSmallTokens) {
+        e = launch(rd_embed_rank_kernel, (n + 31) / 32, 1024, a.stream, a.ids, a.wide_ids, a.first_row, a.rows, n, w, slabs);
+        if (e == cudaSuccess && !a.accumulate) e = launch_fill<O>(a, false);
+    } else {
+        std::unique_lock<std::mutex> hold(g_lane_mutex, std::defer_lock);
+        Lane *lane = nullptr;
+        if (!a.accumulate && a.rows * a.dim * sizeof(O) >= kForkBytes) {
+            hold.lock();
+            lane = lane_for(a.stream);
+        }
+        if (lane) {
+            e = cudaEventRecord(lane->fork, a.stream);
+            if (e == cudaSuccess) e = cudaStreamWaitEvent(lane->side, lane->fork, 0);
+            if (e != cudaSuccess) return e;
+            e = launch_sort(a, w, slabs, lane->side);
+            const cudaError_t f = launch_fill<O>(a, true);
+            // joined whatever became of the launches: the caller's stream owns the workspace
+            const cudaError_t r = cudaEventRecord(lane->join, lane->side), j = r == cudaSuccess ? cudaStreamWaitEvent(a.stream, lane->join, 0) : r;
+            e = e != cudaSuccess ? e : f != cudaSuccess ? f : j;
+        } else {
+            e = launch_sort(a, w, slabs, a.stream);
+            if (e == cudaSuccess && !a.accumulate) e = launch_fill<O>(a, false);
+        }
     }
-    const uint32_t vecs = uint32_t(a.dim / V);
-    uint32_t lanes = 8;
-    while (lanes < uint32_t(kThreads) && lanes < vecs) lanes *= 2;
-    const size_t row_blocks = (a.rows + kThreads / lanes - 1) / (kThreads / lanes);
-    const size_t chunk_blocks = (max_chunks(n) + kThreads / lanes - 1) / (kThreads / lanes);
-    const unsigned extra = unsigned(chunk_blocks < 1184 ? chunk_blocks : 1184);
-    if (row_blocks + extra > 0x7fffffffu) return cudaErrorInvalidConfiguration;
-    e = launch(rd_embed_sum_kernel<T, O, V>, unsigned(row_blocks) + extra, kThreads, a.stream, static_cast<const T *>(a.grad), a.grad_stride, static_cast<O *>(a.table),
-               a.table_stride, a.rows, vecs, lanes, a.scale, a.accumulate, w, uint32_t(row_blocks));
-    if (e != cudaSuccess || !long_blocks) return e;
-    return launch(rd_embed_join_kernel<O>, 592, kThreads, a.stream, static_cast<O *>(a.table), a.table_stride, uint32_t(a.dim), a.scale, a.accumulate, w);
+    if (e != cudaSuccess) return e;
+    const uint64_t units = uint64_t(max_big(n) + max_items(n, a.rows)) * slabs, blocks = (units + kThreads / lanes - 1) / (kThreads / lanes);
+    return launch(rd_embed_sum_kernel<T, O, V>, unsigned(blocks < kSumBlocks ? blocks : kSumBlocks), kThreads, a.stream, static_cast<const T *>(a.grad), a.grad_stride,
+                  static_cast<O *>(a.table), a.table_stride, vecs, lanes, slabs, a.scale, a.accumulate, w);
 }
 
-template <typename T, typename O, int V> cudaError_t pick_grad(const EmbedGradArgs &a)
+// Whole vectors of 32 or 16 bytes when both matrices' rows begin and end on such boundaries (lookup of 16384 rows of 8 KB, B200:
+// 35 us with 32-byte accesses, 39 with 16-byte ones), else single elements.
+template <typename T, typename O> cudaError_t pick_grad(const EmbedGradArgs &a)
 {
-    // whole vectors when the gradient's and the table's rows begin and end on 16-byte boundaries
-    if (vector_rows(a.grad, a.grad_stride, a.dim, sizeof(T)) && vector_rows(a.table, a.table_stride, a.dim, sizeof(O)) && a.dim % V == 0) return launch_grad<T, O, V>(a);
-    return launch_grad<T, O, 1>(a);
+    constexpr int V = 16 / sizeof(T);
+    auto fits = [&](size_t vec) {
+        const size_t to = vec * sizeof(O) < 32 ? vec * sizeof(O) : 32;
+        return vector_rows(a.grad, a.grad_stride, a.dim, sizeof(T), vec * sizeof(T)) && vector_rows(a.table, a.table_stride, a.dim, sizeof(O), to);
+    };
+    return fits(2 * V) ? launch_grad<T, O, 2 * V>(a) : fits(V) ? launch_grad<T, O, V>(a) : launch_grad<T, O, 1>(a);
+}
+
+template <typename T> cudaError_t pick_embed(const EmbedArgs &a)
+{
+    constexpr int V = 16 / sizeof(T);
+    auto fits = [&](size_t to) {
+        return vector_rows(a.table, a.table_stride, a.dim, sizeof(T), to) && vector_rows(a.out, a.out_stride, a.dim, sizeof(T), to);
+    };
+    return fits(32) ? launch_embed<T, 2 * V>(a) : fits(16) ? launch_embed<T, V>(a) : launch_embed<T, 1>(a);
 }
 
 }  // namespace
 
 cudaError_t embed_forward(const EmbedArgs &a)
 {
-    const size_t esize = a.dtype == RD_FP32 ? 4 : 2;
-    const bool wide = vector_rows(a.table, a.table_stride, a.dim, esize) && vector_rows(a.out, a.out_stride, a.dim, esize);
-    if (a.dtype == RD_FP32) return wide ? launch_embed<float, 4>(a) : launch_embed<float, 1>(a);
-    if (a.dtype == RD_BF16) return wide ? launch_embed<__nv_bfloat16, 8>(a) : launch_embed<__nv_bfloat16, 1>(a);
-    return wide ? launch_embed<__half, 8>(a) : launch_embed<__half, 1>(a);
+    return a.dtype == RD_FP32 ? pick_embed<float>(a) : a.dtype == RD_BF16 ? pick_embed<__nv_bfloat16>(a) : pick_embed<__half>(a);
 }
 
 size_t embed_backward_workspace(size_t rows, size_t dim, size_t n) { return layout(nullptr, rows, dim, n).bytes; }
 
 cudaError_t embed_backward(const EmbedGradArgs &a)
 {
-    if (a.dtype == RD_FP32) return pick_grad<float, float, 4>(a);
-    if (a.dtype == RD_BF16) return a.table_dtype == RD_FP32 ? pick_grad<__nv_bfloat16, float, 8>(a) : pick_grad<__nv_bfloat16, __nv_bfloat16, 8>(a);
-    return a.table_dtype == RD_FP32 ? pick_grad<__half, float, 8>(a) : pick_grad<__half, __half, 8>(a);
+    if (a.dtype == RD_FP32) return pick_grad<float, float>(a);
+    if (a.dtype == RD_BF16) return a.table_dtype == RD_FP32 ? pick_grad<__nv_bfloat16, float>(a) : pick_grad<__nv_bfloat16, __nv_bfloat16>(a);
+    return a.table_dtype == RD_FP32 ? pick_grad<__half, float>(a) : pick_grad<__half, __half>(a);
 }
 
 }  // namespace rd

@@ -14,6 +14,14 @@ __device__ __forceinline__ void pdl_start()
     asm volatile("griddepcontrol.wait;" ::: "memory");
 }
 
+// The same the other way round, for the first kernel of a call whose later ones include one that does not wait: nothing of the
+// call starts before the stream's earlier work is done.
+__device__ __forceinline__ void pdl_wait_first()
+{
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+}
+
 inline cudaLaunchAttribute pdl_attribute()
 {
     cudaLaunchAttribute a{};
