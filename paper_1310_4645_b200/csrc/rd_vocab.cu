@@ -260,21 +260,22 @@ struct alignas(64) MmaParams {
     CUtensorMap a_mn;         // dx as the transposed left operand of dw, 64 x 64 boxes
     CUtensorMap b_mn;         // weight as the transposed right operand of dh
     CUtensorMap b2_mn;        // packed hidden as the transposed right operand of dw
+    CUtensorMap dx_out;       // dx, 64 x 32 boxes
+    CUtensorMap dh_out;       // dh, 32 x 32 x 1 boxes
+    CUtensorMap dw_out;       // grad_weight, 64 x 32 boxes
     const Meta *meta;
     const int *label;
     const float *gp, *gt, *lse2;
     float2 *part;             // stats: (maximum, sum) in base 2, [packed row][half tile]
     float *target;            // stats: the label's logit, per packed row
-    uint16_t *dx;             // dlogits: packed rows x dx_stride
-    float *dh;                // grads: [split][packed row][dh_stride]
-    uint16_t *dw;
-    size_t dx_stride, dh_stride, dh_rows, dw_stride;
+    uint16_t *dw;             // grad_weight, for rows that TMA cannot address
+    size_t dh_stride, dw_stride;
     uint32_t parts;           // stats: half tiles per row
     uint32_t piece0, piece;   // first row of the piece and its rows
     uint32_t dim;
     uint32_t group;           // token tiles that go over the vocabulary together
     uint32_t splits;          // parts that the sum over the piece is cut into for dh
-    bool first_piece, want_dh, want_dw, dw_wide;
+    bool first_piece, want_dh, want_dw, dw_tma;
     float scale2;             // scale * log2(e)
     float scale;
 };
@@ -401,28 +402,55 @@ template <bool BF16> __device__ __forceinline__ uint32_t pack2(float lo, float h
     else asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
     return r;
 }
-__device__ __forceinline__ void store32(void *p, const uint32_t (&v)[8])
+__device__ __forceinline__ void tma_store(const CUtensorMap *map, uint32_t src, uint32_t x, uint32_t y)
 {
-    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7])
-                 : "memory");
+    asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.tile.bulk_group [%0, {%2, %3}], [%1];" ::"l"(map), "r"(src), "r"(x), "r"(y) : "memory");
 }
-__device__ __forceinline__ void load32(const void *p, float (&v)[8])
+__device__ __forceinline__ void tma_store(const CUtensorMap *map, uint32_t src, uint32_t x, uint32_t y, uint32_t z)
 {
-    asm volatile("ld.global.v8.f32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
-                 : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7])
-                 : "l"(p)
-                 : "memory");
+    asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.tile.bulk_group [%0, {%2, %3, %4}], [%1];" ::"l"(map), "r"(src), "r"(x), "r"(y), "r"(z) : "memory");
+}
+// Adds to what is there; every value is added to by one thread block per launch, so the order of additions is the launches'.
+__device__ __forceinline__ void tma_add(const CUtensorMap *map, uint32_t src, uint32_t x, uint32_t y, uint32_t z)
+{
+    asm volatile("cp.reduce.async.bulk.tensor.3d.global.shared::cta.add.tile.bulk_group [%0, {%2, %3, %4}], [%1];" ::"l"(map), "r"(src), "r"(x), "r"(y), "r"(z) : "memory");
+}
+// 16 bytes of a box of 32 rows of 128 bytes, in the places the 128-byte swizzle gives them.
+__device__ __forceinline__ void box_put(uint32_t box, int row, int unit, uint32_t a, uint32_t b, uint32_t c, uint32_t d)
+{
+    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(box + row * 128 + ((unit ^ (row & 7)) * 16)), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
 }
 
 // CG thread blocks (one, or a pair) compute a tile of 128 * CG x 256 together: each has 128 rows of the left operand and of the
 // accumulators, and 256 / CG rows of the right operand.
 constexpr int kRowsM = 128;
-template <int CG> struct Shape {
+// Results leave through one box of 4 KB per epilogue warp, except the softmax statistics, which have the room for another stage.
+constexpr uint32_t kBox = 4096;
+template <int KIND, int CG> struct Shape {
     static constexpr int tile_m = kRowsM * CG, rows_n = kTileN / CG;
     static constexpr uint32_t stage_a = kRowsM * kTileK * 2, stage_b = rows_n * kTileK * 2, stage = stage_a + stage_b;
-    static constexpr int stages = CG == 2 ? 6 : 4;
-    static constexpr uint32_t smem = stages * stage + 1024 + 256;
+    static constexpr int stages = CG == 1 ? 4 : KIND == kStats ? 7 : 6;
+    static constexpr uint32_t boxes = KIND == kStats ? 0 : kEpilogueWarps * kBox, smem = stages * stage + boxes + 1024 + 256;
 };
+
+constexpr uint32_t kTileOverhead = 2;     // what a tile costs besides its products, in steps of the summed index
+
+// A warp's box: wait until its last contents have left (unless this is the second half of the present ones); then, when it is
+// full, make the writes visible to the copy and say whether this lane issues it.
+__device__ __forceinline__ void box_wait(int lane, bool second_half)
+{
+    if (second_half) return;
+    if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+    __syncwarp();
+}
+__device__ __forceinline__ bool box_full(int lane, bool full)
+{
+    if (!full) return false;
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    __syncwarp();
+    return lane == 0;
+}
+__device__ __forceinline__ void box_sent() { asm volatile("cp.async.bulk.commit_group;" ::: "memory"); }
 
 // One unit of work: an output tile and the range of the summed index that goes into it.
 struct Work {
@@ -430,47 +458,60 @@ struct Work {
     uint32_t m0, n0, k0, kblocks, split;
 };
 
+// Which units of work a group of thread blocks (one or a pair, number c of g) gets: unit(0), unit(1), ... until it says no.
+// Gradients: the units of dh first, dealt out in turn; their number need not divide by g, so some groups get one more of them,
+// and that many fewer of dw's tiles, by the number of steps of the summed index.
 template <int KIND, int CG> struct Plan {
-    static constexpr uint32_t kTileM = Shape<CG>::tile_m;
-    uint32_t tiles_m, tiles_n, group;                 // logits
-    uint32_t dh_n, dh_tiles, dh_units, k_per_split, k_piece;   // dh
-    uint32_t dw_tiles, k_tokens;                      // dw
-    uint32_t units;
+    static constexpr uint32_t kTileM = Shape<KIND, CG>::tile_m;
+    const MmaParams &p;
+    uint32_t c, g;
+    uint32_t tiles_m, tiles_n;                                 // logits
+    uint32_t dh_n, dh_tiles, k_per_split, k_piece, dh_mine, dh_more;    // dh
+    uint32_t dw_tiles, k_tokens, dw_even;                      // dw
 
-    __device__ __forceinline__ Plan(const MmaParams &p, uint32_t m)
+    __device__ __forceinline__ Plan(const MmaParams &params, uint32_t m) : p(params), c(blockIdx.x / CG), g(gridDim.x / CG)
     {
         tiles_m = (m + kTileM - 1) / kTileM;
-        group = p.group;
         if (KIND != kGrads) {
             tiles_n = (p.piece + kTileN - 1) / kTileN;
-            units = tiles_m * tiles_n;
         } else {
             dh_n = (p.dim + kTileN - 1) / kTileN;
             k_piece = (p.piece + kTileK - 1) / kTileK;
             k_per_split = (k_piece + p.splits - 1) / p.splits;
             dh_tiles = tiles_m * dh_n;
-            dh_units = p.want_dh ? dh_tiles * p.splits : 0;
             k_tokens = (m + kTileK - 1) / kTileK;
             dw_tiles = p.want_dw ? (p.piece + kTileM - 1) / kTileM * dh_n : 0;
-            units = dh_units + dw_tiles;
+            const uint32_t dh_units = p.want_dh ? dh_tiles * p.splits : 0;
+            dh_more = dh_units % g;                            // groups with one more unit of dh
+            dh_mine = dh_units / g + (c < dh_more);
+            // a unit of dh is worth this many tiles of dw, which the other groups take first
+            const uint32_t worth = dh_more ? (2 * (k_per_split + kTileOverhead) + k_tokens) / (2 * (k_tokens + kTileOverhead)) : 0;
+            const uint32_t ahead = worth * (g - dh_more);
+            dw_even = dw_tiles > ahead ? (dw_tiles - ahead + g - 1) / g : 0;      // turns that every group takes part in
         }
     }
-    __device__ __forceinline__ Work at(uint32_t u, const MmaParams &p) const
+    __device__ __forceinline__ bool unit(uint32_t i, Work &w) const
     {
-        Work w;
         if (KIND != kGrads) {
-            const uint32_t per = group * tiles_n, g = u / per, in = u - g * per;
-            const uint32_t wide = min(group, tiles_m - g * group);
-            w = Work{0, (g * group + in % wide) * kTileM, in / wide * kTileN, 0, (p.dim + kTileK - 1) / kTileK, 0};
-        } else if (u < dh_units) {
-            const uint32_t s = u / dh_tiles, t = u - s * dh_tiles;
+            const uint32_t u = c + i * g;
+            if (u >= tiles_m * tiles_n) return false;
+            const uint32_t per = p.group * tiles_n, band = u / per, in = u - band * per;
+            const uint32_t wide = min(p.group, tiles_m - band * p.group);
+            w = Work{0, (band * p.group + in % wide) * kTileM, in / wide * kTileN, 0, (p.dim + kTileK - 1) / kTileK, 0};
+            return true;
+        }
+        if (i < dh_mine) {
+            const uint32_t u = c + i * g, s = u / dh_tiles, t = u - s * dh_tiles;
             const uint32_t k0 = s * k_per_split, k1 = min(k0 + k_per_split, k_piece);
             w = Work{1, t / dh_n * kTileM, t % dh_n * kTileN, k0 * kTileK, k1 > k0 ? k1 - k0 : 0, s};
-        } else {
-            const uint32_t t = u - dh_units;
-            w = Work{2, t / dh_n * kTileM, t % dh_n * kTileN, 0, k_tokens, 0};
+            return true;
         }
-        return w;
+        i -= dh_mine;
+        if (i >= dw_even && c < dh_more) return false;
+        const uint32_t t = i < dw_even ? c + i * g : dw_even * g + (i - dw_even) * (g - dh_more) + (c - dh_more);
+        if (t >= dw_tiles) return false;
+        w = Work{2, t / dh_n * kTileM, t % dh_n * kTileN, 0, k_tokens, 0};
+        return true;
     }
 };
 
@@ -486,15 +527,15 @@ template <int CG> __device__ __forceinline__ void pair_sync()
 template <int KIND, bool BF16, int CG>
 __global__ void __launch_bounds__(kMmaThreads, 1) rd_vocab_mma_kernel(const __grid_constant__ MmaParams p)
 {
-    using S = Shape<CG>;
+    using S = Shape<KIND, CG>;
     constexpr int kStages = S::stages;
     extern __shared__ unsigned char smem_raw[];
     const uint32_t smem = (smem_addr(smem_raw) + 1023) & ~1023u;
-    const uint32_t bars = smem + kStages * S::stage;
+    const uint32_t boxes = smem + kStages * S::stage, bars = boxes + S::boxes;
     // barriers: full[stage], empty[stage], accumulator full[2], empty[2]; then the tensor memory address
     const uint32_t full = bars, empty = bars + 8 * kStages, acc_full = bars + 16 * kStages, acc_empty = acc_full + 16, tmem_slot = acc_empty + 16;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const uint32_t rank = CG == 2 ? blockIdx.x & 1 : 0, first_unit = blockIdx.x / CG, unit_step = gridDim.x / CG;
+    const uint32_t rank = CG == 2 ? blockIdx.x & 1 : 0;
 
     if (threadIdx.x == 0) {
         for (int s = 0; s < kStages; s++) {
@@ -530,8 +571,8 @@ __global__ void __launch_bounds__(kMmaThreads, 1) rd_vocab_mma_kernel(const __gr
     if (warp == 0) {
         if (lane == 0) {
             uint32_t it = 0;
-            for (uint32_t u = first_unit; u < plan.units && !dead; u += unit_step) {
-                const Work w = plan.at(u, p);
+            Work w;
+            for (uint32_t u = 0; !dead && plan.unit(u, w); u++) {
                 for (uint32_t k = 0; k < w.kblocks; k++, it++) {
                     const uint32_t s = it % kStages, a = smem + s * S::stage, b = a + S::stage_a, bar = leader_bar<CG>(full + 8 * s);
                     if (!bar_wait(empty + 8 * s, (it / kStages & 1) ^ 1)) { dead = true; break; }
@@ -562,8 +603,8 @@ __global__ void __launch_bounds__(kMmaThreads, 1) rd_vocab_mma_kernel(const __gr
         if (lane == 0 && rank == 0) {
             constexpr uint32_t kDesc = 1u << 4 | (BF16 ? 1u << 7 | 1u << 10 : 0u) | uint32_t(kTileN / 8) << 17 | uint32_t(S::tile_m / 16) << 24;
             uint32_t it = 0, tile = 0;
-            for (uint32_t u = first_unit; u < plan.units && !dead; u += unit_step) {
-                const Work w = plan.at(u, p);
+            Work w;
+            for (uint32_t u = 0; !dead && plan.unit(u, w); u++) {
                 if (w.kblocks == 0) continue;            // the epilogue takes zeros
                 const uint32_t buf = tile & 1;
                 if (!bar_wait(acc_empty + 8 * buf, (tile / 2 & 1) ^ 1)) { dead = true; break; }
@@ -587,10 +628,11 @@ __global__ void __launch_bounds__(kMmaThreads, 1) rd_vocab_mma_kernel(const __gr
         }
     } else if (warp >= 4) {
         const int quarter = warp & 3, half = (warp - 4) >> 2;        // rows 32 * quarter.., columns 128 * half.. of the tile
+        const uint32_t box = boxes + (warp - 4) * kBox;
         uint32_t tile = 0;
-        for (uint32_t u = first_unit; u < plan.units; u += unit_step) {
-            const Work w = plan.at(u, p);
-            const uint32_t row = w.m0 + rank * kRowsM + 32 * quarter + lane, col0 = w.n0 + 128 * half;
+        Work w;
+        for (uint32_t u = 0; plan.unit(u, w); u++) {
+            const uint32_t row0 = w.m0 + rank * kRowsM + 32 * quarter, row = row0 + lane, col0 = w.n0 + 128 * half;
             const uint32_t buf = tile & 1;
             if (w.kblocks) {
                 if (!bar_wait(acc_full + 8 * buf, tile / 2 & 1)) break;
@@ -658,43 +700,44 @@ __global__ void __launch_bounds__(kMmaThreads, 1) rd_vocab_mma_kernel(const __gr
                         if (col + j == uint32_t(label)) y[j] -= gt;
                         if (row >= m || col + j >= p.piece) y[j] = 0.0f;
                     }
-                    uint16_t *dst = p.dx + size_t(row) * p.dx_stride + col;
+                    box_wait(lane, c & 1);
 #pragma unroll
-                    for (int q = 0; q < 2; q++) {
-                        uint32_t o[8];
-#pragma unroll
-                        for (int j = 0; j < 8; j++) o[j] = pack2<BF16>(y[16 * q + 2 * j], y[16 * q + 2 * j + 1]);
-                        store32(dst + 16 * q, o);
+                    for (int q = 0; q < 4; q++)
+                        box_put(box, lane, 4 * (c & 1) + q, pack2<BF16>(y[8 * q], y[8 * q + 1]), pack2<BF16>(y[8 * q + 2], y[8 * q + 3]), pack2<BF16>(y[8 * q + 4], y[8 * q + 5]),
+                                pack2<BF16>(y[8 * q + 6], y[8 * q + 7]));
+                    if (box_full(lane, c & 1)) {
+                        tma_store(&p.dx_out, box, col - 32, row0);
+                        box_sent();
                     }
                 } else if (w.product == 1) {
-                    if (row < m) {
-                        float *dst = p.dh + (size_t(w.split) * p.dh_rows + row) * p.dh_stride + col;
+                    box_wait(lane, false);
 #pragma unroll
-                        for (int q = 0; q < 4; q++) {
-                            if (col + 8 * q >= p.dh_stride) break;
-                            uint32_t o[8];
-                            float old[8] = {};
-                            if (!p.first_piece) load32(dst + 8 * q, old);
-#pragma unroll
-                            for (int j = 0; j < 8; j++) o[j] = __float_as_uint(old[j] + __uint_as_float(v[8 * q + j]));
-                            store32(dst + 8 * q, o);
-                        }
+                    for (int q = 0; q < 8; q++) box_put(box, lane, q, v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]);
+                    if (box_full(lane, true) && col < p.dh_stride && row0 < m) {
+                        if (p.first_piece) tma_store(&p.dh_out, box, col, row0, w.split);
+                        else tma_add(&p.dh_out, box, col, row0, w.split);
+                        box_sent();
                     }
-                } else if (row < p.piece) {
-                    uint16_t *dst = p.dw + size_t(p.piece0 + row) * p.dw_stride + col;
+                } else if (p.dw_tma) {
+                    box_wait(lane, c & 1);
 #pragma unroll
                     for (int q = 0; q < 4; q++) {
                         uint32_t o[4];
 #pragma unroll
-                        for (int j = 0; j < 4; j++)
-                            o[j] = pack2<BF16>(__uint_as_float(v[8 * q + 2 * j]) * unboost, __uint_as_float(v[8 * q + 2 * j + 1]) * unboost);
-                        if (p.dw_wide && col + 8 * q + 8 <= p.dim) {
-                            *reinterpret_cast<uint4 *>(dst + 8 * q) = make_uint4(o[0], o[1], o[2], o[3]);
-                        } else {
+                        for (int j = 0; j < 4; j++) o[j] = pack2<BF16>(__uint_as_float(v[8 * q + 2 * j]) * unboost, __uint_as_float(v[8 * q + 2 * j + 1]) * unboost);
+                        box_put(box, lane, 4 * (c & 1) + q, o[0], o[1], o[2], o[3]);
+                    }
+                    if (box_full(lane, c & 1) && col - 32 < p.dim && row0 < p.piece) {
+                        tma_store(&p.dw_out, box, col - 32, p.piece0 + row0);
+                        box_sent();
+                    }
+                } else if (row < p.piece) {
+                    uint16_t *dst = p.dw + size_t(p.piece0 + row) * p.dw_stride + col;
 #pragma unroll
-                            for (int j = 0; j < 8; j++)
-                                if (col + 8 * q + j < p.dim) dst[8 * q + j] = uint16_t(o[j / 2] >> (j & 1 ? 16 : 0));
-                        }
+                    for (int j = 0; j < 32; j += 2) {
+                        const uint32_t o = pack2<BF16>(__uint_as_float(v[j]) * unboost, __uint_as_float(v[j + 1]) * unboost);
+                        if (col + j < p.dim) dst[j] = uint16_t(o);
+                        if (col + j + 1 < p.dim) dst[j + 1] = uint16_t(o >> 16);
                     }
                 }
             }
@@ -708,6 +751,7 @@ __global__ void __launch_bounds__(kMmaThreads, 1) rd_vocab_mma_kernel(const __gr
                 tile++;
             }
         }
+        if (KIND != kStats && lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
     }
     __syncwarp();
     pair_sync<CG>();                             // neither block of a pair leaves while the other may still signal it
@@ -836,6 +880,28 @@ bool needs_align(const VocabArgs &a) { return reinterpret_cast<uintptr_t>(a.weig
 // Whether pairs of thread blocks compute tiles of 256 x 256: as soon as there is more than one tile of 128 tokens.
 int pair_or_single(size_t n) { return n > kRowsM ? 2 : 1; }
 
+constexpr size_t kSms = 148;
+
+// Parts that the sum over a piece is cut into for dh.  More parts fill the groups of thread blocks more evenly, but each is a
+// matrix of its own that is written and read once more; times in steps of the summed index (0.28 us on an SM).
+size_t dh_splits(const VocabArgs &a, size_t piece)
+{
+    const size_t tile_m = size_t(kRowsM) * pair_or_single(a.n), groups = kSms * kRowsM / tile_m;
+    const size_t dh_n = (a.dim + kTileN - 1) / kTileN, tiles = (a.n + tile_m - 1) / tile_m * dh_n;
+    const double step_bytes = 0.28e-6 * 6.5e12, k_piece = double(piece / kTileK), k_tokens = double((a.n + kTileK - 1) / kTileK);
+    const double dw = double((piece + tile_m - 1) / tile_m * dh_n) * (k_tokens + kTileOverhead);
+    size_t best = 1;
+    double best_time = 0;
+    for (size_t s = 1; s <= 64 && s * 8 <= size_t(k_piece) + 7; s++) {
+        const size_t units = tiles * s;
+        const double unit = double((size_t(k_piece) + s - 1) / s + kTileOverhead), even = (double(units) * unit + dw) / double(groups);
+        const double longest = double((units + groups - 1) / groups) * unit;
+        const double time = (even > longest ? even : longest) + double(s) * double(a.n * a.dim) * 8 / step_bytes;
+        if (s == 1 || time < best_time) best = s, best_time = time;
+    }
+    return best;
+}
+
 struct Layout {
     Meta *meta;
     TileCount *tiles;
@@ -846,7 +912,6 @@ struct Layout {
     size_t rows_padded, packed_stride, dx_stride, piece, splits, dh_stride, bytes;
 };
 
-constexpr size_t kSms = 148;
 constexpr size_t kDxBytes = size_t(256) << 20;    // what the gradient keeps of dx at a time
 
 Layout lay_out(const VocabArgs &a, bool gradient, bool want_hidden)
@@ -876,11 +941,7 @@ Layout lay_out(const VocabArgs &a, bool gradient, bool want_hidden)
         l.dx_stride = l.piece;
         l.dx = w.take<uint16_t>(l.rows_padded * l.dx_stride);
         l.dh_stride = l.packed_stride;
-        const size_t tile_m = size_t(kRowsM) * pair_or_single(a.n), tiles = (a.n + tile_m - 1) / tile_m * ((a.dim + kTileN - 1) / kTileN);
-        const size_t k_blocks = l.piece / kTileK;
-        const size_t groups = kSms * kRowsM / tile_m;
-        l.splits = tiles >= groups ? 1 : (groups + tiles - 1) / tiles;
-        if (l.splits > (k_blocks + 7) / 8) l.splits = (k_blocks + 7) / 8;
+        l.splits = want_hidden ? dh_splits(a, l.piece) : 1;
         if (want_hidden) l.dh = w.take<float>(l.splits * a.n * l.dh_stride);
     }
     l.bytes = w.at;
@@ -904,7 +965,18 @@ EncodeTiled encoder()
     return f;
 }
 
-// A matrix of 16-bit values, `inner` contiguous ones per row, read in boxes of 64 values x box_rows rows.
+// dh: `parts` matrices of n x stride fp32 values, written in boxes of 32 x 32.
+bool encode_dh(CUtensorMap *map, void *base, size_t stride, size_t n, size_t parts)
+{
+    const EncodeTiled f = encoder();
+    if (!f) return false;
+    const cuuint64_t dims[3] = {stride, n, parts}, strides[2] = {stride * 4, n * stride * 4};
+    const cuuint32_t box[3] = {32, 32, 1}, one[3] = {1, 1, 1};
+    return f(map, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 3, base, dims, strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+             CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// A matrix of 16-bit values, `inner` contiguous ones per row, read or written in boxes of 64 values x box_rows rows.
 bool encode(CUtensorMap *map, bool bf16, const void *base, size_t inner, size_t rows, size_t stride, uint32_t box_rows)
 {
     const EncodeTiled f = encoder();
@@ -929,7 +1001,7 @@ int sm_count_of(int device)
 
 template <int KIND, bool BF16, int CG> cudaError_t launch_mma(const MmaParams &p, int device, size_t most_units, cudaStream_t stream)
 {
-    constexpr uint32_t smem = Shape<CG>::smem;
+    constexpr uint32_t smem = Shape<KIND, CG>::smem;
     static std::atomic<bool> ready[64];
     if (device >= 64 || !ready[device].load(std::memory_order_acquire)) {
         const cudaError_t e = cudaFuncSetAttribute(rd_vocab_mma_kernel<KIND, BF16, CG>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
@@ -1085,21 +1157,19 @@ cudaError_t vocab_loss_grad(const VocabArgs &a)
     logits.gp = l.gp;
     logits.gt = l.gt;
     logits.lse2 = l.lse2;
-    logits.dx = l.dx;
-    logits.dx_stride = l.dx_stride;
-    grads.dh = l.dh;
-    grads.dh_rows = a.n;
     grads.dh_stride = l.dh_stride;
     grads.splits = uint32_t(l.splits);
     grads.dw = static_cast<uint16_t *>(a.grad_weight);
     grads.dw_stride = a.grad_weight_stride;
-    grads.dw_wide = reinterpret_cast<uintptr_t>(a.grad_weight) % 16 == 0 && a.grad_weight_stride % 8 == 0;
+    grads.dw_tma = reinterpret_cast<uintptr_t>(a.grad_weight) % 16 == 0 && a.grad_weight_stride % 8 == 0;
     grads.want_dh = a.grad_hidden != nullptr;
     grads.want_dw = a.grad_weight != nullptr;
     if (!encode(&logits.a_k, a.bf16, l.packed, a.dim, l.rows_padded, l.packed_stride, kRowsM) || !encode(&logits.b_k, a.bf16, weight, a.dim, a.rows, weight_stride, kTileN / cg) ||
         !encode(&grads.a_k, a.bf16, l.dx, l.dx_stride, l.rows_padded, l.dx_stride, kRowsM) || !encode(&grads.a_mn, a.bf16, l.dx, l.dx_stride, l.rows_padded, l.dx_stride, 64) ||
-        !encode(&grads.b_mn, a.bf16, weight, a.dim, a.rows, weight_stride, 64) || !encode(&grads.b2_mn, a.bf16, l.packed, a.dim, l.rows_padded, l.packed_stride, 64))
+        !encode(&logits.dx_out, a.bf16, l.dx, l.dx_stride, l.rows_padded, l.dx_stride, 32) || !encode(&grads.b_mn, a.bf16, weight, a.dim, a.rows, weight_stride, 64) || !encode(&grads.b2_mn, a.bf16, l.packed, a.dim, l.rows_padded, l.packed_stride, 64))
         return cudaErrorInvalidValue;
+    if (grads.want_dh && !encode_dh(&grads.dh_out, l.dh, l.dh_stride, a.n, l.splits)) return cudaErrorInvalidValue;
+    if (grads.want_dw && grads.dw_tma && !encode(&grads.dw_out, a.bf16, a.grad_weight, a.dim, a.rows, a.grad_weight_stride, 32)) return cudaErrorInvalidValue;
     const size_t tiles_m = (a.n + tile_m - 1) / tile_m, tiles_d = (a.dim + kTileN - 1) / kTileN;
     for (size_t v = 0; v < a.rows; v += l.piece) {
         const size_t piece = a.rows - v < l.piece ? a.rows - v : l.piece;
