@@ -154,12 +154,15 @@ template <int R> __global__ void __launch_bounds__(kPackThreads) rd_vocab_pack_k
         const size_t i = size_t(own_tile) * kCountTile + threadIdx.x;
         if (i < base && i < p.n && label_of(p.labels, p.wide_labels, i) >= 0) before++;
     } else {
-        for (size_t i = threadIdx.x; i < p.n; i += kPackThreads) {
-            if (label_of(p.labels, p.wide_labels, i) < 0) continue;
-            all++;
-            if (i < base) before++;
-            if (p.gradient && p.fp16 && first) most = fmaxf(most, largest_factor(p, i));
+#pragma unroll 8
+        for (uint32_t i = threadIdx.x; i < uint32_t(p.n); i += kPackThreads) {
+            const uint32_t counts = label_of(p.labels, p.wide_labels, i) >= 0;
+            all += counts;
+            before += i < base ? counts : 0;
         }
+        if (p.gradient && p.fp16 && first)
+            for (uint32_t i = threadIdx.x; i < uint32_t(p.n); i += kPackThreads)
+                if (label_of(p.labels, p.wide_labels, i) >= 0) most = fmaxf(most, largest_factor(p, i));
     }
 #pragma unroll
     for (int d = 16; d; d /= 2) {
@@ -375,17 +378,26 @@ template <int CG> __device__ __forceinline__ void mma_commit(uint32_t bar)
     else asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
 }
 
-__device__ __forceinline__ void tmem_load32(uint32_t addr, uint32_t (&v)[32])
+// Starts reading 32 columns of a warp's 32 rows; tmem_wait before the values are used.
+__device__ __forceinline__ void tmem_load(uint32_t addr, uint32_t (&v)[32])
 {
     asm volatile(
         "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
-        "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];\n\t"
-        "tcgen05.wait::ld.sync.aligned;"
+        "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
         : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]), "=r"(v[8]), "=r"(v[9]), "=r"(v[10]), "=r"(v[11]),
           "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15]), "=r"(v[16]), "=r"(v[17]), "=r"(v[18]), "=r"(v[19]), "=r"(v[20]), "=r"(v[21]), "=r"(v[22]),
           "=r"(v[23]), "=r"(v[24]), "=r"(v[25]), "=r"(v[26]), "=r"(v[27]), "=r"(v[28]), "=r"(v[29]), "=r"(v[30]), "=r"(v[31])
         : "r"(addr)
         : "memory");
+}
+__device__ __forceinline__ void tmem_wait(uint32_t (&v)[32])
+{
+    asm volatile("tcgen05.wait::ld.sync.aligned;"
+                 : "+r"(v[0]), "+r"(v[1]), "+r"(v[2]), "+r"(v[3]), "+r"(v[4]), "+r"(v[5]), "+r"(v[6]), "+r"(v[7]), "+r"(v[8]), "+r"(v[9]), "+r"(v[10]), "+r"(v[11]),
+                   "+r"(v[12]), "+r"(v[13]), "+r"(v[14]), "+r"(v[15]), "+r"(v[16]), "+r"(v[17]), "+r"(v[18]), "+r"(v[19]), "+r"(v[20]), "+r"(v[21]), "+r"(v[22]),
+                   "+r"(v[23]), "+r"(v[24]), "+r"(v[25]), "+r"(v[26]), "+r"(v[27]), "+r"(v[28]), "+r"(v[29]), "+r"(v[30]), "+r"(v[31])
+                 :
+                 : "memory");
 }
 
 __device__ __forceinline__ float exp2_fast(float x)
@@ -458,60 +470,120 @@ struct Work {
     uint32_t m0, n0, k0, kblocks, split;
 };
 
-// Which units of work a group of thread blocks (one or a pair, number c of g) gets: unit(0), unit(1), ... until it says no.
+// A position in rows of `wide` places, advanced by a constant number of places without divisions.
+struct Cursor {
+    uint32_t x, y, wide, dx, dy;
+    __device__ __forceinline__ void set(uint32_t at, uint32_t step, uint32_t row)
+    {
+        wide = row;
+        x = at % row;
+        y = at / row;
+        dx = step % row;
+        dy = step / row;
+    }
+    __device__ __forceinline__ void advance()
+    {
+        x += dx;
+        y += dy;
+        if (x >= wide) {
+            x -= wide;
+            y++;
+        }
+    }
+};
+
+// Which units of work a group of thread blocks (one or a pair, number c of g) gets: next() until it says no.
+// Logits: bands of p.group token tiles, within a band all token tiles of a vocabulary tile one after the other.
 // Gradients: the units of dh first, dealt out in turn; their number need not divide by g, so some groups get one more of them,
 // and that many fewer of dw's tiles, by the number of steps of the summed index.
 template <int KIND, int CG> struct Plan {
     static constexpr uint32_t kTileM = Shape<KIND, CG>::tile_m;
     const MmaParams &p;
-    uint32_t c, g;
-    uint32_t tiles_m, tiles_n;                                 // logits
-    uint32_t dh_n, dh_tiles, k_per_split, k_piece, dh_mine, dh_more;    // dh
-    uint32_t dw_tiles, k_tokens, dw_even;                      // dw
+    Cursor at;
+    uint32_t c, g, tiles_m;
+    uint32_t tiles_n, band, k_dim;                             // logits
+    uint32_t left, phase, split, dh_n, k_per_split, k_piece, dh_more;    // gradients: units left in the phase (0 dh, 1 dw, 2 dw's rest)
+    uint32_t dw_tiles, k_tokens, dw_even;
 
     __device__ __forceinline__ Plan(const MmaParams &params, uint32_t m) : p(params), c(blockIdx.x / CG), g(gridDim.x / CG)
     {
         tiles_m = (m + kTileM - 1) / kTileM;
         if (KIND != kGrads) {
             tiles_n = (p.piece + kTileN - 1) / kTileN;
+            k_dim = (p.dim + kTileK - 1) / kTileK;
+            band = 0;
+            if (tiles_m) at.set(c, g, min(p.group, tiles_m));
         } else {
             dh_n = (p.dim + kTileN - 1) / kTileN;
             k_piece = (p.piece + kTileK - 1) / kTileK;
             k_per_split = (k_piece + p.splits - 1) / p.splits;
-            dh_tiles = tiles_m * dh_n;
             k_tokens = (m + kTileK - 1) / kTileK;
             dw_tiles = p.want_dw ? (p.piece + kTileM - 1) / kTileM * dh_n : 0;
-            const uint32_t dh_units = p.want_dh ? dh_tiles * p.splits : 0;
+            const uint32_t dh_units = p.want_dh ? tiles_m * dh_n * p.splits : 0;
             dh_more = dh_units % g;                            // groups with one more unit of dh
-            dh_mine = dh_units / g + (c < dh_more);
             // a unit of dh is worth this many tiles of dw, which the other groups take first
             const uint32_t worth = dh_more ? (2 * (k_per_split + kTileOverhead) + k_tokens) / (2 * (k_tokens + kTileOverhead)) : 0;
             const uint32_t ahead = worth * (g - dh_more);
             dw_even = dw_tiles > ahead ? (dw_tiles - ahead + g - 1) / g : 0;      // turns that every group takes part in
+            phase = split = 0;
+            left = dh_units / g + (c < dh_more);
+            at.set(c, g, dh_n);
         }
     }
-    __device__ __forceinline__ bool unit(uint32_t i, Work &w) const
+    __device__ __forceinline__ bool next(Work &w)
     {
-        if (KIND != kGrads) {
-            const uint32_t u = c + i * g;
-            if (u >= tiles_m * tiles_n) return false;
-            const uint32_t per = p.group * tiles_n, band = u / per, in = u - band * per;
-            const uint32_t wide = min(p.group, tiles_m - band * p.group);
-            w = Work{0, (band * p.group + in % wide) * kTileM, in / wide * kTileN, 0, (p.dim + kTileK - 1) / kTileK, 0};
+        if constexpr (KIND != kGrads) {
+            if (tiles_m == 0) return false;
+            while (at.y >= tiles_n) {                          // on to the next band
+                const uint32_t over = (at.y - tiles_n) * at.wide + at.x;
+                if (++band * p.group >= tiles_m) {
+                    band--;                                    // stay at the end
+                    return false;
+                }
+                at.set(over, g, min(p.group, tiles_m - band * p.group));
+            }
+            w = Work{0, (band * p.group + at.x) * kTileM, at.y * kTileN, 0, k_dim, 0};
+            at.advance();
+            return true;
+        } else {
+            while (left == 0) {
+                if (phase == 2 || (phase == 1 && c < dh_more)) return false;
+                phase++;
+                if (phase == 1) {
+                    left = dw_even;
+                    at.set(c, g, dh_n);
+                } else {
+                    at.set(dw_even * g + c - dh_more, g - dh_more, dh_n);
+                    left = 0xffffffffu;                            // until the tiles run out
+                }
+            }
+            if (phase == 0) {
+                while (at.y >= tiles_m) {
+                    at.y -= tiles_m;
+                    split++;
+                }
+                const uint32_t k0 = split * k_per_split, k1 = min(k0 + k_per_split, k_piece);
+                w = Work{1, at.y * kTileM, at.x * kTileN, k0 * kTileK, k1 > k0 ? k1 - k0 : 0, split};
+            } else {
+                if (at.y * dh_n + at.x >= dw_tiles) return false;
+                w = Work{2, at.y * kTileM, at.x * kTileN, 0, k_tokens, 0};
+            }
+            left--;
+            at.advance();
             return true;
         }
-        if (i < dh_mine) {
-            const uint32_t u = c + i * g, s = u / dh_tiles, t = u - s * dh_tiles;
-            const uint32_t k0 = s * k_per_split, k1 = min(k0 + k_per_split, k_piece);
-            w = Work{1, t / dh_n * kTileM, t % dh_n * kTileN, k0 * kTileK, k1 > k0 ? k1 - k0 : 0, s};
-            return true;
+    }
+};
+
+// A ring's stage and the parity of its turn.
+template <int N> struct Turn {
+    uint32_t s = 0, parity = 0;
+    __device__ __forceinline__ void advance()
+    {
+        if (++s == N) {
+            s = 0;
+            parity ^= 1;
         }
-        i -= dh_mine;
-        if (i >= dw_even && c < dh_more) return false;
-        const uint32_t t = i < dw_even ? c + i * g : dw_even * g + (i - dw_even) * (g - dh_more) + (c - dh_more);
-        if (t >= dw_tiles) return false;
-        w = Work{2, t / dh_n * kTileM, t % dh_n * kTileN, 0, k_tokens, 0};
-        return true;
     }
 };
 
@@ -565,27 +637,30 @@ __global__ void __launch_bounds__(kMmaThreads, 1) rd_vocab_mma_kernel(const __gr
 
     pdl_start();
     const uint32_t m = p.meta->m;
-    const Plan<KIND, CG> plan(p, m);
+    Plan<KIND, CG> plan(p, m);
     bool dead = false;
 
-    if (warp == 0) {
+    if (warp == 0 || warp == 3) {
+        // one thread brings in the left operand, another the right one
         if (lane == 0) {
-            uint32_t it = 0;
+            Turn<kStages> turn;
             Work w;
-            for (uint32_t u = 0; !dead && plan.unit(u, w); u++) {
-                for (uint32_t k = 0; k < w.kblocks; k++, it++) {
-                    const uint32_t s = it % kStages, a = smem + s * S::stage, b = a + S::stage_a, bar = leader_bar<CG>(full + 8 * s);
-                    if (!bar_wait(empty + 8 * s, (it / kStages & 1) ^ 1)) { dead = true; break; }
-                    // both thread blocks' copies count at the first one's barrier
-                    if (rank == 0) bar_expect(full + 8 * s, CG * S::stage);
-                    const uint32_t kk = w.k0 + k * kTileK, m0 = w.m0 + rank * kRowsM, n0 = w.n0 + rank * S::rows_n;
-                    if (w.product == 2) {
+            const uint32_t lead = leader_bar<CG>(full);
+            while (!dead && plan.next(w)) {
+                const uint32_t m0 = w.m0 + rank * kRowsM, n0 = w.n0 + rank * S::rows_n;
+                for (uint32_t k = 0, kk = w.k0; k < w.kblocks; k++, kk += kTileK, turn.advance()) {
+                    const uint32_t a = smem + turn.s * S::stage, b = a + S::stage_a, bar = lead + 8 * turn.s;
+                    if (!bar_wait(empty + 8 * turn.s, turn.parity ^ 1)) { dead = true; break; }
+                    if (warp == 0) {
+                        // the copies of both thread blocks and both operands count at the first block's barrier
+                        if (rank == 0) bar_expect(full + 8 * turn.s, CG * S::stage);
+                        if (w.product == 2) {
 #pragma unroll
-                        for (int j = 0; j < kRowsM / 64; j++) tma_load<CG>(a + j * 8192, &p.a_mn, m0 + 64 * j, kk, bar);
-                    } else {
-                        tma_load<CG>(a, &p.a_k, kk, m0, bar);
-                    }
-                    if (KIND != kGrads) {
+                            for (int j = 0; j < kRowsM / 64; j++) tma_load<CG>(a + j * 8192, &p.a_mn, m0 + 64 * j, kk, bar);
+                        } else {
+                            tma_load<CG>(a, &p.a_k, kk, m0, bar);
+                        }
+                    } else if (KIND != kGrads) {
                         tma_load<CG>(b, &p.b_k, kk, p.piece0 + n0, bar);
                     } else {
                         const CUtensorMap *map = w.product == 1 ? &p.b_mn : &p.b2_mn;
@@ -596,15 +671,16 @@ __global__ void __launch_bounds__(kMmaThreads, 1) rd_vocab_mma_kernel(const __gr
                 }
             }
             // the last stages' arrivals have to land while the barriers still exist
-            for (int s = 0; s < kStages && !dead; s++, it++) dead = !bar_wait(empty + 8 * (it % kStages), (it / kStages & 1) ^ 1);
+            for (int s = 0; s < kStages && !dead; s++, turn.advance()) dead = !bar_wait(empty + 8 * turn.s, turn.parity ^ 1);
             if (dead) drain();
         }
     } else if (warp == 1) {
         if (lane == 0 && rank == 0) {
             constexpr uint32_t kDesc = 1u << 4 | (BF16 ? 1u << 7 | 1u << 10 : 0u) | uint32_t(kTileN / 8) << 17 | uint32_t(S::tile_m / 16) << 24;
-            uint32_t it = 0, tile = 0;
+            Turn<kStages> turn;
+            uint32_t tile = 0;
             Work w;
-            for (uint32_t u = 0; !dead && plan.unit(u, w); u++) {
+            while (!dead && plan.next(w)) {
                 if (w.kblocks == 0) continue;            // the epilogue takes zeros
                 const uint32_t buf = tile & 1;
                 if (!bar_wait(acc_empty + 8 * buf, (tile / 2 & 1) ^ 1)) { dead = true; break; }
@@ -612,14 +688,14 @@ __global__ void __launch_bounds__(kMmaThreads, 1) rd_vocab_mma_kernel(const __gr
                 const bool ta = w.product == 2, tb = w.product != 0;
                 const uint32_t idesc = kDesc | (ta ? 1u << 15 : 0u) | (tb ? 1u << 16 : 0u);
                 const uint32_t step_a = ta ? 2048 >> 4 : 32 >> 4, step_b = tb ? 2048 >> 4 : 32 >> 4;
-                for (uint32_t k = 0; k < w.kblocks; k++, it++) {
-                    const uint32_t s = it % kStages, a = smem + s * S::stage, b = a + S::stage_a;
-                    if (!bar_wait(full + 8 * s, it / kStages & 1)) { dead = true; break; }
+                for (uint32_t k = 0; k < w.kblocks; k++, turn.advance()) {
+                    const uint32_t a = smem + turn.s * S::stage, b = a + S::stage_a;
+                    if (!bar_wait(full + 8 * turn.s, turn.parity)) { dead = true; break; }
                     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                     const uint64_t da = operand(a, ta), db = operand(b, tb);
 #pragma unroll
                     for (int j = 0; j < kTileK / 16; j++) mma<CG>(tmem + buf * kTileN, da + j * step_a, db + j * step_b, idesc, k != 0 || j != 0);
-                    mma_commit<CG>(empty + 8 * s);
+                    mma_commit<CG>(empty + 8 * turn.s);
                 }
                 if (!dead) mma_commit<CG>(acc_full + 8 * buf);
                 tile++;
@@ -631,7 +707,7 @@ __global__ void __launch_bounds__(kMmaThreads, 1) rd_vocab_mma_kernel(const __gr
         const uint32_t box = boxes + (warp - 4) * kBox;
         uint32_t tile = 0;
         Work w;
-        for (uint32_t u = 0; plan.unit(u, w); u++) {
+        while (plan.next(w)) {
             const uint32_t row0 = w.m0 + rank * kRowsM + 32 * quarter, row = row0 + lane, col0 = w.n0 + 128 * half;
             const uint32_t buf = tile & 1;
             if (w.kblocks) {
@@ -641,7 +717,7 @@ __global__ void __launch_bounds__(kMmaThreads, 1) rd_vocab_mma_kernel(const __gr
             const uint32_t acc = tmem + buf * kTileN + 128 * half + (uint32_t(32 * quarter) << 16);
             // the row's numbers (stats and dlogits)
             int label = -1;
-            float lse2 = 0.0f, gp = 0.0f, gt = 0.0f, top = -INFINITY, sum = 0.0f;
+            float lse2 = 0.0f, gp = 0.0f, gt = 0.0f;
             if (KIND != kGrads && row < m) {
                 label = p.label[row];
                 if (KIND == kDlogits) {
@@ -653,103 +729,142 @@ __global__ void __launch_bounds__(kMmaThreads, 1) rd_vocab_mma_kernel(const __gr
                 }
             }
             const float unboost = KIND == kGrads ? p.meta->unboost : 1.0f;
-#pragma unroll 1
-            for (int c = 0; c < 4; c++) {
-                const uint32_t col = col0 + 32 * c;
-                uint32_t v[32];
-                if (w.kblocks) {
-                    tmem_load32(acc + 32 * c, v);
-                } else {
-#pragma unroll
-                    for (int j = 0; j < 32; j++) v[j] = 0;
-                }
-                if (KIND == kStats) {
-                    // the lowest value in the columns that the vocabulary does not have
-                    const uint32_t lowest = __float_as_uint(p.scale2 >= 0.0f ? -INFINITY : INFINITY);
-                    if (col + 32 > p.piece) {
-#pragma unroll
-                        for (int j = 0; j < 32; j++)
-                            if (col + j >= p.piece) v[j] = lowest;
-                    }
-                    float most = __uint_as_float(v[0]);
-                    if (p.scale2 >= 0.0f) {
-#pragma unroll
-                        for (int j = 1; j < 32; j++) most = fmaxf(most, __uint_as_float(v[j]));
-                    } else {
-#pragma unroll
-                        for (int j = 1; j < 32; j++) most = fminf(most, __uint_as_float(v[j]));
-                    }
-                    // an infinite maximum must not meet itself in a difference: exp2(inf) and exp2(-inf) are right as they are
-                    most = fmaxf(most * p.scale2, top);
-                    const float ref = fabsf(most) == INFINITY ? 0.0f : most;
-                    float s[4] = {fabsf(top) == INFINITY ? sum : sum * exp2_fast(top - ref), 0.0f, 0.0f, 0.0f};
-#pragma unroll
-                    for (int j = 0; j < 32; j++) s[j & 3] += exp2_fast(fmaf(__uint_as_float(v[j]), p.scale2, -ref));
-                    sum = (s[0] + s[1]) + (s[2] + s[3]);
-                    top = most;
-                    if (label >= 0 && uint32_t(label) - col < 32u && row < m) {
-#pragma unroll
-                        for (int j = 0; j < 32; j++)
-                            if (uint32_t(label) == col + j) p.target[row] = __uint_as_float(v[j]) * p.scale;
-                    }
-                } else if (KIND == kDlogits) {
-                    float y[32];
-#pragma unroll
-                    for (int j = 0; j < 32; j++) {
-                        y[j] = exp2_fast(fmaf(__uint_as_float(v[j]), p.scale2, -lse2)) * gp;
-                        if (col + j == uint32_t(label)) y[j] -= gt;
-                        if (row >= m || col + j >= p.piece) y[j] = 0.0f;
-                    }
-                    box_wait(lane, c & 1);
-#pragma unroll
-                    for (int q = 0; q < 4; q++)
-                        box_put(box, lane, 4 * (c & 1) + q, pack2<BF16>(y[8 * q], y[8 * q + 1]), pack2<BF16>(y[8 * q + 2], y[8 * q + 3]), pack2<BF16>(y[8 * q + 4], y[8 * q + 5]),
-                                pack2<BF16>(y[8 * q + 6], y[8 * q + 7]));
-                    if (box_full(lane, c & 1)) {
-                        tma_store(&p.dx_out, box, col - 32, row0);
-                        box_sent();
-                    }
-                } else if (w.product == 1) {
-                    box_wait(lane, false);
-#pragma unroll
-                    for (int q = 0; q < 8; q++) box_put(box, lane, q, v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]);
-                    if (box_full(lane, true) && col < p.dh_stride && row0 < m) {
-                        if (p.first_piece) tma_store(&p.dh_out, box, col, row0, w.split);
-                        else tma_add(&p.dh_out, box, col, row0, w.split);
-                        box_sent();
-                    }
-                } else if (p.dw_tma) {
-                    box_wait(lane, c & 1);
-#pragma unroll
-                    for (int q = 0; q < 4; q++) {
-                        uint32_t o[4];
-#pragma unroll
-                        for (int j = 0; j < 4; j++) o[j] = pack2<BF16>(__uint_as_float(v[8 * q + 2 * j]) * unboost, __uint_as_float(v[8 * q + 2 * j + 1]) * unboost);
-                        box_put(box, lane, 4 * (c & 1) + q, o[0], o[1], o[2], o[3]);
-                    }
-                    if (box_full(lane, c & 1) && col - 32 < p.dim && row0 < p.piece) {
-                        tma_store(&p.dw_out, box, col - 32, p.piece0 + row0);
-                        box_sent();
-                    }
-                } else if (row < p.piece) {
-                    uint16_t *dst = p.dw + size_t(p.piece0 + row) * p.dw_stride + col;
-#pragma unroll
-                    for (int j = 0; j < 32; j += 2) {
-                        const uint32_t o = pack2<BF16>(__uint_as_float(v[j]) * unboost, __uint_as_float(v[j + 1]) * unboost);
-                        if (col + j < p.dim) dst[j] = uint16_t(o);
-                        if (col + j + 1 < p.dim) dst[j + 1] = uint16_t(o >> 16);
-                    }
-                }
-            }
-            if (KIND == kStats) {
-                if (row < m) p.part[size_t(row) * p.parts + col0 / 128] = make_float2(top, sum);
-            }
-            if (w.kblocks) {
+            // the accumulators are free for the next tile but one as soon as their last columns are in registers
+            auto release = [&]() {
                 asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
                 __syncwarp();
                 if (lane == 0) bar_arrive_leader<CG>(acc_empty + 8 * buf);
-                tile++;
+            };
+            if constexpr (KIND == kStats) {
+                // The warp's 128 columns at once: one maximum, then the sum.  32768 exponentials per thread block and tile at
+                // 16 a cycle are what bounds this, about 2000 cycles of a tile's 512 per 64 of dim.
+                uint32_t v[4][32];
+#pragma unroll
+                for (int c = 0; c < 4; c++) tmem_load(acc + 32 * c, v[c]);
+#pragma unroll
+                for (int c = 0; c < 4; c++) tmem_wait(v[c]);
+                release();
+                if (col0 + 128 > p.piece) {
+                    // the lowest value in the columns that the vocabulary does not have
+                    const uint32_t lowest = __float_as_uint(p.scale2 >= 0.0f ? -INFINITY : INFINITY);
+#pragma unroll
+                    for (int c = 0; c < 4; c++)
+#pragma unroll
+                        for (int j = 0; j < 32; j++)
+                            if (col0 + 32 * c + j >= p.piece) v[c][j] = lowest;
+                }
+                if (label >= 0 && uint32_t(label) - col0 < 128u) {
+#pragma unroll
+                    for (int c = 0; c < 4; c++)
+#pragma unroll
+                        for (int j = 0; j < 32; j++)
+                            if (uint32_t(label) == col0 + 32 * c + j) p.target[row] = __uint_as_float(v[c][j]) * p.scale;
+                }
+                float t[8];
+#pragma unroll
+                for (int j = 0; j < 8; j++) t[j] = __uint_as_float(v[0][j]);
+                if (p.scale2 >= 0.0f) {
+#pragma unroll
+                    for (int j = 8; j < 128; j++) t[j & 7] = fmaxf(t[j & 7], __uint_as_float(v[j / 32][j % 32]));
+#pragma unroll
+                    for (int d = 4; d; d /= 2)
+#pragma unroll
+                        for (int j = 0; j < d; j++) t[j] = fmaxf(t[j], t[j + d]);
+                } else {
+#pragma unroll
+                    for (int j = 8; j < 128; j++) t[j & 7] = fminf(t[j & 7], __uint_as_float(v[j / 32][j % 32]));
+#pragma unroll
+                    for (int d = 4; d; d /= 2)
+#pragma unroll
+                        for (int j = 0; j < d; j++) t[j] = fminf(t[j], t[j + d]);
+                }
+                const float top = t[0] * p.scale2;
+                // an infinite maximum must not meet itself in a difference: exp2(inf) and exp2(-inf) are right as they are
+                const float ref = fabsf(top) == INFINITY ? 0.0f : top;
+                float sum[8] = {};
+#pragma unroll
+                for (int j = 0; j < 128; j++) sum[j & 7] += exp2_fast(fmaf(__uint_as_float(v[j / 32][j % 32]), p.scale2, -ref));
+#pragma unroll
+                for (int d = 4; d; d /= 2)
+#pragma unroll
+                    for (int j = 0; j < d; j++) sum[j] += sum[j + d];
+                if (row < m) p.part[size_t(row) * p.parts + col0 / 128] = make_float2(top, sum[0]);
+            } else {
+                auto take = [&](int c, uint32_t (&v)[32]) {
+                    const uint32_t col = col0 + 32 * c;
+                    if (KIND == kDlogits) {
+                        float y[32];
+#pragma unroll
+                        for (int j = 0; j < 32; j++) {
+                            y[j] = exp2_fast(fmaf(__uint_as_float(v[j]), p.scale2, -lse2)) * gp;
+                            if (col + j == uint32_t(label)) y[j] -= gt;
+                            if (row >= m || col + j >= p.piece) y[j] = 0.0f;
+                        }
+                        box_wait(lane, c & 1);
+#pragma unroll
+                        for (int q = 0; q < 4; q++)
+                            box_put(box, lane, 4 * (c & 1) + q, pack2<BF16>(y[8 * q], y[8 * q + 1]), pack2<BF16>(y[8 * q + 2], y[8 * q + 3]), pack2<BF16>(y[8 * q + 4], y[8 * q + 5]),
+                                    pack2<BF16>(y[8 * q + 6], y[8 * q + 7]));
+                        if (box_full(lane, c & 1)) {
+                            tma_store(&p.dx_out, box, col - 32, row0);
+                            box_sent();
+                        }
+                    } else if (w.product == 1) {
+                        box_wait(lane, false);
+#pragma unroll
+                        for (int q = 0; q < 8; q++) box_put(box, lane, q, v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]);
+                        if (box_full(lane, true) && col < p.dh_stride && row0 < m) {
+                            if (p.first_piece) tma_store(&p.dh_out, box, col, row0, w.split);
+                            else tma_add(&p.dh_out, box, col, row0, w.split);
+                            box_sent();
+                        }
+                    } else if (p.dw_tma) {
+                        box_wait(lane, c & 1);
+#pragma unroll
+                        for (int q = 0; q < 4; q++) {
+                            uint32_t o[4];
+#pragma unroll
+                            for (int j = 0; j < 4; j++) o[j] = pack2<BF16>(__uint_as_float(v[8 * q + 2 * j]) * unboost, __uint_as_float(v[8 * q + 2 * j + 1]) * unboost);
+                            box_put(box, lane, 4 * (c & 1) + q, o[0], o[1], o[2], o[3]);
+                        }
+                        if (box_full(lane, c & 1) && col - 32 < p.dim && row0 < p.piece) {
+                            tma_store(&p.dw_out, box, col - 32, p.piece0 + row0);
+                            box_sent();
+                        }
+                    } else if (row < p.piece) {
+                        uint16_t *dst = p.dw + size_t(p.piece0 + row) * p.dw_stride + col;
+#pragma unroll
+                        for (int j = 0; j < 32; j += 2) {
+                            const uint32_t o = pack2<BF16>(__uint_as_float(v[j]) * unboost, __uint_as_float(v[j + 1]) * unboost);
+                            if (col + j < p.dim) dst[j] = uint16_t(o);
+                            if (col + j + 1 < p.dim) dst[j + 1] = uint16_t(o >> 16);
+                        }
+                    }
+                };
+                // 32 columns are on their way while the 32 before them are worked on
+                uint32_t v0[32], v1[32];
+                if (w.kblocks) {
+                    tmem_load(acc, v0);
+                } else {
+#pragma unroll
+                    for (int j = 0; j < 32; j++) v0[j] = v1[j] = 0;
+                }
+#pragma unroll 1
+                for (int c = 0; c < 4; c += 2) {
+                    if (w.kblocks) {
+                        tmem_wait(v0);
+                        tmem_load(acc + 32 * (c + 1), v1);
+                    }
+                    take(c, v0);
+                    if (w.kblocks) {
+                        tmem_wait(v1);
+                        if (c == 0) tmem_load(acc + 64, v0);
+                        else release();
+                    }
+                    take(c + 1, v1);
+                }
             }
+            if (w.kblocks) tile++;
         }
         if (KIND != kStats && lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
     }
@@ -877,7 +992,9 @@ struct Part {
 // TMA wants 16-byte aligned rows.
 bool needs_align(const VocabArgs &a) { return reinterpret_cast<uintptr_t>(a.weight) % 16 != 0 || a.weight_stride * 2 % 16 != 0; }
 
-// Whether pairs of thread blocks compute tiles of 256 x 256: as soon as there is more than one tile of 128 tokens.
+// Whether pairs of thread blocks compute tiles of 256 x 256: as soon as there is more than one tile of 128 tokens (up to there half
+// of a pair's tile would be empty: gradient of 128 tokens x 131072 x 4096 705 us by single blocks, 866 by pairs; 8192 tokens
+// 22.2 ms by single blocks, 21.6 by pairs, B200).
 int pair_or_single(size_t n) { return n > kRowsM ? 2 : 1; }
 
 constexpr size_t kSms = 148;
@@ -886,7 +1003,7 @@ constexpr size_t kSms = 148;
 // matrix of its own that is written and read once more; times in steps of the summed index (0.28 us on an SM).
 size_t dh_splits(const VocabArgs &a, size_t piece)
 {
-    const size_t tile_m = size_t(kRowsM) * pair_or_single(a.n), groups = kSms * kRowsM / tile_m;
+    const size_t cg = pair_or_single(a.n), tile_m = kRowsM * cg, groups = kSms / cg;
     const size_t dh_n = (a.dim + kTileN - 1) / kTileN, tiles = (a.n + tile_m - 1) / tile_m * dh_n;
     const double step_bytes = 0.28e-6 * 6.5e12, k_piece = double(piece / kTileK), k_tokens = double((a.n + kTileK - 1) / kTileK);
     const double dw = double((piece + tile_m - 1) / tile_m * dh_n) * (k_tokens + kTileOverhead);
