@@ -42,7 +42,7 @@ constexpr float kLn2 = 0.6931471805599453f;
 struct Meta {
     uint32_t m;               // packed rows
     float boost, unboost;     // power of two that dx is multiplied by, and its inverse
-    uint32_t pad;
+    uint32_t done;            // loss of few tokens: thread blocks that have their part of the statistics written
 };
 struct TileCount {
     uint32_t n;               // tokens of the tile that count
@@ -99,7 +99,7 @@ __device__ __forceinline__ float largest_factor(const PackParams &p, size_t i)
 __global__ void __launch_bounds__(kCountTile) rd_vocab_count_kernel(PackParams p, TileCount *tiles)
 {
     __shared__ float warp_most[kCountTile / 32];
-    pdl_start();
+    pdl_wait_first();
     const size_t i = size_t(blockIdx.x) * kCountTile + threadIdx.x;
     const bool counts = i < p.n && label_of(p.labels, p.wide_labels, i) >= 0;
     float most = p.gradient && p.fp16 && counts ? largest_factor(p, i) : 0.0f;
@@ -137,7 +137,7 @@ template <int R> __global__ void __launch_bounds__(kPackThreads) rd_vocab_pack_k
     __shared__ uint32_t sums[2][kWarps];
     __shared__ float mosts[kWarps];
     __shared__ uint32_t mask_of_block;
-    pdl_start();
+    pdl_wait_first();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const bool packs = blockIdx.x < pack_blocks, first = blockIdx.x == 0;
     const size_t base = packs ? size_t(blockIdx.x) * R : p.n;          // first token of the block
@@ -255,10 +255,56 @@ constexpr int kMmaThreads = 128 + 32 * kEpilogueWarps;
 constexpr long long kWaitCycles = 4000000000ll;     // a wait gives up after about two seconds of SM clock
 constexpr long long kDrainCycles = 20000000ll;      // after that, copies in flight get ten milliseconds to land
 
+struct JoinParams {
+    const float2 *part;
+    const float *packed_target;
+    const int *index, *label;
+    const Meta *meta;
+    uint32_t parts;
+    float z;
+    float *loss, *lse, *target;
+};
+
+// Joins a packed row's parts, by a warp.
+__device__ __forceinline__ void join_row(const JoinParams &p, uint32_t row, int lane)
+{
+    float top = -INFINITY, sum = 0.0f;
+    auto add = [&](float2 x) {
+        const float most = fmaxf(top, x.x);
+        const float ref = fabsf(most) == INFINITY ? 0.0f : most;
+        // a part whose maximum is infinite has its sum relative to 0 already
+        const float a = fabsf(top) == INFINITY ? sum : sum * exp2f(top - ref);
+        const float b = fabsf(x.x) == INFINITY ? x.y : x.y * exp2f(x.x - ref);
+        sum = a + b;
+        top = most;
+    };
+    const float2 *part = p.part + size_t(row) * p.parts;
+    uint32_t k = lane;
+    for (; k + 96 < p.parts; k += 128) {
+        float2 x[4];
+#pragma unroll
+        for (int u = 0; u < 4; u++) x[u] = __ldcg(part + k + 32 * u);
+#pragma unroll
+        for (int u = 0; u < 4; u++) add(x[u]);
+    }
+    for (; k < p.parts; k += 32) add(__ldcg(part + k));
+#pragma unroll
+    for (int d = 16; d; d /= 2) add(make_float2(__shfl_down_sync(0xffffffffu, top, d), __shfl_down_sync(0xffffffffu, sum, d)));
+    if (lane) return;
+    const float ref = fabsf(top) == INFINITY ? 0.0f : top;
+    const float lse = (ref + log2f(sum)) * kLn2;
+    const float target = p.label[row] >= 0 ? __ldcg(p.packed_target + row) : 0.0f;
+    const int i = p.index[row];
+    // without the penalty an infinite lse is an infinite loss, not 0 * inf
+    if (p.loss) p.loss[i] = p.z != 0.0f ? lse - target + p.z * lse * lse : lse - target;
+    if (p.lse) p.lse[i] = lse;
+    if (p.target) p.target[i] = target;
+}
+
 enum { kStats = 0, kDlogits = 1, kGrads = 2 };
 
 struct alignas(64) MmaParams {
-    CUtensorMap a_k;          // rows of the left operand, 64 x 128 boxes: packed hidden (stats, dlogits), dx (dh)
+    CUtensorMap a_k;          // rows of the left operand, 64 x a_rows boxes: packed hidden (stats, dlogits), dx (dh)
     CUtensorMap b_k;          // rows of the weight, 64 x 256 boxes (stats, dlogits)
     CUtensorMap a_mn;         // dx as the transposed left operand of dw, 64 x 64 boxes
     CUtensorMap b_mn;         // weight as the transposed right operand of dh
@@ -266,19 +312,24 @@ struct alignas(64) MmaParams {
     CUtensorMap dx_out;       // dx, 64 x 32 boxes
     CUtensorMap dh_out;       // dh, 32 x 32 x 1 boxes
     CUtensorMap dw_out;       // grad_weight, 64 x 32 boxes
-    const Meta *meta;
-    const int *label;
+    Meta *meta;
+    const int *label, *index;
     const float *gp, *gt, *lse2;
+    JoinParams join;
     float2 *part;             // stats: (maximum, sum) in base 2, [packed row][half tile]
     float *target;            // stats: the label's logit, per packed row
     uint16_t *dw;             // grad_weight, for rows that TMA cannot address
-    size_t dh_stride, dw_stride;
+    uint16_t *gh;             // grad_hidden, where one part of dh is all of it
+    size_t dh_stride, dw_stride, gh_stride;
     uint32_t parts;           // stats: half tiles per row
     uint32_t piece0, piece;   // first row of the piece and its rows
     uint32_t dim;
     uint32_t group;           // token tiles that go over the vocabulary together
     uint32_t splits;          // parts that the sum over the piece is cut into for dh
+    uint32_t a_rows;          // rows of a thread block's left operand that are brought in (fewer than 128 for few tokens)
     bool first_piece, want_dh, want_dw, dw_tma;
+    bool early;               // the weight is the caller's own: it may be read before the kernels of this call are done
+    bool gh_wide, joins;      // 16-byte rows of grad_hidden; the last thread block joins the statistics
     float scale2;             // scale * log2(e)
     float scale;
 };
@@ -509,6 +560,7 @@ template <int KIND, int CG> struct Plan {
     {
         tiles_m = (m + kTileM - 1) / kTileM;
         if (KIND != kGrads) {
+            if (CG == 1 && tiles_m == 0) tiles_m = 1;          // its weights may be on their way already
             tiles_n = (p.piece + kTileN - 1) / kTileN;
             k_dim = (p.dim + kTileK - 1) / kTileK;
             band = 0;
@@ -635,7 +687,15 @@ __global__ void __launch_bounds__(kMmaThreads, 1) rd_vocab_mma_kernel(const __gr
     uint32_t tmem;
     asm volatile("ld.shared.b32 %0, [%1];" : "=r"(tmem) : "r"(tmem_slot));
 
-    pdl_start();
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    // One tile of tokens: every block knows its first tile of the weight before the tokens are packed, and fills its ring with it.
+    uint32_t ahead = 0;
+    if (KIND != kGrads && CG == 1 && p.early && warp == 3 && lane == 0 && blockIdx.x * kTileN < p.piece) {
+        const uint32_t k_dim = (p.dim + kTileK - 1) / kTileK;
+        ahead = k_dim < kStages ? k_dim : kStages;
+        for (uint32_t k = 0; k < ahead; k++) tma_load<CG>(smem + k * S::stage + S::stage_a, &p.b_k, k * kTileK, p.piece0 + blockIdx.x * kTileN, full + 8 * k);
+    }
+    asm volatile("griddepcontrol.wait;" ::: "memory");
     const uint32_t m = p.meta->m;
     Plan<KIND, CG> plan(p, m);
     bool dead = false;
@@ -653,7 +713,8 @@ __global__ void __launch_bounds__(kMmaThreads, 1) rd_vocab_mma_kernel(const __gr
                     if (!bar_wait(empty + 8 * turn.s, turn.parity ^ 1)) { dead = true; break; }
                     if (warp == 0) {
                         // the copies of both thread blocks and both operands count at the first block's barrier
-                        if (rank == 0) bar_expect(full + 8 * turn.s, CG * S::stage);
+                        const uint32_t a_bytes = w.product == 2 ? S::stage_a : p.a_rows * kTileK * 2;
+                        if (rank == 0) bar_expect(full + 8 * turn.s, CG * (a_bytes + S::stage_b));
                         if (w.product == 2) {
 #pragma unroll
                             for (int j = 0; j < kRowsM / 64; j++) tma_load<CG>(a + j * 8192, &p.a_mn, m0 + 64 * j, kk, bar);
@@ -661,7 +722,8 @@ __global__ void __launch_bounds__(kMmaThreads, 1) rd_vocab_mma_kernel(const __gr
                             tma_load<CG>(a, &p.a_k, kk, m0, bar);
                         }
                     } else if (KIND != kGrads) {
-                        tma_load<CG>(b, &p.b_k, kk, p.piece0 + n0, bar);
+                        if (ahead) ahead--;
+                        else tma_load<CG>(b, &p.b_k, kk, p.piece0 + n0, bar);
                     } else {
                         const CUtensorMap *map = w.product == 1 ? &p.b_mn : &p.b2_mn;
                         const uint32_t y = w.product == 1 ? p.piece0 + kk : kk;
@@ -809,6 +871,23 @@ __global__ void __launch_bounds__(kMmaThreads, 1) rd_vocab_mma_kernel(const __gr
                             tma_store(&p.dx_out, box, col - 32, row0);
                             box_sent();
                         }
+                    } else if (w.product == 1 && p.gh) {
+                        if (row < m) {
+                            uint16_t *dst = p.gh + size_t(p.index[row]) * p.gh_stride + col;
+#pragma unroll
+                            for (int q = 0; q < 4; q++) {
+                                uint32_t o[4];
+#pragma unroll
+                                for (int j = 0; j < 4; j++) o[j] = pack2<BF16>(__uint_as_float(v[8 * q + 2 * j]) * unboost, __uint_as_float(v[8 * q + 2 * j + 1]) * unboost);
+                                if (p.gh_wide && col + 8 * q + 8 <= p.dim) {
+                                    *reinterpret_cast<uint4 *>(dst + 8 * q) = make_uint4(o[0], o[1], o[2], o[3]);
+                                } else {
+#pragma unroll
+                                    for (int j = 0; j < 8; j++)
+                                        if (col + 8 * q + j < p.dim) dst[8 * q + j] = uint16_t(o[j / 2] >> (j & 1 ? 16 : 0));
+                                }
+                            }
+                        }
                     } else if (w.product == 1) {
                         box_wait(lane, false);
 #pragma unroll
@@ -867,6 +946,19 @@ __global__ void __launch_bounds__(kMmaThreads, 1) rd_vocab_mma_kernel(const __gr
             if (w.kblocks) tile++;
         }
         if (KIND != kStats && lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
+        if (KIND == kStats && p.joins) {
+            // few tokens: the block that is last joins the statistics, a warp per token
+            __threadfence();
+            asm volatile("bar.sync 1, %0;" ::"n"(32 * kEpilogueWarps) : "memory");
+            if (threadIdx.x == 128) asm volatile("st.shared.b32 [%0], %1;" ::"r"(tmem_slot + 4), "r"(atomicAdd(&p.meta->done, 1u)) : "memory");
+            asm volatile("bar.sync 1, %0;" ::"n"(32 * kEpilogueWarps) : "memory");
+            uint32_t before;
+            asm volatile("ld.shared.b32 %0, [%1];" : "=r"(before) : "r"(tmem_slot + 4) : "memory");
+            if (before == gridDim.x - 1) {
+                __threadfence();
+                for (uint32_t row = warp - 4; row < m; row += kEpilogueWarps) join_row(p.join, row, lane);
+            }
+        }
     }
     __syncwarp();
     pair_sync<CG>();                             // neither block of a pair leaves while the other may still signal it
@@ -878,54 +970,11 @@ __global__ void __launch_bounds__(kMmaThreads, 1) rd_vocab_mma_kernel(const __gr
 
 // ------------------------------------------------------------------------------------------------ joins
 
-struct JoinParams {
-    const float2 *part;
-    const float *packed_target;
-    const int *index, *label;
-    const Meta *meta;
-    uint32_t parts;
-    float z;
-    float *loss, *lse, *target;
-};
-
-// A warp per packed row.
 __global__ void __launch_bounds__(256) rd_vocab_join_kernel(JoinParams p)
 {
     pdl_start();
-    const int lane = threadIdx.x & 31;
     const uint32_t row = blockIdx.x * 8 + (threadIdx.x >> 5);
-    if (row >= p.meta->m) return;
-    float top = -INFINITY, sum = 0.0f;
-    auto add = [&](float2 x) {
-        const float most = fmaxf(top, x.x);
-        const float ref = fabsf(most) == INFINITY ? 0.0f : most;
-        // a part whose maximum is infinite has its sum relative to 0 already
-        const float a = fabsf(top) == INFINITY ? sum : sum * exp2f(top - ref);
-        const float b = fabsf(x.x) == INFINITY ? x.y : x.y * exp2f(x.x - ref);
-        sum = a + b;
-        top = most;
-    };
-    const float2 *part = p.part + size_t(row) * p.parts;
-    uint32_t k = lane;
-    for (; k + 96 < p.parts; k += 128) {
-        float2 x[4];
-#pragma unroll
-        for (int u = 0; u < 4; u++) x[u] = part[k + 32 * u];
-#pragma unroll
-        for (int u = 0; u < 4; u++) add(x[u]);
-    }
-    for (; k < p.parts; k += 32) add(part[k]);
-#pragma unroll
-    for (int d = 16; d; d /= 2) add(make_float2(__shfl_down_sync(0xffffffffu, top, d), __shfl_down_sync(0xffffffffu, sum, d)));
-    if (lane) return;
-    const float ref = fabsf(top) == INFINITY ? 0.0f : top;
-    const float lse = (ref + log2f(sum)) * kLn2;
-    const float target = p.label[row] >= 0 ? p.packed_target[row] : 0.0f;
-    const int i = p.index[row];
-    // without the penalty an infinite lse is an infinite loss, not 0 * inf
-    if (p.loss) p.loss[i] = p.z != 0.0f ? lse - target + p.z * lse * lse : lse - target;
-    if (p.lse) p.lse[i] = lse;
-    if (p.target) p.target[i] = target;
+    if (row < p.meta->m) join_row(p, row, threadIdx.x & 31);
 }
 
 struct FinishParams {
@@ -998,6 +1047,7 @@ bool needs_align(const VocabArgs &a) { return reinterpret_cast<uintptr_t>(a.weig
 int pair_or_single(size_t n) { return n > kRowsM ? 2 : 1; }
 
 constexpr size_t kSms = 148;
+constexpr double kFinishSteps = 9;        // what the kernel that adds up dh costs, in steps of the summed index
 
 // Parts that the sum over a piece is cut into for dh.  More parts fill the groups of thread blocks more evenly, but each is a
 // matrix of its own that is written and read once more; times in steps of the summed index (0.28 us on an SM).
@@ -1013,7 +1063,8 @@ size_t dh_splits(const VocabArgs &a, size_t piece)
         const size_t units = tiles * s;
         const double unit = double((size_t(k_piece) + s - 1) / s + kTileOverhead), even = (double(units) * unit + dw) / double(groups);
         const double longest = double((units + groups - 1) / groups) * unit;
-        const double time = (even > longest ? even : longest) + double(s) * double(a.n * a.dim) * 8 / step_bytes;
+        const bool whole = s == 1 && a.rows <= piece;          // written as it is, by no further kernel
+        const double time = (even > longest ? even : longest) + (whole ? 0 : double(s) * double(a.n * a.dim) * 8 / step_bytes + kFinishSteps);
         if (s == 1 || time < best_time) best = s, best_time = time;
     }
     return best;
@@ -1037,7 +1088,7 @@ Layout lay_out(const VocabArgs &a, bool gradient, bool want_hidden)
     if (a.n == 0) return l;
     Part w(a.workspace);
     l.rows_padded = round_up(a.n, kRowPad);
-    l.packed_stride = round_up(a.dim, 8);
+    l.packed_stride = round_up(a.dim, 64);
     l.meta = w.take<Meta>(1);
     l.tiles = w.take<TileCount>((a.n + kCountTile - 1) / kCountTile);
     l.index = w.take<int>(l.rows_padded);
@@ -1059,7 +1110,7 @@ Layout lay_out(const VocabArgs &a, bool gradient, bool want_hidden)
         l.dx = w.take<uint16_t>(l.rows_padded * l.dx_stride);
         l.dh_stride = l.packed_stride;
         l.splits = want_hidden ? dh_splits(a, l.piece) : 1;
-        if (want_hidden) l.dh = w.take<float>(l.splits * a.n * l.dh_stride);
+        if (want_hidden && (l.splits > 1 || a.rows > l.piece)) l.dh = w.take<float>(l.splits * a.n * l.dh_stride);
     }
     l.bytes = w.at;
     return l;
@@ -1212,15 +1263,24 @@ uint32_t token_group(size_t dim, size_t tile_m)
     return uint32_t(g < 1 ? 1 : g > 64 ? 64 : g);
 }
 
+// Rows of a left operand that a thread block brings in: all 128, or as many as there are tokens.
+size_t a_rows(size_t n) { return n < kRowsM ? round_up(n, 8) : kRowsM; }
+
 void common(MmaParams &q, const VocabArgs &a, const Layout &l, int cg)
 {
     q.meta = l.meta;
     q.label = l.label;
     q.dim = uint32_t(a.dim);
     q.group = token_group(a.dim, size_t(kRowsM) * cg);
+    q.index = l.index;
+    q.early = l.weight == nullptr;
+    q.a_rows = uint32_t(a_rows(a.n));
     q.scale = a.scale;
     q.scale2 = a.scale * kLog2e;
 }
+
+// Up to two tokens per epilogue warp the last thread block joins the statistics itself; more get a kernel of their own.
+constexpr size_t kJoinInside = 2 * kEpilogueWarps;
 
 }  // namespace
 
@@ -1240,18 +1300,19 @@ cudaError_t vocab_loss(const VocabArgs &a)
     if (e != cudaSuccess) return e;
     MmaParams q{};
     common(q, a, l, cg);
-    if (!encode(&q.a_k, a.bf16, l.packed, a.dim, l.rows_padded, l.packed_stride, kRowsM) || !encode(&q.b_k, a.bf16, weight, a.dim, a.rows, weight_stride, kTileN / cg))
+    if (!encode(&q.a_k, a.bf16, l.packed, a.dim, l.rows_padded, l.packed_stride, uint32_t(a_rows(a.n))) || !encode(&q.b_k, a.bf16, weight, a.dim, a.rows, weight_stride, kTileN / cg))
         return cudaErrorInvalidValue;
     q.part = l.part;
     q.parts = uint32_t(2 * ((a.rows + kTileN - 1) / kTileN));
     q.target = l.target;
     q.piece0 = 0;
     q.piece = uint32_t(a.rows);
+    q.join = JoinParams{l.part, l.target, l.index, l.label, l.meta, q.parts, a.z_loss, a.loss, a.lse_out, a.target};
+    q.joins = a.n <= kJoinInside;
     const size_t units = (a.n + tile_m - 1) / tile_m * ((a.rows + kTileN - 1) / kTileN);
     e = launch_mma<kStats>(q, a.bf16, cg, device, units, a.stream);
-    if (e != cudaSuccess) return e;
-    const JoinParams j{l.part, l.target, l.index, l.label, l.meta, q.parts, a.z_loss, a.loss, a.lse_out, a.target};
-    return launch(rd_vocab_join_kernel, unsigned((a.n + 7) / 8), 256, a.stream, j);
+    if (e != cudaSuccess || q.joins) return e;
+    return launch(rd_vocab_join_kernel, unsigned((a.n + 7) / 8), 256, a.stream, q.join);
 }
 
 size_t vocab_loss_grad_workspace(const VocabArgs &a, bool want_hidden) { return lay_out(a, true, want_hidden).bytes; }
@@ -1281,11 +1342,17 @@ cudaError_t vocab_loss_grad(const VocabArgs &a)
     grads.dw_tma = reinterpret_cast<uintptr_t>(a.grad_weight) % 16 == 0 && a.grad_weight_stride % 8 == 0;
     grads.want_dh = a.grad_hidden != nullptr;
     grads.want_dw = a.grad_weight != nullptr;
-    if (!encode(&logits.a_k, a.bf16, l.packed, a.dim, l.rows_padded, l.packed_stride, kRowsM) || !encode(&logits.b_k, a.bf16, weight, a.dim, a.rows, weight_stride, kTileN / cg) ||
-        !encode(&grads.a_k, a.bf16, l.dx, l.dx_stride, l.rows_padded, l.dx_stride, kRowsM) || !encode(&grads.a_mn, a.bf16, l.dx, l.dx_stride, l.rows_padded, l.dx_stride, 64) ||
+    if (!encode(&logits.a_k, a.bf16, l.packed, a.dim, l.rows_padded, l.packed_stride, uint32_t(a_rows(a.n))) || !encode(&logits.b_k, a.bf16, weight, a.dim, a.rows, weight_stride, kTileN / cg) ||
+        !encode(&grads.a_k, a.bf16, l.dx, l.dx_stride, l.rows_padded, l.dx_stride, uint32_t(a_rows(a.n))) || !encode(&grads.a_mn, a.bf16, l.dx, l.dx_stride, l.rows_padded, l.dx_stride, 64) ||
         !encode(&logits.dx_out, a.bf16, l.dx, l.dx_stride, l.rows_padded, l.dx_stride, 32) || !encode(&grads.b_mn, a.bf16, weight, a.dim, a.rows, weight_stride, 64) || !encode(&grads.b2_mn, a.bf16, l.packed, a.dim, l.rows_padded, l.packed_stride, 64))
         return cudaErrorInvalidValue;
-    if (grads.want_dh && !encode_dh(&grads.dh_out, l.dh, l.dh_stride, a.n, l.splits)) return cudaErrorInvalidValue;
+    const bool whole = l.splits == 1 && a.rows <= l.piece;
+    if (grads.want_dh && whole) {
+        grads.gh = static_cast<uint16_t *>(a.grad_hidden);
+        grads.gh_stride = a.grad_hidden_stride;
+        grads.gh_wide = reinterpret_cast<uintptr_t>(a.grad_hidden) % 16 == 0 && a.grad_hidden_stride % 8 == 0;
+    }
+    if (grads.want_dh && !whole && !encode_dh(&grads.dh_out, l.dh, l.dh_stride, a.n, l.splits)) return cudaErrorInvalidValue;
     if (grads.want_dw && grads.dw_tma && !encode(&grads.dw_out, a.bf16, a.grad_weight, a.dim, a.rows, a.grad_weight_stride, 32)) return cudaErrorInvalidValue;
     const size_t tiles_m = (a.n + tile_m - 1) / tile_m, tiles_d = (a.dim + kTileN - 1) / kTileN;
     for (size_t v = 0; v < a.rows; v += l.piece) {
@@ -1299,7 +1366,7 @@ cudaError_t vocab_loss_grad(const VocabArgs &a)
         e = launch_mma<kGrads>(grads, a.bf16, cg, device, units, a.stream);
         if (e != cudaSuccess) return e;
     }
-    if (a.grad_hidden) {
+    if (a.grad_hidden && !whole) {
         const bool wide = reinterpret_cast<uintptr_t>(a.grad_hidden) % 8 == 0 && a.grad_hidden_stride % 4 == 0;
         const FinishParams f{l.dh, l.index, l.meta, a.n, l.dh_stride, a.grad_hidden_stride, uint32_t(a.dim), uint32_t(l.splits), static_cast<uint16_t *>(a.grad_hidden), wide};
         const dim3 grid(unsigned(a.n < 65536 ? a.n : 65536), unsigned((a.dim + kFinishColumns - 1) / kFinishColumns));
