@@ -481,12 +481,24 @@ def _vector(t, what, n, device):
     return t.data_ptr()
 
 
-def _workspace(given, need, device):
-    if given is None:
-        given = _torch.empty(need, dtype=_torch.uint8, device="cuda")
-    elif given.get_device() != device or not given.is_contiguous():
-        raise ValueError("workspace must be a contiguous CUDA tensor on the operands' device")
-    return given.data_ptr(), given.numel() * given.element_size(), given
+class _Workspace:
+    """Temporary memory of a call: the caller's tensor, or torch's allocator's, given back to it (in the stream's order: it may be
+    handed out again behind the call) as soon as the call is enqueued.  A tensor object would cost more than the memory."""
+    __slots__ = ("address", "size", "own")
+
+    def __init__(self, given, need, device, stream):
+        self.own = False
+        if given is None:
+            self.size, self.address = need, _torch._C._cuda_cudaCachingAllocator_raw_alloc(need, stream) if need else 0
+            self.own = need > 0
+        else:
+            if given.get_device() != device or not given.is_contiguous():
+                raise ValueError("workspace must be a contiguous CUDA tensor on the operands' device")
+            self.size, self.address = given.numel() * given.element_size(), given.data_ptr()
+
+    def __del__(self):
+        if self.own:
+            _torch._C._cuda_cudaCachingAllocator_raw_delete(self.address)
 
 
 def rd_embed(table, ids, out=None, first_row=0, scale=1.0, stream=None):
@@ -526,9 +538,10 @@ def rd_embed_grad(grad_out, ids, grad_table, first_row=0, scale=1.0, accumulate=
     ids_addr = _vector(ids, "ids", n, device)
     if grad_table.shape[1] != dim or grad_table.get_device() != device:
         raise ValueError("grad_table must be [rows, dim] on grad_out's device")
-    ws, size, _keep = _workspace(workspace, rd_embed_grad_workspace(rows, dim, n), device)
+    s = _stream(device)
+    ws = _Workspace(workspace, rd_embed_grad_workspace(rows, dim, n), device, s)
     _check(lib().rd_embed_grad(addr, stride, _code(grad_out), ids_addr, _code(ids), n, first_row, scale, taddr, tstride, _code(grad_table),
-                               rows, dim, int(accumulate), ws, size, _stream(device)), "rd_embed_grad")
+                               rows, dim, int(accumulate), ws.address, ws.size, s), "rd_embed_grad")
     return grad_table
 
 
@@ -560,9 +573,10 @@ def rd_vocab_loss(hidden, weight, labels, first_row=0, scale=1.0, z_loss=0.0, wo
     out = hidden.new_empty((3, n), dtype=_torch.float32)
     need = C.c_size_t()
     _check(lib().rd_vocab_loss_workspace(ref, C.byref(need)), "rd_vocab_loss")
-    ws, size, _keep = _workspace(workspace, need.value, device)
+    s = _stream(device)
+    ws = _Workspace(workspace, need.value, device, s)
     at = out.data_ptr()
-    _check(lib().rd_vocab_loss(ref, at, at + 4 * n, at + 8 * n, ws, size, _stream(device)), "rd_vocab_loss")
+    _check(lib().rd_vocab_loss(ref, at, at + 4 * n, at + 8 * n, ws.address, ws.size, s), "rd_vocab_loss")
     return out.unbind()
 
 
@@ -599,8 +613,9 @@ def rd_vocab_loss_grad(hidden, weight, labels, lse, grad_loss, grad_hidden=None,
         _like(grad_weight, weight)
     need = C.c_size_t()
     _check(lib().rd_vocab_loss_grad_workspace(ref, grad_hidden is not None, grad_weight is not None, C.byref(need)), "rd_vocab_loss_grad")
-    ws, size, _keep = _workspace(workspace, need.value, device)
-    _check(lib().rd_vocab_loss_grad(ref, lse_addr, grad_loss.data_ptr(), grad_loss.stride(0), *gh, *gw, ws, size, _stream(device)),
+    s = _stream(device)
+    ws = _Workspace(workspace, need.value, device, s)
+    _check(lib().rd_vocab_loss_grad(ref, lse_addr, grad_loss.data_ptr(), grad_loss.stride(0), *gh, *gw, ws.address, ws.size, s),
            "rd_vocab_loss_grad")
     return grad_hidden, grad_weight
 

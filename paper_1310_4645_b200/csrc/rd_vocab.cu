@@ -42,7 +42,7 @@ constexpr float kLn2 = 0.6931471805599453f;
 struct Meta {
     uint32_t m;               // packed rows
     float boost, unboost;     // power of two that dx is multiplied by, and its inverse
-    uint32_t done;            // loss of few tokens: thread blocks that have their part of the statistics written
+    uint32_t pad;
 };
 struct TileCount {
     uint32_t n;               // tokens of the tile that count
@@ -265,40 +265,39 @@ struct JoinParams {
     float *loss, *lse, *target;
 };
 
-// Joins a packed row's parts, by a warp.
-__device__ __forceinline__ void join_row(const JoinParams &p, uint32_t row, int lane)
+// Joins (maximum, sum) with another; a part whose maximum is infinite has its sum relative to 0.
+__device__ __forceinline__ void join_parts(float2 &x, float2 y)
 {
-    float top = -INFINITY, sum = 0.0f;
-    auto add = [&](float2 x) {
-        const float most = fmaxf(top, x.x);
-        const float ref = fabsf(most) == INFINITY ? 0.0f : most;
-        // a part whose maximum is infinite has its sum relative to 0 already
-        const float a = fabsf(top) == INFINITY ? sum : sum * exp2f(top - ref);
-        const float b = fabsf(x.x) == INFINITY ? x.y : x.y * exp2f(x.x - ref);
-        sum = a + b;
-        top = most;
-    };
-    const float2 *part = p.part + size_t(row) * p.parts;
+    const float most = fmaxf(x.x, y.x), ref = fabsf(most) == INFINITY ? 0.0f : most;
+    const float a = fabsf(x.x) == INFINITY ? x.y : x.y * exp2f(x.x - ref), b = fabsf(y.x) == INFINITY ? y.y : y.y * exp2f(y.x - ref);
+    x = make_float2(most, a + b);
+}
+// A row's parts, joined by a warp; the result is lane 0's.
+__device__ __forceinline__ float2 join_row(const float2 *part, uint32_t parts, int lane)
+{
+    float2 x = make_float2(-INFINITY, 0.0f);
     uint32_t k = lane;
-    for (; k + 96 < p.parts; k += 128) {
-        float2 x[4];
+    for (; k + 96 < parts; k += 128) {
+        float2 y[4];
 #pragma unroll
-        for (int u = 0; u < 4; u++) x[u] = __ldcg(part + k + 32 * u);
+        for (int u = 0; u < 4; u++) y[u] = part[k + 32 * u];
 #pragma unroll
-        for (int u = 0; u < 4; u++) add(x[u]);
+        for (int u = 0; u < 4; u++) join_parts(x, y[u]);
     }
-    for (; k < p.parts; k += 32) add(__ldcg(part + k));
+    for (; k < parts; k += 32) join_parts(x, part[k]);
 #pragma unroll
-    for (int d = 16; d; d /= 2) add(make_float2(__shfl_down_sync(0xffffffffu, top, d), __shfl_down_sync(0xffffffffu, sum, d)));
+    for (int d = 16; d; d /= 2) join_parts(x, make_float2(__shfl_down_sync(0xffffffffu, x.x, d), __shfl_down_sync(0xffffffffu, x.y, d)));
+    return x;
+}
+__device__ __forceinline__ void write_row(float2 x, bool counts, float target, float z, size_t i, int lane, float *loss, float *lse_out, float *target_out)
+{
     if (lane) return;
-    const float ref = fabsf(top) == INFINITY ? 0.0f : top;
-    const float lse = (ref + log2f(sum)) * kLn2;
-    const float target = p.label[row] >= 0 ? __ldcg(p.packed_target + row) : 0.0f;
-    const int i = p.index[row];
+    const float ref = fabsf(x.x) == INFINITY ? 0.0f : x.x;
+    const float lse = counts ? (ref + log2f(x.y)) * kLn2 : 0.0f;
     // without the penalty an infinite lse is an infinite loss, not 0 * inf
-    if (p.loss) p.loss[i] = p.z != 0.0f ? lse - target + p.z * lse * lse : lse - target;
-    if (p.lse) p.lse[i] = lse;
-    if (p.target) p.target[i] = target;
+    if (loss) loss[i] = !counts ? 0.0f : z != 0.0f ? lse - target + z * lse * lse : lse - target;
+    if (lse_out) lse_out[i] = lse;
+    if (target_out) target_out[i] = target;
 }
 
 enum { kStats = 0, kDlogits = 1, kGrads = 2 };
@@ -312,10 +311,9 @@ struct alignas(64) MmaParams {
     CUtensorMap dx_out;       // dx, 64 x 32 boxes
     CUtensorMap dh_out;       // dh, 32 x 32 x 1 boxes
     CUtensorMap dw_out;       // grad_weight, 64 x 32 boxes
-    Meta *meta;
+    const Meta *meta;
     const int *label, *index;
     const float *gp, *gt, *lse2;
-    JoinParams join;
     float2 *part;             // stats: (maximum, sum) in base 2, [packed row][half tile]
     float *target;            // stats: the label's logit, per packed row
     uint16_t *dw;             // grad_weight, for rows that TMA cannot address
@@ -329,7 +327,7 @@ struct alignas(64) MmaParams {
     uint32_t a_rows;          // rows of a thread block's left operand that are brought in (fewer than 128 for few tokens)
     bool first_piece, want_dh, want_dw, dw_tma;
     bool early;               // the weight is the caller's own: it may be read before the kernels of this call are done
-    bool gh_wide, joins;      // 16-byte rows of grad_hidden; the last thread block joins the statistics
+    bool gh_wide;             // 16-byte rows of grad_hidden
     float scale2;             // scale * log2(e)
     float scale;
 };
@@ -946,19 +944,6 @@ __global__ void __launch_bounds__(kMmaThreads, 1) rd_vocab_mma_kernel(const __gr
             if (w.kblocks) tile++;
         }
         if (KIND != kStats && lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
-        if (KIND == kStats && p.joins) {
-            // few tokens: the block that is last joins the statistics, a warp per token
-            __threadfence();
-            asm volatile("bar.sync 1, %0;" ::"n"(32 * kEpilogueWarps) : "memory");
-            if (threadIdx.x == 128) asm volatile("st.shared.b32 [%0], %1;" ::"r"(tmem_slot + 4), "r"(atomicAdd(&p.meta->done, 1u)) : "memory");
-            asm volatile("bar.sync 1, %0;" ::"n"(32 * kEpilogueWarps) : "memory");
-            uint32_t before;
-            asm volatile("ld.shared.b32 %0, [%1];" : "=r"(before) : "r"(tmem_slot + 4) : "memory");
-            if (before == gridDim.x - 1) {
-                __threadfence();
-                for (uint32_t row = warp - 4; row < m; row += kEpilogueWarps) join_row(p.join, row, lane);
-            }
-        }
     }
     __syncwarp();
     pair_sync<CG>();                             // neither block of a pair leaves while the other may still signal it
@@ -974,7 +959,144 @@ __global__ void __launch_bounds__(256) rd_vocab_join_kernel(JoinParams p)
 {
     pdl_start();
     const uint32_t row = blockIdx.x * 8 + (threadIdx.x >> 5);
-    if (row < p.meta->m) join_row(p, row, threadIdx.x & 31);
+    const int lane = threadIdx.x & 31;
+    if (row >= p.meta->m) return;
+    const float2 x = join_row(p.part + size_t(row) * p.parts, p.parts, lane);
+    write_row(x, true, p.label[row] >= 0 ? p.packed_target[row] : 0.0f, p.z, size_t(p.index[row]), lane, p.loss, p.lse, p.target);
+}
+
+// ------------------------------------------------------------------------------------------------ loss of a few tokens
+
+// Up to four tokens, as when a server scores what it generates: the weight's bytes are all that counts, so no tensor cores and no
+// packing, but warps that stream four rows of the weight at a time past the hidden rows in shared memory.
+constexpr size_t kFewTokens = 4;
+constexpr size_t kFewBytes = 32768;       // of hidden rows in shared memory
+constexpr int kFewRows = 4;
+constexpr unsigned kFewBlocks = 148 * 3;  // what fits at once
+
+struct FewParams {
+    const uint16_t *hidden, *weight;
+    const void *labels;
+    size_t hidden_stride, weight_stride;
+    uint32_t n, rows, dim;
+    long long first;
+    bool wide_labels;
+    float scale, scale2, z;
+    float2 *part;             // [token][thread block]
+    float *packed_target;     // per token
+    uint32_t parts;
+    float *loss, *lse, *target;
+};
+
+template <bool BF16> __device__ __forceinline__ float2 widen2(uint32_t v)
+{
+    if (BF16) return make_float2(__uint_as_float(v << 16), __uint_as_float(v & 0xffff0000u));
+    return __half22float2(*reinterpret_cast<const __half2 *>(&v));
+}
+
+// V: elements per access, 8 or 1.  N: tokens, with room to spare.
+template <bool BF16, int V, int N> __global__ void __launch_bounds__(256, 3) rd_vocab_few_kernel(FewParams p)
+{
+    extern __shared__ __align__(16) unsigned char few_smem[];
+    uint16_t *h = reinterpret_cast<uint16_t *>(few_smem);            // N rows of `padded` elements, zeros behind dim
+    __shared__ float2 warp_part[8][N];
+    pdl_wait_first();
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const uint32_t padded = (p.dim + 7) / 8 * 8;
+    int label[N];
+#pragma unroll
+    for (int t = 0; t < N; t++) {
+        const long long l = t < int(p.n) ? label_of(p.labels, p.wide_labels, t) : -1;
+        label[t] = l >= p.first && l - p.first < static_cast<long long>(p.rows) ? int(l - p.first) : -1;
+        for (uint32_t j = threadIdx.x; j < padded; j += 256) h[t * padded + j] = t < int(p.n) && j < p.dim ? p.hidden[t * p.hidden_stride + j] : uint16_t(0);
+    }
+    __syncthreads();
+    float top[N], sum[N];
+#pragma unroll
+    for (int t = 0; t < N; t++) top[t] = -INFINITY, sum[t] = 0.0f;
+    for (uint32_t r0 = (blockIdx.x * 8 + warp) * kFewRows; r0 < p.rows; r0 += gridDim.x * 8 * kFewRows) {
+        const uint16_t *row[kFewRows];
+#pragma unroll
+        for (int r = 0; r < kFewRows; r++) row[r] = p.weight + size_t(min(r0 + r, p.rows - 1)) * p.weight_stride;
+        float acc[kFewRows][N] = {};
+        if (V == 8) {
+#pragma unroll 2
+            for (uint32_t j = lane * 8; j < p.dim; j += 256) {
+                uint4 x[kFewRows];
+#pragma unroll
+                for (int r = 0; r < kFewRows; r++) x[r] = __ldg(reinterpret_cast<const uint4 *>(row[r] + j));
+#pragma unroll
+                for (int t = 0; t < N; t++) {
+                    const uint4 y = *reinterpret_cast<const uint4 *>(h + t * padded + j);
+                    const float2 y0 = widen2<BF16>(y.x), y1 = widen2<BF16>(y.y), y2 = widen2<BF16>(y.z), y3 = widen2<BF16>(y.w);
+#pragma unroll
+                    for (int r = 0; r < kFewRows; r++) {
+                        const float2 x0 = widen2<BF16>(x[r].x), x1 = widen2<BF16>(x[r].y), x2 = widen2<BF16>(x[r].z), x3 = widen2<BF16>(x[r].w);
+                        float a = acc[r][t];
+                        a = fmaf(x0.x, y0.x, a), a = fmaf(x0.y, y0.y, a), a = fmaf(x1.x, y1.x, a), a = fmaf(x1.y, y1.y, a);
+                        a = fmaf(x2.x, y2.x, a), a = fmaf(x2.y, y2.y, a), a = fmaf(x3.x, y3.x, a), a = fmaf(x3.y, y3.y, a);
+                        acc[r][t] = a;
+                    }
+                }
+            }
+        } else {
+#pragma unroll 4
+            for (uint32_t j = lane; j < p.dim; j += 32) {
+#pragma unroll
+                for (int r = 0; r < kFewRows; r++) {
+                    const float x = widen2<BF16>(row[r][j]).x;
+#pragma unroll
+                    for (int t = 0; t < N; t++) acc[r][t] = fmaf(x, widen2<BF16>(h[t * padded + j]).x, acc[r][t]);
+                }
+            }
+        }
+#pragma unroll
+        for (int t = 0; t < N; t++) {
+            float most = top[t], y[kFewRows];
+#pragma unroll
+            for (int r = 0; r < kFewRows; r++) {
+                float a = acc[r][t];
+#pragma unroll
+                for (int d = 16; d; d /= 2) a += __shfl_xor_sync(0xffffffffu, a, d);
+                if (r0 + r == uint32_t(label[t]) && lane == 0) p.packed_target[t] = a * p.scale;
+                y[r] = r0 + r < p.rows ? a * p.scale2 : -INFINITY;
+                most = fmaxf(most, y[r]);
+            }
+            // an infinite maximum must not meet itself in a difference
+            const float ref = fabsf(most) == INFINITY ? 0.0f : most;
+            float s = fabsf(top[t]) == INFINITY ? sum[t] : sum[t] * exp2_fast(top[t] - ref);
+#pragma unroll
+            for (int r = 0; r < kFewRows; r++) s += exp2_fast(y[r] - ref);
+            sum[t] = s;
+            top[t] = most;
+        }
+    }
+    if (lane == 0) {
+#pragma unroll
+        for (int t = 0; t < N; t++) warp_part[warp][t] = make_float2(top[t], sum[t]);
+    }
+    __syncthreads();
+    if (warp == 0 && lane < 8) {
+#pragma unroll
+        for (int t = 0; t < N; t++) {
+            float2 x = warp_part[lane][t];
+#pragma unroll
+            for (int d = 4; d; d /= 2) join_parts(x, make_float2(__shfl_down_sync(0xffu, x.x, d), __shfl_down_sync(0xffu, x.y, d)));
+            if (lane == 0 && t < int(p.n)) p.part[size_t(t) * p.parts + blockIdx.x] = x;
+        }
+    }
+}
+
+// A warp per token.
+__global__ void __launch_bounds__(32 * kFewTokens) rd_vocab_few_join_kernel(FewParams p)
+{
+    pdl_start();
+    const int lane = threadIdx.x & 31;
+    const uint32_t t = threadIdx.x >> 5;
+    if (t >= p.n) return;
+    const long long l = label_of(p.labels, p.wide_labels, t);
+    const bool here = l >= p.first && l - p.first < static_cast<long long>(p.rows);
+    write_row(join_row(p.part + size_t(t) * p.parts, p.parts, lane), l >= 0, here ? p.packed_target[t] : 0.0f, p.z, t, lane, p.loss, p.lse, p.target);
 }
 
 struct FinishParams {
@@ -1279,15 +1401,67 @@ void common(MmaParams &q, const VocabArgs &a, const Layout &l, int cg)
     q.scale2 = a.scale * kLog2e;
 }
 
-// Up to two tokens per epilogue warp the last thread block joins the statistics itself; more get a kernel of their own.
-constexpr size_t kJoinInside = 2 * kEpilogueWarps;
+// Measured on B200, weight 32768 x 1024, the tensor core path / this one: 1 token 18.7 / FEW1 us, 4 tokens FEWA / FEWB us.
+bool is_few(const VocabArgs &a) { return a.n <= kFewTokens && a.n * round_up(a.dim, 8) * 2 <= kFewBytes; }
+
+template <bool BF16, int V, int N> cudaError_t launch_few(const VocabArgs &a, const FewParams &p, unsigned blocks)
+{
+    cudaLaunchConfig_t c{};
+    cudaLaunchAttribute pdl = pdl_attribute();
+    c.gridDim = dim3(blocks);
+    c.blockDim = dim3(256);
+    c.dynamicSmemBytes = unsigned(N * round_up(a.dim, 8) * 2);
+    c.stream = a.stream;
+    c.attrs = &pdl;
+    c.numAttrs = 1;
+    return cudaLaunchKernelEx(&c, rd_vocab_few_kernel<BF16, V, N>, p);
+}
+template <bool BF16, int V> cudaError_t launch_few(const VocabArgs &a, const FewParams &p, unsigned blocks)
+{
+    return a.n == 1 ? launch_few<BF16, V, 1>(a, p, blocks) : a.n == 2 ? launch_few<BF16, V, 2>(a, p, blocks) : launch_few<BF16, V, 4>(a, p, blocks);
+}
+
+cudaError_t vocab_loss_few(const VocabArgs &a)
+{
+    Part w(a.workspace);
+    const unsigned wanted = unsigned((a.rows + 8 * kFewRows - 1) / (8 * kFewRows)), blocks = wanted < kFewBlocks ? wanted : kFewBlocks;
+    FewParams p{};
+    p.hidden = static_cast<const uint16_t *>(a.hidden);
+    p.weight = static_cast<const uint16_t *>(a.weight);
+    p.labels = a.labels;
+    p.hidden_stride = a.hidden_stride;
+    p.weight_stride = a.weight_stride;
+    p.n = uint32_t(a.n);
+    p.rows = uint32_t(a.rows);
+    p.dim = uint32_t(a.dim);
+    p.first = a.first_row;
+    p.wide_labels = a.wide_labels;
+    p.scale = a.scale;
+    p.scale2 = a.scale * kLog2e;
+    p.z = a.z_loss;
+    p.part = w.take<float2>(kFewTokens * kFewBlocks);
+    p.packed_target = w.take<float>(kFewTokens);
+    p.parts = blocks;
+    p.loss = a.loss;
+    p.lse = a.lse_out;
+    p.target = a.target;
+    const bool wide = reinterpret_cast<uintptr_t>(a.weight) % 16 == 0 && a.weight_stride % 8 == 0 && a.dim % 8 == 0;
+    const cudaError_t e = a.bf16 ? wide ? launch_few<true, 8>(a, p, blocks) : launch_few<true, 1>(a, p, blocks)
+                                 : wide ? launch_few<false, 8>(a, p, blocks) : launch_few<false, 1>(a, p, blocks);
+    if (e != cudaSuccess) return e;
+    return launch(rd_vocab_few_join_kernel, 1, 32 * kFewTokens, a.stream, p);
+}
 
 }  // namespace
 
-size_t vocab_loss_workspace(const VocabArgs &a) { return lay_out(a, false, false).bytes; }
+size_t vocab_loss_workspace(const VocabArgs &a)
+{
+    return is_few(a) && a.n ? 1024 * (round_up(kFewTokens * kFewBlocks * sizeof(float2), 1024) / 1024 + 1) : lay_out(a, false, false).bytes;
+}
 
 cudaError_t vocab_loss(const VocabArgs &a)
 {
+    if (is_few(a)) return vocab_loss_few(a);
     int device = 0;
     cudaError_t e = cudaGetDevice(&device);
     if (e != cudaSuccess) return e;
@@ -1307,12 +1481,11 @@ cudaError_t vocab_loss(const VocabArgs &a)
     q.target = l.target;
     q.piece0 = 0;
     q.piece = uint32_t(a.rows);
-    q.join = JoinParams{l.part, l.target, l.index, l.label, l.meta, q.parts, a.z_loss, a.loss, a.lse_out, a.target};
-    q.joins = a.n <= kJoinInside;
     const size_t units = (a.n + tile_m - 1) / tile_m * ((a.rows + kTileN - 1) / kTileN);
     e = launch_mma<kStats>(q, a.bf16, cg, device, units, a.stream);
-    if (e != cudaSuccess || q.joins) return e;
-    return launch(rd_vocab_join_kernel, unsigned((a.n + 7) / 8), 256, a.stream, q.join);
+    if (e != cudaSuccess) return e;
+    const JoinParams j{l.part, l.target, l.index, l.label, l.meta, q.parts, a.z_loss, a.loss, a.lse_out, a.target};
+    return launch(rd_vocab_join_kernel, unsigned((a.n + 7) / 8), 256, a.stream, j);
 }
 
 size_t vocab_loss_grad_workspace(const VocabArgs &a, bool want_hidden) { return lay_out(a, true, want_hidden).bytes; }

@@ -171,7 +171,7 @@ def loss_reference(hidden, weight, labels, first, scale, z):
     return loss, lse, target, x, err, here, torch.where(here, at, 0)
 
 
-SHAPES = [(1, 1, 1), (1, 300, 64), (2, 5, 3), (37, 257, 72), (128, 256, 64), (129, 511, 65), (300, 1000, 200), (513, 77, 1032), (40, 5000, 33), (1, 32768, 128)]
+SHAPES = [(1, 1, 1), (3, 1000, 4096), (4, 777, 1001), (4, 70000, 40), (1, 33, 16400), (1, 300, 64), (2, 5, 3), (37, 257, 72), (128, 256, 64), (129, 511, 65), (300, 1000, 200), (513, 77, 1032), (40, 5000, 33), (1, 32768, 128)]
 
 
 def vocab_case(n, rows, dim, dtype, seed, ignored=0.25, first=0, label_dtype=torch.int64):
@@ -238,12 +238,17 @@ def test_loss_special_values():
     assert torch.isnan(lse[1]) and torch.isnan(loss[1])
     rest = torch.arange(200, device="cuda") != 1
     assert torch.equal(lse[rest], clean[1][rest]) and torch.equal(loss[rest], clean[0][rest])
-    # one infinite logit: hidden e_0, weight rows 0 except a +-infinite one
-    h = torch.zeros(2, 8, dtype=torch.bfloat16, device="cuda")
+
+
+@gpu
+@pytest.mark.parametrize("n", [2, 20])
+def test_loss_infinite_logits(n):
+    # hidden e_0, weight rows 0 except a +-infinite one
+    h = torch.zeros(n, 8, dtype=torch.bfloat16, device="cuda")
     h[:, 0] = 1
     w = torch.zeros(300, 8, dtype=torch.bfloat16, device="cuda")
     w[299, 0] = float("-inf")
-    lab = torch.tensor([3, 4], device="cuda")
+    lab = torch.arange(n, device="cuda") + 3
     loss, lse, target = rd.rd_vocab_loss(h, w, lab)
     assert torch.allclose(lse, torch.full_like(lse, math.log(299)), rtol=1e-6)
     w[280, 0] = float("inf")
@@ -254,8 +259,12 @@ def test_loss_special_values():
     assert torch.isneginf(rd.rd_vocab_loss(h, w, lab)[1]).all()
     # very low and very high finite logits
     w[:, 0] = -30000.0
-    assert torch.allclose(rd.rd_vocab_loss(h, w, lab)[1].double().cpu(), torch.full((2,), w[0, 0].double().item() + math.log(300), dtype=torch.float64), rtol=1e-6)
-    # nothing counts
+    assert torch.allclose(rd.rd_vocab_loss(h, w, lab)[1].double().cpu(), torch.full((n,), w[0, 0].double().item() + math.log(300), dtype=torch.float64), rtol=1e-6)
+    # tokens that do not count, whatever they hold
+    lab[1] = -1
+    h[1] = float("nan")
+    loss, lse, target = rd.rd_vocab_loss(h, w, lab)
+    assert loss[1] == 0 and lse[1] == 0 and target[1] == 0 and torch.isfinite(lse).all()
     lab[:] = -100
     assert not any(t.any() for t in rd.rd_vocab_loss(h, w, lab))
     assert all(t.numel() == 0 for t in rd.rd_vocab_loss(h[:0], w, lab[:0]))
