@@ -550,3 +550,46 @@ def test_binding_refusals():
         with pytest.raises(rd.RdError) as e:
             f()
         assert e.value.status == rd.RD_ERR_UNSUPPORTED
+
+
+# ------------------------------------------------------------------------------------------------ the operators together
+
+
+@gpu
+@pytest.mark.parametrize("processes, algo", [(1, rd.RD_UNI_GREEDY), (4, rd.RD_UNI_GREEDY), (3, rd.RD_BINOMIAL), (8, rd.RD_BI_GREEDY)])
+def test_step_over_processes(processes, algo):
+    """A step on a vocabulary cut over processes against the same step on the whole table in 64 bits."""
+    from paper_1310_4645_b200.vocab_step import VocabStep
+    rows, dim, n = 96 * processes, 48, 70
+    table = rand(rows, dim, seed=120, dtype=torch.bfloat16, std=0.3)
+    ids, labels = ints(0, rows, n, seed=121), ints(0, rows, n, seed=122)
+    labels[::5] = -100
+    step = VocabStep(table, processes, n, algo)
+    try:
+        loss, grads = step.run(ids, labels, embed_scale=3.0, logit_scale=0.5, z_loss=1e-3)
+        w = table.double().requires_grad_()
+        h = w[ids] * 3.0
+        x = h @ w.T * 0.5
+        lse = torch.logsumexp(x, 1)
+        counts = labels >= 0
+        t = x.gather(1, labels.clamp(min=0)[:, None])[:, 0]
+        want = (torch.where(counts, lse - t + 1e-3 * lse * lse, 0.0)).sum() / counts.sum()
+        want.backward()
+        # the embedding is rounded to 16 bits once (only one process holds a row): x by 2^-8 of the magnitudes it sums, on average
+        # over dim terms of either sign far less; the loss inherits that absolutely
+        size = (h.abs() @ w.abs().T * 0.5).max().item()
+        assert abs(loss.item() - want.item()) <= 2.0 ** -8 * size
+        # gradients: five roundings to 16 bits (embedding, dx, dh per process, their sum, result), and probabilities off by 2^-8 * size
+        got = torch.cat(grads).double()
+        assert (got - w.grad).norm() <= (5 + size) * 2.0 ** -8 * w.grad.norm()
+        assert rd.rd_vocab_status() == rd.RD_OK
+    finally:
+        step.close()
+
+
+@gpu
+def test_step_command(capsys):
+    from paper_1310_4645_b200 import vocab_step
+    vocab_step.main(["--processes", "2", "--vocab", "512", "--dim", "64", "--tokens", "100", "--steps", "4"])
+    losses = [float(line.split()[3]) for line in capsys.readouterr().out.splitlines()]
+    assert len(losses) == 4 and all(map(math.isfinite, losses)) and losses[-1] < losses[0]
