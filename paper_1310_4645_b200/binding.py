@@ -424,101 +424,44 @@ def rd_destroy(h) -> None:
 # Vocabulary operators
 
 
-# A call costs its user a few microseconds of host time, as much as a small kernel, so the checks below are written for few
-# Python operations: integers instead of device objects, one dictionary per dtype, no context manager on the usual path.
+# A call costs its user host time, as much as a small kernel, so these marshal their tensors in C++ (csrc/rd_torch.cpp, the
+# module _rd_torch built beside librd.so): it checks them, allocates what is not given, calls librd.so on the tensors' device and
+# its current stream, and returns the result or a status.
 
-_DTYPES = None      # torch dtype -> rd_dtype_t, filled on first use (torch is imported lazily)
-_torch = None
+_module = None
 
 
-def _setup():
-    global _torch, _DTYPES
+def _native():
+    global _module
+    if _module is None:
+        import torch  # noqa: F401  (its libraries are the module's)
+        lib()
+        path = os.path.join(_HERE, "_rd_torch.so")
+        if not os.path.exists(path):
+            raise LibraryMissing("%s not found: build it with `python -m paper_1310_4645_b200.build`" % path)
+        from importlib import machinery, util
+        loader = machinery.ExtensionFileLoader("_rd_torch", path)
+        _module = util.module_from_spec(util.spec_from_loader("_rd_torch", loader, origin=path))
+        loader.exec_module(_module)
+    return _module
+
+
+def _on_stream(f, t, stream, *args):
+    """Makes a stream current for a call, so that what it allocates belongs to that stream."""
     import torch
-    _DTYPES = {torch.int32: RD_INT32, torch.float32: RD_FP32, torch.int64: RD_INT64, torch.float64: RD_FP64,
-               torch.bfloat16: RD_BF16, torch.float16: RD_FP16}
-    _torch = torch
-
-
-def _elsewhere(t, stream):
-    """Whether a call has to change the current device or stream first."""
-    if _torch is None:
-        _setup()
-    return stream is not None or t.get_device() != _torch.cuda.current_device()
-
-
-def _there(f, t, stream, *args, **kw):
-    """Makes the tensor's device and the stream current for a call, so that what it allocates belongs to that stream."""
-    if not t.is_cuda:
-        raise ValueError("CUDA tensors are expected")
-    with _torch.cuda.device(t.device):
-        with _torch.cuda.stream(stream if stream is not None else _torch.cuda.current_stream()):
-            return f(*args, **kw)
-
-
-def _stream(device):
-    return _torch._C._cuda_getCurrentRawStream(device)
-
-
-def _code(t):
-    code = _DTYPES.get(t.dtype)
-    return code if code is not None else _dtype_code(t)
-
-
-def _matrix(t, what):
-    """A 2-D CUDA tensor whose rows are contiguous: (address, row stride in elements)."""
-    if not t.is_cuda or t.dim() != 2:
-        raise ValueError("%s must be a 2-D CUDA tensor" % what)
-    stride, inner = t.stride()
-    rows, dim = t.shape
-    if inner != 1 and dim > 1:
-        raise ValueError("the rows of %s must be contiguous" % what)
-    return t.data_ptr(), stride if rows > 1 else dim
-
-
-def _vector(t, what, n, device):
-    if t.get_device() != device or t.shape != (n,) or not t.is_contiguous():
-        raise ValueError("%s must be a contiguous CUDA vector with one value per token, on the operands' device" % what)
-    return t.data_ptr()
-
-
-class _Workspace:
-    """Temporary memory of a call: the caller's tensor, or torch's allocator's, given back to it (in the stream's order: it may be
-    handed out again behind the call) as soon as the call is enqueued.  A tensor object would cost more than the memory."""
-    __slots__ = ("address", "size", "own")
-
-    def __init__(self, given, need, device, stream):
-        self.own = False
-        if given is None:
-            self.size, self.address = need, _torch._C._cuda_cudaCachingAllocator_raw_alloc(need, stream) if need else 0
-            self.own = need > 0
-        else:
-            if given.get_device() != device or not given.is_contiguous():
-                raise ValueError("workspace must be a contiguous CUDA tensor on the operands' device")
-            self.size, self.address = given.numel() * given.element_size(), given.data_ptr()
-
-    def __del__(self):
-        if self.own:
-            _torch._C._cuda_cudaCachingAllocator_raw_delete(self.address)
+    with torch.cuda.device(t.device), torch.cuda.stream(stream):
+        return f(*args)
 
 
 def rd_embed(table, ids, out=None, first_row=0, scale=1.0, stream=None):
     """scale * table[ids - first_row], rows of zeros where the table does not hold an id.  table: [rows, dim] float32,
     bfloat16 or float16; ids: int32 or int64 vector; out: [n, dim] of table's dtype (allocated when None).  Returns out."""
-    if _elsewhere(table, stream):
-        return _there(rd_embed, table, stream, table, ids, out, first_row, scale)
-    addr, stride = _matrix(table, "table")
-    device, n, (rows, dim) = table.get_device(), ids.numel(), table.shape
-    ids_addr = _vector(ids, "ids", n, device)
-    if out is None:
-        out = table.new_empty((n, dim))
-        out_addr, out_stride = out.data_ptr(), dim
-    else:
-        out_addr, out_stride = _matrix(out, "out")
-        if out.shape != (n, dim) or out.dtype != table.dtype or out.get_device() != device:
-            raise ValueError("out must be [n, dim] with table's dtype and device")
-    _check(lib().rd_embed(addr, stride, rows, dim, _code(table), ids_addr, _code(ids), n, first_row, scale, out_addr, out_stride,
-                          _stream(device)), "rd_embed")
-    return out
+    if stream is not None:
+        return _on_stream(rd_embed, table, stream, table, ids, out, first_row, scale)
+    r = _native().embed(table, ids, out, first_row, scale)
+    if r.__class__ is int:
+        raise RdError(r, "rd_embed")
+    return r
 
 
 def rd_embed_grad_workspace(rows, dim, n) -> int:
@@ -530,61 +473,40 @@ def rd_embed_grad_workspace(rows, dim, n) -> int:
 def rd_embed_grad(grad_out, ids, grad_table, first_row=0, scale=1.0, accumulate=False, workspace=None, stream=None):
     """grad_table[v] (+)= scale * sum of grad_out[i] over the tokens with ids[i] - first_row = v.  grad_out: [n, dim]; grad_table:
     [rows, dim] of grad_out's dtype or float32; workspace: rd_embed_grad_workspace bytes (allocated when None).  Returns grad_table."""
-    if _elsewhere(grad_out, stream):
-        return _there(rd_embed_grad, grad_out, stream, grad_out, ids, grad_table, first_row, scale, accumulate, workspace)
-    addr, stride = _matrix(grad_out, "grad_out")
-    taddr, tstride = _matrix(grad_table, "grad_table")
-    device, (n, dim), rows = grad_out.get_device(), grad_out.shape, grad_table.shape[0]
-    ids_addr = _vector(ids, "ids", n, device)
-    if grad_table.shape[1] != dim or grad_table.get_device() != device:
-        raise ValueError("grad_table must be [rows, dim] on grad_out's device")
-    s = _stream(device)
-    ws = _Workspace(workspace, rd_embed_grad_workspace(rows, dim, n), device, s)
-    _check(lib().rd_embed_grad(addr, stride, _code(grad_out), ids_addr, _code(ids), n, first_row, scale, taddr, tstride, _code(grad_table),
-                               rows, dim, int(accumulate), ws.address, ws.size, s), "rd_embed_grad")
-    return grad_table
+    if stream is not None:
+        return _on_stream(rd_embed_grad, grad_out, stream, grad_out, ids, grad_table, first_row, scale, accumulate, workspace)
+    r = _native().embed_grad(grad_out, ids, grad_table, first_row, scale, accumulate, workspace)
+    if r.__class__ is int:
+        raise RdError(r, "rd_embed_grad")
+    return r
 
 
-def _vocab(hidden, weight, labels, first_row, scale, z_loss):
-    addr, stride = _matrix(hidden, "hidden")
-    waddr, wstride = _matrix(weight, "weight")
-    device, (n, dim), rows = hidden.get_device(), hidden.shape, weight.shape[0]
-    if weight.shape[1] != dim or weight.dtype != hidden.dtype or weight.get_device() != device:
-        raise ValueError("weight must be [rows, dim] with hidden's dtype and device")
-    return rd_vocab_t(addr, stride, waddr, wstride, _vector(labels, "labels", n, device), n, rows, dim, first_row, _code(hidden),
-                      _code(labels), scale, z_loss)
+def _vocab_shape(hidden, weight, labels):
+    """The operands as far as the workspace depends on them."""
+    return rd_vocab_t(hidden.data_ptr(), max(hidden.stride(0), hidden.shape[1]), weight.data_ptr(), max(weight.stride(0), weight.shape[1]),
+                      labels.data_ptr(), hidden.shape[0], weight.shape[0], hidden.shape[1], 0, _dtype_code(hidden), _dtype_code(labels), 1.0, 0.0)
 
 
 def rd_vocab_loss_workspace(hidden, weight, labels) -> int:
-    if _torch is None:
-        _setup()
     need = C.c_size_t()
-    _check(lib().rd_vocab_loss_workspace(C.byref(_vocab(hidden, weight, labels, 0, 1.0, 0.0)), C.byref(need)), "rd_vocab_loss_workspace")
+    _check(lib().rd_vocab_loss_workspace(C.byref(_vocab_shape(hidden, weight, labels)), C.byref(need)), "rd_vocab_loss_workspace")
     return need.value
 
 
 def rd_vocab_loss(hidden, weight, labels, first_row=0, scale=1.0, z_loss=0.0, workspace=None, stream=None):
     """Softmax cross entropy of the logits scale * hidden @ weight.T: (loss, lse, target), float32 vectors with one value per token,
     0 where the label is negative.  hidden: [n, dim], weight: [rows, dim], both bfloat16 or float16; labels: int32 or int64."""
-    if _elsewhere(hidden, stream):
-        return _there(rd_vocab_loss, hidden, stream, hidden, weight, labels, first_row, scale, z_loss, workspace)
-    v = _vocab(hidden, weight, labels, first_row, scale, z_loss)
-    device, n, ref = hidden.get_device(), hidden.shape[0], C.byref(v)
-    out = hidden.new_empty((3, n), dtype=_torch.float32)
-    need = C.c_size_t()
-    _check(lib().rd_vocab_loss_workspace(ref, C.byref(need)), "rd_vocab_loss")
-    s = _stream(device)
-    ws = _Workspace(workspace, need.value, device, s)
-    at = out.data_ptr()
-    _check(lib().rd_vocab_loss(ref, at, at + 4 * n, at + 8 * n, ws.address, ws.size, s), "rd_vocab_loss")
-    return out.unbind()
+    if stream is not None:
+        return _on_stream(rd_vocab_loss, hidden, stream, hidden, weight, labels, first_row, scale, z_loss, workspace)
+    r = _native().vocab_loss(hidden, weight, labels, first_row, scale, z_loss, workspace)
+    if r.__class__ is int:
+        raise RdError(r, "rd_vocab_loss")
+    return r
 
 
 def rd_vocab_loss_grad_workspace(hidden, weight, labels, want_hidden=True, want_weight=True) -> int:
-    if _torch is None:
-        _setup()
     need = C.c_size_t()
-    _check(lib().rd_vocab_loss_grad_workspace(C.byref(_vocab(hidden, weight, labels, 0, 1.0, 0.0)), int(want_hidden), int(want_weight),
+    _check(lib().rd_vocab_loss_grad_workspace(C.byref(_vocab_shape(hidden, weight, labels)), int(want_hidden), int(want_weight),
                                               C.byref(need)), "rd_vocab_loss_grad_workspace")
     return need.value
 
@@ -594,35 +516,13 @@ def rd_vocab_loss_grad(hidden, weight, labels, lse, grad_loss, grad_hidden=None,
     """Gradients of sum(grad_loss * loss) into grad_hidden [n, dim] and grad_weight [rows, dim] (one may be None: not computed).
     lse: rd_vocab_loss's, joined over the slices of the vocabulary; grad_loss: float32 vector, may be a broadcast one, or a scalar
     tensor.  Returns (grad_hidden, grad_weight)."""
-    if _elsewhere(hidden, stream):
-        return _there(rd_vocab_loss_grad, hidden, stream, hidden, weight, labels, lse, grad_loss, grad_hidden, grad_weight, first_row, scale,
-                      z_loss, workspace)
-    v = _vocab(hidden, weight, labels, first_row, scale, z_loss)
-    device, n, ref = hidden.get_device(), hidden.shape[0], C.byref(v)
-    lse_addr = _vector(lse, "lse", n, device)
-    if grad_loss.dim() == 0:
-        grad_loss = grad_loss.expand(n)
-    if grad_loss.get_device() != device or grad_loss.shape != (n,) or grad_loss.dtype != _torch.float32 or lse.dtype != _torch.float32:
-        raise ValueError("lse and grad_loss must be float32 CUDA vectors with one value per token")
-    gh = gw = (None, 0)
-    if grad_hidden is not None:
-        gh = _matrix(grad_hidden, "grad_hidden")
-        _like(grad_hidden, hidden)
-    if grad_weight is not None:
-        gw = _matrix(grad_weight, "grad_weight")
-        _like(grad_weight, weight)
-    need = C.c_size_t()
-    _check(lib().rd_vocab_loss_grad_workspace(ref, grad_hidden is not None, grad_weight is not None, C.byref(need)), "rd_vocab_loss_grad")
-    s = _stream(device)
-    ws = _Workspace(workspace, need.value, device, s)
-    _check(lib().rd_vocab_loss_grad(ref, lse_addr, grad_loss.data_ptr(), grad_loss.stride(0), *gh, *gw, ws.address, ws.size, s),
-           "rd_vocab_loss_grad")
+    if stream is not None:
+        return _on_stream(rd_vocab_loss_grad, hidden, stream, hidden, weight, labels, lse, grad_loss, grad_hidden, grad_weight, first_row, scale,
+                          z_loss, workspace)
+    r = _native().vocab_loss_grad(hidden, weight, labels, first_row, scale, z_loss, workspace, lse, grad_loss, grad_hidden, grad_weight)
+    if r is not None:
+        raise RdError(r, "rd_vocab_loss_grad")
     return grad_hidden, grad_weight
-
-
-def _like(grad, operand):
-    if grad.shape != operand.shape or grad.dtype != operand.dtype or grad.get_device() != operand.get_device():
-        raise ValueError("a gradient has its operand's shape, dtype and device")
 
 
 def rd_vocab_status() -> int:

@@ -1,10 +1,12 @@
-"""Builds librd.so (CUDA kernels + C ABI) in-tree with nvcc for sm_100a."""
+"""Builds librd.so (CUDA kernels + C ABI) in-tree with nvcc for sm_100a, and _rd_torch.so (tensor marshalling) beside it."""
 from __future__ import annotations
 
+import importlib.util
 import os
 import shutil
 import subprocess
 import sys
+import sysconfig
 import tempfile
 from concurrent.futures import ThreadPoolExecutor
 
@@ -12,6 +14,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "librd.so")
+TORCH_LIB = os.path.join(HERE, "_rd_torch.so")
 SOURCES = ["rd_api.cpp", "rd_sched.cpp", "rd_compile.cpp", "rd_kernels.cu", "rd_faithful.cu", "rd_broadcast.cu",
            "rd_vocab_api.cpp", "rd_embed.cu", "rd_vocab.cu"]
 HEADERS = ["rd_internal.h", "rd_kernels.h", "rd_vocab.h", "rd_launch.h"]
@@ -34,11 +37,31 @@ def _nvcc() -> str:
 
 
 def stale() -> bool:
-    if not os.path.exists(LIB):
+    if not os.path.exists(LIB) or not os.path.exists(TORCH_LIB):
         return True
-    built = os.path.getmtime(LIB)
-    deps = [os.path.join(CSRC, f) for f in SOURCES + HEADERS] + [os.path.join(ROOT, "include", "rd.h")]
+    built = min(os.path.getmtime(LIB), os.path.getmtime(TORCH_LIB))
+    deps = [os.path.join(CSRC, f) for f in SOURCES + HEADERS + ["rd_torch.cpp"]] + [os.path.join(ROOT, "include", "rd.h")]
     return any(os.path.getmtime(d) > built for d in deps)
+
+
+def _torch_module(work: str) -> str:
+    """Compiles the marshalling module against the installed torch (found, not imported); it is linked to librd.so beside it."""
+    torch_dir = list(importlib.util.find_spec("torch").submodule_search_locations)[0]
+    cuda = os.path.dirname(os.path.dirname(_nvcc())) if os.path.isabs(_nvcc()) else "/usr/local/cuda"
+    obj = os.path.join(work, "rd_torch.o")
+    subprocess.check_call(["g++", "-O2", "-std=c++17", "-fPIC", "-fvisibility=hidden", "-Wall", "-Wextra", "-c", "-o", obj,
+                           os.path.join(CSRC, "rd_torch.cpp"), "-I", os.path.join(ROOT, "include"),
+                           "-isystem", os.path.join(torch_dir, "include"), "-isystem", os.path.join(torch_dir, "include", "torch", "csrc", "api", "include"),
+                           "-isystem", sysconfig.get_paths()["include"], "-isystem", os.path.join(cuda, "include")])
+    return obj
+
+
+def _link_torch_module(obj: str) -> None:
+    torch_dir = list(importlib.util.find_spec("torch").submodule_search_locations)[0]
+    tmp = TORCH_LIB + ".%d.tmp" % os.getpid()
+    subprocess.check_call(["g++", "-shared", "-o", tmp, obj, "-L", os.path.join(torch_dir, "lib"), "-ltorch_python", "-ltorch_cuda", "-ltorch_cpu",
+                           "-lc10_cuda", "-lc10", "-L", HERE, "-l:" + os.path.basename(LIB), "-Wl,-rpath,$ORIGIN"])
+    os.replace(tmp, TORCH_LIB)
 
 
 def build(force: bool = False, verbose: bool = False) -> str:
@@ -66,11 +89,14 @@ def build(force: bool = False, verbose: bool = False) -> str:
             subprocess.check_call(common + extra + ["-c", "-o", obj, os.path.join(CSRC, src)])
             return obj
 
-        with ThreadPoolExecutor(max_workers=min(len(units), os.cpu_count() or 4)) as pool:
+        with ThreadPoolExecutor(max_workers=min(len(units) + 1, os.cpu_count() or 4)) as pool:
+            marshalling = pool.submit(_torch_module, work)
             objs = list(pool.map(compile_one, units))
+            marshalling = marshalling.result()
         tmp = LIB + ".%d.tmp" % os.getpid()
         subprocess.check_call([nvcc, *LINK_FLAGS, "-o", tmp] + objs)
         os.replace(tmp, LIB)
+        _link_torch_module(marshalling)
     finally:
         shutil.rmtree(work, ignore_errors=True)
     return LIB
