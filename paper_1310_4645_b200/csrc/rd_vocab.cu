@@ -670,6 +670,11 @@ __global__ void __launch_bounds__(kMmaThreads, 1) rd_vocab_mma_kernel(const __gr
         }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
+    if (warp == 3 && lane == 0) {
+        for (const CUtensorMap *map : {&p.a_k, KIND == kGrads ? &p.b_mn : &p.b_k}) asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory");
+        if (KIND == kGrads)
+            for (const CUtensorMap *map : {&p.a_mn, &p.b2_mn}) asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory");
+    }
     if (warp == 2) {
         if (CG == 2) {
             asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(tmem_slot) : "memory");
@@ -1014,10 +1019,12 @@ template <bool BF16, int V, int N> __global__ void __launch_bounds__(256, 3) rd_
     float top[N], sum[N];
 #pragma unroll
     for (int t = 0; t < N; t++) top[t] = -INFINITY, sum[t] = 0.0f;
-    for (uint32_t r0 = (blockIdx.x * 8 + warp) * kFewRows; r0 < p.rows; r0 += gridDim.x * 8 * kFewRows) {
+    // an equal share of the rows for every warp; in its last turn the rows it lacks are its last one again, which costs no memory traffic
+    const uint32_t warps = gridDim.x * 8, self = blockIdx.x * 8 + warp, end = uint32_t(uint64_t(p.rows) * (self + 1) / warps);
+    for (uint32_t r0 = uint32_t(uint64_t(p.rows) * self / warps); r0 < end; r0 += kFewRows) {
         const uint16_t *row[kFewRows];
 #pragma unroll
-        for (int r = 0; r < kFewRows; r++) row[r] = p.weight + size_t(min(r0 + r, p.rows - 1)) * p.weight_stride;
+        for (int r = 0; r < kFewRows; r++) row[r] = p.weight + size_t(min(r0 + r, end - 1)) * p.weight_stride;
         float acc[kFewRows][N] = {};
         if (V == 8) {
 #pragma unroll 2
@@ -1058,8 +1065,8 @@ template <bool BF16, int V, int N> __global__ void __launch_bounds__(256, 3) rd_
                 float a = acc[r][t];
 #pragma unroll
                 for (int d = 16; d; d /= 2) a += __shfl_xor_sync(0xffffffffu, a, d);
-                if (r0 + r == uint32_t(label[t]) && lane == 0) p.packed_target[t] = a * p.scale;
-                y[r] = r0 + r < p.rows ? a * p.scale2 : -INFINITY;
+                if (r0 + r < end && r0 + r == uint32_t(label[t]) && lane == 0) p.packed_target[t] = a * p.scale;
+                y[r] = r0 + r < end ? a * p.scale2 : -INFINITY;
                 most = fmaxf(most, y[r]);
             }
             // an infinite maximum must not meet itself in a difference
@@ -1087,16 +1094,32 @@ template <bool BF16, int V, int N> __global__ void __launch_bounds__(256, 3) rd_
     }
 }
 
-// A warp per token.
-__global__ void __launch_bounds__(32 * kFewTokens) rd_vocab_few_join_kernel(FewParams p)
+// A thread block per token.
+__global__ void __launch_bounds__(128) rd_vocab_few_join_kernel(FewParams p)
 {
-    pdl_start();
-    const int lane = threadIdx.x & 31;
-    const uint32_t t = threadIdx.x >> 5;
-    if (t >= p.n) return;
+    __shared__ float2 of_warp[4];
+    // the labels are the caller's: the kernel before this one has seen them there before it let this one start
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const uint32_t t = blockIdx.x;
     const long long l = label_of(p.labels, p.wide_labels, t);
     const bool here = l >= p.first && l - p.first < static_cast<long long>(p.rows);
-    write_row(join_row(p.part + size_t(t) * p.parts, p.parts, lane), l >= 0, here ? p.packed_target[t] : 0.0f, p.z, t, lane, p.loss, p.lse, p.target);
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    const float target = here ? p.packed_target[t] : 0.0f;
+    float2 x = make_float2(-INFINITY, 0.0f), y[(kFewBlocks + 127) / 128];
+#pragma unroll
+    for (uint32_t k = 0; k < sizeof(y) / sizeof(y[0]); k++)
+        y[k] = threadIdx.x + 128 * k < p.parts ? p.part[size_t(t) * p.parts + threadIdx.x + 128 * k] : make_float2(-INFINITY, 0.0f);
+#pragma unroll
+    for (uint32_t k = 0; k < sizeof(y) / sizeof(y[0]); k++) join_parts(x, y[k]);
+#pragma unroll
+    for (int d = 16; d; d /= 2) join_parts(x, make_float2(__shfl_down_sync(0xffffffffu, x.x, d), __shfl_down_sync(0xffffffffu, x.y, d)));
+    if (lane == 0) of_warp[warp] = x;
+    __syncthreads();
+    if (warp) return;
+#pragma unroll
+    for (int k = 1; k < 4; k++) join_parts(x, of_warp[k]);
+    write_row(x, l >= 0, target, p.z, t, lane, p.loss, p.lse, p.target);
 }
 
 struct FinishParams {
@@ -1449,7 +1472,7 @@ cudaError_t vocab_loss_few(const VocabArgs &a)
     const cudaError_t e = a.bf16 ? wide ? launch_few<true, 8>(a, p, blocks) : launch_few<true, 1>(a, p, blocks)
                                  : wide ? launch_few<false, 8>(a, p, blocks) : launch_few<false, 1>(a, p, blocks);
     if (e != cudaSuccess) return e;
-    return launch(rd_vocab_few_join_kernel, 1, 32 * kFewTokens, a.stream, p);
+    return launch(rd_vocab_few_join_kernel, unsigned(a.n), 128, a.stream, p);
 }
 
 }  // namespace
