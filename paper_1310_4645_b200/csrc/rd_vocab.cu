@@ -900,7 +900,7 @@ __global__ void __launch_bounds__(kMmaThreads, 1) rd_vocab_mma_kernel(const __gr
                             else tma_add(&p.dh_out, box, col, row0, w.split);
                             box_sent();
                         }
-                    } else if (p.dw_tma) {
+                    } else {
                         box_wait(lane, c & 1);
 #pragma unroll
                         for (int q = 0; q < 4; q++) {
@@ -909,17 +909,27 @@ __global__ void __launch_bounds__(kMmaThreads, 1) rd_vocab_mma_kernel(const __gr
                             for (int j = 0; j < 4; j++) o[j] = pack2<BF16>(__uint_as_float(v[8 * q + 2 * j]) * unboost, __uint_as_float(v[8 * q + 2 * j + 1]) * unboost);
                             box_put(box, lane, 4 * (c & 1) + q, o[0], o[1], o[2], o[3]);
                         }
-                        if (box_full(lane, c & 1) && col - 32 < p.dim && row0 < p.piece) {
-                            tma_store(&p.dw_out, box, col - 32, p.piece0 + row0);
-                            box_sent();
-                        }
-                    } else if (row < p.piece) {
-                        uint16_t *dst = p.dw + size_t(p.piece0 + row) * p.dw_stride + col;
+                        if (p.dw_tma) {
+                            if (box_full(lane, c & 1) && col - 32 < p.dim && row0 < p.piece) {
+                                tma_store(&p.dw_out, box, col - 32, p.piece0 + row0);
+                                box_sent();
+                            }
+                        } else if (c & 1) {
+                            // rows that TMA cannot address: the warp writes them one after the other, two elements a lane
+                            __syncwarp();
+                            const uint32_t rows = row0 < p.piece ? min(32u, p.piece - row0) : 0;
+                            uint16_t *dst = p.dw + size_t(p.piece0 + row0) * p.dw_stride + (col - 32);
+#pragma unroll 4
+                            for (uint32_t r = 0; r < rows; r++) {
 #pragma unroll
-                        for (int j = 0; j < 32; j += 2) {
-                            const uint32_t o = pack2<BF16>(__uint_as_float(v[j]) * unboost, __uint_as_float(v[j + 1]) * unboost);
-                            if (col + j < p.dim) dst[j] = uint16_t(o);
-                            if (col + j + 1 < p.dim) dst[j + 1] = uint16_t(o >> 16);
+                                for (int i = 0; i < 2; i++) {
+                                    const uint32_t j = lane + 32 * i;
+                                    uint16_t x;
+                                    asm volatile("ld.shared.u16 %0, [%1];" : "=h"(x) : "r"(box + r * 128 + (((j / 8) ^ (r & 7)) * 16) + j % 8 * 2) : "memory");
+                                    if (col - 32 + j < p.dim) dst[size_t(r) * p.dw_stride + j] = x;
+                                }
+                            }
+                            __syncwarp();
                         }
                     }
                 };
