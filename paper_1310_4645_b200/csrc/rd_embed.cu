@@ -130,6 +130,40 @@ __global__ void __launch_bounds__(kThreads) rd_embed_kernel(const T *__restrict_
     }
 }
 
+// Rows that are not made of 16-byte words: a warp per kRowUnroll * 32 elements of a row, single elements side by side.  (With
+// elements dealt out like the vectors above, the divisions took most of the time: 16384 rows of 1001 bf16 values 52 us, this 12.)
+constexpr int kRowUnroll = 16;
+template <typename T>
+__global__ void __launch_bounds__(kThreads) rd_embed_element_kernel(const T *__restrict__ table, size_t table_stride, size_t rows, const void *__restrict__ ids,
+                                                                    bool wide, long long first, uint32_t dim, uint32_t slabs, size_t units, float scale,
+                                                                    T *__restrict__ out, size_t out_stride)
+{
+    pdl_start();
+    const int lane = threadIdx.x & 31;
+    const size_t u = size_t(blockIdx.x) * (kThreads / 32) + (threadIdx.x >> 5);
+    if (u >= units) return;
+    const size_t i = u / slabs;
+    const uint32_t j = uint32_t(u - i * slabs) * (32 * kRowUnroll) + lane;
+    const long long r = row_of(ids, wide, i, first, rows);
+    const T *src = table + (r >= 0 ? size_t(r) * table_stride : 0) + j;
+    T *dst = out + i * out_stride + j;
+    T x[kRowUnroll];
+#pragma unroll
+    for (int e = 0; e < kRowUnroll; e++) x[e] = r >= 0 && j + 32 * e < dim ? src[32 * e] : narrow<T>(0.0f);
+#pragma unroll
+    for (int e = 0; e < kRowUnroll; e++)
+        if (j + 32 * e < dim) dst[32 * e] = scale != 1.0f && r >= 0 ? narrow<T>(widen<T>(x[e]) * scale) : x[e];
+}
+
+template <typename T> cudaError_t launch_elements(const EmbedArgs &a)
+{
+    const uint32_t slabs = uint32_t((a.dim + 32 * kRowUnroll - 1) / (32 * kRowUnroll));
+    const size_t units = a.n * slabs, blocks = (units + kThreads / 32 - 1) / (kThreads / 32);
+    if (blocks > 0x7fffffffu) return cudaErrorInvalidConfiguration;
+    return launch(rd_embed_element_kernel<T>, unsigned(blocks), kThreads, a.stream, static_cast<const T *>(a.table), a.table_stride, a.rows, a.ids, a.wide_ids, a.first_row,
+                  uint32_t(a.dim), slabs, units, a.scale, static_cast<T *>(a.out), a.out_stride);
+}
+
 template <typename T, int V> cudaError_t launch_embed(const EmbedArgs &a)
 {
     const uint32_t vecs = uint32_t(a.dim / V);
@@ -407,13 +441,41 @@ __global__ void __launch_bounds__(kThreads) rd_embed_sort_kernel(const void *__r
     }
 }
 
-// Sum over c tokens of the V values at column col, in order, four of them in flight.  The tokens are in the lanes
-// of the warp (token t in lane t) or, for groups narrower than a warp, in list.
-template <typename T, int V>
-__device__ __forceinline__ void add_rows(const T *__restrict__ grad, size_t stride, uint32_t token, const uint32_t *__restrict__ list, uint32_t c, float (&acc)[V])
+// A thread's V columns: vectors of consecutive ones, or for rows that are not made of 16-byte words (ELEMENTS) single ones that are
+// `step` apart, so that neighbouring lanes have neighbouring columns; `left` of them, counted from the first, exist.
+template <int V, bool ELEMENTS> struct Columns {
+    uint32_t step, left;
+    template <typename T> __device__ __forceinline__ Vec<T, V> get(const T *p) const
+    {
+        if constexpr (!ELEMENTS) {
+            return load<T, V>(p);
+        } else {
+            Vec<T, V> x;
+#pragma unroll
+            for (int e = 0; e < V; e++) x.v[e] = e * step < left ? p[e * step] : narrow<T>(0.0f);
+            return x;
+        }
+    }
+    template <typename T> __device__ __forceinline__ void put(T *p, const Vec<T, V> &x) const
+    {
+        if constexpr (!ELEMENTS) {
+            store<T, V>(p, x);
+        } else {
+#pragma unroll
+            for (int e = 0; e < V; e++)
+                if (e * step < left) p[e * step] = x.v[e];
+        }
+    }
+};
+
+// Sum over c tokens, in order, several of them in flight.  The tokens are in the lanes of the warp (token t in lane t) or, for groups
+// narrower than a warp, in list.
+template <typename T, int V, bool ELEMENTS>
+__device__ __forceinline__ void add_rows(const Columns<V, ELEMENTS> &cols, const T *__restrict__ grad, size_t stride, uint32_t token, const uint32_t *__restrict__ list,
+                                         uint32_t c, float (&acc)[V])
 {
-    constexpr int U = 4;
-    auto row = [&](uint32_t t) { return load<T, V>(grad + size_t(list ? list[t] : __shfl_sync(0xffffffffu, token, t)) * stride); };
+    constexpr int U = ELEMENTS ? 2 : 4;
+    auto row = [&](uint32_t t) { return cols.get(grad + size_t(list ? list[t] : __shfl_sync(0xffffffffu, token, t)) * stride); };
 #pragma unroll
     for (int k = 0; k < V; k++) acc[k] = 0.0f;
     uint32_t t = 0;
@@ -433,26 +495,26 @@ __device__ __forceinline__ void add_rows(const T *__restrict__ grad, size_t stri
     }
 }
 
-template <typename O, int V>
-__device__ __forceinline__ void write_row(O *p, const float (&acc)[V], float scale, bool accumulate)
+template <typename O, int V, bool ELEMENTS>
+__device__ __forceinline__ void write_row(const Columns<V, ELEMENTS> &cols, O *p, const float (&acc)[V], float scale, bool accumulate)
 {
     Vec<O, V> y;
     if (accumulate) {
-        const Vec<O, V> old = load<O, V>(p);
+        const Vec<O, V> old = cols.get(static_cast<const O *>(p));
 #pragma unroll
         for (int k = 0; k < V; k++) y.v[k] = narrow<O>(fmaf(acc[k], scale, widen<O>(old.v[k])));
     } else {
 #pragma unroll
         for (int k = 0; k < V; k++) y.v[k] = narrow<O>(acc[k] * scale);
     }
-    store<O, V>(p, y);
+    cols.put(p, y);
 }
 
 // `lanes` threads (a power of two, within a warp) work on an item and a slab of lanes * V columns.  An item, its tokens and their
 // rows are three loads that depend on each other; the item after the next one and the next one's tokens are on their way
 // while a group adds up the rows of the present one.
-template <typename T, typename O, int V>
-__global__ void __launch_bounds__(kThreads, 3) rd_embed_sum_kernel(const T *__restrict__ grad, size_t grad_stride, O *__restrict__ table, size_t table_stride, uint32_t vecs,
+template <typename T, typename O, int V, bool ELEMENTS>
+__global__ void __launch_bounds__(kThreads, 3) rd_embed_sum_kernel(const T *__restrict__ grad, size_t grad_stride, O *__restrict__ table, size_t table_stride, uint32_t dim,
                                                                 uint32_t lanes, uint32_t slabs, float scale, bool accumulate, GradWork w)
 {
     pdl_start();
@@ -474,14 +536,15 @@ __global__ void __launch_bounds__(kThreads, 3) rd_embed_sum_kernel(const T *__re
         const Item after = item(u + 2 * step);
         const uint32_t next_token = tokens(next);
         if (it.count) {
-            const uint32_t slab = uint32_t(u % slabs), j = slab * lanes + lane;
-            const bool mine = j < vecs;
-            const size_t col = mine ? size_t(j) * V : 0;          // lanes beyond the row read its beginning and write nothing
+            const uint32_t slab = uint32_t(u % slabs), at = slab * lanes * V + (ELEMENTS ? lane : lane * V);
+            const bool mine = at < dim;
+            const size_t col = mine ? at : 0;                     // lanes beyond the row read its beginning and write nothing
+            const Columns<V, ELEMENTS> cols{lanes, mine ? dim - at : 0};
             float acc[V];
-            add_rows<T, V>(grad + col, grad_stride, token, by_lane ? nullptr : w.list + it.begin, it.count, acc);
+            add_rows(cols, grad + col, grad_stride, token, by_lane ? nullptr : w.list + it.begin, it.count, acc);
             O *out = table + size_t(it.row) * table_stride + col;
             if (it.parts == 1) {
-                if (mine) write_row<O, V>(out, acc, scale, accumulate);
+                if (mine) write_row(cols, out, acc, scale, accumulate);
             } else {
                 // a row of several items: whichever group is last adds the partial rows up, in order
                 const uint32_t begin = it.begin - it.part * kChunk;
@@ -490,7 +553,7 @@ __global__ void __launch_bounds__(kThreads, 3) rd_embed_sum_kernel(const T *__re
                     Vec<float, V> x;
 #pragma unroll
                     for (int e = 0; e < V; e++) x.v[e] = acc[e];
-                    store<float, V>(partial + size_t(slot_of(begin, it.part)) * w.partial_stride, x);
+                    cols.put(partial + size_t(slot_of(begin, it.part)) * w.partial_stride, x);
                 }
                 __threadfence();
                 __syncwarp(mask);
@@ -502,11 +565,11 @@ __global__ void __launch_bounds__(kThreads, 3) rd_embed_sum_kernel(const T *__re
                     for (int e = 0; e < V; e++) acc[e] = 0.0f;
 #pragma unroll 2
                     for (uint32_t k = 0; k < it.parts; k++) {
-                        const Vec<float, V> x = load<float, V>(partial + size_t(slot_of(begin, k)) * w.partial_stride);
+                        const Vec<float, V> x = cols.get(const_cast<const float *>(partial) + size_t(slot_of(begin, k)) * w.partial_stride);
 #pragma unroll
                         for (int e = 0; e < V; e++) acc[e] += x.v[e];
                     }
-                    write_row<O, V>(out, acc, scale, accumulate);
+                    write_row(cols, out, acc, scale, accumulate);
                 }
             }
         }
@@ -612,11 +675,11 @@ template <typename O> cudaError_t launch_fill(const EmbedGradArgs &a, bool alone
 // From this size of table on the fork pays: the sort takes some 20 us, a fork and a join a few.
 constexpr size_t kForkBytes = size_t(32) << 20;
 
-template <typename T, typename O, int V> cudaError_t launch_grad(const EmbedGradArgs &a)
+template <typename T, typename O, int V, bool ELEMENTS> cudaError_t launch_grad(const EmbedGradArgs &a)
 {
     const GradWork w = layout(a.workspace, a.rows, a.dim, a.n);
     const uint32_t n = uint32_t(a.n);
-    const uint32_t vecs = uint32_t(a.dim / V), lanes = lanes_for(vecs), slabs = (vecs + lanes - 1) / lanes;
+    const uint32_t vecs = uint32_t((a.dim + V - 1) / V), lanes = lanes_for(vecs), slabs = (vecs + lanes - 1) / lanes;
     if (n == 0) return a.accumulate ? cudaSuccess : launch_fill<O>(a, true);
     cudaError_t e = cudaSuccess;
     if (n <= kSmallTokens) {
@@ -645,8 +708,8 @@ template <typename T, typename O, int V> cudaError_t launch_grad(const EmbedGrad
     }
     if (e != cudaSuccess) return e;
     const uint64_t units = uint64_t(max_big(n) + max_items(n, a.rows)) * slabs, blocks = (units + kThreads / lanes - 1) / (kThreads / lanes);
-    return launch(rd_embed_sum_kernel<T, O, V>, unsigned(blocks < kSumBlocks ? blocks : kSumBlocks), kThreads, a.stream, static_cast<const T *>(a.grad), a.grad_stride,
-                  static_cast<O *>(a.table), a.table_stride, vecs, lanes, slabs, a.scale, a.accumulate, w);
+    return launch(rd_embed_sum_kernel<T, O, V, ELEMENTS>, unsigned(blocks < kSumBlocks ? blocks : kSumBlocks), kThreads, a.stream, static_cast<const T *>(a.grad), a.grad_stride,
+                  static_cast<O *>(a.table), a.table_stride, uint32_t(a.dim), lanes, slabs, a.scale, a.accumulate, w);
 }
 
 // Whole vectors of 32 or 16 bytes when both matrices' rows begin and end on such boundaries (lookup of 16384 rows of 8 KB, B200:
@@ -658,7 +721,7 @@ template <typename T, typename O> cudaError_t pick_grad(const EmbedGradArgs &a)
         const size_t to = vec * sizeof(O) < 32 ? vec * sizeof(O) : 32;
         return vector_rows(a.grad, a.grad_stride, a.dim, sizeof(T), vec * sizeof(T)) && vector_rows(a.table, a.table_stride, a.dim, sizeof(O), to);
     };
-    return fits(2 * V) ? launch_grad<T, O, 2 * V>(a) : fits(V) ? launch_grad<T, O, V>(a) : launch_grad<T, O, 1>(a);
+    return fits(2 * V) ? launch_grad<T, O, 2 * V, false>(a) : fits(V) ? launch_grad<T, O, V, false>(a) : launch_grad<T, O, 8, true>(a);
 }
 
 template <typename T> cudaError_t pick_embed(const EmbedArgs &a)
@@ -667,7 +730,7 @@ template <typename T> cudaError_t pick_embed(const EmbedArgs &a)
     auto fits = [&](size_t to) {
         return vector_rows(a.table, a.table_stride, a.dim, sizeof(T), to) && vector_rows(a.out, a.out_stride, a.dim, sizeof(T), to);
     };
-    return fits(32) ? launch_embed<T, 2 * V>(a) : fits(16) ? launch_embed<T, V>(a) : launch_embed<T, 1>(a);
+    return fits(32) ? launch_embed<T, 2 * V>(a) : fits(16) ? launch_embed<T, V>(a) : launch_elements<T>(a);
 }
 
 }  // namespace
