@@ -79,7 +79,7 @@ struct PackParams {
     bool gradient, fp16;
 };
 
-__device__ __forceinline__ void factors(const PackParams &p, size_t i, float &gp, float &gt)
+template <typename P> __device__ __forceinline__ void factors(const P &p, size_t i, float &gp, float &gt)
 {
     const float g = p.grad_loss[i * p.grad_loss_stride] * p.scale;
     gt = g;
@@ -87,7 +87,7 @@ __device__ __forceinline__ void factors(const PackParams &p, size_t i, float &gp
 }
 
 // The largest finite factor of dx that token i brings (fp16 only: it decides the power of two).
-__device__ __forceinline__ float largest_factor(const PackParams &p, size_t i)
+template <typename P> __device__ __forceinline__ float largest_factor(const P &p, size_t i)
 {
     float gp, gt, most = 0.0f;
     factors(p, i, gp, gt);
@@ -112,6 +112,16 @@ __global__ void __launch_bounds__(kCountTile) rd_vocab_count_kernel(PackParams p
         for (int k = 1; k < kCountTile / 32; k++) most = fmaxf(most, warp_most[k]);
         tiles[blockIdx.x] = TileCount{uint32_t(n), most};
     }
+}
+
+// fp16: the power of two that takes the largest factor to [2^13, 2^14); probabilities down to 2^-27 of it stay normal numbers.
+__device__ __forceinline__ float boost_for(float most)
+{
+    if (!(most > 0.0f)) return 1.0f;
+    int e;
+    frexpf(most, &e);
+    e = 14 - e;
+    return ldexpf(1.0f, e > 100 ? 100 : e < -100 ? -100 : e);
 }
 
 // `threads` threads copy a row; the copy's row has room for a multiple of 8 elements, and zeros there.
@@ -190,14 +200,7 @@ template <int R> __global__ void __launch_bounds__(kPackThreads) rd_vocab_pack_k
         most = fmaxf(most, mosts[k]);
     }
     if (first && threadIdx.x == 0) {
-        // fp16: the largest factor goes to [2^13, 2^14): probabilities down to 2^-27 of it stay normal numbers
-        float boost = 1.0f;
-        if (p.fp16 && most > 0.0f) {
-            int e;
-            frexpf(most, &e);
-            e = 14 - e;
-            boost = ldexpf(1.0f, e > 100 ? 100 : e < -100 ? -100 : e);
-        }
+        const float boost = p.fp16 ? boost_for(most) : 1.0f;
         *p.meta = Meta{all, boost, 1.0f / boost, 0};
     }
     const int row = threadIdx.x / kRowThreads, t = threadIdx.x % kRowThreads;
@@ -255,11 +258,46 @@ constexpr int kMmaThreads = 128 + 32 * kEpilogueWarps;
 constexpr long long kWaitCycles = 4000000000ll;     // a wait gives up after about two seconds of SM clock
 constexpr long long kDrainCycles = 20000000ll;      // after that, copies in flight get ten milliseconds to land
 
+// Where a row of the products comes from: packed rows have their tokens and labels in lists, direct ones are the tokens themselves.
+struct Rows {
+    const int *index, *label;
+    const void *labels;
+    long long first;
+    size_t rows;
+    bool direct, wide;
+    __device__ __forceinline__ size_t token(uint32_t row) const { return direct ? row : size_t(index[row]); }
+    __device__ __forceinline__ bool counts(uint32_t row) const { return !direct || label_of(labels, wide, row) >= 0; }
+    // the label's row in this weight, -1 where it has none
+    __device__ __forceinline__ int label_row(uint32_t row, bool &counts) const
+    {
+        counts = true;
+        if (!direct) return label[row];
+        const long long l = label_of(labels, wide, row);
+        counts = l >= 0;
+        return l >= first && l - first < static_cast<long long>(rows) ? int(l - first) : -1;
+    }
+};
+
+// Direct rows of the gradient: what the packing kernel would have worked out.
+struct Direct {
+    uint32_t n;
+    const uint16_t *hidden;
+    size_t hidden_stride;
+    uint16_t *packed;         // the copy that dw reads, null where it is not wanted
+    uint32_t packed_stride;
+    const float *lse, *grad_loss;
+    size_t grad_loss_stride;
+    float scale, z;
+    Meta *meta;
+    bool copy16;
+};
+
 struct JoinParams {
     const float2 *part;
     const float *packed_target;
-    const int *index, *label;
+    Rows rows;
     const Meta *meta;
+    uint32_t n;               // direct rows
     uint32_t parts;
     float z;
     float *loss, *lse, *target;
@@ -312,21 +350,22 @@ struct alignas(64) MmaParams {
     CUtensorMap dh_out;       // dh, 32 x 32 x 1 boxes
     CUtensorMap dw_out;       // grad_weight, 64 x 32 boxes
     const Meta *meta;
-    const int *label, *index;
+    Rows rows;
+    Direct direct;            // logits
     const float *gp, *gt, *lse2;
-    float2 *part;             // stats: (maximum, sum) in base 2, [packed row][half tile]
+    float2 *part;             // stats: (maximum, sum) in base 2, [row][part]
     float *target;            // stats: the label's logit, per packed row
     uint16_t *dw;             // grad_weight, for rows that TMA cannot address
     uint16_t *gh;             // grad_hidden, where one part of dh is all of it
     size_t dh_stride, dw_stride, gh_stride;
-    uint32_t parts;           // stats: half tiles per row
+    uint32_t parts;           // stats: parts per row, two to a tile of 256 columns, one to a smaller one
     uint32_t piece0, piece;   // first row of the piece and its rows
     uint32_t dim;
+    uint32_t tile_n;          // logits: columns of a tile, 256, 128 or 64
     uint32_t group;           // token tiles that go over the vocabulary together
     uint32_t splits;          // parts that the sum over the piece is cut into for dh
     uint32_t a_rows;          // rows of a thread block's left operand that are brought in (fewer than 128 for few tokens)
     bool first_piece, want_dh, want_dw, dw_tma;
-    bool early;               // the weight is the caller's own: it may be read before the kernels of this call are done
     bool gh_wide;             // 16-byte rows of grad_hidden
     float scale2;             // scale * log2(e)
     float scale;
@@ -558,8 +597,7 @@ template <int KIND, int CG> struct Plan {
     {
         tiles_m = (m + kTileM - 1) / kTileM;
         if (KIND != kGrads) {
-            if (CG == 1 && tiles_m == 0) tiles_m = 1;          // its weights may be on their way already
-            tiles_n = (p.piece + kTileN - 1) / kTileN;
+            tiles_n = (p.piece + p.tile_n - 1) / p.tile_n;
             k_dim = (p.dim + kTileK - 1) / kTileK;
             band = 0;
             if (tiles_m) at.set(c, g, min(p.group, tiles_m));
@@ -592,7 +630,7 @@ template <int KIND, int CG> struct Plan {
                 }
                 at.set(over, g, min(p.group, tiles_m - band * p.group));
             }
-            w = Work{0, (band * p.group + at.x) * kTileM, at.y * kTileN, 0, k_dim, 0};
+            w = Work{0, (band * p.group + at.x) * kTileM, at.y * p.tile_n, 0, k_dim, 0};
             at.advance();
             return true;
         } else {
@@ -690,16 +728,11 @@ __global__ void __launch_bounds__(kMmaThreads, 1) rd_vocab_mma_kernel(const __gr
     uint32_t tmem;
     asm volatile("ld.shared.b32 %0, [%1];" : "=r"(tmem) : "r"(tmem_slot));
 
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-    // One tile of tokens: every block knows its first tile of the weight before the tokens are packed, and fills its ring with it.
-    uint32_t ahead = 0;
-    if (KIND != kGrads && CG == 1 && p.early && warp == 3 && lane == 0 && blockIdx.x * kTileN < p.piece) {
-        const uint32_t k_dim = (p.dim + kTileK - 1) / kTileK;
-        ahead = k_dim < kStages ? k_dim : kStages;
-        for (uint32_t k = 0; k < ahead; k++) tma_load<CG>(smem + k * S::stage + S::stage_a, &p.b_k, k * kTileK, p.piece0 + blockIdx.x * kTileN, full + 8 * k);
-    }
-    asm volatile("griddepcontrol.wait;" ::: "memory");
-    const uint32_t m = p.meta->m;
+    // direct rows: this is the call's first kernel
+    const bool direct = KIND != kGrads && CG == 1 && p.rows.direct;
+    if (direct) pdl_wait_first();
+    else pdl_start();
+    const uint32_t m = direct ? p.direct.n : p.meta->m;
     Plan<KIND, CG> plan(p, m);
     bool dead = false;
 
@@ -710,14 +743,15 @@ __global__ void __launch_bounds__(kMmaThreads, 1) rd_vocab_mma_kernel(const __gr
             Work w;
             const uint32_t lead = leader_bar<CG>(full);
             while (!dead && plan.next(w)) {
-                const uint32_t m0 = w.m0 + rank * kRowsM, n0 = w.n0 + rank * S::rows_n;
+                const uint32_t rows_n = KIND != kGrads ? p.tile_n / CG : uint32_t(S::rows_n);
+                const uint32_t m0 = w.m0 + rank * kRowsM, n0 = w.n0 + rank * rows_n;
                 for (uint32_t k = 0, kk = w.k0; k < w.kblocks; k++, kk += kTileK, turn.advance()) {
                     const uint32_t a = smem + turn.s * S::stage, b = a + S::stage_a, bar = lead + 8 * turn.s;
                     if (!bar_wait(empty + 8 * turn.s, turn.parity ^ 1)) { dead = true; break; }
                     if (warp == 0) {
                         // the copies of both thread blocks and both operands count at the first block's barrier
                         const uint32_t a_bytes = w.product == 2 ? S::stage_a : p.a_rows * kTileK * 2;
-                        if (rank == 0) bar_expect(full + 8 * turn.s, CG * (a_bytes + S::stage_b));
+                        if (rank == 0) bar_expect(full + 8 * turn.s, CG * (a_bytes + rows_n * kTileK * 2));
                         if (w.product == 2) {
 #pragma unroll
                             for (int j = 0; j < kRowsM / 64; j++) tma_load<CG>(a + j * 8192, &p.a_mn, m0 + 64 * j, kk, bar);
@@ -725,8 +759,7 @@ __global__ void __launch_bounds__(kMmaThreads, 1) rd_vocab_mma_kernel(const __gr
                             tma_load<CG>(a, &p.a_k, kk, m0, bar);
                         }
                     } else if (KIND != kGrads) {
-                        if (ahead) ahead--;
-                        else tma_load<CG>(b, &p.b_k, kk, p.piece0 + n0, bar);
+                        tma_load<CG>(b, &p.b_k, kk, p.piece0 + n0, bar);
                     } else {
                         const CUtensorMap *map = w.product == 1 ? &p.b_mn : &p.b2_mn;
                         const uint32_t y = w.product == 1 ? p.piece0 + kk : kk;
@@ -741,7 +774,7 @@ __global__ void __launch_bounds__(kMmaThreads, 1) rd_vocab_mma_kernel(const __gr
         }
     } else if (warp == 1) {
         if (lane == 0 && rank == 0) {
-            constexpr uint32_t kDesc = 1u << 4 | (BF16 ? 1u << 7 | 1u << 10 : 0u) | uint32_t(kTileN / 8) << 17 | uint32_t(S::tile_m / 16) << 24;
+            const uint32_t desc = 1u << 4 | (BF16 ? 1u << 7 | 1u << 10 : 0u) | (KIND != kGrads ? p.tile_n : kTileN) / 8 << 17 | uint32_t(S::tile_m / 16) << 24;
             Turn<kStages> turn;
             uint32_t tile = 0;
             Work w;
@@ -751,7 +784,7 @@ __global__ void __launch_bounds__(kMmaThreads, 1) rd_vocab_mma_kernel(const __gr
                 if (!bar_wait(acc_empty + 8 * buf, (tile / 2 & 1) ^ 1)) { dead = true; break; }
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                 const bool ta = w.product == 2, tb = w.product != 0;
-                const uint32_t idesc = kDesc | (ta ? 1u << 15 : 0u) | (tb ? 1u << 16 : 0u);
+                const uint32_t idesc = desc | (ta ? 1u << 15 : 0u) | (tb ? 1u << 16 : 0u);
                 const uint32_t step_a = ta ? 2048 >> 4 : 32 >> 4, step_b = tb ? 2048 >> 4 : 32 >> 4;
                 for (uint32_t k = 0; k < w.kblocks; k++, turn.advance()) {
                     const uint32_t a = smem + turn.s * S::stage, b = a + S::stage_a;
@@ -772,6 +805,33 @@ __global__ void __launch_bounds__(kMmaThreads, 1) rd_vocab_mma_kernel(const __gr
         const uint32_t box = boxes + (warp - 4) * kBox;
         uint32_t tile = 0;
         Work w;
+        float boost = 1.0f;
+        if (KIND == kDlogits && direct) {
+            // what the packing kernel does otherwise: the power of two, and for dw the rows that count, with zeros in the others' place
+            // and behind the last one
+            const Direct &d = p.direct;
+            if (!BF16) {
+                float most = 0.0f;
+                for (uint32_t i = lane; i < d.n; i += 32)
+                    if (p.rows.counts(i)) most = fmaxf(most, largest_factor(d, i));
+#pragma unroll
+                for (int x = 16; x; x /= 2) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, x));
+                boost = boost_for(most);
+            }
+            if (p.first_piece) {
+                if (blockIdx.x == 0 && threadIdx.x == 128) *d.meta = Meta{d.n, boost, 1.0f / boost, 0};
+                if (d.packed)
+                    for (uint32_t r = blockIdx.x * kEpilogueWarps + warp - 4; r < (d.n + kZeroPad - 1) / kZeroPad * kZeroPad; r += gridDim.x * kEpilogueWarps) {
+                        const bool counts = r < d.n && p.rows.counts(r);
+                        uint16_t *dst = d.packed + size_t(r) * d.packed_stride;
+                        if (counts) copy_row(dst, d.hidden + size_t(r) * d.hidden_stride, p.dim, d.packed_stride, d.copy16, lane, 32);
+                        else
+                            for (uint32_t j = lane; j < d.packed_stride / 8; j += 32) reinterpret_cast<uint4 *>(dst)[j] = make_uint4(0, 0, 0, 0);
+                    }
+            }
+        } else if (KIND == kDlogits) {
+            boost = p.meta->boost;
+        }
         while (plan.next(w)) {
             const uint32_t row0 = w.m0 + rank * kRowsM + 32 * quarter, row = row0 + lane, col0 = w.n0 + 128 * half;
             const uint32_t buf = tile & 1;
@@ -783,16 +843,25 @@ __global__ void __launch_bounds__(kMmaThreads, 1) rd_vocab_mma_kernel(const __gr
             // the row's numbers (stats and dlogits)
             int label = -1;
             float lse2 = 0.0f, gp = 0.0f, gt = 0.0f;
-            if (KIND != kGrads && row < m) {
-                label = p.label[row];
-                if (KIND == kDlogits) {
-                    const float boost = p.meta->boost;
-                    lse2 = p.lse2[row];
-                    gp = p.gp[row] * boost;
-                    gt = p.gt[row] * boost;
+            bool live = KIND != kGrads && row < m;
+            if (live) {
+                label = p.rows.label_row(row, live);
+                if (KIND == kDlogits && live) {
+                    if (direct) {
+                        factors(p.direct, row, gp, gt);
+                        lse2 = p.direct.lse[row] * kLog2e;
+                    } else {
+                        lse2 = p.lse2[row];
+                        gp = p.gp[row];
+                        gt = p.gt[row];
+                    }
+                    gp *= boost;
+                    gt *= boost;
                     label = label < int(p.piece0) ? -1 : label - int(p.piece0);
                 }
             }
+            // columns of the tile that the vocabulary has; in tiles of fewer than 256 the rest is another tile's
+            const uint32_t limit = KIND != kGrads ? min(p.piece, w.n0 + p.tile_n) : 0;
             const float unboost = KIND == kGrads ? p.meta->unboost : 1.0f;
             // the accumulators are free for the next tile but one as soon as their last columns are in registers
             auto release = [&]() {
@@ -809,16 +878,16 @@ __global__ void __launch_bounds__(kMmaThreads, 1) rd_vocab_mma_kernel(const __gr
 #pragma unroll
                 for (int c = 0; c < 4; c++) tmem_wait(v[c]);
                 release();
-                if (col0 + 128 > p.piece) {
+                if (col0 + 128 > limit) {
                     // the lowest value in the columns that the vocabulary does not have
                     const uint32_t lowest = __float_as_uint(p.scale2 >= 0.0f ? -INFINITY : INFINITY);
 #pragma unroll
                     for (int c = 0; c < 4; c++)
 #pragma unroll
                         for (int j = 0; j < 32; j++)
-                            if (col0 + 32 * c + j >= p.piece) v[c][j] = lowest;
+                            if (col0 + 32 * c + j >= limit) v[c][j] = lowest;
                 }
-                if (label >= 0 && uint32_t(label) - col0 < 128u) {
+                if (label >= 0 && uint32_t(label) - col0 < 128u && uint32_t(label) < limit) {
 #pragma unroll
                     for (int c = 0; c < 4; c++)
 #pragma unroll
@@ -853,83 +922,86 @@ __global__ void __launch_bounds__(kMmaThreads, 1) rd_vocab_mma_kernel(const __gr
                 for (int d = 4; d; d /= 2)
 #pragma unroll
                     for (int j = 0; j < d; j++) sum[j] += sum[j + d];
-                if (row < m) p.part[size_t(row) * p.parts + col0 / 128] = make_float2(top, sum[0]);
+                if (row < m && col0 < w.n0 + p.tile_n) p.part[size_t(row) * p.parts + (p.tile_n == kTileN ? col0 / 128 : w.n0 / p.tile_n)] = make_float2(top, sum[0]);
             } else {
                 auto take = [&](int c, uint32_t (&v)[32]) {
                     const uint32_t col = col0 + 32 * c;
-                    if (KIND == kDlogits) {
+                    if constexpr (KIND == kDlogits) {
                         float y[32];
 #pragma unroll
                         for (int j = 0; j < 32; j++) {
                             y[j] = exp2_fast(fmaf(__uint_as_float(v[j]), p.scale2, -lse2)) * gp;
                             if (col + j == uint32_t(label)) y[j] -= gt;
-                            if (row >= m || col + j >= p.piece) y[j] = 0.0f;
+                            if (!live || col + j >= limit) y[j] = 0.0f;
                         }
                         box_wait(lane, c & 1);
 #pragma unroll
                         for (int q = 0; q < 4; q++)
                             box_put(box, lane, 4 * (c & 1) + q, pack2<BF16>(y[8 * q], y[8 * q + 1]), pack2<BF16>(y[8 * q + 2], y[8 * q + 3]), pack2<BF16>(y[8 * q + 4], y[8 * q + 5]),
                                     pack2<BF16>(y[8 * q + 6], y[8 * q + 7]));
-                        if (box_full(lane, c & 1)) {
+                        if (box_full(lane, c & 1) && col - 32 < w.n0 + p.tile_n) {
                             tma_store(&p.dx_out, box, col - 32, row0);
                             box_sent();
                         }
-                    } else if (w.product == 1 && p.gh) {
-                        if (row < m) {
-                            uint16_t *dst = p.gh + size_t(p.index[row]) * p.gh_stride + col;
+                    } else {
+                        if (w.product == 1 && p.gh) {
+                            if (row < m) {
+                                uint16_t *dst = p.gh + p.rows.token(row) * p.gh_stride + col;
+                                const bool counts = p.rows.counts(row);         // else zeros, whatever the weight holds
+#pragma unroll
+                                for (int q = 0; q < 4; q++) {
+                                    uint32_t o[4];
+#pragma unroll
+                                    for (int j = 0; j < 4; j++) o[j] = counts ? pack2<BF16>(__uint_as_float(v[8 * q + 2 * j]) * unboost, __uint_as_float(v[8 * q + 2 * j + 1]) * unboost) : 0;
+                                    if (p.gh_wide && col + 8 * q + 8 <= p.dim) {
+                                        *reinterpret_cast<uint4 *>(dst + 8 * q) = make_uint4(o[0], o[1], o[2], o[3]);
+                                    } else {
+#pragma unroll
+                                        for (int j = 0; j < 8; j++)
+                                            if (col + 8 * q + j < p.dim) dst[8 * q + j] = uint16_t(o[j / 2] >> (j & 1 ? 16 : 0));
+                                    }
+                                }
+                            }
+                        } else if (w.product == 1) {
+                            box_wait(lane, false);
+#pragma unroll
+                            for (int q = 0; q < 8; q++) box_put(box, lane, q, v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]);
+                            if (box_full(lane, true) && col < p.dh_stride && row0 < m) {
+                                if (p.first_piece) tma_store(&p.dh_out, box, col, row0, w.split);
+                                else tma_add(&p.dh_out, box, col, row0, w.split);
+                                box_sent();
+                            }
+                        } else {
+                            box_wait(lane, c & 1);
 #pragma unroll
                             for (int q = 0; q < 4; q++) {
                                 uint32_t o[4];
 #pragma unroll
                                 for (int j = 0; j < 4; j++) o[j] = pack2<BF16>(__uint_as_float(v[8 * q + 2 * j]) * unboost, __uint_as_float(v[8 * q + 2 * j + 1]) * unboost);
-                                if (p.gh_wide && col + 8 * q + 8 <= p.dim) {
-                                    *reinterpret_cast<uint4 *>(dst + 8 * q) = make_uint4(o[0], o[1], o[2], o[3]);
-                                } else {
-#pragma unroll
-                                    for (int j = 0; j < 8; j++)
-                                        if (col + 8 * q + j < p.dim) dst[8 * q + j] = uint16_t(o[j / 2] >> (j & 1 ? 16 : 0));
+                                box_put(box, lane, 4 * (c & 1) + q, o[0], o[1], o[2], o[3]);
+                            }
+                            if (p.dw_tma) {
+                                if (box_full(lane, c & 1) && col - 32 < p.dim && row0 < p.piece) {
+                                    tma_store(&p.dw_out, box, col - 32, p.piece0 + row0);
+                                    box_sent();
                                 }
-                            }
-                        }
-                    } else if (w.product == 1) {
-                        box_wait(lane, false);
-#pragma unroll
-                        for (int q = 0; q < 8; q++) box_put(box, lane, q, v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]);
-                        if (box_full(lane, true) && col < p.dh_stride && row0 < m) {
-                            if (p.first_piece) tma_store(&p.dh_out, box, col, row0, w.split);
-                            else tma_add(&p.dh_out, box, col, row0, w.split);
-                            box_sent();
-                        }
-                    } else {
-                        box_wait(lane, c & 1);
-#pragma unroll
-                        for (int q = 0; q < 4; q++) {
-                            uint32_t o[4];
-#pragma unroll
-                            for (int j = 0; j < 4; j++) o[j] = pack2<BF16>(__uint_as_float(v[8 * q + 2 * j]) * unboost, __uint_as_float(v[8 * q + 2 * j + 1]) * unboost);
-                            box_put(box, lane, 4 * (c & 1) + q, o[0], o[1], o[2], o[3]);
-                        }
-                        if (p.dw_tma) {
-                            if (box_full(lane, c & 1) && col - 32 < p.dim && row0 < p.piece) {
-                                tma_store(&p.dw_out, box, col - 32, p.piece0 + row0);
-                                box_sent();
-                            }
-                        } else if (c & 1) {
-                            // rows that TMA cannot address: the warp writes them one after the other, two elements a lane
-                            __syncwarp();
-                            const uint32_t rows = row0 < p.piece ? min(32u, p.piece - row0) : 0;
-                            uint16_t *dst = p.dw + size_t(p.piece0 + row0) * p.dw_stride + (col - 32);
+                            } else if (c & 1) {
+                                // rows that TMA cannot address: the warp writes them one after the other, two elements a lane
+                                __syncwarp();
+                                const uint32_t rows = row0 < p.piece ? min(32u, p.piece - row0) : 0;
+                                uint16_t *dst = p.dw + size_t(p.piece0 + row0) * p.dw_stride + (col - 32);
 #pragma unroll 4
-                            for (uint32_t r = 0; r < rows; r++) {
+                                for (uint32_t r = 0; r < rows; r++) {
 #pragma unroll
-                                for (int i = 0; i < 2; i++) {
-                                    const uint32_t j = lane + 32 * i;
-                                    uint16_t x;
-                                    asm volatile("ld.shared.u16 %0, [%1];" : "=h"(x) : "r"(box + r * 128 + (((j / 8) ^ (r & 7)) * 16) + j % 8 * 2) : "memory");
-                                    if (col - 32 + j < p.dim) dst[size_t(r) * p.dw_stride + j] = x;
+                                    for (int i = 0; i < 2; i++) {
+                                        const uint32_t j = lane + 32 * i;
+                                        uint16_t x;
+                                        asm volatile("ld.shared.u16 %0, [%1];" : "=h"(x) : "r"(box + r * 128 + (((j / 8) ^ (r & 7)) * 16) + j % 8 * 2) : "memory");
+                                        if (col - 32 + j < p.dim) dst[size_t(r) * p.dw_stride + j] = x;
+                                    }
                                 }
+                                __syncwarp();
                             }
-                            __syncwarp();
                         }
                     }
                 };
@@ -975,9 +1047,11 @@ __global__ void __launch_bounds__(256) rd_vocab_join_kernel(JoinParams p)
     pdl_start();
     const uint32_t row = blockIdx.x * 8 + (threadIdx.x >> 5);
     const int lane = threadIdx.x & 31;
-    if (row >= p.meta->m) return;
+    if (row >= (p.rows.direct ? p.n : p.meta->m)) return;
+    bool counts;
+    const int label = p.rows.label_row(row, counts);
     const float2 x = join_row(p.part + size_t(row) * p.parts, p.parts, lane);
-    write_row(x, true, p.label[row] >= 0 ? p.packed_target[row] : 0.0f, p.z, size_t(p.index[row]), lane, p.loss, p.lse, p.target);
+    write_row(x, counts, label >= 0 ? p.packed_target[row] : 0.0f, p.z, p.rows.token(row), lane, p.loss, p.lse, p.target);
 }
 
 // ------------------------------------------------------------------------------------------------ loss of a few tokens
@@ -1134,7 +1208,7 @@ __global__ void __launch_bounds__(128) rd_vocab_few_join_kernel(FewParams p)
 
 struct FinishParams {
     const float *dh;
-    const int *index;
+    Rows rows;
     const Meta *meta;
     size_t dh_rows, dh_stride, out_stride;
     uint32_t dim, splits;
@@ -1155,7 +1229,8 @@ template <bool BF16> __global__ void __launch_bounds__(256) rd_vocab_finish_kern
     const size_t step = p.dh_rows * p.dh_stride;
     for (uint32_t row = blockIdx.x; row < m; row += gridDim.x) {
         const float *src = p.dh + size_t(row) * p.dh_stride + j;        // rows hold a multiple of 8 values
-        uint16_t *dst = p.out + size_t(p.index[row]) * p.out_stride + j;
+        uint16_t *dst = p.out + p.rows.token(row) * p.out_stride + j;
+        const bool counts = p.rows.counts(row);            // else zeros, whatever the weight holds
         float4 sum = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
 #pragma unroll 4
         for (uint32_t s = 0; s < p.splits; s++) {
@@ -1165,7 +1240,7 @@ template <bool BF16> __global__ void __launch_bounds__(256) rd_vocab_finish_kern
             sum.z += x.z;
             sum.w += x.w;
         }
-        const uint32_t lo = pack2<BF16>(sum.x * unboost, sum.y * unboost), hi = pack2<BF16>(sum.z * unboost, sum.w * unboost);
+        const uint32_t lo = counts ? pack2<BF16>(sum.x * unboost, sum.y * unboost) : 0, hi = counts ? pack2<BF16>(sum.z * unboost, sum.w * unboost) : 0;
         if (p.wide && j + 4 <= p.dim) {
             *reinterpret_cast<uint2 *>(dst) = make_uint2(lo, hi);
         } else {
@@ -1252,7 +1327,8 @@ Layout lay_out(const VocabArgs &a, bool gradient, bool want_hidden)
     if (needs_align(a)) l.weight = w.take<uint16_t>(a.rows * l.packed_stride);
     if (!gradient) {
         l.target = w.take<float>(l.rows_padded);
-        l.part = w.take<float2>(l.rows_padded * (2 * ((a.rows + kTileN - 1) / kTileN)));
+        const size_t halves = 2 * ((a.rows + kTileN - 1) / kTileN);
+        l.part = w.take<float2>(l.rows_padded * (halves > kSms ? halves : kSms));    // smaller tiles: at most one per SM
     } else {
         l.gp = w.take<float>(l.rows_padded);
         l.gt = w.take<float>(l.rows_padded);
@@ -1351,9 +1427,21 @@ template <int KIND> cudaError_t launch_mma(const MmaParams &p, bool bf16, int cg
     return bf16 ? launch_mma<KIND, true, 1>(p, device, most_units, stream) : launch_mma<KIND, false, 1>(p, device, most_units, stream);
 }
 
+// Whether the products read the hidden rows where they lie: one tile of tokens, in rows that TMA can address.
+bool is_direct(const VocabArgs &a) { return a.n <= kRowsM && reinterpret_cast<uintptr_t>(a.hidden) % 16 == 0 && a.hidden_stride % 8 == 0 && a.hidden_stride > 0; }
+
 // Counting and packing, and the weight's aligned copy where one is needed.
 cudaError_t prepare(const VocabArgs &a, const Layout &l, bool gradient, const uint16_t **weight, size_t *weight_stride)
 {
+    cudaError_t e = cudaSuccess;
+    *weight = static_cast<const uint16_t *>(a.weight);
+    *weight_stride = a.weight_stride;
+    if (l.weight) {
+        e = launch(rd_vocab_align_kernel, 1184, kPackThreads, a.stream, l.weight, uint32_t(l.packed_stride), *weight, a.weight_stride, a.rows, uint32_t(a.dim));
+        *weight = l.weight;
+        *weight_stride = l.packed_stride;
+    }
+    if (e != cudaSuccess || is_direct(a)) return e;
     PackParams p{};
     p.hidden = static_cast<const uint16_t *>(a.hidden);
     p.labels = a.labels;
@@ -1385,7 +1473,6 @@ cudaError_t prepare(const VocabArgs &a, const Layout &l, bool gradient, const ui
     p.grad_hidden_stride = a.grad_hidden_stride;
     p.gradient = gradient;
     p.fp16 = !a.bf16;
-    cudaError_t e = cudaSuccess;
     unsigned tiles = 0;
     if (a.n >= kCountFrom) {
         tiles = unsigned((a.n + kCountTile - 1) / kCountTile);
@@ -1400,14 +1487,6 @@ cudaError_t prepare(const VocabArgs &a, const Layout &l, bool gradient, const ui
         const unsigned blocks = unsigned((a.n + 7) / 8);
         e = launch(rd_vocab_pack_kernel<8>, blocks + (gradient ? kZeroPad / 8 : 0), kPackThreads, a.stream, p, blocks, tiles);
     }
-    if (e != cudaSuccess) return e;
-    *weight = static_cast<const uint16_t *>(a.weight);
-    *weight_stride = a.weight_stride;
-    if (l.weight) {
-        e = launch(rd_vocab_align_kernel, 1184, kPackThreads, a.stream, l.weight, uint32_t(l.packed_stride), *weight, a.weight_stride, a.rows, uint32_t(a.dim));
-        *weight = l.weight;
-        *weight_stride = l.packed_stride;
-    }
     return e;
 }
 
@@ -1421,14 +1500,30 @@ uint32_t token_group(size_t dim, size_t tile_m)
 // Rows of a left operand that a thread block brings in: all 128, or as many as there are tokens.
 size_t a_rows(size_t n) { return n < kRowsM ? round_up(n, 8) : kRowsM; }
 
+Rows rows_of(const VocabArgs &a, const Layout &l) { return Rows{l.index, l.label, a.labels, a.first_row, a.rows, is_direct(a), a.wide_labels}; }
+
+// The hidden rows as the logits' left operand.
+bool encode_hidden(CUtensorMap *map, const VocabArgs &a, const Layout &l)
+{
+    return is_direct(a) ? encode(map, a.bf16, a.hidden, a.dim, a.n, a.hidden_stride, uint32_t(a_rows(a.n)))
+                        : encode(map, a.bf16, l.packed, a.dim, l.rows_padded, l.packed_stride, uint32_t(a_rows(a.n)));
+}
+
+// Columns of the logits' tiles: 256, or fewer where that leaves half of the thread blocks (pairs) without a tile.
+uint32_t tile_columns(size_t tiles_m, size_t rows, int cg)
+{
+    size_t n = kTileN;
+    while (n > 64 && tiles_m * ((rows + n - 1) / n) * 2 <= kSms / cg) n /= 2;
+    return uint32_t(n);
+}
+
 void common(MmaParams &q, const VocabArgs &a, const Layout &l, int cg)
 {
     q.meta = l.meta;
-    q.label = l.label;
+    q.rows = rows_of(a, l);
+    q.direct.n = uint32_t(a.n);
     q.dim = uint32_t(a.dim);
     q.group = token_group(a.dim, size_t(kRowsM) * cg);
-    q.index = l.index;
-    q.early = l.weight == nullptr;
     q.a_rows = uint32_t(a_rows(a.n));
     q.scale = a.scale;
     q.scale2 = a.scale * kLog2e;
@@ -1507,17 +1602,18 @@ cudaError_t vocab_loss(const VocabArgs &a)
     if (e != cudaSuccess) return e;
     MmaParams q{};
     common(q, a, l, cg);
-    if (!encode(&q.a_k, a.bf16, l.packed, a.dim, l.rows_padded, l.packed_stride, uint32_t(a_rows(a.n))) || !encode(&q.b_k, a.bf16, weight, a.dim, a.rows, weight_stride, kTileN / cg))
-        return cudaErrorInvalidValue;
+    const size_t tiles_m = (a.n + tile_m - 1) / tile_m;
+    q.tile_n = tile_columns(tiles_m, a.rows, cg);
+    const size_t tiles_n = (a.rows + q.tile_n - 1) / q.tile_n;
+    if (!encode_hidden(&q.a_k, a, l) || !encode(&q.b_k, a.bf16, weight, a.dim, a.rows, weight_stride, q.tile_n / cg)) return cudaErrorInvalidValue;
     q.part = l.part;
-    q.parts = uint32_t(2 * ((a.rows + kTileN - 1) / kTileN));
+    q.parts = uint32_t(q.tile_n == kTileN ? 2 * tiles_n : tiles_n);
     q.target = l.target;
     q.piece0 = 0;
     q.piece = uint32_t(a.rows);
-    const size_t units = (a.n + tile_m - 1) / tile_m * ((a.rows + kTileN - 1) / kTileN);
-    e = launch_mma<kStats>(q, a.bf16, cg, device, units, a.stream);
+    e = launch_mma<kStats>(q, a.bf16, cg, device, tiles_m * tiles_n, a.stream);
     if (e != cudaSuccess) return e;
-    const JoinParams j{l.part, l.target, l.index, l.label, l.meta, q.parts, a.z_loss, a.loss, a.lse_out, a.target};
+    const JoinParams j{l.part, l.target, q.rows, l.meta, uint32_t(a.n), q.parts, a.z_loss, a.loss, a.lse_out, a.target};
     return launch(rd_vocab_join_kernel, unsigned((a.n + 7) / 8), 256, a.stream, j);
 }
 
@@ -1548,7 +1644,12 @@ cudaError_t vocab_loss_grad(const VocabArgs &a)
     grads.dw_tma = reinterpret_cast<uintptr_t>(a.grad_weight) % 16 == 0 && a.grad_weight_stride % 8 == 0;
     grads.want_dh = a.grad_hidden != nullptr;
     grads.want_dw = a.grad_weight != nullptr;
-    if (!encode(&logits.a_k, a.bf16, l.packed, a.dim, l.rows_padded, l.packed_stride, uint32_t(a_rows(a.n))) || !encode(&logits.b_k, a.bf16, weight, a.dim, a.rows, weight_stride, kTileN / cg) ||
+    const size_t tiles_m = (a.n + tile_m - 1) / tile_m, tiles_d = (a.dim + kTileN - 1) / kTileN;
+    logits.tile_n = tile_columns(tiles_m, a.rows < l.piece ? a.rows : l.piece, cg);
+    if (is_direct(a))
+        logits.direct = Direct{uint32_t(a.n), static_cast<const uint16_t *>(a.hidden), a.hidden_stride, a.grad_weight ? l.packed : nullptr, uint32_t(l.packed_stride), a.lse,
+                               a.grad_loss, a.grad_loss_stride, a.scale, a.z_loss, l.meta, a.dim % 8 == 0};
+    if (!encode_hidden(&logits.a_k, a, l) || !encode(&logits.b_k, a.bf16, weight, a.dim, a.rows, weight_stride, logits.tile_n / cg) ||
         !encode(&grads.a_k, a.bf16, l.dx, l.dx_stride, l.rows_padded, l.dx_stride, uint32_t(a_rows(a.n))) || !encode(&grads.a_mn, a.bf16, l.dx, l.dx_stride, l.rows_padded, l.dx_stride, 64) ||
         !encode(&logits.dx_out, a.bf16, l.dx, l.dx_stride, l.rows_padded, l.dx_stride, 32) || !encode(&grads.b_mn, a.bf16, weight, a.dim, a.rows, weight_stride, 64) || !encode(&grads.b2_mn, a.bf16, l.packed, a.dim, l.rows_padded, l.packed_stride, 64))
         return cudaErrorInvalidValue;
@@ -1560,13 +1661,12 @@ cudaError_t vocab_loss_grad(const VocabArgs &a)
     }
     if (grads.want_dh && !whole && !encode_dh(&grads.dh_out, l.dh, l.dh_stride, a.n, l.splits)) return cudaErrorInvalidValue;
     if (grads.want_dw && grads.dw_tma && !encode(&grads.dw_out, a.bf16, a.grad_weight, a.dim, a.rows, a.grad_weight_stride, 32)) return cudaErrorInvalidValue;
-    const size_t tiles_m = (a.n + tile_m - 1) / tile_m, tiles_d = (a.dim + kTileN - 1) / kTileN;
     for (size_t v = 0; v < a.rows; v += l.piece) {
         const size_t piece = a.rows - v < l.piece ? a.rows - v : l.piece;
         logits.piece0 = grads.piece0 = uint32_t(v);
         logits.piece = grads.piece = uint32_t(piece);
-        grads.first_piece = v == 0;
-        e = launch_mma<kDlogits>(logits, a.bf16, cg, device, tiles_m * ((piece + kTileN - 1) / kTileN), a.stream);
+        logits.first_piece = grads.first_piece = v == 0;
+        e = launch_mma<kDlogits>(logits, a.bf16, cg, device, tiles_m * ((piece + logits.tile_n - 1) / logits.tile_n), a.stream);
         if (e != cudaSuccess) return e;
         const size_t units = (grads.want_dh ? tiles_m * tiles_d * l.splits : 0) + (grads.want_dw ? (piece + tile_m - 1) / tile_m * tiles_d : 0);
         e = launch_mma<kGrads>(grads, a.bf16, cg, device, units, a.stream);
@@ -1574,7 +1674,7 @@ cudaError_t vocab_loss_grad(const VocabArgs &a)
     }
     if (a.grad_hidden && !whole) {
         const bool wide = reinterpret_cast<uintptr_t>(a.grad_hidden) % 8 == 0 && a.grad_hidden_stride % 4 == 0;
-        const FinishParams f{l.dh, l.index, l.meta, a.n, l.dh_stride, a.grad_hidden_stride, uint32_t(a.dim), uint32_t(l.splits), static_cast<uint16_t *>(a.grad_hidden), wide};
+        const FinishParams f{l.dh, grads.rows, l.meta, a.n, l.dh_stride, a.grad_hidden_stride, uint32_t(a.dim), uint32_t(l.splits), static_cast<uint16_t *>(a.grad_hidden), wide};
         const dim3 grid(unsigned(a.n < 65536 ? a.n : 65536), unsigned((a.dim + kFinishColumns - 1) / kFinishColumns));
         e = a.bf16 ? launch(rd_vocab_finish_kernel<true>, grid, 256, a.stream, f) : launch(rd_vocab_finish_kernel<false>, grid, 256, a.stream, f);
     }

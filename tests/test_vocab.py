@@ -171,7 +171,7 @@ def loss_reference(hidden, weight, labels, first, scale, z):
     return loss, lse, target, x, err, here, torch.where(here, at, 0)
 
 
-SHAPES = [(1, 1, 1), (3, 1000, 4096), (4, 777, 1001), (4, 70000, 40), (1, 33, 16400), (1, 300, 64), (2, 5, 3), (37, 257, 72), (128, 256, 64), (129, 511, 65), (300, 1000, 200), (513, 77, 1032), (40, 5000, 33), (1, 32768, 128)]
+SHAPES = [(1, 1, 1), (3, 1000, 4096), (4, 777, 1001), (4, 70000, 40), (1, 33, 16400), (9, 100, 72), (64, 9000, 128), (100, 20000, 40), (1, 300, 64), (2, 5, 3), (37, 257, 72), (128, 256, 64), (129, 511, 65), (300, 1000, 200), (513, 77, 1032), (40, 5000, 33), (1, 32768, 128)]
 
 
 def vocab_case(n, rows, dim, dtype, seed, ignored=0.25, first=0, label_dtype=torch.int64):
