@@ -362,6 +362,7 @@ struct alignas(64) MmaParams {
     uint32_t piece0, piece;   // first row of the piece and its rows
     uint32_t dim;
     uint32_t tile_n;          // logits: columns of a tile, 256, 128 or 64
+    uint32_t stages, stage;   // logits: stages of the ring and bytes of one
     uint32_t group;           // token tiles that go over the vocabulary together
     uint32_t splits;          // parts that the sum over the piece is cut into for dh
     uint32_t a_rows;          // rows of a thread block's left operand that are brought in (fewer than 128 for few tokens)
@@ -415,6 +416,33 @@ __device__ __noinline__ bool bar_wait_slow(uint32_t bar, uint32_t parity)
     atomicExch(&g_vocab_status, 1);
     return false;
 }
+// The same by a whole warp, whose lanes go on together.  The copies and products are issued by one lane, but the loops around them
+// are the warp's: what is the same in every lane then stays in uniform registers, which is where the instructions want their
+// operands.  (Loops of a single lane spent some 500 cycles a step on moving them there, as long as the products of the step.)
+__device__ __noinline__ bool warp_wait_slow(uint32_t bar, uint32_t parity)
+{
+    const long long t0 = clock64();
+    do {
+        if (__all_sync(0xffffffffu, bar_try(bar, parity))) return true;
+    } while (__any_sync(0xffffffffu, clock64() - t0 < kWaitCycles));
+    atomicExch(&g_vocab_status, 1);
+    return false;
+}
+__device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity)
+{
+    return __all_sync(0xffffffffu, bar_try(bar, parity)) || __all_sync(0xffffffffu, warp_wait_slow(bar, parity));
+}
+__device__ __forceinline__ bool elect_one()
+{
+    uint32_t one;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "elect.sync _|p, 0xffffffff;\n\t"
+        "selp.b32 %0, 1, 0, p;\n\t}"
+        : "=r"(one));
+    return one;
+}
+
 __device__ __noinline__ void drain()
 {
     const long long t0 = clock64();
@@ -526,11 +554,12 @@ __device__ __forceinline__ void box_put(uint32_t box, int row, int unit, uint32_
 constexpr int kRowsM = 128;
 // Results leave through one box of 4 KB per epilogue warp, except the softmax statistics, which have the room for another stage.
 constexpr uint32_t kBox = 4096;
+constexpr uint32_t kMostStages = 16;      // logits with small tiles have more stages in the same room
 template <int KIND, int CG> struct Shape {
     static constexpr int tile_m = kRowsM * CG, rows_n = kTileN / CG;
     static constexpr uint32_t stage_a = kRowsM * kTileK * 2, stage_b = rows_n * kTileK * 2, stage = stage_a + stage_b;
     static constexpr int stages = CG == 1 ? 4 : KIND == kStats ? 7 : 6;
-    static constexpr uint32_t boxes = KIND == kStats ? 0 : kEpilogueWarps * kBox, smem = stages * stage + boxes + 1024 + 256;
+    static constexpr uint32_t boxes = KIND == kStats ? 0 : kEpilogueWarps * kBox, ring = stages * stage, smem = ring + boxes + 1024 + 512;
 };
 
 constexpr uint32_t kTileOverhead = 2;     // what a tile costs besides its products, in steps of the summed index
@@ -664,11 +693,12 @@ template <int KIND, int CG> struct Plan {
 };
 
 // A ring's stage and the parity of its turn.
-template <int N> struct Turn {
-    uint32_t s = 0, parity = 0;
+struct Turn {
+    uint32_t s = 0, parity = 0, stages;
+    __device__ __forceinline__ explicit Turn(uint32_t n) : stages(n) {}
     __device__ __forceinline__ void advance()
     {
-        if (++s == N) {
+        if (++s == stages) {
             s = 0;
             parity ^= 1;
         }
@@ -688,17 +718,18 @@ template <int KIND, bool BF16, int CG>
 __global__ void __launch_bounds__(kMmaThreads, 1) rd_vocab_mma_kernel(const __grid_constant__ MmaParams p)
 {
     using S = Shape<KIND, CG>;
-    constexpr int kStages = S::stages;
+    const uint32_t stages = KIND == kGrads ? uint32_t(S::stages) : p.stages, stage = KIND == kGrads ? uint32_t(S::stage) : p.stage;
+    const uint32_t stage_a = KIND == kGrads ? uint32_t(S::stage_a) : p.a_rows * kTileK * 2;
     extern __shared__ unsigned char smem_raw[];
     const uint32_t smem = (smem_addr(smem_raw) + 1023) & ~1023u;
-    const uint32_t boxes = smem + kStages * S::stage, bars = boxes + S::boxes;
+    const uint32_t boxes = smem + S::ring, bars = boxes + S::boxes;
     // barriers: full[stage], empty[stage], accumulator full[2], empty[2]; then the tensor memory address
-    const uint32_t full = bars, empty = bars + 8 * kStages, acc_full = bars + 16 * kStages, acc_empty = acc_full + 16, tmem_slot = acc_empty + 16;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t full = bars, empty = bars + 8 * kMostStages, acc_full = bars + 16 * kMostStages, acc_empty = acc_full + 16, tmem_slot = acc_empty + 16;
+    const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
     const uint32_t rank = CG == 2 ? blockIdx.x & 1 : 0;
 
     if (threadIdx.x == 0) {
-        for (int s = 0; s < kStages; s++) {
+        for (uint32_t s = 0; s < stages; s++) {
             bar_init(full + 8 * s, 1);
             bar_init(empty + 8 * s, 1);
         }
@@ -732,70 +763,77 @@ __global__ void __launch_bounds__(kMmaThreads, 1) rd_vocab_mma_kernel(const __gr
     const bool direct = KIND != kGrads && CG == 1 && p.rows.direct;
     if (direct) pdl_wait_first();
     else pdl_start();
-    const uint32_t m = direct ? p.direct.n : p.meta->m;
+    const uint32_t m = __shfl_sync(0xffffffffu, direct ? p.direct.n : p.meta->m, 0);
     Plan<KIND, CG> plan(p, m);
     bool dead = false;
 
     if (warp == 0 || warp == 3) {
-        // one thread brings in the left operand, another the right one
-        if (lane == 0) {
-            Turn<kStages> turn;
-            Work w;
-            const uint32_t lead = leader_bar<CG>(full);
-            while (!dead && plan.next(w)) {
-                const uint32_t rows_n = KIND != kGrads ? p.tile_n / CG : uint32_t(S::rows_n);
-                const uint32_t m0 = w.m0 + rank * kRowsM, n0 = w.n0 + rank * rows_n;
-                for (uint32_t k = 0, kk = w.k0; k < w.kblocks; k++, kk += kTileK, turn.advance()) {
-                    const uint32_t a = smem + turn.s * S::stage, b = a + S::stage_a, bar = lead + 8 * turn.s;
-                    if (!bar_wait(empty + 8 * turn.s, turn.parity ^ 1)) { dead = true; break; }
-                    if (warp == 0) {
+        // one warp brings in the left operand, another the right one
+        const bool elected = elect_one();
+        Turn turn(stages);
+        Work w;
+        const uint32_t lead = leader_bar<CG>(full);
+        while (!dead && plan.next(w)) {
+            const uint32_t rows_n = KIND != kGrads ? p.tile_n / CG : uint32_t(S::rows_n);
+            const uint32_t m0 = w.m0 + rank * kRowsM, n0 = w.n0 + rank * rows_n;
+            const uint32_t bytes = CG * ((w.product == 2 ? S::stage_a : p.a_rows * kTileK * 2) + rows_n * kTileK * 2);
+            const CUtensorMap *map_b = w.product == 1 ? &p.b_mn : &p.b2_mn;
+            const uint32_t y0 = w.product == 1 ? p.piece0 : 0;
+            for (uint32_t k = 0, kk = w.k0; k < w.kblocks; k++, kk += kTileK, turn.advance()) {
+                const uint32_t a = smem + turn.s * stage, b = a + stage_a, bar = lead + 8 * turn.s;
+                if (!warp_wait(empty + 8 * turn.s, turn.parity ^ 1)) { dead = true; break; }
+                if (warp == 0) {
+                    if (elected) {
                         // the copies of both thread blocks and both operands count at the first block's barrier
-                        const uint32_t a_bytes = w.product == 2 ? S::stage_a : p.a_rows * kTileK * 2;
-                        if (rank == 0) bar_expect(full + 8 * turn.s, CG * (a_bytes + rows_n * kTileK * 2));
+                        if (rank == 0) bar_expect(full + 8 * turn.s, bytes);
                         if (w.product == 2) {
 #pragma unroll
                             for (int j = 0; j < kRowsM / 64; j++) tma_load<CG>(a + j * 8192, &p.a_mn, m0 + 64 * j, kk, bar);
                         } else {
                             tma_load<CG>(a, &p.a_k, kk, m0, bar);
                         }
-                    } else if (KIND != kGrads) {
+                    }
+                } else if (elected) {
+                    if (KIND != kGrads) {
                         tma_load<CG>(b, &p.b_k, kk, p.piece0 + n0, bar);
                     } else {
-                        const CUtensorMap *map = w.product == 1 ? &p.b_mn : &p.b2_mn;
-                        const uint32_t y = w.product == 1 ? p.piece0 + kk : kk;
 #pragma unroll
-                        for (int j = 0; j < S::rows_n / 64; j++) tma_load<CG>(b + j * 8192, map, n0 + 64 * j, y, bar);
+                        for (int j = 0; j < S::rows_n / 64; j++) tma_load<CG>(b + j * 8192, map_b, n0 + 64 * j, y0 + kk, bar);
                     }
                 }
             }
-            // the last stages' arrivals have to land while the barriers still exist
-            for (int s = 0; s < kStages && !dead; s++, turn.advance()) dead = !bar_wait(empty + 8 * turn.s, turn.parity ^ 1);
-            if (dead) drain();
         }
+        // the last stages' arrivals have to land while the barriers still exist
+        for (uint32_t s = 0; s < stages && !dead; s++, turn.advance()) dead = !warp_wait(empty + 8 * turn.s, turn.parity ^ 1);
+        if (dead) drain();
     } else if (warp == 1) {
-        if (lane == 0 && rank == 0) {
+        if (rank == 0) {
+            const bool elected = elect_one();
             const uint32_t desc = 1u << 4 | (BF16 ? 1u << 7 | 1u << 10 : 0u) | (KIND != kGrads ? p.tile_n : kTileN) / 8 << 17 | uint32_t(S::tile_m / 16) << 24;
-            Turn<kStages> turn;
+            Turn turn(stages);
             uint32_t tile = 0;
             Work w;
             while (!dead && plan.next(w)) {
                 if (w.kblocks == 0) continue;            // the epilogue takes zeros
                 const uint32_t buf = tile & 1;
-                if (!bar_wait(acc_empty + 8 * buf, (tile / 2 & 1) ^ 1)) { dead = true; break; }
+                if (!warp_wait(acc_empty + 8 * buf, (tile / 2 & 1) ^ 1)) { dead = true; break; }
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                 const bool ta = w.product == 2, tb = w.product != 0;
                 const uint32_t idesc = desc | (ta ? 1u << 15 : 0u) | (tb ? 1u << 16 : 0u);
                 const uint32_t step_a = ta ? 2048 >> 4 : 32 >> 4, step_b = tb ? 2048 >> 4 : 32 >> 4;
+                const uint32_t acc = tmem + buf * kTileN;
                 for (uint32_t k = 0; k < w.kblocks; k++, turn.advance()) {
-                    const uint32_t a = smem + turn.s * S::stage, b = a + S::stage_a;
-                    if (!bar_wait(full + 8 * turn.s, turn.parity)) { dead = true; break; }
+                    const uint32_t a = smem + turn.s * stage, b = a + stage_a;
+                    if (!warp_wait(full + 8 * turn.s, turn.parity)) { dead = true; break; }
                     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                     const uint64_t da = operand(a, ta), db = operand(b, tb);
+                    if (elected) {
 #pragma unroll
-                    for (int j = 0; j < kTileK / 16; j++) mma<CG>(tmem + buf * kTileN, da + j * step_a, db + j * step_b, idesc, k != 0 || j != 0);
-                    mma_commit<CG>(empty + 8 * turn.s);
+                        for (int j = 0; j < kTileK / 16; j++) mma<CG>(acc, da + j * step_a, db + j * step_b, idesc, k != 0 || j != 0);
+                        mma_commit<CG>(empty + 8 * turn.s);
+                    }
                 }
-                if (!dead) mma_commit<CG>(acc_full + 8 * buf);
+                if (!dead && elected) mma_commit<CG>(acc_full + 8 * buf);
                 tile++;
             }
             if (dead) drain();
@@ -1517,6 +1555,14 @@ uint32_t tile_columns(size_t tiles_m, size_t rows, int cg)
     return uint32_t(n);
 }
 
+// The ring of a logits kernel: as many stages as its room holds.
+template <int KIND> void set_ring(MmaParams &q, int cg)
+{
+    q.stage = (q.a_rows + q.tile_n / uint32_t(cg)) * kTileK * 2;
+    const uint32_t room = cg == 2 ? Shape<KIND, 2>::ring : Shape<KIND, 1>::ring;
+    q.stages = room / q.stage < kMostStages ? room / q.stage : kMostStages;
+}
+
 void common(MmaParams &q, const VocabArgs &a, const Layout &l, int cg)
 {
     q.meta = l.meta;
@@ -1604,6 +1650,7 @@ cudaError_t vocab_loss(const VocabArgs &a)
     common(q, a, l, cg);
     const size_t tiles_m = (a.n + tile_m - 1) / tile_m;
     q.tile_n = tile_columns(tiles_m, a.rows, cg);
+    set_ring<kStats>(q, cg);
     const size_t tiles_n = (a.rows + q.tile_n - 1) / q.tile_n;
     if (!encode_hidden(&q.a_k, a, l) || !encode(&q.b_k, a.bf16, weight, a.dim, a.rows, weight_stride, q.tile_n / cg)) return cudaErrorInvalidValue;
     q.part = l.part;
@@ -1646,6 +1693,7 @@ cudaError_t vocab_loss_grad(const VocabArgs &a)
     grads.want_dw = a.grad_weight != nullptr;
     const size_t tiles_m = (a.n + tile_m - 1) / tile_m, tiles_d = (a.dim + kTileN - 1) / kTileN;
     logits.tile_n = tile_columns(tiles_m, a.rows < l.piece ? a.rows : l.piece, cg);
+    set_ring<kDlogits>(logits, cg);
     if (is_direct(a))
         logits.direct = Direct{uint32_t(a.n), static_cast<const uint16_t *>(a.hidden), a.hidden_stride, a.grad_weight ? l.packed : nullptr, uint32_t(l.packed_stride), a.lse,
                                a.grad_loss, a.grad_loss_stride, a.scale, a.z_loss, l.meta, a.dim % 8 == 0};
