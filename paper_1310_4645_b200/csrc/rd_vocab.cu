@@ -900,7 +900,7 @@ __global__ void __launch_bounds__(kMmaThreads, 1) rd_vocab_mma_kernel(const __gr
             }
             // columns of the tile that the vocabulary has; in tiles of fewer than 256 the rest is another tile's
             const uint32_t limit = KIND != kGrads ? min(p.piece, w.n0 + p.tile_n) : 0;
-            const float unboost = KIND == kGrads ? p.meta->unboost : 1.0f;
+            const float unboost = KIND == kGrads && !BF16 ? p.meta->unboost : 1.0f;      // bf16: always 1, and no multiplication
             // the accumulators are free for the next tile but one as soon as their last columns are in registers
             auto release = [&]() {
                 asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
