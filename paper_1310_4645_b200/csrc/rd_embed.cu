@@ -25,10 +25,12 @@
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
+#include <atomic>
 #include <mutex>
 
 #include "rd.h"
 #include "rd_launch.h"
+#include "rd_ptx.h"
 
 namespace rd {
 
@@ -579,6 +581,167 @@ __global__ void __launch_bounds__(kThreads, 3) rd_embed_sum_kernel(const T *__re
     }
 }
 
+// The same for rows of whole 16-byte words from kStreamBytes on: the gradients' rows come through shared memory by bulk copies, so
+// that a warp has up to 24 KB on its way whatever the items look like (through registers a warp had the 1 to 4 KB of one item: the
+// whole gradient of 16384 tokens x 4096 bf16 into 131072 rows 216 us, this 209; of 65536 tokens into a slice of 32768 x 2048 92, 84).
+//   A warp takes 32 items at a time, one per lane, and sees their tokens as one sequence.  Lanes look up 32 tokens of it at a
+//   time; groups of 8 are copied to a ring of 3 groups, two groups ahead of the one that is added up.
+constexpr int kGroup = 8, kGroups = 3;
+constexpr uint32_t kSlab = 1024;          // bytes of a row that a warp takes: two words of 16 bytes per lane, 512 apart
+constexpr size_t kStreamBytes = 512;
+constexpr int kStreamThreads = 256;
+constexpr uint32_t kStreamSmem = kStreamThreads / 32 * (kGroups * kGroup * kSlab) + 128;
+
+__device__ int g_embed_status;
+
+template <typename T, typename O>
+__global__ void __launch_bounds__(kStreamThreads, 1) rd_embed_stream_kernel(const T *__restrict__ grad, size_t grad_stride, O *__restrict__ table, size_t table_stride,
+                                                                            uint32_t dim, uint32_t slabs, float scale, bool accumulate, GradWork w)
+{
+    constexpr uint32_t V = 16 / sizeof(T), kWords = kSlab / 16 / 32, kColumns = kSlab / sizeof(T);
+    extern __shared__ __align__(128) unsigned char ring[];
+    __shared__ __align__(8) unsigned long long bars[kStreamThreads / 32][kGroups];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const uint32_t slots = smem_addr(ring) + warp * (kGroups * kGroup * kSlab), bar0 = smem_addr(&bars[warp][0]);
+    if (lane < kGroups) bar_init(bar0 + 8 * lane, 1);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    __syncwarp();
+    pdl_start();
+    const uint32_t n_big = w.meta->n_big, others = w.big_room - n_big;
+    const uint64_t units = (uint64_t(n_big) + w.meta->n_items) * slabs, step = uint64_t(gridDim.x) * (kStreamThreads / 32);
+    uint32_t sent = 0;                                       // groups since the kernel began
+    for (uint64_t first = uint64_t(blockIdx.x) * (kStreamThreads / 32) + warp; first < units; first += 32 * step) {
+        // a lane's item, its slab, and where its tokens lie in the sequence
+        const uint64_t u = first + lane * step;
+        Item it{};
+        if (u < units) {
+            const size_t k = u / slabs;
+            it = w.items[k < n_big ? k : k + others];
+        }
+        const uint32_t slab = uint32_t(u % slabs);
+        uint32_t upto = it.count;
+#pragma unroll
+        for (int d = 1; d < 32; d *= 2) {
+            const uint32_t o = __shfl_up_sync(0xffffffffu, upto, d);
+            if (lane >= d) upto += o;
+        }
+        const uint32_t total = __shfl_sync(0xffffffffu, upto, 31), groups = (total + kGroup - 1) / kGroup, sent0 = sent;
+        const T *src = nullptr;
+        uint32_t bytes = 0;
+        int cur = -1;                                        // the item being added up, and its tokens that are left
+        uint32_t left = 0;
+        float acc[kWords][V];
+        for (uint32_t g = 0; g < groups + 2; g++) {
+            if (g < groups) {
+                if (g % (32 / kGroup) == 0) {
+                    // the next 32 tokens: whose they are, and their rows
+                    const uint32_t f = g * kGroup + lane;
+                    uint32_t owner = 0;                      // the first item that reaches beyond f
+#pragma unroll
+                    for (int d = 16; d; d /= 2)
+                        if (__shfl_sync(0xffffffffu, upto, owner + d - 1) <= f) owner += d;
+                    owner &= 31;
+                    const uint32_t begin = __shfl_sync(0xffffffffu, it.begin, owner), before = __shfl_sync(0xffffffffu, upto - it.count, owner);
+                    const uint32_t col = __shfl_sync(0xffffffffu, slab, owner) * kColumns;
+                    bytes = 0;
+                    if (f < total) {
+                        src = grad + size_t(w.list[begin + f - before]) * grad_stride + col;
+                        bytes = min(kSlab, uint32_t((dim - col) * sizeof(T)));
+                    }
+                }
+                const bool mine = uint32_t(lane) / kGroup == g % (32 / kGroup);
+                const uint32_t all = __reduce_add_sync(0xffffffffu, mine ? bytes : 0), s = sent % kGroups, bar = bar0 + 8 * s;
+                if (lane == 0) bar_expect(bar, all);
+                __syncwarp();
+                if (mine && bytes)
+                    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(slots + (s * kGroup + lane % kGroup) * kSlab),
+                                 "l"(src), "r"(bytes), "r"(bar)
+                                 : "memory");
+                sent++;
+            }
+            if (g < 2) continue;
+            // the group two back
+            const uint32_t t0 = (g - 2) * kGroup, G = sent0 + g - 2, s = G % kGroups, parity = G / kGroups & 1, bar = bar0 + 8 * s;
+            if (!__all_sync(0xffffffffu, bar_try(bar, parity))) {
+                const long long began = clock64();
+                bool done = false;
+                do done = __all_sync(0xffffffffu, bar_try(bar, parity));
+                while (!done && __any_sync(0xffffffffu, clock64() - began < kWaitCycles));
+                if (!done) {
+                    atomicExch(&g_embed_status, 1);
+                    drain();
+                    return;
+                }
+            }
+            for (int t = 0; t < kGroup && t0 + t < total; t++) {
+                if (left == 0) {
+                    do left = __shfl_sync(0xffffffffu, it.count, ++cur);
+                    while (left == 0);
+#pragma unroll
+                    for (uint32_t h = 0; h < kWords; h++)
+#pragma unroll
+                        for (uint32_t e = 0; e < V; e++) acc[h][e] = 0.0f;
+                }
+#pragma unroll
+                for (uint32_t h = 0; h < kWords; h++) {
+                    Vec<T, V> x;
+                    uint32_t(&b)[4] = *reinterpret_cast<uint32_t(*)[4]>(&x);
+                    asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
+                                 : "=r"(b[0]), "=r"(b[1]), "=r"(b[2]), "=r"(b[3])
+                                 : "r"(slots + (s * kGroup + t) * kSlab + h * 512 + lane * 16)
+                                 : "memory");
+#pragma unroll
+                    for (uint32_t e = 0; e < V; e++) acc[h][e] += widen<T>(x.v[e]);
+                }
+                if (--left) continue;
+                // the item is complete
+                const uint32_t row = __shfl_sync(0xffffffffu, it.row, cur), part = __shfl_sync(0xffffffffu, it.part, cur), parts = __shfl_sync(0xffffffffu, it.parts, cur);
+                const uint32_t begin = __shfl_sync(0xffffffffu, it.begin, cur) - part * kChunk, at_slab = __shfl_sync(0xffffffffu, slab, cur);
+                const uint32_t col0 = at_slab * kColumns + lane * V;
+                const Columns<int(V), false> cols{0, 0};
+                bool write = parts == 1;
+                if (parts > 1) {
+#pragma unroll
+                    for (uint32_t h = 0; h < kWords; h++) {
+                        Vec<float, V> x;
+#pragma unroll
+                        for (uint32_t e = 0; e < V; e++) x.v[e] = acc[h][e];
+                        if (col0 + h * 32 * V < dim) store<float, V>(w.partial + size_t(slot_of(begin, part)) * w.partial_stride + col0 + h * 32 * V, x);
+                    }
+                    __threadfence();
+                    __syncwarp();
+                    uint32_t finished = lane == 0 ? atomicAdd(&w.done[size_t(slot_of(begin, 0)) * slabs + at_slab], 1u) + 1 : 0;
+                    finished = __shfl_sync(0xffffffffu, finished, 0);
+                    write = finished == parts;
+                    if (write) {
+                        // whichever warp is last adds the row's partial sums up, in order
+                        __threadfence();
+#pragma unroll
+                        for (uint32_t h = 0; h < kWords; h++) {
+#pragma unroll
+                            for (uint32_t e = 0; e < V; e++) acc[h][e] = 0.0f;
+                            if (col0 + h * 32 * V < dim) {
+#pragma unroll 4
+                                for (uint32_t k = 0; k < parts; k++) {
+                                    const Vec<float, V> x = load<float, V>(w.partial + size_t(slot_of(begin, k)) * w.partial_stride + col0 + h * 32 * V);
+#pragma unroll
+                                    for (uint32_t e = 0; e < V; e++) acc[h][e] += x.v[e];
+                                }
+                            }
+                        }
+                    }
+                }
+                if (write) {
+#pragma unroll
+                    for (uint32_t h = 0; h < kWords; h++)
+                        if (col0 + h * 32 * V < dim) write_row(cols, table + size_t(row) * table_stride + col0 + h * 32 * V, acc[h], scale, accumulate);
+                }
+            }
+            __syncwarp();                                    // everyone has read the group's slots before they are filled again
+        }
+    }
+}
+
 // Zeros.  Thread blocks of a plain grid write 16 KB each, one after the other in memory: at 7.4 TB/s against 6.3 TB/s when the
 // blocks of a resident grid stride over the table (1 GiB, B200), whose stores drift apart.
 constexpr uint32_t kFillBytes = 16384;
@@ -675,11 +838,37 @@ template <typename O> cudaError_t launch_fill(const EmbedGradArgs &a, bool alone
 // From this size of table on the fork pays: the sort takes some 20 us, a fork and a join a few.
 constexpr size_t kForkBytes = size_t(32) << 20;
 
+template <typename T, typename O> cudaError_t launch_stream(const EmbedGradArgs &a, const GradWork &w, uint32_t slabs)
+{
+    static std::atomic<bool> ready[kMaxDevices];
+    int device = 0;
+    cudaError_t e = cudaGetDevice(&device);
+    if (e != cudaSuccess) return e;
+    if (device >= kMaxDevices || !ready[device].load(std::memory_order_acquire)) {
+        e = cudaFuncSetAttribute(rd_embed_stream_kernel<T, O>, cudaFuncAttributeMaxDynamicSharedMemorySize, kStreamSmem);
+        if (e != cudaSuccess) return e;
+        if (device < kMaxDevices) ready[device].store(true, std::memory_order_release);
+    }
+    const uint64_t units = uint64_t(max_big(a.n) + max_items(a.n, a.rows)) * slabs, blocks = (units + kStreamThreads / 32 - 1) / (kStreamThreads / 32);
+    cudaLaunchConfig_t c{};
+    cudaLaunchAttribute pdl = pdl_attribute();
+    c.gridDim = dim3(unsigned(blocks < 148 ? blocks : 148));
+    c.blockDim = dim3(kStreamThreads);
+    c.dynamicSmemBytes = kStreamSmem;
+    c.stream = a.stream;
+    c.attrs = &pdl;
+    c.numAttrs = 1;
+    return cudaLaunchKernelEx(&c, rd_embed_stream_kernel<T, O>, static_cast<const T *>(a.grad), a.grad_stride, static_cast<O *>(a.table), a.table_stride, uint32_t(a.dim), slabs,
+                              a.scale, a.accumulate, w);
+}
+
 template <typename T, typename O, int V, bool ELEMENTS> cudaError_t launch_grad(const EmbedGradArgs &a)
 {
     const GradWork w = layout(a.workspace, a.rows, a.dim, a.n);
     const uint32_t n = uint32_t(a.n);
-    const uint32_t vecs = uint32_t((a.dim + V - 1) / V), lanes = lanes_for(vecs), slabs = (vecs + lanes - 1) / lanes;
+    const bool stream = !ELEMENTS && a.dim * sizeof(T) >= kStreamBytes;
+    const uint32_t vecs = uint32_t((a.dim + V - 1) / V), lanes = lanes_for(vecs);
+    const uint32_t slabs = stream ? uint32_t((a.dim * sizeof(T) + kSlab - 1) / kSlab) : (vecs + lanes - 1) / lanes;
     if (n == 0) return a.accumulate ? cudaSuccess : launch_fill<O>(a, true);
     cudaError_t e = cudaSuccess;
     if (n <= kSmallTokens) {
@@ -707,6 +896,7 @@ template <typename T, typename O, int V, bool ELEMENTS> cudaError_t launch_grad(
         }
     }
     if (e != cudaSuccess) return e;
+    if (stream) return launch_stream<T, O>(a, w, slabs);
     const uint64_t units = uint64_t(max_big(n) + max_items(n, a.rows)) * slabs, blocks = (units + kThreads / lanes - 1) / (kThreads / lanes);
     return launch(rd_embed_sum_kernel<T, O, V, ELEMENTS>, unsigned(blocks < kSumBlocks ? blocks : kSumBlocks), kThreads, a.stream, static_cast<const T *>(a.grad), a.grad_stride,
                   static_cast<O *>(a.table), a.table_stride, uint32_t(a.dim), lanes, slabs, a.scale, a.accumulate, w);
@@ -741,6 +931,13 @@ cudaError_t embed_forward(const EmbedArgs &a)
 }
 
 size_t embed_backward_workspace(size_t rows, size_t dim, size_t n) { return layout(nullptr, rows, dim, n).bytes; }
+
+cudaError_t embed_status(int *status)
+{
+    cudaError_t e = cudaMemcpyFromSymbol(status, g_embed_status, sizeof(int));
+    const int zero = 0;
+    return e == cudaSuccess && *status ? cudaMemcpyToSymbol(g_embed_status, &zero, sizeof(int)) : e;
+}
 
 cudaError_t embed_backward(const EmbedGradArgs &a)
 {

@@ -26,6 +26,7 @@
 
 #include "rd.h"
 #include "rd_launch.h"
+#include "rd_ptx.h"
 
 namespace rd {
 
@@ -255,8 +256,6 @@ constexpr int kTileN = 256;
 constexpr int kTileK = 64;                // 128 bytes: one swizzle span
 constexpr int kEpilogueWarps = 8;
 constexpr int kMmaThreads = 128 + 32 * kEpilogueWarps;
-constexpr long long kWaitCycles = 4000000000ll;     // a wait gives up after about two seconds of SM clock
-constexpr long long kDrainCycles = 20000000ll;      // after that, copies in flight get ten milliseconds to land
 
 // Where a row of the products comes from: packed rows have their tokens and labels in lists, direct ones are the tokens themselves.
 struct Rows {
@@ -314,15 +313,13 @@ __device__ __forceinline__ void join_parts(float2 &x, float2 y)
 __device__ __forceinline__ float2 join_row(const float2 *part, uint32_t parts, int lane)
 {
     float2 x = make_float2(-INFINITY, 0.0f);
-    uint32_t k = lane;
-    for (; k + 96 < parts; k += 128) {
-        float2 y[4];
+    for (uint32_t k = lane; k < parts; k += 256) {
+        float2 y[8];
 #pragma unroll
-        for (int u = 0; u < 4; u++) y[u] = part[k + 32 * u];
+        for (int u = 0; u < 8; u++) y[u] = k + 32 * u < parts ? part[k + 32 * u] : make_float2(-INFINITY, 0.0f);
 #pragma unroll
-        for (int u = 0; u < 4; u++) join_parts(x, y[u]);
+        for (int u = 0; u < 8; u++) join_parts(x, y[u]);
     }
-    for (; k < parts; k += 32) join_parts(x, part[k]);
 #pragma unroll
     for (int d = 16; d; d /= 2) join_parts(x, make_float2(__shfl_down_sync(0xffffffffu, x.x, d), __shfl_down_sync(0xffffffffu, x.y, d)));
     return x;
@@ -372,16 +369,6 @@ struct alignas(64) MmaParams {
     float scale;
 };
 
-__device__ __forceinline__ uint32_t smem_addr(const void *p) { return uint32_t(__cvta_generic_to_shared(p)); }
-
-__device__ __forceinline__ void bar_init(uint32_t bar, uint32_t count)
-{
-    asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory");
-}
-__device__ __forceinline__ void bar_expect(uint32_t bar, uint32_t bytes)
-{
-    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
-}
 // The same barrier in the first thread block of the pair.
 template <int CG> __device__ __forceinline__ uint32_t leader_bar(uint32_t bar)
 {
@@ -394,18 +381,6 @@ template <int CG> __device__ __forceinline__ void bar_arrive_leader(uint32_t bar
 {
     if (CG == 1) asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
     else asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(leader_bar<CG>(bar)) : "memory");
-}
-__device__ __forceinline__ bool bar_try(uint32_t bar, uint32_t parity)
-{
-    uint32_t ok;
-    asm volatile(
-        "{\n\t.reg .pred p;\n\t"
-        "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
-        "selp.b32 %0, 1, 0, p;\n\t}"
-        : "=r"(ok)
-        : "r"(bar), "r"(parity)
-        : "memory");
-    return ok;
 }
 __device__ __noinline__ bool bar_wait_slow(uint32_t bar, uint32_t parity)
 {
@@ -443,11 +418,6 @@ __device__ __forceinline__ bool elect_one()
     return one;
 }
 
-__device__ __noinline__ void drain()
-{
-    const long long t0 = clock64();
-    while (clock64() - t0 < kDrainCycles) {}
-}
 // False when the wait gave up.
 __device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity) { return bar_try(bar, parity) || bar_wait_slow(bar, parity); }
 
@@ -1733,10 +1703,15 @@ cudaError_t vocab_status(int *status)
 {
     cudaError_t e = cudaDeviceSynchronize();
     if (e != cudaSuccess) return e;
+    int of_embed = 0;
+    e = embed_status(&of_embed);
+    if (e != cudaSuccess) return e;
     e = cudaMemcpyFromSymbol(status, g_vocab_status, sizeof(int));
     if (e != cudaSuccess) return e;
     const int zero = 0;
-    return *status ? cudaMemcpyToSymbol(g_vocab_status, &zero, sizeof(int)) : cudaSuccess;
+    if (*status) e = cudaMemcpyToSymbol(g_vocab_status, &zero, sizeof(int));
+    *status |= of_embed;
+    return e;
 }
 
 }  // namespace rd

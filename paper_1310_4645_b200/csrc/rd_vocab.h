@@ -61,7 +61,8 @@ size_t vocab_loss_workspace(const VocabArgs &a);
 cudaError_t vocab_loss(const VocabArgs &a);
 size_t vocab_loss_grad_workspace(const VocabArgs &a, bool want_hidden);
 cudaError_t vocab_loss_grad(const VocabArgs &a);
-// Waits for the device, returns and clears the word in which a kernel notes a wait that it gave up.
+// The word in which a kernel notes a wait that it gave up, cleared; vocab_status waits for the device first and covers both files.
+cudaError_t embed_status(int *status);
 cudaError_t vocab_status(int *status);
 
 }  // namespace rd
