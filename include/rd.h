@@ -489,7 +489,7 @@ RD_API int rd_embed(const void *d_table, size_t table_stride, size_t rows, size_
 /*
  * rd_embed_grad -- the gradient of rd_embed with respect to the table:
  *   grad_table[v] = (accumulate ? grad_table[v] : 0) + scale * sum over the i with ids[i] - first_row = v of grad_out[i].
- * Tokens are sorted by row; sums are fp32, in ascending order of i (in runs of 64 tokens, whose sums are added in
+ * Tokens are sorted by row; sums are fp32, in ascending order of i (in runs of 32 tokens, whose sums are added in
  * ascending order), rounded once.  Every row of the table is written; with accumulate only those that have tokens.
  *   dtype        RD_FP32, RD_BF16 or RD_FP16: grad_out.
  *   table_dtype  dtype, or RD_FP32.
