@@ -39,7 +39,8 @@ namespace {
 constexpr int kThreads = 256;
 constexpr uint32_t kChunk = 32;         // tokens that one thread group adds up
 constexpr uint32_t kBigItem = 8;        // items with more tokens are dealt out first, so that no thread group meets one at its end
-constexpr uint32_t kSmallTokens = 8192; // up to here every token counts over all others
+constexpr uint32_t kSmallTokens = 4096; // up to here every token counts over all others (4096 tokens 9 us, 8000 tokens 33 us; the
+                                        // sort of more takes 16 us)
 
 template <typename T> __device__ __forceinline__ float widen(T v);
 template <> __device__ __forceinline__ float widen<float>(float v) { return v; }
@@ -565,7 +566,7 @@ __global__ void __launch_bounds__(kThreads, 3) rd_embed_sum_kernel(const T *__re
                     __threadfence();
 #pragma unroll
                     for (int e = 0; e < V; e++) acc[e] = 0.0f;
-#pragma unroll 2
+#pragma unroll 4
                     for (uint32_t k = 0; k < it.parts; k++) {
                         const Vec<float, V> x = cols.get(const_cast<const float *>(partial) + size_t(slot_of(begin, k)) * w.partial_stride);
 #pragma unroll
@@ -902,18 +903,16 @@ template <typename T, typename O, int V, bool ELEMENTS> cudaError_t launch_grad(
                   static_cast<O *>(a.table), a.table_stride, uint32_t(a.dim), lanes, slabs, a.scale, a.accumulate, w);
 }
 
-// Whole vectors of 32 or 16 bytes when both matrices' rows begin and end on such boundaries (lookup of 16384 rows of 8 KB, B200:
-// 35 us with 32-byte accesses, 39 with 16-byte ones), else single elements.
+// Vectors of 16 bytes of the gradient's rows when both matrices' rows are made of such, else single elements.
 template <typename T, typename O> cudaError_t pick_grad(const EmbedGradArgs &a)
 {
     constexpr int V = 16 / sizeof(T);
-    auto fits = [&](size_t vec) {
-        const size_t to = vec * sizeof(O) < 32 ? vec * sizeof(O) : 32;
-        return vector_rows(a.grad, a.grad_stride, a.dim, sizeof(T), vec * sizeof(T)) && vector_rows(a.table, a.table_stride, a.dim, sizeof(O), to);
-    };
-    return fits(2 * V) ? launch_grad<T, O, 2 * V, false>(a) : fits(V) ? launch_grad<T, O, V, false>(a) : launch_grad<T, O, 8, true>(a);
+    const bool wide = vector_rows(a.grad, a.grad_stride, a.dim, sizeof(T), 16) && vector_rows(a.table, a.table_stride, a.dim, sizeof(O), V * sizeof(O));
+    return wide ? launch_grad<T, O, V, false>(a) : launch_grad<T, O, 8, true>(a);
 }
 
+// Vectors of 32 or 16 bytes when both matrices' rows begin and end on such boundaries (16384 rows of 8 KB, B200: 35 us with 32-byte
+// accesses, 39 with 16-byte ones), else single elements.
 template <typename T> cudaError_t pick_embed(const EmbedArgs &a)
 {
     constexpr int V = 16 / sizeof(T);

@@ -99,7 +99,7 @@ def grad_reference(grad, ids, rows, first, scale, base=None):
 @pytest.mark.parametrize("dtype, out", [(torch.float32, torch.float32), (torch.bfloat16, torch.bfloat16), (torch.bfloat16, torch.float32),
                                         (torch.float16, torch.float16), (torch.float16, torch.float32)])
 @pytest.mark.parametrize("n, rows, dim, pad, ids", [(1, 5, 8, 0, "uniform"), (3, 1, 1, 0, "uniform"), (500, 37, 24, 0, "uniform"), (64, 9, 65, 1, "same"),
-                                                    (65, 9, 64, 0, "same"), (1000, 3000, 520, 8, "skewed"), (4096, 3, 48, 0, "skewed"), (8193, 900, 64, 16, "uniform"), (9001, 1025, 40, 0, "skewed"),
+                                                    (65, 9, 64, 0, "same"), (1000, 3000, 520, 8, "skewed"), (4096, 3, 48, 0, "skewed"), (4097, 900, 64, 16, "uniform"), (9001, 1025, 40, 0, "skewed"),
                                                     (70000, 2050, 8, 0, "skewed"), (300000, 11, 4, 0, "same"), (20000, 3, 520, 0, "same"), (5000, 70, 1032, 8, "skewed"), (50, 40, 33, 0, "outside")])
 @pytest.mark.parametrize("accumulate", [False, True])
 def test_embed_grad(dtype, out, n, rows, dim, pad, ids, accumulate):
