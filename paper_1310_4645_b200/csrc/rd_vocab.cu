@@ -1064,8 +1064,10 @@ __global__ void __launch_bounds__(256) rd_vocab_join_kernel(JoinParams p)
 
 // ------------------------------------------------------------------------------------------------ loss of a few tokens
 
-// Up to four tokens, as when a server scores what it generates: the weight's bytes are all that counts, so no tensor cores and no
-// packing, but warps that stream four rows of the weight at a time past the hidden rows in shared memory.
+// One token, as when a server scores what it generates, and up to four on a weight that TMA cannot address: the weight's bytes are
+// all that counts, so no tensor cores, but warps that stream four rows of the weight at a time past the hidden rows in shared memory.
+// Weight 32768 x 1024, B200, tensor cores / this: 1 token 17.3 / 16.4 us, 2 17.9 / 19.2, 4 17.6 / 27.6; dim 1001, which the tensor
+// cores need a copy for: 1 token 74 / 32, 4 75 / 40.
 constexpr size_t kFewTokens = 4;
 constexpr size_t kFewBytes = 32768;       // of hidden rows in shared memory
 constexpr int kFewRows = 4;
@@ -1545,8 +1547,7 @@ void common(MmaParams &q, const VocabArgs &a, const Layout &l, int cg)
     q.scale2 = a.scale * kLog2e;
 }
 
-// Measured on B200, weight 32768 x 1024, the tensor core path / this one: 1 token 18.7 / FEW1 us, 4 tokens FEWA / FEWB us.
-bool is_few(const VocabArgs &a) { return a.n <= kFewTokens && a.n * round_up(a.dim, 8) * 2 <= kFewBytes; }
+bool is_few(const VocabArgs &a) { return a.n <= (needs_align(a) ? kFewTokens : 1) && a.n * round_up(a.dim, 8) * 2 <= kFewBytes; }
 
 template <bool BF16, int V, int N> cudaError_t launch_few(const VocabArgs &a, const FewParams &p, unsigned blocks)
 {
@@ -1560,9 +1561,11 @@ template <bool BF16, int V, int N> cudaError_t launch_few(const VocabArgs &a, co
     c.numAttrs = 1;
     return cudaLaunchKernelEx(&c, rd_vocab_few_kernel<BF16, V, N>, p);
 }
-template <bool BF16, int V> cudaError_t launch_few(const VocabArgs &a, const FewParams &p, unsigned blocks)
+template <bool BF16> cudaError_t launch_few(const VocabArgs &a, const FewParams &p, unsigned blocks)
 {
-    return a.n == 1 ? launch_few<BF16, V, 1>(a, p, blocks) : a.n == 2 ? launch_few<BF16, V, 2>(a, p, blocks) : launch_few<BF16, V, 4>(a, p, blocks);
+    // TMA's alignment and whole words of 16 bytes
+    if (!needs_align(a) && a.dim % 8 == 0) return launch_few<BF16, 8, 1>(a, p, blocks);
+    return a.n == 1 ? launch_few<BF16, 1, 1>(a, p, blocks) : a.n == 2 ? launch_few<BF16, 1, 2>(a, p, blocks) : launch_few<BF16, 1, 4>(a, p, blocks);
 }
 
 cudaError_t vocab_loss_few(const VocabArgs &a)
@@ -1589,9 +1592,7 @@ cudaError_t vocab_loss_few(const VocabArgs &a)
     p.loss = a.loss;
     p.lse = a.lse_out;
     p.target = a.target;
-    const bool wide = reinterpret_cast<uintptr_t>(a.weight) % 16 == 0 && a.weight_stride % 8 == 0 && a.dim % 8 == 0;
-    const cudaError_t e = a.bf16 ? wide ? launch_few<true, 8>(a, p, blocks) : launch_few<true, 1>(a, p, blocks)
-                                 : wide ? launch_few<false, 8>(a, p, blocks) : launch_few<false, 1>(a, p, blocks);
+    const cudaError_t e = a.bf16 ? launch_few<true>(a, p, blocks) : launch_few<false>(a, p, blocks);
     if (e != cudaSuccess) return e;
     return launch(rd_vocab_few_join_kernel, unsigned(a.n), 128, a.stream, p);
 }
