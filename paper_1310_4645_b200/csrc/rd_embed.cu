@@ -583,14 +583,15 @@ __global__ void __launch_bounds__(kThreads, 3) rd_embed_sum_kernel(const T *__re
 }
 
 // The same for rows of whole 16-byte words from kStreamBytes on: the gradients' rows come through shared memory by bulk copies, so
-// that a warp has up to 24 KB on its way whatever the items look like (through registers a warp had the 1 to 4 KB of one item: the
-// whole gradient of 16384 tokens x 4096 bf16 into 131072 rows 216 us, this 209; of 65536 tokens into a slice of 32768 x 2048 92, 84).
+// that a warp has up to 12 KB on its way whatever the items look like (through registers a warp had the 1 to 4 KB of one item: the
+// whole gradient of 16384 tokens x 4096 bf16 into 131072 rows 216 us, this 201; of 65536 tokens into a slice of 32768 x 2048 92, 77.
+// 8 warps with 24 KB each: 207, 81; 24 with 8 KB: 201, 81; 32 with 6 KB: 208, 95).
 //   A warp takes 32 items at a time, one per lane, and sees their tokens as one sequence.  Lanes look up 32 tokens of it at a
-//   time; groups of 8 are copied to a ring of 3 groups, two groups ahead of the one that is added up.
-constexpr int kGroup = 8, kGroups = 3;
+//   time; groups of 4 are copied to a ring of 3 groups, two groups ahead of the one that is added up.
+constexpr int kGroup = 4, kGroups = 3;
 constexpr uint32_t kSlab = 1024;          // bytes of a row that a warp takes: two words of 16 bytes per lane, 512 apart
 constexpr size_t kStreamBytes = 512;
-constexpr int kStreamThreads = 256;
+constexpr int kStreamThreads = 512;
 constexpr uint32_t kStreamSmem = kStreamThreads / 32 * (kGroups * kGroup * kSlab) + 128;
 
 __device__ int g_embed_status;
@@ -718,17 +719,24 @@ __global__ void __launch_bounds__(kStreamThreads, 1) rd_embed_stream_kernel(cons
                         // whichever warp is last adds the row's partial sums up, in order
                         __threadfence();
 #pragma unroll
-                        for (uint32_t h = 0; h < kWords; h++) {
+                        for (uint32_t h = 0; h < kWords; h++)
 #pragma unroll
                             for (uint32_t e = 0; e < V; e++) acc[h][e] = 0.0f;
-                            if (col0 + h * 32 * V < dim) {
-#pragma unroll 4
-                                for (uint32_t k = 0; k < parts; k++) {
-                                    const Vec<float, V> x = load<float, V>(w.partial + size_t(slot_of(begin, k)) * w.partial_stride + col0 + h * 32 * V);
+                        constexpr uint32_t kAhead = 4;       // partial sums on their way
+                        for (uint32_t k0 = 0; k0 < parts; k0 += kAhead) {
+                            Vec<float, V> x[kAhead][kWords];
 #pragma unroll
-                                    for (uint32_t e = 0; e < V; e++) acc[h][e] += x.v[e];
-                                }
-                            }
+                            for (uint32_t k = 0; k < kAhead; k++)
+#pragma unroll
+                                for (uint32_t h = 0; h < kWords; h++)
+                                    if (k0 + k < parts && col0 + h * 32 * V < dim)
+                                        x[k][h] = load<float, V>(w.partial + size_t(slot_of(begin, k0 + k)) * w.partial_stride + col0 + h * 32 * V);
+#pragma unroll
+                            for (uint32_t k = 0; k < kAhead; k++)
+#pragma unroll
+                                for (uint32_t h = 0; h < kWords; h++)
+#pragma unroll
+                                    for (uint32_t e = 0; e < V; e++) acc[h][e] += k0 + k < parts && col0 + h * 32 * V < dim ? x[k][h].v[e] : 0.0f;
                         }
                     }
                 }
