@@ -526,7 +526,7 @@ def rd_vocab_loss_grad(hidden, weight, labels, lse, grad_loss, grad_hidden=None,
 
 
 def rd_vocab_status() -> int:
-    """Waits for the current device and returns (and clears) the status word of the loss kernels: 0 or RD_ERR_TIMEOUT."""
+    """Waits for the current device and returns (and clears) the vocabulary kernels' status word: 0 or RD_ERR_TIMEOUT."""
     st = C.c_int(0)
     _check(lib().rd_vocab_status(C.byref(st)), "rd_vocab_status")
     return st.value

@@ -6,16 +6,22 @@
 //
 // Tokens with a negative label count for nothing: a first kernel packs the hidden rows of the others one after another, in
 // order, so that ignored rows cost no products and nothing they hold (infinities, NaN) can reach a sum.  Everything after it
-// works on the packed rows; how many there are is known on the device only.
+// works on the packed rows; how many there are is known on the device only.  Up to 128 tokens are one tile anyway and are taken as
+// they lie ("direct"): what ignored rows give is never used, and for dw they are copied, with zeros in their place, beside the
+// first product.
 //
-// Loss.  One matrix product of n x rows x dim whose epilogue keeps, per token and vocabulary tile, the running maximum and
-// the sum of exponentials instead of the logits, and picks out the label's logit; a small kernel joins the tiles.
+// Loss.  One matrix product of n x rows x dim whose epilogue keeps, per token and 128 entries of the vocabulary, the maximum and the
+// sum of exponentials instead of the logits, and picks out the label's logit; a small kernel joins them.
 // Gradient.  In pieces of the vocabulary: the product once more, its epilogue turns logits into dx (16 bits, one rounding:
 // the operand type of the products that follow; fp16 dx is scaled by a power of two so that the largest factor g comes near
 // the top of the type's range), then both products of the piece in one launch, dw complete, dh added up in fp32 over the pieces.
 //
-// All three products run on one kernel: tiles of 128 x 256 accumulators in tensor memory (two of them, so that one is read
-// while the next is computed), operands brought in by TMA into a ring of shared-memory stages, one thread issuing tcgen05.mma.
+// All three products run on one kernel (tcgen05): a thread block, or a pair of them, computes tiles of 128 x 256 (256 x 256) with
+// the accumulators in tensor memory, two sets, so that one is read while the next is computed; operands come in by TMA into a ring
+// of stages of 64 summed indices; one warp per operand issues the copies, one the products, eight take the results.
+// What bounds it (B200): many tokens, the tensor cores (2048 tokens x 18944 x 4096: 265400 cycles a block, 262144 of them products)
+// at the clock that the board's power limit leaves, 1.25 to 1.4 GHz: 8192 tokens x 131072 x 4096 loss 6.1 ms = 1.43 PFLOP/s,
+// gradient 19.6 to 20.2 ms = 1.31 to 1.35.  Few tokens, the memory: 128 tokens x 131072 x 4096 gradient 0.66 ms for 3.2 GB.
 #include "rd_vocab.h"
 
 #include <cuda.h>
@@ -297,6 +303,7 @@ struct JoinParams {
     Rows rows;
     const Meta *meta;
     uint32_t n;               // direct rows
+    uint32_t row0, rows_most; // the band, as below
     uint32_t parts;
     float z;
     float *loss, *lse, *target;
@@ -355,6 +362,7 @@ struct alignas(64) MmaParams {
     uint16_t *dw;             // grad_weight, for rows that TMA cannot address
     uint16_t *gh;             // grad_hidden, where one part of dh is all of it
     size_t dh_stride, dw_stride, gh_stride;
+    uint32_t row0, rows_most; // stats: first row of the band of rows that the launch covers, and its room
     uint32_t parts;           // stats: parts per row, two to a tile of 256 columns, one to a smaller one
     uint32_t piece0, piece;   // first row of the piece and its rows
     uint32_t dim;
@@ -382,18 +390,9 @@ template <int CG> __device__ __forceinline__ void bar_arrive_leader(uint32_t bar
     if (CG == 1) asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
     else asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(leader_bar<CG>(bar)) : "memory");
 }
-__device__ __noinline__ bool bar_wait_slow(uint32_t bar, uint32_t parity)
-{
-    const long long t0 = clock64();
-    do {
-        if (bar_try(bar, parity)) return true;
-    } while (clock64() - t0 < kWaitCycles);
-    atomicExch(&g_vocab_status, 1);
-    return false;
-}
-// The same by a whole warp, whose lanes go on together.  The copies and products are issued by one lane, but the loops around them
-// are the warp's: what is the same in every lane then stays in uniform registers, which is where the instructions want their
-// operands.  (Loops of a single lane spent some 500 cycles a step on moving them there, as long as the products of the step.)
+// Waits by a whole warp, whose lanes go on together; false when the wait gave up.  The copies and products are issued by one
+// lane, but the loops around them are the warp's: what is the same in every lane then stays in uniform registers, which is where
+// the instructions want their operands.  (Loops of a single lane spent some 500 cycles a step on moving them there, as long as the products of the step.)
 __device__ __noinline__ bool warp_wait_slow(uint32_t bar, uint32_t parity)
 {
     const long long t0 = clock64();
@@ -417,9 +416,6 @@ __device__ __forceinline__ bool elect_one()
         : "=r"(one));
     return one;
 }
-
-// False when the wait gave up.
-__device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity) { return bar_try(bar, parity) || bar_wait_slow(bar, parity); }
 
 template <int CG> __device__ __forceinline__ void tma_load(uint32_t dst, const CUtensorMap *map, uint32_t x, uint32_t y, uint32_t bar)
 {
@@ -597,6 +593,7 @@ template <int KIND, int CG> struct Plan {
 
     __device__ __forceinline__ Plan(const MmaParams &params, uint32_t m) : p(params), c(blockIdx.x / CG), g(gridDim.x / CG)
     {
+        if (KIND == kStats) m = m > p.row0 ? min(m - p.row0, p.rows_most) : 0;
         tiles_m = (m + kTileM - 1) / kTileM;
         if (KIND != kGrads) {
             tiles_n = (p.piece + p.tile_n - 1) / p.tile_n;
@@ -649,7 +646,7 @@ template <int KIND, int CG> struct Plan {
                 }
                 at.set(over, g, min(p.group, tiles_m - band * p.group));
             }
-            w = Work{0, (band * p.group + at.x) * kTileM, at.y * p.tile_n, 0, k_dim, 0};
+            w = Work{0, (KIND == kStats ? p.row0 : 0) + (band * p.group + at.x) * kTileM, at.y * p.tile_n, 0, k_dim, 0};
             at.advance();
             return true;
         } else {
@@ -864,7 +861,7 @@ __global__ void __launch_bounds__(kMmaThreads, 1) rd_vocab_mma_kernel(const __gr
             const uint32_t row0 = w.m0 + rank * kRowsM + 32 * quarter, row = row0 + lane, col0 = w.n0 + 128 * half;
             const uint32_t buf = tile & 1;
             if (w.kblocks) {
-                if (!bar_wait(acc_full + 8 * buf, tile / 2 & 1)) break;
+                if (!warp_wait(acc_full + 8 * buf, tile / 2 & 1)) break;
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
             }
             const uint32_t acc = tmem + buf * kTileN + 128 * half + (uint32_t(32 * quarter) << 16);
@@ -950,7 +947,8 @@ __global__ void __launch_bounds__(kMmaThreads, 1) rd_vocab_mma_kernel(const __gr
                 for (int d = 4; d; d /= 2)
 #pragma unroll
                     for (int j = 0; j < d; j++) sum[j] += sum[j + d];
-                if (row < m && col0 < w.n0 + p.tile_n) p.part[size_t(row) * p.parts + (p.tile_n == kTileN ? col0 / 128 : w.n0 / p.tile_n)] = make_float2(top, sum[0]);
+                if (row < min(m, p.row0 + p.rows_most) && col0 < w.n0 + p.tile_n)
+                    p.part[size_t(row - p.row0) * p.parts + (p.tile_n == kTileN ? col0 / 128 : w.n0 / p.tile_n)] = make_float2(top, sum[0]);
             } else {
                 auto take = [&](int c, uint32_t (&v)[32]) {
                     const uint32_t col = col0 + 32 * c;
@@ -1073,12 +1071,12 @@ __global__ void __launch_bounds__(kMmaThreads, 1) rd_vocab_mma_kernel(const __gr
 __global__ void __launch_bounds__(256) rd_vocab_join_kernel(JoinParams p)
 {
     pdl_start();
-    const uint32_t row = blockIdx.x * 8 + (threadIdx.x >> 5);
+    const uint32_t in_band = blockIdx.x * 8 + (threadIdx.x >> 5), row = p.row0 + in_band;
     const int lane = threadIdx.x & 31;
-    if (row >= (p.rows.direct ? p.n : p.meta->m)) return;
+    if (in_band >= p.rows_most || row >= (p.rows.direct ? p.n : p.meta->m)) return;
     bool counts;
     const int label = p.rows.label_row(row, counts);
-    const float2 x = join_row(p.part + size_t(row) * p.parts, p.parts, lane);
+    const float2 x = join_row(p.part + size_t(in_band) * p.parts, p.parts, lane);
     write_row(x, counts, label >= 0 ? p.packed_target[row] : 0.0f, p.z, p.rows.token(row), lane, p.loss, p.lse, p.target);
 }
 
@@ -1307,6 +1305,8 @@ bool needs_align(const VocabArgs &a) { return reinterpret_cast<uintptr_t>(a.weig
 int pair_or_single(size_t n) { return n > kRowsM ? 2 : 1; }
 
 constexpr size_t kSms = 148;
+// Tokens whose softmax statistics are kept at a time, 16 bytes for 256 logits of each: 134 MB for 131072 logits however many tokens.
+constexpr size_t kBandRows = 16384;
 constexpr double kFinishSteps = 9;        // what the kernel that adds up dh costs, in steps of the summed index
 
 // Parts that the sum over a piece is cut into for dh.  More parts fill the groups of thread blocks more evenly, but each is a
@@ -1337,7 +1337,7 @@ struct Layout {
     float *gp, *gt, *lse2, *target, *dh;
     float2 *part;
     uint16_t *packed, *dx, *weight;
-    size_t rows_padded, packed_stride, dx_stride, piece, splits, dh_stride, bytes;
+    size_t rows_padded, packed_stride, dx_stride, piece, splits, dh_stride, band, bytes;
 };
 
 constexpr size_t kDxBytes = size_t(256) << 20;    // what the gradient keeps of dx at a time
@@ -1358,7 +1358,8 @@ Layout lay_out(const VocabArgs &a, bool gradient, bool want_hidden)
     if (!gradient) {
         l.target = w.take<float>(l.rows_padded);
         const size_t halves = 2 * ((a.rows + kTileN - 1) / kTileN);
-        l.part = w.take<float2>(l.rows_padded * (halves > kSms ? halves : kSms));    // smaller tiles: at most one per SM
+        l.band = l.rows_padded < kBandRows ? l.rows_padded : kBandRows;
+        l.part = w.take<float2>(l.band * (halves > kSms ? halves : kSms));           // smaller tiles: at most one per SM
     } else {
         l.gp = w.take<float>(l.rows_padded);
         l.gt = w.take<float>(l.rows_padded);
@@ -1649,10 +1650,18 @@ cudaError_t vocab_loss(const VocabArgs &a)
     q.target = l.target;
     q.piece0 = 0;
     q.piece = uint32_t(a.rows);
-    e = launch_mma<kStats>(q, a.bf16, cg, device, tiles_m * tiles_n, a.stream);
-    if (e != cudaSuccess) return e;
-    const JoinParams j{l.part, l.target, q.rows, l.meta, uint32_t(a.n), q.parts, a.z_loss, a.loss, a.lse_out, a.target};
-    return launch(rd_vocab_join_kernel, unsigned((a.n + 7) / 8), 256, a.stream, j);
+    for (size_t row0 = 0; row0 < a.n; row0 += l.band) {
+        const size_t rows = a.n - row0 < l.band ? a.n - row0 : l.band;
+        q.row0 = uint32_t(row0);
+        q.rows_most = uint32_t(rows);
+        e = launch_mma<kStats>(q, a.bf16, cg, device, (rows + tile_m - 1) / tile_m * tiles_n, a.stream);
+        if (e != cudaSuccess) return e;
+        const JoinParams j{l.part, l.target, q.rows, l.meta, uint32_t(a.n), q.row0, q.rows_most, q.parts, a.z_loss,
+                           a.loss, a.lse_out, a.target};
+        e = launch(rd_vocab_join_kernel, unsigned((rows + 7) / 8), 256, a.stream, j);
+        if (e != cudaSuccess) return e;
+    }
+    return e;
 }
 
 size_t vocab_loss_grad_workspace(const VocabArgs &a, bool want_hidden) { return lay_out(a, true, want_hidden).bytes; }

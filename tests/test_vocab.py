@@ -345,8 +345,9 @@ def test_loss_grad_sizes_of_the_upstream_gradient(dtype, size):
 
 @gpu
 def test_loss_grad_pieces():
-    """More tokens than one piece of the vocabulary has room for: several pieces, dh added up over them."""
+    """More tokens than one piece of the vocabulary, or one band of statistics, has room for."""
     hidden, weight, labels = vocab_case(40000, 9000, 64, torch.bfloat16, seed=80)
+    check_loss(hidden[:, :64], weight[:1500], labels % 1500)            # and several bands of tokens in the loss
     check_grad(hidden, weight, labels, torch.full((40000,), 1.0 / 30000, device="cuda"))
 
 
