@@ -1299,9 +1299,9 @@ struct Part {
 // TMA wants 16-byte aligned rows.
 bool needs_align(const VocabArgs &a) { return reinterpret_cast<uintptr_t>(a.weight) % 16 != 0 || a.weight_stride * 2 % 16 != 0; }
 
-// Whether pairs of thread blocks compute tiles of 256 x 256: as soon as there is more than one tile of 128 tokens (up to there half
-// of a pair's tile would be empty: gradient of 128 tokens x 131072 x 4096 705 us by single blocks, 866 by pairs; 8192 tokens
-// 22.2 ms by single blocks, 21.6 by pairs, B200).
+// Whether pairs of thread blocks compute tiles of 256 x 256: as soon as there is more than one tile of 128 tokens.  Up to there half
+// of a pair's tile would be empty (both measured when pairs were brought in, with the loops of that time: gradient of 128 tokens x
+// 131072 x 4096 705 us by single blocks, 866 by pairs; of 8192 tokens 22.2 ms by single blocks, 21.6 by pairs, B200).
 int pair_or_single(size_t n) { return n > kRowsM ? 2 : 1; }
 
 constexpr size_t kSms = 148;
