@@ -768,14 +768,32 @@ __device__ __forceinline__ void fill_span(char *p, size_t bytes, uint32_t t, uin
     for (size_t i = wide + 2 * t; i < bytes; i += 2 * threads) *reinterpret_cast<uint16_t *>(p + i) = 0;
 }
 
+// The same for 16 KB of a table whose rows follow each other without gaps, except rows with tokens.  Everything is made of units of
+// `unit` bytes (16 or 32), which lie within a row.
+__device__ __forceinline__ void fill_empty(char *table, size_t span, uint32_t row_bytes, const uint32_t *__restrict__ cnt, uint32_t unit)
+{
+    const size_t from = size_t(blockIdx.x) * kFillBytes, row0 = from / row_bytes;
+    const uint32_t in_row = uint32_t(from - row0 * row_bytes), bytes = uint32_t(span - from < kFillBytes ? span - from : kFillBytes);
+    for (uint32_t i = threadIdx.x * unit; i < bytes; i += kThreads * unit) {
+        if (__ldg(cnt + row0 + (in_row + i) / row_bytes)) continue;
+        if (unit == 32) asm volatile("st.global.v8.b32 [%0], {%1, %1, %1, %1, %1, %1, %1, %1};" ::"l"(table + from + i), "r"(0) : "memory");
+        else *reinterpret_cast<uint4 *>(table + from + i) = make_uint4(0, 0, 0, 0);
+    }
+}
+
 // span > 0: the table is one piece of memory of that many bytes.  Otherwise rows of row_bytes, pitch apart, a warp each.
+// cnt: tokens of every row; rows that have some are left alone.  Null: all rows.
 // Only the last thread block waits for the kernels before: what comes after this kernel then comes after them too.  That the
 // stream's earlier work is done is known from the first of them, which waits for it before it lets anything follow.
-__global__ void __launch_bounds__(kThreads) rd_embed_fill_kernel(char *__restrict__ table, size_t span, size_t rows, size_t row_bytes, size_t pitch, bool alone)
+__global__ void __launch_bounds__(kThreads) rd_embed_fill_kernel(char *__restrict__ table, size_t span, size_t rows, size_t row_bytes, size_t pitch,
+                                                                 const uint32_t *__restrict__ cnt, bool alone)
 {
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     if (alone || blockIdx.x == gridDim.x - 1) asm volatile("griddepcontrol.wait;" ::: "memory");
-    if (span) {
+    if (span && cnt) {
+        if (size_t(blockIdx.x) * kFillBytes < span)
+            fill_empty(table, span, uint32_t(row_bytes), cnt, (reinterpret_cast<uintptr_t>(table) | row_bytes) % 32 ? 16 : 32);
+    } else if (span) {
         const size_t from = size_t(blockIdx.x) * kFillBytes;
         // cut at addresses that are multiples of 32 bytes
         const size_t skew = reinterpret_cast<uintptr_t>(table) % 32;
@@ -783,39 +801,55 @@ __global__ void __launch_bounds__(kThreads) rd_embed_fill_kernel(char *__restric
         if (begin < span) fill_span(table + begin, (end < span ? end : span) - begin, threadIdx.x, kThreads);
     } else {
         const size_t row = size_t(blockIdx.x) * (kThreads / 32) + threadIdx.x / 32;
-        if (row < rows) fill_span(table + row * pitch, row_bytes, threadIdx.x % 32, 32);
+        if (row < rows && !(cnt && cnt[row])) fill_span(table + row * pitch, row_bytes, threadIdx.x % 32, 32);
     }
 }
 
-// A stream and two events of the library's own per device, made on the first call that wants them and kept.  Calls take turns to
+// A stream and four events of the library's own per device, made on the first call that wants them and kept.  Calls take turns to
 // enqueue, so the events always stand for the call that holds the lock.
 struct Lane {
     bool tried = false, ready = false;
+    unsigned long long user = 0;              // the stream of the last call
     cudaStream_t side = nullptr;
-    cudaEvent_t fork = nullptr, join = nullptr;
+    cudaEvent_t fork = nullptr, sorted = nullptr, filled = nullptr, join = nullptr;
 };
 constexpr int kMaxDevices = 64;
 Lane g_lane[kMaxDevices];
 std::mutex g_lane_mutex;
 
-// Null where the sort has to stay on the caller's stream: no such stream to be had, or the call is being recorded into a graph.
+// Null where everything has to stay on the caller's stream: no such stream to be had, the call is being recorded into a graph, or
+// another stream's call is still under way on it, which this one must not wait for.
 Lane *lane_for(cudaStream_t stream)
 {
     int device = 0;
     cudaStreamCaptureStatus capture = cudaStreamCaptureStatusNone;
+    unsigned long long user = 0;
     if (cudaGetDevice(&device) != cudaSuccess || device >= kMaxDevices) return nullptr;
     if (cudaStreamIsCapturing(stream, &capture) != cudaSuccess || capture != cudaStreamCaptureStatusNone) return nullptr;
+    if (cudaStreamGetId(stream, &user) != cudaSuccess) return nullptr;
+    // what follows is no part of a recording that another thread may be at
+    cudaStreamCaptureMode mode = cudaStreamCaptureModeRelaxed;
+    if (cudaThreadExchangeStreamCaptureMode(&mode) != cudaSuccess) return nullptr;
     Lane &l = g_lane[device];
     if (!l.tried) {
         l.tried = true;
         // of the highest priority: its few thread blocks go ahead of the many of the fill that are queued already
         int lowest = 0, highest = 0;
         l.ready = cudaDeviceGetStreamPriorityRange(&lowest, &highest) == cudaSuccess &&
-                  cudaStreamCreateWithPriority(&l.side, cudaStreamNonBlocking, highest) == cudaSuccess && cudaEventCreateWithFlags(&l.fork, cudaEventDisableTiming) == cudaSuccess &&
-                  cudaEventCreateWithFlags(&l.join, cudaEventDisableTiming) == cudaSuccess;
+                  cudaStreamCreateWithPriority(&l.side, cudaStreamNonBlocking, highest) == cudaSuccess;
+        for (cudaEvent_t *event : {&l.fork, &l.sorted, &l.filled, &l.join})
+            l.ready = l.ready && cudaEventCreateWithFlags(event, cudaEventDisableTiming) == cudaSuccess;
         if (!l.ready) (void)cudaGetLastError();
     }
-    return l.ready ? &l : nullptr;
+    bool free = l.ready;
+    if (free && l.user != user) {
+        const cudaError_t e = cudaEventQuery(l.join);
+        free = e == cudaSuccess;
+        if (!free) (void)cudaGetLastError();
+    }
+    (void)cudaThreadExchangeStreamCaptureMode(&mode);
+    if (free) l.user = user;
+    return free ? &l : nullptr;
 }
 
 // The work list of more than kSmallTokens tokens.
@@ -834,20 +868,24 @@ cudaError_t launch_sort(const EmbedGradArgs &a, const GradWork &w, uint32_t slab
     return e;
 }
 
-// `alone`: nothing of the call before it has waited for the stream's earlier work.
-template <typename O> cudaError_t launch_fill(const EmbedGradArgs &a, bool alone)
+// Rows row0 to row1; `alone`: nothing of the call before it has waited for the stream's earlier work.
+template <typename O> cudaError_t launch_fill(const EmbedGradArgs &a, size_t row0, size_t row1, const uint32_t *cnt, bool alone)
 {
-    const size_t row_bytes = a.dim * sizeof(O), pitch = a.table_stride * sizeof(O);
-    const size_t span = pitch == row_bytes || a.rows == 1 ? a.rows * row_bytes : 0;
-    const size_t blocks = span ? (span + 31) / kFillBytes + 1 : (a.rows + kThreads / 32 - 1) / (kThreads / 32);
+    const size_t row_bytes = a.dim * sizeof(O), pitch = a.table_stride * sizeof(O), rows = row1 - row0;
+    const size_t span = pitch == row_bytes || rows == 1 ? rows * row_bytes : 0;
+    const size_t blocks = span ? (span + 31) / kFillBytes + 1 : (rows + kThreads / 32 - 1) / (kThreads / 32);
     if (blocks > 0x7fffffffu) return cudaErrorInvalidConfiguration;
-    return launch(rd_embed_fill_kernel, unsigned(blocks), kThreads, a.stream, static_cast<char *>(a.table), span, a.rows, row_bytes, pitch, alone);
+    return launch(rd_embed_fill_kernel, unsigned(blocks), kThreads, a.stream, static_cast<char *>(a.table) + row0 * pitch, span, rows, row_bytes, pitch,
+                  cnt ? cnt + row0 : nullptr, alone);
 }
 
 // From this size of table on the fork pays: the sort takes some 20 us, a fork and a join a few.
 constexpr size_t kForkBytes = size_t(32) << 20;
+// Of a larger table this much is filled while the tokens are sorted, whatever rows have tokens.  The rest, without the rows that
+// have tokens, is filled beside the sums.
+constexpr size_t kFirstBytes = size_t(128) << 20;
 
-template <typename T, typename O> cudaError_t launch_stream(const EmbedGradArgs &a, const GradWork &w, uint32_t slabs)
+template <typename T, typename O> cudaError_t launch_stream(const EmbedGradArgs &a, const GradWork &w, uint32_t slabs, cudaStream_t on)
 {
     static std::atomic<bool> ready[kMaxDevices];
     int device = 0;
@@ -855,6 +893,8 @@ template <typename T, typename O> cudaError_t launch_stream(const EmbedGradArgs 
     if (e != cudaSuccess) return e;
     if (device >= kMaxDevices || !ready[device].load(std::memory_order_acquire)) {
         e = cudaFuncSetAttribute(rd_embed_stream_kernel<T, O>, cudaFuncAttributeMaxDynamicSharedMemorySize, kStreamSmem);
+        // the fill that runs beside this kernel leaves the shared memory to it: an SM divides its memory anew only when it is idle
+        if (e == cudaSuccess) e = cudaFuncSetAttribute(rd_embed_fill_kernel, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared);
         if (e != cudaSuccess) return e;
         if (device < kMaxDevices) ready[device].store(true, std::memory_order_release);
     }
@@ -864,7 +904,7 @@ template <typename T, typename O> cudaError_t launch_stream(const EmbedGradArgs 
     c.gridDim = dim3(unsigned(blocks < 148 ? blocks : 148));
     c.blockDim = dim3(kStreamThreads);
     c.dynamicSmemBytes = kStreamSmem;
-    c.stream = a.stream;
+    c.stream = on;
     c.attrs = &pdl;
     c.numAttrs = 1;
     return cudaLaunchKernelEx(&c, rd_embed_stream_kernel<T, O>, static_cast<const T *>(a.grad), a.grad_stride, static_cast<O *>(a.table), a.table_stride, uint32_t(a.dim), slabs,
@@ -878,11 +918,11 @@ template <typename T, typename O, int V, bool ELEMENTS> cudaError_t launch_grad(
     const bool stream = !ELEMENTS && a.dim * sizeof(T) >= kStreamBytes;
     const uint32_t vecs = uint32_t((a.dim + V - 1) / V), lanes = lanes_for(vecs);
     const uint32_t slabs = stream ? uint32_t((a.dim * sizeof(T) + kSlab - 1) / kSlab) : (vecs + lanes - 1) / lanes;
-    if (n == 0) return a.accumulate ? cudaSuccess : launch_fill<O>(a, true);
+    if (n == 0) return a.accumulate ? cudaSuccess : launch_fill<O>(a, 0, a.rows, nullptr, true);
     cudaError_t e = cudaSuccess;
     if (n <= kSmallTokens) {
         e = launch(rd_embed_rank_kernel, (n + 31) / 32, 1024, a.stream, a.ids, a.wide_ids, a.first_row, a.rows, n, w, slabs);
-        if (e == cudaSuccess && !a.accumulate) e = launch_fill<O>(a, false);
+        if (e == cudaSuccess && !a.accumulate) e = launch_fill<O>(a, 0, a.rows, nullptr, false);
     } else {
         std::unique_lock<std::mutex> hold(g_lane_mutex, std::defer_lock);
         Lane *lane = nullptr;
@@ -891,21 +931,32 @@ template <typename T, typename O, int V, bool ELEMENTS> cudaError_t launch_grad(
             lane = lane_for(a.stream);
         }
         if (lane) {
-            e = cudaEventRecord(lane->fork, a.stream);
-            if (e == cudaSuccess) e = cudaStreamWaitEvent(lane->side, lane->fork, 0);
-            if (e != cudaSuccess) return e;
+            const size_t pitch = a.table_stride * sizeof(O), first = !stream ? a.rows : kFirstBytes > pitch ? kFirstBytes / pitch : 1;
+            const bool split = first < a.rows;
+            cudaError_t f = cudaEventRecord(lane->fork, a.stream);
+            if (f == cudaSuccess) f = cudaStreamWaitEvent(lane->side, lane->fork, 0);
+            if (f != cudaSuccess) return f;
             e = launch_sort(a, w, slabs, lane->side);
-            const cudaError_t f = launch_fill<O>(a, true);
+            if (e == cudaSuccess && split) e = cudaEventRecord(lane->sorted, lane->side);
+            f = launch_fill<O>(a, 0, split ? first : a.rows, nullptr, true);
+            if (e == cudaSuccess && f == cudaSuccess && split) {
+                f = cudaEventRecord(lane->filled, a.stream);
+                if (f == cudaSuccess) f = cudaStreamWaitEvent(lane->side, lane->filled, 0);
+                if (f == cudaSuccess) e = launch_stream<T, O>(a, w, slabs, lane->side);
+                if (f == cudaSuccess) f = cudaStreamWaitEvent(a.stream, lane->sorted, 0);
+                if (f == cudaSuccess) f = launch_fill<O>(a, first, a.rows, w.cnt, false);
+            }
             // joined whatever became of the launches: the caller's stream owns the workspace
             const cudaError_t r = cudaEventRecord(lane->join, lane->side), j = r == cudaSuccess ? cudaStreamWaitEvent(a.stream, lane->join, 0) : r;
             e = e != cudaSuccess ? e : f != cudaSuccess ? f : j;
+            if (e != cudaSuccess || split) return e;
         } else {
             e = launch_sort(a, w, slabs, a.stream);
-            if (e == cudaSuccess && !a.accumulate) e = launch_fill<O>(a, false);
+            if (e == cudaSuccess && !a.accumulate) e = launch_fill<O>(a, 0, a.rows, nullptr, false);
         }
     }
     if (e != cudaSuccess) return e;
-    if (stream) return launch_stream<T, O>(a, w, slabs);
+    if (stream) return launch_stream<T, O>(a, w, slabs, a.stream);
     const uint64_t units = uint64_t(max_big(n) + max_items(n, a.rows)) * slabs, blocks = (units + kThreads / lanes - 1) / (kThreads / lanes);
     return launch(rd_embed_sum_kernel<T, O, V, ELEMENTS>, unsigned(blocks < kSumBlocks ? blocks : kSumBlocks), kThreads, a.stream, static_cast<const T *>(a.grad), a.grad_stride,
                   static_cast<O *>(a.table), a.table_stride, uint32_t(a.dim), lanes, slabs, a.scale, a.accumulate, w);
