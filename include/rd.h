@@ -467,7 +467,7 @@ RD_API void rd_destroy(rd_schedule_t *s);
  *   - Matrices are row-major with a row stride in elements (>= dim; grad_out and hidden also 0: every row is the
  *     same one); rows need only be aligned to the element.  Rows that begin and end on 16-byte boundaries are faster: see each function.
  *   - Every call is asynchronous on cuda_stream, allocates no memory, and may be recorded into a CUDA graph.  The library
- *     keeps nothing of a call (rd_embed_grad makes one stream and two events per device for itself).  A workspace belongs to the call until the stream has passed it; its contents need not be
+ *     keeps nothing of a call (rd_embed_grad makes one stream and four events per device for itself).  A workspace belongs to the call until the stream has passed it; its contents need not be
  *     kept or cleared between calls.  It is aligned to 256 bytes; too small a one is RD_ERR_TOO_SMALL.
  *   - Results depend on the arguments alone: no sum depends on timing.
  *   - RD_ERR_INVALID_ARG: null pointers, misaligned pointers, a stride below dim, a dim outside 1..65536, no rows, a negative
@@ -489,8 +489,9 @@ RD_API int rd_embed(const void *d_table, size_t table_stride, size_t rows, size_
 /*
  * rd_embed_grad -- the gradient of rd_embed with respect to the table:
  *   grad_table[v] = (accumulate ? grad_table[v] : 0) + scale * sum over the i with ids[i] - first_row = v of grad_out[i].
- * More than 4096 tokens and a table of 32 MiB or more without accumulate: the tokens are sorted on a stream of the library's
- * own, forked from cuda_stream and joined to it, while the table's empty rows are filled; not while a graph is recorded.
+ * More than 4096 tokens and a table of 32 MiB or more without accumulate: sort and sums run on a stream of the library's own,
+ * forked from cuda_stream and joined to it, beside the filling of empty rows; not while a graph is recorded, nor while another
+ * stream's call is under way there (the results are the same).
  * Tokens are sorted by row; sums are fp32, in ascending order of i (in runs of 32 tokens, whose sums are added in
  * ascending order), rounded once.  Every row of the table is written; with accumulate only those that have tokens.
  *   dtype        RD_FP32, RD_BF16 or RD_FP16: grad_out.

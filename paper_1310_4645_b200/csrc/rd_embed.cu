@@ -17,7 +17,8 @@
 //          sort    ... and in ascending order here: each token looks up how many of its row's tokens come before it; rows with
 //                  more than kChunk tokens go through a bitmap of token positions in shared memory instead.
 //   fill   zeros in the whole table.  It needs nothing of the above, so it runs beside it: beside rank, because it does not wait
-//          for it; beside the others, because those go to a stream of the library's own, forked off and joined by events.
+//          for it; beside the others, because those go to a stream of the library's own, forked off and joined by events.  Of a large
+//          table only a first part: the rest beside the sums, where the rows with tokens are known and left out.
 //   sum    a group of threads per item and slab of columns adds up the gradients; a row with several items has them added in
 //          ascending order by whichever group finishes last.
 #include "rd_vocab.h"
@@ -583,8 +584,8 @@ __global__ void __launch_bounds__(kThreads, 3) rd_embed_sum_kernel(const T *__re
 }
 
 // The same for rows of whole 16-byte words from kStreamBytes on: the gradients' rows come through shared memory by bulk copies, so
-// that a warp has up to 12 KB on its way whatever the items look like (through registers a warp had the 1 to 4 KB of one item: the
-// whole gradient of 16384 tokens x 4096 bf16 into 131072 rows 216 us, this 201; of 65536 tokens into a slice of 32768 x 2048 92, 77.
+// that a warp has up to 12 KB on its way whatever the items look like (through registers a warp had the 1 to 4 KB of one item; when
+// the whole table was filled before: the gradient of 16384 tokens x 4096 bf16 into 131072 rows 216 us, this 201; of 65536 tokens into a slice of 32768 x 2048 92, 77.
 // 8 warps with 24 KB each: 207, 81; 24 with 8 KB: 201, 81; 32 with 6 KB: 208, 95).
 //   A warp takes 32 items at a time, one per lane, and sees their tokens as one sequence.  Lanes look up 32 tokens of it at a
 //   time; groups of 4 are copied to a ring of 3 groups, two groups ahead of the one that is added up.
@@ -882,8 +883,10 @@ template <typename O> cudaError_t launch_fill(const EmbedGradArgs &a, size_t row
 // From this size of table on the fork pays: the sort takes some 20 us, a fork and a join a few.
 constexpr size_t kForkBytes = size_t(32) << 20;
 // Of a larger table this much is filled while the tokens are sorted, whatever rows have tokens.  The rest, without the rows that
-// have tokens, is filled beside the sums.
-constexpr size_t kFirstBytes = size_t(128) << 20;
+// have tokens, is filled beside the sums, on the SMs that are done with them (both kernels on an SM at once, which takes 96 instead of
+// 118 registers here, was slower: a slice of 32768 x 2048 fp32 75 us, this 68).  First part of 64, 128, 192 MB: 69.2, 67.8, 68.0 us
+// there, 186.6, 186.8, 185.2 for 131072 x 4096 bf16; everything filled first: 76.7 and 201.6.
+constexpr size_t kFirstBytes = size_t(192) << 20;
 
 template <typename T, typename O> cudaError_t launch_stream(const EmbedGradArgs &a, const GradWork &w, uint32_t slabs, cudaStream_t on)
 {
@@ -894,6 +897,7 @@ template <typename T, typename O> cudaError_t launch_stream(const EmbedGradArgs 
     if (device >= kMaxDevices || !ready[device].load(std::memory_order_acquire)) {
         e = cudaFuncSetAttribute(rd_embed_stream_kernel<T, O>, cudaFuncAttributeMaxDynamicSharedMemorySize, kStreamSmem);
         // the fill that runs beside this kernel leaves the shared memory to it: an SM divides its memory anew only when it is idle
+        // (slice of 32768 x 2048 fp32: 72 us without this, 68 with it)
         if (e == cudaSuccess) e = cudaFuncSetAttribute(rd_embed_fill_kernel, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared);
         if (e != cudaSuccess) return e;
         if (device < kMaxDevices) ready[device].store(true, std::memory_order_release);

@@ -124,6 +124,38 @@ def test_embed_grad(dtype, out, n, rows, dim, pad, ids, accumulate):
 
 
 @gpu
+@pytest.mark.parametrize("dtype, out, n, rows, dim, pad", [(torch.bfloat16, torch.bfloat16, 9001, 401003, 264, 0), (torch.bfloat16, torch.float32, 30000, 110007, 512, 0),
+                                                           (torch.float32, torch.float32, 5001, 100001, 516, 8), (torch.float16, torch.float16, 70000, 20011, 8192, 0),
+                                                           (torch.bfloat16, torch.bfloat16, 6000, 300001, 40, 600)])
+def test_embed_grad_large_tables(dtype, out, n, rows, dim, pad):
+    """Tables that are filled in two parts, the second beside the sums: on two streams at once, and recorded into a graph as well."""
+    grad, tokens = rand(n, dim, seed=30, dtype=dtype), (torch.exp(torch.rand(n, generator=gen(31), device="cuda") * math.log(rows + 1)).long() - 1).flip(0)
+    tokens = torch.where(tokens % 2 == 0, tokens, rows - 1 - tokens)      # frequent rows in both parts
+    fresh = lambda: strided(torch.full((rows, dim), 7.0, dtype=out, device="cuda"), pad)
+    want, bound, touched = grad_reference(grad, tokens, rows, 0, 1.25)
+    table = rd.rd_embed_grad(grad, tokens, fresh(), scale=1.25)
+    within(table, want, bound + U[out] * want.abs() + TINY[out])
+    assert not table[~touched].any()
+    del want, bound
+    streams, tables = [torch.cuda.Stream() for _ in range(2)], [fresh() for _ in range(2)]
+    torch.cuda.synchronize()
+    for _ in range(3):
+        for s, t in zip(streams, tables):
+            with torch.cuda.stream(s):
+                t.fill_(7.0)
+                rd.rd_embed_grad(grad, tokens, t, scale=1.25)
+    torch.cuda.synchronize()
+    assert all(torch.equal(t, table) for t in tables)
+    graph, ws = torch.cuda.CUDAGraph(), torch.empty(rd.rd_embed_grad_workspace(rows, dim, n), dtype=torch.uint8, device="cuda")
+    with torch.cuda.graph(graph):
+        rd.rd_embed_grad(grad, tokens, tables[0], scale=1.25, workspace=ws)
+    tables[0].fill_(7.0)
+    graph.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(tables[0], table) and rd.rd_vocab_status() == rd.RD_OK
+
+
+@gpu
 def test_embed_grad_is_the_derivative():
     """The lookup is linear, so a difference quotient of <grad, lookup(table)> is the gradient's entry up to rounding."""
     table, ids, grad = rand(11, 6, seed=10), ints(0, 11, 40, seed=11), rand(40, 6, seed=12)
