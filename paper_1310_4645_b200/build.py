@@ -17,7 +17,7 @@ LIB = os.path.join(HERE, "librd.so")
 TORCH_LIB = os.path.join(HERE, "_rd_torch.so")
 SOURCES = ["rd_api.cpp", "rd_sched.cpp", "rd_compile.cpp", "rd_kernels.cu", "rd_faithful.cu", "rd_broadcast.cu",
            "rd_vocab_api.cpp", "rd_embed.cu", "rd_vocab.cu"]
-HEADERS = ["rd_internal.h", "rd_kernels.h", "rd_vocab.h", "rd_launch.h", "rd_ptx.h"]
+HEADERS = ["rd_internal.h", "rd_kernels.h", "rd_vocab.h", "rd_launch.h", "rd_ptx.h", "rd_ring.h"]
 # rd_kernels.cu is compiled once per element type (-DRD_DT=k: that type's kernels; the 16-bit types count
 # twice, once for sum and product and once for max and min) and once without (launch shapes and dispatch),
 # side by side

@@ -33,6 +33,7 @@
 #include "rd.h"
 #include "rd_launch.h"
 #include "rd_ptx.h"
+#include "rd_ring.h"
 
 namespace rd {
 
@@ -258,9 +259,6 @@ __global__ void __launch_bounds__(kPackThreads) rd_vocab_align_kernel(uint16_t *
 
 // ------------------------------------------------------------------------------------------------ the products
 
-constexpr int kTileN = 256;
-constexpr int kTileK = 64;                // 128 bytes: one swizzle span
-constexpr int kEpilogueWarps = 8;
 constexpr int kMmaThreads = 128 + 32 * kEpilogueWarps;
 
 // Where a row of the products comes from: packed rows have their tokens and labels in lists, direct ones are the tokens themselves.
@@ -341,8 +339,6 @@ __device__ __forceinline__ void write_row(float2 x, bool counts, float target, f
     if (lse_out) lse_out[i] = lse;
     if (target_out) target_out[i] = target;
 }
-
-enum { kStats = 0, kDlogits = 1, kGrads = 2 };
 
 struct alignas(64) MmaParams {
     CUtensorMap a_k;          // rows of the left operand, 64 x a_rows boxes: packed hidden (stats, dlogits), dx (dh)
@@ -514,19 +510,6 @@ __device__ __forceinline__ void box_put(uint32_t box, int row, int unit, uint32_
 {
     asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(box + row * 128 + ((unit ^ (row & 7)) * 16)), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
 }
-
-// CG thread blocks (one, or a pair) compute a tile of 128 * CG x 256 together: each has 128 rows of the left operand and of the
-// accumulators, and 256 / CG rows of the right operand.
-constexpr int kRowsM = 128;
-// Results leave through one box of 4 KB per epilogue warp, except the softmax statistics, which have the room for another stage.
-constexpr uint32_t kBox = 4096;
-constexpr uint32_t kMostStages = 16;      // logits with small tiles have more stages in the same room
-template <int KIND, int CG> struct Shape {
-    static constexpr int tile_m = kRowsM * CG, rows_n = kTileN / CG;
-    static constexpr uint32_t stage_a = kRowsM * kTileK * 2, stage_b = rows_n * kTileK * 2, stage = stage_a + stage_b;
-    static constexpr int stages = CG == 1 ? 4 : KIND == kStats ? 7 : 6;
-    static constexpr uint32_t boxes = KIND == kStats ? 0 : kEpilogueWarps * kBox, ring = stages * stage, smem = ring + boxes + 1024 + 512;
-};
 
 constexpr uint32_t kTileOverhead = 2;     // what a tile costs besides its products, in steps of the summed index
 
@@ -1548,12 +1531,11 @@ uint32_t tile_columns(size_t tiles_m, size_t rows, int cg)
     return uint32_t(n);
 }
 
-// The ring of a logits kernel: as many stages as its room holds.
 template <int KIND> void set_ring(MmaParams &q, int cg)
 {
-    q.stage = (q.a_rows + q.tile_n / uint32_t(cg)) * kTileK * 2;
-    const uint32_t room = cg == 2 ? Shape<KIND, 2>::ring : Shape<KIND, 1>::ring;
-    q.stages = room / q.stage < kMostStages ? room / q.stage : kMostStages;
+    const Ring r = ring_of(cg == 2 ? Shape<KIND, 2>::ring : Shape<KIND, 1>::ring, q.a_rows, q.tile_n / uint32_t(cg));
+    q.stage = r.stage;
+    q.stages = r.stages;
 }
 
 void common(MmaParams &q, const VocabArgs &a, const Layout &l, int cg)
