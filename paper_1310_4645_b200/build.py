@@ -1,4 +1,7 @@
-"""Builds librd.so (CUDA kernels + C ABI) in-tree with nvcc for sm_100a, and _rd_torch.so (tensor marshalling) beside it."""
+"""Builds librd.so (CUDA kernels + C ABI) in-tree with nvcc for sm_100a, and _rd_torch.so (tensor marshalling) beside it.
+
+librd.so needs no torch; where there is none, or one without CUDA, it is all that is built.
+"""
 from __future__ import annotations
 
 import importlib.util
@@ -36,17 +39,28 @@ def _nvcc() -> str:
     return "nvcc"
 
 
+def _torch_dir() -> str | None:
+    """The installed torch's folder (found, not imported); None where there is none, or one without CUDA."""
+    spec = importlib.util.find_spec("torch")
+    for place in (spec and spec.submodule_search_locations) or ():
+        if os.path.exists(os.path.join(place, "lib", "libc10_cuda.so")):
+            return place
+    return None
+
+
 def stale() -> bool:
-    if not os.path.exists(LIB) or not os.path.exists(TORCH_LIB):
+    libraries, sources = [LIB], SOURCES + HEADERS
+    if _torch_dir():
+        libraries, sources = libraries + [TORCH_LIB], sources + ["rd_torch.cpp"]
+    if not all(map(os.path.exists, libraries)):
         return True
-    built = min(os.path.getmtime(LIB), os.path.getmtime(TORCH_LIB))
-    deps = [os.path.join(CSRC, f) for f in SOURCES + HEADERS + ["rd_torch.cpp"]] + [os.path.join(ROOT, "include", "rd.h")]
+    built = min(map(os.path.getmtime, libraries))
+    deps = [os.path.join(CSRC, f) for f in sources] + [os.path.join(ROOT, "include", "rd.h")]
     return any(os.path.getmtime(d) > built for d in deps)
 
 
-def _torch_module(work: str) -> str:
-    """Compiles the marshalling module against the installed torch (found, not imported); it is linked to librd.so beside it."""
-    torch_dir = list(importlib.util.find_spec("torch").submodule_search_locations)[0]
+def _torch_module(work: str, torch_dir: str) -> str:
+    """Compiles the marshalling module against the installed torch; it is linked to librd.so beside it."""
     cuda = os.path.dirname(os.path.dirname(_nvcc())) if os.path.isabs(_nvcc()) else "/usr/local/cuda"
     obj = os.path.join(work, "rd_torch.o")
     subprocess.check_call(["g++", "-O2", "-std=c++17", "-fPIC", "-fvisibility=hidden", "-Wall", "-Wextra", "-c", "-o", obj,
@@ -56,8 +70,7 @@ def _torch_module(work: str) -> str:
     return obj
 
 
-def _link_torch_module(obj: str) -> None:
-    torch_dir = list(importlib.util.find_spec("torch").submodule_search_locations)[0]
+def _link_torch_module(obj: str, torch_dir: str) -> None:
     tmp = TORCH_LIB + ".%d.tmp" % os.getpid()
     subprocess.check_call(["g++", "-shared", "-o", tmp, obj, "-L", os.path.join(torch_dir, "lib"), "-ltorch_python", "-ltorch_cuda", "-ltorch_cpu",
                            "-lc10_cuda", "-lc10", "-L", HERE, "-l:" + os.path.basename(LIB), "-Wl,-rpath,$ORIGIN"])
@@ -90,13 +103,14 @@ def build(force: bool = False, verbose: bool = False) -> str:
             return obj
 
         with ThreadPoolExecutor(max_workers=min(len(units) + 1, os.cpu_count() or 4)) as pool:
-            marshalling = pool.submit(_torch_module, work)
+            torch_dir = _torch_dir()
+            marshalling = pool.submit(_torch_module, work, torch_dir) if torch_dir else None
             objs = list(pool.map(compile_one, units))
-            marshalling = marshalling.result()
         tmp = LIB + ".%d.tmp" % os.getpid()
         subprocess.check_call([nvcc, *LINK_FLAGS, "-o", tmp] + objs)
         os.replace(tmp, LIB)
-        _link_torch_module(marshalling)
+        if marshalling:
+            _link_torch_module(marshalling.result(), torch_dir)
     finally:
         shutil.rmtree(work, ignore_errors=True)
     return LIB
