@@ -6,6 +6,7 @@ from __future__ import annotations
 
 import importlib.util
 import os
+import re
 import shutil
 import subprocess
 import sys
@@ -48,9 +49,32 @@ def _torch_dir() -> str | None:
     return None
 
 
+def _torch_built_for(torch_dir: str) -> str:
+    """What the tensor module depends on besides its sources: it uses torch's and the interpreter's C++ and C interfaces."""
+    with open(os.path.join(torch_dir, "version.py")) as f:
+        version = re.search(r"^__version__\s*=\s*['\"](.+?)['\"]", f.read(), re.M)
+    return "torch %s, %s\n" % (version.group(1) if version else "", sys.implementation.cache_tag)
+
+
+def _torch_stamp() -> str:
+    """The file that says what the tensor module was built for."""
+    return os.path.join(os.path.dirname(TORCH_LIB), "_build", "rd_torch.txt")
+
+
+def _stamped() -> str:
+    try:
+        with open(_torch_stamp()) as f:
+            return f.read()
+    except FileNotFoundError:
+        return ""
+
+
 def stale() -> bool:
     libraries, sources = [LIB], SOURCES + HEADERS
-    if _torch_dir():
+    torch_dir = _torch_dir()
+    if torch_dir:
+        if _stamped() != _torch_built_for(torch_dir):
+            return True
         libraries, sources = libraries + [TORCH_LIB], sources + ["rd_torch.cpp"]
     if not all(map(os.path.exists, libraries)):
         return True
@@ -75,6 +99,9 @@ def _link_torch_module(obj: str, torch_dir: str) -> None:
     subprocess.check_call(["g++", "-shared", "-o", tmp, obj, "-L", os.path.join(torch_dir, "lib"), "-ltorch_python", "-ltorch_cuda", "-ltorch_cpu",
                            "-lc10_cuda", "-lc10", "-L", HERE, "-l:" + os.path.basename(LIB), "-Wl,-rpath,$ORIGIN"])
     os.replace(tmp, TORCH_LIB)
+    os.makedirs(os.path.dirname(_torch_stamp()), exist_ok=True)
+    with open(_torch_stamp(), "w") as f:
+        f.write(_torch_built_for(torch_dir))
 
 
 def build(force: bool = False, verbose: bool = False) -> str:

@@ -56,3 +56,23 @@ def test_the_c_library_outlives_a_failure_of_the_tensor_module(compilers, monkey
     with pytest.raises(B.subprocess.CalledProcessError):
         B.build()
     assert os.path.exists(B.LIB) and not os.path.exists(B.TORCH_LIB) and B.stale()
+
+
+def test_another_torch_means_another_tensor_module(compilers, monkeypatch, tmp_path):
+    """A torch whose version differs from the one that _rd_torch.so was built against, whatever the files' times say."""
+    torch_dir = tmp_path / "torch"
+    (torch_dir / "lib").mkdir(parents=True)
+    (torch_dir / "lib" / "libc10_cuda.so").write_text("")
+    (torch_dir / "version.py").write_text("__version__ = '2.11.0+cu128'\n")
+    spec = importlib.util.spec_from_loader("torch", None)
+    spec.submodule_search_locations = [str(torch_dir)]
+    find = importlib.util.find_spec
+    monkeypatch.setattr(importlib.util, "find_spec", lambda name, *a: spec if name == "torch" else find(name, *a))
+    B.build()
+    assert not B.stale()
+    (torch_dir / "version.py").write_text("__version__ = '2.12.0+cu128'\n")
+    for f in (torch_dir / "version.py", torch_dir / "lib" / "libc10_cuda.so"):
+        os.utime(f, (1, 1))                                   # an installer keeps the files' own, older times
+    assert B.stale()
+    B.build()
+    assert not B.stale()
