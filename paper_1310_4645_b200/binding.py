@@ -482,9 +482,10 @@ def rd_embed_grad(grad_out, ids, grad_table, first_row=0, scale=1.0, accumulate=
 
 
 def _vocab_shape(hidden, weight, labels):
-    """The operands as far as the workspace depends on them."""
-    return rd_vocab_t(hidden.data_ptr(), max(hidden.stride(0), hidden.shape[1]), weight.data_ptr(), max(weight.stride(0), weight.shape[1]),
-                      labels.data_ptr(), hidden.shape[0], weight.shape[0], hidden.shape[1], 0, _dtype_code(hidden), _dtype_code(labels), 1.0, 0.0)
+    """The operands as far as the workspace depends on them.  A matrix of one row has no stride, as in the calls."""
+    stride = lambda t: t.stride(0) if t.shape[0] > 1 else t.shape[1]
+    return rd_vocab_t(hidden.data_ptr(), stride(hidden), weight.data_ptr(), stride(weight), labels.data_ptr(), hidden.shape[0], weight.shape[0], hidden.shape[1], 0,
+                      _dtype_code(hidden), _dtype_code(labels), 1.0, 0.0)
 
 
 def rd_vocab_loss_workspace(hidden, weight, labels) -> int:

@@ -53,3 +53,34 @@ def test_tokens_of_a_quarter_of_a_tile(dtype, n):
     hidden, weight, labels = vocab_case(n, 9000, 1032, dtype, seed=200)
     check_loss(hidden, weight, labels)
     check_grad(hidden, weight, labels, torch.rand(n, generator=gen(201), device="cuda"))
+
+
+def one_row(dim, stride, dtype=torch.bfloat16, device="cpu"):
+    """A weight of one row, cut from a matrix whose rows are `stride` apart."""
+    return torch.ones(3, stride, dtype=dtype, device=device)[:1, :dim]
+
+
+@pytest.mark.parametrize("dim, stride", [(1000, 1001), (1001, 1008), (64, 64)])
+def test_workspace_of_a_single_row(dim, stride):
+    """What lies between rows is nothing to a matrix of one."""
+    hidden, labels = torch.ones(3, dim, dtype=torch.bfloat16), torch.zeros(3, dtype=torch.int64)
+    cut, alone = one_row(dim, stride), torch.ones(1, dim, dtype=torch.bfloat16)
+    assert rd.rd_vocab_loss_workspace(hidden, cut, labels) == rd.rd_vocab_loss_workspace(hidden, alone, labels)
+    assert rd.rd_vocab_loss_grad_workspace(hidden, cut, labels) == rd.rd_vocab_loss_grad_workspace(hidden, alone, labels)
+
+
+@gpu
+@pytest.mark.parametrize("dim, stride", [(1000, 1001), (1001, 1008)])
+def test_workspace_of_a_single_row_suffices(dim, stride):
+    weight = one_row(dim, stride, device="cuda")
+    hidden, labels = torch.ones(3, dim, dtype=torch.bfloat16, device="cuda"), torch.zeros(3, dtype=torch.int64, device="cuda")
+    ws = torch.empty(rd.rd_vocab_loss_workspace(hidden, weight, labels), dtype=torch.uint8, device="cuda")
+    loss, lse, target = rd.rd_vocab_loss(hidden, weight, labels, workspace=ws)
+    assert (target == dim).all()
+    # the only logit times log2(e) and times ln(2) again: two constants and two products, each rounded to 2^-24
+    assert (lse - dim).abs().max() <= dim * 2.0 ** -22 and loss.abs().max() <= dim * 2.0 ** -22
+    ws = torch.empty(rd.rd_vocab_loss_grad_workspace(hidden, weight, labels), dtype=torch.uint8, device="cuda")
+    up = torch.ones(3, device="cuda")
+    gh, gw = rd.rd_vocab_loss_grad(hidden, weight, labels, lse, up, torch.empty_like(hidden), torch.empty_like(weight), workspace=ws)
+    # the only entry has all of the probability: what is left is lse's error and that of the exponent, which is formed the same way
+    assert gh.abs().max() <= dim * 2.0 ** -20 and gw.abs().max() <= 3 * dim * 2.0 ** -20
