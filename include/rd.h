@@ -472,6 +472,7 @@ RD_API void rd_destroy(rd_schedule_t *s);
  *   - Results depend on the arguments alone: no sum depends on timing.
  *   - RD_ERR_INVALID_ARG: null pointers, misaligned pointers, a stride below dim, a dim outside 1..65536, no rows, a negative
  *     first_row, factors that are not finite, an output that overlaps an input, another output or the workspace.
+ *     Columns side by side in rows of one stride do not overlap; matrices of different strides do when their address ranges meet.
  *     RD_ERR_UNSUPPORTED: an element type that the operator does not have, or 2^31 or more rows or tokens.
  *   - Thread safety: any calls from any threads.
  */

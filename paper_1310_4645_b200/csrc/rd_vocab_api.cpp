@@ -18,12 +18,29 @@ size_t size_of(int dtype) { return dtype == RD_INT64 || dtype == RD_FP64 ? 8 : d
 bool known(int dtype) { return dtype >= RD_INT32 && dtype <= RD_FP16; }
 bool aligned(const void *p, size_t to) { return p && reinterpret_cast<uintptr_t>(p) % to == 0; }
 
-// Memory that a call reads or writes; rows of `dim` elements, `stride` apart.
+// Memory that a call reads or writes: one run of bytes, or rows of `width` bytes that begin `stride` bytes apart.
 struct Span {
     uintptr_t begin, end;
-    Span(const void *p, size_t bytes) : begin(reinterpret_cast<uintptr_t>(p)), end(p ? begin + bytes : begin) {}
-    Span(const void *p, size_t rows, size_t stride, size_t dim, size_t esize) : Span(p, rows ? ((rows - 1) * stride + dim) * esize : 0) {}
-    bool meets(const Span &o) const { return begin < o.end && o.begin < end; }
+    size_t width, stride;     // stride 0: one run
+    Span(const void *p, size_t bytes) : begin(reinterpret_cast<uintptr_t>(p)), end(p ? begin + bytes : begin), width(end - begin), stride(0) {}
+    Span(const void *p, size_t rows, size_t row_stride, size_t dim, size_t esize) : Span(p, rows ? ((rows - 1) * row_stride + dim) * esize : 0)
+    {
+        if (p && rows > 1 && row_stride > dim) {
+            width = dim * esize;
+            stride = row_stride * esize;
+        }
+    }
+    // Spans that lie apart do not meet, nor do columns side by side in rows of the same buffer, which are rows of the same stride (or
+    // one run beside such rows).  Rows of different strides are taken to meet when their spans do.
+    bool meets(const Span &o) const
+    {
+        if (begin >= o.end || o.begin >= end) return false;
+        if (stride && o.stride && stride != o.stride) return true;
+        const size_t s = stride ? stride : o.stride;
+        if (!s) return true;
+        const size_t at = o.begin >= begin ? (o.begin - begin) % s : (s - (begin - o.begin) % s) % s;       // where o's rows begin in this one's
+        return at < width || at + o.width > s;
+    }
 };
 
 // A matrix's stride: at least a row (0 for an input whose rows are all the same one), and the whole matrix within the address space.

@@ -84,3 +84,41 @@ def test_workspace_of_a_single_row_suffices(dim, stride):
     gh, gw = rd.rd_vocab_loss_grad(hidden, weight, labels, lse, up, torch.empty_like(hidden), torch.empty_like(weight), workspace=ws)
     # the only entry has all of the probability: what is left is lse's error and that of the exponent, which is formed the same way
     assert gh.abs().max() <= dim * 2.0 ** -20 and gw.abs().max() <= 3 * dim * 2.0 ** -20
+
+
+def lookup_overlaps(table, tstride, out, ostride, rows=16, n=4, dim=8, ids=1 << 24):
+    """Whether rd_embed takes these addresses for overlapping memory.  They are no memory at all: without a device nothing is launched."""
+    return rd.lib().rd_embed(table, tstride, rows, dim, rd.RD_BF16, ids, rd.RD_INT64, n, 0, 1.0, out, ostride, None) == rd.RD_ERR_INVALID_ARG
+
+
+@pytest.mark.skipif(torch.cuda.is_available(), reason="calls with made-up addresses must find no device")
+def test_columns_beside_each_other_do_not_overlap():
+    P, row = 1 << 20, 48                                      # rows of 24 elements, in bytes
+    assert not lookup_overlaps(P, 24, P + 16, 24)             # columns 0 to 7 and 8 to 15
+    assert not lookup_overlaps(P + 32, 24, P, 24)             # 16 to 23 and 0 to 7
+    assert not lookup_overlaps(P + 32, 24, P + row, 24)       # the same, from the next row on
+    assert not lookup_overlaps(P, 24, P + 5 * row + 16, 24)
+    assert not lookup_overlaps(P, 24, P + 5 * row + 16, 24, n=1) and not lookup_overlaps(P, 24, P + 5 * row + 16, 8, n=1)      # one row, whatever its stride
+    assert lookup_overlaps(P, 24, P + 14, 24) and lookup_overlaps(P + 32, 24, P + 2, 24, dim=16)                              # columns that meet, in the next row too
+    assert lookup_overlaps(P, 24, P + 5 * row + 14, 24, n=1) and lookup_overlaps(P, 24, P + 5 * row + 34, 24, n=1)            # 34: beyond the row's end
+    assert lookup_overlaps(P, 24, P, 24) and lookup_overlaps(P, 24, P + 16, 32) and lookup_overlaps(P, 8, P + 16, 24)         # strides that differ
+    assert lookup_overlaps(P, 24, P + 16, 24, ids=P + 16)     # the ids lie in the output
+
+
+@gpu
+def test_columns_of_one_buffer():
+    """Operands and results side by side in one allocation."""
+    n, rows, dim = 37, 61, 24
+    buffer = torch.randn(rows, 5 * dim, device="cuda", generator=gen(210)).bfloat16()
+    table, out, grad, grad_table, rest = (buffer[:, k * dim:(k + 1) * dim] for k in range(5))
+    ids = torch.randint(0, rows, (n,), device="cuda", generator=gen(211))
+    before = rest.clone()
+    assert torch.equal(rd.rd_embed(table, ids, out[:n]), table.contiguous()[ids])
+    want = rd.rd_embed_grad(grad[:n].contiguous(), ids, torch.empty(rows, dim, dtype=torch.bfloat16, device="cuda"))
+    assert torch.equal(rd.rd_embed_grad(grad[:n], ids, grad_table), want)
+    hidden, weight = grad[:n], table
+    _, lse, _ = rd.rd_vocab_loss(hidden, weight, ids)
+    up = torch.ones(n, device="cuda")
+    fresh = rd.rd_vocab_loss_grad(hidden, weight, ids, lse, up, torch.empty(n, dim, dtype=torch.bfloat16, device="cuda"), torch.empty(rows, dim, dtype=torch.bfloat16, device="cuda"))
+    got = rd.rd_vocab_loss_grad(hidden, weight, ids, lse, up, out[:n], grad_table)
+    assert torch.equal(got[0], fresh[0]) and torch.equal(got[1], fresh[1]) and torch.equal(rest, before)
