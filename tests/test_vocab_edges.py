@@ -2,12 +2,14 @@
 import os
 import shutil
 import subprocess
+import threading
 
 import pytest
 import torch
 
 import paper_1310_4645_b200 as rd
-from test_vocab import HALF, check_grad, check_loss, gen, vocab_case
+import test_vocab
+from test_vocab import HALF, U, check_grad, check_loss, gen, test_embed_grad_large_tables as large_tables, vocab_case, within
 
 CSRC = os.path.join(os.path.dirname(os.path.abspath(rd.__file__)), "csrc")
 gpu = pytest.mark.gpu
@@ -122,3 +124,18 @@ def test_columns_of_one_buffer():
     fresh = rd.rd_vocab_loss_grad(hidden, weight, ids, lse, up, torch.empty(n, dim, dtype=torch.bfloat16, device="cuda"), torch.empty(rows, dim, dtype=torch.bfloat16, device="cuda"))
     got = rd.rd_vocab_loss_grad(hidden, weight, ids, lse, up, out[:n], grad_table)
     assert torch.equal(got[0], fresh[0]) and torch.equal(got[1], fresh[1]) and torch.equal(rest, before)
+
+
+@gpu
+@pytest.mark.parametrize("dtype, out, n, rows, dim, pad", [
+    # sort on the library's stream, the whole table filled meanwhile, sums on the caller's stream after both:
+    (torch.bfloat16, torch.bfloat16, 9001, 100003, 264, 0),       # 53 MB, rows through shared memory
+    (torch.bfloat16, torch.float32, 30000, 30011, 512, 8),        # 61 MB and gaps between the rows
+    (torch.bfloat16, torch.bfloat16, 6000, 450001, 40, 0),        # 36 MB, rows below 512 bytes
+    (torch.float16, torch.float16, 6000, 60013, 333, 3),          # 40 MB, element by element
+    (torch.float32, torch.float32, 5000, 700001, 100, 0),         # 280 MB, more than is filled first, but rows below 512 bytes
+    # no fork: just below 32 MiB
+    (torch.bfloat16, torch.bfloat16, 9001, 63000, 264, 0),
+])
+def test_table_gradient_filled_at_once(dtype, out, n, rows, dim, pad):
+    large_tables(dtype, out, n, rows, dim, pad)
