@@ -139,3 +139,44 @@ def test_columns_of_one_buffer():
 ])
 def test_table_gradient_filled_at_once(dtype, out, n, rows, dim, pad):
     large_tables(dtype, out, n, rows, dim, pad)
+
+
+def within_type(got, want, bound):
+    """within, for a result type whose largest finite number the definition's value may exceed."""
+    most = torch.finfo(got.dtype).max
+    over, under = want.abs() - bound > most * (1 + U[got.dtype]), want.abs() + bound < most
+    assert torch.equal(got[over].double(), torch.copysign(torch.full_like(want, float("inf")), want)[over])
+    within(got[under], want[under], bound[under])
+    either = got[~over & ~under]
+    assert (torch.isinf(either) | (either.double().abs() >= (want.abs() - bound)[~over & ~under])).all()
+
+
+@gpu
+@pytest.mark.parametrize("dtype", HALF)
+@pytest.mark.parametrize("n", [1024, 1025, 4096, 4097, 5003])
+def test_packed_tokens(dtype, n):
+    """Blocks that pack one token (up to 1024) or eight, that count for themselves (up to 4096) or look at the tiles' counts; a dim that
+    needs the weight's copy, and one that fills no step."""
+    for rows, dim in ((701, 101), (300, 200)):
+        hidden, weight, labels = vocab_case(n, rows, dim, dtype, seed=220)
+        labels[-1] = rows - 1
+        check_loss(hidden, weight, labels, scale=0.7, z=1e-2)
+        up = (0.5 + torch.rand(n, generator=gen(221), device="cuda")) / n
+        check_grad(hidden, weight, labels, up, z=1e-2)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", HALF)
+@pytest.mark.parametrize("n", [200, 1500, 5003])
+@pytest.mark.parametrize("size", [1e-9, 1.0, 1e3])
+def test_packed_sizes_of_the_upstream_gradient(dtype, n, size, monkeypatch):
+    """The largest one in the last tile of tokens, or an ignored token's: fp16's power of two goes by the tokens that count."""
+    # 64000 times a hidden value is beyond fp16: an infinity of its sign there, as one rounding of the definition's value gives
+    monkeypatch.setattr(test_vocab, "within", within_type)
+    hidden, weight, labels = vocab_case(n, 400, 72, dtype, seed=230)
+    up = torch.rand(n, generator=gen(231), device="cuda") * size
+    labels[-1], up[-1] = 7, 64 * size
+    check_grad(hidden, weight, labels, up)
+    labels[n // 2], up[n // 2] = -100, 2.0 ** 40
+    up[-1] = size
+    check_grad(hidden, weight, labels, up)
