@@ -180,3 +180,46 @@ def test_packed_sizes_of_the_upstream_gradient(dtype, n, size, monkeypatch):
     labels[n // 2], up[n // 2] = -100, 2.0 ** 40
     up[-1] = size
     check_grad(hidden, weight, labels, up)
+
+
+@gpu
+def test_calls_from_threads():
+    """Threads with streams of their own: two that want the library's second stream at once, one on the loss, one on small tables."""
+    n, rows, dim = 9000, 40000, 512
+    ids = torch.randint(0, rows, (n,), generator=gen(240), device="cuda")
+    grads = [torch.randn(n, dim, generator=gen(241 + k), device="cuda").bfloat16() for k in range(2)]
+    hidden, weight, labels = vocab_case(300, 2000, 64, torch.bfloat16, seed=243)
+    up = torch.ones(300, device="cuda")
+
+    def large(k):
+        return lambda: (rd.rd_embed_grad(grads[k], ids, torch.full((rows, dim), 7.0, dtype=torch.bfloat16, device="cuda")),)
+
+    def loss():
+        out = rd.rd_vocab_loss(hidden, weight, labels)
+        return (*out, *rd.rd_vocab_loss_grad(hidden, weight, labels, out[1], up, torch.empty_like(hidden), torch.empty_like(weight)))
+
+    def small():
+        return (rd.rd_embed(weight, labels), rd.rd_embed_grad(hidden, labels, torch.empty_like(weight)))
+
+    calls = (large(0), large(1), loss, small)
+    want = [f() for f in calls]
+    torch.cuda.synchronize()
+    ready, wrong = threading.Barrier(len(calls)), []
+
+    def work(f, expected):
+        try:
+            with torch.cuda.stream(torch.cuda.Stream()):
+                ready.wait(60)
+                got = [f() for _ in range(20)]
+                torch.cuda.current_stream().synchronize()
+            if not all(torch.equal(a, b) for out in got for a, b in zip(out, expected)):
+                wrong.append("results differ")
+        except Exception as e:
+            wrong.append(repr(e))
+
+    threads = [threading.Thread(target=work, args=c) for c in zip(calls, want)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not wrong and rd.rd_vocab_status() == rd.RD_OK
