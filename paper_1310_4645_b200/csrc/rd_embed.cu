@@ -52,8 +52,11 @@ template <> __device__ __forceinline__ float narrow<float>(float v) { return v; 
 template <> __device__ __forceinline__ __nv_bfloat16 narrow<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
 template <> __device__ __forceinline__ __half narrow<__half>(float v) { return __float2half_rn(v); }
 
-// V consecutive elements, moved in accesses of up to 32 bytes (of up to 16 when the vector's type only promises that much).
-template <typename T, int V> struct alignas(sizeof(T) * V < 32 ? sizeof(T) * V : 32) Vec { T v[V]; };
+// V consecutive elements, at most 32 bytes of them, moved in one access.
+template <typename T, int V> struct alignas(sizeof(T) * V) Vec {
+    static_assert(sizeof(T) * V <= 32, "one access");
+    T v[V];
+};
 
 template <typename T, int V> __device__ __forceinline__ Vec<T, V> load(const T *p)
 {
@@ -63,9 +66,6 @@ template <typename T, int V> __device__ __forceinline__ Vec<T, V> load(const T *
         asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
                      : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]), "=r"(w[4]), "=r"(w[5]), "=r"(w[6]), "=r"(w[7])
                      : "l"(p));
-    } else if constexpr (sizeof(x) > 32) {
-#pragma unroll
-        for (int k = 0; k < V; k += 32 / sizeof(T)) *reinterpret_cast<Vec<T, 32 / sizeof(T)> *>(x.v + k) = load<T, 32 / sizeof(T)>(p + k);
     } else {
         x = *reinterpret_cast<const Vec<T, V> *>(p);
     }
@@ -77,9 +77,6 @@ template <typename T, int V> __device__ __forceinline__ void store(T *p, const V
         const uint32_t(&w)[8] = *reinterpret_cast<const uint32_t(*)[8]>(&x);
         asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7])
                      : "memory");
-    } else if constexpr (sizeof(x) > 32) {
-#pragma unroll
-        for (int k = 0; k < V; k += 32 / sizeof(T)) store<T, 32 / sizeof(T)>(p + k, *reinterpret_cast<const Vec<T, 32 / sizeof(T)> *>(x.v + k));
     } else {
         *reinterpret_cast<Vec<T, V> *>(p) = x;
     }
