@@ -19,9 +19,10 @@
 // All three products run on one kernel (tcgen05): a thread block, or a pair of them, computes tiles of 128 x 256 (256 x 256) with
 // the accumulators in tensor memory, two sets, so that one is read while the next is computed; operands come in by TMA into a ring
 // of stages of 64 summed indices; one warp per operand issues the copies, one the products, eight take the results.
-// What bounds it (B200): many tokens, the tensor cores (2048 tokens x 18944 x 4096: 265400 cycles a block, 262144 of them products)
-// at the clock that the board's power limit leaves, 1.25 to 1.4 GHz: 8192 tokens x 131072 x 4096 loss 6.1 ms = 1.43 PFLOP/s,
-// gradient 19.6 to 20.2 ms = 1.31 to 1.35.  Few tokens, the memory: 128 tokens x 131072 x 4096 gradient 0.66 ms for 3.2 GB.
+// What bounds it (B200): many tokens, the tensor cores (2048 tokens x 18944 x 4096: 276400 active cycles an SM, 262144 of them
+// products) at the clock that the board's power limit leaves, 1.25 to 1.45 GHz: 8192 tokens x 131072 x 4096 loss 6.1 ms = 1.44
+// PFLOP/s, gradient 19.4 to 20.5 ms = 1.29 to 1.36.  Few tokens, the memory: 128 tokens x 131072 x 4096 gradient 0.66 ms for 3.2 GB.
+// Rows of at most some 256 values, the exponentials: 8192 tokens x 131072 loss 0.54 ms at dim 64 and 128, 0.6 at 256, 0.8 to 0.9 at 512.
 #include "rd_vocab.h"
 
 #include <cuda.h>
@@ -478,6 +479,8 @@ __device__ __forceinline__ void tmem_wait(uint32_t (&v)[32])
                  : "memory");
 }
 
+// The exponentials of the softmax: one instruction, within about 2^-22 of the value and 0 below 2^-126.  That is less than a
+// logit's own error moves it, and 32768 of them come with every tile of 128 x 256.
 __device__ __forceinline__ float exp2_fast(float x)
 {
     float y;
@@ -1067,8 +1070,9 @@ __global__ void __launch_bounds__(256) rd_vocab_join_kernel(JoinParams p)
 
 // One token, as when a server scores what it generates, and up to four on a weight that TMA cannot address: the weight's bytes are
 // all that counts, so no tensor cores, but warps that stream four rows of the weight at a time past the hidden rows in shared memory.
-// Weight 32768 x 1024, B200, tensor cores / this: 1 token 17.3 / 16.4 us, 2 17.9 / 19.2, 4 17.6 / 27.6; dim 1001, which the tensor
-// cores need a copy for: 1 token 74 / 32, 4 75 / 40.
+// B200, us, tensor cores / this: 1 token of 131072 x 4096 168.9 / 159.6, 131072 x 256 22.4 / 17.4, 32768 x 1024 19.2 / 16.7, 8192 x 4096
+// 22.4 / 17.1, 4096 x 512 11.3 / 7.1, 1009 x 256 8.5 / 7.4; of 32768 x 1024 2 tokens 17.9 / 19.2, 4 17.6 / 27.6; dim 1001, which the
+// tensor cores need a copy for: 1 token 74 / 32 to 37, 4 75 / 40 to 50.
 constexpr size_t kFewTokens = 4;
 constexpr size_t kFewBytes = 32768;       // of hidden rows in shared memory
 constexpr int kFewRows = 4;
