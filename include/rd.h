@@ -98,8 +98,11 @@ typedef enum { RD_SUM = 0, RD_MAX = 1, RD_MIN = 2, RD_PROD = 3 } rd_op_t;
  * gradual underflow).  (Max and min select one of their operands, so the kernels take them on the 16-bit values
  * directly; the bits are the same.)  n_elems counts 16-bit elements (msg_bytes / 2, always even); buffers must be aligned
  * to 4 bytes.  Tree mode only: the schedule-faithful execution would have to hand fp32 partial segments
- * between processes and returns RD_ERR_UNSUPPORTED. */
-typedef enum { RD_INT32 = 0, RD_FP32 = 1, RD_INT64 = 2, RD_FP64 = 3, RD_BF16 = 4, RD_FP16 = 5 } rd_dtype_t;
+ * between processes and returns RD_ERR_UNSUPPORTED.
+ *
+ * RD_E4M3: 8-bit floating point with 4 bits of exponent and 3 of mantissa, no infinities, at most 448; the operators of a
+ * feed-forward block alone have it (the reductions return RD_ERR_INVALID_ARG). */
+typedef enum { RD_INT32 = 0, RD_FP32 = 1, RD_INT64 = 2, RD_FP64 = 3, RD_BF16 = 4, RD_FP16 = 5, RD_E4M3 = 6 } rd_dtype_t;
 typedef enum { RD_EXEC_TREE = 0, RD_EXEC_FAITHFUL = 1 } rd_exec_t;
 
 /* Linear model of Section II.  alpha in seconds, beta and gamma in seconds per
@@ -563,6 +566,89 @@ RD_API int rd_vocab_loss_grad(const rd_vocab_t *v, const float *d_lse, const flo
  * last query did (its results are then not valid); the word is cleared.
  */
 RD_API int rd_vocab_status(int *device_status);
+
+/* ------------------------------------------------------------------------------------------------------
+ * Operators of a feed-forward block (the paper has no counterpart).  A model cut over processes sums partial results of its blocks
+ * with rd_allreduce; these operators are what stands between two such sums on one process: dropout, the residual's addition and a
+ * norm of the joined rows, then the gated projections, of which a process holds a slice of the width.
+ *   - Matrices, streams, errors and overlaps as for the operators on a vocabulary, with one exception: an output may be the very same
+ *     matrix (address, stride, element size) as one of the call's inputs, where a function says so.
+ *   - n = 0 is RD_OK (gradients of weights are then zeros).  Results depend on the arguments alone: no sum depends on timing.
+ *   - Dropout: drop in [0, 1); a value is dropped where its 16 random bits are below border = drop * 65536, rounded to nearest even
+ *     (a border of 65536: RD_ERR_INVALID_ARG), and multiplied by 65536 / (65536 - border), in fp32, where they are not.  The random
+ *     bits of column j of row i are number j mod 8 (word (j mod 8) / 2, lower half first) of Philox 4x32 with 10 rounds at the counter
+ *     (j / 8, first_row + i, offset mod 2^32, offset / 2^32) with the key (seed mod 2^32, seed / 2^32): a function of the place
+ *     alone, so a gradient draws the same mask again, and a process that holds rows first_row.. of a batch draws its own.
+ *     Use another offset (or seed) for every layer and step.  first_row + n at most 2^32, else RD_ERR_UNSUPPORTED.
+ */
+
+/* The operands of rd_norm. */
+typedef struct {
+    const void *x;            /* DEVICE; n x dim, dtype                                                     */
+    size_t x_stride;
+    const void *residual;     /* DEVICE; n x dim, sum_dtype; or NULL: none                                  */
+    size_t residual_stride;
+    const void *weight;       /* DEVICE; dim values, weight_dtype                                           */
+    size_t n, dim;
+    rd_dtype_t dtype;         /* RD_FP32, RD_BF16 or RD_FP16                                                */
+    rd_dtype_t sum_dtype;     /* dtype or RD_FP32                                                           */
+    rd_dtype_t weight_dtype;  /* dtype or RD_FP32                                                           */
+    float eps, drop;          /* eps: finite, not negative                                                  */
+    uint64_t seed, offset;
+    size_t first_row;
+} rd_norm_t;
+
+/*
+ * rd_norm -- the residual's addition and a root-mean-square norm, row by row:
+ *   s = residual + dropout(x),  rstd = 1 / sqrt(mean of s^2 + eps),  out = s * rstd * weight;
+ * all in fp32, sums in an order that the row's length fixes; s, rstd and out are rounded once each, out from the s that has not been rounded.
+ *   out_dtype    dtype, or RD_E4M3: every row has a scale, out_scale = (largest |out| of the row) / 448, and holds out / out_scale,
+ *                rounded to nearest even; a row of zeros has the scale 0.  A NaN in a row makes its scale NaN.
+ *   d_out_scale  DEVICE; n values, with RD_E4M3 alone (else NULL).
+ *   d_sum        DEVICE; n x dim, sum_dtype: s; or NULL.      d_rstd  DEVICE; n values; or NULL.
+ * out and sum may be x or residual (where the types agree).
+ * Rows of 8 values that begin on 16-byte boundaries (8 for RD_E4M3), in every matrix and the weight, move as words of 16 bytes, others
+ * by element.
+ */
+RD_API int rd_norm(const rd_norm_t *v, void *d_out, size_t out_stride, rd_dtype_t out_dtype, float *d_out_scale, void *d_sum, size_t sum_stride,
+                   float *d_rstd, void *cuda_stream);
+
+/* The operands of rd_norm_grad: what rd_norm was given and left. */
+typedef struct {
+    const void *grad_out;     /* DEVICE; n x dim, dtype: gradient of out                                    */
+    size_t grad_out_stride;
+    const void *sum;          /* DEVICE; n x dim, sum_dtype: s (x itself, without residual and dropout)     */
+    size_t sum_stride;
+    const float *rstd;        /* DEVICE; n values                                                           */
+    const void *weight;       /* DEVICE; dim values, weight_dtype                                           */
+    const void *grad_sum;     /* DEVICE; n x dim, sum_dtype: gradient that reaches s past the norm; or NULL */
+    size_t grad_sum_stride;
+    size_t n, dim;
+    rd_dtype_t dtype, sum_dtype, weight_dtype;
+    float drop;               /* as in rd_norm, with the same seed, offset and first_row                    */
+    uint64_t seed, offset;
+    size_t first_row;
+} rd_norm_grad_t;
+
+/*
+ * rd_norm_grad -- its gradients, with xhat = s * rstd and g = grad_out * weight:
+ *   grad_residual = rstd * (g - xhat * mean of g * xhat) + grad_sum,   grad_x = dropout(grad_residual, before it is rounded),
+ *   grad_weight = sum over rows of grad_out * xhat;
+ * in fp32, each rounded once.
+ *   d_grad_x         DEVICE; n x dim, dtype; or NULL.      d_grad_residual  DEVICE; n x dim, sum_dtype; or NULL.
+ *   d_grad_weight    DEVICE; dim values, weight_dtype; or NULL.  Not all three NULL.  Workspace: for grad_weight alone, else NULL, 0.
+ * grad_x and grad_residual may each be grad_out, sum or grad_sum (where the types agree).
+ */
+RD_API int rd_norm_grad_workspace(size_t n, size_t dim, size_t *bytes);
+RD_API int rd_norm_grad(const rd_norm_grad_t *v, void *d_grad_x, size_t grad_x_stride, void *d_grad_residual, size_t grad_residual_stride,
+                        void *d_grad_weight, void *d_workspace, size_t workspace_bytes, void *cuda_stream);
+
+/*
+ * rd_dropout -- out = dropout(x) alone, as of an embedding; its gradient is the same call on the gradient.
+ *   dtype  RD_FP32, RD_BF16 or RD_FP16: x and out.  out may be x.
+ */
+RD_API int rd_dropout(const void *d_x, size_t x_stride, size_t n, size_t dim, rd_dtype_t dtype, float drop, uint64_t seed, uint64_t offset,
+                      size_t first_row, void *d_out, size_t out_stride, void *cuda_stream);
 
 /* rd_strerror -- static, never NULL. */
 RD_API const char *rd_strerror(int status);

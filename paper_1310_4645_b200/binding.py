@@ -20,7 +20,7 @@ RD_ERR_TOO_LARGE = -9
 RD_UNI_GREEDY, RD_BI_GREEDY, RD_BINOMIAL, RD_PIPELINE, RD_BINARY, RD_BUTTERFLY = range(6)
 RD_PORT_UNI, RD_PORT_BI = 0, 1
 RD_SUM, RD_MAX, RD_MIN, RD_PROD = 0, 1, 2, 3
-RD_INT32, RD_FP32, RD_INT64, RD_FP64, RD_BF16, RD_FP16 = 0, 1, 2, 3, 4, 5
+RD_INT32, RD_FP32, RD_INT64, RD_FP64, RD_BF16, RD_FP16, RD_E4M3 = range(7)
 RD_EXEC_TREE, RD_EXEC_FAITHFUL = 0, 1
 RD_TREE_AUTO, RD_TREE_STREAM, RD_TREE_DIRECT, RD_TREE_STREAM_PAIRED = 0, 1, 2, 3
 
@@ -33,7 +33,8 @@ EXPORTS = ("rd_schedule_create", "rd_schedule_create_segments", "rd_optimal_segm
            "rd_schedule_trace", "rd_schedule_faithful_shape", "rd_schedule_actions", "rd_reduce_faithful_static", "rd_search_segmentation", "rd_schedule_status",
            "rd_reduce_batch", "rd_schedule_set_tree_variant", "rd_schedule_tree_shape", "rd_allreduce",
            "rd_embed", "rd_embed_grad", "rd_embed_grad_workspace", "rd_vocab_loss", "rd_vocab_loss_workspace", "rd_vocab_loss_grad",
-           "rd_vocab_loss_grad_workspace", "rd_vocab_status")
+           "rd_vocab_loss_grad_workspace", "rd_vocab_status",
+           "rd_norm", "rd_norm_grad", "rd_norm_grad_workspace", "rd_dropout")
 
 
 class rd_model_t(C.Structure):
@@ -50,6 +51,19 @@ class rd_vocab_t(C.Structure):
     _fields_ = [("hidden", C.c_void_p), ("hidden_stride", C.c_size_t), ("weight", C.c_void_p), ("weight_stride", C.c_size_t),
                 ("labels", C.c_void_p), ("n", C.c_size_t), ("rows", C.c_size_t), ("dim", C.c_size_t), ("first_row", C.c_int64),
                 ("dtype", C.c_int), ("label_type", C.c_int), ("scale", C.c_float), ("z_loss", C.c_float)]
+
+
+class rd_norm_t(C.Structure):
+    _fields_ = [("x", C.c_void_p), ("x_stride", C.c_size_t), ("residual", C.c_void_p), ("residual_stride", C.c_size_t), ("weight", C.c_void_p),
+                ("n", C.c_size_t), ("dim", C.c_size_t), ("dtype", C.c_int), ("sum_dtype", C.c_int), ("weight_dtype", C.c_int), ("eps", C.c_float),
+                ("drop", C.c_float), ("seed", C.c_uint64), ("offset", C.c_uint64), ("first_row", C.c_size_t)]
+
+
+class rd_norm_grad_t(C.Structure):
+    _fields_ = [("grad_out", C.c_void_p), ("grad_out_stride", C.c_size_t), ("sum", C.c_void_p), ("sum_stride", C.c_size_t), ("rstd", C.c_void_p),
+                ("weight", C.c_void_p), ("grad_sum", C.c_void_p), ("grad_sum_stride", C.c_size_t), ("n", C.c_size_t), ("dim", C.c_size_t),
+                ("dtype", C.c_int), ("sum_dtype", C.c_int), ("weight_dtype", C.c_int), ("drop", C.c_float), ("seed", C.c_uint64),
+                ("offset", C.c_uint64), ("first_row", C.c_size_t)]
 
 
 EVENT_DTYPE = np.dtype(
@@ -107,6 +121,11 @@ def lib():
         L.rd_embed_grad.argtypes = [vp, sz, i32, vp, i32, sz, i64, f32, vp, sz, i32, sz, sz, i32, vp, sz, vp]
         L.rd_vocab_loss_workspace.argtypes = [C.POINTER(rd_vocab_t), C.POINTER(sz)]
         L.rd_vocab_loss.argtypes = [C.POINTER(rd_vocab_t), vp, vp, vp, vp, sz, vp]
+        u64 = C.c_uint64
+        L.rd_norm.argtypes = [C.POINTER(rd_norm_t), vp, sz, i32, vp, vp, sz, vp, vp]
+        L.rd_norm_grad_workspace.argtypes = [sz, sz, C.POINTER(sz)]
+        L.rd_norm_grad.argtypes = [C.POINTER(rd_norm_grad_t), vp, sz, vp, sz, vp, vp, sz, vp]
+        L.rd_dropout.argtypes = [vp, sz, sz, sz, i32, f32, u64, u64, sz, vp, sz, vp]
         L.rd_vocab_loss_grad_workspace.argtypes = [C.POINTER(rd_vocab_t), i32, i32, C.POINTER(sz)]
         L.rd_vocab_loss_grad.argtypes = [C.POINTER(rd_vocab_t), vp, vp, sz, vp, sz, vp, sz, vp, sz, vp]
         L.rd_vocab_status.argtypes = [C.POINTER(i32)]
@@ -531,3 +550,56 @@ def rd_vocab_status() -> int:
     st = C.c_int(0)
     _check(lib().rd_vocab_status(C.byref(st)), "rd_vocab_status")
     return st.value
+
+
+# ---------------------------------------------------------------------------------------------------------------
+# Operators of a feed-forward block
+
+
+def rd_norm(x, weight, residual=None, eps=1e-6, out_dtype=None, drop=0.0, seed=0, offset=0, first_row=0, out=None, total=None, stream=None):
+    """total = residual + dropout(x), rstd = 1 / sqrt(mean(total ** 2) + eps), out = total * rstd * weight, row by row.
+    x: [n, dim] float32, bfloat16 or float16; residual: [n, dim] of x's dtype or float32; weight: [dim] of x's dtype or float32;
+    out_dtype: x's (None) or torch.float8_e4m3fn, whose rows hold out / scale.  out and total are allocated when None; out may be x,
+    total may be x or residual.  Returns (out, total, rstd, scale): total is None without residual and dropout (it is x then), scale
+    is None unless out is in 8 bits.  The mask is a function of (seed, offset, first_row + row, column): see rd_dropout."""
+    if stream is not None:
+        return _on_stream(rd_norm, x, stream, x, weight, residual, eps, out_dtype, drop, seed, offset, first_row, out, total)
+    r = _native().norm(x, weight, residual, eps, out_dtype, drop, seed, offset, first_row, out, total)
+    if r.__class__ is int:
+        raise RdError(r, "rd_norm")
+    return r
+
+
+def rd_norm_grad_workspace(n, dim) -> int:
+    need = C.c_size_t()
+    _check(lib().rd_norm_grad_workspace(n, dim, C.byref(need)), "rd_norm_grad_workspace")
+    return need.value
+
+
+def rd_norm_grad(grad_out, total, weight, rstd, grad_total=None, want_residual=True, want_weight=True, drop=0.0, seed=0, offset=0, first_row=0,
+                 grad_x=None, grad_residual=None, grad_weight=None, workspace=None, stream=None):
+    """Gradients of rd_norm: (grad_x, grad_residual, grad_weight).  total, rstd: what rd_norm returned (total: x where that was None);
+    grad_total: gradient that reaches total past the norm, of total's dtype, or None; drop, seed, offset, first_row: rd_norm's.
+    Outputs are allocated when None; grad_x and grad_residual may be grad_out, total or grad_total.  Without dropout and in one dtype
+    grad_residual is grad_x, unless one is given.  want_residual, want_weight: False leaves that gradient out (None).
+    workspace: rd_norm_grad_workspace bytes (allocated when None)."""
+    if stream is not None:
+        return _on_stream(rd_norm_grad, grad_out, stream, grad_out, total, weight, rstd, grad_total, want_residual, want_weight, drop, seed, offset,
+                          first_row, grad_x, grad_residual, grad_weight, workspace)
+    r = _native().norm_grad(grad_out, total, weight, rstd, grad_total, want_residual, want_weight, drop, seed, offset, first_row, grad_x, grad_residual,
+                            grad_weight, workspace)
+    if r.__class__ is int:
+        raise RdError(r, "rd_norm_grad")
+    return r
+
+
+def rd_dropout(x, drop, seed, offset=0, first_row=0, out=None, stream=None):
+    """x with a share `drop` of its values set to 0 and the others multiplied by 1 / (1 - drop) (drop as a multiple of 2^-16); which ones
+    depends on (seed, offset, first_row + row, column) alone, so the gradient is the same call on the gradient.  x: [n, dim] float32,
+    bfloat16 or float16; out: like x (allocated when None), may be x.  Returns out."""
+    if stream is not None:
+        return _on_stream(rd_dropout, x, stream, x, drop, seed, offset, first_row, out)
+    r = _native().dropout(x, drop, seed, offset, first_row, out)
+    if r.__class__ is int:
+        raise RdError(r, "rd_dropout")
+    return r

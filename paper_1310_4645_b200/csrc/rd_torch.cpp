@@ -1,4 +1,4 @@
-// Marshalling of the vocabulary operators' tensors: the same checks and calls that ctypes would make, without the interpreter.
+// Marshalling of the operators' tensors (vocabulary, feed-forward block): the same checks and calls that ctypes would make, without the interpreter.
 // A call on one token takes some 3 microseconds on the device; reading its tensors' properties, allocating and calling from Python
 // took 9 to 17 on the host (passes back to back: rd_embed of one token 8.4 us with ctypes, 3.7 with this; rd_embed_grad of 257 tokens
 // 16.3, 10.4).  Nothing is computed here.
@@ -12,6 +12,7 @@
 #include <c10/cuda/CUDACachingAllocator.h>
 #include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
+#include <torch/csrc/Dtype.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <new>
@@ -44,9 +45,10 @@ rd_dtype_t code(const at::Tensor &t)
     case at::kDouble: return RD_FP64;
     case at::kBFloat16: return RD_BF16;
     case at::kHalf: return RD_FP16;
+    case at::kFloat8_e4m3fn: return RD_E4M3;
     default: break;
     }
-    PyErr_SetString(PyExc_TypeError, "int32, float32, int64, float64, bfloat16 or float16 expected");
+    PyErr_SetString(PyExc_TypeError, "int32, float32, int64, float64, bfloat16, float16 or float8_e4m3fn expected");
     throw PythonError();
 }
 
@@ -281,11 +283,203 @@ PyObject *vocab_loss_grad(PyObject *, PyObject *const *a, Py_ssize_t n_args)
     });
 }
 
+uint64_t bits(PyObject *o)
+{
+    const unsigned long long v = PyLong_AsUnsignedLongLong(o);
+    if (v == ~0ull && PyErr_Occurred()) throw PythonError();
+    return v;
+}
+size_t count(PyObject *o)
+{
+    const int64_t v = whole(o);
+    if (v < 0) wrong("first_row must not be negative");
+    return size_t(v);
+}
+bool truth(PyObject *o)
+{
+    const int v = PyObject_IsTrue(o);
+    if (v < 0) throw PythonError();
+    return v;
+}
+
+// The given tensor, or a new one; [rows, dim] of a type on a device.
+at::Tensor matrix_or_new(PyObject *given, size_t rows, size_t dim, at::ScalarType type, c10::Device device, const char *what)
+{
+    if (given == Py_None) return empty({int64_t(rows), int64_t(dim)}, type, device);
+    const at::Tensor &t = tensor(given, what);
+    if (t.dim() != 2 || size_t(t.size(0)) != rows || size_t(t.size(1)) != dim || t.scalar_type() != type || t.device() != device) wrong(what);
+    return t;
+}
+const at::Tensor &weight_vector(PyObject *o, size_t dim, c10::Device device)
+{
+    const at::Tensor &t = tensor(o, "weight must be a CUDA vector");
+    vector(t, dim, device, "weight must be a contiguous CUDA vector with one value per column, on the operands' device");
+    return t;
+}
+PyObject *wrap_or_none(const at::Tensor &t) { return t.defined() ? THPVariable_Wrap(t) : Py_NewRef(Py_None); }
+
+// x, weight, residual, eps, out_dtype, drop, seed, offset, first_row, out, total
+PyObject *norm(PyObject *, PyObject *const *a, Py_ssize_t n_args)
+{
+    return guarded(n_args, 11, [&]() -> PyObject * {
+        const at::Tensor &x = tensor(a[0], "x must be a 2-D CUDA tensor");
+        const Matrix m(x, "x must be a 2-D CUDA tensor with contiguous rows");
+        const c10::Device device = x.device();
+        const c10::cuda::OptionalCUDAGuard guard(device);
+        const at::Tensor &weight = weight_vector(a[1], m.dim, device);
+        rd_norm_t v{};
+        v.x = m.data;
+        v.x_stride = m.stride;
+        v.weight = weight.data_ptr();
+        v.n = m.rows;
+        v.dim = m.dim;
+        v.dtype = v.sum_dtype = code(x);
+        v.weight_dtype = code(weight);
+        v.eps = real(a[3]);
+        v.drop = real(a[5]);
+        v.seed = bits(a[6]);
+        v.offset = bits(a[7]);
+        v.first_row = count(a[8]);
+        at::ScalarType out_type = x.scalar_type(), sum_type = x.scalar_type();
+        if (a[4] != Py_None) {
+            if (!THPDtype_Check(a[4])) wrong("out_dtype must be x's dtype or torch.float8_e4m3fn");
+            out_type = reinterpret_cast<THPDtype *>(a[4])->scalar_type;
+            if (out_type != x.scalar_type() && out_type != at::kFloat8_e4m3fn) wrong("out_dtype must be x's dtype or torch.float8_e4m3fn");
+        }
+        if (a[2] != Py_None) {
+            const at::Tensor &residual = tensor(a[2], "residual must be a 2-D CUDA tensor");
+            const Matrix r(residual, "residual must be a 2-D CUDA tensor with contiguous rows");
+            if (r.rows != m.rows || r.dim != m.dim || residual.device() != device) wrong("residual must be [n, dim] on x's device");
+            v.residual = r.data;
+            v.residual_stride = r.stride;
+            v.sum_dtype = code(residual);
+            sum_type = residual.scalar_type();
+        } else if (a[10] != Py_None) {
+            sum_type = tensor(a[10], "total must be a 2-D CUDA tensor").scalar_type();
+            v.sum_dtype = code(tensor(a[10], ""));
+        }
+        const at::Tensor out = matrix_or_new(a[9], m.rows, m.dim, out_type, device, "out must be [n, dim] of out_dtype on x's device");
+        at::Tensor total, rstd = empty({int64_t(m.rows)}, at::kFloat, device), scale;
+        const Matrix o(out, "out must be a 2-D CUDA tensor with contiguous rows");
+        Matrix s = o;
+        s.data = nullptr;
+        if (a[2] != Py_None || a[10] != Py_None || v.drop != 0.0f) {
+            total = matrix_or_new(a[10], m.rows, m.dim, sum_type, device, "total must be [n, dim] of residual's dtype on x's device");
+            s = Matrix(total, "total must be a 2-D CUDA tensor with contiguous rows");
+        }
+        if (out_type == at::kFloat8_e4m3fn) scale = empty({int64_t(m.rows)}, at::kFloat, device);
+        float *at_scale = scale.defined() ? static_cast<float *>(scale.data_ptr()) : nullptr, *at_rstd = static_cast<float *>(rstd.data_ptr());
+        const rd_dtype_t out_code = code(out);
+        const cudaStream_t stream = c10::cuda::getCurrentCUDAStream(device.index());
+        const int rc = without_gil([&] { return rd_norm(&v, o.data, o.stride, out_code, at_scale, s.data, s.stride, at_rstd, stream); });
+        if (rc != RD_OK) return status(rc);
+        PyObject *r = PyTuple_New(4);
+        if (!r) throw PythonError();
+        PyTuple_SET_ITEM(r, 0, a[9] == Py_None ? THPVariable_Wrap(out) : Py_NewRef(a[9]));
+        PyTuple_SET_ITEM(r, 1, a[10] == Py_None ? wrap_or_none(total) : Py_NewRef(a[10]));
+        PyTuple_SET_ITEM(r, 2, THPVariable_Wrap(rstd));
+        PyTuple_SET_ITEM(r, 3, wrap_or_none(scale));
+        return r;
+    });
+}
+
+// grad_out, total, weight, rstd, grad_total, want_residual, want_weight, drop, seed, offset, first_row, grad_x, grad_residual, grad_weight, workspace
+PyObject *norm_grad(PyObject *, PyObject *const *a, Py_ssize_t n_args)
+{
+    return guarded(n_args, 15, [&]() -> PyObject * {
+        const at::Tensor &up = tensor(a[0], "grad_out must be a 2-D CUDA tensor"), &total = tensor(a[1], "total must be a 2-D CUDA tensor");
+        const Matrix g(up, "grad_out must be a 2-D CUDA tensor with contiguous rows"), t(total, "total must be a 2-D CUDA tensor with contiguous rows");
+        const c10::Device device = up.device();
+        const c10::cuda::OptionalCUDAGuard guard(device);
+        if (t.rows != g.rows || t.dim != g.dim || total.device() != device) wrong("total must be [n, dim] on grad_out's device");
+        const at::Tensor &weight = weight_vector(a[2], g.dim, device), &rstd = tensor(a[3], "rstd must be a CUDA vector");
+        rd_norm_grad_t v{};
+        v.grad_out = g.data;
+        v.grad_out_stride = g.stride;
+        v.sum = t.data;
+        v.sum_stride = t.stride;
+        v.rstd = static_cast<const float *>(vector(rstd, g.rows, device, "rstd must be a contiguous CUDA vector with one value per row, on the operands' device"));
+        if (rstd.scalar_type() != at::kFloat) wrong("rstd must be float32");
+        v.weight = weight.data_ptr();
+        v.n = g.rows;
+        v.dim = g.dim;
+        v.dtype = code(up);
+        v.sum_dtype = code(total);
+        v.weight_dtype = code(weight);
+        if (a[4] != Py_None) {
+            const at::Tensor &more = tensor(a[4], "grad_total must be a 2-D CUDA tensor");
+            const Matrix m(more, "grad_total must be a 2-D CUDA tensor with contiguous rows");
+            if (m.rows != g.rows || m.dim != g.dim || more.scalar_type() != total.scalar_type() || more.device() != device) wrong("grad_total must be [n, dim] with total's dtype and device");
+            v.grad_sum = m.data;
+            v.grad_sum_stride = m.stride;
+        }
+        const bool want_residual = truth(a[5]) || a[12] != Py_None, want_weight = truth(a[6]) || a[13] != Py_None;
+        v.drop = real(a[7]);
+        v.seed = bits(a[8]);
+        v.offset = bits(a[9]);
+        v.first_row = count(a[10]);
+        const at::Tensor gx = matrix_or_new(a[11], g.rows, g.dim, up.scalar_type(), device, "grad_x must be [n, dim] with grad_out's dtype and device");
+        // without dropout, in one type, the two gradients are the same matrix
+        const bool shared = want_residual && a[12] == Py_None && v.drop == 0.0f && total.scalar_type() == up.scalar_type();
+        at::Tensor gr, gw;
+        const Matrix x(gx, "grad_x must be a 2-D CUDA tensor with contiguous rows");
+        Matrix r = x;
+        r.data = nullptr;
+        if (want_residual && !shared) {
+            gr = matrix_or_new(a[12], g.rows, g.dim, total.scalar_type(), device, "grad_residual must be [n, dim] with total's dtype and device");
+            r = Matrix(gr, "grad_residual must be a 2-D CUDA tensor with contiguous rows");
+        }
+        const cudaStream_t stream = c10::cuda::getCurrentCUDAStream(device.index());
+        void *at_weight = nullptr;
+        size_t need = 0;
+        if (want_weight) {
+            if (a[13] == Py_None) gw = empty({int64_t(g.dim)}, weight.scalar_type(), device);
+            else gw = tensor(a[13], "grad_weight must be a CUDA vector");
+            at_weight = vector(gw, g.dim, device, "grad_weight must be a contiguous CUDA vector with one value per column, on the operands' device");
+            if (gw.scalar_type() != weight.scalar_type()) wrong("grad_weight must have weight's dtype");
+            if (const int rc = rd_norm_grad_workspace(v.n, v.dim, &need)) return status(rc);
+        }
+        const Workspace w(a[14], need, device, stream);
+        const int rc = without_gil([&] { return rd_norm_grad(&v, x.data, x.stride, r.data, r.stride, at_weight, w.data, w.size, stream); });
+        if (rc != RD_OK) return status(rc);
+        PyObject *o = PyTuple_New(3);
+        if (!o) throw PythonError();
+        PyObject *first = a[11] == Py_None ? THPVariable_Wrap(gx) : Py_NewRef(a[11]);
+        PyTuple_SET_ITEM(o, 0, first);
+        PyTuple_SET_ITEM(o, 1, shared ? Py_NewRef(first) : a[12] == Py_None ? wrap_or_none(gr) : Py_NewRef(a[12]));
+        PyTuple_SET_ITEM(o, 2, a[13] == Py_None ? wrap_or_none(gw) : Py_NewRef(a[13]));
+        return o;
+    });
+}
+
+// x, drop, seed, offset, first_row, out
+PyObject *dropout(PyObject *, PyObject *const *a, Py_ssize_t n_args)
+{
+    return guarded(n_args, 6, [&]() -> PyObject * {
+        const at::Tensor &x = tensor(a[0], "x must be a 2-D CUDA tensor");
+        const Matrix m(x, "x must be a 2-D CUDA tensor with contiguous rows");
+        const c10::cuda::OptionalCUDAGuard guard(x.device());
+        const at::Tensor out = matrix_or_new(a[5], m.rows, m.dim, x.scalar_type(), x.device(), "out must be [n, dim] with x's dtype and device");
+        const Matrix o(out, "out must be a 2-D CUDA tensor with contiguous rows");
+        const rd_dtype_t dtype = code(x);
+        const float drop = real(a[1]);
+        const uint64_t seed = bits(a[2]), offset = bits(a[3]);
+        const size_t first = count(a[4]);
+        const cudaStream_t stream = c10::cuda::getCurrentCUDAStream(x.device().index());
+        const int rc = without_gil([&] { return rd_dropout(m.data, m.stride, m.rows, m.dim, dtype, drop, seed, offset, first, o.data, o.stride, stream); });
+        if (rc != RD_OK) return status(rc);
+        return a[5] == Py_None ? THPVariable_Wrap(out) : Py_NewRef(a[5]);
+    });
+}
+
 PyMethodDef methods[] = {
     {"embed", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(embed)), METH_FASTCALL, nullptr},
     {"embed_grad", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(embed_grad)), METH_FASTCALL, nullptr},
     {"vocab_loss", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(vocab_loss)), METH_FASTCALL, nullptr},
     {"vocab_loss_grad", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(vocab_loss_grad)), METH_FASTCALL, nullptr},
+    {"norm", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(norm)), METH_FASTCALL, nullptr},
+    {"norm_grad", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(norm_grad)), METH_FASTCALL, nullptr},
+    {"dropout", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(dropout)), METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_rd_torch", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
