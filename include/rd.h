@@ -650,6 +650,62 @@ RD_API int rd_norm_grad(const rd_norm_grad_t *v, void *d_grad_x, size_t grad_x_s
 RD_API int rd_dropout(const void *d_x, size_t x_stride, size_t n, size_t dim, rd_dtype_t dtype, float drop, uint64_t seed, uint64_t offset,
                       size_t first_row, void *d_out, size_t out_stride, void *cuda_stream);
 
+/* Activations of the gated projections. */
+typedef enum {
+    RD_SILU = 0, /* g / (1 + exp(-g))                                                                */
+    RD_GELU = 1, /* g (1 + tanh(sqrt(2 / pi) (g + 0.044715 g^3))) / 2                                */
+    RD_RELU = 2  /* max(g, 0); its slope at 0 is 0                                                   */
+} rd_activation_t;
+
+/* The operands of rd_gated and rd_gated_grad.  A process's slice of the width is `width` rows of both weights. */
+typedef struct {
+    const void *x;            /* DEVICE; n x dim                                                            */
+    size_t x_stride;
+    const void *gate_weight;  /* DEVICE; width x dim                                                        */
+    size_t gate_weight_stride;
+    const void *up_weight;    /* DEVICE; width x dim                                                        */
+    size_t up_weight_stride;
+    const float *x_scale, *gate_scale, *up_scale;     /* DEVICE; RD_E4M3: n, width and width values that the rows are to be multiplied by; else NULL */
+    size_t n, dim, width;     /* width: at most 2^20                                                        */
+    rd_dtype_t dtype;         /* RD_BF16, RD_FP16 or (rd_gated alone) RD_E4M3: x and the weights             */
+    rd_activation_t activation;
+} rd_gated_t;
+
+/*
+ * rd_gated -- both projections of a gated feed-forward block, the activation and the product:
+ *   gate = x . gate_weight^T,  up = x . up_weight^T  (RD_E4M3: times x_scale and gate_scale, x_scale and up_scale),
+ *   out = act(gate) * up;
+ * products exact, sums fp32 as the tensor cores add them up, out computed from fp32 gate and up and rounded once.  (exp and 1/x of the
+ * activation are within about 2^-22.)
+ *   out_dtype      dtype; with RD_E4M3 RD_BF16 or RD_FP16: out, gate and up.
+ *   d_gate, d_up   DEVICE; n x width: gate and up, rounded once, as rd_gated_grad reads them; each may be NULL.
+ * x or a weight whose base or stride is not a multiple of 16 bytes (or is 0: one row for all) is copied into the workspace by every call.
+ * Results that begin on 16-byte boundaries in every row are stored 16 bytes at a time.
+ */
+RD_API int rd_gated_workspace(const rd_gated_t *v, size_t *bytes);
+RD_API int rd_gated(const rd_gated_t *v, void *d_out, size_t out_stride, rd_dtype_t out_dtype, void *d_gate, size_t gate_stride, void *d_up, size_t up_stride,
+                    void *d_workspace, size_t workspace_bytes, void *cuda_stream);
+
+/*
+ * rd_gated_grad -- its gradients, from gate and up as rd_gated left them (RD_BF16, RD_FP16):
+ *   dgate = grad_out * up * act'(gate),  dup = grad_out * act(gate), each rounded to dtype once;
+ *   grad_x = dgate . gate_weight + dup . up_weight,  grad_gate_weight = dgate^T . x,  grad_up_weight = dup^T . x;
+ * sums fp32, results (dtype) rounded once.
+ *   d_grad_x                                   DEVICE; n x dim; or NULL.  For a slice: the slice's part; add the parts (rd_allreduce).
+ *   d_grad_gate_weight, d_grad_up_weight       DEVICE; width x dim; each may be NULL.  Not all three NULL.
+ */
+RD_API int rd_gated_grad_workspace(const rd_gated_t *v, int want_x, size_t *bytes);
+RD_API int rd_gated_grad(const rd_gated_t *v, const void *d_grad_out, size_t grad_out_stride, const void *d_gate, size_t gate_stride, const void *d_up, size_t up_stride,
+                         void *d_grad_x, size_t grad_x_stride, void *d_grad_gate_weight, size_t grad_gate_weight_stride, void *d_grad_up_weight, size_t grad_up_weight_stride,
+                         void *d_workspace, size_t workspace_bytes, void *cuda_stream);
+
+/*
+ * rd_gated_status -- waits for the current device and returns the word in which the kernels of rd_gated and rd_gated_grad note a bounded
+ * wait that they gave up (it should never happen): 0, or RD_ERR_TIMEOUT if some launch since the last query did (its results are then
+ * not valid); the word is cleared.
+ */
+RD_API int rd_gated_status(int *device_status);
+
 /* rd_strerror -- static, never NULL. */
 RD_API const char *rd_strerror(int status);
 

@@ -22,6 +22,7 @@ RD_PORT_UNI, RD_PORT_BI = 0, 1
 RD_SUM, RD_MAX, RD_MIN, RD_PROD = 0, 1, 2, 3
 RD_INT32, RD_FP32, RD_INT64, RD_FP64, RD_BF16, RD_FP16, RD_E4M3 = range(7)
 RD_EXEC_TREE, RD_EXEC_FAITHFUL = 0, 1
+RD_SILU, RD_GELU, RD_RELU = 0, 1, 2
 RD_TREE_AUTO, RD_TREE_STREAM, RD_TREE_DIRECT, RD_TREE_STREAM_PAIRED = 0, 1, 2, 3
 
 ALGOS = {"uni_greedy": RD_UNI_GREEDY, "bi_greedy": RD_BI_GREEDY, "binomial": RD_BINOMIAL,
@@ -34,7 +35,8 @@ EXPORTS = ("rd_schedule_create", "rd_schedule_create_segments", "rd_optimal_segm
            "rd_reduce_batch", "rd_schedule_set_tree_variant", "rd_schedule_tree_shape", "rd_allreduce",
            "rd_embed", "rd_embed_grad", "rd_embed_grad_workspace", "rd_vocab_loss", "rd_vocab_loss_workspace", "rd_vocab_loss_grad",
            "rd_vocab_loss_grad_workspace", "rd_vocab_status",
-           "rd_norm", "rd_norm_grad", "rd_norm_grad_workspace", "rd_dropout")
+           "rd_norm", "rd_norm_grad", "rd_norm_grad_workspace", "rd_dropout", "rd_gated", "rd_gated_workspace", "rd_gated_grad",
+           "rd_gated_grad_workspace", "rd_gated_status")
 
 
 class rd_model_t(C.Structure):
@@ -64,6 +66,12 @@ class rd_norm_grad_t(C.Structure):
                 ("weight", C.c_void_p), ("grad_sum", C.c_void_p), ("grad_sum_stride", C.c_size_t), ("n", C.c_size_t), ("dim", C.c_size_t),
                 ("dtype", C.c_int), ("sum_dtype", C.c_int), ("weight_dtype", C.c_int), ("drop", C.c_float), ("seed", C.c_uint64),
                 ("offset", C.c_uint64), ("first_row", C.c_size_t)]
+
+
+class rd_gated_t(C.Structure):
+    _fields_ = [("x", C.c_void_p), ("x_stride", C.c_size_t), ("gate_weight", C.c_void_p), ("gate_weight_stride", C.c_size_t), ("up_weight", C.c_void_p),
+                ("up_weight_stride", C.c_size_t), ("x_scale", C.c_void_p), ("gate_scale", C.c_void_p), ("up_scale", C.c_void_p), ("n", C.c_size_t),
+                ("dim", C.c_size_t), ("width", C.c_size_t), ("dtype", C.c_int), ("activation", C.c_int)]
 
 
 EVENT_DTYPE = np.dtype(
@@ -125,6 +133,11 @@ def lib():
         L.rd_norm.argtypes = [C.POINTER(rd_norm_t), vp, sz, i32, vp, vp, sz, vp, vp]
         L.rd_norm_grad_workspace.argtypes = [sz, sz, C.POINTER(sz)]
         L.rd_norm_grad.argtypes = [C.POINTER(rd_norm_grad_t), vp, sz, vp, sz, vp, vp, sz, vp]
+        L.rd_gated_workspace.argtypes = [C.POINTER(rd_gated_t), C.POINTER(sz)]
+        L.rd_gated.argtypes = [C.POINTER(rd_gated_t), vp, sz, i32, vp, sz, vp, sz, vp, sz, vp]
+        L.rd_gated_grad_workspace.argtypes = [C.POINTER(rd_gated_t), i32, C.POINTER(sz)]
+        L.rd_gated_grad.argtypes = [C.POINTER(rd_gated_t), vp, sz, vp, sz, vp, sz, vp, sz, vp, sz, vp, sz, vp, sz, vp]
+        L.rd_gated_status.argtypes = [C.POINTER(i32)]
         L.rd_dropout.argtypes = [vp, sz, sz, sz, i32, f32, u64, u64, sz, vp, sz, vp]
         L.rd_vocab_loss_grad_workspace.argtypes = [C.POINTER(rd_vocab_t), i32, i32, C.POINTER(sz)]
         L.rd_vocab_loss_grad.argtypes = [C.POINTER(rd_vocab_t), vp, vp, sz, vp, sz, vp, sz, vp, sz, vp]
@@ -603,3 +616,60 @@ def rd_dropout(x, drop, seed, offset=0, first_row=0, out=None, stream=None):
     if r.__class__ is int:
         raise RdError(r, "rd_dropout")
     return r
+
+
+def _gated_shape(x, gate_weight, up_weight, scales):
+    """The operands as far as the workspace depends on them.  A matrix of one row has no stride, as in the calls."""
+    stride = lambda t: t.stride(0) if t.shape[0] > 1 else t.shape[1]
+    at = lambda t: None if t is None else t.data_ptr()
+    import torch
+    code = RD_E4M3 if x.dtype == torch.float8_e4m3fn else _dtype_code(x)
+    return rd_gated_t(at(x), stride(x), at(gate_weight), stride(gate_weight), at(up_weight), stride(up_weight), *map(at, scales), x.shape[0], x.shape[1],
+                      gate_weight.shape[0], code, RD_SILU)
+
+
+def rd_gated_workspace(x, gate_weight, up_weight, x_scale=None, gate_scale=None, up_scale=None) -> int:
+    need = C.c_size_t()
+    _check(lib().rd_gated_workspace(C.byref(_gated_shape(x, gate_weight, up_weight, (x_scale, gate_scale, up_scale))), C.byref(need)), "rd_gated_workspace")
+    return need.value
+
+
+def rd_gated(x, gate_weight, up_weight, activation=RD_SILU, keep=False, x_scale=None, gate_scale=None, up_scale=None, out_dtype=None, out=None, gate=None,
+             up=None, workspace=None, stream=None):
+    """out = act(gate) * up with gate = x @ gate_weight.T and up = x @ up_weight.T.  x: [n, dim], weights: [width, dim], all bfloat16, float16 or
+    float8_e4m3fn; with the last x_scale [n], gate_scale and up_scale [width] (float32) multiply the rows, and out_dtype is
+    bfloat16 (None) or float16.  keep: gate and up are wanted, too, as rd_gated_grad reads them.  out, gate, up: [n, width], allocated when
+    None; workspace: rd_gated_workspace bytes (allocated when None).  Returns (out, gate, up), None for what is not kept."""
+    if stream is not None:
+        return _on_stream(rd_gated, x, stream, x, gate_weight, up_weight, activation, keep, x_scale, gate_scale, up_scale, out_dtype, out, gate, up, workspace)
+    r = _native().gated(x, gate_weight, up_weight, activation, keep, x_scale, gate_scale, up_scale, out_dtype, out, gate, up, workspace)
+    if r.__class__ is int:
+        raise RdError(r, "rd_gated")
+    return r
+
+
+def rd_gated_grad_workspace(x, gate_weight, up_weight, want_x=True) -> int:
+    need = C.c_size_t()
+    _check(lib().rd_gated_grad_workspace(C.byref(_gated_shape(x, gate_weight, up_weight, (None,) * 3)), int(want_x), C.byref(need)), "rd_gated_grad_workspace")
+    return need.value
+
+
+def rd_gated_grad(grad_out, x, gate_weight, up_weight, gate, up, activation=RD_SILU, want_x=True, want_weights=True, grad_x=None, grad_gate_weight=None,
+                  grad_up_weight=None, workspace=None, stream=None):
+    """Gradients of rd_gated: (grad_x, grad_gate_weight, grad_up_weight), of the operands' dtype (bfloat16 or float16).  gate, up: what
+    rd_gated kept.  want_x, want_weights: False leaves those out (None), unless a tensor for them is given; outputs are allocated when
+    None.  workspace: rd_gated_grad_workspace bytes (allocated when None)."""
+    if stream is not None:
+        return _on_stream(rd_gated_grad, x, stream, grad_out, x, gate_weight, up_weight, gate, up, activation, want_x, want_weights, grad_x, grad_gate_weight,
+                          grad_up_weight, workspace)
+    r = _native().gated_grad(grad_out, x, gate_weight, up_weight, gate, up, activation, want_x, want_weights, grad_x, grad_gate_weight, grad_up_weight, workspace)
+    if r.__class__ is int:
+        raise RdError(r, "rd_gated_grad")
+    return r
+
+
+def rd_gated_status() -> int:
+    """Waits for the current device and returns (and clears) the gated kernels' status word: 0 or RD_ERR_TIMEOUT."""
+    st = C.c_int(0)
+    _check(lib().rd_gated_status(C.byref(st)), "rd_gated_status")
+    return st.value

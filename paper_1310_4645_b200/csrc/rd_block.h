@@ -48,6 +48,31 @@ struct DropoutArgs {
     cudaStream_t stream;
 };
 
+// Operands of the gated projections and of their gradient.
+struct GatedArgs {
+    const void *x, *gate_weight, *up_weight;            // n x dim, width x dim
+    size_t x_stride, gate_weight_stride, up_weight_stride, n, dim, width;
+    const float *x_scale, *gate_scale, *up_scale;       // 8 bits: n, width, width
+    int dtype, out_dtype, activation;                   // rd_dtype_t, rd_activation_t
+    void *out;                                          // n x width
+    size_t out_stride;
+    // what the projections give before the activation: written where not null, read by the gradient
+    void *gate, *up;
+    size_t gate_stride, up_stride;
+    // gradient: outputs may be null
+    const void *grad_out;
+    void *grad_x, *grad_gate_weight, *grad_up_weight;
+    size_t grad_out_stride, grad_x_stride, grad_gate_weight_stride, grad_up_weight_stride;
+    void *workspace;
+    cudaStream_t stream;
+};
+
+size_t gated_workspace(const GatedArgs &a);
+cudaError_t gated_forward(const GatedArgs &a);
+size_t gated_backward_workspace(const GatedArgs &a, bool want_x);
+cudaError_t gated_backward(const GatedArgs &a);
+cudaError_t gated_status(int *status);
+
 cudaError_t norm_forward(const NormArgs &a);
 cudaError_t norm_backward(const NormGradArgs &a);
 size_t norm_backward_workspace(size_t n, size_t dim);

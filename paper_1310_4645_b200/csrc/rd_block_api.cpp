@@ -44,6 +44,47 @@ int check_rows(int dtype, int sum_dtype, int weight_dtype, size_t n, size_t dim)
     return RD_OK;
 }
 
+constexpr size_t kMostWidth = size_t(1) << 20;
+
+int check_gated(const rd_gated_t *v)
+{
+    if (!v || (!known(v->dtype) && v->dtype != RD_E4M3) || int(v->activation) < RD_SILU || int(v->activation) > RD_RELU) return RD_ERR_INVALID_ARG;
+    if (v->dim < 1 || v->dim > kMostDim || v->width < 1) return RD_ERR_INVALID_ARG;
+    const bool eight = v->dtype == RD_E4M3;
+    if (!eight && v->dtype != RD_BF16 && v->dtype != RD_FP16) return RD_ERR_UNSUPPORTED;
+    if (v->n > kMostRows || v->width > kMostWidth) return RD_ERR_UNSUPPORTED;
+    // output tiles are counted in 32 bits
+    if ((v->n / 128 + 1) * (v->width / 16 + 1) >= size_t(1) << 31 || (v->n / 128 + 1) * (v->dim / 256 + 1) >= size_t(1) << 24) return RD_ERR_UNSUPPORTED;
+    const size_t esize = eight ? 1 : 2;
+    for (const void *w : {v->gate_weight, v->up_weight})
+        if (!aligned(w, esize)) return RD_ERR_INVALID_ARG;
+    if (!stride_ok(v->width, v->gate_weight_stride, v->dim, esize) || !stride_ok(v->width, v->up_weight_stride, v->dim, esize)) return RD_ERR_INVALID_ARG;
+    if (v->n && (!aligned(v->x, esize) || !stride_ok(v->n, v->x_stride, v->dim, esize, true))) return RD_ERR_INVALID_ARG;
+    for (const float *s : {v->x_scale, v->gate_scale, v->up_scale})
+        if (eight ? (v->n && !aligned(s, 4)) : s != nullptr) return RD_ERR_INVALID_ARG;
+    return RD_OK;
+}
+
+GatedArgs gated_args(const rd_gated_t *v)
+{
+    GatedArgs a{};
+    a.x = v->x;
+    a.x_stride = v->x_stride;
+    a.gate_weight = v->gate_weight;
+    a.gate_weight_stride = v->gate_weight_stride;
+    a.up_weight = v->up_weight;
+    a.up_weight_stride = v->up_weight_stride;
+    a.x_scale = v->x_scale;
+    a.gate_scale = v->gate_scale;
+    a.up_scale = v->up_scale;
+    a.n = v->n;
+    a.dim = v->dim;
+    a.width = v->width;
+    a.dtype = int(v->dtype);
+    a.activation = int(v->activation);
+    return a;
+}
+
 }  // namespace
 
 extern "C" {
@@ -134,6 +175,109 @@ int rd_dropout(const void *d_x, size_t x_stride, size_t n, size_t dim, rd_dtype_
     if (!x.ok(true) || !out.ok(false) || spoils(out, x)) return RD_ERR_INVALID_ARG;
     const DropoutArgs a{d_x, d_out, x_stride, out_stride, n, dim, int(dtype), d, static_cast<cudaStream_t>(cuda_stream)};
     return status_of(dropout(a));
+}
+
+int rd_gated_workspace(const rd_gated_t *v, size_t *bytes)
+{
+    if (!bytes) return RD_ERR_INVALID_ARG;
+    if (int rc = check_gated(v)) return rc;
+    *bytes = gated_workspace(gated_args(v));
+    return RD_OK;
+}
+
+int rd_gated(const rd_gated_t *v, void *d_out, size_t out_stride, rd_dtype_t out_dtype, void *d_gate, size_t gate_stride, void *d_up, size_t up_stride, void *d_workspace,
+             size_t workspace_bytes, void *cuda_stream)
+{
+    if (int rc = check_gated(v)) return rc;
+    if (!known(out_dtype) && out_dtype != RD_E4M3) return RD_ERR_INVALID_ARG;
+    const bool eight = v->dtype == RD_E4M3;
+    if (eight ? out_dtype != RD_BF16 && out_dtype != RD_FP16 : out_dtype != v->dtype) return RD_ERR_UNSUPPORTED;
+    if (v->n == 0) return RD_OK;
+    const size_t n = v->n, dim = v->dim, width = v->width, esize = eight ? 1 : 2;
+    const Rows out{d_out, out_stride, n, width, 2}, gate{d_gate, gate_stride, n, width, 2}, up{d_up, up_stride, n, width, 2};
+    if (!out.ok(false) || (gate.p && !gate.ok(false)) || (up.p && !up.ok(false))) return RD_ERR_INVALID_ARG;
+    GatedArgs a = gated_args(v);
+    const size_t need = gated_workspace(a);
+    if (need && !aligned(d_workspace, 256)) return RD_ERR_INVALID_ARG;
+    if (workspace_bytes < need) return RD_ERR_TOO_SMALL;
+    const Span written[] = {out.span(), gate.span(), up.span(), Span(need ? d_workspace : nullptr, need)};
+    const Span read[] = {Span(v->x, n, v->x_stride, dim, esize), Span(v->gate_weight, width, v->gate_weight_stride, dim, esize),
+                         Span(v->up_weight, width, v->up_weight_stride, dim, esize), Span(v->x_scale, n * 4), Span(v->gate_scale, width * 4), Span(v->up_scale, width * 4)};
+    if (overlap(written, read)) return RD_ERR_INVALID_ARG;
+    a.out = d_out;
+    a.out_stride = out_stride;
+    a.out_dtype = int(out_dtype);
+    a.gate = d_gate;
+    a.gate_stride = gate_stride;
+    a.up = d_up;
+    a.up_stride = up_stride;
+    a.workspace = d_workspace;
+    a.stream = static_cast<cudaStream_t>(cuda_stream);
+    return status_of(gated_forward(a));
+}
+
+int rd_gated_grad_workspace(const rd_gated_t *v, int want_x, size_t *bytes)
+{
+    if (!bytes) return RD_ERR_INVALID_ARG;
+    if (int rc = check_gated(v)) return rc;
+    if (v->dtype == RD_E4M3) return RD_ERR_UNSUPPORTED;
+    *bytes = gated_backward_workspace(gated_args(v), want_x != 0);
+    return RD_OK;
+}
+
+int rd_gated_grad(const rd_gated_t *v, const void *d_grad_out, size_t grad_out_stride, const void *d_gate, size_t gate_stride, const void *d_up, size_t up_stride, void *d_grad_x,
+                  size_t grad_x_stride, void *d_grad_gate_weight, size_t grad_gate_weight_stride, void *d_grad_up_weight, size_t grad_up_weight_stride, void *d_workspace,
+                  size_t workspace_bytes, void *cuda_stream)
+{
+    if (int rc = check_gated(v)) return rc;
+    if (v->dtype == RD_E4M3) return RD_ERR_UNSUPPORTED;
+    if (!d_grad_x && !d_grad_gate_weight && !d_grad_up_weight) return RD_ERR_INVALID_ARG;
+    const size_t n = v->n, dim = v->dim, width = v->width;
+    const Rows up_grad{d_grad_out, grad_out_stride, n, width, 2}, gate{d_gate, gate_stride, n, width, 2}, up{d_up, up_stride, n, width, 2};
+    const Rows gx{d_grad_x, grad_x_stride, n, dim, 2}, gg{d_grad_gate_weight, grad_gate_weight_stride, width, dim, 2}, gu{d_grad_up_weight, grad_up_weight_stride, width, dim, 2};
+    for (const Rows *r : {&gx, &gg, &gu})
+        if (r->p && r->n && !r->ok(false)) return RD_ERR_INVALID_ARG;
+    if (n && (!up_grad.ok(true) || !gate.ok(true) || !up.ok(true))) return RD_ERR_INVALID_ARG;
+    GatedArgs a = gated_args(v);
+    const size_t need = gated_backward_workspace(a, d_grad_x != nullptr);
+    if (need && !aligned(d_workspace, 256)) return RD_ERR_INVALID_ARG;
+    if (workspace_bytes < need) return RD_ERR_TOO_SMALL;
+    auto of = [&](const Rows &r) { return Span(n ? r.p : nullptr, r.n, r.stride, r.dim, r.esize); };
+    const Span written[] = {of(gx), gg.span(), gu.span(), Span(need ? d_workspace : nullptr, need)};
+    const Span read[] = {Span(n ? v->x : nullptr, n, v->x_stride, dim, 2), Span(v->gate_weight, width, v->gate_weight_stride, dim, 2),
+                         Span(v->up_weight, width, v->up_weight_stride, dim, 2), of(up_grad), of(gate), of(up)};
+    if (overlap(written, read)) return RD_ERR_INVALID_ARG;
+    const cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
+    if (n == 0) {
+        for (const Rows *r : {&gg, &gu})
+            if (r->p)
+                if (const cudaError_t e = cudaMemset2DAsync(const_cast<void *>(r->p), r->stride * 2, 0, dim * 2, width, stream); e != cudaSuccess) return status_of(e);
+        return RD_OK;
+    }
+    a.grad_out = d_grad_out;
+    a.grad_out_stride = grad_out_stride;
+    a.gate = const_cast<void *>(d_gate);
+    a.gate_stride = gate_stride;
+    a.up = const_cast<void *>(d_up);
+    a.up_stride = up_stride;
+    a.grad_x = d_grad_x;
+    a.grad_x_stride = grad_x_stride;
+    a.grad_gate_weight = d_grad_gate_weight;
+    a.grad_gate_weight_stride = grad_gate_weight_stride;
+    a.grad_up_weight = d_grad_up_weight;
+    a.grad_up_weight_stride = grad_up_weight_stride;
+    a.workspace = d_workspace;
+    a.stream = stream;
+    return status_of(gated_backward(a));
+}
+
+int rd_gated_status(int *device_status)
+{
+    if (!device_status) return RD_ERR_INVALID_ARG;
+    int s = 0;
+    if (gated_status(&s) != cudaSuccess) return RD_ERR_CUDA;
+    *device_status = s ? RD_ERR_TIMEOUT : RD_OK;
+    return RD_OK;
 }
 
 }  // extern "C"

@@ -1,0 +1,879 @@
+// sm_100a kernels of the gated projections of a feed-forward block and of their gradient.
+//
+//   gate = x Wgᵀ,  up = x Wuᵀ,  out = act(gate) up                          (8 bits: each product times its row's and its column's scale)
+//   dgate = dout up act'(gate),  dup = dout act(gate):   dx = dgate Wg + dup Wu,  dWg = dgateᵀ x,  dWu = dupᵀ x
+//
+// act is g σ(k(g)): silu with k = g, the tanh form of gelu (Hendrycks and Gimpel, 2016) with k = 2 sqrt(2/π) (g + 0.044715 g³), as
+// (1 + tanh(k/2)) / 2 = σ(k); or max(g, 0).
+//
+// Forward: one kernel.  A thread block, or a pair of them, computes tiles of 128 (256) rows by w columns of both projections at once: the
+// right operand is w rows of Wg followed by the same w rows of Wu, so that a value's gate and up lie in one lane of tensor memory and
+// their product never leaves the thread.  Of a pair one block brings in Wg's rows, the other Wu's.
+// Gradient: a pass over gate, up and dout leaves dgate and dup side by side, rounded to 16 bits (the operand type of the products), then
+// one launch has both kinds of products, dx over the two widths in one sum, dWg and dWu over the tokens.
+//
+// Operands come in by TMA into a ring of stages of 128 bytes of the summed index; one warp per operand issues the copies, one the
+// products, eight take the results; two sets of accumulators, so that one is read while the next is computed.
+#include "rd_block.h"
+
+#include <cuda.h>
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <cuda_fp8.h>
+
+#include <type_traits>
+
+#include "rd.h"
+#include "rd_launch.h"
+#include "rd_mma.h"
+#include "rd_ptx.h"
+#include "rd_ring.h"
+
+namespace rd {
+
+namespace {
+
+constexpr int kMmaThreads = 128 + 32 * kEpilogueWarps;
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr uint32_t kTileOverhead = 2;     // what a tile costs besides its products, in steps of the summed index
+constexpr size_t kSms = 148;
+
+// ------------------------------------------------------------------------------------------------ activations
+
+__device__ __forceinline__ float reciprocal(float x)
+{
+    float y;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+template <int ACT> __device__ __forceinline__ float sigmoid_of(float g)
+{
+    constexpr float c = 1.5957691216057308f;          // 2 sqrt(2 / pi)
+    const float k = ACT == RD_SILU ? g : c * g * fmaf(0.044715f * g, g, 1.0f);
+    // ex2 and rcp are within 2^-22; results are rounded to 16 bits
+    return reciprocal(1.0f + exp2_fast(-k * kLog2e));
+}
+template <int ACT> __device__ __forceinline__ float act_value(float g)
+{
+    if (ACT == RD_RELU) return g < 0.0f ? 0.0f : g;
+    return g * sigmoid_of<ACT>(g);
+}
+template <int ACT> __device__ __forceinline__ void act_both(float g, float &value, float &slope)
+{
+    if (ACT == RD_RELU) {
+        value = g < 0.0f ? 0.0f : g;
+        slope = g > 0.0f ? 1.0f : 0.0f;
+        return;
+    }
+    constexpr float c = 1.5957691216057308f;
+    const float s = sigmoid_of<ACT>(g), t = s * (1.0f - s), dk = ACT == RD_SILU ? 1.0f : c * fmaf(3.0f * 0.044715f * g, g, 1.0f);
+    value = g * s;
+    slope = t != 0.0f ? fmaf(g * dk, t, s) : s;       // far out t vanishes before g k'(g) overflows
+}
+// Calls f with the activation as a constant.
+template <class F> __device__ __forceinline__ void with_act(int act, F &&f)
+{
+    if (act == RD_SILU) f(std::integral_constant<int, RD_SILU>());
+    else if (act == RD_GELU) f(std::integral_constant<int, RD_GELU>());
+    else f(std::integral_constant<int, RD_RELU>());
+}
+
+__device__ __forceinline__ uint32_t pack2(bool bf16, float lo, float hi) { return bf16 ? pack2<true>(lo, hi) : pack2<false>(lo, hi); }
+__device__ __forceinline__ float2 widen2(bool bf16, uint32_t v)
+{
+    if (bf16) return make_float2(__uint_as_float(v << 16), __uint_as_float(v & 0xffff0000u));
+    return __half22float2(*reinterpret_cast<const __half2 *>(&v));
+}
+
+// ------------------------------------------------------------------------------------------------ the products
+
+struct Out {
+    uint16_t *p;              // null: not wanted
+    size_t stride;
+    int units;                // elements that an access may take: 8, 2 or 1
+};
+// 16 values of a row from column `col` on, of which the row has `left`.
+__device__ __forceinline__ void put16(const Out &o, size_t row, uint32_t col, uint32_t left, const uint32_t (&v)[8])
+{
+    uint16_t *dst = o.p + row * o.stride + col;
+    if (o.units == 8 && left >= 16) {
+        reinterpret_cast<uint4 *>(dst)[0] = make_uint4(v[0], v[1], v[2], v[3]);
+        reinterpret_cast<uint4 *>(dst)[1] = make_uint4(v[4], v[5], v[6], v[7]);
+    } else if (o.units >= 2 && left >= 16) {
+#pragma unroll
+        for (int j = 0; j < 8; j++) reinterpret_cast<uint32_t *>(dst)[j] = v[j];
+    } else {
+#pragma unroll
+        for (int j = 0; j < 16; j++)
+            if (j < left) dst[j] = uint16_t(v[j / 2] >> (j & 1 ? 16 : 0));
+    }
+}
+
+struct alignas(64) GatedParams {
+    CUtensorMap a;            // x, boxes of 128 bytes x a_rows
+    CUtensorMap gate, up;     // weights, boxes of 128 bytes x tile_w
+    uint32_t n, width, steps; // steps: of 128 bytes of the summed index
+    uint32_t tile_w;          // columns of a tile, of each projection
+    uint32_t stages, stage, a_rows;
+    uint32_t group;           // row tiles that go over the width together
+    uint32_t idesc;
+    int act;
+    bool bf16;                // results
+    Out out, kept_gate, kept_up;
+    const float *x_scale, *gate_scale, *up_scale;
+};
+
+struct alignas(64) GradParams {
+    CUtensorMap a_k;          // dgate and dup as the left operand of dx, boxes of 64 x a_rows
+    CUtensorMap a_mn;         // the same as the transposed left operand of dW, 64 x 64 boxes
+    CUtensorMap gate_mn, up_mn;       // weights as the transposed right operand of dx
+    CUtensorMap x_mn;         // x as the transposed right operand of dW
+    CUtensorMap dx_out, gate_out, up_out;     // results, 64 x 32 boxes
+    CUtensorMap dx_parts;     // parts of dx in 32 bits, 32 x 32 x 1 boxes
+    uint32_t n, dim, width;
+    uint32_t half;            // columns of dgate, a multiple of 64: where dup begins
+    uint32_t splits, steps_per_split;         // parts that the sum over both widths is cut into for dx
+    uint32_t a_rows;
+    uint32_t idesc;
+    uint32_t weights;         // which of dWg (1) and dWu (2) are wanted
+    bool want_dx, bf16;
+    bool dx_tma, gate_tma, up_tma;            // results that TMA can address
+    uint16_t *dx, *dgate, *dup;               // the others
+    size_t dx_stride, dgate_stride, dup_stride;
+};
+
+// One unit of work: an output tile and the range of the summed index that goes into it.
+struct Work {
+    int product;              // 0 gate and up, 1 dx, 2 dW
+    uint32_t m0, n0, k0, steps, split;
+    bool second;              // dWu
+};
+
+// Which units a group of thread blocks (one or a pair, number c of g) gets.
+// Forward: bands of p.group row tiles, within a band all row tiles of a column tile one after the other.
+template <int CG> struct GatedPlan {
+    const GatedParams &p;
+    Cursor at;
+    uint32_t g, tiles_m, tiles_n, band = 0;
+    __device__ __forceinline__ explicit GatedPlan(const GatedParams &params) : p(params), g(gridDim.x / CG)
+    {
+        tiles_m = (p.n + kRowsM * CG - 1) / (kRowsM * CG);
+        tiles_n = (p.width + p.tile_w - 1) / p.tile_w;
+        at.set(blockIdx.x / CG, g, min(p.group, tiles_m));
+    }
+    __device__ __forceinline__ bool next(Work &w)
+    {
+        while (at.y >= tiles_n) {                          // on to the next band
+            const uint32_t over = (at.y - tiles_n) * at.wide + at.x;
+            if (++band * p.group >= tiles_m) {
+                band--;                                    // stay at the end
+                return false;
+            }
+            at.set(over, g, min(p.group, tiles_m - band * p.group));
+        }
+        w = Work{0, (band * p.group + at.x) * kRowsM * CG, at.y * p.tile_w, 0, p.steps, 0, false};
+        at.advance();
+        return true;
+    }
+};
+// Gradient: the units of dx first, dealt out in turn; their number need not divide by g, so some groups get one more of them, and that
+// many fewer of dW's tiles, by the number of steps of the summed index.
+template <int CG> struct GradPlan {
+    static constexpr uint32_t kTileM = kRowsM * CG;
+    const GradParams &p;
+    Cursor at;
+    uint32_t c, g, tiles_n, tiles_m, tiles_w, dw_tiles, dw_even, dx_more, left, phase = 0, split = 0, steps_n, steps_w;
+    __device__ __forceinline__ explicit GradPlan(const GradParams &params) : p(params), c(blockIdx.x / CG), g(gridDim.x / CG)
+    {
+        tiles_n = (p.dim + kTileN - 1) / kTileN;
+        tiles_m = (p.n + kTileM - 1) / kTileM;
+        tiles_w = (p.width + kTileM - 1) / kTileM;
+        steps_n = (p.n + kTileK - 1) / kTileK;
+        steps_w = 2 * p.half / kTileK;
+        const uint32_t dx_units = p.want_dx ? tiles_m * tiles_n * p.splits : 0;
+        dw_tiles = __popc(p.weights) * tiles_w * tiles_n;
+        dx_more = dx_units % g;
+        // a unit of dx is worth this many tiles of dW, which the groups without it take first
+        const uint32_t worth = dx_more ? (2 * (p.steps_per_split + kTileOverhead) + steps_n) / (2 * (steps_n + kTileOverhead)) : 0;
+        const uint32_t ahead = worth * (g - dx_more);
+        dw_even = dw_tiles > ahead ? (dw_tiles - ahead + g - 1) / g : 0;      // turns that every group takes part in
+        left = dx_units / g + (c < dx_more);
+        at.set(c, g, tiles_n);
+    }
+    __device__ __forceinline__ bool next(Work &w)
+    {
+        while (left == 0 || (phase != 0 && at.y * tiles_n + at.x >= dw_tiles)) {
+            if (phase == 2) {
+                left = 0;
+                return false;
+            }
+            if (++phase == 1) {
+                left = dw_even;
+                at.set(c, g, tiles_n);
+            } else {
+                left = c < dx_more ? 0 : 0xffffffffu;         // until the tiles run out
+                at.set(dw_even * g + c - dx_more, g - dx_more, tiles_n);
+            }
+        }
+        if (phase == 0) {
+            while (at.y >= tiles_m) {
+                at.y -= tiles_m;
+                split++;
+            }
+            const uint32_t k0 = split * p.steps_per_split;
+            w = Work{1, at.y * kTileM, at.x * kTileN, k0 * kTileK, min(p.steps_per_split, steps_w - k0), split, false};
+        } else {
+            const bool second = p.weights == 2 || at.y >= tiles_w;
+            w = Work{2, (at.y >= tiles_w ? at.y - tiles_w : at.y) * kTileM, at.x * kTileN, 0, steps_n, 0, second};
+        }
+        left--;
+        at.advance();
+        return true;
+    }
+};
+
+template <bool GRADS, int CG> using ShapeOf = Shape<GRADS ? kGrads : kStats, CG>;
+
+template <bool GRADS, bool F8, int CG>
+__global__ void __launch_bounds__(kMmaThreads, 1) rd_gated_mma_kernel(const __grid_constant__ std::conditional_t<GRADS, GradParams, GatedParams> p)
+{
+    using S = ShapeOf<GRADS, CG>;
+    uint32_t stages, stage, stage_a;
+    if constexpr (GRADS) stages = S::stages, stage = S::stage, stage_a = S::stage_a;
+    else stages = p.stages, stage = p.stage, stage_a = p.a_rows * 128;
+    extern __shared__ unsigned char smem_raw[];
+    const uint32_t smem = (smem_addr(smem_raw) + 1023) & ~1023u;
+    const uint32_t boxes = smem + S::ring, bars = boxes + S::boxes;
+    // barriers: full[stage], empty[stage], accumulator full[2], empty[2]; then the tensor memory address
+    const uint32_t full = bars, empty = bars + 8 * kMostStages, acc_full = bars + 16 * kMostStages, acc_empty = acc_full + 16, tmem_slot = acc_empty + 16;
+    const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
+    const uint32_t rank = CG == 2 ? blockIdx.x & 1 : 0;
+
+    if (threadIdx.x == 0) {
+        for (uint32_t s = 0; s < stages; s++) {
+            bar_init(full + 8 * s, 1);
+            bar_init(empty + 8 * s, 1);
+        }
+        for (int b = 0; b < 2; b++) {
+            bar_init(acc_full + 8 * b, 1);
+            bar_init(acc_empty + 8 * b, kEpilogueWarps * CG);
+        }
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 3 && lane == 0) {
+        if constexpr (GRADS) {
+            for (const CUtensorMap *map : {&p.a_k, &p.a_mn, &p.gate_mn, &p.up_mn, &p.x_mn}) asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory");
+        } else {
+            for (const CUtensorMap *map : {&p.a, &p.gate, &p.up}) asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory");
+        }
+    }
+    if (warp == 2) {
+        if (CG == 2) {
+            asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(tmem_slot) : "memory");
+            asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+        } else {
+            asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(tmem_slot) : "memory");
+            asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+        }
+    }
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    pair_sync<CG>();
+    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+    uint32_t tmem;
+    asm volatile("ld.shared.b32 %0, [%1];" : "=r"(tmem) : "r"(tmem_slot));
+
+    pdl_start();
+    std::conditional_t<GRADS, GradPlan<CG>, GatedPlan<CG>> plan(p);
+    bool dead = false;
+    Work w;
+
+    if (warp == 0 || warp == 3) {
+        // one warp brings in the left operand, another the right one; the copies of both thread blocks and both operands count at
+        // the first block's barrier
+        const bool elected = elect_one();
+        Turn turn(stages);
+        const uint32_t lead = leader_bar<CG>(full);
+        while (!dead && plan.next(w)) {
+            for (uint32_t k = 0; k < w.steps; k++, turn.advance()) {
+                const uint32_t a = smem + turn.s * stage, b = a + stage_a, bar = lead + 8 * turn.s;
+                if (!warp_wait(empty + 8 * turn.s, turn.parity ^ 1)) { dead = true; break; }
+                if (!elected) continue;
+                if constexpr (!GRADS) {
+                    const uint32_t x = k * (F8 ? 128 : 64);
+                    if (warp == 0) {
+                        if (rank == 0) bar_expect(full + 8 * turn.s, CG * p.a_rows * 128 + 2 * p.tile_w * 128);
+                        tma_load<CG>(a, &p.a, x, w.m0 + rank * kRowsM, bar);
+                    } else if (CG == 2) {
+                        tma_load<CG>(b, rank ? &p.up : &p.gate, x, w.n0, bar);
+                    } else {
+                        tma_load<CG>(b, &p.gate, x, w.n0, bar);
+                        tma_load<CG>(b + p.tile_w * 128, &p.up, x, w.n0, bar);
+                    }
+                } else {
+                    const uint32_t kk = w.k0 + k * kTileK, m0 = w.m0 + rank * kRowsM, n0 = w.n0 + rank * S::rows_n;
+                    if (warp == 0) {
+                        if (rank == 0) bar_expect(full + 8 * turn.s, CG * ((w.product == 2 ? S::stage_a : p.a_rows * 128) + S::stage_b));
+                        if (w.product == 2) {
+#pragma unroll
+                            for (int j = 0; j < kRowsM / 64; j++) tma_load<CG>(a + j * 8192, &p.a_mn, (w.second ? p.half : 0) + m0 + 64 * j, kk, bar);
+                        } else {
+                            tma_load<CG>(a, &p.a_k, kk, m0, bar);
+                        }
+                    } else {
+                        const CUtensorMap *map = w.product == 2 ? &p.x_mn : kk < p.half ? &p.gate_mn : &p.up_mn;
+                        const uint32_t y = w.product == 1 && kk >= p.half ? kk - p.half : kk;
+#pragma unroll
+                        for (int j = 0; j < S::rows_n / 64; j++) tma_load<CG>(b + j * 8192, map, n0 + 64 * j, y, bar);
+                    }
+                }
+            }
+        }
+        // the last stages' arrivals have to land while the barriers still exist
+        for (uint32_t s = 0; s < stages && !dead; s++, turn.advance()) dead = !warp_wait(empty + 8 * turn.s, turn.parity ^ 1);
+        if (dead) drain();
+    } else if (warp == 1) {
+        if (rank == 0) {
+            const bool elected = elect_one();
+            Turn turn(stages);
+            uint32_t tile = 0;
+            while (!dead && plan.next(w)) {
+                const uint32_t buf = tile & 1;
+                if (!warp_wait(acc_empty + 8 * buf, (tile / 2 & 1) ^ 1)) { dead = true; break; }
+                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                const bool ta = w.product == 2, tb = w.product != 0;
+                const uint32_t idesc = p.idesc | (ta ? 1u << 15 : 0u) | (tb ? 1u << 16 : 0u);
+                const uint32_t step_a = ta ? 2048 >> 4 : 32 >> 4, step_b = tb ? 2048 >> 4 : 32 >> 4;
+                const uint32_t acc = tmem + buf * kTileN;
+                for (uint32_t k = 0; k < w.steps; k++, turn.advance()) {
+                    const uint32_t a = smem + turn.s * stage, b = a + stage_a;
+                    if (!warp_wait(full + 8 * turn.s, turn.parity)) { dead = true; break; }
+                    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                    const uint64_t da = operand(a, ta), db = operand(b, tb);
+                    if (elected) {
+                        // 32 bytes of the summed index at a time, whatever the type
+#pragma unroll
+                        for (int j = 0; j < 4; j++) mma<CG, F8>(acc, da + j * step_a, db + j * step_b, idesc, k != 0 || j != 0);
+                        mma_commit<CG>(empty + 8 * turn.s);
+                    }
+                }
+                if (!dead && elected) mma_commit<CG>(acc_full + 8 * buf);
+                tile++;
+            }
+            if (dead) drain();
+        }
+    } else if (warp >= 4) {
+        const int quarter = warp & 3, half = (warp - 4) >> 2;        // rows 32 * quarter.. of the tile; every other 16 columns, or half of them
+        uint32_t tile = 0;
+        while (plan.next(w)) {
+            const uint32_t row0 = w.m0 + rank * kRowsM + 32 * quarter, row = row0 + lane, buf = tile & 1;
+            if (!warp_wait(acc_full + 8 * buf, tile / 2 & 1)) break;
+            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+            const uint32_t acc = tmem + buf * kTileN + (uint32_t(32 * quarter) << 16);
+            // the accumulators are free for the next tile but one as soon as their last columns are in registers
+            auto release = [&]() {
+                asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+                __syncwarp();
+                if (lane == 0) bar_arrive_leader<CG>(acc_empty + 8 * buf);
+            };
+            if constexpr (!GRADS) {
+                const bool live = row < p.n;
+                const float x_scale = F8 && live ? p.x_scale[row] : 1.0f;
+                const uint32_t chunks = p.tile_w / 16;
+                if (uint32_t(half) >= chunks) release();
+                for (uint32_t c = half; c < chunks; c += 2) {
+                    uint32_t g[16], u[16];
+                    tmem_load(acc + 16 * c, g);
+                    tmem_load(acc + p.tile_w + 16 * c, u);
+                    tmem_wait(g);
+                    tmem_wait(u);
+                    if (c + 2 >= chunks) release();
+                    const uint32_t col = w.n0 + 16 * c;
+                    if (col >= p.width) continue;
+                    const uint32_t left = p.width - col;
+                    if (F8) {
+#pragma unroll
+                        for (int j = 0; j < 16; j++) {
+                            const uint32_t at = col + (j < left ? j : 0);
+                            g[j] = __float_as_uint(__uint_as_float(g[j]) * (x_scale * __ldg(p.gate_scale + at)));
+                            u[j] = __float_as_uint(__uint_as_float(u[j]) * (x_scale * __ldg(p.up_scale + at)));
+                        }
+                    }
+                    if (live) {
+                        uint32_t o[8];
+                        with_act(p.act, [&](auto ACT) {
+#pragma unroll
+                            for (int j = 0; j < 8; j++)
+                                o[j] = pack2(p.bf16, act_value<decltype(ACT)::value>(__uint_as_float(g[2 * j])) * __uint_as_float(u[2 * j]),
+                                             act_value<decltype(ACT)::value>(__uint_as_float(g[2 * j + 1])) * __uint_as_float(u[2 * j + 1]));
+                        });
+                        put16(p.out, row, col, left, o);
+                        if (p.kept_gate.p) {
+#pragma unroll
+                            for (int j = 0; j < 8; j++) o[j] = pack2(p.bf16, __uint_as_float(g[2 * j]), __uint_as_float(g[2 * j + 1]));
+                            put16(p.kept_gate, row, col, left, o);
+                        }
+                        if (p.kept_up.p) {
+#pragma unroll
+                            for (int j = 0; j < 8; j++) o[j] = pack2(p.bf16, __uint_as_float(u[2 * j]), __uint_as_float(u[2 * j + 1]));
+                            put16(p.kept_up, row, col, left, o);
+                        }
+                    }
+                    __syncwarp();                // the next load of the accumulators is the whole warp's
+                }
+            } else {
+                const uint32_t box = boxes + (warp - 4) * kBox, col0 = w.n0 + 128 * half;
+                const bool parts = w.product == 1 && p.splits > 1;
+                const CUtensorMap *map = w.product == 1 ? &p.dx_out : w.second ? &p.up_out : &p.gate_out;
+                const bool tma = w.product == 1 ? p.dx_tma : w.second ? p.up_tma : p.gate_tma;
+                const uint32_t rows = w.product == 1 ? p.n : p.width;
+                // 32 columns are on their way while the 32 before them are worked on
+                uint32_t v[2][32];
+                tmem_load(acc + 128 * half, v[0]);
+#pragma unroll
+                for (int c = 0; c < 4; c++) {
+                    uint32_t(&x)[32] = v[c & 1];
+                    tmem_wait(x);
+                    if (c < 3) tmem_load(acc + 128 * half + 32 * (c + 1), v[(c + 1) & 1]);
+                    else release();
+                    const uint32_t col = col0 + 32 * c;
+                    if (parts) {
+                        box_wait(lane, false);
+#pragma unroll
+                        for (int q = 0; q < 8; q++) box_put(box, lane, q, x[4 * q], x[4 * q + 1], x[4 * q + 2], x[4 * q + 3]);
+                        if (box_full(lane, true) && col < p.dim && row0 < rows) {
+                            tma_store(&p.dx_parts, box, col, row0, w.split);
+                            box_sent();
+                        }
+                        continue;
+                    }
+                    // a box of 64 columns
+                    box_wait(lane, c & 1);
+#pragma unroll
+                    for (int q = 0; q < 4; q++) {
+                        uint32_t o[4];
+#pragma unroll
+                        for (int j = 0; j < 4; j++) o[j] = pack2(p.bf16, __uint_as_float(x[8 * q + 2 * j]), __uint_as_float(x[8 * q + 2 * j + 1]));
+                        box_put(box, lane, 4 * (c & 1) + q, o[0], o[1], o[2], o[3]);
+                    }
+                    if (tma) {
+                        if (box_full(lane, c & 1) && col - 32 < p.dim && row0 < rows) {
+                            tma_store(map, box, col - 32, row0);
+                            box_sent();
+                        }
+                    } else if (c & 1) {
+                        // rows that TMA cannot address: the warp writes them one after the other, two elements a lane
+                        __syncwarp();
+                        const size_t stride = w.product == 1 ? p.dx_stride : w.second ? p.dup_stride : p.dgate_stride;
+                        uint16_t *dst = (w.product == 1 ? p.dx : w.second ? p.dup : p.dgate) + size_t(row0) * stride + (col - 32);
+                        const uint32_t here = row0 < rows ? min(32u, rows - row0) : 0;
+#pragma unroll 4
+                        for (uint32_t r = 0; r < here; r++) {
+#pragma unroll
+                            for (int i = 0; i < 2; i++) {
+                                const uint32_t j = lane + 32 * i;
+                                uint16_t y;
+                                asm volatile("ld.shared.u16 %0, [%1];" : "=h"(y) : "r"(box + r * 128 + (((j / 8) ^ (r & 7)) * 16) + j % 8 * 2) : "memory");
+                                if (col - 32 + j < p.dim) dst[size_t(r) * stride + j] = y;
+                            }
+                        }
+                        __syncwarp();
+                    }
+                }
+            }
+            tile++;
+        }
+        if (GRADS && lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
+    }
+    __syncwarp();
+    pair_sync<CG>();                             // neither block of a pair leaves while the other may still signal it
+    if (warp == 2) {
+        if (CG == 2) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
+        else asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
+    }
+}
+
+// ------------------------------------------------------------------------------------------------ beside the products
+
+// Copies a matrix whose rows TMA cannot address (unaligned base or stride) to rows that it can, a warp a row.
+template <typename E> __global__ void __launch_bounds__(256) rd_gated_align_kernel(E *dst, size_t dst_stride, const E *src, size_t src_stride, size_t rows, uint32_t dim)
+{
+    pdl_start();
+    for (size_t r = size_t(blockIdx.x) * 8 + (threadIdx.x >> 5); r < rows; r += size_t(gridDim.x) * 8) {
+#pragma unroll 4
+        for (uint32_t j = threadIdx.x & 31; j < dim; j += 32) dst[r * dst_stride + j] = src[r * src_stride + j];
+    }
+}
+
+struct SlopeParams {
+    const uint16_t *gate, *up, *grad_out;
+    size_t gate_stride, up_stride, grad_out_stride;
+    uint16_t *both;           // rows of 2 * half values: dgate, zeros up to half, dup, zeros
+    size_t n;
+    uint32_t width, half, across;
+    int act;
+    bool bf16;
+};
+
+// dgate and dup, V values a thread at a time.
+template <int V> __global__ void __launch_bounds__(256) rd_gated_slope_kernel(const __grid_constant__ SlopeParams p)
+{
+    pdl_start();
+    const uint32_t x = threadIdx.x % p.across, y = threadIdx.x / p.across, down = 256 / p.across;
+    const uint32_t col = (blockIdx.y * p.across + x) * V;
+    if (col >= p.half) return;
+    for (size_t row = size_t(blockIdx.x) * down + y; row < p.n; row += size_t(gridDim.x) * down) {
+        uint16_t *dst = p.both + row * 2 * p.half + col;
+        if constexpr (V == 8) {
+            uint32_t a[4] = {}, b[4] = {};
+            if (col < p.width) {
+                const uint4 g = *reinterpret_cast<const uint4 *>(p.gate + row * p.gate_stride + col), u = *reinterpret_cast<const uint4 *>(p.up + row * p.up_stride + col),
+                            d = *reinterpret_cast<const uint4 *>(p.grad_out + row * p.grad_out_stride + col);
+                const uint32_t gs[4] = {g.x, g.y, g.z, g.w}, us[4] = {u.x, u.y, u.z, u.w}, ds[4] = {d.x, d.y, d.z, d.w};
+                with_act(p.act, [&](auto ACT) {
+#pragma unroll
+                    for (int i = 0; i < 4; i++) {
+                        const float2 gi = widen2(p.bf16, gs[i]), ui = widen2(p.bf16, us[i]), di = widen2(p.bf16, ds[i]);
+                        float v0, s0, v1, s1;
+                        act_both<decltype(ACT)::value>(gi.x, v0, s0);
+                        act_both<decltype(ACT)::value>(gi.y, v1, s1);
+                        a[i] = pack2(p.bf16, di.x * ui.x * s0, di.y * ui.y * s1);
+                        b[i] = pack2(p.bf16, di.x * v0, di.y * v1);
+                    }
+                });
+            }
+            *reinterpret_cast<uint4 *>(dst) = make_uint4(a[0], a[1], a[2], a[3]);
+            *reinterpret_cast<uint4 *>(dst + p.half) = make_uint4(b[0], b[1], b[2], b[3]);
+        } else {
+            uint32_t a = 0, b = 0;
+            if (col < p.width) {
+                const float g = widen2(p.bf16, p.gate[row * p.gate_stride + col]).x, u = widen2(p.bf16, p.up[row * p.up_stride + col]).x,
+                            d = widen2(p.bf16, p.grad_out[row * p.grad_out_stride + col]).x;
+                with_act(p.act, [&](auto ACT) {
+                    float v, s;
+                    act_both<decltype(ACT)::value>(g, v, s);
+                    a = pack2(p.bf16, d * u * s, 0.0f);
+                    b = pack2(p.bf16, d * v, 0.0f);
+                });
+            }
+            dst[0] = uint16_t(a);
+            dst[p.half] = uint16_t(b);
+        }
+    }
+}
+
+// Adds the parts of dx in order and rounds.
+__global__ void __launch_bounds__(256) rd_gated_finish_kernel(uint16_t *out, size_t out_stride, const float *parts, size_t stride, size_t n, uint32_t dim, uint32_t splits, bool bf16, bool wide)
+{
+    pdl_start();
+    const uint32_t j = blockIdx.y * 1024 + threadIdx.x * 4;
+    if (j >= dim) return;
+    for (size_t row = blockIdx.x; row < n; row += gridDim.x) {
+        const float *src = parts + row * stride + j;
+        float4 sum = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll 4
+        for (uint32_t s = 0; s < splits; s++) {
+            const float4 x = *reinterpret_cast<const float4 *>(src + s * n * stride);
+            sum.x += x.x;
+            sum.y += x.y;
+            sum.z += x.z;
+            sum.w += x.w;
+        }
+        const uint32_t lo = pack2(bf16, sum.x, sum.y), hi = pack2(bf16, sum.z, sum.w);
+        uint16_t *dst = out + row * out_stride + j;
+        if (wide && j + 4 <= dim) {
+            *reinterpret_cast<uint2 *>(dst) = make_uint2(lo, hi);
+        } else {
+            const uint16_t v[4] = {uint16_t(lo), uint16_t(lo >> 16), uint16_t(hi), uint16_t(hi >> 16)};
+#pragma unroll
+            for (int k = 0; k < 4; k++)
+                if (j + k < dim) dst[k] = v[k];
+        }
+    }
+}
+
+// ------------------------------------------------------------------------------------------------ host
+
+size_t bytes_of(int dtype) { return dtype == RD_E4M3 ? 1 : 2; }
+
+// Bytes between rows that TMA can address: a multiple of 16, as the base.
+bool tma_rows(const void *p, size_t stride, size_t esize) { return reinterpret_cast<uintptr_t>(p) % 16 == 0 && stride * esize % 16 == 0; }
+// An input whose rows are all the same one has no stride that TMA takes, either.
+bool tma_input(const void *p, size_t stride, size_t esize) { return tma_rows(p, stride, esize) && stride > 0; }
+
+// Whether pairs of thread blocks compute tiles of twice the rows: as soon as there is more than one tile of 128.
+int pair_or_single(size_t n) { return n > kRowsM ? 2 : 1; }
+uint32_t rows_in(size_t n) { return uint32_t(n < kRowsM ? round_up(n, 8) : kRowsM); }
+
+struct Layout {
+    void *x, *gate_weight, *up_weight;        // aligned copies, null where none is needed
+    size_t copy_stride;                       // in elements
+    uint16_t *both;
+    size_t half;
+    float *parts;
+    size_t splits, steps_per_split, part_stride, bytes;
+};
+
+// Parts that the sum over both widths is cut into for dx.  More parts fill the groups of thread blocks more evenly, but each is a
+// matrix of its own that is written and read once more; times in steps of the summed index.
+size_t dx_splits(const GatedArgs &a, size_t half)
+{
+    const size_t cg = pair_or_single(a.n), tile_m = kRowsM * cg, groups = kSms / cg, steps = 2 * half / kTileK;
+    const size_t tiles_n = (a.dim + kTileN - 1) / kTileN, tiles = (a.n + tile_m - 1) / tile_m * tiles_n;
+    const double step_bytes = 0.28e-6 * 6.5e12, finish = 9;
+    const double dw = double(2 * ((a.width + tile_m - 1) / tile_m) * tiles_n) * double((a.n + kTileK - 1) / kTileK + kTileOverhead);
+    size_t best = 1;
+    double best_time = 0;
+    for (size_t s = 1; s <= 64 && s * 4 <= steps + 3; s++) {
+        const size_t units = tiles * s;
+        const double unit = double((steps + s - 1) / s + kTileOverhead), even = (double(units) * unit + dw) / double(groups);
+        const double longest = double((units + groups - 1) / groups) * unit;
+        const double time = (even > longest ? even : longest) + (s == 1 ? 0 : double(s) * double(a.n * a.dim) * 8 / step_bytes + finish);
+        if (s == 1 || time < best_time) best = s, best_time = time;
+    }
+    return best;
+}
+
+Layout lay_out(const GatedArgs &a, bool gradient, bool want_x)
+{
+    Layout l{};
+    if (a.n == 0) return l;
+    Part w(a.workspace);
+    const size_t esize = bytes_of(a.dtype);
+    l.copy_stride = round_up(a.dim, 128 / esize);
+    auto copy = [&](const void *p, size_t stride, size_t rows) -> void * { return tma_input(p, stride, esize) ? nullptr : w.take<char>(rows * l.copy_stride * esize); };
+    l.x = copy(a.x, a.x_stride, a.n);
+    l.gate_weight = copy(a.gate_weight, a.gate_weight_stride, a.width);
+    l.up_weight = copy(a.up_weight, a.up_weight_stride, a.width);
+    if (gradient) {
+        l.half = round_up(a.width, 64);
+        l.both = w.take<uint16_t>(a.n * 2 * l.half);
+        const size_t steps = 2 * l.half / kTileK, splits = want_x ? dx_splits(a, l.half) : 1;
+        l.steps_per_split = (steps + splits - 1) / splits;
+        l.splits = (steps + l.steps_per_split - 1) / l.steps_per_split;
+        l.part_stride = round_up(a.dim, 32);
+        if (l.splits > 1) l.parts = w.take<float>(l.splits * a.n * l.part_stride);
+    }
+    l.bytes = w.at;
+    return l;
+}
+
+// An aligned operand: the caller's, or its copy, made by this call.
+struct Operand {
+    const void *p;
+    size_t stride;
+};
+cudaError_t align(Operand *o, const void *p, size_t stride, size_t rows, size_t dim, void *copy, size_t copy_stride, size_t esize, cudaStream_t stream)
+{
+    *o = Operand{p, stride};
+    if (!copy) return cudaSuccess;
+    *o = Operand{copy, copy_stride};
+    const unsigned blocks = unsigned(rows < 8 * 1184 ? (rows + 7) / 8 : 1184);
+    if (esize == 1) return launch(rd_gated_align_kernel<uint8_t>, blocks, 256, stream, static_cast<uint8_t *>(copy), copy_stride, static_cast<const uint8_t *>(p), stride, rows, uint32_t(dim));
+    return launch(rd_gated_align_kernel<uint16_t>, blocks, 256, stream, static_cast<uint16_t *>(copy), copy_stride, static_cast<const uint16_t *>(p), stride, rows, uint32_t(dim));
+}
+struct Operands {
+    Operand x, gate, up;
+};
+cudaError_t align_all(Operands *o, const GatedArgs &a, const Layout &l)
+{
+    const size_t esize = bytes_of(a.dtype);
+    cudaError_t e = align(&o->x, a.x, a.x_stride, a.n, a.dim, l.x, l.copy_stride, esize, a.stream);
+    if (e == cudaSuccess) e = align(&o->gate, a.gate_weight, a.gate_weight_stride, a.width, a.dim, l.gate_weight, l.copy_stride, esize, a.stream);
+    if (e == cudaSuccess) e = align(&o->up, a.up_weight, a.up_weight_stride, a.width, a.dim, l.up_weight, l.copy_stride, esize, a.stream);
+    return e;
+}
+
+// A matrix of 8-bit values, read in boxes of 128 values x box_rows rows.
+bool encode8(CUtensorMap *map, const void *base, size_t inner, size_t rows, size_t stride, uint32_t box_rows)
+{
+    const EncodeTiled f = encoder();
+    if (!f) return false;
+    const cuuint64_t dims[2] = {inner, rows}, strides[1] = {stride};
+    const cuuint32_t box[2] = {128, box_rows}, one[2] = {1, 1};
+    return f(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void *>(base), dims, strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+             CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+bool encode_rows(CUtensorMap *map, int dtype, const Operand &o, size_t inner, size_t rows, uint32_t box_rows)
+{
+    return dtype == RD_E4M3 ? encode8(map, o.p, inner, rows, o.stride, box_rows) : encode(map, dtype == RD_BF16, o.p, inner, rows, o.stride, box_rows);
+}
+
+// fp32 accumulators; operand types e4m3 (0), fp16 (0) or bf16 (1); columns and rows of a tile
+uint32_t descriptor(int dtype, uint32_t columns, uint32_t rows) { return 1u << 4 | (dtype == RD_BF16 ? 1u << 7 | 1u << 10 : 0u) | columns / 8 << 17 | rows / 16 << 24; }
+
+Out out_of(void *p, size_t stride)
+{
+    const uintptr_t at = reinterpret_cast<uintptr_t>(p);
+    return Out{static_cast<uint16_t *>(p), stride, at % 16 == 0 && stride % 8 == 0 ? 8 : at % 4 == 0 && stride % 2 == 0 ? 2 : 1};
+}
+
+// Row tiles that go over the width together: their rows of x (tile x dim) should stay in L2 beside the weights'.
+uint32_t row_group(size_t row_bytes, size_t tile_m)
+{
+    const size_t g = (size_t(32) << 20) / (tile_m * row_bytes);
+    return uint32_t(g < 1 ? 1 : g > 64 ? 64 : g);
+}
+
+// Columns of a tile (of each projection): what takes the fewest turns of the groups of thread blocks, by the columns of a turn.  Pairs
+// compute narrow tiles at the rate that the left operand comes out of shared memory, as if they had 48 columns.
+uint32_t tile_columns(size_t tiles_m, size_t width, size_t groups, bool pairs)
+{
+    size_t best = 128, best_cost = 0;
+    for (size_t w = 128; w >= 16; w -= 16) {
+        const size_t turns = (tiles_m * ((width + w - 1) / w) + groups - 1) / groups, cost = turns * ((pairs && w < 48 ? 48 : w) + 8);
+        if (w == 128 || cost < best_cost) best = w, best_cost = cost;
+    }
+    return uint32_t(best);
+}
+
+template <bool GRADS, bool F8, int CG, typename P> cudaError_t launch_mma(const P &p, int device, size_t most_units, cudaStream_t stream)
+{
+    constexpr uint32_t smem = ShapeOf<GRADS, CG>::smem;
+    static std::atomic<bool> ready[64];
+    if (device >= 64 || !ready[device].load(std::memory_order_acquire)) {
+        const cudaError_t e = cudaFuncSetAttribute(rd_gated_mma_kernel<GRADS, F8, CG>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+        if (e != cudaSuccess) return e;
+        if (device < 64) ready[device].store(true, std::memory_order_release);
+    }
+    const size_t groups = size_t(sm_count_of(device)) / CG;
+    cudaLaunchConfig_t c{};
+    c.gridDim = dim3(unsigned((most_units < groups ? most_units : groups) * CG));
+    c.blockDim = dim3(kMmaThreads);
+    c.dynamicSmemBytes = smem;
+    c.stream = stream;
+    cudaLaunchAttribute attrs[2] = {pdl_attribute()};
+    attrs[1].id = cudaLaunchAttributeClusterDimension;
+    attrs[1].val.clusterDim.x = CG;
+    attrs[1].val.clusterDim.y = attrs[1].val.clusterDim.z = 1;
+    c.attrs = attrs;
+    c.numAttrs = 2;
+    return cudaLaunchKernelEx(&c, rd_gated_mma_kernel<GRADS, F8, CG>, p);
+}
+
+}  // namespace
+
+size_t gated_workspace(const GatedArgs &a) { return lay_out(a, false, false).bytes; }
+
+cudaError_t gated_forward(const GatedArgs &a)
+{
+    int device = 0;
+    cudaError_t e = cudaGetDevice(&device);
+    if (e != cudaSuccess) return e;
+    const int cg = pair_or_single(a.n);
+    const size_t tile_m = size_t(kRowsM) * cg, tiles_m = (a.n + tile_m - 1) / tile_m, esize = bytes_of(a.dtype);
+    const Layout l = lay_out(a, false, false);
+    Operands o;
+    e = align_all(&o, a, l);
+    if (e != cudaSuccess) return e;
+    GatedParams p{};
+    p.n = uint32_t(a.n);
+    p.width = uint32_t(a.width);
+    p.steps = uint32_t((a.dim * esize + 127) / 128);
+    p.tile_w = tile_columns(tiles_m, a.width, kSms / cg, cg == 2);
+    p.a_rows = rows_in(a.n);
+    const Ring r = ring_of(cg == 2 ? ShapeOf<false, 2>::ring : ShapeOf<false, 1>::ring, p.a_rows, 2 * p.tile_w / uint32_t(cg));
+    p.stage = r.stage;
+    p.stages = r.stages;
+    p.group = row_group(a.dim * esize, tile_m);
+    p.idesc = descriptor(a.dtype, 2 * p.tile_w, uint32_t(tile_m));
+    p.act = a.activation;
+    p.bf16 = a.out_dtype == RD_BF16;
+    p.out = out_of(a.out, a.out_stride);
+    p.kept_gate = out_of(a.gate, a.gate_stride);
+    p.kept_up = out_of(a.up, a.up_stride);
+    p.x_scale = a.x_scale;
+    p.gate_scale = a.gate_scale;
+    p.up_scale = a.up_scale;
+    if (!encode_rows(&p.a, a.dtype, o.x, a.dim, a.n, p.a_rows) || !encode_rows(&p.gate, a.dtype, o.gate, a.dim, a.width, p.tile_w) ||
+        !encode_rows(&p.up, a.dtype, o.up, a.dim, a.width, p.tile_w))
+        return cudaErrorInvalidValue;
+    const size_t units = tiles_m * ((a.width + p.tile_w - 1) / p.tile_w);
+    if (a.dtype == RD_E4M3) return cg == 2 ? launch_mma<false, true, 2>(p, device, units, a.stream) : launch_mma<false, true, 1>(p, device, units, a.stream);
+    return cg == 2 ? launch_mma<false, false, 2>(p, device, units, a.stream) : launch_mma<false, false, 1>(p, device, units, a.stream);
+}
+
+size_t gated_backward_workspace(const GatedArgs &a, bool want_x) { return lay_out(a, true, want_x).bytes; }
+
+cudaError_t gated_backward(const GatedArgs &a)
+{
+    int device = 0;
+    cudaError_t e = cudaGetDevice(&device);
+    if (e != cudaSuccess) return e;
+    const int cg = pair_or_single(a.n);
+    const size_t tile_m = size_t(kRowsM) * cg, tiles_m = (a.n + tile_m - 1) / tile_m, tiles_n = (a.dim + kTileN - 1) / kTileN;
+    const bool want_x = a.grad_x != nullptr, bf16 = a.dtype == RD_BF16;
+    const Layout l = lay_out(a, true, want_x);
+    Operands o;
+    e = align_all(&o, a, l);
+    if (e != cudaSuccess) return e;
+
+    SlopeParams s{};
+    s.gate = static_cast<const uint16_t *>(a.gate);
+    s.up = static_cast<const uint16_t *>(a.up);
+    s.grad_out = static_cast<const uint16_t *>(a.grad_out);
+    s.gate_stride = a.gate_stride;
+    s.up_stride = a.up_stride;
+    s.grad_out_stride = a.grad_out_stride;
+    s.both = l.both;
+    s.n = a.n;
+    s.width = uint32_t(a.width);
+    s.half = uint32_t(l.half);
+    s.act = a.activation;
+    s.bf16 = bf16;
+    const bool wide = a.width % 8 == 0 && tma_rows(a.gate, a.gate_stride, 2) && tma_rows(a.up, a.up_stride, 2) && tma_rows(a.grad_out, a.grad_out_stride, 2);
+    const uint32_t units = s.half / (wide ? 8 : 1);
+    s.across = 256;
+    while (s.across > 8 && s.across >= 2 * units) s.across /= 2;
+    const size_t down = 256 / s.across, tall = (a.n + down - 1) / down;
+    const dim3 grid(unsigned(tall < 65536 ? tall : 65536), (units + s.across - 1) / s.across);
+    e = wide ? launch(rd_gated_slope_kernel<8>, grid, 256, a.stream, s) : launch(rd_gated_slope_kernel<1>, grid, 256, a.stream, s);
+    if (e != cudaSuccess) return e;
+
+    GradParams p{};
+    p.n = uint32_t(a.n);
+    p.dim = uint32_t(a.dim);
+    p.width = uint32_t(a.width);
+    p.half = uint32_t(l.half);
+    p.splits = uint32_t(l.splits);
+    p.steps_per_split = uint32_t(l.steps_per_split);
+    p.a_rows = rows_in(a.n);
+    p.idesc = descriptor(a.dtype, kTileN, uint32_t(tile_m));
+    p.weights = (a.grad_gate_weight ? 1u : 0u) | (a.grad_up_weight ? 2u : 0u);
+    p.want_dx = want_x;
+    p.bf16 = bf16;
+    p.dx = static_cast<uint16_t *>(a.grad_x);
+    p.dgate = static_cast<uint16_t *>(a.grad_gate_weight);
+    p.dup = static_cast<uint16_t *>(a.grad_up_weight);
+    p.dx_stride = a.grad_x_stride;
+    p.dgate_stride = a.grad_gate_weight_stride;
+    p.dup_stride = a.grad_up_weight_stride;
+    p.dx_tma = want_x && tma_rows(a.grad_x, a.grad_x_stride, 2);
+    p.gate_tma = a.grad_gate_weight && tma_rows(a.grad_gate_weight, a.grad_gate_weight_stride, 2);
+    p.up_tma = a.grad_up_weight && tma_rows(a.grad_up_weight, a.grad_up_weight_stride, 2);
+    if (!encode(&p.a_k, bf16, l.both, 2 * l.half, a.n, 2 * l.half, p.a_rows) || !encode(&p.a_mn, bf16, l.both, 2 * l.half, a.n, 2 * l.half, 64) ||
+        !encode(&p.gate_mn, bf16, o.gate.p, a.dim, a.width, o.gate.stride, 64) || !encode(&p.up_mn, bf16, o.up.p, a.dim, a.width, o.up.stride, 64) ||
+        !encode(&p.x_mn, bf16, o.x.p, a.dim, a.n, o.x.stride, 64) || (p.dx_tma && !encode(&p.dx_out, bf16, a.grad_x, a.dim, a.n, a.grad_x_stride, 32)) ||
+        (p.gate_tma && !encode(&p.gate_out, bf16, a.grad_gate_weight, a.dim, a.width, a.grad_gate_weight_stride, 32)) ||
+        (p.up_tma && !encode(&p.up_out, bf16, a.grad_up_weight, a.dim, a.width, a.grad_up_weight_stride, 32)) ||
+        (l.splits > 1 && !encode_dh(&p.dx_parts, l.parts, l.part_stride, a.n, l.splits)))
+        return cudaErrorInvalidValue;
+    const size_t work = (want_x ? tiles_m * tiles_n * l.splits : 0) + __builtin_popcount(p.weights) * ((a.width + tile_m - 1) / tile_m) * tiles_n;
+    e = cg == 2 ? launch_mma<true, false, 2>(p, device, work, a.stream) : launch_mma<true, false, 1>(p, device, work, a.stream);
+    if (e != cudaSuccess || l.splits == 1) return e;
+    const bool wide_x = reinterpret_cast<uintptr_t>(a.grad_x) % 8 == 0 && a.grad_x_stride % 4 == 0;
+    const dim3 rows(unsigned(a.n < 65536 ? a.n : 65536), unsigned((a.dim + 1023) / 1024));
+    return launch(rd_gated_finish_kernel, rows, 256, a.stream, p.dx, a.grad_x_stride, static_cast<const float *>(l.parts), l.part_stride, a.n, uint32_t(a.dim), p.splits, bf16, wide_x);
+}
+
+cudaError_t gated_status(int *status)
+{
+    cudaError_t e = cudaDeviceSynchronize();
+    if (e != cudaSuccess) return e;
+    e = cudaMemcpyFromSymbol(status, g_wait_status, sizeof(int));
+    if (e != cudaSuccess) return e;
+    const int zero = 0;
+    if (*status) e = cudaMemcpyToSymbol(g_wait_status, &zero, sizeof(int));
+    return e;
+}
+
+}  // namespace rd

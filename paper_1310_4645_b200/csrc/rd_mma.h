@@ -76,21 +76,20 @@ __device__ __forceinline__ uint64_t operand(uint32_t addr, bool transposed)
     return uint64_t(addr >> 4) | uint64_t(transposed ? 8192 >> 4 : 1) << 16 | uint64_t(1024 >> 4) << 32 | uint64_t(1) << 46 | uint64_t(2) << 61;
 }
 
-template <int CG> __device__ __forceinline__ void mma(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool add)
+// F8: e4m3 operands, 32 summed indices an instruction; else 16-bit ones, 16.
+template <int CG, bool F8 = false> __device__ __forceinline__ void mma(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool add)
 {
-    if (CG == 2)
-        asm volatile(
-            "{\n\t.reg .pred p;\n\t"
-            "setp.ne.b32 p, %4, 0;\n\t"
-            "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d),
-            "l"(a), "l"(b), "r"(idesc), "r"(uint32_t(add))
-            : "memory");
-    else asm volatile(
-        "{\n\t.reg .pred p;\n\t"
-        "setp.ne.b32 p, %4, 0;\n\t"
-        "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d),
-        "l"(a), "l"(b), "r"(idesc), "r"(uint32_t(add))
-        : "memory");
+#define RD_MMA(GROUP, KIND)                                                                             \
+    asm volatile(                                                                                       \
+        "{\n\t.reg .pred p;\n\t"                                                                        \
+        "setp.ne.b32 p, %4, 0;\n\t"                                                                     \
+        "tcgen05.mma.cta_group::" GROUP ".kind::" KIND " [%0], %1, %2, %3, p;\n\t}" ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(uint32_t(add)) \
+        : "memory")
+    if constexpr (CG == 2 && F8) RD_MMA("2", "f8f6f4");
+    else if constexpr (CG == 2) RD_MMA("2", "f16");
+    else if constexpr (F8) RD_MMA("1", "f8f6f4");
+    else RD_MMA("1", "f16");
+#undef RD_MMA
 }
 // Arrives, once the products issued so far are done, at the barrier of every thread block that took part.
 template <int CG> __device__ __forceinline__ void mma_commit(uint32_t bar)
@@ -122,7 +121,26 @@ __device__ __forceinline__ void tmem_wait(uint32_t (&v)[32])
                  : "memory");
 }
 
-// The exponentials of the softmax: one instruction, within about 2^-22 of the value and 0 below 2^-126.  That is less than a
+// The same for 16 columns.
+__device__ __forceinline__ void tmem_load(uint32_t addr, uint32_t (&v)[16])
+{
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+        : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]), "=r"(v[8]), "=r"(v[9]), "=r"(v[10]), "=r"(v[11]),
+          "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15])
+        : "r"(addr)
+        : "memory");
+}
+__device__ __forceinline__ void tmem_wait(uint32_t (&v)[16])
+{
+    asm volatile("tcgen05.wait::ld.sync.aligned;"
+                 : "+r"(v[0]), "+r"(v[1]), "+r"(v[2]), "+r"(v[3]), "+r"(v[4]), "+r"(v[5]), "+r"(v[6]), "+r"(v[7]), "+r"(v[8]), "+r"(v[9]), "+r"(v[10]), "+r"(v[11]),
+                   "+r"(v[12]), "+r"(v[13]), "+r"(v[14]), "+r"(v[15])
+                 :
+                 : "memory");
+}
+
+// Exponentials (the loss's softmax): one instruction, within about 2^-22 of the value and 0 below 2^-126.  That is less than a
 // logit's own error moves it, and 32768 of them come with every tile of 128 x 256.
 __device__ __forceinline__ float exp2_fast(float x)
 {

@@ -472,6 +472,129 @@ PyObject *dropout(PyObject *, PyObject *const *a, Py_ssize_t n_args)
     });
 }
 
+const float *scale_vector(PyObject *o, size_t n, c10::Device device, const char *what)
+{
+    if (o == Py_None) return nullptr;
+    const at::Tensor &t = tensor(o, what);
+    if (t.scalar_type() != at::kFloat) wrong(what);
+    return static_cast<const float *>(vector(t, n, device, what));
+}
+
+// x, gate_weight, up_weight; x_scale, gate_scale, up_scale from `scales` on (null: none); activation
+rd_gated_t projections(const at::Tensor &x, const at::Tensor &gate, const at::Tensor &up, PyObject *const *scales, PyObject *activation)
+{
+    const Matrix m(x, "x must be a 2-D CUDA tensor with contiguous rows"), g(gate, "gate_weight must be a 2-D CUDA tensor with contiguous rows"),
+        u(up, "up_weight must be a 2-D CUDA tensor with contiguous rows");
+    if (g.dim != m.dim || u.dim != m.dim || u.rows != g.rows || gate.scalar_type() != x.scalar_type() || up.scalar_type() != x.scalar_type() || gate.device() != x.device() ||
+        up.device() != x.device())
+        wrong("gate_weight and up_weight must be [width, dim] with x's dtype and device");
+    rd_gated_t v{};
+    v.x = m.data;
+    v.x_stride = m.stride;
+    v.gate_weight = g.data;
+    v.gate_weight_stride = g.stride;
+    v.up_weight = u.data;
+    v.up_weight_stride = u.stride;
+    v.n = m.rows;
+    v.dim = m.dim;
+    v.width = g.rows;
+    v.dtype = code(x);
+    v.activation = static_cast<rd_activation_t>(whole(activation));
+    if (scales) {
+        v.x_scale = scale_vector(scales[0], m.rows, x.device(), "x_scale must be a contiguous float32 CUDA vector with one value per row, on the operands' device");
+        v.gate_scale = scale_vector(scales[1], g.rows, x.device(), "gate_scale must be a contiguous float32 CUDA vector with one value per weight row, on the operands' device");
+        v.up_scale = scale_vector(scales[2], g.rows, x.device(), "up_scale must be a contiguous float32 CUDA vector with one value per weight row, on the operands' device");
+    }
+    return v;
+}
+
+// x, gate_weight, up_weight, activation, keep, x_scale, gate_scale, up_scale, out_dtype, out, gate, up, workspace
+PyObject *gated(PyObject *, PyObject *const *a, Py_ssize_t n_args)
+{
+    return guarded(n_args, 13, [&]() -> PyObject * {
+        const at::Tensor &x = tensor(a[0], "x must be a 2-D CUDA tensor");
+        const rd_gated_t v = projections(x, tensor(a[1], "gate_weight must be a 2-D CUDA tensor"), tensor(a[2], "up_weight must be a 2-D CUDA tensor"), a + 5, a[3]);
+        const c10::Device device = x.device();
+        const c10::cuda::OptionalCUDAGuard guard(device);
+        at::ScalarType type = x.scalar_type() == at::kFloat8_e4m3fn ? at::kBFloat16 : x.scalar_type();
+        if (a[8] != Py_None) {
+            if (!THPDtype_Check(a[8])) wrong("out_dtype must be a torch.dtype");
+            type = reinterpret_cast<THPDtype *>(a[8])->scalar_type;
+        }
+        const bool keep = truth(a[4]);
+        const char *const names[3] = {"out must be [n, width] of out_dtype on x's device", "gate must be [n, width] of out_dtype on x's device", "up must be [n, width] of out_dtype on x's device"};
+        at::Tensor t[3];
+        void *data[3] = {};
+        size_t stride[3] = {};
+        for (int k = 0; k < 3; k++) {
+            if (k > 0 && !keep && a[9 + k] == Py_None) continue;
+            t[k] = matrix_or_new(a[9 + k], v.n, v.width, type, device, names[k]);
+            const Matrix m(t[k], names[k]);
+            data[k] = m.data;
+            stride[k] = m.stride;
+        }
+        const rd_dtype_t out_type = code(t[0]);
+        const cudaStream_t stream = c10::cuda::getCurrentCUDAStream(device.index());
+        size_t need = 0;
+        if (const int rc = rd_gated_workspace(&v, &need)) return status(rc);
+        const Workspace w(a[12], need, device, stream);
+        const int rc = without_gil([&] { return rd_gated(&v, data[0], stride[0], out_type, data[1], stride[1], data[2], stride[2], w.data, w.size, stream); });
+        if (rc != RD_OK) return status(rc);
+        PyObject *r = PyTuple_New(3);
+        if (!r) throw PythonError();
+        for (int k = 0; k < 3; k++) PyTuple_SET_ITEM(r, k, a[9 + k] == Py_None ? wrap_or_none(t[k]) : Py_NewRef(a[9 + k]));
+        return r;
+    });
+}
+
+// grad_out, x, gate_weight, up_weight, gate, up, activation, want_x, want_weights, grad_x, grad_gate_weight, grad_up_weight, workspace
+PyObject *gated_grad(PyObject *, PyObject *const *a, Py_ssize_t n_args)
+{
+    return guarded(n_args, 13, [&]() -> PyObject * {
+        const at::Tensor &x = tensor(a[1], "x must be a 2-D CUDA tensor"), &gate_weight = tensor(a[2], "gate_weight must be a 2-D CUDA tensor");
+        const at::Tensor &up_weight = tensor(a[3], "up_weight must be a 2-D CUDA tensor");
+        const rd_gated_t v = projections(x, gate_weight, up_weight, nullptr, a[6]);
+        const c10::Device device = x.device();
+        const c10::cuda::OptionalCUDAGuard guard(device);
+        const char *const names[3] = {"grad_out must be [n, width] with x's dtype and device", "gate must be [n, width] with x's dtype and device", "up must be [n, width] with x's dtype and device"};
+        const void *in[3];
+        size_t in_stride[3];
+        PyObject *const given[3] = {a[0], a[4], a[5]};
+        for (int k = 0; k < 3; k++) {
+            const at::Tensor &t = tensor(given[k], names[k]);
+            const Matrix m(t, names[k]);
+            if (m.rows != v.n || m.dim != v.width || t.scalar_type() != x.scalar_type() || t.device() != device) wrong(names[k]);
+            in[k] = m.data;
+            in_stride[k] = m.stride;
+        }
+        const bool wanted[3] = {truth(a[7]), truth(a[8]), truth(a[8])};
+        const char *const outs[3] = {"grad_x must be a 2-D CUDA tensor like x, with contiguous rows", "grad_gate_weight must be a 2-D CUDA tensor like gate_weight, with contiguous rows",
+                                     "grad_up_weight must be a 2-D CUDA tensor like up_weight, with contiguous rows"};
+        at::Tensor t[3];
+        void *out[3] = {};
+        size_t out_stride[3] = {};
+        for (int k = 0; k < 3; k++) {
+            if (!wanted[k] && a[9 + k] == Py_None) continue;
+            t[k] = matrix_or_new(a[9 + k], k ? v.width : v.n, v.dim, x.scalar_type(), device, outs[k]);
+            const Matrix m(t[k], outs[k]);
+            out[k] = m.data;
+            out_stride[k] = m.stride;
+        }
+        const cudaStream_t stream = c10::cuda::getCurrentCUDAStream(device.index());
+        size_t need = 0;
+        if (const int rc = rd_gated_grad_workspace(&v, out[0] != nullptr, &need)) return status(rc);
+        const Workspace w(a[12], need, device, stream);
+        const int rc = without_gil([&] {
+            return rd_gated_grad(&v, in[0], in_stride[0], in[1], in_stride[1], in[2], in_stride[2], out[0], out_stride[0], out[1], out_stride[1], out[2], out_stride[2], w.data, w.size, stream);
+        });
+        if (rc != RD_OK) return status(rc);
+        PyObject *r = PyTuple_New(3);
+        if (!r) throw PythonError();
+        for (int k = 0; k < 3; k++) PyTuple_SET_ITEM(r, k, a[9 + k] == Py_None ? wrap_or_none(t[k]) : Py_NewRef(a[9 + k]));
+        return r;
+    });
+}
+
 PyMethodDef methods[] = {
     {"embed", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(embed)), METH_FASTCALL, nullptr},
     {"embed_grad", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(embed_grad)), METH_FASTCALL, nullptr},
@@ -480,6 +603,8 @@ PyMethodDef methods[] = {
     {"norm", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(norm)), METH_FASTCALL, nullptr},
     {"norm_grad", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(norm_grad)), METH_FASTCALL, nullptr},
     {"dropout", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(dropout)), METH_FASTCALL, nullptr},
+    {"gated", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(gated)), METH_FASTCALL, nullptr},
+    {"gated_grad", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(gated_grad)), METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_rd_torch", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
