@@ -700,11 +700,11 @@ RD_API int rd_gated_grad(const rd_gated_t *v, const void *d_grad_out, size_t gra
                          void *d_workspace, size_t workspace_bytes, void *cuda_stream);
 
 /*
- * rd_gated_status -- waits for the current device and returns the word in which the kernels of rd_gated and rd_gated_grad note a bounded
- * wait that they gave up (it should never happen): 0, or RD_ERR_TIMEOUT if some launch since the last query did (its results are then
+ * rd_block_status -- waits for the current device and returns the word in which the kernels of rd_norm, rd_norm_grad, rd_gated and
+ * rd_gated_grad note a bounded wait that they gave up (it should never happen): 0, or RD_ERR_TIMEOUT if some launch since the last query did (its results are then
  * not valid); the word is cleared.
  */
-RD_API int rd_gated_status(int *device_status);
+RD_API int rd_block_status(int *device_status);
 
 /* rd_strerror -- static, never NULL. */
 RD_API const char *rd_strerror(int status);

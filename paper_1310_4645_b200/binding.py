@@ -36,7 +36,7 @@ EXPORTS = ("rd_schedule_create", "rd_schedule_create_segments", "rd_optimal_segm
            "rd_embed", "rd_embed_grad", "rd_embed_grad_workspace", "rd_vocab_loss", "rd_vocab_loss_workspace", "rd_vocab_loss_grad",
            "rd_vocab_loss_grad_workspace", "rd_vocab_status",
            "rd_norm", "rd_norm_grad", "rd_norm_grad_workspace", "rd_dropout", "rd_gated", "rd_gated_workspace", "rd_gated_grad",
-           "rd_gated_grad_workspace", "rd_gated_status")
+           "rd_gated_grad_workspace", "rd_block_status")
 
 
 class rd_model_t(C.Structure):
@@ -137,7 +137,7 @@ def lib():
         L.rd_gated.argtypes = [C.POINTER(rd_gated_t), vp, sz, i32, vp, sz, vp, sz, vp, sz, vp]
         L.rd_gated_grad_workspace.argtypes = [C.POINTER(rd_gated_t), i32, C.POINTER(sz)]
         L.rd_gated_grad.argtypes = [C.POINTER(rd_gated_t), vp, sz, vp, sz, vp, sz, vp, sz, vp, sz, vp, sz, vp, sz, vp]
-        L.rd_gated_status.argtypes = [C.POINTER(i32)]
+        L.rd_block_status.argtypes = [C.POINTER(i32)]
         L.rd_dropout.argtypes = [vp, sz, sz, sz, i32, f32, u64, u64, sz, vp, sz, vp]
         L.rd_vocab_loss_grad_workspace.argtypes = [C.POINTER(rd_vocab_t), i32, i32, C.POINTER(sz)]
         L.rd_vocab_loss_grad.argtypes = [C.POINTER(rd_vocab_t), vp, vp, sz, vp, sz, vp, sz, vp, sz, vp]
@@ -668,8 +668,8 @@ def rd_gated_grad(grad_out, x, gate_weight, up_weight, gate, up, activation=RD_S
     return r
 
 
-def rd_gated_status() -> int:
-    """Waits for the current device and returns (and clears) the gated kernels' status word: 0 or RD_ERR_TIMEOUT."""
+def rd_block_status() -> int:
+    """Waits for the current device and returns (and clears) the block operators' status word: 0 or RD_ERR_TIMEOUT."""
     st = C.c_int(0)
-    _check(lib().rd_gated_status(C.byref(st)), "rd_gated_status")
+    _check(lib().rd_block_status(C.byref(st)), "rd_block_status")
     return st.value

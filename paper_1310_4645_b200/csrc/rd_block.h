@@ -71,7 +71,9 @@ size_t gated_workspace(const GatedArgs &a);
 cudaError_t gated_forward(const GatedArgs &a);
 size_t gated_backward_workspace(const GatedArgs &a, bool want_x);
 cudaError_t gated_backward(const GatedArgs &a);
-cudaError_t gated_status(int *status);
+// The word in which a kernel notes a wait that it gave up, cleared; block_status waits for the device first and covers both files.
+cudaError_t norm_status(int *status);
+cudaError_t block_status(int *status);
 
 cudaError_t norm_forward(const NormArgs &a);
 cudaError_t norm_backward(const NormGradArgs &a);

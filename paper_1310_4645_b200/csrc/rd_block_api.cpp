@@ -271,11 +271,11 @@ int rd_gated_grad(const rd_gated_t *v, const void *d_grad_out, size_t grad_out_s
     return status_of(gated_backward(a));
 }
 
-int rd_gated_status(int *device_status)
+int rd_block_status(int *device_status)
 {
     if (!device_status) return RD_ERR_INVALID_ARG;
     int s = 0;
-    if (gated_status(&s) != cudaSuccess) return RD_ERR_CUDA;
+    if (block_status(&s) != cudaSuccess) return RD_ERR_CUDA;
     *device_status = s ? RD_ERR_TIMEOUT : RD_OK;
     return RD_OK;
 }

@@ -865,14 +865,18 @@ cudaError_t gated_backward(const GatedArgs &a)
     return launch(rd_gated_finish_kernel, rows, 256, a.stream, p.dx, a.grad_x_stride, static_cast<const float *>(l.parts), l.part_stride, a.n, uint32_t(a.dim), p.splits, bf16, wide_x);
 }
 
-cudaError_t gated_status(int *status)
+cudaError_t block_status(int *status)
 {
     cudaError_t e = cudaDeviceSynchronize();
+    if (e != cudaSuccess) return e;
+    int of_norm = 0;
+    e = norm_status(&of_norm);
     if (e != cudaSuccess) return e;
     e = cudaMemcpyFromSymbol(status, g_wait_status, sizeof(int));
     if (e != cudaSuccess) return e;
     const int zero = 0;
     if (*status) e = cudaMemcpyToSymbol(g_wait_status, &zero, sizeof(int));
+    *status |= of_norm;
     return e;
 }
 

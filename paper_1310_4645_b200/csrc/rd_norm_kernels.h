@@ -1,0 +1,382 @@
+// sm_100a kernels of the root-mean-square norm and of its gradient, for rows of one type: RD_NORM_ROWS is F32, B16 or H16 (a file that
+// includes this one each).  The formulas, and what bounds the kernels: rd_norm.cu.
+#include "rd_norm_rows.h"
+
+namespace rd {
+
+namespace {
+
+// What a kernel does besides: constants where a branch in its loops would cost, the call's otherwise (kAsk).
+enum Mode { kPlain = 0, kDrop = 1, kEight = 2, kAsk = 4 };
+
+// T: x and out, R: residual and sum, W: the weight.  A thread holds NV units of a row; what it has no unit for is zeros.
+template <class T, class R, class W, bool SPREAD, int NV, bool WARP, int MODE> __global__ void __launch_bounds__(kThreads, SPREAD ? 2 : 3) rd_norm_kernel(const __grid_constant__ NormParams p)
+{
+    using UnitT = Unit<T, SPREAD>;
+    using UnitR = Unit<R, SPREAD>;
+    constexpr uint32_t kT = UnitT::bytes / 8, kR = UnitR::bytes / 8;
+    const bool drops = MODE & kAsk ? p.drop.border != 0 : bool(MODE & kDrop), eight = MODE & kAsk ? p.out8 : bool(MODE & kEight);
+    __shared__ Meeting meeting;
+    __shared__ uint4 bits[SPREAD ? kWarps : 1][32];
+    __shared__ uint64_t bars[WARP ? kWarps : 1][kMostStages];
+    Stream<WARP> stream(bars, SPREAD ? RowRing{0, 0} : p.ring);
+    pdl_wait();
+    if (p.release_early) pdl_release();
+    const Place<SPREAD, WARP> at(p.units, p.per_block, p.blocks, p.threads);
+    const uint32_t unit0 = WARP ? 0 : at.rank * p.per_block, own = at.end - unit0;
+    const Piece pieces[2] = {{p.x, p.x_stride * kT, UnitT::bytes}, {p.residual, p.residual_stride * kR, UnitR::bytes}};
+    if (!SPREAD && stream.asks)
+        for (uint32_t i = 0; i < stream.stages && at.row + i * at.rows < p.n; i++) stream.ask(i, pieces, at.row + i * at.rows, unit0, own);
+    uint32_t turn = 0;
+    for (size_t row = at.row; row < p.n; row += at.rows, turn++) {
+        UnitT x[NV];
+        UnitR res[NV];
+        const void *x_row, *res_row;
+        if (SPREAD) {
+            x_row = at_byte(p.x, row * p.x_stride * kT);
+            res_row = at_byte(p.residual, row * p.residual_stride * kR);
+        } else {
+            const unsigned char *here = stream.wait();
+            x_row = here - unit0 * UnitT::bytes;
+            res_row = here + own * UnitT::bytes - unit0 * UnitR::bytes;
+        }
+#pragma unroll
+        for (int k = 0; k < NV; k++) {
+            x[k].load(x_row, at.unit + k * at.step, p.dim, at.has(k));
+            res[k].load(res_row, at.unit + k * at.step, p.dim, at.has(k) && p.residual);
+        }
+        void *const sum_row = at_byte(p.sum, row * p.sum_stride * kR);
+        Pair s[NV][4], squares = 0;
+        float2 stat = make_float2(0.0f, 0.0f);        // sum of squares, largest |s w|
+#pragma unroll
+        for (int k = 0; k < NV; k++) {
+            const uint32_t unit = at.unit + k * at.step;
+            x[k].get(s[k]);
+            if (drops) drop_values<SPREAD>(p.drop, bits[SPREAD ? threadIdx.x >> 5 : 0], unit, uint32_t(row), s[k]);
+            Pair r[4], w[4];
+            res[k].get(r);
+#pragma unroll
+            for (int i = 0; i < 4; i++) s[k][i] = add2(s[k][i], r[i]);
+            if (p.sum && at.has(k)) {
+                UnitR o;
+                o.set(s[k]);
+                o.store(sum_row, unit, p.dim);
+            }
+            Unit<W, SPREAD> weight;
+            weight.load(p.weight, unit, p.dim, at.has(k));
+            weight.get(w);
+#pragma unroll
+            for (int i = 0; i < 4; i++) {
+                squares = fma2(s[k][i], s[k][i], squares);
+                s[k][i] = mul2(s[k][i], w[i]);
+            }
+            if (eight)
+#pragma unroll
+                for (int i = 0; i < 4; i++) {
+                    const float2 v = both(s[k][i]);
+                    stat.y = fmaxf(fmaxf(stat.y, fabsf(v.x)), fabsf(v.y));
+                }
+        }
+        const float2 sums = both(squares);
+        stat.x = sums.x + sums.y;
+        stat = join_row<WARP>(stat, eight, meeting, turn, p.blocks, at.rank);
+        if (!SPREAD) {
+            // everyone has read this row
+            const size_t later = row + stream.stages * at.rows;
+            if (stream.asks && later < p.n && !stream.dead) stream.ask(stream.s, pieces, later, unit0, own);
+            stream.advance();
+        }
+        const float rstd = rsqrtf(fmaf(stat.x, p.inv_dim, p.eps));
+        float factor = rstd;
+        if (eight) {
+            // the row's largest value becomes 448; very small ones are taken near 1 first, so that no quotient overflows
+            const float lift = stat.y < 0x1p-60f ? 0x1p64f : 1.0f;
+            factor = stat.y > 0.0f ? 448.0f / (stat.y * lift) : 0.0f;
+            if (lift != 1.0f) {
+#pragma unroll
+                for (int k = 0; k < NV; k++)
+#pragma unroll
+                    for (int i = 0; i < 4; i++) s[k][i] = mul2(s[k][i], pair(lift, lift));
+            }
+        }
+        if (at.first()) {
+            if (p.rstd) p.rstd[row] = rstd;
+            if (eight) p.out_scale[row] = stat.y * rstd / 448.0f;
+        }
+        const Pair factors = pair(factor, factor);
+        void *const out_row = at_byte(p.out, row * p.out_stride * (eight ? 1 : kT));
+#pragma unroll
+        for (int k = 0; k < NV; k++) {
+            const uint32_t unit = at.unit + k * at.step;
+#pragma unroll
+            for (int i = 0; i < 4; i++) s[k][i] = mul2(s[k][i], factors);
+            if (eight) {
+                uint8_t *out = static_cast<uint8_t *>(out_row);
+                uint32_t q[4];
+#pragma unroll
+                for (int i = 0; i < 4; i++) q[i] = __nv_cvt_float2_to_fp8x2(both(s[k][i]), __NV_SATFINITE, __NV_E4M3);
+                if constexpr (!SPREAD) {
+                    if (at.has(k)) *reinterpret_cast<uint2 *>(out + unit * 8) = make_uint2(q[0] | q[1] << 16, q[2] | q[3] << 16);
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 8; i++)
+                        if (at.has(k) && column_of<true>(unit, i) < p.dim) out[column_of<true>(unit, i)] = uint8_t(i & 1 ? q[i / 2] >> 8 : q[i / 2]);
+                }
+            } else if (at.has(k)) {
+                UnitT o;
+                o.set(s[k]);
+                o.store(out_row, unit, p.dim);
+            }
+        }
+    }
+    if (!p.release_early) pdl_release();
+    if (stream.dead) drain();
+}
+
+// ------------------------------------------------------------------------------------------------ gradient
+
+// Persistent groups of threads that take rows in turn; a thread's columns stay the same, so that grad_weight adds up in its registers.
+// With the sum over a row of grad_out w s = m:  grad = r (grad_out w - s (r^2 m / dim)) + grad_sum.
+template <class T, class R, class W, bool SPREAD, int NV, bool WARP, int MODE>
+__global__ void __launch_bounds__(SPREAD ? 2 * kThreads : kThreads, SPREAD ? 1 : 3) rd_norm_grad_kernel(const __grid_constant__ NormGradParams p)
+{
+    using UnitT = Unit<T, SPREAD>;
+    using UnitR = Unit<R, SPREAD>;
+    constexpr uint32_t kT = UnitT::bytes / 8, kR = UnitR::bytes / 8;
+    const bool drops = MODE & kAsk ? p.drop.border != 0 : bool(MODE & kDrop);
+    __shared__ Meeting meeting;
+    __shared__ uint4 bits[SPREAD ? kMostWarps : 1][32];
+    __shared__ uint64_t bars[WARP ? kWarps : 1][kMostStages];
+    Stream<WARP> stream(bars, SPREAD ? RowRing{0, 0} : p.ring);
+    pdl_wait();
+    if (p.release_early) pdl_release();
+    const Place<SPREAD, WARP> at(p.units, p.per_block, p.blocks, p.threads);
+    const uint32_t unit0 = WARP ? 0 : at.rank * p.per_block, own = at.end - unit0;
+    const Piece pieces[3] = {{p.grad_out, p.grad_out_stride * kT, UnitT::bytes}, {p.sum, p.sum_stride * kR, UnitR::bytes}, {p.grad_sum, p.grad_sum_stride * kR, UnitR::bytes}};
+    if (!SPREAD && stream.asks)
+        for (uint32_t i = 0; i < stream.stages && at.row + i * at.rows < p.n; i++) stream.ask(i, pieces, at.row + i * at.rows, unit0, own);
+    Pair acc[NV][4] = {};
+    uint32_t turn = 0;
+    float next_rstd = at.row < p.n ? p.rstd[at.row] : 0.0f;
+    for (size_t row = at.row; row < p.n; row += at.rows, turn++) {
+        const float rstd = next_rstd;
+        if (row + at.rows < p.n) next_rstd = p.rstd[row + at.rows];
+        const Pair rstds = pair(rstd, rstd);
+        const void *up_row, *sum_row, *more_row;
+        if (SPREAD) {
+            up_row = at_byte(p.grad_out, row * p.grad_out_stride * kT);
+            sum_row = at_byte(p.sum, row * p.sum_stride * kR);
+            more_row = at_byte(p.grad_sum, row * p.grad_sum_stride * kR);
+        } else {
+            const unsigned char *here = stream.wait();
+            up_row = here - unit0 * UnitT::bytes;
+            sum_row = here + own * UnitT::bytes - unit0 * UnitR::bytes;
+            more_row = here + own * (UnitT::bytes + UnitR::bytes) - unit0 * UnitR::bytes;
+        }
+        // from the ring every operand is read where it is needed, twice; otherwise once, ahead
+        UnitT up[NV];
+        UnitR sum[NV], more[NV];
+        auto load = [&](int k) {
+            up[k].load(up_row, at.unit + k * at.step, p.dim, at.has(k));
+            sum[k].load(sum_row, at.unit + k * at.step, p.dim, at.has(k));
+        };
+        auto load_more = [&](int k) { more[k].load(more_row, at.unit + k * at.step, p.dim, at.has(k) && p.grad_sum); };
+        if (SPREAD) {
+#pragma unroll
+            for (int k = 0; k < NV; k++) {
+                load(k);
+                load_more(k);
+            }
+        }
+        Pair dots = 0;
+#pragma unroll
+        for (int k = 0; k < NV; k++) {
+            if (!SPREAD) load(k);
+            Pair u[4], s[4], w[4];
+            up[k].get(u);
+            sum[k].get(s);
+            Unit<W, SPREAD> weight;
+            weight.load(p.weight, at.unit + k * at.step, p.dim, at.has(k));
+            weight.get(w);
+#pragma unroll
+            for (int i = 0; i < 4; i++) {
+                const Pair y = mul2(u[i], s[i]);
+                acc[k][i] = fma2(y, rstds, acc[k][i]);
+                dots = fma2(y, w[i], dots);
+            }
+        }
+        const float2 dot = both(dots);
+        const float slope = join_row<WARP>(make_float2(dot.x + dot.y, 0.0f), false, meeting, turn, p.blocks, at.rank).x * p.inv_dim * rstd * rstd;
+        const Pair slopes = pair(-slope, -slope);
+        if (!SPREAD) {
+            // everyone is through with the row before this one
+            const size_t later = row + (stream.stages - 1) * at.rows;
+            if (stream.asks && turn > 0 && later < p.n && !stream.dead) stream.ask(stream.s == 0 ? stream.stages - 1 : stream.s - 1, pieces, later, unit0, own);
+            stream.advance();
+        }
+        if (!p.want_rows) continue;
+        void *const gr_row = at_byte(p.grad_residual, row * p.grad_residual_stride * kR), *const gx_row = at_byte(p.grad_x, row * p.grad_x_stride * kT);
+#pragma unroll
+        for (int k = 0; k < NV; k++) {
+            const uint32_t unit = at.unit + k * at.step;
+            if (!SPREAD) {
+                load(k);
+                load_more(k);
+            }
+            Pair u[4], s[4], w[4];
+            up[k].get(u);
+            sum[k].get(s);
+            Unit<W, SPREAD> weight;
+            weight.load(p.weight, unit, p.dim, at.has(k));
+            weight.get(w);
+#pragma unroll
+            for (int i = 0; i < 4; i++) u[i] = fma2(slopes, s[i], mul2(u[i], w[i]));
+            more[k].get(s);
+#pragma unroll
+            for (int i = 0; i < 4; i++) u[i] = fma2(rstds, u[i], s[i]);
+            if (p.grad_residual && at.has(k)) {
+                UnitR o;
+                o.set(u);
+                o.store(gr_row, unit, p.dim);
+            }
+            if (p.grad_x) {
+                if (drops) drop_values<SPREAD>(p.drop, bits[SPREAD ? threadIdx.x >> 5 : 0], unit, uint32_t(row), u);
+                if (at.has(k)) {
+                    UnitT o;
+                    o.set(u);
+                    o.store(gx_row, unit, p.dim);
+                }
+            }
+        }
+    }
+    if (!p.release_early) pdl_release();
+    if (stream.dead) drain();
+    if (!p.part) return;
+    if constexpr (WARP) {
+        // the block's warps, one after the other in shared memory (the ring's, which no copy is on its way to), in order
+        float *of_warp = reinterpret_cast<float *>(ring);
+        const uint32_t warp = threadIdx.x >> 5;
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < NV; k++)
+            if (at.has(k))
+#pragma unroll
+                for (int i = 0; i < 8; i++) {
+                    const uint32_t j = column_of<SPREAD>(at.unit + k * at.step, i);
+                    if (!SPREAD || j < p.dim) of_warp[warp * p.dim + j] = i & 1 ? both(acc[k][i / 2]).y : both(acc[k][i / 2]).x;
+                }
+        __syncthreads();
+        for (uint32_t j = threadIdx.x; j < p.dim; j += kThreads) {
+            float v = of_warp[j];
+#pragma unroll
+            for (int k = 1; k < kWarps; k++) v += of_warp[k * p.dim + j];
+            p.part[size_t(blockIdx.x) * p.dim + j] = v;
+        }
+    } else {
+#pragma unroll
+        for (int k = 0; k < NV; k++)
+            if (at.has(k)) {
+                Unit<F32, SPREAD> o;
+                o.set(acc[k]);
+                o.store(p.part + at.row * p.dim, at.unit + k * at.step, p.dim);
+            }
+    }
+}
+
+// ------------------------------------------------------------------------------------------------ launches
+
+template <auto KERNEL, typename P> cudaError_t launch_rows(const P &p, const RowShape &s, const RowDeal &d, cudaStream_t stream)
+{
+    if (s.smem > 0) {
+        static std::atomic<bool> ready[64];
+        int device = 0;
+        cudaError_t e = cudaGetDevice(&device);
+        if (e == cudaSuccess && (device >= 64 || !ready[device].load(std::memory_order_acquire))) {
+            e = cudaFuncSetAttribute(KERNEL, cudaFuncAttributeMaxDynamicSharedMemorySize, int(kRingBytes));
+            if (e == cudaSuccess && device < 64) ready[device].store(true, std::memory_order_release);
+        }
+        if (e != cudaSuccess) return e;
+    }
+    cudaLaunchConfig_t c{};
+    c.gridDim = dim3(unsigned(s.groups * d.blocks));
+    c.blockDim = dim3(d.threads);
+    c.dynamicSmemBytes = s.smem;
+    c.stream = stream;
+    cudaLaunchAttribute attrs[2] = {pdl_attribute()};
+    attrs[1].id = cudaLaunchAttributeClusterDimension;
+    attrs[1].val.clusterDim.x = d.blocks;
+    attrs[1].val.clusterDim.y = attrs[1].val.clusterDim.z = 1;
+    c.attrs = attrs;
+    c.numAttrs = d.blocks > 1 ? 2 : 1;
+    return cudaLaunchKernelEx(&c, KERNEL, p);
+}
+
+// Calls f with the kernel's template arguments: how the row lies, the types of residual and weight.
+template <class F> cudaError_t with_shape(bool spread, const RowDeal &d, F &&f)
+{
+    using std::integral_constant;
+    using Yes = integral_constant<bool, true>;
+    using No = integral_constant<bool, false>;
+    using One = integral_constant<int, 1>;
+    using Two = integral_constant<int, 2>;
+    using Four = integral_constant<int, 4>;
+    if (!spread && d.warp) return d.nv == 1 ? f(No(), One(), Yes()) : d.nv == 2 ? f(No(), Two(), Yes()) : f(No(), Four(), Yes());
+    if (!spread) return d.nv == 2 ? f(No(), Two(), No()) : f(No(), Four(), No());
+    if (d.warp) return d.nv <= 2 ? f(Yes(), Two(), Yes()) : f(Yes(), Four(), Yes());
+    return d.nv == 2 ? f(Yes(), Two(), No()) : f(Yes(), Four(), No());
+}
+template <class T, class F> cudaError_t with_types(int sum_dtype, int weight_dtype, F &&f)
+{
+    if constexpr (std::is_same_v<T, F32>) return f(F32(), F32());
+    else if (sum_dtype == RD_FP32) return weight_dtype == RD_FP32 ? f(F32(), F32()) : f(F32(), T());
+    else return weight_dtype == RD_FP32 ? f(T(), F32()) : f(T(), T());
+}
+
+}  // namespace
+
+template <> cudaError_t launch_norm<RD_NORM_ROWS>(const NormParams &p, const NormCall &c)
+{
+    using T = RD_NORM_ROWS;
+    return with_shape(c.spread, c.deal, [&](auto SPREAD, auto NV, auto WARP) {
+        return with_types<T>(c.sum_dtype, c.weight_dtype, [&](auto R, auto W) {
+            using RT = decltype(R);
+            using WT = decltype(W);
+            if constexpr (SPREAD()) {
+                return launch_rows<rd_norm_kernel<T, RT, WT, true, NV(), WARP(), kAsk>>(p, c.shape, c.deal, c.stream);
+            } else {
+                if (p.out8 && p.drop.border) return launch_rows<rd_norm_kernel<T, RT, WT, false, NV(), WARP(), kDrop | kEight>>(p, c.shape, c.deal, c.stream);
+                if (p.out8) return launch_rows<rd_norm_kernel<T, RT, WT, false, NV(), WARP(), kEight>>(p, c.shape, c.deal, c.stream);
+                if (p.drop.border) return launch_rows<rd_norm_kernel<T, RT, WT, false, NV(), WARP(), kDrop>>(p, c.shape, c.deal, c.stream);
+                return launch_rows<rd_norm_kernel<T, RT, WT, false, NV(), WARP(), kPlain>>(p, c.shape, c.deal, c.stream);
+            }
+        });
+    });
+}
+
+template <> cudaError_t launch_norm_grad<RD_NORM_ROWS>(const NormGradParams &p, const NormCall &c)
+{
+    using T = RD_NORM_ROWS;
+    return with_shape(c.spread, c.deal, [&](auto SPREAD, auto NV, auto WARP) {
+        return with_types<T>(c.sum_dtype, c.weight_dtype, [&](auto R, auto W) {
+            using RT = decltype(R);
+            using WT = decltype(W);
+            if constexpr (SPREAD()) {
+                return launch_rows<rd_norm_grad_kernel<T, RT, WT, true, NV(), WARP(), kAsk>>(p, c.shape, c.deal, c.stream);
+            } else {
+                if (p.drop.border) return launch_rows<rd_norm_grad_kernel<T, RT, WT, false, NV(), WARP(), kDrop>>(p, c.shape, c.deal, c.stream);
+                return launch_rows<rd_norm_grad_kernel<T, RT, WT, false, NV(), WARP(), kPlain>>(p, c.shape, c.deal, c.stream);
+            }
+        });
+    });
+}
+
+template <> cudaError_t norm_rows_status<RD_NORM_ROWS>(int *status)
+{
+    cudaError_t e = cudaMemcpyFromSymbol(status, g_wait_status, sizeof(int));
+    if (e != cudaSuccess) return e;
+    const int zero = 0;
+    if (*status) e = cudaMemcpyToSymbol(g_wait_status, &zero, sizeof(int));
+    return e;
+}
+
+}  // namespace rd

@@ -1,0 +1,144 @@
+// What the norm's host code and its kernels share: parameters, how rows are dealt out, launches by the rows' type.
+#ifndef RD_NORM_SHAPE_H_
+#define RD_NORM_SHAPE_H_
+
+#include <cuda_runtime.h>
+
+#include <cstddef>
+#include <cstdint>
+
+namespace rd {
+
+constexpr int kThreads = 256, kWarps = kThreads / 32;       // of blocks whose warps have a row each, and of dropout alone
+constexpr uint32_t kBlockUnits = 1024;    // units of 8 columns of a row that a thread block has at most
+constexpr int kUnits = 4;                 // units that a thread has at most; two in the gradient without a ring, whose operands stay in registers
+constexpr int kMostWarps = 16;
+constexpr size_t kDropoutBlocks = 6;      // of dropout alone, an SM
+constexpr uint32_t kMostStages = 8;
+constexpr size_t kRingBytes = 200 << 10;  // of an SM's shared memory that rows on their way may take
+constexpr size_t kSms = 148;
+
+// Types of values.
+struct F32 {
+    static constexpr int words = 8;       // of 8 values
+};
+struct B16 {
+    static constexpr int words = 4;
+};
+struct H16 {
+    static constexpr int words = 4;
+};
+
+// Dropout, as the kernels want it.
+constexpr int kRounds = 10;
+struct DropKeys {
+    uint32_t border, border16;                // border16: border << 16
+    float keep;
+    uint32_t key[2 * kRounds];                // both key words of every round
+    uint32_t offset0, offset1, first;
+};
+
+// The ring of stages that rows come in through.
+struct RowRing {
+    uint32_t stages, stage;   // how many, and bytes of one
+};
+
+struct NormParams {
+    RowRing ring;
+    const void *x, *residual, *weight;
+    void *out, *sum;
+    float *out_scale, *rstd;
+    size_t x_stride, residual_stride, out_stride, sum_stride, n;
+    uint32_t dim, units, per_block, blocks, threads;
+    float eps, inv_dim;
+    DropKeys drop;
+    bool out8, release_early;
+};
+
+struct NormGradParams {
+    RowRing ring;
+    const void *grad_out, *sum, *weight, *grad_sum;
+    const float *rstd;
+    void *grad_x, *grad_residual;
+    float *part;              // [groups][dim]: every group's part of grad_weight; null where it is not wanted
+    size_t grad_out_stride, sum_stride, grad_sum_stride, grad_x_stride, grad_residual_stride, n;
+    uint32_t dim, units, per_block, blocks, threads;
+    float inv_dim;
+    DropKeys drop;
+    bool want_rows, release_early;
+};
+
+// How a row is dealt out: to a warp if that holds it with four units a thread (`few`: two), or else to as few warps of a thread block
+// as hold it with four, so that the join of a row costs few instructions a value, or to a cluster of up to eight blocks.
+// few: two units a thread and twice the warps while one block of them holds the row; beyond that only where registers hold no more
+// (`always`).  The gradient of 16384 x 4096 bf16 with dropout takes 129 us so, 137 with four (B200); of 8192 x 8192, with blocks of 512
+// threads, 106 and 101.
+struct RowDeal {
+    uint32_t units, per_block, blocks, threads;
+    int nv;                   // units a thread
+    bool warp;
+};
+enum RowUnits { kFour, kFew, kFewAlways };
+inline RowDeal deal(size_t dim, RowUnits wanted)
+{
+    RowDeal d{};
+    d.units = uint32_t((dim + 7) / 8);
+    const bool few = wanted == kFewAlways || (wanted == kFew && d.units > 32 * kUnits && d.units <= kThreads * kUnits / 2);
+    d.nv = few ? kUnits / 2 : kUnits;
+    d.warp = d.units <= uint32_t(32 * d.nv);
+    d.blocks = 1;
+    d.threads = kThreads;
+    d.per_block = d.units;
+    if (d.warp) {
+        while (d.nv > 1 && d.units <= uint32_t(16 * d.nv)) d.nv /= 2;
+        return d;
+    }
+    while ((d.units + d.blocks - 1) / d.blocks > kBlockUnits) d.blocks *= 2;
+    // whole warps' columns, so that no 256 columns are two blocks'
+    d.per_block = ((d.units + d.blocks - 1) / d.blocks + 31) / 32 * 32;
+    d.threads = (d.per_block + 32 * d.nv - 1) / (32 * d.nv) * 32;
+    return d;
+}
+
+// How many groups of threads (a block of warps with a row each, or the blocks of one row) work at a time, and the ring of each block
+// (unit_bytes: of all matrices that come in, for 8 columns; 0: none): as many blocks an SM as registers allow (80 a thread with a ring)
+// and shared memory with two stages or more.
+struct RowShape {
+    size_t groups, smem;
+    bool one_turn;            // no group has more than one row
+    RowRing ring;
+};
+inline RowShape shape_of(size_t n, const RowDeal &d, size_t unit_bytes)
+{
+    RowShape s{};
+    const size_t rows = d.warp ? kWarps : 1, wanted = (n + rows - 1) / rows;
+    size_t per_sm = 65536 / (d.threads * (unit_bytes ? 80 : 128));
+    if (unit_bytes) {
+        const size_t stage = d.per_block * unit_bytes, all = stage * rows;
+        while (per_sm > 1 && kRingBytes / per_sm / all < 2) per_sm--;
+        const size_t fit = kRingBytes / per_sm / all;
+        s.ring = RowRing{uint32_t(fit < kMostStages ? fit : kMostStages), uint32_t(stage)};
+        s.smem = s.ring.stages * all;
+    }
+    const size_t most = kSms * per_sm / d.blocks;
+    s.groups = wanted < most ? wanted : most;
+    s.one_turn = wanted <= most;
+    return s;
+}
+
+// A launch, besides the kernel's parameters.
+struct NormCall {
+    bool spread;
+    RowDeal deal;
+    RowShape shape;
+    int sum_dtype, weight_dtype;
+    cudaStream_t stream;
+};
+template <class T> cudaError_t launch_norm(const NormParams &p, const NormCall &c);
+template <class T> cudaError_t launch_norm_grad(const NormGradParams &p, const NormCall &c);
+// The word in which a file's kernels note a wait that they gave up, cleared.
+template <class T> cudaError_t norm_rows_status(int *status);
+
+}  // namespace rd
+
+#endif  // RD_NORM_SHAPE_H_

@@ -81,7 +81,7 @@ def test_gated(dtype, n, dim, width):
         # the same bits wherever the operands lie, and whatever is kept
         o2, g2, u2 = rd.rd_gated(x, wg, wu, act)
         assert g2 is None and u2 is None and torch.equal(o2, out)
-    assert rd.rd_gated_status() == rd.RD_OK
+    assert rd.rd_block_status() == rd.RD_OK
 
 
 @gpu
@@ -117,7 +117,7 @@ def test_gated_8bit(n, dim, width):
         o2, _, _ = rd.rd_gated(x, wg, wu, act, x_scale=sx, gate_scale=sg, up_scale=su, out_dtype=dtype)
         assert torch.equal(o2, out)
     assert rd.rd_gated(x, wg, wu, x_scale=sx, gate_scale=sg, up_scale=su)[0].dtype == torch.bfloat16
-    assert rd.rd_gated_status() == rd.RD_OK
+    assert rd.rd_block_status() == rd.RD_OK
 
 
 @gpu
@@ -190,7 +190,7 @@ def test_gated_grad(dtype, n, dim, width):
     into = torch.empty_like(wu)
     up_alone = rd.rd_gated_grad(d, x, wg, wu, gate, up, act, want_x=False, want_weights=False, grad_up_weight=into)
     assert up_alone[0] is None and up_alone[1] is None and torch.equal(into, outs[2])
-    assert rd.rd_gated_status() == rd.RD_OK
+    assert rd.rd_block_status() == rd.RD_OK
 
 
 @gpu
@@ -265,7 +265,7 @@ def test_gated_streams_and_graphs(n):
             graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for r in results for a, b in zip(r, w))
-    assert rd.rd_gated_status() == rd.RD_OK
+    assert rd.rd_block_status() == rd.RD_OK
 
 
 # ------------------------------------------------------------------------------------------------ refusals
@@ -297,7 +297,7 @@ def test_gated_refusals():
             UNSUPPORTED_GATED + [dict(ot=rd.RD_FP16), dict(ot=rd.RD_FP32), {**eight, "ot": rd.RD_FP32}, {**eight, "ot": rd.RD_E4M3}])
     assert call(**{**good, "x": P + 2, "ws": 16 * P, "size": need.value - 1}) == rd.RD_ERR_TOO_SMALL
     assert call(**{**good, "n": 0, "x": None, "out": None}) == rd.RD_OK
-    assert L.rd_gated_status(None) == rd.RD_ERR_INVALID_ARG
+    assert L.rd_block_status(None) == rd.RD_ERR_INVALID_ARG
 
 
 def test_gated_grad_refusals():
