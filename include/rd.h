@@ -607,7 +607,7 @@ typedef struct {
  *   d_out_scale  DEVICE; n values, with RD_E4M3 alone (else NULL).
  *   d_sum        DEVICE; n x dim, sum_dtype: s; or NULL.      d_rstd  DEVICE; n values; or NULL.
  * out and sum may be x or residual (where the types agree).
- * Rows of 8 values that begin on 16-byte boundaries (8 for RD_E4M3), in every matrix and the weight, move as words of 16 bytes, others
+ * Rows of a multiple of 8 values that begin on boundaries of 8 values, in every matrix and the weight, move in words of 8 values, others
  * by element.
  */
 RD_API int rd_norm(const rd_norm_t *v, void *d_out, size_t out_stride, rd_dtype_t out_dtype, float *d_out_scale, void *d_sum, size_t sum_stride,

@@ -42,8 +42,8 @@ template <class T, class R, class W, bool SPREAD, int NV, bool WARP, int MODE> _
         }
 #pragma unroll
         for (int k = 0; k < NV; k++) {
-            x[k].load(x_row, at.unit + k * at.step, p.dim, at.has(k));
-            res[k].load(res_row, at.unit + k * at.step, p.dim, at.has(k) && p.residual);
+            x[k].template load<!SPREAD>(x_row, at.unit + k * at.step, p.dim, at.has(k));
+            res[k].template load<!SPREAD>(res_row, at.unit + k * at.step, p.dim, at.has(k) && p.residual);
         }
         void *const sum_row = at_byte(p.sum, row * p.sum_stride * kR);
         Pair s[NV][4], squares = 0;
@@ -177,10 +177,10 @@ __global__ void __launch_bounds__(SPREAD ? 2 * kThreads : kThreads, SPREAD ? 1 :
         UnitT up[NV];
         UnitR sum[NV], more[NV];
         auto load = [&](int k) {
-            up[k].load(up_row, at.unit + k * at.step, p.dim, at.has(k));
-            sum[k].load(sum_row, at.unit + k * at.step, p.dim, at.has(k));
+            up[k].template load<!SPREAD>(up_row, at.unit + k * at.step, p.dim, at.has(k));
+            sum[k].template load<!SPREAD>(sum_row, at.unit + k * at.step, p.dim, at.has(k));
         };
-        auto load_more = [&](int k) { more[k].load(more_row, at.unit + k * at.step, p.dim, at.has(k) && p.grad_sum); };
+        auto load_more = [&](int k) { more[k].template load<!SPREAD>(more_row, at.unit + k * at.step, p.dim, at.has(k) && p.grad_sum); };
         if (SPREAD) {
 #pragma unroll
             for (int k = 0; k < NV; k++) {

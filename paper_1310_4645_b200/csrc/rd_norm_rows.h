@@ -58,7 +58,7 @@ __device__ __forceinline__ Pair fma2(Pair x, Pair y, Pair z)
 }
 
 // Columns are dealt out in units of 8, a thread's value i of unit u being
-//   column 8 u + i, where rows begin on 16-byte boundaries and are made of whole units: one or two accesses of 16 bytes;
+//   column 8 u + i, where rows are made of whole units and begin on 16-byte boundaries (fp32: 32): one access of 16 or 32 bytes;
 //   otherwise (SPREAD) column 32 i + u mod 32 of the 256 columns that a warp's 32 units are: accesses by element, side by side.
 template <bool SPREAD> __device__ __forceinline__ uint32_t column_of(uint32_t unit, int i) { return SPREAD ? (unit & ~31u) * 8 + (unit & 31u) + 32 * i : unit * 8 + i; }
 
@@ -66,13 +66,17 @@ template <bool SPREAD> __device__ __forceinline__ uint32_t column_of(uint32_t un
 template <class T, bool SPREAD> struct Unit {
     static constexpr uint32_t bytes = 4 * T::words;
     uint32_t w[T::words];
-    // `row`: where the row begins; zeros where there is nothing to read
-    __device__ __forceinline__ void load(const void *row, uint32_t unit, uint32_t dim, bool there)
+    // `row`: where the row begins; zeros where there is nothing to read.  SHARED: in shared memory
+    template <bool SHARED = false> __device__ __forceinline__ void load(const void *row, uint32_t unit, uint32_t dim, bool there)
     {
 #pragma unroll
         for (int i = 0; i < T::words; i++) w[i] = 0;
         if (!there) return;
-        if constexpr (!SPREAD) {
+        if constexpr (!SPREAD && !SHARED && T::words == 8) {
+            asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                         : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]), "=r"(w[4]), "=r"(w[5]), "=r"(w[6]), "=r"(w[7])
+                         : "l"(static_cast<const char *>(row) + unit * bytes));
+        } else if constexpr (!SPREAD) {
             const uint4 *p = reinterpret_cast<const uint4 *>(static_cast<const char *>(row) + unit * bytes);
 #pragma unroll
             for (int i = 0; i < T::words / 4; i++) {
@@ -97,7 +101,11 @@ template <class T, bool SPREAD> struct Unit {
     }
     __device__ __forceinline__ void store(void *row, uint32_t unit, uint32_t dim) const
     {
-        if constexpr (!SPREAD) {
+        if constexpr (!SPREAD && T::words == 8) {
+            asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(static_cast<char *>(row) + unit * bytes), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(w[4]),
+                         "r"(w[5]), "r"(w[6]), "r"(w[7])
+                         : "memory");
+        } else if constexpr (!SPREAD) {
             uint4 *p = reinterpret_cast<uint4 *>(static_cast<char *>(row) + unit * bytes);
 #pragma unroll
             for (int i = 0; i < T::words / 4; i++) p[i] = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
