@@ -110,6 +110,11 @@ bool in_units(const void *p, size_t stride, int dtype)
     return !p || (reinterpret_cast<uintptr_t>(p) % to == 0 && stride * size_of(dtype) % to == 0);
 }
 
+// Whether grad_weight is summed up by blocks of its own beside the rows', 16 columns each, instead of from the groups' parts by another
+// launch: few rows and not too many columns, which are read twice.  B200, us a call, this and the other way: 16 rows of 1000 bf16 5.1
+// and 7.1, 257 of them 5.1 and 7.1, 384 6.2 and 7.4; 100 rows of 4096 5.2 and 6.9, 320 7.9 and 7.8, 384 11.0 and 8.0.
+bool by_columns(size_t n, size_t dim, const RowDeal &d) { return n <= 384 && n * dim <= size_t(1) << 20 && d.blocks == 1; }
+
 }  // namespace
 
 cudaError_t norm_forward(const NormArgs &a)
@@ -142,13 +147,14 @@ cudaError_t norm_forward(const NormArgs &a)
     p.threads = d.threads;
     p.release_early = shape.one_turn;
     p.out8 = a.out_dtype == RD_E4M3;
-    const NormCall call{spread, d, shape, a.sum_dtype, a.weight_dtype, a.stream};
+    const NormCall call{spread, d, shape, a.sum_dtype, a.weight_dtype, a.stream, 0};
     return a.dtype == RD_FP32 ? launch_norm<F32>(p, call) : a.dtype == RD_BF16 ? launch_norm<B16>(p, call) : launch_norm<H16>(p, call);
 }
 
 size_t norm_backward_workspace(size_t n, size_t dim)
 {
     // a part of grad_weight of every group; fewest bytes a value, most groups
+    if (by_columns(n, dim, deal(dim, kFew))) return 0;
     const size_t whole = shape_of(n, deal(dim, kFew), 8 * 4).groups, spread = shape_of(n, deal(dim, kFewAlways), 0).groups;
     return (whole > spread ? whole : spread) * dim * sizeof(float);
 }
@@ -158,7 +164,10 @@ cudaError_t norm_backward(const NormGradArgs &a)
     const bool spread = a.dim % 8 != 0 || !in_units(a.grad_out, a.grad_out_stride, a.dtype) || !in_units(a.sum, a.sum_stride, a.sum_dtype) || !in_units(a.weight, 0, a.weight_dtype) ||
                         !in_units(a.grad_sum, a.grad_sum_stride, a.sum_dtype) || !in_units(a.grad_x, a.grad_x_stride, a.dtype) ||
                         !in_units(a.grad_residual, a.grad_residual_stride, a.sum_dtype);
-    const RowDeal d = deal(a.dim, spread ? kFewAlways : kFew);
+    RowDeal d = deal(a.dim, spread ? kFewAlways : kFew);
+    const bool few = a.n > 0 && by_columns(a.n, a.dim, d), columns = few && a.grad_weight;
+    // blocks that columns want; whether they are wanted or not, so that the rows' bits do not depend on it
+    if (few && d.threads < kThreads) d.threads = kThreads;
     RowShape shape = shape_of(a.n, d, spread ? 0 : 8 * (size_of(a.dtype) + size_of(a.sum_dtype) * (a.grad_sum ? 2 : 1)));
     // where warps have rows, their parts of grad_weight are joined in shared memory
     if (d.warp && shape.smem < kWarps * a.dim * sizeof(float)) shape.smem = kWarps * a.dim * sizeof(float);
@@ -187,10 +196,30 @@ cudaError_t norm_backward(const NormGradArgs &a)
     p.threads = d.threads;
     p.release_early = shape.one_turn;
     p.want_rows = a.grad_x || a.grad_residual;
-    const NormCall call{spread, d, shape, a.sum_dtype, a.weight_dtype, a.stream};
+    p.row_blocks = uint32_t(shape.groups * d.blocks);
+    if (columns) {
+        p.part = nullptr;
+        p.grad_weight = a.grad_weight;
+    }
+    auto run = [&](const NormGradParams &q, const NormCall &c) {
+        return a.dtype == RD_FP32 ? launch_norm_grad<F32>(q, c) : a.dtype == RD_BF16 ? launch_norm_grad<B16>(q, c) : launch_norm_grad<H16>(q, c);
+    };
+    NormCall call{spread, d, shape, a.sum_dtype, a.weight_dtype, a.stream, columns ? (a.dim + kSumColumns - 1) / kSumColumns : 0};
     cudaError_t e = cudaSuccess;
-    if (shape.groups) e = a.dtype == RD_FP32 ? launch_norm_grad<F32>(p, call) : a.dtype == RD_BF16 ? launch_norm_grad<B16>(p, call) : launch_norm_grad<H16>(p, call);
-    if (e != cudaSuccess || !a.grad_weight) return e;
+    bool in_place = false;        // gradients in the place of what the columns read
+    for (const void *w : {a.grad_x, a.grad_residual}) in_place |= w && (w == a.grad_out || w == a.sum);
+    if (columns && in_place) {
+        // then the columns go first, by themselves
+        NormGradParams q = p;
+        NormCall c = call;
+        q.row_blocks = 0;
+        c.shape.groups = 0;
+        e = run(q, c);
+        if (e != cudaSuccess) return e;
+        call.more_blocks = 0;
+    }
+    if (shape.groups) e = run(p, call);
+    if (e != cudaSuccess || !a.grad_weight || columns) return e;
     auto *join = a.weight_dtype == RD_FP32 ? rd_norm_weight_kernel<F32> : a.weight_dtype == RD_BF16 ? rd_norm_weight_kernel<B16> : rd_norm_weight_kernel<H16>;
     return launch(join, unsigned((a.dim + 31) / 32), kJoinThreads, a.stream, a.grad_weight, static_cast<const float *>(a.workspace), uint32_t(shape.groups), uint32_t(a.dim));
 }

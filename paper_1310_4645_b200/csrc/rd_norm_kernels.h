@@ -22,7 +22,7 @@ template <class T, class R, class W, bool SPREAD, int NV, bool WARP, int MODE> _
     Stream<WARP> stream(bars, SPREAD ? RowRing{0, 0} : p.ring);
     pdl_wait();
     if (p.release_early) pdl_release();
-    const Place<SPREAD, WARP> at(p.units, p.per_block, p.blocks, p.threads);
+    const Place<SPREAD, WARP> at(p.units, p.per_block, p.blocks, p.threads, gridDim.x);
     const uint32_t unit0 = WARP ? 0 : at.rank * p.per_block, own = at.end - unit0;
     const Piece pieces[2] = {{p.x, p.x_stride * kT, UnitT::bytes}, {p.residual, p.residual_stride * kR, UnitR::bytes}};
     if (!SPREAD && stream.asks)
@@ -135,6 +135,31 @@ template <class T, class R, class W, bool SPREAD, int NV, bool WARP, int MODE> _
 
 // ------------------------------------------------------------------------------------------------ gradient
 
+template <class T> __device__ __forceinline__ float element(const void *p, size_t at)
+{
+    if constexpr (std::is_same_v<T, F32>) return static_cast<const float *>(p)[at];
+    else if constexpr (std::is_same_v<T, B16>) return __bfloat162float(static_cast<const __nv_bfloat16 *>(p)[at]);
+    else return __half2float(static_cast<const __half *>(p)[at]);
+}
+
+// grad_weight of 16 columns over all rows, by one block: for few rows, where another launch would cost more than reading twice.
+template <class T, class R, class W> __device__ __forceinline__ void sum_columns(const NormGradParams &p, float (*sums)[kSumColumns])
+{
+    const uint32_t x = threadIdx.x % kSumColumns, y = threadIdx.x / kSumColumns, down = blockDim.x / kSumColumns, column = (blockIdx.x - p.row_blocks) * kSumColumns + x;
+    float v = 0.0f;
+    if (column < p.dim)
+#pragma unroll 8
+        for (uint32_t row = y; row < uint32_t(p.n); row += down)
+            v = fmaf(element<T>(p.grad_out, row * p.grad_out_stride + column) * element<R>(p.sum, row * p.sum_stride + column), p.rstd[row], v);
+    sums[y][x] = v;
+    __syncthreads();
+    if (y || column >= p.dim) return;
+    for (uint32_t k = 1; k < down; k++) v += sums[k][x];
+    if constexpr (std::is_same_v<W, F32>) static_cast<float *>(p.grad_weight)[column] = v;
+    else if constexpr (std::is_same_v<W, B16>) static_cast<__nv_bfloat16 *>(p.grad_weight)[column] = __float2bfloat16_rn(v);
+    else static_cast<__half *>(p.grad_weight)[column] = __float2half_rn(v);
+}
+
 // Persistent groups of threads that take rows in turn; a thread's columns stay the same, so that grad_weight adds up in its registers.
 // With the sum over a row of grad_out w s = m:  grad = r (grad_out w - s (r^2 m / dim)) + grad_sum.
 template <class T, class R, class W, bool SPREAD, int NV, bool WARP, int MODE>
@@ -144,13 +169,18 @@ __global__ void __launch_bounds__(SPREAD ? 2 * kThreads : kThreads, SPREAD ? 1 :
     using UnitR = Unit<R, SPREAD>;
     constexpr uint32_t kT = UnitT::bytes / 8, kR = UnitR::bytes / 8;
     const bool drops = MODE & kAsk ? p.drop.border != 0 : bool(MODE & kDrop);
+    __shared__ float column_sums[kMostWarps * 32 / kSumColumns][kSumColumns];
     __shared__ Meeting meeting;
     __shared__ uint4 bits[SPREAD ? kMostWarps : 1][32];
     __shared__ uint64_t bars[WARP ? kWarps : 1][kMostStages];
     Stream<WARP> stream(bars, SPREAD ? RowRing{0, 0} : p.ring);
     pdl_wait();
     if (p.release_early) pdl_release();
-    const Place<SPREAD, WARP> at(p.units, p.per_block, p.blocks, p.threads);
+    if (blockIdx.x >= p.row_blocks) {
+        sum_columns<T, R, W>(p, column_sums);
+        return;
+    }
+    const Place<SPREAD, WARP> at(p.units, p.per_block, p.blocks, p.threads, p.row_blocks);
     const uint32_t unit0 = WARP ? 0 : at.rank * p.per_block, own = at.end - unit0;
     const Piece pieces[3] = {{p.grad_out, p.grad_out_stride * kT, UnitT::bytes}, {p.sum, p.sum_stride * kR, UnitR::bytes}, {p.grad_sum, p.grad_sum_stride * kR, UnitR::bytes}};
     if (!SPREAD && stream.asks)
@@ -285,7 +315,7 @@ __global__ void __launch_bounds__(SPREAD ? 2 * kThreads : kThreads, SPREAD ? 1 :
 
 // ------------------------------------------------------------------------------------------------ launches
 
-template <auto KERNEL, typename P> cudaError_t launch_rows(const P &p, const RowShape &s, const RowDeal &d, cudaStream_t stream)
+template <auto KERNEL, typename P> cudaError_t launch_rows(const P &p, const RowShape &s, const RowDeal &d, cudaStream_t stream, size_t more_blocks = 0)
 {
     if (s.smem > 0) {
         static std::atomic<bool> ready[64];
@@ -298,7 +328,7 @@ template <auto KERNEL, typename P> cudaError_t launch_rows(const P &p, const Row
         if (e != cudaSuccess) return e;
     }
     cudaLaunchConfig_t c{};
-    c.gridDim = dim3(unsigned(s.groups * d.blocks));
+    c.gridDim = dim3(unsigned(s.groups * d.blocks + more_blocks));
     c.blockDim = dim3(d.threads);
     c.dynamicSmemBytes = s.smem;
     c.stream = stream;
@@ -361,10 +391,10 @@ template <> cudaError_t launch_norm_grad<RD_NORM_ROWS>(const NormGradParams &p, 
             using RT = decltype(R);
             using WT = decltype(W);
             if constexpr (SPREAD()) {
-                return launch_rows<rd_norm_grad_kernel<T, RT, WT, true, NV(), WARP(), kAsk>>(p, c.shape, c.deal, c.stream);
+                return launch_rows<rd_norm_grad_kernel<T, RT, WT, true, NV(), WARP(), kAsk>>(p, c.shape, c.deal, c.stream, c.more_blocks);
             } else {
-                if (p.drop.border) return launch_rows<rd_norm_grad_kernel<T, RT, WT, false, NV(), WARP(), kDrop>>(p, c.shape, c.deal, c.stream);
-                return launch_rows<rd_norm_grad_kernel<T, RT, WT, false, NV(), WARP(), kPlain>>(p, c.shape, c.deal, c.stream);
+                if (p.drop.border) return launch_rows<rd_norm_grad_kernel<T, RT, WT, false, NV(), WARP(), kDrop>>(p, c.shape, c.deal, c.stream, c.more_blocks);
+                return launch_rows<rd_norm_grad_kernel<T, RT, WT, false, NV(), WARP(), kPlain>>(p, c.shape, c.deal, c.stream, c.more_blocks);
             }
         });
     });

@@ -245,17 +245,17 @@ template <bool WARP> __device__ __forceinline__ float2 join_row(float2 v, bool w
     return v;
 }
 
-// Which rows and which units of them a thread has: unit, unit + step, ...  (`threads`: of the block.)
+// Which rows and which units of them a thread has: unit, unit + step, ...  (`threads`: of the block; `grid`: blocks that have rows.)
 template <bool SPREAD, bool WARP> struct Place {
     size_t row, rows;         // first row, and how many rows further the next is
     uint32_t unit, step, end, rank;
-    __device__ __forceinline__ Place(uint32_t units, uint32_t per_block, uint32_t blocks, uint32_t threads)
+    __device__ __forceinline__ Place(uint32_t units, uint32_t per_block, uint32_t blocks, uint32_t threads, uint32_t grid)
     {
         uint32_t thread;
         asm volatile("mov.u32 %0, %%tid.x;" : "=r"(thread));        // once
         if (WARP) {
             row = size_t(blockIdx.x) * kWarps + (thread >> 5);
-            rows = size_t(gridDim.x) * kWarps;
+            rows = size_t(grid) * kWarps;
             unit = thread & 31;
             step = 32;
             end = units;
@@ -263,7 +263,7 @@ template <bool SPREAD, bool WARP> struct Place {
         } else {
             rank = blocks > 1 ? cluster_rank() : 0;
             row = blocks > 1 ? blockIdx.x / blocks : blockIdx.x;
-            rows = blocks > 1 ? gridDim.x / blocks : gridDim.x;
+            rows = blocks > 1 ? grid / blocks : grid;
             unit = rank * per_block + thread;
             step = threads;
             end = min(units, (rank + 1) * per_block);

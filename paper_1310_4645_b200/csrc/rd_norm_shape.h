@@ -14,6 +14,7 @@ constexpr uint32_t kBlockUnits = 1024;    // units of 8 columns of a row that a 
 constexpr int kUnits = 4;                 // units that a thread has at most; two in the gradient without a ring, whose operands stay in registers
 constexpr int kMostWarps = 16;
 constexpr size_t kDropoutBlocks = 6;      // of dropout alone, an SM
+constexpr uint32_t kSumColumns = 16;      // of grad_weight, that a block sums up where rows are few
 constexpr uint32_t kMostStages = 8;
 constexpr size_t kRingBytes = 200 << 10;  // of an SM's shared memory that rows on their way may take
 constexpr size_t kSms = 148;
@@ -60,7 +61,9 @@ struct NormGradParams {
     const void *grad_out, *sum, *weight, *grad_sum;
     const float *rstd;
     void *grad_x, *grad_residual;
-    float *part;              // [groups][dim]: every group's part of grad_weight; null where it is not wanted
+    float *part;              // [groups][dim]: every group's part of grad_weight; null where it is not wanted, or summed up by columns
+    void *grad_weight;        // by columns: blocks beyond row_blocks
+    uint32_t row_blocks;
     size_t grad_out_stride, sum_stride, grad_sum_stride, grad_x_stride, grad_residual_stride, n;
     uint32_t dim, units, per_block, blocks, threads;
     float inv_dim;
@@ -133,6 +136,7 @@ struct NormCall {
     RowShape shape;
     int sum_dtype, weight_dtype;
     cudaStream_t stream;
+    size_t more_blocks;       // behind those that have rows
 };
 template <class T> cudaError_t launch_norm(const NormParams &p, const NormCall &c);
 template <class T> cudaError_t launch_norm_grad(const NormGradParams &p, const NormCall &c);

@@ -210,7 +210,7 @@ def test_norm_special_rows(dim):
 
 @gpu
 @pytest.mark.parametrize("dtype, sum_dtype, weight_dtype", TYPES)
-@pytest.mark.parametrize("n, dim, pad, offset", NORM_SHAPES + [(1000, 1024, 0, 0), (600, 1200, 0, 0), (700, 333, 0, 0)])
+@pytest.mark.parametrize("n, dim, pad, offset", NORM_SHAPES + [(1000, 1024, 0, 0), (600, 1200, 0, 0), (700, 333, 0, 0), (384, 264, 0, 0), (385, 265, 0, 0), (384, 2000, 3, 1), (385, 2000, 8, 0)])
 def test_norm_grad(dtype, sum_dtype, weight_dtype, n, dim, pad, offset):
     up = strided(rand(n, dim, seed=11, dtype=dtype), pad, offset)
     total = strided(rand(n, dim, seed=12, dtype=sum_dtype, std=2.0), pad, offset)
@@ -248,16 +248,17 @@ def test_norm_grad(dtype, sum_dtype, weight_dtype, n, dim, pad, offset):
 
 
 @gpu
-def test_norm_grad_weight_alone_and_no_rows():
+@pytest.mark.parametrize("n", [50, 500])
+def test_norm_grad_weight_alone_and_no_rows(n):
     L = rd.lib()
-    up, total, weight = rand(50, 96, seed=15), rand(50, 96, seed=16), rand(1, 96, seed=17)[0]
-    rstd = torch.ones(50, device="cuda")
+    up, total, weight = rand(n, 96, seed=15), rand(n, 96, seed=16), rand(1, 96, seed=17)[0]
+    rstd = torch.ones(n, device="cuda")
     _, _, want = rd.rd_norm_grad(up, total, weight, rstd)
     got = torch.empty_like(weight)
-    ws = torch.empty(rd.rd_norm_grad_workspace(50, 96), dtype=torch.uint8, device="cuda")
-    v = rd.rd_norm_grad_t(up.data_ptr(), 96, total.data_ptr(), 96, rstd.data_ptr(), weight.data_ptr(), None, 0, 50, 96, rd.RD_FP32, rd.RD_FP32, rd.RD_FP32, 0.0, 0, 0, 0)
+    ws = torch.empty(rd.rd_norm_grad_workspace(n, 96), dtype=torch.uint8, device="cuda")
+    v = rd.rd_norm_grad_t(up.data_ptr(), 96, total.data_ptr(), 96, rstd.data_ptr(), weight.data_ptr(), None, 0, n, 96, rd.RD_FP32, rd.RD_FP32, rd.RD_FP32, 0.0, 0, 0, 0)
     stream = torch.cuda.current_stream().cuda_stream
-    assert L.rd_norm_grad(C.byref(v), None, 0, None, 0, got.data_ptr(), ws.data_ptr(), ws.numel(), stream) == rd.RD_OK
+    assert L.rd_norm_grad(C.byref(v), None, 0, None, 0, got.data_ptr(), ws.data_ptr() if ws.numel() else None, ws.numel(), stream) == rd.RD_OK
     assert torch.equal(got, want)
     x, r, w = rd.rd_norm_grad(up[:0], total[:0], weight, rstd[:0])
     assert x.shape == (0, 96) and not w.any()
@@ -267,10 +268,11 @@ def test_norm_grad_weight_alone_and_no_rows():
 
 
 @gpu
-@pytest.mark.parametrize("dim", [24, 1040, 8208])
-def test_norm_grad_in_place(dim):
-    up, total, more = (rand(21, dim, seed=18 + k, dtype=BF16) for k in range(3))
-    weight, rstd = rand(1, dim, seed=21, dtype=BF16)[0], torch.rand(21, generator=gen(22), device="cuda")
+@pytest.mark.parametrize("n", [21, 384, 385])
+@pytest.mark.parametrize("dim", [24, 1040, 1041, 8208])
+def test_norm_grad_in_place(n, dim):
+    up, total, more = (rand(n, dim, seed=18 + k, dtype=BF16) for k in range(3))
+    weight, rstd = rand(1, dim, seed=21, dtype=BF16)[0], torch.rand(n, generator=gen(22), device="cuda")
     gx, gr, gw = rd.rd_norm_grad(up, total, weight, rstd, more, drop=0.2, seed=1)
     for x_into, r_into in ((0, 1), (1, 2), (2, 0), (0, 2)):
         t = [up.clone(), total.clone(), more.clone()]
@@ -375,14 +377,15 @@ def test_norm_refusals():
 
 def test_norm_grad_refusals():
     L, need = rd.lib(), C.c_size_t()
-    assert L.rd_norm_grad_workspace(4, 8, C.byref(need)) == rd.RD_OK and need.value >= 32
+    assert L.rd_norm_grad_workspace(4, 8, C.byref(need)) == rd.RD_OK and need.value == 0          # few rows
+    assert L.rd_norm_grad_workspace(1000, 8, C.byref(need)) == rd.RD_OK and need.value >= 32
     assert L.rd_norm_grad_workspace(4, 8, None) == L.rd_norm_grad_workspace(4, 0, C.byref(need)) == L.rd_norm_grad_workspace(4, 65537, C.byref(need)) == rd.RD_ERR_INVALID_ARG
     assert L.rd_norm_grad_workspace(1 << 31, 8, C.byref(need)) == rd.RD_ERR_UNSUPPORTED
 
     def call(gx, gxs, gr, grs, gw, ws, size, **kw):
         return L.rd_norm_grad(C.byref(rd.rd_norm_grad_t(*kw.values())), gx, gxs, gr, grs, gw, ws, size, None)
 
-    good = dict(gx=5 * P, gxs=8, gr=6 * P, grs=8, gw=7 * P, ws=8 * P, size=need.value, up=P, ups=8, sum=2 * P, ss=8, rstd=3 * P, weight=4 * P, more=9 * P, ms=8, n=4, dim=8,
+    good = dict(gx=5 * P, gxs=8, gr=6 * P, grs=8, gw=7 * P, ws=8 * P, size=need.value, up=P, ups=8, sum=2 * P, ss=8, rstd=3 * P, weight=4 * P, more=9 * P, ms=8, n=1000, dim=8,
                 dtype=rd.RD_BF16, sum_dtype=rd.RD_BF16, weight_dtype=rd.RD_BF16, drop=0.0, seed=0, offset=0, first=0)
     refused(call, good, [dict(gx=None, gr=None, gw=None), dict(up=None), dict(sum=None), dict(rstd=None), dict(weight=None), dict(up=P + 1), dict(sum=2 * P + 1), dict(rstd=3 * P + 2),
                          dict(weight=4 * P + 1), dict(gx=5 * P + 1), dict(gr=6 * P + 1), dict(gw=7 * P + 1), dict(more=9 * P + 1), dict(ws=None), dict(ws=8 * P + 128), dict(ups=7),
