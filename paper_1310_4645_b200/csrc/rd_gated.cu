@@ -92,20 +92,47 @@ struct Out {
     size_t stride;
     int units;                // elements that an access may take: 8, 2 or 1
 };
-// 16 values of a row from column `col` on, of which the row has `left`.
-__device__ __forceinline__ void put16(const Out &o, size_t row, uint32_t col, uint32_t left, const uint32_t (&v)[8])
+// 16 columns of a warp's 32 rows from column `col` on, of which there are `left`; a lane has a row's.  Where rows do not begin on 16-byte
+// boundaries the values change places in 1 KB of shared memory, so that a store has few rows: 4096 x 2048 x 8191 bf16 404 us
+// with a lane's values stored by itself, gate and up kept 974; STAGED so (B200).
+__device__ __forceinline__ void put16(const Out &o, uint32_t stage, uint32_t row0, uint32_t rows, uint32_t col, uint32_t left, const uint32_t (&v)[8])
 {
-    uint16_t *dst = o.p + row * o.stride + col;
-    if (o.units == 8 && left >= 16) {
-        reinterpret_cast<uint4 *>(dst)[0] = make_uint4(v[0], v[1], v[2], v[3]);
-        reinterpret_cast<uint4 *>(dst)[1] = make_uint4(v[4], v[5], v[6], v[7]);
-    } else if (o.units >= 2 && left >= 16) {
+    const uint32_t lane = threadIdx.x & 31;
+    if (o.units == 8) {
+        if (lane >= rows) return;
+        uint16_t *dst = o.p + size_t(row0 + lane) * o.stride + col;
+        if (left >= 8) reinterpret_cast<uint4 *>(dst)[0] = make_uint4(v[0], v[1], v[2], v[3]);
+        if (left >= 16) {
+            reinterpret_cast<uint4 *>(dst)[1] = make_uint4(v[4], v[5], v[6], v[7]);
+        } else {
 #pragma unroll
-        for (int j = 0; j < 8; j++) reinterpret_cast<uint32_t *>(dst)[j] = v[j];
+            for (int j = 0; j < 16; j++)
+                if (j < left && (j >= 8 || left < 8)) dst[j] = uint16_t(v[j / 2] >> (j & 1 ? 16 : 0));
+        }
+        return;
+    }
+    __syncwarp();
+    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(stage + lane * 32), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]) : "memory");
+    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(stage + lane * 32 + 16), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]) : "memory");
+    __syncwarp();
+    if (o.units == 2) {
+#pragma unroll
+        for (uint32_t i = 0; i < 8; i++) {
+            const uint32_t r = 4 * i + lane / 8, j = lane % 8 * 2;
+            uint32_t x;
+            asm volatile("ld.shared.b32 %0, [%1];" : "=r"(x) : "r"(stage + r * 32 + j * 2) : "memory");
+            uint16_t *dst = o.p + size_t(row0 + r) * o.stride + col + j;
+            if (r < rows && j + 1 < left) *reinterpret_cast<uint32_t *>(dst) = x;
+            else if (r < rows && j < left) *dst = uint16_t(x);
+        }
     } else {
 #pragma unroll
-        for (int j = 0; j < 16; j++)
-            if (j < left) dst[j] = uint16_t(v[j / 2] >> (j & 1 ? 16 : 0));
+        for (uint32_t i = 0; i < 16; i++) {
+            const uint32_t r = 2 * i + lane / 16, j = lane % 16;
+            uint16_t x;
+            asm volatile("ld.shared.u16 %0, [%1];" : "=h"(x) : "r"(stage + r * 32 + j * 2) : "memory");
+            if (r < rows && j < left) o.p[size_t(row0 + r) * o.stride + col + j] = x;
+        }
     }
 }
 
@@ -115,6 +142,7 @@ struct alignas(64) GatedParams {
     uint32_t n, width, steps; // steps: of 128 bytes of the summed index
     uint32_t tile_w;          // columns of a tile, of each projection
     uint32_t stages, stage, a_rows;
+    uint32_t staging;         // where in shared memory results change places, 1 KB a warp
     uint32_t group;           // row tiles that go over the width together
     uint32_t idesc;
     int act;
@@ -362,7 +390,7 @@ __global__ void __launch_bounds__(kMmaThreads, 1) rd_gated_mma_kernel(const __gr
             if (dead) drain();
         }
     } else if (warp >= 4) {
-        const int quarter = warp & 3, half = (warp - 4) >> 2;        // rows 32 * quarter.. of the tile; every other 16 columns, or half of them
+        const int quarter = warp & 3, half = (warp - 4) >> 2;        // rows 32 * quarter.. of the tile, half of its columns
         uint32_t tile = 0;
         while (plan.next(w)) {
             const uint32_t row0 = w.m0 + rank * kRowsM + 32 * quarter, row = row0 + lane, buf = tile & 1;
@@ -376,20 +404,20 @@ __global__ void __launch_bounds__(kMmaThreads, 1) rd_gated_mma_kernel(const __gr
                 if (lane == 0) bar_arrive_leader<CG>(acc_empty + 8 * buf);
             };
             if constexpr (!GRADS) {
-                const bool live = row < p.n;
-                const float x_scale = F8 && live ? p.x_scale[row] : 1.0f;
-                const uint32_t chunks = p.tile_w / 16;
-                if (uint32_t(half) >= chunks) release();
-                for (uint32_t c = half; c < chunks; c += 2) {
+                const float x_scale = F8 && row < p.n ? p.x_scale[row] : 1.0f;
+                // a tile's columns by 16, half of them each warp's; the last 16 may be 8, and what lies behind them the other projection's
+                const uint32_t chunks = (p.tile_w + 15) / 16, first = half ? (chunks + 1) / 2 : 0, last = half ? chunks : (chunks + 1) / 2;
+                const uint32_t columns = min(p.tile_w, p.width - w.n0), rows = row0 < p.n ? min(32u, p.n - row0) : 0, stage = smem + p.staging + (warp - 4) * 1024;
+                if (first >= last) release();
+                for (uint32_t c = first; c < last; c++) {
                     uint32_t g[16], u[16];
                     tmem_load(acc + 16 * c, g);
                     tmem_load(acc + p.tile_w + 16 * c, u);
                     tmem_wait(g);
                     tmem_wait(u);
-                    if (c + 2 >= chunks) release();
-                    const uint32_t col = w.n0 + 16 * c;
-                    if (col >= p.width) continue;
-                    const uint32_t left = p.width - col;
+                    if (c + 1 == last) release();
+                    if (16 * c >= columns) continue;
+                    const uint32_t col = w.n0 + 16 * c, left = columns - 16 * c;
                     if (F8) {
 #pragma unroll
                         for (int j = 0; j < 16; j++) {
@@ -398,25 +426,23 @@ __global__ void __launch_bounds__(kMmaThreads, 1) rd_gated_mma_kernel(const __gr
                             u[j] = __float_as_uint(__uint_as_float(u[j]) * (x_scale * __ldg(p.up_scale + at)));
                         }
                     }
-                    if (live) {
-                        uint32_t o[8];
-                        with_act(p.act, [&](auto ACT) {
+                    uint32_t o[8];
+                    with_act(p.act, [&](auto ACT) {
 #pragma unroll
-                            for (int j = 0; j < 8; j++)
-                                o[j] = pack2(p.bf16, act_value<decltype(ACT)::value>(__uint_as_float(g[2 * j])) * __uint_as_float(u[2 * j]),
-                                             act_value<decltype(ACT)::value>(__uint_as_float(g[2 * j + 1])) * __uint_as_float(u[2 * j + 1]));
-                        });
-                        put16(p.out, row, col, left, o);
-                        if (p.kept_gate.p) {
+                        for (int j = 0; j < 8; j++)
+                            o[j] = pack2(p.bf16, act_value<decltype(ACT)::value>(__uint_as_float(g[2 * j])) * __uint_as_float(u[2 * j]),
+                                         act_value<decltype(ACT)::value>(__uint_as_float(g[2 * j + 1])) * __uint_as_float(u[2 * j + 1]));
+                    });
+                    put16(p.out, stage, row0, rows, col, left, o);
+                    if (p.kept_gate.p) {
 #pragma unroll
-                            for (int j = 0; j < 8; j++) o[j] = pack2(p.bf16, __uint_as_float(g[2 * j]), __uint_as_float(g[2 * j + 1]));
-                            put16(p.kept_gate, row, col, left, o);
-                        }
-                        if (p.kept_up.p) {
+                        for (int j = 0; j < 8; j++) o[j] = pack2(p.bf16, __uint_as_float(g[2 * j]), __uint_as_float(g[2 * j + 1]));
+                        put16(p.kept_gate, stage, row0, rows, col, left, o);
+                    }
+                    if (p.kept_up.p) {
 #pragma unroll
-                            for (int j = 0; j < 8; j++) o[j] = pack2(p.bf16, __uint_as_float(u[2 * j]), __uint_as_float(u[2 * j + 1]));
-                            put16(p.kept_up, row, col, left, o);
-                        }
+                        for (int j = 0; j < 8; j++) o[j] = pack2(p.bf16, __uint_as_float(u[2 * j]), __uint_as_float(u[2 * j + 1]));
+                        put16(p.kept_up, stage, row0, rows, col, left, o);
                     }
                     __syncwarp();                // the next load of the accumulators is the whole warp's
                 }
@@ -494,13 +520,48 @@ __global__ void __launch_bounds__(kMmaThreads, 1) rd_gated_mma_kernel(const __gr
 
 // ------------------------------------------------------------------------------------------------ beside the products
 
-// Copies a matrix whose rows TMA cannot address (unaligned base or stride) to rows that it can, a warp a row.
-template <typename E> __global__ void __launch_bounds__(256) rd_gated_align_kernel(E *dst, size_t dst_stride, const E *src, size_t src_stride, size_t rows, uint32_t dim)
+// Copies of matrices whose rows TMA cannot address (unaligned base or stride) in rows that it can, all of a call's in one launch: a warp
+// copies 1 KB of a row at a time, words of 4 bytes put together from what the source's alignment allows.
+constexpr uint32_t kCopyBytes = 1024;
+struct CopyParams {
+    struct {
+        char *dst;
+        const char *src;
+        size_t dst_stride, src_stride, first, chunks;     // bytes; number of the first chunk, chunks of a row
+        uint32_t bytes;       // of a row
+    } m[3];
+    uint32_t matrices;
+    size_t total;             // chunks
+};
+template <typename E> __device__ __forceinline__ uint32_t word_of(const char *src, uint32_t left)
+{
+    uint32_t w = 0;
+#pragma unroll
+    for (uint32_t i = 0; i < 4; i += sizeof(E))
+        if (i < left) w |= uint32_t(*reinterpret_cast<const E *>(src + i)) << 8 * (i % 4);
+    return w;
+}
+__global__ void __launch_bounds__(256) rd_gated_align_kernel(const __grid_constant__ CopyParams p)
 {
     pdl_start();
-    for (size_t r = size_t(blockIdx.x) * 8 + (threadIdx.x >> 5); r < rows; r += size_t(gridDim.x) * 8) {
-#pragma unroll 4
-        for (uint32_t j = threadIdx.x & 31; j < dim; j += 32) dst[r * dst_stride + j] = src[r * src_stride + j];
+    const uint32_t lane = threadIdx.x & 31;
+    for (size_t c = size_t(blockIdx.x) * 8 + (threadIdx.x >> 5); c < p.total; c += size_t(gridDim.x) * 8) {
+        const auto &m = p.matrices > 2 && c >= p.m[2].first ? p.m[2] : p.matrices > 1 && c >= p.m[1].first ? p.m[1] : p.m[0];
+        const size_t row = (c - m.first) / m.chunks;
+        const uint32_t at = uint32_t((c - m.first) % m.chunks) * kCopyBytes + lane * 4;
+        const char *src = m.src + row * m.src_stride;
+        char *dst = m.dst + row * m.dst_stride;
+        const uint32_t odd = uint32_t(reinterpret_cast<uintptr_t>(src)) & 3;
+        uint32_t w[kCopyBytes / 128];
+#pragma unroll
+        for (uint32_t i = 0; i < kCopyBytes / 128; i++) {
+            const uint32_t j = at + 128 * i, left = j < m.bytes ? m.bytes - j : 0;
+            w[i] = odd & 1 ? word_of<uint8_t>(src + j, left) : odd || left < 4 ? m.bytes & 1 ? word_of<uint8_t>(src + j, left) : word_of<uint16_t>(src + j, left) : word_of<uint32_t>(src + j, left);
+        }
+        // a word that begins in a row lies in the copy's, which is a multiple of 128 bytes
+#pragma unroll
+        for (uint32_t i = 0; i < kCopyBytes / 128; i++)
+            if (at + 128 * i < m.bytes) *reinterpret_cast<uint32_t *>(dst + at + 128 * i) = w[i];
     }
 }
 
@@ -657,30 +718,30 @@ Layout lay_out(const GatedArgs &a, bool gradient, bool want_x)
     return l;
 }
 
-// An aligned operand: the caller's, or its copy, made by this call.
+// An operand that TMA can address: the caller's, or its copy, made by this call.
 struct Operand {
     const void *p;
     size_t stride;
 };
-cudaError_t align(Operand *o, const void *p, size_t stride, size_t rows, size_t dim, void *copy, size_t copy_stride, size_t esize, cudaStream_t stream)
-{
-    *o = Operand{p, stride};
-    if (!copy) return cudaSuccess;
-    *o = Operand{copy, copy_stride};
-    const unsigned blocks = unsigned(rows < 8 * 1184 ? (rows + 7) / 8 : 1184);
-    if (esize == 1) return launch(rd_gated_align_kernel<uint8_t>, blocks, 256, stream, static_cast<uint8_t *>(copy), copy_stride, static_cast<const uint8_t *>(p), stride, rows, uint32_t(dim));
-    return launch(rd_gated_align_kernel<uint16_t>, blocks, 256, stream, static_cast<uint16_t *>(copy), copy_stride, static_cast<const uint16_t *>(p), stride, rows, uint32_t(dim));
-}
 struct Operands {
     Operand x, gate, up;
 };
 cudaError_t align_all(Operands *o, const GatedArgs &a, const Layout &l)
 {
-    const size_t esize = bytes_of(a.dtype);
-    cudaError_t e = align(&o->x, a.x, a.x_stride, a.n, a.dim, l.x, l.copy_stride, esize, a.stream);
-    if (e == cudaSuccess) e = align(&o->gate, a.gate_weight, a.gate_weight_stride, a.width, a.dim, l.gate_weight, l.copy_stride, esize, a.stream);
-    if (e == cudaSuccess) e = align(&o->up, a.up_weight, a.up_weight_stride, a.width, a.dim, l.up_weight, l.copy_stride, esize, a.stream);
-    return e;
+    const size_t esize = bytes_of(a.dtype), chunks = (a.dim * esize + kCopyBytes - 1) / kCopyBytes;
+    CopyParams p{};
+    auto operand = [&](const void *given, size_t stride, size_t rows, void *copy) {
+        if (!copy) return Operand{given, stride};
+        p.m[p.matrices++] = {static_cast<char *>(copy), static_cast<const char *>(given), l.copy_stride * esize, stride * esize, p.total, chunks, uint32_t(a.dim * esize)};
+        p.total += rows * chunks;
+        return Operand{copy, l.copy_stride};
+    };
+    o->x = operand(a.x, a.x_stride, a.n, l.x);
+    o->gate = operand(a.gate_weight, a.gate_weight_stride, a.width, l.gate_weight);
+    o->up = operand(a.up_weight, a.up_weight_stride, a.width, l.up_weight);
+    if (!p.total) return cudaSuccess;
+    const size_t blocks = (p.total + 7) / 8;
+    return launch(rd_gated_align_kernel, unsigned(blocks < 8192 ? blocks : 8192), 256, a.stream, p);
 }
 
 // A matrix of 8-bit values, read in boxes of 128 values x box_rows rows.
@@ -714,12 +775,12 @@ uint32_t row_group(size_t row_bytes, size_t tile_m)
     return uint32_t(g < 1 ? 1 : g > 64 ? 64 : g);
 }
 
-// Columns of a tile (of each projection): what takes the fewest turns of the groups of thread blocks, by the columns of a turn.  Pairs
-// compute narrow tiles at the rate that the left operand comes out of shared memory, as if they had 48 columns.
+// Columns of a tile (of each projection), a multiple of 8 (pairs: 16, as their products want it): what takes the fewest turns of the groups of thread blocks, by the columns of a
+// turn.  Pairs compute narrow tiles at the rate that the left operand comes out of shared memory, as if they had 48 columns.
 uint32_t tile_columns(size_t tiles_m, size_t width, size_t groups, bool pairs)
 {
     size_t best = 128, best_cost = 0;
-    for (size_t w = 128; w >= 16; w -= 16) {
+    for (size_t w = 128; w >= 16; w -= pairs ? 16 : 8) {
         const size_t turns = (tiles_m * ((width + w - 1) / w) + groups - 1) / groups, cost = turns * ((pairs && w < 48 ? 48 : w) + 8);
         if (w == 128 || cost < best_cost) best = w, best_cost = cost;
     }
@@ -771,16 +832,21 @@ cudaError_t gated_forward(const GatedArgs &a)
     p.steps = uint32_t((a.dim * esize + 127) / 128);
     p.tile_w = tile_columns(tiles_m, a.width, kSms / cg, cg == 2);
     p.a_rows = rows_in(a.n);
-    const Ring r = ring_of(cg == 2 ? ShapeOf<false, 2>::ring : ShapeOf<false, 1>::ring, p.a_rows, 2 * p.tile_w / uint32_t(cg));
+    p.out = out_of(a.out, a.out_stride);
+    p.kept_gate = out_of(a.gate, a.gate_stride);
+    p.kept_up = out_of(a.up, a.up_stride);
+    // the ring has the room, but for what results change places in
+    bool staged = false;
+    for (const Out &o : {p.out, p.kept_gate, p.kept_up}) staged |= o.p && o.units != 8;
+    const uint32_t room = cg == 2 ? ShapeOf<false, 2>::ring : ShapeOf<false, 1>::ring;
+    p.staging = room - kEpilogueWarps * 1024;
+    const Ring r = ring_of(staged ? p.staging : room, p.a_rows, 2 * p.tile_w / uint32_t(cg));
     p.stage = r.stage;
     p.stages = r.stages;
     p.group = row_group(a.dim * esize, tile_m);
     p.idesc = descriptor(a.dtype, 2 * p.tile_w, uint32_t(tile_m));
     p.act = a.activation;
     p.bf16 = a.out_dtype == RD_BF16;
-    p.out = out_of(a.out, a.out_stride);
-    p.kept_gate = out_of(a.gate, a.gate_stride);
-    p.kept_up = out_of(a.up, a.up_stride);
     p.x_scale = a.x_scale;
     p.gate_scale = a.gate_scale;
     p.up_scale = a.up_scale;

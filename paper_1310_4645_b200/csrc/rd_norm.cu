@@ -113,7 +113,7 @@ bool in_units(const void *p, size_t stride, int dtype)
 // Whether grad_weight is summed up by blocks of its own beside the rows', 16 columns each, instead of from the groups' parts by another
 // launch: few rows and not too many columns, which are read twice.  B200, us a call, this and the other way: 16 rows of 1000 bf16 5.1
 // and 7.1, 257 of them 5.1 and 7.1, 384 6.2 and 7.4; 100 rows of 4096 5.2 and 6.9, 320 7.9 and 7.8, 384 11.0 and 8.0.
-bool by_columns(size_t n, size_t dim, const RowDeal &d) { return n <= 384 && n * dim <= size_t(1) << 20 && d.blocks == 1; }
+bool by_columns(size_t n, size_t dim) { return n <= 384 && n * dim <= size_t(1) << 20; }
 
 }  // namespace
 
@@ -121,8 +121,9 @@ cudaError_t norm_forward(const NormArgs &a)
 {
     const bool spread = a.dim % 8 != 0 || !in_units(a.x, a.x_stride, a.dtype) || !in_units(a.residual, a.residual_stride, a.sum_dtype) || !in_units(a.weight, 0, a.weight_dtype) ||
                         !in_units(a.out, a.out_stride, a.out_dtype) || !in_units(a.sum, a.sum_stride, a.sum_dtype);
-    const RowDeal d = deal(a.dim, kFour);
-    const RowShape shape = shape_of(a.n, d, spread ? 0 : 8 * (size_of(a.dtype) + (a.residual ? size_of(a.sum_dtype) : 0)));
+    const size_t unit_bytes = spread ? 0 : 8 * (size_of(a.dtype) + (a.residual ? size_of(a.sum_dtype) : 0));
+    const RowDeal d = deal(a.dim, unit_bytes, false);
+    const RowShape shape = shape_of(a.n, d, unit_bytes);
     NormParams p{};
     p.ring = shape.ring;
     p.x = a.x;
@@ -153,10 +154,14 @@ cudaError_t norm_forward(const NormArgs &a)
 
 size_t norm_backward_workspace(size_t n, size_t dim)
 {
-    // a part of grad_weight of every group; fewest bytes a value, most groups
-    if (by_columns(n, dim, deal(dim, kFew))) return 0;
-    const size_t whole = shape_of(n, deal(dim, kFew), 8 * 4).groups, spread = shape_of(n, deal(dim, kFewAlways), 0).groups;
-    return (whole > spread ? whole : spread) * dim * sizeof(float);
+    if (by_columns(n, dim)) return 0;
+    // a part of grad_weight of every group: the most that any types, strides and inputs give (two or three matrices of 2 or 4 bytes a value)
+    size_t most = 0;
+    for (const size_t unit_bytes : {0, 32, 48, 64, 80, 96}) {
+        const size_t groups = shape_of(n, deal(dim, unit_bytes, true), unit_bytes).groups;
+        most = groups > most ? groups : most;
+    }
+    return most * dim * sizeof(float);
 }
 
 cudaError_t norm_backward(const NormGradArgs &a)
@@ -164,11 +169,12 @@ cudaError_t norm_backward(const NormGradArgs &a)
     const bool spread = a.dim % 8 != 0 || !in_units(a.grad_out, a.grad_out_stride, a.dtype) || !in_units(a.sum, a.sum_stride, a.sum_dtype) || !in_units(a.weight, 0, a.weight_dtype) ||
                         !in_units(a.grad_sum, a.grad_sum_stride, a.sum_dtype) || !in_units(a.grad_x, a.grad_x_stride, a.dtype) ||
                         !in_units(a.grad_residual, a.grad_residual_stride, a.sum_dtype);
-    RowDeal d = deal(a.dim, spread ? kFewAlways : kFew);
-    const bool few = a.n > 0 && by_columns(a.n, a.dim, d), columns = few && a.grad_weight;
+    const size_t unit_bytes = spread ? 0 : 8 * (size_of(a.dtype) + size_of(a.sum_dtype) * (a.grad_sum ? 2 : 1));
+    RowDeal d = deal(a.dim, unit_bytes, true);
+    const bool few = a.n > 0 && by_columns(a.n, a.dim), columns = few && a.grad_weight;
     // blocks that columns want; whether they are wanted or not, so that the rows' bits do not depend on it
     if (few && d.threads < kThreads) d.threads = kThreads;
-    RowShape shape = shape_of(a.n, d, spread ? 0 : 8 * (size_of(a.dtype) + size_of(a.sum_dtype) * (a.grad_sum ? 2 : 1)));
+    RowShape shape = shape_of(a.n, d, unit_bytes);
     // where warps have rows, their parts of grad_weight are joined in shared memory
     if (d.warp && shape.smem < kWarps * a.dim * sizeof(float)) shape.smem = kWarps * a.dim * sizeof(float);
     NormGradParams p{};
@@ -204,7 +210,7 @@ cudaError_t norm_backward(const NormGradArgs &a)
     auto run = [&](const NormGradParams &q, const NormCall &c) {
         return a.dtype == RD_FP32 ? launch_norm_grad<F32>(q, c) : a.dtype == RD_BF16 ? launch_norm_grad<B16>(q, c) : launch_norm_grad<H16>(q, c);
     };
-    NormCall call{spread, d, shape, a.sum_dtype, a.weight_dtype, a.stream, columns ? (a.dim + kSumColumns - 1) / kSumColumns : 0};
+    NormCall call{spread, d, shape, a.sum_dtype, a.weight_dtype, a.stream, columns ? ((a.dim + kSumColumns - 1) / kSumColumns + d.blocks - 1) / d.blocks * d.blocks : 0};
     cudaError_t e = cudaSuccess;
     bool in_place = false;        // gradients in the place of what the columns read
     for (const void *w : {a.grad_x, a.grad_residual}) in_place |= w && (w == a.grad_out || w == a.sum);

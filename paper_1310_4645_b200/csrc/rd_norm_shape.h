@@ -71,41 +71,44 @@ struct NormGradParams {
     bool want_rows, release_early;
 };
 
-// How a row is dealt out: to a warp if that holds it with four units a thread (`few`: two), or else to as few warps of a thread block
-// as hold it with four, so that the join of a row costs few instructions a value, or to a cluster of up to eight blocks.
-// few: two units a thread and twice the warps while one block of them holds the row; beyond that only where registers hold no more
-// (`always`).  The gradient of 16384 x 4096 bf16 with dropout takes 129 us so, 137 with four (B200); of 8192 x 8192, with blocks of 512
-// threads, 106 and 101.
+// How a row is dealt out, brought in and how many rows at a time.
+//   A warp has a row if it holds it with four units a thread (`few`: two), else as few warps of a thread block as hold it with four, so that
+//   the join of a row costs few instructions a value, or a cluster of up to eight blocks.
+//   few (the gradient): two units a thread and twice the warps while one block of them holds a block's part; without a ring always, because
+//   operands stay in registers then.  The gradient of 16384 x 4096 bf16 with dropout takes 129 us so, 137 with four (B200).
+//   A cluster has as few blocks as hold the row: its meetings cost more than blocks an SM gain (gradient of 8192 x 16384 bf16 by two blocks
+//   245 us, by four 430).
+//   As many groups (a block of warps with a row each, or the blocks of one row) as registers (80 a thread with a ring, 128 without) and
+//   shared memory with two stages or more allow.
+// unit_bytes: of all matrices that come in by the ring, for 8 columns; 0: none does.
 struct RowDeal {
     uint32_t units, per_block, blocks, threads;
     int nv;                   // units a thread
     bool warp;
 };
-enum RowUnits { kFour, kFew, kFewAlways };
-inline RowDeal deal(size_t dim, RowUnits wanted)
+inline RowDeal deal(size_t dim, size_t unit_bytes, bool few)
 {
     RowDeal d{};
     d.units = uint32_t((dim + 7) / 8);
-    const bool few = wanted == kFewAlways || (wanted == kFew && d.units > 32 * kUnits && d.units <= kThreads * kUnits / 2);
-    d.nv = few ? kUnits / 2 : kUnits;
-    d.warp = d.units <= uint32_t(32 * d.nv);
     d.blocks = 1;
     d.threads = kThreads;
     d.per_block = d.units;
-    if (d.warp) {
+    if (d.units <= uint32_t(32 * (few && !unit_bytes ? kUnits / 2 : kUnits))) {
+        d.warp = true;
+        d.nv = few && !unit_bytes ? kUnits / 2 : kUnits;
         while (d.nv > 1 && d.units <= uint32_t(16 * d.nv)) d.nv /= 2;
         return d;
     }
-    while ((d.units + d.blocks - 1) / d.blocks > kBlockUnits) d.blocks *= 2;
-    // whole warps' columns, so that no 256 columns are two blocks'
-    d.per_block = ((d.units + d.blocks - 1) / d.blocks + 31) / 32 * 32;
+    auto part = [&] { return (d.units + d.blocks - 1) / d.blocks; };
+    while (part() > kBlockUnits) d.blocks *= 2;
+    // whole warps' columns, so that no 256 columns are two blocks'; then perhaps fewer blocks, none without columns
+    d.per_block = (part() + 31) / 32 * 32;
+    d.blocks = (d.units + d.per_block - 1) / d.per_block;
+    d.nv = few && (!unit_bytes || d.per_block <= uint32_t(kThreads * kUnits / 2)) ? kUnits / 2 : kUnits;
     d.threads = (d.per_block + 32 * d.nv - 1) / (32 * d.nv) * 32;
     return d;
 }
 
-// How many groups of threads (a block of warps with a row each, or the blocks of one row) work at a time, and the ring of each block
-// (unit_bytes: of all matrices that come in, for 8 columns; 0: none): as many blocks an SM as registers allow (80 a thread with a ring)
-// and shared memory with two stages or more.
 struct RowShape {
     size_t groups, smem;
     bool one_turn;            // no group has more than one row

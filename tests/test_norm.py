@@ -7,6 +7,9 @@ pairs, warps and thread blocks: fewer than 64 additions on any value's way, each
 """
 import ctypes as C
 import math
+import os
+import shutil
+import subprocess
 
 import numpy as np
 import pytest
@@ -16,6 +19,7 @@ import paper_1310_4645_b200 as rd
 from test_vocab import TINY, U, gen, ints, rand, strided, within
 
 gpu = pytest.mark.gpu
+CSRC = os.path.join(os.path.dirname(os.path.abspath(rd.__file__)), "csrc")
 E = 2.0 ** -24
 BF16, FP16, FP32, E4M3 = torch.bfloat16, torch.float16, torch.float32, torch.float8_e4m3fn
 # rows' type, type of residual and sum, type of the weight
@@ -52,6 +56,40 @@ def kept(n, dim, drop, seed=0, offset=0, first=0):
     bits = np.stack([w >> np.uint64(s) & np.uint64(0xFFFF) for w in words for s in (0, 16)], -1).reshape(n, units * 8)[:, :dim]
     factor = float(np.float32(65536 / (65536 - border)))
     return torch.from_numpy((bits >= border) * factor).cuda()
+
+
+DEALS = r"""
+#include <cstdio>
+#include "rd_norm_shape.h"
+using namespace rd;
+int main()
+{
+    int bad = 0;
+    for (size_t dim = 1; dim <= 65536; dim++)
+        for (const size_t unit_bytes : {0, 16, 32, 48, 64, 80, 96})
+            for (const bool few : {false, true}) {
+                const RowDeal d = deal(dim, unit_bytes, few);
+                const RowShape s = shape_of(1000, d, unit_bytes);
+                const size_t all = size_t(d.per_block) * d.blocks, threads = d.warp ? 32 : d.threads;
+                // every unit is somebody's, every block has some, no thread more than its registers hold, no stage beyond the ring
+                bool ok = all >= d.units && all - d.per_block < d.units && size_t(d.nv) * threads >= d.per_block && d.blocks <= 8 && (d.blocks == 1 || d.per_block % 32 == 0);
+                ok = ok && d.threads % 32 == 0 && d.threads <= (unit_bytes ? 256 : 512) && (d.warp || d.threads >= 64) && s.groups > 0;
+                if (unit_bytes) ok = ok && s.ring.stages >= 2 && s.ring.stages <= kMostStages && s.ring.stage >= d.per_block * unit_bytes && s.smem <= kRingBytes && s.smem >= size_t(s.ring.stages) * s.ring.stage * (d.warp ? kWarps : 1);
+                if (!ok) bad += std::printf("dim %zu, %zu bytes, few %d\n", dim, unit_bytes, few) > 0;
+            }
+    return bad != 0;
+}
+"""
+
+
+def test_rows_are_dealt_out(tmp_path):
+    """Which threads have which columns, and the shared memory that rows come in through, for every row length, on the host."""
+    source, program = tmp_path / "deals.cpp", tmp_path / "deals"
+    source.write_text(DEALS)
+    include = ["-I", CSRC, "-I", os.path.join(os.path.dirname(shutil.which("nvcc") or "/usr/local/cuda/bin/nvcc"), "..", "include")]
+    subprocess.check_call(["g++", "-std=c++17", "-O1", *include, "-o", str(program), str(source)])
+    done = subprocess.run([str(program)], capture_output=True, text=True)
+    assert done.returncode == 0, done.stdout[:2000]
 
 
 # ------------------------------------------------------------------------------------------------ dropout
@@ -112,7 +150,8 @@ def norm_reference(x, weight, residual, eps, keep):
 
 NORM_SHAPES = [(1, 1, 0, 0), (1, 8, 0, 0), (3, 7, 0, 0), (9, 64, 0, 0), (20, 65, 0, 0), (8, 256, 0, 0), (9, 264, 8, 0), (17, 512, 0, 0), (40, 1000, 0, 0), (40, 1000, 3, 1), (31, 1024, 0, 0),
                (33, 1025, 0, 0), (33, 1032, 0, 0), (5, 2048, 0, 0), (5, 2056, 8, 8), (300, 4096, 0, 0), (3, 8192, 0, 0), (3, 8200, 0, 0), (3, 8193, 0, 0), (2, 16384, 0, 0),
-               (2, 20001, 0, 0), (3, 65536, 0, 0), (2, 65535, 0, 0), (5000, 72, 0, 0)]
+               (2, 20001, 0, 0), (3, 65536, 0, 0), (2, 65535, 0, 0), (5000, 72, 0, 0),
+               (2, 3048, 0, 0), (2, 8240, 0, 0), (2, 12320, 0, 0), (3, 24584, 0, 0)]
 
 
 @gpu
