@@ -622,33 +622,43 @@ template <int V> __global__ void __launch_bounds__(256) rd_gated_slope_kernel(co
     }
 }
 
-// Adds the parts of dx in order and rounds.
+// Adds the parts of dx and rounds: four threads to four columns, each with every fourth part in order, then those in order.
+constexpr uint32_t kFinishColumns = 256;
 __global__ void __launch_bounds__(256) rd_gated_finish_kernel(uint16_t *out, size_t out_stride, const float *parts, size_t stride, size_t n, uint32_t dim, uint32_t splits, bool bf16, bool wide)
 {
+    __shared__ float4 sums[3][64];
     pdl_start();
-    const uint32_t j = blockIdx.y * 1024 + threadIdx.x * 4;
-    if (j >= dim) return;
+    const uint32_t x = threadIdx.x & 63, y = threadIdx.x >> 6, j = blockIdx.y * kFinishColumns + x * 4;
     for (size_t row = blockIdx.x; row < n; row += gridDim.x) {
-        const float *src = parts + row * stride + j;
         float4 sum = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-#pragma unroll 4
-        for (uint32_t s = 0; s < splits; s++) {
-            const float4 x = *reinterpret_cast<const float4 *>(src + s * n * stride);
-            sum.x += x.x;
-            sum.y += x.y;
-            sum.z += x.z;
-            sum.w += x.w;
+        if (j < dim) {
+            const float *src = parts + row * stride + j;           // rows hold a multiple of 32 values
+#pragma unroll 8
+            for (uint32_t s = y; s < splits; s += 4) {
+                const float4 v = *reinterpret_cast<const float4 *>(src + s * n * stride);
+                sum = make_float4(sum.x + v.x, sum.y + v.y, sum.z + v.z, sum.w + v.w);
+            }
         }
-        const uint32_t lo = pack2(bf16, sum.x, sum.y), hi = pack2(bf16, sum.z, sum.w);
-        uint16_t *dst = out + row * out_stride + j;
-        if (wide && j + 4 <= dim) {
-            *reinterpret_cast<uint2 *>(dst) = make_uint2(lo, hi);
-        } else {
-            const uint16_t v[4] = {uint16_t(lo), uint16_t(lo >> 16), uint16_t(hi), uint16_t(hi >> 16)};
+        if (y) sums[y - 1][x] = sum;
+        __syncthreads();
+        if (y == 0 && j < dim) {
 #pragma unroll
-            for (int k = 0; k < 4; k++)
-                if (j + k < dim) dst[k] = v[k];
+            for (int k = 0; k < 3; k++) {
+                const float4 v = sums[k][x];
+                sum = make_float4(sum.x + v.x, sum.y + v.y, sum.z + v.z, sum.w + v.w);
+            }
+            const uint32_t lo = pack2(bf16, sum.x, sum.y), hi = pack2(bf16, sum.z, sum.w);
+            uint16_t *dst = out + row * out_stride + j;
+            if (wide && j + 4 <= dim) {
+                *reinterpret_cast<uint2 *>(dst) = make_uint2(lo, hi);
+            } else {
+                const uint16_t v[4] = {uint16_t(lo), uint16_t(lo >> 16), uint16_t(hi), uint16_t(hi >> 16)};
+#pragma unroll
+                for (int k = 0; k < 4; k++)
+                    if (j + k < dim) dst[k] = v[k];
+            }
         }
+        __syncthreads();
     }
 }
 
@@ -927,7 +937,7 @@ cudaError_t gated_backward(const GatedArgs &a)
     e = cg == 2 ? launch_mma<true, false, 2>(p, device, work, a.stream) : launch_mma<true, false, 1>(p, device, work, a.stream);
     if (e != cudaSuccess || l.splits == 1) return e;
     const bool wide_x = reinterpret_cast<uintptr_t>(a.grad_x) % 8 == 0 && a.grad_x_stride % 4 == 0;
-    const dim3 rows(unsigned(a.n < 65536 ? a.n : 65536), unsigned((a.dim + 1023) / 1024));
+    const dim3 rows(unsigned(a.n < 65536 ? a.n : 65536), unsigned((a.dim + kFinishColumns - 1) / kFinishColumns));
     return launch(rd_gated_finish_kernel, rows, 256, a.stream, p.dx, a.grad_x_stride, static_cast<const float *>(l.parts), l.part_stride, a.n, uint32_t(a.dim), p.splits, bf16, wide_x);
 }
 
