@@ -10,7 +10,7 @@ namespace {
 enum Mode { kPlain = 0, kDrop = 1, kEight = 2, kAsk = 4 };
 
 // T: x and out, R: residual and sum, W: the weight.  A thread holds NV units of a row; what it has no unit for is zeros.
-template <class T, class R, class W, bool SPREAD, int NV, bool WARP, int MODE> __global__ void __launch_bounds__(kThreads, SPREAD ? 2 : 3) rd_norm_kernel(const __grid_constant__ NormParams p)
+template <class T, class R, class W, bool SPREAD, int NV, bool WARP, int MODE> __global__ void __launch_bounds__(kThreads, SPREAD && NV == 4 ? 2 : 3) rd_norm_kernel(const __grid_constant__ NormParams p)
 {
     using UnitT = Unit<T, SPREAD>;
     using UnitR = Unit<R, SPREAD>;
@@ -163,7 +163,7 @@ template <class T, class R, class W> __device__ __forceinline__ void sum_columns
 // Persistent groups of threads that take rows in turn; a thread's columns stay the same, so that grad_weight adds up in its registers.
 // With the sum over a row of grad_out w s = m:  grad = r (grad_out w - s (r^2 m / dim)) + grad_sum.
 template <class T, class R, class W, bool SPREAD, int NV, bool WARP, int MODE>
-__global__ void __launch_bounds__(SPREAD ? 2 * kThreads : kThreads, SPREAD ? 1 : 3) rd_norm_grad_kernel(const __grid_constant__ NormGradParams p)
+__global__ void __launch_bounds__(kThreads, SPREAD && NV == 4 ? 2 : 3) rd_norm_grad_kernel(const __grid_constant__ NormGradParams p)
 {
     using UnitT = Unit<T, SPREAD>;
     using UnitR = Unit<R, SPREAD>;
@@ -342,7 +342,7 @@ template <auto KERNEL, typename P> cudaError_t launch_rows(const P &p, const Row
 }
 
 // Calls f with the kernel's template arguments: how the row lies, the types of residual and weight.
-template <class F> cudaError_t with_shape(bool spread, const RowDeal &d, F &&f)
+template <bool GRADIENT, class F> cudaError_t with_shape(bool spread, const RowDeal &d, F &&f)
 {
     using std::integral_constant;
     using Yes = integral_constant<bool, true>;
@@ -350,10 +350,12 @@ template <class F> cudaError_t with_shape(bool spread, const RowDeal &d, F &&f)
     using One = integral_constant<int, 1>;
     using Two = integral_constant<int, 2>;
     using Four = integral_constant<int, 4>;
-    if (!spread && d.warp) return d.nv == 1 ? f(No(), One(), Yes()) : d.nv == 2 ? f(No(), Two(), Yes()) : f(No(), Four(), Yes());
-    if (!spread) return d.nv == 2 ? f(No(), Two(), No()) : f(No(), Four(), No());
-    if (d.warp) return d.nv <= 2 ? f(Yes(), Two(), Yes()) : f(Yes(), Four(), Yes());
-    return d.nv == 2 ? f(Yes(), Two(), No()) : f(Yes(), Four(), No());
+    if (spread && d.warp) return f(Yes(), Two(), Yes());
+    if (spread) return d.nv == 2 ? f(Yes(), Two(), No()) : f(Yes(), Four(), No());
+    if (d.warp) return d.nv == 1 ? f(No(), One(), Yes()) : d.nv == 2 ? f(No(), Two(), Yes()) : f(No(), Four(), Yes());
+    if constexpr (GRADIENT)
+        if (d.nv == 2) return f(No(), Two(), No());
+    return f(No(), Four(), No());
 }
 template <class T, class F> cudaError_t with_types(int sum_dtype, int weight_dtype, F &&f)
 {
@@ -367,7 +369,7 @@ template <class T, class F> cudaError_t with_types(int sum_dtype, int weight_dty
 template <> cudaError_t launch_norm<RD_NORM_ROWS>(const NormParams &p, const NormCall &c)
 {
     using T = RD_NORM_ROWS;
-    return with_shape(c.spread, c.deal, [&](auto SPREAD, auto NV, auto WARP) {
+    return with_shape<false>(c.spread, c.deal, [&](auto SPREAD, auto NV, auto WARP) {
         return with_types<T>(c.sum_dtype, c.weight_dtype, [&](auto R, auto W) {
             using RT = decltype(R);
             using WT = decltype(W);
@@ -386,7 +388,7 @@ template <> cudaError_t launch_norm<RD_NORM_ROWS>(const NormParams &p, const Nor
 template <> cudaError_t launch_norm_grad<RD_NORM_ROWS>(const NormGradParams &p, const NormCall &c)
 {
     using T = RD_NORM_ROWS;
-    return with_shape(c.spread, c.deal, [&](auto SPREAD, auto NV, auto WARP) {
+    return with_shape<true>(c.spread, c.deal, [&](auto SPREAD, auto NV, auto WARP) {
         return with_types<T>(c.sum_dtype, c.weight_dtype, [&](auto R, auto W) {
             using RT = decltype(R);
             using WT = decltype(W);

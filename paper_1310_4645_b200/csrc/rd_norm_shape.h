@@ -72,14 +72,15 @@ struct NormGradParams {
 };
 
 // How a row is dealt out, brought in and how many rows at a time.
-//   A warp has a row if it holds it with four units a thread (`few`: two), else as few warps of a thread block as hold it with four, so that
-//   the join of a row costs few instructions a value, or a cluster of up to eight blocks.
-//   few (the gradient): two units a thread and twice the warps while one block of them holds a block's part; without a ring always, because
-//   operands stay in registers then.  The gradient of 16384 x 4096 bf16 with dropout takes 129 us so, 137 with four (B200).
-//   A cluster has as few blocks as hold the row: its meetings cost more than blocks an SM gain (gradient of 8192 x 16384 bf16 by two blocks
-//   245 us, by four 430).
-//   As many groups (a block of warps with a row each, or the blocks of one row) as registers (80 a thread with a ring, 128 without) and
-//   shared memory with two stages or more allow.
+//   A warp has a row if it holds it with four units a thread, two without a ring; else as few warps of a thread block as hold it, or a
+//   cluster of up to eight blocks, as few as do: their meetings cost more than blocks an SM gain (gradient of 8192 x 16384 bf16 by two
+//   blocks 245 us, by four 430).
+//   Four units a thread: then the join of a row costs few instructions a value.  Two, and twice the warps, in the gradient (few) while one
+//   block of them holds a block's part (16384 x 4096 bf16 with dropout 129 us, with four 137), and without a ring, where operands
+//   stay in registers (16384 x 4095 bf16 norm 195 us, with four 233; gradient 210 and 269), but for norms of more than 8192 columns
+//   (4096 x 10001: 168 us, in four blocks with two units 228, with four and 80 registers 211).
+//   As many groups (a block of warps with a row each, or the blocks of one row) as registers (80 a thread, 128 with four units and no ring)
+//   and shared memory with two stages or more allow.  (All B200.)
 // unit_bytes: of all matrices that come in by the ring, for 8 columns; 0: none does.
 struct RowDeal {
     uint32_t units, per_block, blocks, threads;
@@ -93,18 +94,19 @@ inline RowDeal deal(size_t dim, size_t unit_bytes, bool few)
     d.blocks = 1;
     d.threads = kThreads;
     d.per_block = d.units;
-    if (d.units <= uint32_t(32 * (few && !unit_bytes ? kUnits / 2 : kUnits))) {
+    const int most = unit_bytes ? kUnits : kUnits / 2;
+    if (d.units <= uint32_t(32 * most)) {
         d.warp = true;
-        d.nv = few && !unit_bytes ? kUnits / 2 : kUnits;
+        d.nv = most;
         while (d.nv > 1 && d.units <= uint32_t(16 * d.nv)) d.nv /= 2;
         return d;
     }
     auto part = [&] { return (d.units + d.blocks - 1) / d.blocks; };
-    while (part() > kBlockUnits) d.blocks *= 2;
+    while (d.blocks < 8 && part() > (unit_bytes || (!few && d.units > kBlockUnits) ? kBlockUnits : kBlockUnits / 2)) d.blocks *= 2;
     // whole warps' columns, so that no 256 columns are two blocks'; then perhaps fewer blocks, none without columns
     d.per_block = (part() + 31) / 32 * 32;
     d.blocks = (d.units + d.per_block - 1) / d.per_block;
-    d.nv = few && (!unit_bytes || d.per_block <= uint32_t(kThreads * kUnits / 2)) ? kUnits / 2 : kUnits;
+    d.nv = (few || !unit_bytes) && d.per_block <= uint32_t(kThreads * kUnits / 2) ? kUnits / 2 : kUnits;
     d.threads = (d.per_block + 32 * d.nv - 1) / (32 * d.nv) * 32;
     return d;
 }
@@ -118,7 +120,7 @@ inline RowShape shape_of(size_t n, const RowDeal &d, size_t unit_bytes)
 {
     RowShape s{};
     const size_t rows = d.warp ? kWarps : 1, wanted = (n + rows - 1) / rows;
-    size_t per_sm = 65536 / (d.threads * (unit_bytes ? 80 : 128));
+    size_t per_sm = 65536 / (d.threads * (unit_bytes || d.nv < kUnits ? 80 : 128));
     if (unit_bytes) {
         const size_t stage = d.per_block * unit_bytes, all = stage * rows;
         while (per_sm > 1 && kRingBytes / per_sm / all < 2) per_sm--;
