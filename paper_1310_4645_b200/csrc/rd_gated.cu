@@ -260,6 +260,14 @@ template <int CG> struct GradPlan {
     }
 };
 
+// A warp has its accumulators in registers: arrives at the first block's barrier.  No release of the cluster's scope: that would wait for
+// the results that the warp has stored meanwhile, and nothing in memory is handed over.
+template <int CG> __device__ __forceinline__ void accumulators_read(uint32_t bar)
+{
+    if (CG == 1) asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
+    else asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(leader_bar<CG>(bar)) : "memory");
+}
+
 template <bool GRADS, int CG> using ShapeOf = Shape<GRADS ? kGrads : kStats, CG>;
 
 template <bool GRADS, bool F8, int CG>
@@ -401,21 +409,31 @@ __global__ void __launch_bounds__(kMmaThreads, 1) rd_gated_mma_kernel(const __gr
             auto release = [&]() {
                 asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
                 __syncwarp();
-                if (lane == 0) bar_arrive_leader<CG>(acc_empty + 8 * buf);
+                if (lane == 0) accumulators_read<CG>(acc_empty + 8 * buf);
             };
             if constexpr (!GRADS) {
                 const float x_scale = F8 && row < p.n ? p.x_scale[row] : 1.0f;
                 // a tile's columns by 16, half of them each warp's; the last 16 may be 8, and what lies behind them the other projection's
                 const uint32_t chunks = (p.tile_w + 15) / 16, first = half ? (chunks + 1) / 2 : 0, last = half ? chunks : (chunks + 1) / 2;
                 const uint32_t columns = min(p.tile_w, p.width - w.n0), rows = row0 < p.n ? min(32u, p.n - row0) : 0, stage = smem + p.staging + (warp - 4) * 1024;
-                if (first >= last) release();
-                for (uint32_t c = first; c < last; c++) {
-                    uint32_t g[16], u[16];
-                    tmem_load(acc + 16 * c, g);
-                    tmem_load(acc + p.tile_w + 16 * c, u);
+                const int count = int(last - first);
+                // 16 columns of both are on their way while the 16 before them are worked on
+                uint32_t gates[2][16], ups[2][16];
+                auto load = [&](int k) {
+                    tmem_load(acc + 16 * (first + k), gates[k & 1]);
+                    tmem_load(acc + p.tile_w + 16 * (first + k), ups[k & 1]);
+                };
+                if (count > 0) load(0);
+                else release();
+#pragma unroll
+                for (int k = 0; k < 4; k++) {
+                    if (k >= count) break;
+                    uint32_t(&g)[16] = gates[k & 1], (&u)[16] = ups[k & 1];
                     tmem_wait(g);
                     tmem_wait(u);
-                    if (c + 1 == last) release();
+                    if (k + 1 < count) load(k + 1);
+                    else release();
+                    const uint32_t c = first + k;
                     if (16 * c >= columns) continue;
                     const uint32_t col = w.n0 + 16 * c, left = columns - 16 * c;
                     if (F8) {
