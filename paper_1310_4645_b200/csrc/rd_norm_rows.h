@@ -246,7 +246,8 @@ template <bool WARP> __device__ __forceinline__ float2 join_row(float2 v, bool w
 }
 
 // Which rows and which units of them a thread has: unit, unit + step, ...  (`threads`: of the block; `grid`: blocks that have rows.)
-template <bool SPREAD, bool WARP> struct Place {
+// FULL: every thread has every unit it could have.
+template <bool SPREAD, bool WARP, bool FULL> struct Place {
     size_t row, rows;         // first row, and how many rows further the next is
     uint32_t unit, step, end, rank;
     __device__ __forceinline__ Place(uint32_t units, uint32_t per_block, uint32_t blocks, uint32_t threads, uint32_t grid)
@@ -270,7 +271,7 @@ template <bool SPREAD, bool WARP> struct Place {
         }
     }
     // whether there is a unit k; SPREAD: a warp has the 256 columns of its units together
-    __device__ __forceinline__ bool has(int k) const { return (SPREAD ? (unit + k * step) & ~31u : unit + k * step) < end; }
+    __device__ __forceinline__ bool has(int k) const { return FULL || (SPREAD ? (unit + k * step) & ~31u : unit + k * step) < end; }
     __device__ __forceinline__ bool first() const { return rank == 0 && (WARP ? threadIdx.x & 31 : threadIdx.x) == 0; }
 };
 

@@ -86,6 +86,7 @@ struct RowDeal {
     uint32_t units, per_block, blocks, threads;
     int nv;                   // units a thread
     bool warp;
+    bool full() const { return size_t(blocks) * per_block == units && per_block == (warp ? 32 : threads) * uint32_t(nv); }
 };
 inline RowDeal deal(size_t dim, size_t unit_bytes, bool few)
 {
