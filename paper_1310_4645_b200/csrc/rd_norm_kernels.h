@@ -171,9 +171,9 @@ __global__ void __launch_bounds__(kThreads, SPREAD && NV == 4 ? 2 : 3) rd_norm_g
     using UnitR = Unit<R, SPREAD>;
     constexpr uint32_t kT = UnitT::bytes / 8, kR = UnitR::bytes / 8;
     const bool drops = MODE & kAsk ? p.drop.border != 0 : bool(MODE & kDrop);
-    __shared__ float column_sums[kMostWarps * 32 / kSumColumns][kSumColumns];
+    __shared__ float column_sums[kThreads / kSumColumns][kSumColumns];
     __shared__ Meeting meeting;
-    __shared__ uint4 bits[SPREAD ? kMostWarps : 1][32];
+    __shared__ uint4 bits[SPREAD ? kWarps : 1][32];
     __shared__ uint64_t bars[WARP ? kWarps : 1][kMostStages];
     Stream<WARP> stream(bars, SPREAD ? RowRing{0, 0} : p.ring);
     pdl_wait();

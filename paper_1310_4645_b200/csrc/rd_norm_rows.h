@@ -203,7 +203,7 @@ __device__ __forceinline__ uint32_t cluster_rank()
 }
 
 struct Meeting {
-    float2 of_warp[2][kMostWarps];
+    float2 of_warp[2][kWarps];
     float2 of_block[2][8];
 };
 

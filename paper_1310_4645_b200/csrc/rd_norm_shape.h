@@ -9,10 +9,9 @@
 
 namespace rd {
 
-constexpr int kThreads = 256, kWarps = kThreads / 32;       // of blocks whose warps have a row each, and of dropout alone
+constexpr int kThreads = 256, kWarps = kThreads / 32;       // of a block: whose warps have rows of their own, or at most
 constexpr uint32_t kBlockUnits = 1024;    // units of 8 columns of a row that a thread block has at most
-constexpr int kUnits = 4;                 // units that a thread has at most; two in the gradient without a ring, whose operands stay in registers
-constexpr int kMostWarps = 16;
+constexpr int kUnits = 4;                 // units that a thread has at most
 constexpr size_t kDropoutBlocks = 6;      // of dropout alone, an SM
 constexpr uint32_t kSumColumns = 16;      // of grad_weight, that a block sums up where rows are few
 constexpr uint32_t kMostStages = 8;
