@@ -7,7 +7,7 @@
 // 10 rounds (Salmon, Moraes, Dror, Shaw, "Parallel random numbers: as easy as 1, 2, 3", 2011), whose counter is the value's place:
 // (column / 8, row, offset), key: the seed.  So a mask is never stored; whoever knows the place knows the bits.
 //
-// A row is held by a warp (up to 1024 values), a thread block (up to 8192) or a cluster of up to eight of them, whose partial sums meet in
+// A row is held by 8, 16 or 32 lanes (up to 256 values), a warp (up to 1024), a thread block (up to 8192) or a cluster of up to eight of them, whose partial sums meet in
 // each other's shared memory.  Everything is read and written once, the weight and, in the gradient, a row in shared memory excepted.
 // What bounds it (B200): the memory, at 0.84 to 0.92 of the rate of a copy: 16384 x 4096 bf16 with dropout and residual 89 to 97 us for 537 MB,
 // gradient 114 to 125 for 671, dropout alone 45 to 50 for 268; 2000 x 5120 into 8 bits 18 for 113.  A row alone: 2.4 us, the latency of a
@@ -178,7 +178,7 @@ cudaError_t norm_backward(const NormGradArgs &a)
     if (few && d.threads < kThreads) d.threads = kThreads;
     RowShape shape = shape_of(a.n, d, unit_bytes);
     // where warps have rows, their parts of grad_weight are joined in shared memory
-    if (d.warp && shape.smem < kWarps * a.dim * sizeof(float)) shape.smem = kWarps * a.dim * sizeof(float);
+    if (d.warp && !d.lanes && shape.smem < kWarps * a.dim * sizeof(float)) shape.smem = kWarps * a.dim * sizeof(float);
     NormGradParams p{};
     p.ring = shape.ring;
     p.grad_out = a.grad_out;

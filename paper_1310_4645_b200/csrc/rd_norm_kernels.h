@@ -11,6 +11,13 @@ namespace {
 // 120.5 / 114.3 us, B200).
 enum Mode { kPlain = 0, kDrop = 1, kEight = 2, kAsk = 4, kFull = 8 };
 
+// What takes a row's largest value to 448.  Very small ones are taken near 1 first (by `lift`), so that no quotient overflows.
+__device__ __forceinline__ float eighth_factor(float most, float &lift)
+{
+    lift = most < 0x1p-60f ? 0x1p64f : 1.0f;
+    return most > 0.0f ? 448.0f / (most * lift) : 0.0f;
+}
+
 // T: x and out, R: residual and sum, W: the weight.  A thread holds NV units of a row; what it has no unit for is zeros.
 template <class T, class R, class W, bool SPREAD, int NV, bool WARP, int MODE> __global__ void __launch_bounds__(kThreads, SPREAD && NV == 4 ? 2 : 3) rd_norm_kernel(const __grid_constant__ NormParams p)
 {
@@ -91,9 +98,8 @@ template <class T, class R, class W, bool SPREAD, int NV, bool WARP, int MODE> _
         const float rstd = rsqrtf(fmaf(stat.x, p.inv_dim, p.eps));
         float factor = rstd;
         if (eight) {
-            // the row's largest value becomes 448; very small ones are taken near 1 first, so that no quotient overflows
-            const float lift = stat.y < 0x1p-60f ? 0x1p64f : 1.0f;
-            factor = stat.y > 0.0f ? 448.0f / (stat.y * lift) : 0.0f;
+            float lift;
+            factor = eighth_factor(stat.y, lift);
             if (lift != 1.0f) {
 #pragma unroll
                 for (int k = 0; k < NV; k++)
@@ -133,6 +139,84 @@ template <class T, class R, class W, bool SPREAD, int NV, bool WARP, int MODE> _
     }
     if (!p.release_early) pdl_release();
     if (stream.dead) drain();
+}
+
+// Rows of at most 32 units, as of a head: LANES lanes (8, 16 or 32) have one, so that a warp has four, two or one at a time; a lane has a
+// unit, the next row's operands on their way, and the weight for good.
+template <class T, class R, class W, int LANES> __global__ void __launch_bounds__(kThreads, kShortBlocks) rd_norm_short_kernel(const __grid_constant__ NormParams p)
+{
+    using UnitT = Unit<T, false>;
+    using UnitR = Unit<R, false>;
+    constexpr uint32_t kT = UnitT::bytes / 8, kR = UnitR::bytes / 8, kRows = 32 / LANES;
+    pdl_wait();
+    if (p.release_early) pdl_release();
+    const uint32_t lane = threadIdx.x & 31, unit = lane % LANES;
+    const bool mine = unit < p.units;
+    const size_t step = size_t(gridDim.x) * kWarps * kRows;
+    size_t base = (size_t(blockIdx.x) * kWarps + (threadIdx.x >> 5)) * kRows;          // the warp's first row
+    UnitT x;
+    UnitR res;
+    Unit<W, false> weight;
+    Pair w[4];
+    auto load = [&](size_t row) {
+        x.load(at_byte(p.x, row * p.x_stride * kT), unit, p.dim, mine && row < p.n);
+        res.load(at_byte(p.residual, row * p.residual_stride * kR), unit, p.dim, mine && row < p.n && p.residual);
+    };
+    weight.load(p.weight, unit, p.dim, mine);
+    weight.get(w);
+    load(base + lane / LANES);
+    for (; base < p.n; base += step) {
+        const size_t row = base + lane / LANES;
+        const bool live = mine && row < p.n;
+        Pair s[4], r[4];
+        x.get(s);
+        res.get(r);
+        load(row + step);
+        if (p.drop.border) drop_values<false>(p.drop, nullptr, unit, uint32_t(row), s);
+#pragma unroll
+        for (int i = 0; i < 4; i++) s[i] = add2(s[i], r[i]);
+        if (p.sum && live) {
+            UnitR o;
+            o.set(s);
+            o.store(at_byte(p.sum, row * p.sum_stride * kR), unit, p.dim);
+        }
+        Pair squares = 0;
+#pragma unroll
+        for (int i = 0; i < 4; i++) {
+            squares = fma2(s[i], s[i], squares);
+            s[i] = mul2(s[i], w[i]);
+        }
+        float sum = both(squares).x + both(squares).y, most = 0.0f;
+#pragma unroll
+        for (int d = LANES / 2; d; d /= 2) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+        if (p.out8) {
+#pragma unroll
+            for (int i = 0; i < 4; i++) most = fmaxf(fmaxf(most, fabsf(both(s[i]).x)), fabsf(both(s[i]).y));
+#pragma unroll
+            for (int d = LANES / 2; d; d /= 2) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, d));
+        }
+        const float rstd = rsqrtf(fmaf(sum, p.inv_dim, p.eps));
+        float lift = 1.0f;
+        const float factor = p.out8 ? eighth_factor(most, lift) : rstd;
+        if (unit == 0 && live) {
+            if (p.rstd) p.rstd[row] = rstd;
+            if (p.out8) p.out_scale[row] = most * rstd / 448.0f;
+        }
+#pragma unroll
+        for (int i = 0; i < 4; i++) s[i] = mul2(lift != 1.0f ? mul2(s[i], pair(lift, lift)) : s[i], pair(factor, factor));
+        if (!live) continue;
+        if (p.out8) {
+            uint32_t q[4];
+#pragma unroll
+            for (int i = 0; i < 4; i++) q[i] = __nv_cvt_float2_to_fp8x2(both(s[i]), __NV_SATFINITE, __NV_E4M3);
+            *reinterpret_cast<uint2 *>(static_cast<uint8_t *>(p.out) + row * p.out_stride + unit * 8) = make_uint2(q[0] | q[1] << 16, q[2] | q[3] << 16);
+        } else {
+            UnitT o;
+            o.set(s);
+            o.store(at_byte(p.out, row * p.out_stride * kT), unit, p.dim);
+        }
+    }
+    if (!p.release_early) pdl_release();
 }
 
 // ------------------------------------------------------------------------------------------------ gradient
@@ -315,6 +399,87 @@ __global__ void __launch_bounds__(kThreads, SPREAD && NV == 4 ? 2 : 3) rd_norm_g
     }
 }
 
+// The same for the gradient.
+template <class T, class R, class W, int LANES> __global__ void __launch_bounds__(kThreads, kShortBlocks) rd_norm_grad_short_kernel(const __grid_constant__ NormGradParams p)
+{
+    using UnitT = Unit<T, false>;
+    using UnitR = Unit<R, false>;
+    constexpr uint32_t kT = UnitT::bytes / 8, kR = UnitR::bytes / 8, kRows = 32 / LANES;
+    __shared__ float column_sums[kThreads / kSumColumns][kSumColumns];
+    __shared__ float of_row[kWarps * kRows][LANES * 8];
+    pdl_wait();
+    if (p.release_early) pdl_release();
+    if (blockIdx.x >= p.row_blocks) {
+        sum_columns<T, R, W>(p, column_sums);
+        return;
+    }
+    const uint32_t lane = threadIdx.x & 31, unit = lane % LANES, place = (threadIdx.x >> 5) * kRows + lane / LANES;
+    const bool mine = unit < p.units;
+    const size_t step = size_t(p.row_blocks) * kWarps * kRows;
+    size_t base = (size_t(blockIdx.x) * kWarps + (threadIdx.x >> 5)) * kRows;          // the warp's first row
+    UnitT up;
+    UnitR sum, more;
+    Unit<W, false> weight;
+    float rstd;
+    Pair w[4], acc[4] = {};
+    auto load = [&](size_t row) {
+        const bool live = mine && row < p.n;
+        up.load(at_byte(p.grad_out, row * p.grad_out_stride * kT), unit, p.dim, live);
+        sum.load(at_byte(p.sum, row * p.sum_stride * kR), unit, p.dim, live);
+        more.load(at_byte(p.grad_sum, row * p.grad_sum_stride * kR), unit, p.dim, live && p.grad_sum);
+        rstd = live ? p.rstd[row] : 0.0f;
+    };
+    weight.load(p.weight, unit, p.dim, mine);
+    weight.get(w);
+    load(base + lane / LANES);
+    for (; base < p.n; base += step) {
+        const size_t row = base + lane / LANES;
+        const bool live = mine && row < p.n;
+        Pair u[4], s[4], m[4], dots = 0;
+        up.get(u);
+        sum.get(s);
+        more.get(m);
+        const float r = rstd;
+        load(row + step);
+#pragma unroll
+        for (int i = 0; i < 4; i++) {
+            const Pair y = mul2(u[i], s[i]);
+            acc[i] = fma2(y, pair(r, r), acc[i]);
+            dots = fma2(y, w[i], dots);
+        }
+        float dot = both(dots).x + both(dots).y;
+#pragma unroll
+        for (int d = LANES / 2; d; d /= 2) dot += __shfl_xor_sync(0xffffffffu, dot, d);
+        if (!live || !p.want_rows) continue;
+        const float slope = dot * p.inv_dim * r * r;
+#pragma unroll
+        for (int i = 0; i < 4; i++) u[i] = fma2(pair(r, r), fma2(pair(-slope, -slope), s[i], mul2(u[i], w[i])), m[i]);
+        if (p.grad_residual) {
+            UnitR o;
+            o.set(u);
+            o.store(at_byte(p.grad_residual, row * p.grad_residual_stride * kR), unit, p.dim);
+        }
+        if (p.grad_x) {
+            if (p.drop.border) drop_values<false>(p.drop, nullptr, unit, uint32_t(row), u);
+            UnitT o;
+            o.set(u);
+            o.store(at_byte(p.grad_x, row * p.grad_x_stride * kT), unit, p.dim);
+        }
+    }
+    if (!p.release_early) pdl_release();
+    if (!p.part) return;
+    if (mine)
+#pragma unroll
+        for (int i = 0; i < 4; i++) of_row[place][unit * 8 + 2 * i] = both(acc[i]).x, of_row[place][unit * 8 + 2 * i + 1] = both(acc[i]).y;
+    __syncthreads();
+    for (uint32_t j = threadIdx.x; j < p.dim; j += kThreads) {
+        float v = of_row[0][j];
+#pragma unroll
+        for (int k = 1; k < int(kWarps * kRows); k++) v += of_row[k][j];
+        p.part[size_t(blockIdx.x) * p.dim + j] = v;
+    }
+}
+
 // ------------------------------------------------------------------------------------------------ launches
 
 template <auto KERNEL, typename P> cudaError_t launch_rows(const P &p, const RowShape &s, const RowDeal &d, cudaStream_t stream, size_t more_blocks = 0)
@@ -351,16 +516,16 @@ template <bool GRADIENT, class F> cudaError_t with_shape(bool spread, const RowD
     using std::integral_constant;
     using Yes = integral_constant<bool, true>;
     using No = integral_constant<bool, false>;
-    using One = integral_constant<int, 1>;
     using Two = integral_constant<int, 2>;
     using Four = integral_constant<int, 4>;
     if (spread && d.warp) return f(Yes(), Two(), Yes());
     if (spread) return d.nv == 2 ? f(Yes(), Two(), No()) : f(Yes(), Four(), No());
-    if (d.warp) return d.nv == 1 ? f(No(), One(), Yes()) : d.nv == 2 ? f(No(), Two(), Yes()) : f(No(), Four(), Yes());
+    if (d.warp) return d.nv == 2 ? f(No(), Two(), Yes()) : f(No(), Four(), Yes());
     if constexpr (GRADIENT)
         if (d.nv == 2) return f(No(), Two(), No());
     return f(No(), Four(), No());
 }
+template <class F> cudaError_t with_lanes(int lanes, F &&f) { return lanes == 8 ? f(Constant<8>()) : lanes == 16 ? f(Constant<16>()) : f(Constant<32>()); }
 template <class T, class F> cudaError_t with_types(int sum_dtype, int weight_dtype, F &&f)
 {
     if constexpr (std::is_same_v<T, F32>) return f(F32(), F32());
@@ -373,6 +538,12 @@ template <class T, class F> cudaError_t with_types(int sum_dtype, int weight_dty
 template <> cudaError_t launch_norm<RD_NORM_ROWS>(const NormParams &p, const NormCall &c)
 {
     using T = RD_NORM_ROWS;
+    if (c.deal.lanes)
+        return with_types<T>(c.sum_dtype, c.weight_dtype, [&](auto R, auto W) {
+            using RT = decltype(R);
+            using WT = decltype(W);
+            return with_lanes(c.deal.lanes, [&](auto LANES) { return launch_rows<rd_norm_short_kernel<T, RT, WT, LANES()>>(p, c.shape, c.deal, c.stream); });
+        });
     return with_shape<false>(c.spread, c.deal, [&](auto SPREAD, auto NV, auto WARP) {
         return with_types<T>(c.sum_dtype, c.weight_dtype, [&](auto R, auto W) {
             using RT = decltype(R);
@@ -394,6 +565,12 @@ template <> cudaError_t launch_norm<RD_NORM_ROWS>(const NormParams &p, const Nor
 template <> cudaError_t launch_norm_grad<RD_NORM_ROWS>(const NormGradParams &p, const NormCall &c)
 {
     using T = RD_NORM_ROWS;
+    if (c.deal.lanes)
+        return with_types<T>(c.sum_dtype, c.weight_dtype, [&](auto R, auto W) {
+            using RT = decltype(R);
+            using WT = decltype(W);
+            return with_lanes(c.deal.lanes, [&](auto LANES) { return launch_rows<rd_norm_grad_short_kernel<T, RT, WT, LANES()>>(p, c.shape, c.deal, c.stream, c.more_blocks); });
+        });
     return with_shape<true>(c.spread, c.deal, [&](auto SPREAD, auto NV, auto WARP) {
         return with_types<T>(c.sum_dtype, c.weight_dtype, [&](auto R, auto W) {
             using RT = decltype(R);

@@ -13,6 +13,7 @@ constexpr int kThreads = 256, kWarps = kThreads / 32;       // of a block: whose
 constexpr uint32_t kBlockUnits = 1024;    // units of 8 columns of a row that a thread block has at most
 constexpr int kUnits = 4;                 // units that a thread has at most
 constexpr size_t kDropoutBlocks = 6;      // of dropout alone, an SM
+constexpr int kShortBlocks = 4;           // of short rows, an SM
 constexpr uint32_t kSumColumns = 16;      // of grad_weight, that a block sums up where rows are few
 constexpr uint32_t kMostStages = 8;
 constexpr size_t kRingBytes = 200 << 10;  // of an SM's shared memory that rows on their way may take
@@ -71,6 +72,8 @@ struct NormGradParams {
 };
 
 // How a row is dealt out, brought in and how many rows at a time.
+//   Rows of up to 32 units have 8, 16 or 32 lanes of a warp each and no ring: those would be copies of a few hundred bytes (262144 x 128
+//   bf16 by a warp a row and a ring 81 us, gradient 145; so 44 and 50).
 //   A warp has a row if it holds it with four units a thread, two without a ring; else as few warps of a thread block as hold it, or a
 //   cluster of up to eight blocks, as few as do: their meetings cost more than blocks an SM gain (gradient of 8192 x 16384 bf16 by two
 //   blocks 245 us, by four 430).
@@ -84,6 +87,7 @@ struct NormGradParams {
 struct RowDeal {
     uint32_t units, per_block, blocks, threads;
     int nv;                   // units a thread
+    int lanes;                // short rows: the lanes that have one; 0: others
     bool warp;
     bool full() const { return size_t(blocks) * per_block == units && per_block == (warp ? 32 : threads) * uint32_t(nv); }
 };
@@ -95,10 +99,16 @@ inline RowDeal deal(size_t dim, size_t unit_bytes, bool few)
     d.threads = kThreads;
     d.per_block = d.units;
     const int most = unit_bytes ? kUnits : kUnits / 2;
+    if (unit_bytes && d.units <= 32) {
+        d.warp = true;
+        d.nv = 1;
+        d.lanes = d.units <= 8 ? 8 : d.units <= 16 ? 16 : 32;
+        return d;
+    }
     if (d.units <= uint32_t(32 * most)) {
         d.warp = true;
         d.nv = most;
-        while (d.nv > 1 && d.units <= uint32_t(16 * d.nv)) d.nv /= 2;
+        while (d.nv > 2 && d.units <= uint32_t(16 * d.nv)) d.nv /= 2;
         return d;
     }
     auto part = [&] { return (d.units + d.blocks - 1) / d.blocks; };
@@ -119,9 +129,11 @@ struct RowShape {
 inline RowShape shape_of(size_t n, const RowDeal &d, size_t unit_bytes)
 {
     RowShape s{};
-    const size_t rows = d.warp ? kWarps : 1, wanted = (n + rows - 1) / rows;
+    const size_t rows = d.lanes ? kWarps * 32 / d.lanes : d.warp ? kWarps : 1, wanted = (n + rows - 1) / rows;
     size_t per_sm = 65536 / (d.threads * (unit_bytes || d.nv < kUnits ? 80 : 128));
-    if (unit_bytes) {
+    if (d.lanes) {
+        per_sm = kShortBlocks;
+    } else if (unit_bytes) {
         const size_t stage = d.per_block * unit_bytes, all = stage * rows;
         while (per_sm > 1 && kRingBytes / per_sm / all < 2) per_sm--;
         const size_t fit = kRingBytes / per_sm / all;

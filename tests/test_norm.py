@@ -70,11 +70,11 @@ int main()
             for (const bool few : {false, true}) {
                 const RowDeal d = deal(dim, unit_bytes, few);
                 const RowShape s = shape_of(1000, d, unit_bytes);
-                const size_t all = size_t(d.per_block) * d.blocks, threads = d.warp ? 32 : d.threads;
+                const size_t all = size_t(d.per_block) * d.blocks, threads = d.lanes ? d.lanes : d.warp ? 32 : d.threads;
                 // every unit is somebody's, every block has some, no thread more than its registers hold, no stage beyond the ring
                 bool ok = all >= d.units && all - d.per_block < d.units && size_t(d.nv) * threads >= d.per_block && d.blocks <= 8 && (d.blocks == 1 || d.per_block % 32 == 0);
                 ok = ok && d.threads % 32 == 0 && d.threads <= (unit_bytes ? 256 : 512) && (d.warp || d.threads >= 64) && s.groups > 0;
-                if (unit_bytes) ok = ok && s.ring.stages >= 2 && s.ring.stages <= kMostStages && s.ring.stage >= d.per_block * unit_bytes && s.smem <= kRingBytes && s.smem >= size_t(s.ring.stages) * s.ring.stage * (d.warp ? kWarps : 1);
+                if (unit_bytes && !d.lanes) ok = ok && s.ring.stages >= 2 && s.ring.stages <= kMostStages && s.ring.stage >= d.per_block * unit_bytes && s.smem <= kRingBytes && s.smem >= size_t(s.ring.stages) * s.ring.stage * (d.warp ? kWarps : 1);
                 if (!ok) bad += std::printf("dim %zu, %zu bytes, few %d\n", dim, unit_bytes, few) > 0;
             }
     return bad != 0;
@@ -151,7 +151,7 @@ def norm_reference(x, weight, residual, eps, keep):
 NORM_SHAPES = [(1, 1, 0, 0), (1, 8, 0, 0), (3, 7, 0, 0), (9, 64, 0, 0), (20, 65, 0, 0), (8, 256, 0, 0), (9, 264, 8, 0), (17, 512, 0, 0), (40, 1000, 0, 0), (40, 1000, 3, 1), (31, 1024, 0, 0),
                (33, 1025, 0, 0), (33, 1032, 0, 0), (5, 2048, 0, 0), (5, 2056, 8, 8), (300, 4096, 0, 0), (3, 8192, 0, 0), (3, 8200, 0, 0), (3, 8193, 0, 0), (2, 16384, 0, 0),
                (2, 20001, 0, 0), (3, 65536, 0, 0), (2, 65535, 0, 0), (5000, 72, 0, 0),
-               (2, 3048, 0, 0), (2, 8240, 0, 0), (2, 12320, 0, 0), (3, 24584, 0, 0)]
+               (700, 8, 0, 0), (33, 48, 8, 8), (5, 128, 0, 0), (700, 120, 8, 0), (129, 136, 0, 0), (2, 3048, 0, 0), (2, 8240, 0, 0), (2, 12320, 0, 0), (3, 24584, 0, 0)]
 
 
 @gpu
@@ -189,7 +189,7 @@ def test_norm(dtype, sum_dtype, weight_dtype, n, dim, pad, offset):
 
 
 @gpu
-@pytest.mark.parametrize("dim", [40, 1024, 1041, 4096, 9000])
+@pytest.mark.parametrize("dim", [40, 128, 256, 1024, 1041, 4096, 9000])
 def test_norm_in_place(dim):
     """out may be x, the sum may be the residual or x; the bits do not change."""
     x, residual, weight = rand(19, dim, seed=5, dtype=BF16), rand(19, dim, seed=6, dtype=BF16), rand(1, dim, seed=7, dtype=BF16)[0]
@@ -206,7 +206,7 @@ def test_norm_in_place(dim):
 
 
 @gpu
-@pytest.mark.parametrize("dim", [64, 2000, 2001])
+@pytest.mark.parametrize("dim", [64, 120, 256, 2000, 2001])
 def test_norm_special_rows(dim):
     """Rows of zeros, infinities, NaN, very large and very small values, each on its own."""
     x = rand(8, dim, seed=8)
@@ -308,7 +308,7 @@ def test_norm_grad_weight_alone_and_no_rows(n):
 
 @gpu
 @pytest.mark.parametrize("n", [21, 384, 385])
-@pytest.mark.parametrize("dim", [24, 1040, 1041, 8208])
+@pytest.mark.parametrize("dim", [24, 128, 1040, 1041, 8208])
 def test_norm_grad_in_place(n, dim):
     up, total, more = (rand(n, dim, seed=18 + k, dtype=BF16) for k in range(3))
     weight, rstd = rand(1, dim, seed=21, dtype=BF16)[0], torch.rand(n, generator=gen(22), device="cuda")
