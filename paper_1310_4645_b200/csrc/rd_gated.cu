@@ -406,6 +406,18 @@ __global__ void __launch_bounds__(kMmaThreads, 1) rd_gated_mma_kernel(const __gr
         uint32_t tile = 0;
         while (plan.next(w)) {
             const uint32_t row0 = w.m0 + rank * kRowsM + 32 * quarter, row = row0 + lane, buf = tile & 1;
+            // 8 bits: the row's scale, and those of the warp's up to 64 columns, two a lane, fetched while the products are under way
+            float x_scale = 1.0f, gate_scales[2], up_scales[2];
+            if constexpr (!GRADS && F8) {
+                const uint32_t at = w.n0 + 16 * (half ? ((p.tile_w + 15) / 16 + 1) / 2 : 0) + lane;
+                if (row < p.n) x_scale = p.x_scale[row];
+#pragma unroll
+                for (int i = 0; i < 2; i++) {
+                    const bool there = at + 32 * i < p.width;
+                    gate_scales[i] = there ? p.gate_scale[at + 32 * i] : 0.0f;
+                    up_scales[i] = there ? p.up_scale[at + 32 * i] : 0.0f;
+                }
+            }
             if (!warp_wait(acc_full + 8 * buf, tile / 2 & 1)) break;
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
             const uint32_t acc = tmem + buf * kTileN + (uint32_t(32 * quarter) << 16);
@@ -416,7 +428,6 @@ __global__ void __launch_bounds__(kMmaThreads, 1) rd_gated_mma_kernel(const __gr
                 if (lane == 0) accumulators_read<CG>(acc_empty + 8 * buf);
             };
             if constexpr (!GRADS) {
-                const float x_scale = F8 && row < p.n ? p.x_scale[row] : 1.0f;
                 // a tile's columns by 16, half of them each warp's; the last 16 may be 8, and what lies behind them the other projection's
                 const uint32_t chunks = (p.tile_w + 15) / 16, first = half ? (chunks + 1) / 2 : 0, last = half ? chunks : (chunks + 1) / 2;
                 const uint32_t columns = min(p.tile_w, p.width - w.n0), rows = row0 < p.n ? min(32u, p.n - row0) : 0, stage = smem + p.staging + (warp - 4) * 1024;
@@ -443,9 +454,9 @@ __global__ void __launch_bounds__(kMmaThreads, 1) rd_gated_mma_kernel(const __gr
                     if (F8) {
 #pragma unroll
                         for (int j = 0; j < 16; j++) {
-                            const uint32_t at = col + (j < left ? j : 0);
-                            g[j] = __float_as_uint(__uint_as_float(g[j]) * (x_scale * __ldg(p.gate_scale + at)));
-                            u[j] = __float_as_uint(__uint_as_float(u[j]) * (x_scale * __ldg(p.up_scale + at)));
+                            const int at = (16 * k + j) % 32;
+                            g[j] = __float_as_uint(__uint_as_float(g[j]) * (x_scale * __shfl_sync(0xffffffffu, gate_scales[k / 2], at)));
+                            u[j] = __float_as_uint(__uint_as_float(u[j]) * (x_scale * __shfl_sync(0xffffffffu, up_scales[k / 2], at)));
                         }
                     }
                     uint32_t o[8];
