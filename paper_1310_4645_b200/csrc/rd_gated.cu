@@ -161,10 +161,12 @@ struct alignas(64) GradParams {
     CUtensorMap gate_mn, up_mn;       // weights as the transposed right operand of dx
     CUtensorMap x_mn;         // x as the transposed right operand of dW
     CUtensorMap dx_out, gate_out, up_out;     // results, 64 x 32 boxes
-    CUtensorMap dx_parts;     // parts of dx in 32 bits, 32 x 32 x 1 boxes
+    CUtensorMap dx_parts, dw_parts;           // parts of dx, of dWg and dWu one below the other, in 32 bits, 32 x 32 x 1 boxes
     uint32_t n, dim, width;
     uint32_t half;            // columns of dgate, a multiple of 64: where dup begins
-    uint32_t splits, steps_per_split;         // parts that the sum over both widths is cut into for dx
+    uint32_t splits, steps_per_split;         // parts that the sum over both widths is cut into for dx, and steps of one
+    uint32_t splits_w, steps_per_split_w;     // the same of the sum over rows for dWg and dWu
+    uint32_t part_rows;       // rows of a part of dWg: the width, up to whole tiles
     uint32_t a_rows;
     uint32_t idesc;
     uint32_t weights;         // which of dWg (1) and dWu (2) are wanted
@@ -208,43 +210,45 @@ template <int CG> struct GatedPlan {
         return true;
     }
 };
-// Gradient: the units of dx first, dealt out in turn; their number need not divide by g, so some groups get one more of them, and that
-// many fewer of dW's tiles, by the number of steps of the summed index.
+// How the gradient's units are dealt out over g groups: those of dx first, in turn.  Their number need not divide by g, so the first `more`
+// groups get one more of them.  The others then take as many units of dW as that is worth by the steps of the summed index, or come
+// first where dW's do not divide either.
+struct Deal {
+    uint32_t dx_each, more, even;             // units of dx that every group gets; turns of dW that all take part in, the others first
+    __host__ __device__ Deal(uint32_t dx_units, uint32_t dx_steps, uint32_t dw_units, uint32_t dw_steps, uint32_t g) : dx_each(dx_units / g), more(dx_units % g)
+    {
+        const uint32_t worth = more ? (2 * (dx_steps + kTileOverhead) + dw_steps) / (2 * (dw_steps + kTileOverhead)) : 0, ahead = worth * (g - more);
+        even = dw_units > ahead ? (dw_units - ahead + g - 1) / g : 0;
+    }
+};
 template <int CG> struct GradPlan {
     static constexpr uint32_t kTileM = kRowsM * CG;
     const GradParams &p;
     Cursor at;
-    uint32_t c, g, tiles_n, tiles_m, tiles_w, dw_tiles, dw_even, dx_more, left, phase = 0, split = 0, steps_n, steps_w;
-    __device__ __forceinline__ explicit GradPlan(const GradParams &params) : p(params), c(blockIdx.x / CG), g(gridDim.x / CG)
+    uint32_t c, g, tiles_n, tiles_m, tiles_w, down, dw_units, left, phase = 0, split = 0, steps_n, steps_w;
+    Deal deal;
+    __device__ __forceinline__ explicit GradPlan(const GradParams &params)
+        : p(params), c(blockIdx.x / CG), g(gridDim.x / CG), tiles_n((p.dim + kTileN - 1) / kTileN), tiles_m((p.n + kTileM - 1) / kTileM), tiles_w((p.width + kTileM - 1) / kTileM),
+          down(((p.weights & 1) + (p.weights >> 1)) * tiles_w),              // tiles of dWg and dWu one below the other
+          dw_units(down * tiles_n * p.splits_w), steps_n((p.n + kTileK - 1) / kTileK), steps_w(2 * p.half / kTileK),
+          deal(p.want_dx ? tiles_m * tiles_n * p.splits : 0, p.steps_per_split, dw_units, p.steps_per_split_w, g)
     {
-        tiles_n = (p.dim + kTileN - 1) / kTileN;
-        tiles_m = (p.n + kTileM - 1) / kTileM;
-        tiles_w = (p.width + kTileM - 1) / kTileM;
-        steps_n = (p.n + kTileK - 1) / kTileK;
-        steps_w = 2 * p.half / kTileK;
-        const uint32_t dx_units = p.want_dx ? tiles_m * tiles_n * p.splits : 0;
-        dw_tiles = __popc(p.weights) * tiles_w * tiles_n;
-        dx_more = dx_units % g;
-        // a unit of dx is worth this many tiles of dW, which the groups without it take first
-        const uint32_t worth = dx_more ? (2 * (p.steps_per_split + kTileOverhead) + steps_n) / (2 * (steps_n + kTileOverhead)) : 0;
-        const uint32_t ahead = worth * (g - dx_more);
-        dw_even = dw_tiles > ahead ? (dw_tiles - ahead + g - 1) / g : 0;      // turns that every group takes part in
-        left = dx_units / g + (c < dx_more);
+        left = deal.dx_each + (c < deal.more);
         at.set(c, g, tiles_n);
     }
     __device__ __forceinline__ bool next(Work &w)
     {
-        while (left == 0 || (phase != 0 && at.y * tiles_n + at.x >= dw_tiles)) {
+        while (left == 0 || (phase != 0 && at.y * tiles_n + at.x >= dw_units)) {
             if (phase == 2) {
                 left = 0;
                 return false;
             }
             if (++phase == 1) {
-                left = dw_even;
-                at.set(c, g, tiles_n);
+                left = deal.even;
+                at.set(c < deal.more ? c + g - deal.more : c - deal.more, g, tiles_n);
             } else {
-                left = c < dx_more ? 0 : 0xffffffffu;         // until the tiles run out
-                at.set(dw_even * g + c - dx_more, g - dx_more, tiles_n);
+                left = c < deal.more ? 0 : 0xffffffffu;       // until the units run out
+                at.set(deal.even * g + c - deal.more, g - deal.more, tiles_n);
             }
         }
         if (phase == 0) {
@@ -255,8 +259,9 @@ template <int CG> struct GradPlan {
             const uint32_t k0 = split * p.steps_per_split;
             w = Work{1, at.y * kTileM, at.x * kTileN, k0 * kTileK, min(p.steps_per_split, steps_w - k0), split, false};
         } else {
-            const bool second = p.weights == 2 || at.y >= tiles_w;
-            w = Work{2, (at.y >= tiles_w ? at.y - tiles_w : at.y) * kTileM, at.x * kTileN, 0, steps_n, 0, second};
+            const uint32_t part = p.splits_w == 1 ? 0 : at.y / down, y = at.y - part * down, k0 = part * p.steps_per_split_w;
+            const bool second = p.weights == 2 || y >= tiles_w;
+            w = Work{2, (y >= tiles_w ? y - tiles_w : y) * kTileM, at.x * kTileN, k0 * kTileK, min(p.steps_per_split_w, steps_n - k0), part, second};
         }
         left--;
         at.advance();
@@ -481,7 +486,9 @@ __global__ void __launch_bounds__(kMmaThreads, 1) rd_gated_mma_kernel(const __gr
                 }
             } else {
                 const uint32_t box = boxes + (warp - 4) * kBox, col0 = w.n0 + 128 * half;
-                const bool parts = w.product == 1 && p.splits > 1;
+                const bool parts = (w.product == 1 ? p.splits : p.splits_w) > 1;
+                const CUtensorMap *parts_map = w.product == 1 ? &p.dx_parts : &p.dw_parts;
+                const uint32_t parts_row = row0 + (w.second ? p.part_rows : 0);
                 const CUtensorMap *map = w.product == 1 ? &p.dx_out : w.second ? &p.up_out : &p.gate_out;
                 const bool tma = w.product == 1 ? p.dx_tma : w.second ? p.up_tma : p.gate_tma;
                 const uint32_t rows = w.product == 1 ? p.n : p.width;
@@ -500,7 +507,7 @@ __global__ void __launch_bounds__(kMmaThreads, 1) rd_gated_mma_kernel(const __gr
 #pragma unroll
                         for (int q = 0; q < 8; q++) box_put(box, lane, q, x[4 * q], x[4 * q + 1], x[4 * q + 2], x[4 * q + 3]);
                         if (box_full(lane, true) && col < p.dim && row0 < rows) {
-                            tma_store(&p.dx_parts, box, col, row0, w.split);
+                            tma_store(parts_map, box, col, parts_row, w.split);
                             box_sent();
                         }
                         continue;
@@ -637,6 +644,22 @@ template <int V> __global__ void __launch_bounds__(256) rd_gated_slope_kernel(co
             }
             *reinterpret_cast<uint4 *>(dst) = make_uint4(a[0], a[1], a[2], a[3]);
             *reinterpret_cast<uint4 *>(dst + p.half) = make_uint4(b[0], b[1], b[2], b[3]);
+        } else if constexpr (V == 2) {
+            uint32_t a = 0, b = 0;
+            if (col < p.width) {
+                const float2 g = widen2(p.bf16, *reinterpret_cast<const uint32_t *>(p.gate + row * p.gate_stride + col)),
+                             u = widen2(p.bf16, *reinterpret_cast<const uint32_t *>(p.up + row * p.up_stride + col)),
+                             d = widen2(p.bf16, *reinterpret_cast<const uint32_t *>(p.grad_out + row * p.grad_out_stride + col));
+                with_act(p.act, [&](auto ACT) {
+                    float v0, s0, v1, s1;
+                    act_both<decltype(ACT)::value>(g.x, v0, s0);
+                    act_both<decltype(ACT)::value>(g.y, v1, s1);
+                    a = pack2(p.bf16, d.x * u.x * s0, d.y * u.y * s1);
+                    b = pack2(p.bf16, d.x * v0, d.y * v1);
+                });
+            }
+            *reinterpret_cast<uint32_t *>(dst) = a;
+            *reinterpret_cast<uint32_t *>(dst + p.half) = b;
         } else {
             uint32_t a = 0, b = 0;
             if (col < p.width) {
@@ -655,40 +678,54 @@ template <int V> __global__ void __launch_bounds__(256) rd_gated_slope_kernel(co
     }
 }
 
-// Adds the parts of dx and rounds: four threads to four columns, each with every fourth part in order, then those in order.
+// Adds parts of results and rounds: four threads to four columns, each with every fourth part in order, then those in order.
 constexpr uint32_t kFinishColumns = 256;
-__global__ void __launch_bounds__(256) rd_gated_finish_kernel(uint16_t *out, size_t out_stride, const float *parts, size_t stride, size_t n, uint32_t dim, uint32_t splits, bool bf16, bool wide)
+struct FinishParams {
+    struct {
+        uint16_t *out;
+        const float *parts;
+        size_t out_stride, step, first;       // step: from one part to the next; number of the first row
+        uint32_t splits;
+        bool wide;
+    } m[3];
+    uint32_t matrices, dim, stride;           // stride: of a part's rows, a multiple of 32
+    size_t rows;
+    bool bf16;
+};
+__global__ void __launch_bounds__(256) rd_gated_finish_kernel(const __grid_constant__ FinishParams p)
 {
     __shared__ float4 sums[3][64];
     pdl_start();
     const uint32_t x = threadIdx.x & 63, y = threadIdx.x >> 6, j = blockIdx.y * kFinishColumns + x * 4;
-    for (size_t row = blockIdx.x; row < n; row += gridDim.x) {
+    for (size_t r = blockIdx.x; r < p.rows; r += gridDim.x) {
+        const auto &m = p.matrices > 2 && r >= p.m[2].first ? p.m[2] : p.matrices > 1 && r >= p.m[1].first ? p.m[1] : p.m[0];
+        const size_t row = r - m.first;
         float4 sum = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-        if (j < dim) {
-            const float *src = parts + row * stride + j;           // rows hold a multiple of 32 values
+        if (j < p.dim) {
+            const float *src = m.parts + row * p.stride + j;
 #pragma unroll 8
-            for (uint32_t s = y; s < splits; s += 4) {
-                const float4 v = *reinterpret_cast<const float4 *>(src + s * n * stride);
+            for (uint32_t s = y; s < m.splits; s += 4) {
+                const float4 v = *reinterpret_cast<const float4 *>(src + s * m.step);
                 sum = make_float4(sum.x + v.x, sum.y + v.y, sum.z + v.z, sum.w + v.w);
             }
         }
         if (y) sums[y - 1][x] = sum;
         __syncthreads();
-        if (y == 0 && j < dim) {
+        if (y == 0 && j < p.dim) {
 #pragma unroll
             for (int k = 0; k < 3; k++) {
                 const float4 v = sums[k][x];
                 sum = make_float4(sum.x + v.x, sum.y + v.y, sum.z + v.z, sum.w + v.w);
             }
-            const uint32_t lo = pack2(bf16, sum.x, sum.y), hi = pack2(bf16, sum.z, sum.w);
-            uint16_t *dst = out + row * out_stride + j;
-            if (wide && j + 4 <= dim) {
+            const uint32_t lo = pack2(p.bf16, sum.x, sum.y), hi = pack2(p.bf16, sum.z, sum.w);
+            uint16_t *dst = m.out + row * m.out_stride + j;
+            if (m.wide && j + 4 <= p.dim) {
                 *reinterpret_cast<uint2 *>(dst) = make_uint2(lo, hi);
             } else {
                 const uint16_t v[4] = {uint16_t(lo), uint16_t(lo >> 16), uint16_t(hi), uint16_t(hi >> 16)};
 #pragma unroll
                 for (int k = 0; k < 4; k++)
-                    if (j + k < dim) dst[k] = v[k];
+                    if (j + k < p.dim) dst[k] = v[k];
             }
         }
         __syncthreads();
@@ -713,27 +750,43 @@ struct Layout {
     size_t copy_stride;                       // in elements
     uint16_t *both;
     size_t half;
-    float *parts;
-    size_t splits, steps_per_split, part_stride, bytes;
+    float *parts, *parts_w;
+    size_t splits, steps_per_split, splits_w, steps_per_split_w, part_stride, part_rows, bytes;
 };
 
-// Parts that the sum over both widths is cut into for dx.  More parts fill the groups of thread blocks more evenly, but each is a
-// matrix of its own that is written and read once more; times in steps of the summed index.
-size_t dx_splits(const GatedArgs &a, size_t half)
+// Parts that the sums are cut into, over both widths for dx and over the rows for dWg and dWu.  More parts fill the groups of thread blocks
+// more evenly, but each is a matrix of its own that is written and read once more; times in steps of the summed index, of which parts
+// have to save a fifth, as groups without work leave the others more power and bandwidth.  B200, without parts and with: 200 x 1000 x 2730
+// (6 of dx) 31 / 18 us, 32768 x 512 x 512 (8 of the weights' gradients) 194 / 103, 65536 x 1024 x 1024 (2) 665 / 587, 16384 x 1024 x 4096 (2)
+// 573 / 581 and therefore none.
+struct Splits {
+    size_t x, w;
+};
+Splits splits_of(const GatedArgs &a, size_t half)
 {
-    const size_t cg = pair_or_single(a.n), tile_m = kRowsM * cg, groups = kSms / cg, steps = 2 * half / kTileK;
-    const size_t tiles_n = (a.dim + kTileN - 1) / kTileN, tiles = (a.n + tile_m - 1) / tile_m * tiles_n;
+    const size_t cg = pair_or_single(a.n), tile_m = kRowsM * cg, groups = kSms / cg, steps_x = 2 * half / kTileK, steps_w = (a.n + kTileK - 1) / kTileK;
+    const size_t tiles_n = (a.dim + kTileN - 1) / kTileN, tiles_x = (a.n + tile_m - 1) / tile_m * tiles_n, tiles_w = 2 * ((a.width + tile_m - 1) / tile_m) * tiles_n;
     const double step_bytes = 0.28e-6 * 6.5e12, finish = 9;
-    const double dw = double(2 * ((a.width + tile_m - 1) / tile_m) * tiles_n) * double((a.n + kTileK - 1) / kTileK + kTileOverhead);
-    size_t best = 1;
-    double best_time = 0;
-    for (size_t s = 1; s <= 64 && s * 4 <= steps + 3; s++) {
-        const size_t units = tiles * s;
-        const double unit = double((steps + s - 1) / s + kTileOverhead), even = (double(units) * unit + dw) / double(groups);
-        const double longest = double((units + groups - 1) / groups) * unit;
-        const double time = (even > longest ? even : longest) + (s == 1 ? 0 : double(s) * double(a.n * a.dim) * 8 / step_bytes + finish);
-        if (s == 1 || time < best_time) best = s, best_time = time;
-    }
+    auto steps_of = [](size_t steps, size_t s) { return uint32_t((steps + s - 1) / s); };
+    auto most = [&](size_t x, size_t w) {     // steps of the group that gets the most: one with one more unit of dx, or another
+        const size_t units_x = tiles_x * x, units_w = tiles_w * w, g = units_x + units_w < groups ? units_x + units_w : groups;
+        const uint32_t sx = steps_of(steps_x, x), sw = steps_of(steps_w, w);
+        const Deal d(uint32_t(units_x), sx, uint32_t(units_w), sw, uint32_t(g));
+        const size_t in_turns = size_t(d.even) * g, others = g - d.more, last = units_w < in_turns ? units_w + g - in_turns : g;   // last: units of the last turn
+        const size_t w_more = d.even - (last <= others && last < g), w_others = d.even + (units_w > in_turns ? (units_w - in_turns + others - 1) / others : 0);
+        const size_t one_x = sx + kTileOverhead, one_w = sw + kTileOverhead, more = d.more ? (d.dx_each + 1) * one_x + w_more * one_w : 0, other = d.dx_each * one_x + w_others * one_w;
+        return double(more > other ? more : other);
+    };
+    Splits best{1, 1};
+    double best_time = 0.8 * most(1, 1);
+    for (const size_t x : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64})
+        for (const size_t w : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64}) {
+            if ((x == 1 && w == 1) || (x > 1 && x * 4 > steps_x) || (w > 1 && w * 4 > steps_w)) continue;
+            const double parts = ((x > 1 ? double(x * a.n) : 0) + (w > 1 ? double(w * 2 * a.width) : 0)) * double(a.dim) * 8 / step_bytes + finish;
+            if (parts >= best_time) continue;
+            const double time = most(x, w) + parts;
+            if (time < best_time) best = Splits{x, w}, best_time = time;
+        }
     return best;
 }
 
@@ -751,11 +804,18 @@ Layout lay_out(const GatedArgs &a, bool gradient, bool want_x)
     if (gradient) {
         l.half = round_up(a.width, 64);
         l.both = w.take<uint16_t>(a.n * 2 * l.half);
-        const size_t steps = 2 * l.half / kTileK, splits = want_x ? dx_splits(a, l.half) : 1;
-        l.steps_per_split = (steps + splits - 1) / splits;
-        l.splits = (steps + l.steps_per_split - 1) / l.steps_per_split;
+        // whatever is wanted, so that the bits do not depend on it
+        const Splits splits = splits_of(a, l.half);
+        auto cut = [](size_t steps, size_t parts, size_t *each, size_t *number) {
+            *each = (steps + parts - 1) / parts;
+            *number = (steps + *each - 1) / *each;
+        };
+        cut(2 * l.half / kTileK, splits.x, &l.steps_per_split, &l.splits);
+        cut((a.n + kTileK - 1) / kTileK, splits.w, &l.steps_per_split_w, &l.splits_w);
         l.part_stride = round_up(a.dim, 32);
-        if (l.splits > 1) l.parts = w.take<float>(l.splits * a.n * l.part_stride);
+        l.part_rows = round_up(a.width, size_t(kRowsM) * pair_or_single(a.n));
+        if (l.splits > 1 && want_x) l.parts = w.take<float>(l.splits * a.n * l.part_stride);
+        if (l.splits_w > 1) l.parts_w = w.take<float>(l.splits_w * 2 * l.part_rows * l.part_stride);
     }
     l.bytes = w.at;
     return l;
@@ -929,13 +989,16 @@ cudaError_t gated_backward(const GatedArgs &a)
     s.half = uint32_t(l.half);
     s.act = a.activation;
     s.bf16 = bf16;
-    const bool wide = a.width % 8 == 0 && tma_rows(a.gate, a.gate_stride, 2) && tma_rows(a.up, a.up_stride, 2) && tma_rows(a.grad_out, a.grad_out_stride, 2);
-    const uint32_t units = s.half / (wide ? 8 : 1);
+    // values that an access takes
+    int v = a.width % 8 == 0 ? 8 : a.width % 2 == 0 ? 2 : 1;
+    for (const auto &m : {Operand{a.gate, a.gate_stride}, Operand{a.up, a.up_stride}, Operand{a.grad_out, a.grad_out_stride}})
+        while (v > 1 && (reinterpret_cast<uintptr_t>(m.p) % (2 * v) != 0 || m.stride % v != 0)) v = v == 8 ? 2 : 1;
+    const uint32_t units = s.half / v;
     s.across = 256;
     while (s.across > 8 && s.across >= 2 * units) s.across /= 2;
     const size_t down = 256 / s.across, tall = (a.n + down - 1) / down;
     const dim3 grid(unsigned(tall < 65536 ? tall : 65536), (units + s.across - 1) / s.across);
-    e = wide ? launch(rd_gated_slope_kernel<8>, grid, 256, a.stream, s) : launch(rd_gated_slope_kernel<1>, grid, 256, a.stream, s);
+    e = v == 8 ? launch(rd_gated_slope_kernel<8>, grid, 256, a.stream, s) : v == 2 ? launch(rd_gated_slope_kernel<2>, grid, 256, a.stream, s) : launch(rd_gated_slope_kernel<1>, grid, 256, a.stream, s);
     if (e != cudaSuccess) return e;
 
     GradParams p{};
@@ -945,6 +1008,9 @@ cudaError_t gated_backward(const GatedArgs &a)
     p.half = uint32_t(l.half);
     p.splits = uint32_t(l.splits);
     p.steps_per_split = uint32_t(l.steps_per_split);
+    p.splits_w = uint32_t(l.splits_w);
+    p.steps_per_split_w = uint32_t(l.steps_per_split_w);
+    p.part_rows = uint32_t(l.part_rows);
     p.a_rows = rows_in(a.n);
     p.idesc = descriptor(a.dtype, kTileN, uint32_t(tile_m));
     p.weights = (a.grad_gate_weight ? 1u : 0u) | (a.grad_up_weight ? 2u : 0u);
@@ -964,14 +1030,25 @@ cudaError_t gated_backward(const GatedArgs &a)
         !encode(&p.x_mn, bf16, o.x.p, a.dim, a.n, o.x.stride, 64) || (p.dx_tma && !encode(&p.dx_out, bf16, a.grad_x, a.dim, a.n, a.grad_x_stride, 32)) ||
         (p.gate_tma && !encode(&p.gate_out, bf16, a.grad_gate_weight, a.dim, a.width, a.grad_gate_weight_stride, 32)) ||
         (p.up_tma && !encode(&p.up_out, bf16, a.grad_up_weight, a.dim, a.width, a.grad_up_weight_stride, 32)) ||
-        (l.splits > 1 && !encode_dh(&p.dx_parts, l.parts, l.part_stride, a.n, l.splits)))
+        (l.parts && !encode_dh(&p.dx_parts, l.parts, l.part_stride, a.n, l.splits)) ||
+        (l.parts_w && !encode_dh(&p.dw_parts, l.parts_w, l.part_stride, 2 * l.part_rows, l.splits_w)))
         return cudaErrorInvalidValue;
-    const size_t work = (want_x ? tiles_m * tiles_n * l.splits : 0) + __builtin_popcount(p.weights) * ((a.width + tile_m - 1) / tile_m) * tiles_n;
+    const size_t work = (want_x ? tiles_m * tiles_n * l.splits : 0) + __builtin_popcount(p.weights) * ((a.width + tile_m - 1) / tile_m) * tiles_n * l.splits_w;
     e = cg == 2 ? launch_mma<true, false, 2>(p, device, work, a.stream) : launch_mma<true, false, 1>(p, device, work, a.stream);
-    if (e != cudaSuccess || l.splits == 1) return e;
-    const bool wide_x = reinterpret_cast<uintptr_t>(a.grad_x) % 8 == 0 && a.grad_x_stride % 4 == 0;
-    const dim3 rows(unsigned(a.n < 65536 ? a.n : 65536), unsigned((a.dim + kFinishColumns - 1) / kFinishColumns));
-    return launch(rd_gated_finish_kernel, rows, 256, a.stream, p.dx, a.grad_x_stride, static_cast<const float *>(l.parts), l.part_stride, a.n, uint32_t(a.dim), p.splits, bf16, wide_x);
+    if (e != cudaSuccess) return e;
+    FinishParams f{};
+    auto add = [&](void *out, size_t stride, const float *parts, size_t rows, size_t part_rows, size_t splits) {
+        f.m[f.matrices++] = {static_cast<uint16_t *>(out), parts, stride, part_rows * l.part_stride, f.rows, uint32_t(splits), reinterpret_cast<uintptr_t>(out) % 8 == 0 && stride % 4 == 0};
+        f.rows += rows;
+    };
+    if (want_x && l.parts) add(a.grad_x, a.grad_x_stride, l.parts, a.n, a.n, l.splits);
+    if (a.grad_gate_weight && l.parts_w) add(a.grad_gate_weight, a.grad_gate_weight_stride, l.parts_w, a.width, 2 * l.part_rows, l.splits_w);
+    if (a.grad_up_weight && l.parts_w) add(a.grad_up_weight, a.grad_up_weight_stride, l.parts_w + l.part_rows * l.part_stride, a.width, 2 * l.part_rows, l.splits_w);
+    if (!f.rows) return e;
+    f.dim = uint32_t(a.dim);
+    f.stride = uint32_t(l.part_stride);
+    f.bf16 = bf16;
+    return launch(rd_gated_finish_kernel, dim3(unsigned(f.rows < 65536 ? f.rows : 65536), unsigned((a.dim + kFinishColumns - 1) / kFinishColumns)), 256, a.stream, f);
 }
 
 cudaError_t block_status(int *status)

@@ -5,9 +5,9 @@ import pytest
 import torch
 
 import paper_1310_4645_b200 as rd
-from test_gated import activation, project
+from test_gated import ACTS, HALF, activation, blank, grad_reference, outside_untouched, project
 from test_norm import BF16, E, E4M3, FP32, kept
-from test_vocab import TINY, U, gen, rand, within
+from test_vocab import TINY, U, gen, rand, strided, within
 
 gpu = pytest.mark.gpu
 
@@ -119,4 +119,43 @@ def test_gated_of_more_than_two_to_the_31_values():
     # the same products, added up in other parts: each sum within 2 * width (2) terms' roundings of the magnitudes
     assert (gx[-2:].double() - sx.double()).norm() <= 2 * U[BF16] * sx.double().norm()
     assert (gg.double() - sg.double()).norm() <= 2 * U[BF16] * sg.double().norm() and (gu.double() - su.double()).norm() <= 2 * U[BF16] * su.double().norm()
+    assert rd.rd_block_status() == rd.RD_OK
+
+
+@gpu
+@pytest.mark.parametrize("dtype", HALF)
+@pytest.mark.parametrize("n, dim, width", [(300, 40, 24), (1924, 64, 256), (1025, 1, 1), (4046, 192, 128), (3001, 130, 77), (6550, 256, 1003), (8170, 128, 2048), (2000, 24, 4100), (20000, 65, 129)])
+def test_gated_grad_of_few_columns(dtype, n, dim, width):
+    """Few tiles of the weights' gradients, and many rows that each is a sum over."""
+    x, wg, wu = rand(n, dim, seed=61, dtype=dtype), rand(width, dim, seed=62, dtype=dtype, std=dim ** -0.5), rand(width, dim, seed=63, dtype=dtype, std=dim ** -0.5)
+    gate, up, d = (rand(n, width, seed=64 + k, dtype=dtype) for k in range(3))
+    act = ACTS[(n + width) % 3]
+    want = grad_reference(*(t.double() for t in (d, x, wg, wu, gate, up)), act, dtype)
+    first = None
+    for pad, offset in ((0, 0), (8, 0), (2, 0), (2, 2), (3, 1)):
+        put = lambda t: strided(t, pad, offset)
+        outs = [blank(r, dim, dtype, pad, offset) for r in (n, width, width)]
+        rd.rd_gated_grad(put(d), put(x), put(wg), put(wu), put(gate), put(up), act, grad_x=outs[0], grad_gate_weight=outs[1], grad_up_weight=outs[2])
+        if first is None:
+            first = outs
+            for o, (w, e) in zip(outs, want):
+                within(o, w, e + U[dtype] * (w.abs() + e) + TINY[dtype])
+        assert all(map(torch.equal, outs, first)) and all(map(outside_untouched, outs))
+    # what is wanted does not change the bits
+    args = (d, x, wg, wu, gate, up, act)
+    assert torch.equal(rd.rd_gated_grad(*args, want_weights=False)[0], first[0])
+    assert all(map(torch.equal, rd.rd_gated_grad(*args, want_x=False)[1:], first[1:]))
+    for k, name in ((1, "grad_gate_weight"), (2, "grad_up_weight")):
+        for want_x in (False, True):
+            into = torch.empty_like(wg)
+            rd.rd_gated_grad(*args, want_x=want_x, want_weights=False, **{name: into})
+            assert torch.equal(into, first[k])
+    # recorded, and played again on other rows
+    graph, inputs = torch.cuda.CUDAGraph(), [t.clone() for t in args[:-1]]
+    with torch.cuda.graph(graph):
+        got = rd.rd_gated_grad(*inputs, act)
+    inputs[0].copy_(d.flip(0)), inputs[1].copy_(x.flip(0)), inputs[4].copy_(gate.flip(0)), inputs[5].copy_(up.flip(0))
+    graph.replay()
+    assert torch.equal(got[0], first[0].flip(0))
+    assert all(map(torch.equal, got, rd.rd_gated_grad(*inputs, act)))
     assert rd.rd_block_status() == rd.RD_OK
