@@ -615,66 +615,53 @@ struct SlopeParams {
     bool bf16;
 };
 
-// dgate and dup, V values a thread at a time.
-template <int V> __global__ void __launch_bounds__(256) rd_gated_slope_kernel(const __grid_constant__ SlopeParams p)
+// dgate and dup, V values at a time, as many as the rows' alignment allows.  Where there are enough of them for all threads, a thread has 8
+// values of a row in accesses p.across threads apart that are all under way together.  B200, with one access a thread and with these:
+// 6550 x 256 x 4978 (pairs of values) 162 and 148 us, 4979 (single ones) 218 and 181, 200 x 1000 x 2730 17.5 and 19.5.
+template <int V, int kWords> __global__ void __launch_bounds__(256) rd_gated_slope_kernel(const __grid_constant__ SlopeParams p)
 {
+    using Word = std::conditional_t<V == 8, uint4, std::conditional_t<V == 2, uint32_t, uint16_t>>;
+    constexpr int kPairs = (V + 1) / 2;                  // pairs of values of an access
+    union Values {
+        Word word;
+        uint32_t pair[kPairs];
+    };
     pdl_start();
-    const uint32_t x = threadIdx.x % p.across, y = threadIdx.x / p.across, down = 256 / p.across;
-    const uint32_t col = (blockIdx.y * p.across + x) * V;
-    if (col >= p.half) return;
+    const uint32_t x = threadIdx.x % p.across, y = threadIdx.x / p.across, down = 256 / p.across, col = (blockIdx.y * p.across * kWords + x) * V, apart = p.across * V;
     for (size_t row = size_t(blockIdx.x) * down + y; row < p.n; row += size_t(gridDim.x) * down) {
-        uint16_t *dst = p.both + row * 2 * p.half + col;
-        if constexpr (V == 8) {
-            uint32_t a[4] = {}, b[4] = {};
-            if (col < p.width) {
-                const uint4 g = *reinterpret_cast<const uint4 *>(p.gate + row * p.gate_stride + col), u = *reinterpret_cast<const uint4 *>(p.up + row * p.up_stride + col),
-                            d = *reinterpret_cast<const uint4 *>(p.grad_out + row * p.grad_out_stride + col);
-                const uint32_t gs[4] = {g.x, g.y, g.z, g.w}, us[4] = {u.x, u.y, u.z, u.w}, ds[4] = {d.x, d.y, d.z, d.w};
-                with_act(p.act, [&](auto ACT) {
+        Values g[kWords], u[kWords], d[kWords];
+        auto load = [&](Values &v, const uint16_t *matrix, size_t stride, uint32_t j) {
+            v.pair[0] = 0;
+            if (j < p.width) v.word = *reinterpret_cast<const Word *>(matrix + row * stride + j);
+        };
 #pragma unroll
-                    for (int i = 0; i < 4; i++) {
-                        const float2 gi = widen2(p.bf16, gs[i]), ui = widen2(p.bf16, us[i]), di = widen2(p.bf16, ds[i]);
-                        float v0, s0, v1, s1;
-                        act_both<decltype(ACT)::value>(gi.x, v0, s0);
-                        act_both<decltype(ACT)::value>(gi.y, v1, s1);
-                        a[i] = pack2(p.bf16, di.x * ui.x * s0, di.y * ui.y * s1);
-                        b[i] = pack2(p.bf16, di.x * v0, di.y * v1);
-                    }
-                });
-            }
-            *reinterpret_cast<uint4 *>(dst) = make_uint4(a[0], a[1], a[2], a[3]);
-            *reinterpret_cast<uint4 *>(dst + p.half) = make_uint4(b[0], b[1], b[2], b[3]);
-        } else if constexpr (V == 2) {
-            uint32_t a = 0, b = 0;
-            if (col < p.width) {
-                const float2 g = widen2(p.bf16, *reinterpret_cast<const uint32_t *>(p.gate + row * p.gate_stride + col)),
-                             u = widen2(p.bf16, *reinterpret_cast<const uint32_t *>(p.up + row * p.up_stride + col)),
-                             d = widen2(p.bf16, *reinterpret_cast<const uint32_t *>(p.grad_out + row * p.grad_out_stride + col));
-                with_act(p.act, [&](auto ACT) {
-                    float v0, s0, v1, s1;
-                    act_both<decltype(ACT)::value>(g.x, v0, s0);
-                    act_both<decltype(ACT)::value>(g.y, v1, s1);
-                    a = pack2(p.bf16, d.x * u.x * s0, d.y * u.y * s1);
-                    b = pack2(p.bf16, d.x * v0, d.y * v1);
-                });
-            }
-            *reinterpret_cast<uint32_t *>(dst) = a;
-            *reinterpret_cast<uint32_t *>(dst + p.half) = b;
-        } else {
-            uint32_t a = 0, b = 0;
-            if (col < p.width) {
-                const float g = widen2(p.bf16, p.gate[row * p.gate_stride + col]).x, u = widen2(p.bf16, p.up[row * p.up_stride + col]).x,
-                            d = widen2(p.bf16, p.grad_out[row * p.grad_out_stride + col]).x;
-                with_act(p.act, [&](auto ACT) {
-                    float v, s;
-                    act_both<decltype(ACT)::value>(g, v, s);
-                    a = pack2(p.bf16, d * u * s, 0.0f);
-                    b = pack2(p.bf16, d * v, 0.0f);
-                });
-            }
-            dst[0] = uint16_t(a);
-            dst[p.half] = uint16_t(b);
+        for (int i = 0; i < kWords; i++) {
+            load(g[i], p.gate, p.gate_stride, col + i * apart);
+            load(u[i], p.up, p.up_stride, col + i * apart);
+            load(d[i], p.grad_out, p.grad_out_stride, col + i * apart);
         }
+        with_act(p.act, [&](auto ACT) {
+#pragma unroll
+            for (int i = 0; i < kWords; i++) {
+                const uint32_t j = col + i * apart;
+                if (j >= p.half) break;
+                Values a = {}, b = {};
+                if (j < p.width) {
+#pragma unroll
+                    for (int k = 0; k < kPairs; k++) {
+                        const float2 gk = widen2(p.bf16, g[i].pair[k]), uk = widen2(p.bf16, u[i].pair[k]), dk = widen2(p.bf16, d[i].pair[k]);
+                        float v0, s0, v1, s1;
+                        act_both<decltype(ACT)::value>(gk.x, v0, s0);
+                        act_both<decltype(ACT)::value>(gk.y, v1, s1);
+                        a.pair[k] = pack2(p.bf16, dk.x * uk.x * s0, dk.y * uk.y * s1);
+                        b.pair[k] = pack2(p.bf16, dk.x * v0, dk.y * v1);
+                    }
+                }
+                uint16_t *dst = p.both + row * 2 * p.half + j;
+                *reinterpret_cast<Word *>(dst) = a.word;
+                *reinterpret_cast<Word *>(dst + p.half) = b.word;
+            }
+        });
     }
 }
 
@@ -993,12 +980,15 @@ cudaError_t gated_backward(const GatedArgs &a)
     int v = a.width % 8 == 0 ? 8 : a.width % 2 == 0 ? 2 : 1;
     for (const auto &m : {Operand{a.gate, a.gate_stride}, Operand{a.up, a.up_stride}, Operand{a.grad_out, a.grad_out_stride}})
         while (v > 1 && (reinterpret_cast<uintptr_t>(m.p) % (2 * v) != 0 || m.stride % v != 0)) v = v == 8 ? 2 : 1;
-    const uint32_t units = s.half / v;
+    const bool many = a.n * s.half >= kSms * 1024 * 8;   // half of the threads that there can be, with 8 values each
+    const uint32_t units = s.half / (many ? 8 : v);      // threads to a row
     s.across = 256;
     while (s.across > 8 && s.across >= 2 * units) s.across /= 2;
     const size_t down = 256 / s.across, tall = (a.n + down - 1) / down;
     const dim3 grid(unsigned(tall < 65536 ? tall : 65536), (units + s.across - 1) / s.across);
-    e = v == 8 ? launch(rd_gated_slope_kernel<8>, grid, 256, a.stream, s) : v == 2 ? launch(rd_gated_slope_kernel<2>, grid, 256, a.stream, s) : launch(rd_gated_slope_kernel<1>, grid, 256, a.stream, s);
+    void (*const slope)(SlopeParams) = v == 8 ? rd_gated_slope_kernel<8, 1> : v == 2 ? many ? rd_gated_slope_kernel<2, 4> : rd_gated_slope_kernel<2, 1>
+                                                                              : many ? rd_gated_slope_kernel<1, 8> : rd_gated_slope_kernel<1, 1>;
+    e = launch(slope, grid, 256, a.stream, s);
     if (e != cudaSuccess) return e;
 
     GradParams p{};
