@@ -10,7 +10,8 @@
 // right operand is w rows of Wg followed by the same w rows of Wu, so that a value's gate and up lie in one lane of tensor memory and
 // their product never leaves the thread.  Of a pair one block brings in Wg's rows, the other Wu's.
 // Gradient: a pass over gate, up and dout leaves dgate and dup side by side, rounded to 16 bits (the operand type of the products), then
-// one launch has both kinds of products, dx over the two widths in one sum, dWg and dWu over the tokens.
+// one launch has both kinds of products, dx over the two widths in one sum, dWg and dWu over the tokens.  Where there are few tiles the sums
+// are cut into parts in 32 bits, which a last launch adds up in order.
 //
 // Operands come in by TMA into a ring of stages of 128 bytes of the summed index; one warp per operand issues the copies, one the
 // products, eight take the results; two sets of accumulators, so that one is read while the next is computed.
