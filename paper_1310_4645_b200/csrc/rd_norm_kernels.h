@@ -31,11 +31,13 @@ template <class T, class R, class W, bool SPREAD, int NV, bool WARP, int MODE> _
     Stream<WARP> stream(bars, SPREAD ? RowRing{0, 0} : p.ring);
     pdl_wait();
     if (p.release_early) pdl_release();
+    if (!WARP) cluster_begins(p.blocks);
     const Place<SPREAD, WARP, bool(MODE & kFull)> at(p.units, p.per_block, p.blocks, p.threads, gridDim.x);
     const uint32_t unit0 = WARP ? 0 : at.rank * p.per_block, own = at.end - unit0;
     const Piece pieces[2] = {{p.x, p.x_stride * kT, UnitT::bytes}, {p.residual, p.residual_stride * kR, UnitR::bytes}};
     if (!SPREAD && stream.asks)
         for (uint32_t i = 0; i < stream.stages && at.row + i * at.rows < p.n; i++) stream.ask(i, pieces, at.row + i * at.rows, unit0, own);
+    if (!WARP) cluster_has_begun(p.blocks);
     uint32_t turn = 0;
     for (size_t row = at.row; row < p.n; row += at.rows, turn++) {
         UnitT x[NV];
@@ -264,8 +266,9 @@ __global__ void __launch_bounds__(kThreads, SPREAD && NV == 4 ? 2 : 3) rd_norm_g
     if (p.release_early) pdl_release();
     if (blockIdx.x >= p.row_blocks) {
         sum_columns<T, R, W>(p, column_sums);
-        return;
+        return;                       // whole clusters of them
     }
+    if (!WARP) cluster_begins(p.blocks);
     const Place<SPREAD, WARP, bool(MODE & kFull)> at(p.units, p.per_block, p.blocks, p.threads, p.row_blocks);
     const uint32_t unit0 = WARP ? 0 : at.rank * p.per_block, own = at.end - unit0;
     const Piece pieces[3] = {{p.grad_out, p.grad_out_stride * kT, UnitT::bytes}, {p.sum, p.sum_stride * kR, UnitR::bytes}, {p.grad_sum, p.grad_sum_stride * kR, UnitR::bytes}};
@@ -274,6 +277,7 @@ __global__ void __launch_bounds__(kThreads, SPREAD && NV == 4 ? 2 : 3) rd_norm_g
     Pair acc[NV][4] = {};
     uint32_t turn = 0;
     float next_rstd = at.row < p.n ? p.rstd[at.row] : 0.0f;
+    if (!WARP) cluster_has_begun(p.blocks);
     for (size_t row = at.row; row < p.n; row += at.rows, turn++) {
         const float rstd = next_rstd;
         if (row + at.rows < p.n) next_rstd = p.rstd[row + at.rows];

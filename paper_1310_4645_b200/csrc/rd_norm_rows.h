@@ -207,6 +207,17 @@ struct Meeting {
     float2 of_block[2][8];
 };
 
+// Before the first meeting of a row's thread blocks: nobody writes to a block's shared memory until that block has begun.  Said first and
+// waited for after the first rows have been asked for, which lie in a block's own.
+__device__ __forceinline__ void cluster_begins(uint32_t blocks)
+{
+    if (blocks > 1) asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+}
+__device__ __forceinline__ void cluster_has_begun(uint32_t blocks)
+{
+    if (blocks > 1) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+
 // (sum, maximum of what is not negative) over the threads of a row: a warp, or `blocks` thread blocks of a cluster.  Two sets of places
 // take turns: whoever writes to one has seen every thread arrive after its last reading.
 template <bool WARP> __device__ __forceinline__ float2 join_row(float2 v, bool want_most, Meeting &m, uint32_t turn, uint32_t blocks, uint32_t rank)
