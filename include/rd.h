@@ -673,7 +673,7 @@ typedef struct {
 
 /*
  * rd_gated -- both projections of a gated feed-forward block, the activation and the product:
- *   gate = x . gate_weight^T,  up = x . up_weight^T  (RD_E4M3: times x_scale and gate_scale, x_scale and up_scale),
+ *   gate = x . gate_weight^T,  up = x . up_weight^T  (RD_E4M3: times x_scale, then times gate_scale or up_scale, in fp32),
  *   out = act(gate) * up;
  * products exact, sums fp32 as the tensor cores add them up, out computed from fp32 gate and up and rounded once.  (exp and 1/x of the
  * activation are within about 2^-22.)

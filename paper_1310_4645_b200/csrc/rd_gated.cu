@@ -461,8 +461,9 @@ __global__ void __launch_bounds__(kMmaThreads, 1) rd_gated_mma_kernel(const __gr
 #pragma unroll
                         for (int j = 0; j < 16; j++) {
                             const int at = (16 * k + j) % 32;
-                            g[j] = __float_as_uint(__uint_as_float(g[j]) * (x_scale * __shfl_sync(0xffffffffu, gate_scales[k / 2], at)));
-                            u[j] = __float_as_uint(__uint_as_float(u[j]) * (x_scale * __shfl_sync(0xffffffffu, up_scales[k / 2], at)));
+                            // one after the other: the product of two scales may leave fp32's range where the result does not
+                            g[j] = __float_as_uint(__uint_as_float(g[j]) * x_scale * __shfl_sync(0xffffffffu, gate_scales[k / 2], at));
+                            u[j] = __float_as_uint(__uint_as_float(u[j]) * x_scale * __shfl_sync(0xffffffffu, up_scales[k / 2], at));
                         }
                     }
                     uint32_t o[8];
