@@ -603,7 +603,8 @@ typedef struct {
  *   s = residual + dropout(x),  rstd = 1 / sqrt(mean of s^2 + eps),  out = s * rstd * weight;
  * all in fp32, sums in an order that the row's length fixes; s, rstd and out are rounded once each, out from the s that has not been rounded.
  *   out_dtype    dtype, or RD_E4M3: every row has a scale, out_scale = (largest |out| of the row) / 448, and holds out / out_scale,
- *                rounded to nearest even; a row of zeros has the scale 0.  A NaN in a row makes its scale NaN.
+ *                rounded to nearest even; a row of zeros has the scale 0.  Where a value of out is NaN (a NaN of x, residual or weight; an
+ *                infinite s, whose row has the rstd 0; a row of zeros with eps = 0) the row's scale is NaN, and so are all of its values.
  *   d_out_scale  DEVICE; n values, with RD_E4M3 alone (else NULL).
  *   d_sum        DEVICE; n x dim, sum_dtype: s; or NULL.      d_rstd  DEVICE; n values; or NULL.
  * out and sum may be x or residual (where the types agree).

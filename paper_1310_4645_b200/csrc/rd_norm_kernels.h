@@ -11,11 +11,12 @@ namespace {
 // 120.5 / 114.3 us, B200).
 enum Mode { kPlain = 0, kDrop = 1, kEight = 2, kAsk = 4, kFull = 8 };
 
-// What takes a row's largest value to 448.  Very small ones are taken near 1 first (by `lift`), so that no quotient overflows.
-__device__ __forceinline__ float eighth_factor(float most, float &lift)
+// What takes a row's largest value (`most` before rstd, `largest` after) to 448.  Very small ones are taken near 1 first (by `lift`), so that
+// no quotient overflows.  A largest value that is NaN (a NaN in the row, or an infinity beside its rstd of 0) makes every value NaN.
+__device__ __forceinline__ float eighth_factor(float most, float largest, float &lift)
 {
     lift = most < 0x1p-60f ? 0x1p64f : 1.0f;
-    return most > 0.0f ? 448.0f / (most * lift) : 0.0f;
+    return isnan(largest) ? largest : most > 0.0f ? 448.0f / (most * lift) : 0.0f;
 }
 
 // T: x and out, R: residual and sum, W: the weight.  A thread holds NV units of a row; what it has no unit for is zeros.
@@ -83,10 +84,7 @@ template <class T, class R, class W, bool SPREAD, int NV, bool WARP, int MODE> _
             }
             if (eight)
 #pragma unroll
-                for (int i = 0; i < 4; i++) {
-                    const float2 v = both(s[k][i]);
-                    stat.y = fmaxf(fmaxf(stat.y, fabsf(v.x)), fabsf(v.y));
-                }
+                for (int i = 0; i < 4; i++) stat.y = most_of(stat.y, both(s[k][i]));
         }
         const float2 sums = both(squares);
         stat.x = sums.x + sums.y;
@@ -98,10 +96,11 @@ template <class T, class R, class W, bool SPREAD, int NV, bool WARP, int MODE> _
             stream.advance();
         }
         const float rstd = rsqrtf(fmaf(stat.x, p.inv_dim, p.eps));
+        const float largest = stat.y * rstd;
         float factor = rstd;
         if (eight) {
             float lift;
-            factor = eighth_factor(stat.y, lift);
+            factor = eighth_factor(stat.y, largest, lift);
             if (lift != 1.0f) {
 #pragma unroll
                 for (int k = 0; k < NV; k++)
@@ -111,7 +110,7 @@ template <class T, class R, class W, bool SPREAD, int NV, bool WARP, int MODE> _
         }
         if (at.first()) {
             if (p.rstd) p.rstd[row] = rstd;
-            if (eight) p.out_scale[row] = stat.y * rstd / 448.0f;
+            if (eight) p.out_scale[row] = largest / 448.0f;
         }
         const Pair factors = pair(factor, factor);
         void *const out_row = at_byte(p.out, row * p.out_stride * (eight ? 1 : kT));
@@ -193,16 +192,17 @@ template <class T, class R, class W, int LANES> __global__ void __launch_bounds_
         for (int d = LANES / 2; d; d /= 2) sum += __shfl_xor_sync(0xffffffffu, sum, d);
         if (p.out8) {
 #pragma unroll
-            for (int i = 0; i < 4; i++) most = fmaxf(fmaxf(most, fabsf(both(s[i]).x)), fabsf(both(s[i]).y));
+            for (int i = 0; i < 4; i++) most = most_of(most, both(s[i]));
 #pragma unroll
-            for (int d = LANES / 2; d; d /= 2) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, d));
+            for (int d = LANES / 2; d; d /= 2) most = max_nan(most, __shfl_xor_sync(0xffffffffu, most, d));
         }
         const float rstd = rsqrtf(fmaf(sum, p.inv_dim, p.eps));
+        const float largest = most * rstd;
         float lift = 1.0f;
-        const float factor = p.out8 ? eighth_factor(most, lift) : rstd;
+        const float factor = p.out8 ? eighth_factor(most, largest, lift) : rstd;
         if (unit == 0 && live) {
             if (p.rstd) p.rstd[row] = rstd;
-            if (p.out8) p.out_scale[row] = most * rstd / 448.0f;
+            if (p.out8) p.out_scale[row] = largest / 448.0f;
         }
 #pragma unroll
         for (int i = 0; i < 4; i++) s[i] = mul2(lift != 1.0f ? mul2(s[i], pair(lift, lift)) : s[i], pair(factor, factor));

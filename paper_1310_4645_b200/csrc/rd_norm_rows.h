@@ -202,6 +202,22 @@ __device__ __forceinline__ uint32_t cluster_rank()
     return r;
 }
 
+// The larger one; NaN where either is (fmaxf would drop it).
+__device__ __forceinline__ float max_nan(float x, float y)
+{
+    float r;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(x), "f"(y));
+    return r;
+}
+
+// The largest magnitude of most and two values at once.
+__device__ __forceinline__ float most_of(float most, float2 v)
+{
+    float r;
+    asm("max.NaN.abs.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(most), "f"(v.x), "f"(v.y));
+    return r;
+}
+
 struct Meeting {
     float2 of_warp[2][kWarps];
     float2 of_block[2][8];
@@ -218,12 +234,13 @@ __device__ __forceinline__ void cluster_has_begun(uint32_t blocks)
     if (blocks > 1) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 
-// (sum, maximum of what is not negative) over the threads of a row: a warp, or `blocks` thread blocks of a cluster.  Two sets of places
+// (sum, maximum of what is not negative, NaN where one is) over the threads of a row: a warp, or `blocks` thread blocks of a cluster.  Two sets of places
 // take turns: whoever writes to one has seen every thread arrive after its last reading.
 template <bool WARP> __device__ __forceinline__ float2 join_row(float2 v, bool want_most, Meeting &m, uint32_t turn, uint32_t blocks, uint32_t rank)
 {
 #pragma unroll
     for (int d = 16; d; d /= 2) v.x += __shfl_xor_sync(0xffffffffu, v.x, d);
+    // the bits of numbers that are not negative are in their order, NaN's (max_nan's, positive) above infinity's
     if (want_most) v.y = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(v.y)));
     if (WARP) {
         __syncwarp();
@@ -236,7 +253,7 @@ template <bool WARP> __device__ __forceinline__ float2 join_row(float2 v, bool w
         v = m.of_warp[set][0];
         for (uint32_t k = 1; k < warps; k++) {
             const float2 o = m.of_warp[set][k];
-            v = make_float2(v.x + o.x, fmaxf(v.y, o.y));
+            v = make_float2(v.x + o.x, max_nan(v.y, o.y));
         }
     }
     if (blocks == 1) return v;
@@ -251,7 +268,7 @@ template <bool WARP> __device__ __forceinline__ float2 join_row(float2 v, bool w
     v = m.of_block[set][0];
     for (uint32_t k = 1; k < blocks; k++) {
         const float2 o = m.of_block[set][k];
-        v = make_float2(v.x + o.x, fmaxf(v.y, o.y));
+        v = make_float2(v.x + o.x, max_nan(v.y, o.y));
     }
     return v;
 }

@@ -1,9 +1,10 @@
-"""Values at which the block operators are easily wrong: scales whose product leaves fp32's range."""
+"""Values at which the block operators are easily wrong: scales whose product leaves fp32's range, NaN and infinities before 8 bits."""
 import pytest
 import torch
 
 import paper_1310_4645_b200 as rd
 from test_gated import E4M3, HALF, project
+from test_norm import BF16
 from test_vocab import TINY, U, gen, rand, within
 
 gpu = pytest.mark.gpu
@@ -35,3 +36,43 @@ def test_gated_8bit_scales_one_after_the_other(dtype, n, x_power, w_power):
         zero = torch.zeros_like(y)
         within(torch.where(fits, got.double(), zero), torch.where(fits, y, zero), torch.where(fits, bound, zero))
         assert (got.double().abs()[y.abs() - bound > most * (1 + U[dtype])] == torch.inf).all()
+
+@gpu
+@pytest.mark.parametrize("dim", [64, 120, 256, 2000, 2001, 4096, 9000])
+@pytest.mark.parametrize("dtype", [torch.float32, BF16])
+def test_norm_8bit_with_a_nan(dtype, dim):
+    """A NaN anywhere in a row's values, also one that the weight brings, is in the row's scale and in all of its 8-bit values."""
+    x, weight = rand(5, dim, seed=1, dtype=dtype), 1 + rand(1, dim, seed=2, std=0.2)[0]
+    clean, _, _, scale = rd.rd_norm(x, weight, x, out_dtype=E4M3)
+    for bad in (torch.nan, torch.inf):
+        for at in (0, dim // 2, dim - 1):
+            y = x.clone()
+            y[3, at] = bad
+            q, _, _, s = rd.rd_norm(y, weight, x, out_dtype=E4M3)
+            rest = torch.arange(5, device="cuda") != 3
+            # an infinity times the reciprocal root 0 of its row
+            assert torch.isnan(s[3]) and torch.isnan(q[3].float()).all()
+            assert torch.equal(s[rest], scale[rest]) and torch.equal(q[rest].float(), clean[rest].float())
+            w = weight.clone()
+            w[at] = torch.nan
+            q, _, _, s = rd.rd_norm(x, w, x, out_dtype=E4M3)
+            assert torch.isnan(s).all() and torch.isnan(q.float()).all()
+            # an infinite weight: the largest value is infinite, and times a zero NaN
+            w[at] = torch.inf
+            z = x.clone()
+            z[2, at] = 0
+            q, _, _, s = rd.rd_norm(z, w, z, out_dtype=E4M3)
+            rest = torch.arange(5, device="cuda") != 2
+            assert torch.isnan(s[2]) and torch.isnan(q[2].float()).all() and (s[rest] == torch.inf).all()
+            assert torch.isnan(q[rest, at].float()).all() and not q[rest][:, torch.arange(dim, device="cuda") != at].float().any()
+
+
+@gpu
+@pytest.mark.parametrize("dim", [96, 2000, 4095])
+def test_norm_8bit_of_zeros_without_eps(dim):
+    """0 / 0, as without 8 bits; with an eps the scale is 0."""
+    x, weight = torch.zeros(3, dim, device="cuda"), torch.ones(dim, device="cuda")
+    q, _, rstd, scale = rd.rd_norm(x, weight, eps=0.0, out_dtype=E4M3)
+    assert torch.isinf(rstd).all() and torch.isnan(scale).all() and torch.isnan(q.float()).all()
+    q, _, _, scale = rd.rd_norm(x, weight, eps=2.0 ** -126, out_dtype=E4M3)
+    assert not scale.any() and not q.float().any()
