@@ -499,7 +499,8 @@ rd_gated_t projections(const at::Tensor &x, const at::Tensor &gate, const at::Te
     v.dim = m.dim;
     v.width = g.rows;
     v.dtype = code(x);
-    v.activation = static_cast<rd_activation_t>(whole(activation));
+    const int64_t act = whole(activation);
+    v.activation = static_cast<rd_activation_t>(act == int32_t(act) ? int32_t(act) : -1);      // -1: refused by the call
     if (scales) {
         v.x_scale = scale_vector(scales[0], m.rows, x.device(), "x_scale must be a contiguous float32 CUDA vector with one value per row, on the operands' device");
         v.gate_scale = scale_vector(scales[1], g.rows, x.device(), "gate_scale must be a contiguous float32 CUDA vector with one value per weight row, on the operands' device");
