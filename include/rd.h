@@ -571,11 +571,13 @@ RD_API int rd_vocab_status(int *device_status);
  * Operators of a feed-forward block (the paper has no counterpart).  A model cut over processes sums partial results of its blocks
  * with rd_allreduce; these operators are what stands between two such sums on one process: dropout, the residual's addition and a
  * norm of the joined rows, then the gated projections, of which a process holds a slice of the width.
- *   - Matrices, streams, errors and overlaps as for the operators on a vocabulary, with one exception: an output may be the very same
- *     matrix (address, stride, element size) as one of the call's inputs, where a function says so.
+ *   - Matrices, streams, errors and overlaps as for the operators on a vocabulary, with two exceptions: an output may be the very same
+ *     matrix (address, stride, element size) as one of the call's inputs, where a function says so; and every input of n rows may have
+ *     the stride 0 (every row is the same one), weights may not.
  *   - n = 0 is RD_OK (gradients of weights are then zeros).  Results depend on the arguments alone: no sum depends on timing.
  *   - Dropout: drop in [0, 1); a value is dropped where its 16 random bits are below border = drop * 65536, rounded to nearest even
- *     (a border of 65536: RD_ERR_INVALID_ARG), and multiplied by 65536 / (65536 - border), in fp32, where they are not.  The random
+ *     (a border of 65536: RD_ERR_INVALID_ARG), and multiplied by 65536 / (65536 - border), in fp32, where they are not.  A dropped
+ *     value is 0 whatever it was, an infinity or NaN as well.  The random
  *     bits of column j of row i are number j mod 8 (word (j mod 8) / 2, lower half first) of Philox 4x32 with 10 rounds at the counter
  *     (j / 8, first_row + i, offset mod 2^32, offset / 2^32) with the key (seed mod 2^32, seed / 2^32): a function of the place
  *     alone, so a gradient draws the same mask again, and a process that holds rows first_row.. of a batch draws its own.
@@ -601,7 +603,9 @@ typedef struct {
 /*
  * rd_norm -- the residual's addition and a root-mean-square norm, row by row:
  *   s = residual + dropout(x),  rstd = 1 / sqrt(mean of s^2 + eps),  out = s * rstd * weight;
- * all in fp32, sums in an order that the row's length fixes; s, rstd and out are rounded once each, out from the s that has not been rounded.
+ * all in fp32, out as (s * weight) * rstd; s, rstd and out are rounded once each, out from the s that has not been rounded.  The order in
+ * which a row is summed depends on its length and on whether it moves in words or by element (below), so that last bits may differ
+ * between a matrix and the same values in other places.
  *   out_dtype    dtype, or RD_E4M3: every row has a scale, out_scale = (largest |out| of the row) / 448, and holds out / out_scale,
  *                rounded to nearest even; a row of zeros has the scale 0.  Where a value of out is NaN (a NaN of x, residual or weight; an
  *                infinite s, whose row has the rstd 0; a row of zeros with eps = 0) the row's scale is NaN, and so are all of its values.
@@ -635,7 +639,8 @@ typedef struct {
  * rd_norm_grad -- its gradients, with xhat = s * rstd and g = grad_out * weight:
  *   grad_residual = rstd * (g - xhat * mean of g * xhat) + grad_sum,   grad_x = dropout(grad_residual, before it is rounded),
  *   grad_weight = sum over rows of grad_out * xhat;
- * in fp32, each rounded once.
+ * in fp32, each rounded once.  The order in which a row is summed depends on its length, on whether rows move in words or by element (as for
+ * rd_norm) and on whether n is at most 384 and n * dim at most 2^20; that of grad_weight on n, the types and whether grad_sum is given, too.
  *   d_grad_x         DEVICE; n x dim, dtype; or NULL.      d_grad_residual  DEVICE; n x dim, sum_dtype; or NULL.
  *   d_grad_weight    DEVICE; dim values, weight_dtype; or NULL.  Not all three NULL.  Workspace: for grad_weight alone, else NULL, 0.
  * grad_x and grad_residual may each be grad_out, sum or grad_sum (where the types agree).
@@ -651,7 +656,8 @@ RD_API int rd_norm_grad(const rd_norm_grad_t *v, void *d_grad_x, size_t grad_x_s
 RD_API int rd_dropout(const void *d_x, size_t x_stride, size_t n, size_t dim, rd_dtype_t dtype, float drop, uint64_t seed, uint64_t offset,
                       size_t first_row, void *d_out, size_t out_stride, void *cuda_stream);
 
-/* Activations of the gated projections. */
+/* Activations of the gated projections.  At g = inf the value is inf and the slope 1; at -inf the slope is 0 and the value NaN, a product
+ * with 0 (RD_RELU: 0). */
 typedef enum {
     RD_SILU = 0, /* g / (1 + exp(-g))                                                                */
     RD_GELU = 1, /* g (1 + tanh(sqrt(2 / pi) (g + 0.044715 g^3))) / 2                                */
@@ -677,10 +683,10 @@ typedef struct {
  *   gate = x . gate_weight^T,  up = x . up_weight^T  (RD_E4M3: times x_scale, then times gate_scale or up_scale, in fp32),
  *   out = act(gate) * up;
  * products exact, sums fp32 as the tensor cores add them up, out computed from fp32 gate and up and rounded once.  (exp and 1/x of the
- * activation are within about 2^-22.)
+ * activation are within about 2^-22, the exponent within some 2^-24 of itself; a factor 1 / (1 + exp) below 2^-126 is 0.)
  *   out_dtype      dtype; with RD_E4M3 RD_BF16 or RD_FP16: out, gate and up.
  *   d_gate, d_up   DEVICE; n x width: gate and up, rounded once, as rd_gated_grad reads them; each may be NULL.
- * x or a weight whose base or stride is not a multiple of 16 bytes (or is 0: one row for all) is copied into the workspace by every call.
+ * x or a weight whose base or stride is not a multiple of 16 bytes, and an x of one row for all, is copied into the workspace by every call.
  * Results that begin on 16-byte boundaries in every row are stored 16 bytes at a time.
  */
 RD_API int rd_gated_workspace(const rd_gated_t *v, size_t *bytes);
@@ -691,7 +697,9 @@ RD_API int rd_gated(const rd_gated_t *v, void *d_out, size_t out_stride, rd_dtyp
  * rd_gated_grad -- its gradients, from gate and up as rd_gated left them (RD_BF16, RD_FP16):
  *   dgate = grad_out * up * act'(gate),  dup = grad_out * act(gate), each rounded to dtype once;
  *   grad_x = dgate . gate_weight + dup . up_weight,  grad_gate_weight = dgate^T . x,  grad_up_weight = dup^T . x;
- * sums fp32, results (dtype) rounded once.
+ * sums fp32, results (dtype) rounded once.  dgate and dup are operands of the tensor cores' products and have their type's range: with
+ * RD_FP16 a value above 65504 becomes an infinity, in its row of grad_x and its row of a weight's gradient, also where those would fit,
+ * and one below 2^-14 is rounded to a multiple of 2^-24 (as by a step that keeps them in fp16: scale the loss).  RD_BF16 has fp32's range.
  *   d_grad_x                                   DEVICE; n x dim; or NULL.  For a slice: the slice's part; add the parts (rd_allreduce).
  *   d_grad_gate_weight, d_grad_up_weight       DEVICE; width x dim; each may be NULL.  Not all three NULL.
  */

@@ -607,9 +607,9 @@ def rd_norm_grad(grad_out, total, weight, rstd, grad_total=None, want_residual=T
 
 
 def rd_dropout(x, drop, seed, offset=0, first_row=0, out=None, stream=None):
-    """x with a share `drop` of its values set to 0 and the others multiplied by 1 / (1 - drop) (drop as a multiple of 2^-16); which ones
-    depends on (seed, offset, first_row + row, column) alone, so the gradient is the same call on the gradient.  x: [n, dim] float32,
-    bfloat16 or float16; out: like x (allocated when None), may be x.  Returns out."""
+    """x with a share `drop` of its values set to 0 (whatever they were) and the others multiplied by 1 / (1 - drop) (drop as a multiple of
+    2^-16); which ones depends on (seed, offset, first_row + row, column) alone, so the gradient is the same call on the gradient.
+    x: [n, dim] float32, bfloat16 or float16; out: like x (allocated when None), may be x.  Returns out."""
     if stream is not None:
         return _on_stream(rd_dropout, x, stream, x, drop, seed, offset, first_row, out)
     r = _native().dropout(x, drop, seed, offset, first_row, out)
@@ -657,8 +657,9 @@ def rd_gated_grad_workspace(x, gate_weight, up_weight, want_x=True) -> int:
 def rd_gated_grad(grad_out, x, gate_weight, up_weight, gate, up, activation=RD_SILU, want_x=True, want_weights=True, grad_x=None, grad_gate_weight=None,
                   grad_up_weight=None, workspace=None, stream=None):
     """Gradients of rd_gated: (grad_x, grad_gate_weight, grad_up_weight), of the operands' dtype (bfloat16 or float16).  gate, up: what
-    rd_gated kept.  want_x, want_weights: False leaves those out (None), unless a tensor for them is given; outputs are allocated when
-    None.  workspace: rd_gated_grad_workspace bytes (allocated when None)."""
+    rd_gated kept; what they and grad_out make is rounded to that dtype before the products, so float16 has its range there.  want_x,
+    want_weights: False leaves those out (None), unless a tensor for them is given; outputs are allocated when None.  workspace:
+    rd_gated_grad_workspace bytes (allocated when None)."""
     if stream is not None:
         return _on_stream(rd_gated_grad, x, stream, grad_out, x, gate_weight, up_weight, gate, up, activation, want_x, want_weights, grad_x, grad_gate_weight,
                           grad_up_weight, workspace)
