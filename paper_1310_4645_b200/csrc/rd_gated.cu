@@ -15,9 +15,9 @@
 //
 // Operands come in by TMA into a ring of stages of 128 bytes of the summed index; one warp per operand issues the copies, one the
 // products, eight take the results; two sets of accumulators, so that one is read while the next is computed.
-// What bounds it (B200): many rows, the tensor cores (2048 x 4096 x 12288 bf16: busy 93 % of the active cycles, gradients 97 %) at the clock that
+// What bounds it (B200): many rows, the tensor cores (2048 x 4096 x 12288 bf16: busy 94 % of the active cycles, gradients 97 %) at the clock that
 // the board's power limit leaves: 8192 x 4096 x 12288 1.2 to 1.29 ms with gate and up kept = 1.28 to 1.37 PFLOP/s, gradients 2.7 to 3.05; 4096 rows
-// in 8 bits 0.31 to 0.33 = 2.5 to 2.6.  Up to some 128 rows, the memory: 36 to 41 us for the weights' 201 MB.  Rows of at most some 256 values, taking
+// in 8 bits 0.31 to 0.39 = 2.1 to 2.6.  Up to some 128 rows, the memory: 36 to 41 us for the weights' 201 MB.  Rows of at most some 256 values, taking
 // the results out: 4096 x 64 x 12288 52 us.
 #include "rd_block.h"
 

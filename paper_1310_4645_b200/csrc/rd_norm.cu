@@ -9,9 +9,9 @@
 //
 // A row is held by 8, 16 or 32 lanes (up to 256 values), a warp (up to 1024), a thread block (up to 8192) or a cluster of up to eight of them, whose partial sums meet in
 // each other's shared memory.  Everything is read and written once, the weight and, in the gradient, a row in shared memory excepted.
-// What bounds it (B200): the memory, at 0.84 to 0.92 of the rate of a copy: 16384 x 4096 bf16 with dropout and residual 89 to 97 us for 537 MB,
-// gradient 114 to 125 for 671, dropout alone 45 to 50 for 268; 2000 x 5120 into 8 bits 18 for 113.  A row alone: 2.4 us, the latency of a
-// launch, a load, a reduction and a store.
+// What bounds it (B200): the memory, at 0.80 to 0.92 of the rate of a copy: 16384 x 4096 bf16 with dropout and residual 89 to 102 us for 537 MB,
+// gradient 114 to 125 for 671, dropout alone 45 to 50 for 268; without dropout in fp32 170 for 1074, gradient 172; 2000 x 5120 into 8 bits 18.0 to
+// 20.5 for 113.  A row alone: 2.4 us, the latency of a launch, a load, a reduction and a store.
 #include "rd_norm_rows.h"
 
 namespace rd {
