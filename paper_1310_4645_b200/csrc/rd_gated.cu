@@ -173,7 +173,7 @@ struct alignas(64) GradParams {
     uint32_t weights;         // which of dWg (1) and dWu (2) are wanted
     bool want_dx, bf16;
     bool dx_tma, gate_tma, up_tma;            // results that TMA can address
-    uint16_t *dx, *dgate, *dup;               // the others
+    uint16_t *dx, *dgate, *dup;               // the others, and ends of rows
     size_t dx_stride, dgate_stride, dup_stride;
 };
 
@@ -523,13 +523,14 @@ __global__ void __launch_bounds__(kMmaThreads, 1) rd_gated_mma_kernel(const __gr
                         for (int j = 0; j < 4; j++) o[j] = pack2(p.bf16, __uint_as_float(x[8 * q + 2 * j]), __uint_as_float(x[8 * q + 2 * j + 1]));
                         box_put(box, lane, 4 * (c & 1) + q, o[0], o[1], o[2], o[3]);
                     }
-                    if (tma) {
+                    if (tma && box_within(col - 32 * (c & 1), p.dim)) {
                         if (box_full(lane, c & 1) && col - 32 < p.dim && row0 < rows) {
                             tma_store(map, box, col - 32, row0);
                             box_sent();
                         }
                     } else if (c & 1) {
-                        // rows that TMA cannot address: the warp writes them one after the other, two elements a lane
+                        // rows that TMA cannot address, or whose end it would overwrite: the warp writes them one after the other, two
+                        // elements a lane
                         __syncwarp();
                         const size_t stride = w.product == 1 ? p.dx_stride : w.second ? p.dup_stride : p.dgate_stride;
                         uint16_t *dst = (w.product == 1 ? p.dx : w.second ? p.dup : p.dgate) + size_t(row0) * stride + (col - 32);

@@ -190,6 +190,9 @@ __device__ __forceinline__ bool box_full(int lane, bool full)
     __syncwarp();
     return lane == 0;
 }
+// Whether a box of 64 columns of 16 bits from `col` on may be stored by TMA in rows of `dim`: it writes whole words of 16 bytes, and zeros
+// beyond the row's end to fill the last, where something else may lie (rows of 14 values, 16 apart: the next 2 were lost).
+__device__ __forceinline__ bool box_within(uint32_t col, uint32_t dim) { return dim % 8 == 0 || col + 64 <= dim || col >= dim; }
 __device__ __forceinline__ void box_sent() { asm volatile("cp.async.bulk.commit_group;" ::: "memory"); }
 
 // A position in rows of `wide` places, advanced by a constant number of places without divisions.
