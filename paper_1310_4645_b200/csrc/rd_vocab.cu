@@ -790,13 +790,14 @@ __global__ void __launch_bounds__(kMmaThreads, 1) rd_vocab_mma_kernel(const __gr
                                 for (int j = 0; j < 4; j++) o[j] = pack2<BF16>(__uint_as_float(v[8 * q + 2 * j]) * unboost, __uint_as_float(v[8 * q + 2 * j + 1]) * unboost);
                                 box_put(box, lane, 4 * (c & 1) + q, o[0], o[1], o[2], o[3]);
                             }
-                            if (p.dw_tma) {
+                            if (p.dw_tma && box_within(col - 32 * (c & 1), p.dim)) {
                                 if (box_full(lane, c & 1) && col - 32 < p.dim && row0 < p.piece) {
                                     tma_store(&p.dw_out, box, col - 32, p.piece0 + row0);
                                     box_sent();
                                 }
                             } else if (c & 1) {
-                                // rows that TMA cannot address: the warp writes them one after the other, two elements a lane
+                                // rows that TMA cannot address, or whose end it would overwrite: the warp writes them one after the
+                                // other, two elements a lane
                                 __syncwarp();
                                 const uint32_t rows = row0 < p.piece ? min(32u, p.piece - row0) : 0;
                                 uint16_t *dst = p.dw + size_t(p.piece0 + row0) * p.dw_stride + (col - 32);

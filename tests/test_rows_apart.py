@@ -6,7 +6,7 @@ import torch
 import paper_1310_4645_b200 as rd
 from test_gated import ACTS, E4M3, HALF, outside_untouched
 from test_norm import BF16, FP32
-from test_vocab import gen, rand
+from test_vocab import gen, ints, rand
 
 gpu = pytest.mark.gpu
 WIDTHS = [1, 2, 3, 4, 5, 6, 7, 22, 63, 66, 70, 190, 253, 258, 318, 1001, 1446]
@@ -84,6 +84,30 @@ def test_gated_8bit_of_rows_apart(n, dim):
         out = [room(n, width, BF16, more) for _ in range(3)]
         rd.rd_gated(*(apart(t, to, more) for t in (x, wg, wu)), out=out[0], gate=out[1], up=out[2], **scales)
         kept_apart(out, want)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", HALF)
+@pytest.mark.parametrize("n, rows", [(1, 61), (3, 700), (40, 300), (200, 1000), (1500, 5000)])
+@pytest.mark.parametrize("dim", WIDTHS)
+def test_vocabulary_of_rows_apart(dtype, n, rows, dim):
+    hidden, weight, ids = rand(n, dim, seed=1, dtype=dtype), rand(rows, dim, seed=2, dtype=dtype), ints(-1, rows, n, seed=3)
+    up = torch.rand(n, generator=gen(4), device="cuda")
+    for more in (0, 8):
+        h, w = apart(hidden, more=more), apart(weight, more=more)
+        want = rd.rd_vocab_loss(hidden, weight, ids)
+        got = rd.rd_vocab_loss(h, w, ids)
+        assert all(torch.allclose(a, b, rtol=1e-4, atol=1e-4) for a, b in zip(got, want))          # not the same bits: few tokens go other ways
+        grads = rd.rd_vocab_loss_grad(hidden, weight, ids, want[1], up, torch.empty_like(hidden), torch.empty_like(weight))
+        into = room(n, dim, dtype, more), room(rows, dim, dtype, more)
+        rd.rd_vocab_loss_grad(h, w, ids, want[1], up, *into)
+        for a, b in zip(into, grads):
+            assert outside_untouched(a) and (a.double() - b.double()).norm() <= 0.01 * b.double().norm()
+        table, looked = room(rows, dim, dtype, more), room(n, dim, dtype, more)
+        rd.rd_embed(w, ids, looked)
+        rd.rd_embed_grad(h, ids, table)
+        kept_apart((looked, table), (rd.rd_embed(weight, ids), rd.rd_embed_grad(hidden, ids, torch.empty_like(weight))))
+    assert rd.rd_vocab_status() == rd.RD_OK
 
 
 @gpu
